@@ -66,7 +66,7 @@ enum {
   AWSRC_EDEVICE = -4   /* a HIP runtime call failed                               */
 };
 
-enum { AWSRC_DTYPE_F32 = 0, AWSRC_DTYPE_BF16 = 1 };
+enum { AWSRC_DTYPE_F32 = 0, AWSRC_DTYPE_BF16 = 1, AWSRC_DTYPE_F16 = 2 /* 8-bit serving calls only */ };
 enum { AWSRC_D_PER_COL = 0, AWSRC_D_PER_ELEM = 1 };
 enum { AWSRC_MODE_GLOBAL = 0, AWSRC_MODE_PER_MODULE = 1 };
 enum { AWSRC_SCALE_FP16 = 0, AWSRC_SCALE_POW2 = 1 };
@@ -463,6 +463,152 @@ awsrc_status awsrc_reconstruct_bf16_sdq(const awsrc_decode_plan* plan, int32_t n
                                         void* const* out_ptrs, int32_t group, const uint8_t* const* codes,
                                         const int8_t* const* sdq_code, const float* const* sdq_mean,
                                         const float* const* sdq_step, const uint8_t* const* zero, void* stream);
+
+/*
+ * 8-bit serving of repaired weights: linear layers on int8 codes, and a paged
+ * int8 cache of keys and values with the attention that reads it.
+ *
+ * The 8-bit recipe, fp32 with every operation rounded once, is the same for
+ * all of them: over a group of values (a row of a matrix; the keys, or the
+ * values, of one head in one page)
+ *   scale = amax / 127,  inverse = 1 / scale,  code = rint(x * inverse), ties to even,
+ * with scale = 0 and codes 0 where amax = max |x| is below 2^-100, and scale
+ * NaN and codes 0 where a value is infinite or NaN (whatever the scale then
+ * multiplies is NaN).  The value that a code stands for is code * scale.
+ * Codes lie in [-127, 127]; -128 is taken as input and never written.
+ *
+ * dtype arguments take AWSRC_DTYPE_F32, _BF16 and _F16 unless a call says
+ * otherwise.  Leading dimensions count elements.  All calls are asynchronous on
+ * `stream`, allocate nothing and can be captured.  Inputs that live on the
+ * device (lengths, page tables) are not checked on the host: the kernels
+ * follow no page outside the cache and write no row outside the buffers,
+ * whatever they hold.
+ */
+
+/*
+ * Rows as int8 codes with one scale each.
+ *  X      [rows, cols] x_dtype, row i at X + i * ldx, ldx >= cols.
+ *  codes  row i at codes + i * ldc, ldc >= cols.  Up to the next multiple of 16
+ *         the codes of a row are filled with 0 as far as ldc reaches.
+ *  scale  [rows] fp32.
+ * cols >= 1.  EINVAL: bad shape or dtype, NULL buffer, X not aligned to its type.
+ */
+awsrc_status awsrc_quantize_rows_i8(const void* X, int32_t x_dtype, int64_t rows, int64_t cols, int64_t ldx,
+                                    int8_t* codes, int64_t ldc, float* scale, void* stream);
+
+/*
+ * Product of int8 matrices with a scale per row of each operand (per token and
+ * per output channel):
+ *   out[m, n] = a_scale[m] * b_scale[n] * sum_k A[m, k] B[n, k] + bias[n],
+ * the sum exact in int32, then fp32 (sum * (a_scale * b_scale) + bias), rounded
+ * once to out_dtype (nearest even).
+ *  A, B     int8, row i at A + i * lda; 16-byte aligned, lda and ldb multiples
+ *           of 16 and >= K rounded up to 16.  Each row is readable up to K
+ *           rounded up to 16; what lies past K does not matter.
+ *  bias_or_null  [N] fp32.
+ *  out      [M, N], row m at out + m * ldo, ldo >= N, aligned to its type.
+ * 1 <= K <= 131071 (no sum can pass 2^31).  M or N of 0 is a no-op.
+ * Workspace: two-phase query as described above (the query needs no pointers);
+ * the size may be 0, and then no workspace is needed.
+ */
+awsrc_status awsrc_matmul_i8(const int8_t* A, int64_t lda, const float* a_scale, const int8_t* B, int64_t ldb,
+                             const float* b_scale, const float* bias_or_null, int64_t M, int64_t N, int64_t K, void* out,
+                             int32_t out_dtype, int64_t ldo, void* workspace, size_t* ws_bytes, void* stream);
+
+/*
+ * A linear layer on int8 weights: awsrc_quantize_rows_i8 of X (one scale per
+ * token) and awsrc_matmul_i8 of its codes with B, with the same results.  X is
+ * [M, K] x_dtype, row m at X + m * ldx; the codes live in the workspace.
+ * Workspace: two-phase query as described above, never 0.
+ */
+awsrc_status awsrc_linear_i8(const void* X, int32_t x_dtype, int64_t ldx, const int8_t* B, int64_t ldb,
+                             const float* b_scale, const float* bias_or_null, int64_t M, int64_t N, int64_t K, void* out,
+                             int32_t out_dtype, int64_t ldo, void* workspace, size_t* ws_bytes, void* stream);
+
+/*
+ * A paged cache of keys and values in int8 (device pointers, caller's memory).
+ *  k        [n_pages][kv_heads][page_tokens][head_dim] codes.
+ *  v        [n_pages][kv_heads][head_dim][page_tokens] codes.
+ *  k_scale, v_scale  [n_pages][kv_heads] fp32.
+ * head_dim 64, 128 or 256; page_tokens 16, 32, 64 or 128; k and v 16-byte
+ * aligned.  Nothing needs initialising: a page's scale starts with its first slot.
+ *
+ * A batch of n_seq sequences is described, in device memory, by
+ *  cu       [n_seq + 1] int32, non-decreasing from 0: sequence s owns the packed
+ *           rows cu[s] .. cu[s + 1] - 1 of the call's tensors, which are its
+ *           LAST tokens in order.
+ *  kv_len   [n_seq] int32: the tokens of the sequence in the cache, those of this
+ *           call included.  Row cu[s + 1] - 1 is the token at position kv_len[s] - 1.
+ *  page_table  [n_seq][table_ld] int32: token t lies in slot t % page_tokens of
+ *           page page_table[s][t / page_tokens].  Entries past the last token are
+ *           not read.
+ * max_new (host) is at least the largest cu[s + 1] - cu[s].
+ */
+typedef struct awsrc_kv_cache {
+  int8_t* k;
+  int8_t* v;
+  float* k_scale;
+  float* v_scale;
+  int64_t n_pages;
+  int32_t kv_heads, head_dim, page_tokens;
+  int32_t reserved; /* must be 0 */
+} awsrc_kv_cache;
+
+/*
+ * Appends the batch's rows to the cache, keys rotated by their positions, and
+ * rotates the queries of the same rows on the way.
+ * Per touched page and head, for keys and values each: the scale is the larger
+ * of the page's scale (0 where the page's first slot is among the new tokens)
+ * and the new tokens' amax / 127; where it grew, the codes already there become
+ * rint(code * (old scale * inverse)); new codes are rint(x * inverse).  A page that
+ * took one value that is not finite stays NaN until its first slot is written anew.
+ *  k, v     [n_rows][kv_heads][head_dim], row i at k + i * ldk, heads adjacent.
+ *  q_or_null, q_out  [n_rows][q_heads][head_dim], rows ldq and ldqo apart; q_out
+ *           receives the rotated rows in `dtype` and does not overlap q.  Both NULL to skip.
+ *  cos, sin [rope_len][rot / 2] fp32, row = position; rot even, 0 <= rot <= head_dim
+ *           channels are rotated (0: none, cos and sin may be NULL).  Channel pairs
+ *           are (i, i + rot / 2), or (2 i, 2 i + 1) with interleaved != 0:
+ *           x1 cos - x2 sin, x2 cos + x1 sin.  A token past the table gets NaN.
+ * Tokens whose page lies outside the cache or the table are dropped.  A page
+ * belongs to one sequence of the batch.
+ */
+awsrc_status awsrc_kv_append(const awsrc_kv_cache* cache, const void* k, int64_t ldk, const void* v, int64_t ldv,
+                             const void* q_or_null, int64_t ldq, int32_t q_heads, void* q_out, int64_t ldqo,
+                             int32_t dtype, const float* cos, const float* sin, int64_t rope_len, int32_t rot,
+                             int32_t interleaved, int32_t n_seq, int64_t n_rows, const int32_t* cu, const int32_t* kv_len,
+                             const int32_t* page_table, int64_t table_ld, int64_t max_new, void* stream);
+
+/*
+ * The values that the cache holds for the batch's rows (the last
+ * cu[s + 1] - cu[s] tokens of each sequence), as dense [n_rows][kv_heads][head_dim]
+ * rows of `dtype`: code * scale, rounded once.  A token whose page lies outside
+ * the cache or the table reads as NaN.  For moving a sequence elsewhere, or
+ * for code that takes dense keys.
+ */
+awsrc_status awsrc_kv_read(const awsrc_kv_cache* cache, int32_t n_seq, int64_t n_rows, const int32_t* cu,
+                           const int32_t* kv_len, const int32_t* page_table, int64_t table_ld, int64_t max_new,
+                           void* k_out, void* v_out, int32_t dtype, void* stream);
+
+/*
+ * Attention of the batch's query rows over the cache:
+ *   o = sum_t softmax_t(scale * q . k_t) v_t
+ * over the sequence's tokens, for the row at position p those with t <= p where
+ * causal != 0, all kv_len[s] of them otherwise.  q_heads is a multiple of
+ * kv_heads; query head h reads cached head h / (q_heads / kv_heads).  A row that
+ * sees no token is 0.  Tokens whose page lies outside the cache or the table are
+ * not seen.  Scores, maximum and sums in fp32; products in fp16 with fp32 sums.
+ *  q, out   [n_rows][q_heads][head_dim] bf16 or fp16 (dtype), rows ldq and ldo
+ *           apart, 16-byte aligned, ldq and ldo multiples of 8.
+ *  max_kv   (host) at least the largest kv_len[s]: how far the work may be split.
+ *           Longer sequences are cut there.
+ *  scale    finite.
+ * Workspace: two-phase query as described above (the query needs no pointers
+ * but `cache`); the size may be 0, and then no workspace is needed.
+ */
+awsrc_status awsrc_kv_attention(const awsrc_kv_cache* cache, const void* q, int64_t ldq, int32_t q_heads, int32_t dtype,
+                                int32_t n_seq, int64_t n_rows, const int32_t* cu, const int32_t* kv_len,
+                                const int32_t* page_table, int64_t table_ld, int64_t max_new, int64_t max_kv, float scale,
+                                int32_t causal, void* out, int64_t ldo, void* workspace, size_t* ws_bytes, void* stream);
 
 /* Host-only helpers (no device needed). */
 /* L_rec in bytes for T_total tiles; -1 if p is invalid. */

@@ -19,7 +19,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libawsrc.so")
 
 AWSRC_OK, AWSRC_EINVAL, AWSRC_ENOSPC, AWSRC_ECORRUPT, AWSRC_EDEVICE = 0, -1, -2, -3, -4
-AWSRC_DTYPE_F32, AWSRC_DTYPE_BF16 = 0, 1
+AWSRC_DTYPE_F32, AWSRC_DTYPE_BF16, AWSRC_DTYPE_F16 = 0, 1, 2
 AWSRC_D_PER_COL, AWSRC_D_PER_ELEM = 0, 1
 AWSRC_MODE_GLOBAL, AWSRC_MODE_PER_MODULE = 0, 1
 AWSRC_SCALE_FP16, AWSRC_SCALE_POW2 = 0, 1
@@ -28,7 +28,9 @@ EXPORTED = ("awsrc_abi_version", "awsrc_last_error", "awsrc_backbone_rtn", "awsr
             "awsrc_backbone_sdq_dequant", "awsrc_encode_tiles",
             "awsrc_encode_modules", "awsrc_encode_screen_lists", "awsrc_encode_tiles_noalloc", "awsrc_encode_noalloc_max_bytes",
             "awsrc_encode_scored", "awsrc_rank_prefix", "awsrc_decode_add", "awsrc_decode_prepare", "awsrc_decode_apply",
-            "awsrc_reconstruct_bf16", "awsrc_reconstruct_bf16_prefixes", "awsrc_reconstruct_bf16_sdq", "awsrc_record_bytes", "awsrc_header_bytes", "awsrc_budget_bytes", "awsrc_prefix_K")
+            "awsrc_reconstruct_bf16", "awsrc_reconstruct_bf16_prefixes", "awsrc_reconstruct_bf16_sdq",
+            "awsrc_quantize_rows_i8", "awsrc_matmul_i8", "awsrc_linear_i8", "awsrc_kv_append", "awsrc_kv_read",
+            "awsrc_kv_attention", "awsrc_record_bytes", "awsrc_header_bytes", "awsrc_budget_bytes", "awsrc_prefix_K")
 
 
 class AwsrcError(RuntimeError):
@@ -49,6 +51,12 @@ class awsrc_decode_plan(ctypes.Structure):
                 ("n_modules", ctypes.c_int32), ("w0_dtype", ctypes.c_int32), ("scale_fmt", ctypes.c_int32),
                 ("K", ctypes.c_int64), ("T_total", ctypes.c_uint64), ("h", ctypes.c_uint64),
                 ("records", ctypes.c_void_p), ("workspace", ctypes.c_void_p)]
+
+
+class awsrc_kv_cache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("n_pages", ctypes.c_int64), ("kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("page_tokens", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
 def make_params(C: int, P: int, b: int, S: int, basis_key: int = 0, ridge_lambda: float = 1e-6,
@@ -92,6 +100,16 @@ def _load() -> ctypes.CDLL:
         "awsrc_reconstruct_bf16_sdq": (i32, [ctypes.POINTER(awsrc_decode_plan), i32, P64, ctypes.POINTER(vp), i32,
                                              ctypes.POINTER(vp), ctypes.POINTER(vp), ctypes.POINTER(vp),
                                              ctypes.POINTER(vp), ctypes.POINTER(vp), vp]),
+        "awsrc_quantize_rows_i8": (i32, [vp, i32, i64, i64, i64, vp, i64, vp, vp]),
+        "awsrc_matmul_i8": (i32, [vp, i64, vp, vp, i64, vp, vp, i64, i64, i64, vp, i32, i64, vp, ctypes.POINTER(sz),
+                                  vp]),
+        "awsrc_linear_i8": (i32, [vp, i32, i64, vp, i64, vp, vp, i64, i64, i64, vp, i32, i64, vp, ctypes.POINTER(sz),
+                                  vp]),
+        "awsrc_kv_append": (i32, [ctypes.POINTER(awsrc_kv_cache), vp, i64, vp, i64, vp, i64, i32, vp, i64, i32, vp, vp,
+                                  i64, i32, i32, i32, i64, vp, vp, vp, i64, i64, vp]),
+        "awsrc_kv_read": (i32, [ctypes.POINTER(awsrc_kv_cache), i32, i64, vp, vp, vp, i64, i64, vp, vp, i32, vp]),
+        "awsrc_kv_attention": (i32, [ctypes.POINTER(awsrc_kv_cache), vp, i64, i32, i32, i32, i64, vp, vp, vp, i64, i64,
+                                     i64, ctypes.c_float, i32, vp, i64, vp, ctypes.POINTER(sz), vp]),
         "awsrc_record_bytes": (i64, [pp, i64]),
         "awsrc_header_bytes": (i64, [i32]),
         "awsrc_budget_bytes": (i64, [ctypes.c_double, i64]),
@@ -503,3 +521,286 @@ def awsrc_reconstruct_bf16_sdq(plan: awsrc_decode_plan,
         optr = (ctypes.c_void_p * (n * n_out))(*[t.data_ptr() for o in outs for t in o])
     _check(LIB.awsrc_reconstruct_bf16_sdq(ctypes.byref(plan), n_out, kp, optr, group, arr[0], arr[2], arr[3], arr[4],
                                           arr[1], _stream(stream)))
+
+
+# ------------------------------------------------------------------ 8-bit serving
+KVCache = Tuple[torch.Tensor, torch.Tensor, torch.Tensor, torch.Tensor]  # codes of keys and values, their scales
+
+_ACT_CODE = {torch.float32: AWSRC_DTYPE_F32, torch.bfloat16: AWSRC_DTYPE_BF16, torch.float16: AWSRC_DTYPE_F16}
+
+
+def _act_code(dtype: torch.dtype) -> int:
+    try:
+        return _ACT_CODE[dtype]
+    except KeyError:
+        raise TypeError(f"unsupported dtype {dtype}") from None
+
+
+def _on_device(dev: torch.device, *ts: Optional[torch.Tensor]) -> None:
+    for t in ts:
+        if t is not None and (not t.is_cuda or t.device != dev):
+            raise ValueError(f"tensors must be on one device: {t.device} and {dev}")
+
+
+def _empty(shape, dtype, dev, stream):
+    """A new tensor whose memory belongs to the stream that will use it."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=dev)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=dev)
+
+
+def _raw_stream(dev: torch.device, stream) -> int:
+    if stream is None:
+        return torch.cuda.current_stream(dev).cuda_stream
+    if stream.device != dev:
+        raise ValueError(f"stream on {stream.device}, tensors on {dev}")
+    return stream.cuda_stream
+
+
+def _rows_of(t: torch.Tensor, what: str):
+    """(rows, cols, row stride) of a matrix whose rows are contiguous."""
+    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+        raise ValueError(f"{what} must be a matrix with contiguous rows")
+    rows, cols = t.shape
+    return rows, cols, t.stride(0) if rows > 1 else max(cols, t.stride(0))
+
+
+def _i8_rows(t: torch.Tensor, what: str):
+    """_rows_of for an int8 operand: its rows are read in pieces of 16 bytes."""
+    rows, cols, ld = _rows_of(t, what)
+    if t.dtype != torch.int8:
+        raise TypeError(f"{what} must be int8, not {t.dtype}")
+    if rows == 1:
+        ld = max(ld, -(-cols // 16) * 16) if ld % 16 == 0 else -(-cols // 16) * 16
+    if rows and cols % 16 and t.untyped_storage().nbytes() < t.storage_offset() + (rows - 1) * ld + -(-cols // 16) * 16:
+        raise ValueError(f"{what}: the last row must be readable up to a multiple of 16 bytes")
+    return rows, cols, ld
+
+
+def _heads_of(t: torch.Tensor, what: str, heads: Optional[int], dim: int, dtype: torch.dtype):
+    """Row stride of a [rows, heads, dim] tensor whose heads lie side by side."""
+    if t.dim() != 3 or t.shape[2] != dim or (heads is not None and t.shape[1] != heads):
+        raise ValueError(f"{what}: expected [rows, {heads if heads else 'heads'}, {dim}], got {tuple(t.shape)}")
+    if t.dtype != dtype:
+        raise TypeError(f"{what}: expected {dtype}, got {t.dtype}")
+    if t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != dim):
+        raise ValueError(f"{what}: the heads of a row must lie side by side")
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * dim
+
+
+def make_kv_cache(n_pages: int, kv_heads: int, head_dim: int, page_tokens: int = 64, device="cuda") -> KVCache:
+    """An empty paged cache: codes k [n_pages, kv_heads, page_tokens, head_dim], v [n_pages, kv_heads, head_dim,
+    page_tokens], scales [n_pages, kv_heads] (not initialised: a page's scale starts with its first token)."""
+    k = torch.empty(n_pages, kv_heads, page_tokens, head_dim, dtype=torch.int8, device=device)
+    v = torch.empty(n_pages, kv_heads, head_dim, page_tokens, dtype=torch.int8, device=device)
+    return (k, v, torch.empty(n_pages, kv_heads, dtype=torch.float32, device=device),
+            torch.empty(n_pages, kv_heads, dtype=torch.float32, device=device))
+
+
+def _cache_of(cache: KVCache) -> awsrc_kv_cache:
+    k, v, ks, vs = cache
+    n, h, p, d = k.shape
+    if v.shape != (n, h, d, p) or ks.shape != (n, h) or vs.shape != (n, h):
+        raise ValueError("cache: k [pages, heads, tokens, dim], v [pages, heads, dim, tokens], scales [pages, heads]")
+    if k.dtype != torch.int8 or v.dtype != torch.int8 or ks.dtype != torch.float32 or vs.dtype != torch.float32:
+        raise TypeError("cache: int8 codes and fp32 scales")
+    _dev(k, v, ks, vs)
+    _on_device(k.device, v, ks, vs)
+    return awsrc_kv_cache(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), n, h, d, p, 0)
+
+
+def _batch_of(dev, cu, kv_len, page_table):
+    """(sequences, table stride) of a batch's int32 device tensors."""
+    for t in (cu, kv_len, page_table):
+        if t.dtype != torch.int32:
+            raise TypeError("cu, kv_len and page_table must be int32")
+    _on_device(dev, cu, kv_len, page_table)
+    n = kv_len.shape[0]
+    if cu.shape != (n + 1,) or page_table.dim() != 2 or page_table.shape[0] != n:
+        raise ValueError("cu [sequences + 1], kv_len [sequences], page_table [sequences, pages]")
+    if not (cu.is_contiguous() and kv_len.is_contiguous() and page_table.is_contiguous()):
+        raise ValueError("cu, kv_len and page_table must be contiguous")
+    return n, page_table.shape[1]
+
+
+def awsrc_quantize_rows_i8(x: torch.Tensor, out=None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """int8 codes [rows, cols] and fp32 scales [rows] of a matrix (activations per token, weights per output channel).
+    The codes' rows lie a multiple of 16 bytes apart, as awsrc_matmul_i8 and awsrc_linear_i8 take them."""
+    rows, cols, ld = _rows_of(x, "x")
+    dev = x.device
+    _on_device(dev, x)
+    if out is None:
+        out = (_empty((rows, -(-cols // 16) * 16), torch.int8, dev, stream)[:, :cols],
+               _empty((rows,), torch.float32, dev, stream))
+    codes, scale = out
+    _on_device(dev, codes, scale)
+    if codes.shape != x.shape or codes.dtype != torch.int8 or scale.shape != (rows,) or scale.dtype != torch.float32 or not scale.is_contiguous():
+        raise ValueError("out: int8 codes of x's shape and fp32 scales [rows]")
+    _check(LIB.awsrc_quantize_rows_i8(x.data_ptr(), _act_code(x.dtype), rows, cols, ld, codes.data_ptr(),
+                                      _rows_of(codes, "codes")[2], scale.data_ptr(), _raw_stream(dev, stream)))
+    return codes, scale
+
+
+def _check_product_args(dev, N, scale, bias, out, M):
+    _on_device(dev, scale, bias, out)
+    if scale.shape != (N,) or scale.dtype != torch.float32 or not scale.is_contiguous():
+        raise ValueError("weight scales: fp32 [N]")
+    if bias is not None and (bias.shape != (N,) or bias.dtype != torch.float32 or not bias.is_contiguous()):
+        raise ValueError("bias: fp32 [N]")
+    if out.shape != (M, N):
+        raise ValueError(f"out: expected {(M, N)}, got {tuple(out.shape)}")
+
+
+def awsrc_matmul_i8(a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor, b_scale: torch.Tensor,
+                    bias: Optional[torch.Tensor] = None, out_dtype: torch.dtype = torch.bfloat16,
+                    out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                    stream=None) -> torch.Tensor:
+    """a [M, K] times b [N, K] transposed, int8 codes with fp32 scales per row: [M, N] in out_dtype (or out's)."""
+    M, K, lda = _i8_rows(a, "a")
+    N, Kb, ldb = _i8_rows(b, "b")
+    if K != Kb:
+        raise ValueError(f"a has {K} columns, b {Kb}")
+    dev = a.device
+    _on_device(dev, a, a_scale, b)
+    if a_scale.shape != (M,) or a_scale.dtype != torch.float32 or not a_scale.is_contiguous():
+        raise ValueError("a_scale: fp32 [M]")
+    if out is None:
+        out = _empty((M, N), out_dtype, dev, stream)
+    _check_product_args(dev, N, b_scale, bias, out, M)
+    n = ctypes.c_size_t(0)
+    _check(LIB.awsrc_matmul_i8(None, lda, None, None, ldb, None, None, M, N, K, None, _act_code(out.dtype), N, None,
+                               ctypes.byref(n), None))
+    if n.value and (workspace is None or workspace.numel() < n.value):
+        workspace = _empty((n.value,), torch.uint8, dev, stream)
+    n = ctypes.c_size_t(0 if workspace is None else workspace.numel())
+    if M and N:
+        _check(LIB.awsrc_matmul_i8(a.data_ptr(), lda, a_scale.data_ptr(), b.data_ptr(), ldb, b_scale.data_ptr(),
+                                   None if bias is None else bias.data_ptr(), M, N, K, out.data_ptr(), _act_code(out.dtype),
+                                   _rows_of(out, "out")[2], None if workspace is None else workspace.data_ptr(),
+                                   ctypes.byref(n), _raw_stream(dev, stream)))
+    return out
+
+
+def linear_i8_workspace_bytes(M: int, N: int, K: int) -> int:
+    n = ctypes.c_size_t(0)
+    ld = -(-K // 16) * 16
+    _check(LIB.awsrc_linear_i8(None, AWSRC_DTYPE_F32, K, None, ld, None, None, M, N, K, None, AWSRC_DTYPE_F32, N, None,
+                               ctypes.byref(n), None))
+    return n.value
+
+
+def awsrc_linear_i8(x: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                    out_dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None,
+                    workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """A linear layer on int8 weights: x [M, K] quantized per row, times w [N, K] (codes and scales as
+    awsrc_quantize_rows_i8 makes them from the weight matrix) transposed, plus bias; [M, N] in x's type by default."""
+    M, K, ldx = _rows_of(x, "x")
+    N, Kw, ldw = _i8_rows(w, "w")
+    if K != Kw:
+        raise ValueError(f"x has {K} columns, w {Kw}")
+    dev = x.device
+    _on_device(dev, x, w)
+    if out is None:
+        out = _empty((M, N), x.dtype if out_dtype is None else out_dtype, dev, stream)
+    _check_product_args(dev, N, w_scale, bias, out, M)
+    need = linear_i8_workspace_bytes(M, N, K)
+    if workspace is None or workspace.numel() < need:
+        workspace = _empty((need,), torch.uint8, dev, stream)
+    n = ctypes.c_size_t(workspace.numel())
+    if M and N:
+        _check(LIB.awsrc_linear_i8(x.data_ptr(), _act_code(x.dtype), ldx, w.data_ptr(), ldw, w_scale.data_ptr(),
+                                   None if bias is None else bias.data_ptr(), M, N, K, out.data_ptr(), _act_code(out.dtype),
+                                   _rows_of(out, "out")[2], workspace.data_ptr(), ctypes.byref(n), _raw_stream(dev, stream)))
+    return out
+
+
+def awsrc_kv_append(cache: KVCache, k: torch.Tensor, v: torch.Tensor, cu: torch.Tensor, kv_len: torch.Tensor,
+                    page_table: torch.Tensor, max_new: int, cos: Optional[torch.Tensor] = None,
+                    sin: Optional[torch.Tensor] = None, q: Optional[torch.Tensor] = None, interleaved: bool = False,
+                    q_out: Optional[torch.Tensor] = None, stream=None) -> Optional[torch.Tensor]:
+    """Appends rows of k and v [rows, kv_heads, head_dim] (views of a fused projection's output will do) to the cache,
+    keys rotated by the tables cos, sin [positions, rot / 2]; returns q [rows, q_heads, head_dim] rotated the same way.
+    kv_len counts the appended tokens; max_new is at least the most rows that one sequence brings."""
+    c = _cache_of(cache)
+    dev = cache[0].device
+    n_seq, table_ld = _batch_of(dev, cu, kv_len, page_table)
+    _on_device(dev, k, v, q, cos, sin, q_out)
+    rows = k.shape[0]
+    ldk = _heads_of(k, "k", c.kv_heads, c.head_dim, k.dtype)
+    ldv = _heads_of(v, "v", c.kv_heads, c.head_dim, k.dtype)
+    if v.shape[0] != rows or (q is not None and q.shape[0] != rows):
+        raise ValueError("k, v and q must have the same rows")
+    if (cos is None) != (sin is None):
+        raise ValueError("cos and sin go together")
+    rot = rope_len = 0
+    if cos is not None:
+        if cos.shape != sin.shape or cos.dim() != 2 or cos.dtype != torch.float32 or sin.dtype != torch.float32:
+            raise ValueError("cos, sin: fp32 [positions, rot / 2]")
+        _dev(cos, sin)
+        rope_len, rot = cos.shape[0], 2 * cos.shape[1]
+    ldq = ldqo = heads = 0
+    if q is not None:
+        heads = q.shape[1]
+        ldq = _heads_of(q, "q", None, c.head_dim, k.dtype)
+        if q_out is None:
+            q_out = _empty((rows, heads, c.head_dim), q.dtype, dev, stream)
+        elif q_out.shape != q.shape:
+            raise ValueError("q_out: q's shape")
+        ldqo = _heads_of(q_out, "q_out", heads, c.head_dim, k.dtype)
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    _check(LIB.awsrc_kv_append(ctypes.byref(c), k.data_ptr(), ldk, v.data_ptr(), ldv, None if q is None else q.data_ptr(), ldq,
+                               heads, None if q is None else q_out.data_ptr(), ldqo, _act_code(k.dtype),
+                               None if cos is None else cos.data_ptr(), None if cos is None else sin.data_ptr(), rope_len, rot,
+                               int(interleaved), n_seq, rows, cu.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(),
+                               table_ld, min(int(max_new), rows), _raw_stream(dev, stream)))
+    return q_out
+
+
+def awsrc_kv_read(cache: KVCache, cu: torch.Tensor, kv_len: torch.Tensor, page_table: torch.Tensor, rows: int, max_new: int,
+                  dtype: torch.dtype = torch.bfloat16, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """What the cache holds for the last cu[s + 1] - cu[s] tokens of each sequence: dense keys and values
+    [rows, kv_heads, head_dim], rows = cu[-1]."""
+    c = _cache_of(cache)
+    dev = cache[0].device
+    n_seq, table_ld = _batch_of(dev, cu, kv_len, page_table)
+    k = _empty((rows, c.kv_heads, c.head_dim), dtype, dev, stream)
+    v = _empty((rows, c.kv_heads, c.head_dim), dtype, dev, stream)
+    _check(LIB.awsrc_kv_read(ctypes.byref(c), n_seq, rows, cu.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(), table_ld,
+                             min(int(max_new), rows), k.data_ptr(), v.data_ptr(), _act_code(dtype), _raw_stream(dev, stream)))
+    return k, v
+
+
+def awsrc_kv_attention(cache: KVCache, q: torch.Tensor, cu: torch.Tensor, kv_len: torch.Tensor, page_table: torch.Tensor,
+                       max_new: int, max_kv: int, scale: Optional[float] = None, causal: bool = True,
+                       out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                       stream=None) -> torch.Tensor:
+    """Attention of q [rows, q_heads, head_dim] (rotated, bf16 or fp16) over the cache; scale defaults to
+    head_dim ** -0.5.  max_new and max_kv bound the rows and the cached tokens of a sequence."""
+    c = _cache_of(cache)
+    dev = cache[0].device
+    n_seq, table_ld = _batch_of(dev, cu, kv_len, page_table)
+    _on_device(dev, q, out)
+    rows, heads = q.shape[0], q.shape[1]
+    ldq = _heads_of(q, "q", None, c.head_dim, q.dtype)
+    if out is None:
+        out = _empty((rows, heads, c.head_dim), q.dtype, dev, stream)
+    elif out.shape != q.shape:
+        raise ValueError("out: q's shape")
+    ldo = _heads_of(out, "out", heads, c.head_dim, q.dtype)
+    if scale is None:
+        scale = c.head_dim ** -0.5
+    code, max_new = _act_code(q.dtype), min(int(max_new), rows)
+    n = ctypes.c_size_t(0)
+    _check(LIB.awsrc_kv_attention(ctypes.byref(c), None, ldq, heads, code, n_seq, rows, None, None, None, table_ld, max_new,
+                                  max_kv, scale, int(causal), None, ldo, None, ctypes.byref(n), None))
+    if n.value and (workspace is None or workspace.numel() < n.value):
+        workspace = _empty((n.value,), torch.uint8, dev, stream)
+    n = ctypes.c_size_t(0 if workspace is None else workspace.numel())
+    if rows:
+        _check(LIB.awsrc_kv_attention(ctypes.byref(c), q.data_ptr(), ldq, heads, code, n_seq, rows, cu.data_ptr(),
+                                      kv_len.data_ptr(), page_table.data_ptr(), table_ld, max_new, max_kv, scale, int(causal),
+                                      out.data_ptr(), ldo, None if workspace is None else workspace.data_ptr(),
+                                      ctypes.byref(n), _raw_stream(dev, stream)))
+    return out

@@ -1,6 +1,8 @@
 // extern "C" entry points of libawsrc: argument validation, workspace layout
 // and kernel orchestration.  Every step of the codec itself runs in the HIP
-// kernels of basis.hip, backbone.hip, encode*.hip, rank.hip and decode.hip.
+// kernels of basis.hip, backbone.hip, encode*.hip, rank.hip and decode.hip,
+// the 8-bit serving calls in those of quant_i8.hip, linear_i8.hip,
+// kv_cache.hip and kv_attention.hip.
 #include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
@@ -13,6 +15,7 @@
 
 #include "awsrc_internal.h"
 #include "host_slot.h"
+#include "serve_internal.h"
 
 using namespace awsrc;
 
@@ -1054,4 +1057,243 @@ extern "C" awsrc_status awsrc_decode_add(const uint8_t* stream_bytes, uint64_t s
                                          &plan, workspace, ws_bytes, stream);
   if (st != AWSRC_OK || !workspace) return st;
   return awsrc_decode_apply(&plan, stream);
+}
+
+// ---------------------------------------------------------------- 8-bit serving
+namespace {
+
+int64_t round16(int64_t n) { return (n + 15) / 16 * 16; }
+bool act_dtype(int32_t t) { return t == AWSRC_DTYPE_F32 || t == AWSRC_DTYPE_BF16 || t == AWSRC_DTYPE_F16; }
+int64_t act_size(int32_t t) { return t == AWSRC_DTYPE_F32 ? 4 : 2; }
+bool misaligned(const void* p, uintptr_t a) { return reinterpret_cast<uintptr_t>(p) & (a - 1); }
+
+constexpr int64_t kMaxDim = 1ll << 31;  // rows, columns and leading dimensions
+
+awsrc_status check_quantize(const void* X, int32_t x_dtype, int64_t rows, int64_t cols, int64_t ldx) {
+  if (!act_dtype(x_dtype)) return fail(AWSRC_EINVAL, "bad x_dtype %d", x_dtype);
+  if (rows < 0 || rows >= kMaxDim || cols < 1 || cols >= kMaxDim)
+    return fail(AWSRC_EINVAL, "bad shape %lld x %lld", (long long)rows, (long long)cols);
+  if (ldx < cols || ldx >= kMaxDim) return fail(AWSRC_EINVAL, "ldx=%lld: must be at least cols", (long long)ldx);
+  if (X && misaligned(X, act_size(x_dtype))) return fail(AWSRC_EINVAL, "X must be aligned to its type");
+  return AWSRC_OK;
+}
+
+awsrc_status check_product(const int8_t* B, int64_t ldb, const float* b_scale, int64_t M, int64_t N, int64_t K,
+                           const void* out, int32_t out_dtype, int64_t ldo) {
+  if (!act_dtype(out_dtype)) return fail(AWSRC_EINVAL, "bad out_dtype %d", out_dtype);
+  if (M < 0 || N < 0 || M >= kMaxDim || N >= kMaxDim) return fail(AWSRC_EINVAL, "bad shape %lld x %lld", (long long)M, (long long)N);
+  if (K < 1 || K > kMaxSumI8) return fail(AWSRC_EINVAL, "K=%lld out of range 1..%lld", (long long)K, (long long)kMaxSumI8);
+  if (ldb % 16 || ldb < round16(K) || ldb >= kMaxDim)
+    return fail(AWSRC_EINVAL, "ldb=%lld: must be a multiple of 16, at least K", (long long)ldb);
+  if (ldo < N || ldo >= kMaxDim) return fail(AWSRC_EINVAL, "ldo=%lld: must be at least N", (long long)ldo);
+  if (B && misaligned(B, 16)) return fail(AWSRC_EINVAL, "int8 operands must be 16-byte aligned");
+  if (b_scale && misaligned(b_scale, 4)) return fail(AWSRC_EINVAL, "scales must be 4-byte aligned");
+  if (out && misaligned(out, act_size(out_dtype))) return fail(AWSRC_EINVAL, "out must be aligned to its type");
+  return AWSRC_OK;
+}
+
+// The common tail of the two products; a.A and a.a_scale are filled in by the caller.
+awsrc_status run_product(const LinearArgs& a, char* ws, hipStream_t s) {
+  HIPCHK(launch_matmul_i8(a, ws, s));
+  return AWSRC_OK;
+}
+
+awsrc_status check_cache(const awsrc_kv_cache* c, bool pointers) {
+  if (!c) return fail(AWSRC_EINVAL, "cache is NULL");
+  if (c->reserved != 0) return fail(AWSRC_EINVAL, "reserved field must be 0");
+  if (c->n_pages < 1 || c->n_pages >= kMaxDim) return fail(AWSRC_EINVAL, "n_pages=%lld out of range", (long long)c->n_pages);
+  if (c->kv_heads < 1 || c->kv_heads > 65536) return fail(AWSRC_EINVAL, "kv_heads=%d out of range", c->kv_heads);
+  if (c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 256)
+    return fail(AWSRC_EINVAL, "head_dim=%d: must be 64, 128 or 256", c->head_dim);
+  if (c->page_tokens != 16 && c->page_tokens != 32 && c->page_tokens != 64 && c->page_tokens != 128)
+    return fail(AWSRC_EINVAL, "page_tokens=%d: must be 16, 32, 64 or 128", c->page_tokens);
+  if (!pointers) return AWSRC_OK;
+  if (!c->k || !c->v || !c->k_scale || !c->v_scale) return fail(AWSRC_EINVAL, "NULL cache buffer");
+  if (misaligned(c->k, 16) || misaligned(c->v, 16)) return fail(AWSRC_EINVAL, "cache codes must be 16-byte aligned");
+  if (misaligned(c->k_scale, 4) || misaligned(c->v_scale, 4)) return fail(AWSRC_EINVAL, "cache scales must be 4-byte aligned");
+  return AWSRC_OK;
+}
+
+awsrc_status check_batch(const awsrc_kv_cache* c, int32_t n_seq, int64_t n_rows, int64_t table_ld, int64_t max_new) {
+  if (n_seq < 0 || n_seq > (1 << 24)) return fail(AWSRC_EINVAL, "n_seq=%d out of range", n_seq);
+  if (n_rows < 0 || n_rows >= kMaxDim) return fail(AWSRC_EINVAL, "n_rows=%lld out of range", (long long)n_rows);
+  if (table_ld < 1 || table_ld > kMaxDim / c->page_tokens) return fail(AWSRC_EINVAL, "table_ld=%lld out of range", (long long)table_ld);
+  if (max_new < 0 || max_new > n_rows) return fail(AWSRC_EINVAL, "max_new=%lld out of range 0..n_rows", (long long)max_new);
+  return AWSRC_OK;
+}
+
+awsrc_status check_batch_pointers(const int32_t* cu, const int32_t* kv_len, const int32_t* table) {
+  if (!cu || !kv_len || !table) return fail(AWSRC_EINVAL, "cu, kv_len or page_table is NULL");
+  if (misaligned(cu, 4) || misaligned(kv_len, 4) || misaligned(table, 4))
+    return fail(AWSRC_EINVAL, "cu, kv_len and page_table must be 4-byte aligned");
+  return AWSRC_OK;
+}
+
+awsrc_status check_rows(const char* what, const void* p, int64_t ld, int64_t width, int32_t dtype) {
+  if (!p) return fail(AWSRC_EINVAL, "%s is NULL", what);
+  if (ld < width || ld >= kMaxDim) return fail(AWSRC_EINVAL, "%s: rows %lld apart hold %lld values", what, (long long)ld, (long long)width);
+  if (misaligned(p, act_size(dtype))) return fail(AWSRC_EINVAL, "%s must be aligned to its type", what);
+  return AWSRC_OK;
+}
+
+}  // namespace
+
+extern "C" awsrc_status awsrc_quantize_rows_i8(const void* X, int32_t x_dtype, int64_t rows, int64_t cols, int64_t ldx,
+                                               int8_t* codes, int64_t ldc, float* scale, void* stream) {
+  awsrc_status st = check_quantize(X, x_dtype, rows, cols, ldx);
+  if (st != AWSRC_OK) return st;
+  if (ldc < cols || ldc >= kMaxDim) return fail(AWSRC_EINVAL, "ldc=%lld: must be at least cols", (long long)ldc);
+  if (rows == 0) return AWSRC_OK;
+  if (!X || !codes || !scale) return fail(AWSRC_EINVAL, "NULL buffer");
+  if (misaligned(scale, 4)) return fail(AWSRC_EINVAL, "scale must be 4-byte aligned");
+  HIPCHK(launch_quantize_rows(X, x_dtype, rows, cols, ldx, codes, ldc, scale, (hipStream_t)stream));
+  return AWSRC_OK;
+}
+
+extern "C" awsrc_status awsrc_matmul_i8(const int8_t* A, int64_t lda, const float* a_scale, const int8_t* B, int64_t ldb,
+                                        const float* b_scale, const float* bias_or_null, int64_t M, int64_t N, int64_t K,
+                                        void* out, int32_t out_dtype, int64_t ldo, void* workspace, size_t* ws_bytes,
+                                        void* stream) {
+  awsrc_status st = check_product(B, ldb, b_scale, M, N, K, out, out_dtype, ldo);
+  if (st != AWSRC_OK) return st;
+  if (lda % 16 || lda < round16(K) || lda >= kMaxDim)
+    return fail(AWSRC_EINVAL, "lda=%lld: must be a multiple of 16, at least K", (long long)lda);
+  if (!ws_bytes) return fail(AWSRC_EINVAL, "ws_bytes is NULL");
+  const size_t need = M && N ? matmul_i8_ws_bytes(M, N, K) : 0;
+  if (!workspace && !A && !B && !out) {
+    *ws_bytes = need;
+    return AWSRC_OK;
+  }
+  if (M == 0 || N == 0) return AWSRC_OK;
+  if (!A || !B || !a_scale || !b_scale || !out) return fail(AWSRC_EINVAL, "NULL buffer");
+  if (misaligned(A, 16)) return fail(AWSRC_EINVAL, "int8 operands must be 16-byte aligned");
+  if (misaligned(a_scale, 4) || misaligned(bias_or_null, 4)) return fail(AWSRC_EINVAL, "scales and bias must be 4-byte aligned");
+  if (need && (!workspace || *ws_bytes < need)) return fail(AWSRC_ENOSPC, "workspace of %zu bytes needed", need);
+  if (need && misaligned(workspace, 16)) return fail(AWSRC_EINVAL, "workspace must be 16-byte aligned");
+  const LinearArgs a{A, lda, a_scale, B, ldb, b_scale, bias_or_null, M, N, K, out, out_dtype, ldo};
+  return run_product(a, static_cast<char*>(workspace), (hipStream_t)stream);
+}
+
+extern "C" awsrc_status awsrc_linear_i8(const void* X, int32_t x_dtype, int64_t ldx, const int8_t* B, int64_t ldb,
+                                        const float* b_scale, const float* bias_or_null, int64_t M, int64_t N, int64_t K,
+                                        void* out, int32_t out_dtype, int64_t ldo, void* workspace, size_t* ws_bytes,
+                                        void* stream) {
+  awsrc_status st = check_product(B, ldb, b_scale, M, N, K, out, out_dtype, ldo);
+  if (st != AWSRC_OK) return st;
+  st = check_quantize(X, x_dtype, M, K, ldx);
+  if (st != AWSRC_OK) return st;
+  if (!ws_bytes) return fail(AWSRC_EINVAL, "ws_bytes is NULL");
+  const size_t b_codes = align_up((size_t)M * (size_t)round16(K), 256), b_scales = align_up((size_t)M * 4, 256);
+  const size_t need = 256 + b_codes + b_scales + (M && N ? matmul_i8_ws_bytes(M, N, K) : 0);
+  if (!workspace) {
+    *ws_bytes = need;
+    return AWSRC_OK;
+  }
+  if (M == 0 || N == 0) return AWSRC_OK;
+  if (!X || !B || !b_scale || !out) return fail(AWSRC_EINVAL, "NULL buffer");
+  if (misaligned(bias_or_null, 4)) return fail(AWSRC_EINVAL, "bias must be 4-byte aligned");
+  if (*ws_bytes < need) return fail(AWSRC_ENOSPC, "workspace of %zu bytes needed", need);
+  if (misaligned(workspace, 16)) return fail(AWSRC_EINVAL, "workspace must be 16-byte aligned");
+  char* ws = static_cast<char*>(workspace);
+  int8_t* codes = reinterpret_cast<int8_t*>(ws);
+  float* scales = reinterpret_cast<float*>(ws + b_codes);
+  hipStream_t s = (hipStream_t)stream;
+  HIPCHK(launch_quantize_rows(X, x_dtype, M, K, ldx, codes, round16(K), scales, s));
+  const LinearArgs a{codes, round16(K), scales, B, ldb, b_scale, bias_or_null, M, N, K, out, out_dtype, ldo};
+  return run_product(a, ws + b_codes + b_scales, s);
+}
+
+extern "C" awsrc_status awsrc_kv_append(const awsrc_kv_cache* cache, const void* k, int64_t ldk, const void* v, int64_t ldv,
+                                        const void* q_or_null, int64_t ldq, int32_t q_heads, void* q_out, int64_t ldqo,
+                                        int32_t dtype, const float* cos, const float* sin, int64_t rope_len, int32_t rot,
+                                        int32_t interleaved, int32_t n_seq, int64_t n_rows, const int32_t* cu,
+                                        const int32_t* kv_len, const int32_t* page_table, int64_t table_ld, int64_t max_new,
+                                        void* stream) {
+  awsrc_status st = check_cache(cache, true);
+  if (st != AWSRC_OK) return st;
+  st = check_batch(cache, n_seq, n_rows, table_ld, max_new);
+  if (st != AWSRC_OK) return st;
+  if (!act_dtype(dtype)) return fail(AWSRC_EINVAL, "bad dtype %d", dtype);
+  if (rot < 0 || rot > cache->head_dim || rot % 2) return fail(AWSRC_EINVAL, "rot=%d: must be even, at most head_dim", rot);
+  if (rope_len < 0 || rope_len >= kMaxDim) return fail(AWSRC_EINVAL, "rope_len=%lld out of range", (long long)rope_len);
+  if (rot && (!cos || !sin)) return fail(AWSRC_EINVAL, "cos or sin is NULL");
+  if (rot && (misaligned(cos, 4) || misaligned(sin, 4))) return fail(AWSRC_EINVAL, "cos and sin must be 4-byte aligned");
+  if (!q_or_null != !q_out) return fail(AWSRC_EINVAL, "q and q_out go together");
+  if (q_or_null && (q_heads < 1 || q_heads > 65536)) return fail(AWSRC_EINVAL, "q_heads=%d out of range", q_heads);
+  if (n_seq == 0 || n_rows == 0 || max_new == 0) return AWSRC_OK;
+  if ((st = check_batch_pointers(cu, kv_len, page_table)) != AWSRC_OK) return st;
+  const int64_t w = (int64_t)cache->kv_heads * cache->head_dim, wq = (int64_t)q_heads * cache->head_dim;
+  if ((st = check_rows("k", k, ldk, w, dtype)) != AWSRC_OK || (st = check_rows("v", v, ldv, w, dtype)) != AWSRC_OK) return st;
+  if (q_or_null && ((st = check_rows("q", q_or_null, ldq, wq, dtype)) != AWSRC_OK ||
+                    (st = check_rows("q_out", q_out, ldqo, wq, dtype)) != AWSRC_OK))
+    return st;
+  AppendArgs a{};
+  a.c = *cache;
+  a.k = k; a.v = v; a.q = q_or_null; a.ldk = ldk; a.ldv = ldv; a.ldq = ldq; a.ldqo = ldqo;
+  a.dtype = dtype; a.q_heads = q_heads; a.q_out = q_out;
+  a.cos = cos; a.sin = sin; a.rope_len = rope_len; a.rot = rot; a.interleaved = interleaved != 0;
+  a.n_seq = n_seq; a.n_rows = n_rows; a.cu = cu; a.kv_len = kv_len; a.table = page_table; a.table_ld = table_ld;
+  a.max_new = max_new;
+  HIPCHK(launch_kv_append(a, (hipStream_t)stream));
+  return AWSRC_OK;
+}
+
+extern "C" awsrc_status awsrc_kv_read(const awsrc_kv_cache* cache, int32_t n_seq, int64_t n_rows, const int32_t* cu,
+                                      const int32_t* kv_len, const int32_t* page_table, int64_t table_ld, int64_t max_new,
+                                      void* k_out, void* v_out, int32_t dtype, void* stream) {
+  awsrc_status st = check_cache(cache, true);
+  if (st != AWSRC_OK) return st;
+  st = check_batch(cache, n_seq, n_rows, table_ld, max_new);
+  if (st != AWSRC_OK) return st;
+  if (!act_dtype(dtype)) return fail(AWSRC_EINVAL, "bad dtype %d", dtype);
+  if (n_seq == 0 || n_rows == 0 || max_new == 0) return AWSRC_OK;
+  if ((st = check_batch_pointers(cu, kv_len, page_table)) != AWSRC_OK) return st;
+  const int64_t w = (int64_t)cache->kv_heads * cache->head_dim;
+  if ((st = check_rows("k_out", k_out, w, w, dtype)) != AWSRC_OK || (st = check_rows("v_out", v_out, w, w, dtype)) != AWSRC_OK)
+    return st;
+  ReadArgs a{};
+  a.c = *cache;
+  a.n_seq = n_seq; a.n_rows = n_rows; a.cu = cu; a.kv_len = kv_len; a.table = page_table; a.table_ld = table_ld;
+  a.max_rows = max_new; a.k_out = k_out; a.v_out = v_out; a.dtype = dtype;
+  HIPCHK(launch_kv_read(a, (hipStream_t)stream));
+  return AWSRC_OK;
+}
+
+extern "C" awsrc_status awsrc_kv_attention(const awsrc_kv_cache* cache, const void* q, int64_t ldq, int32_t q_heads,
+                                           int32_t dtype, int32_t n_seq, int64_t n_rows, const int32_t* cu,
+                                           const int32_t* kv_len, const int32_t* page_table, int64_t table_ld,
+                                           int64_t max_new, int64_t max_kv, float scale, int32_t causal, void* out,
+                                           int64_t ldo, void* workspace, size_t* ws_bytes, void* stream) {
+  const bool query = !workspace && !q && !out;
+  awsrc_status st = check_cache(cache, !query);
+  if (st != AWSRC_OK) return st;
+  st = check_batch(cache, n_seq, n_rows, table_ld, max_new);
+  if (st != AWSRC_OK) return st;
+  if (dtype != AWSRC_DTYPE_BF16 && dtype != AWSRC_DTYPE_F16) return fail(AWSRC_EINVAL, "bad dtype %d: bf16 or fp16", dtype);
+  if (q_heads < 1 || q_heads > 65536 || q_heads % cache->kv_heads)
+    return fail(AWSRC_EINVAL, "q_heads=%d: must be a multiple of kv_heads=%d", q_heads, cache->kv_heads);
+  if (max_kv < 0 || max_kv >= kMaxDim) return fail(AWSRC_EINVAL, "max_kv=%lld out of range", (long long)max_kv);
+  if (!isfinite(scale)) return fail(AWSRC_EINVAL, "scale must be finite");
+  if (!ws_bytes) return fail(AWSRC_EINVAL, "ws_bytes is NULL");
+  AttentionArgs a{};
+  a.c = *cache;
+  a.q = q; a.ldq = ldq; a.dtype = dtype; a.q_heads = q_heads;
+  a.n_seq = n_seq; a.n_rows = n_rows; a.cu = cu; a.kv_len = kv_len; a.table = page_table; a.table_ld = table_ld;
+  a.max_new = max_new; a.max_kv = max_kv; a.scale = scale; a.causal = causal != 0;
+  a.out = out; a.ldo = ldo;
+  const size_t need = n_seq && n_rows && max_new ? kv_attention_ws_bytes(a) : 0;
+  if (query) {
+    *ws_bytes = need;
+    return AWSRC_OK;
+  }
+  if (n_seq == 0 || n_rows == 0 || max_new == 0) return AWSRC_OK;
+  if ((st = check_batch_pointers(cu, kv_len, page_table)) != AWSRC_OK) return st;
+  const int64_t w = (int64_t)q_heads * cache->head_dim;
+  if ((st = check_rows("q", q, ldq, w, dtype)) != AWSRC_OK || (st = check_rows("out", out, ldo, w, dtype)) != AWSRC_OK) return st;
+  if (misaligned(q, 16) || misaligned(out, 16) || ldq % 8 || ldo % 8)
+    return fail(AWSRC_EINVAL, "q and out must be 16-byte aligned with rows a multiple of 8 apart");
+  if (need && (!workspace || *ws_bytes < need)) return fail(AWSRC_ENOSPC, "workspace of %zu bytes needed", need);
+  if (need && misaligned(workspace, 16)) return fail(AWSRC_EINVAL, "workspace must be 16-byte aligned");
+  HIPCHK(launch_kv_attention(a, workspace, (hipStream_t)stream));
+  return AWSRC_OK;
 }

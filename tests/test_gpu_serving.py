@@ -1,0 +1,656 @@
+"""The 8-bit serving calls on the GPU: codes, scales and rotations to the bit
+against the fp32 recipe, products exact up to the epilogue's roundings,
+attention within the bound that tests/serving_ref.py derives."""
+import numpy as np
+import pytest
+import torch
+
+import serving_ref as R
+
+pytestmark = pytest.mark.gpu
+
+awsrc = pytest.importorskip("paper_2608_23144_amd")
+
+DEV = "cuda"
+TYPES = [torch.float32, torch.bfloat16, torch.float16]
+EPS = {t: torch.finfo(t).eps / 2 for t in TYPES}  # half an ulp, relative
+FLOOR = {torch.float32: 2.0 ** -149, torch.bfloat16: 2.0 ** -134, torch.float16: 2.0 ** -25}  # of subnormals
+
+
+def _gen(*key):
+    g = torch.Generator()
+    g.manual_seed(sum((i + 1) * ord(c) for i, c in enumerate(repr(key))))
+    return g
+
+
+def _randn(g, *shape):
+    return torch.randn(*shape, generator=g)
+
+
+def _same_bits(a, b):
+    a, b = np.asarray(a), np.asarray(b)
+    assert a.shape == b.shape and a.dtype == b.dtype
+    if a.dtype.kind == "f":
+        assert np.array_equal(np.isnan(a), np.isnan(b))
+        a, b = np.nan_to_num(a, nan=0.0), np.nan_to_num(b, nan=0.0)
+    assert np.array_equal(a, b), f"{np.sum(a != b)} of {a.size} differ"
+
+
+# ------------------------------------------------------------------ rows
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols", [(1, 1), (3, 16), (5, 17), (2, 255), (7, 1000), (4, 4096), (3, 5121), (2, 16384), (2, 40003)])
+def test_quantize_rows_bits(dtype, rows, cols):
+    g = _gen("rows", rows, cols)
+    x = (_randn(g, rows, cols) * torch.exp(2 * _randn(g, rows, 1))).to(dtype)
+    c, s = awsrc.awsrc_quantize_rows_i8(x.to(DEV))
+    want_c, want_s = R.quantize_rows(R.f32(x))
+    _same_bits(s.cpu().numpy(), want_s)
+    _same_bits(c.cpu().numpy(), want_c)
+    assert c.stride(0) % 16 == 0
+    full = c.as_strided((rows, c.stride(0)), (c.stride(0), 1))
+    assert not full[:, cols:].any()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("cols", [33, 256, 3001])
+def test_quantize_rows_special_values(dtype, cols):
+    g = _gen("special", cols)
+    x = _randn(g, 9, cols)
+    x[0] = 0
+    x[1] = 2.0 ** -110  # below the smallest stored magnitude (0 in fp16 already)
+    x[2, cols - 1] = float("inf")
+    x[3, 0] = float("nan")
+    x[4, cols // 2] = -float("inf")
+    x[5] = -x[5].abs()
+    x[6] = 0
+    x[6, cols - 1] = 1e-3
+    x[7] = 3.0
+    x[8, :] = torch.finfo(dtype).max if dtype != torch.float32 else 3e38
+    x = x.to(dtype)
+    c, s = awsrc.awsrc_quantize_rows_i8(x.to(DEV))
+    want_c, want_s = R.quantize_rows(R.f32(x))
+    _same_bits(s.cpu().numpy(), want_s)
+    _same_bits(c.cpu().numpy(), want_c)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("offset,stride", [(0, 131), (1, 136), (3, 129), (8, 144)])
+def test_quantize_rows_views(dtype, offset, stride):
+    """Rows of a wider buffer at any alignment; codes into a given buffer, whose other bytes stay."""
+    rows, cols = 6, 119
+    g = _gen("views", offset, stride)
+    buf = _randn(g, rows * stride + offset).to(dtype).to(DEV)
+    x = buf[offset:].as_strided((rows, cols), (stride, 1))
+    out = torch.full((rows, 160), 77, dtype=torch.int8, device=DEV)
+    s = torch.empty(rows, device=DEV)
+    awsrc.awsrc_quantize_rows_i8(x, out=(out[:, :cols], s))
+    want_c, want_s = R.quantize_rows(R.f32(x))
+    _same_bits(out[:, :cols].cpu().numpy(), want_c)
+    _same_bits(s.cpu().numpy(), want_s)
+    assert not out[:, cols:128].any() and (out[:, 128:] == 77).all()
+    tight = torch.full((rows * cols + 5,), 77, dtype=torch.int8, device=DEV)  # rows side by side: nothing to fill
+    awsrc.awsrc_quantize_rows_i8(x, out=(tight[:rows * cols].view(rows, cols), s))
+    _same_bits(tight[:rows * cols].view(rows, cols).cpu().numpy(), want_c)
+    assert (tight[rows * cols:] == 77).all()
+
+
+# ------------------------------------------------------------------ products
+def _codes(g, rows, cols, lo=-128, fill=0):
+    ld = -(-cols // 16) * 16
+    buf = torch.randint(lo, 128, (rows, ld), generator=g, dtype=torch.int32).to(torch.int8)
+    if fill is not None:
+        buf[:, cols:] = fill
+    return buf.to(DEV)[:, :cols]
+
+
+def _check_product(out, a, sa, b, sb, bias, dtype):
+    acc = a.cpu().double() @ b.cpu().double().T  # exact: below 2^53
+    f = (sa.cpu().double()[:, None] * sb.cpu().double()[None])
+    want = acc * f
+    mag = want.abs()
+    if bias is not None:
+        want = want + bias.cpu().double()
+        mag = mag + bias.cpu().double().abs()
+    got, big = out.cpu().double(), torch.finfo(dtype).max
+    over = want.abs() > big * 1.01  # rounds to infinity
+    assert torch.equal(got[over], want[over].sign() * float("inf"))
+    sure = want.abs() < big * 0.99
+    err = torch.where(sure, got - want, torch.zeros_like(want)).abs()
+    # the sum to fp32, the scales' product, their product, the bias: half an ulp each; then the output's
+    tol = 4 * 2.0 ** -24 * mag + EPS[dtype] * want.abs() * (1 + 2.0 ** -20) + FLOOR[dtype]
+    assert (err <= tol).all(), f"{float((err / tol).max())} times the bound"
+
+
+SHAPES = [(1, 1, 1), (1, 16, 16), (1, 2560, 2048), (2, 17, 33), (3, 100, 1000), (13, 96, 4100), (16, 64, 64), (17, 130, 127),
+          (31, 48, 272), (33, 256, 128), (64, 300, 513), (65, 65, 65), (100, 257, 1040), (128, 128, 128), (129, 127, 2000),
+          (255, 513, 96), (256, 256, 256), (300, 1003, 1337), (511, 260, 144), (1, 33, 131071), (70, 40, 20000)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("M,N,K", SHAPES)
+def test_matmul_i8(M, N, K, dtype):
+    g = _gen("mm", M, N, K)
+    a, b = _codes(g, M, K, fill=3), _codes(g, N, K, fill=5)  # what lies past K must not matter
+    sa, sb = torch.exp(_randn(g, M)).to(DEV) * 1e-3, torch.exp(_randn(g, N)).to(DEV) * 1e-3
+    bias = _randn(g, N).to(DEV) if (M + N) % 2 else None
+    out = awsrc.awsrc_matmul_i8(a, sa, b, sb, bias=bias, out_dtype=dtype)
+    assert out.dtype == dtype
+    _check_product(out, a, sa, b, sb, bias, dtype)
+
+
+@pytest.mark.parametrize("M,N,K", [(5, 33, 100), (40, 70, 600), (150, 301, 260), (300, 300, 300)])
+def test_matmul_i8_extremes(M, N, K):
+    """Every code at the end of its range: the largest sums, of both signs."""
+    a = torch.full((M, -(-K // 16) * 16), -128, dtype=torch.int8, device=DEV)[:, :K]
+    b = torch.full((N, -(-K // 16) * 16), -128, dtype=torch.int8, device=DEV)[:, :K]
+    b[::2] = 127
+    one = torch.ones(max(M, N), device=DEV)
+    out = awsrc.awsrc_matmul_i8(a, one[:M], b, one[:N], out_dtype=torch.float32)
+    want = a.cpu().double() @ b.cpu().double().T
+    assert torch.equal(out.cpu().double(), want.float().double())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("M,N,K", [(3, 37, 80), (20, 129, 65), (140, 270, 130), (260, 515, 400)])
+def test_matmul_i8_strided_and_guarded(M, N, K, dtype):
+    """Operands and results inside wider buffers; nothing around the result is written."""
+    g = _gen("guard", M, N, K)
+    A, B = _codes(g, M + 2, K + 64, fill=None), _codes(g, N + 2, K + 96, fill=None)
+    a, b = A[1:M + 1, 16:16 + K], B[1:N + 1, 32:32 + K]
+    sa, sb = torch.rand(M, generator=g).to(DEV), torch.rand(N, generator=g).to(DEV)
+    for pad, off in ((3, 0), (8, 0), (5, 1), (0, 0)):
+        buf = torch.full(((M + 2) * (N + pad) + off,), 7.0, dtype=dtype, device=DEV)
+        out = buf[off:].view(M + 2, N + pad)[1:M + 1, :N]
+        awsrc.awsrc_matmul_i8(a, sa, b, sb, out=out)
+        _check_product(out, a, sa, b, sb, None, dtype)
+        mask = torch.ones_like(buf, dtype=torch.bool)
+        mask[off:].view(M + 2, N + pad)[1:M + 1, :N] = False
+        assert (buf[mask] == 7.0).all()
+
+
+def test_matmul_i8_nan_scales_stay_in_their_rows():
+    g = _gen("nan")
+    a, b = _codes(g, 70, 128), _codes(g, 90, 128)
+    sa, sb = torch.ones(70, device=DEV), torch.ones(90, device=DEV)
+    sa[3], sb[5] = float("nan"), float("inf")
+    out = awsrc.awsrc_matmul_i8(a, sa, b, sb, out_dtype=torch.float32).cpu()
+    bad = ~torch.isfinite(out)
+    assert bad[3].all() and bad[:, 5].sum() >= 69
+    bad[3], bad[:, 5] = False, False
+    assert not bad.any()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("M,N,K", [(1, 70, 96), (1, 2560, 2048), (4, 65, 1000), (13, 200, 4100), (40, 90, 33), (200, 130, 257)])
+def test_linear_is_quantize_then_matmul(M, N, K, dtype):
+    g = _gen("lin", M, N, K)
+    x = (_randn(g, M, K) * torch.exp(_randn(g, K))).to(dtype).to(DEV)
+    if M > 2:
+        x[1] = 0
+    w, ws = awsrc.awsrc_quantize_rows_i8(_randn(g, N, K).to(DEV))
+    bias = _randn(g, N).to(DEV)
+    got = awsrc.awsrc_linear_i8(x, w, ws, bias=bias)
+    c, s = awsrc.awsrc_quantize_rows_i8(x)
+    want = awsrc.awsrc_matmul_i8(c, s, w, ws, bias=bias, out_dtype=dtype)
+    assert got.dtype == dtype and torch.equal(got, want)
+    wide = torch.zeros(M, K + 5, dtype=dtype, device=DEV)  # rows that lie apart, at odd places
+    wide[:, 3:3 + K] = x
+    assert torch.equal(awsrc.awsrc_linear_i8(wide[:, 3:3 + K], w, ws, bias=bias), want)
+    assert torch.equal(awsrc.awsrc_linear_i8(x, w, ws, bias=bias, out_dtype=torch.float32),
+                       awsrc.awsrc_matmul_i8(c, s, w, ws, bias=bias, out_dtype=torch.float32))
+
+
+def test_linear_row_that_is_not_finite():
+    g = _gen("inf")
+    x = _randn(g, 5, 300).to(DEV)
+    x[2, 7] = float("inf")
+    x[4, 299] = float("nan")
+    w, ws = awsrc.awsrc_quantize_rows_i8(_randn(g, 40, 300).to(DEV))
+    y = awsrc.awsrc_linear_i8(x, w, ws).cpu()
+    assert torch.isnan(y[[2, 4]]).all() and torch.isfinite(y[[0, 1, 3]]).all()
+
+
+def test_products_of_nothing():
+    z = torch.empty(0, 64, device=DEV)
+    w, ws = awsrc.awsrc_quantize_rows_i8(torch.randn(8, 64, device=DEV))
+    assert awsrc.awsrc_linear_i8(z, w, ws).shape == (0, 8)
+    c, s = awsrc.awsrc_quantize_rows_i8(z)
+    assert c.shape == (0, 64) and s.shape == (0,)
+    assert awsrc.awsrc_matmul_i8(c, s, w, ws).shape == (0, 8)
+    assert awsrc.awsrc_linear_i8(torch.randn(3, 64, device=DEV), w[:0], ws[:0]).shape == (3, 0)
+
+
+def test_integer_sums_do_not_depend_on_the_run():
+    g = _gen("again")
+    for M, N, K in ((2, 500, 9000), (96, 700, 5000), (600, 600, 3000)):
+        a, b = _codes(g, M, K), _codes(g, N, K)
+        sa, sb = torch.rand(M, generator=g).to(DEV), torch.rand(N, generator=g).to(DEV)
+        one = awsrc.awsrc_matmul_i8(a, sa, b, sb)
+        for _ in range(3):
+            assert torch.equal(one, awsrc.awsrc_matmul_i8(a, sa, b, sb))
+
+
+# ------------------------------------------------------------------ the cache
+class Batch:
+    """A batch over a cache of random pages in a random order."""
+
+    def __init__(self, key, hq, hk, D, T, lens, news, dtype, spare=2, table_extra=1, scatter=True):
+        g = self.g = _gen(*key)
+        self.hq, self.hk, self.D, self.T, self.dtype = hq, hk, D, T, dtype
+        need = [-(-n // T) for n in lens]
+        self.pages = sum(need) + spare
+        order = torch.randperm(self.pages, generator=g) if scatter else torch.arange(self.pages)
+        width = max(need + [1]) + table_extra
+        table = torch.full((len(lens), width), 10 ** 9, dtype=torch.int32)  # entries past the end are not to be read
+        at = 0
+        for s, n in enumerate(need):
+            table[s, :n] = order[at:at + n].int()
+            at += n
+        self.table = table
+        self.lens, self.news = list(lens), list(news)
+        self.cu = torch.tensor([0] + list(np.cumsum(news)), dtype=torch.int32)
+        self.kv_len = torch.tensor(lens, dtype=torch.int32)
+        self.rows = int(sum(news))
+        self.cache = [torch.randint(-127, 128, (self.pages, hk, T, D), generator=g, dtype=torch.int32).to(torch.int8),
+                      torch.randint(-127, 128, (self.pages, hk, D, T), generator=g, dtype=torch.int32).to(torch.int8),
+                      torch.rand(self.pages, hk, generator=g) * 0.02 + 0.005, torch.rand(self.pages, hk, generator=g) * 0.02 + 0.005]
+        self.q = _randn(g, self.rows, hq, D).to(dtype)
+
+    def dev(self):
+        self.dcache = tuple(t.to(DEV) for t in self.cache)
+        return self.dcache, self.cu.to(DEV), self.kv_len.to(DEV), self.table.to(DEV)
+
+    def np_cache(self):
+        return [t.numpy().copy() for t in self.cache]
+
+
+def _rope(T, rot, g):
+    a = torch.rand(T, rot // 2, generator=g) * 6.28
+    return torch.cos(a), torch.sin(a)
+
+
+def _check_append(b, rot, interleaved, with_q, kscale=1.0, mutate=None):
+    g = b.g
+    qkv = (_randn(g, b.rows, b.hq + 2 * b.hk, b.D) * torch.exp(_randn(g, 1, b.hq + 2 * b.hk, 1)) * kscale).to(b.dtype)
+    if mutate:
+        mutate(qkv)
+    cos = sin = None
+    if rot:
+        cos, sin = _rope(max(b.lens + [1]), rot, g)
+    cache, cu, kv_len, table = b.dev()
+    x = qkv.to(DEV)
+    q = x[:, :b.hq] if with_q else None
+    got_q = awsrc.awsrc_kv_append(cache, x[:, b.hq:b.hq + b.hk], x[:, b.hq + b.hk:], cu, kv_len, table, max(b.news + [0]),
+                                  cos=cos.to(DEV) if rot else None, sin=sin.to(DEV) if rot else None, q=q,
+                                  interleaved=interleaved)
+    want = b.np_cache()
+    xf = R.f32(qkv)
+    want_q = R.append(want, xf[:, b.hq:b.hq + b.hk], xf[:, b.hq + b.hk:], xf[:, :b.hq], b.cu.numpy(), b.kv_len.numpy(),
+                      b.table.numpy(), cos.numpy() if rot else None, sin.numpy() if rot else None, interleaved)
+    _same_bits(cache[2].cpu().numpy(), want[2])
+    _same_bits(cache[3].cpu().numpy(), want[3])
+    for got, ref in zip(cache[:2], want[:2]):
+        _same_bits(got.cpu().numpy(), ref)  # every page: what was not appended is untouched
+    if with_q:
+        _same_bits(R.f32(got_q), R.f32(torch.from_numpy(want_q).to(b.dtype)))
+    else:
+        assert got_q is None
+    return qkv, cos, sin, cache
+
+
+APPENDS = [  # hq, hk, D, T, lens, news
+    (16, 2, 128, 64, [1, 64, 65, 130], [1, 1, 1, 1]),
+    (4, 4, 64, 16, [5, 16, 17, 40, 33], [5, 3, 17, 1, 20]),
+    (8, 1, 256, 32, [70, 3], [70, 3]),
+    (10, 2, 128, 128, [129, 300], [2, 172]),
+    (2, 2, 64, 32, [100, 0, 31], [0, 0, 31]),
+    (3, 1, 128, 64, [200], [137]),
+]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("case", range(len(APPENDS)))
+def test_append_bits(case, dtype):
+    hq, hk, D, T, lens, news = APPENDS[case]
+    for interleaved, rot, with_q in ((False, D, True), (True, D, True), (False, D // 2, True), (True, 2, False), (False, 0, True)):
+        b = Batch(("append", case, interleaved, rot), hq, hk, D, T, lens, news, dtype)
+        _check_append(b, rot, interleaved, with_q)
+
+
+@pytest.mark.parametrize("kscale", [1e-3, 1.0, 300.0])
+def test_append_into_pages_in_use(kscale):
+    """Louder tokens make the page's scale grow and re-round its codes; quieter ones leave it."""
+    b = Batch(("grow", kscale), 2, 2, 64, 16, [9, 16, 23, 40], [1, 2, 4, 3], torch.float32)
+    _check_append(b, 64, False, True, kscale=kscale)
+
+
+def test_append_token_by_token_is_the_recipe_each_time():
+    b = Batch(("steps",), 4, 2, 64, 16, [1, 1], [1, 1], torch.bfloat16)
+    b.lens = [40, 25]
+    need = 3
+    b.pages = 8
+    b.table = torch.tensor([[5, 1, 7, 10 ** 9], [0, 3, 10 ** 9, 10 ** 9]], dtype=torch.int32)
+    b.cache = [torch.randint(-127, 128, (8, 2, 16, 64), generator=b.g, dtype=torch.int32).to(torch.int8),
+               torch.randint(-127, 128, (8, 2, 64, 16), generator=b.g, dtype=torch.int32).to(torch.int8),
+               torch.full((8, 2), float("nan")), torch.full((8, 2), 1e9)]
+    cos, sin = _rope(64, 64, b.g)
+    cache, cu, _, table = b.dev()
+    want = b.np_cache()
+    for step in range(1, 41):
+        lens = torch.tensor([step, min(step, 25)], dtype=torch.int32)
+        news = [1, 1 if step <= 25 else 0]
+        cu = torch.tensor([0] + list(np.cumsum(news)), dtype=torch.int32)
+        k, v = _randn(b.g, sum(news), 2, 64).bfloat16(), _randn(b.g, sum(news), 2, 64).bfloat16()
+        awsrc.awsrc_kv_append(cache, k.to(DEV), v.to(DEV), cu.to(DEV), lens.to(DEV), table, 1, cos=cos.to(DEV), sin=sin.to(DEV))
+        R.append(want, R.f32(k), R.f32(v), None, cu.numpy(), lens.numpy(), b.table.numpy(), cos.numpy(), sin.numpy(), False)
+    for got, ref in zip(cache, want):
+        _same_bits(got.cpu().numpy(), ref)
+    assert need == 3
+
+
+def test_append_values_that_are_not_finite():
+    """They take the scale of their page and head to NaN, and no other; a new first token starts it anew."""
+    def spoil(x):
+        x[3, 2, 5] = float("nan")      # key head 0 (after 2 query heads)
+        x[7, 5, 1] = float("inf")      # value head 1
+    b = Batch(("spoil",), 2, 2, 64, 16, [30], [12], torch.float32)
+    *_, cache = _check_append(b, 64, False, True, mutate=spoil)
+    assert int(torch.isnan(cache[2]).sum()) == 1 and int(torch.isnan(cache[3]).sum()) == 1
+
+
+def test_append_positions_past_the_table_are_nan():
+    b = Batch(("past",), 2, 1, 64, 16, [20], [20], torch.float32)
+    cos, sin = _rope(18, 64, b.g)
+    cache, cu, kv_len, table = b.dev()
+    k, v, q = (_randn(b.g, 20, h, 64).to(DEV) for h in (1, 1, 2))
+    got = awsrc.awsrc_kv_append(cache, k, v, cu, kv_len, table, 20, cos=cos.to(DEV), sin=sin.to(DEV), q=q).cpu()
+    assert torch.isfinite(got[:18]).all() and torch.isnan(got[18:]).all()
+    want = b.np_cache()
+    R.append(want, R.f32(k), R.f32(v), None, b.cu.numpy(), b.kv_len.numpy(), b.table.numpy(), cos.numpy(), sin.numpy(), False)
+    for x, y in zip(cache, want):
+        _same_bits(x.cpu().numpy(), y)
+
+
+@pytest.mark.parametrize("bad", [-1, 10 ** 9])
+def test_append_and_read_drop_tokens_without_a_page(bad):
+    b = Batch(("nopage", bad), 2, 1, 64, 16, [40], [40], torch.bfloat16, table_extra=0)
+    b.table[0, 1] = bad
+    _check_append(b, 64, False, True)
+    cache, cu, kv_len, table = b.dcache, b.cu.to(DEV), b.kv_len.to(DEV), b.table.to(DEV)
+    k, v = awsrc.awsrc_kv_read(cache, cu, kv_len, table, 40, 40)
+    for x in (k, v):
+        assert torch.isnan(x[16:32]).all() and torch.isfinite(x[:16]).all() and torch.isfinite(x[32:]).all()
+    # a table that is too short: the rest has nowhere to go
+    short = b.table[:, :2].contiguous()
+    short[0, 1] = int(b.table[0, 2])
+    b.table = short
+    _check_append(b, 64, False, True)
+    k, _ = awsrc.awsrc_kv_read(b.dcache, cu, kv_len, short.to(DEV), 40, 40)
+    assert torch.isfinite(k[:32]).all() and torch.isnan(k[32:]).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("D,T", [(64, 16), (128, 64), (256, 32), (128, 128)])
+def test_read_is_code_times_scale(D, T, dtype):
+    lens = [1, T, T + 1, 3 * T - 1, 0]
+    news = [1, T - 3, 2, 3 * T - 1, 0]
+    b = Batch(("read", D, T), 2, 2, D, T, lens, news, dtype)
+    cache, cu, kv_len, table = b.dev()
+    k, v = awsrc.awsrc_kv_read(cache, cu, kv_len, table, b.rows, max(news), dtype)
+    row = 0
+    for s in range(len(lens)):
+        for h in range(2):
+            kd, vd, _ = R.dense(b.np_cache(), s, b.table.numpy(), lens[s], h)
+            for got, ref in ((k, kd), (v, vd)):
+                want = torch.from_numpy(ref[lens[s] - news[s]:].astype(np.float32)).to(dtype)  # the product is exact in 64 bits
+                assert torch.equal(got[row:row + news[s], h].cpu(), want)
+        row += news[s]
+
+
+# ------------------------------------------------------------------ attention
+def _check_attention(b, causal=True, scale=None, max_new=None, max_kv=None, cache_np=None, **kw):
+    cache, cu, kv_len, table = b.dev()
+    out = awsrc.awsrc_kv_attention(cache, b.q.to(DEV), cu, kv_len, table, max(b.news + [0]) if max_new is None else max_new,
+                                   max(b.lens + [0]) if max_kv is None else max_kv, scale=scale, causal=causal, **kw)
+    want, tol = R.attention(b.np_cache(), R.f32(b.q), b.cu.numpy(), b.kv_len.numpy(), b.table.numpy(),
+                            b.D ** -0.5 if scale is None else scale, causal)
+    got = out.cpu().double().numpy()
+    err = np.abs(got - want)
+    tol = tol + EPS[b.dtype] * (np.abs(want) + tol) + FLOOR[b.dtype]
+    assert np.isfinite(got).all()
+    assert (err <= tol).all(), f"{(err / tol).max()} times the bound at {np.unravel_index(np.argmax(err / tol), err.shape)}"
+    return out
+
+
+ATTENTIONS = [  # hq, hk, D, T, lens, news
+    (16, 2, 128, 64, [1], [1]),
+    (16, 2, 128, 64, [63, 64, 65, 128, 200], [1, 1, 1, 1, 1]),
+    (40, 8, 128, 16, [17, 500, 1], [1, 1, 1]),
+    (12, 12, 64, 32, [33, 257], [1, 1]),
+    (8, 4, 256, 64, [700, 15], [1, 1]),
+    (16, 1, 64, 128, [1000], [1]),
+    (34, 2, 64, 16, [100, 40], [1, 3]),          # a group of 17
+    (16, 2, 128, 64, [300, 90], [5, 2]),         # a few rows against a history
+    (4, 2, 128, 32, [77, 200, 10, 0], [77, 13, 1, 0]),
+    (2, 2, 64, 64, [150, 129], [150, 129]),
+    (5, 1, 128, 16, [333], [333]),
+    (2, 1, 256, 128, [260, 130], [260, 64]),
+    (3, 3, 64, 16, [70, 20, 45], [0, 20, 45]),
+]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("case", range(len(ATTENTIONS)))
+def test_attention(case, causal, dtype):
+    hq, hk, D, T, lens, news = ATTENTIONS[case]
+    _check_attention(Batch(("att", case), hq, hk, D, T, lens, news, dtype), causal)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("hq,hk,D", [(8, 1, 128), (4, 2, 64), (2, 1, 256)])
+def test_attention_over_long_sequences(hq, hk, D, dtype):
+    """Long enough to be split; single rows and a few."""
+    _check_attention(Batch(("long", hq, hk, D), hq, hk, D, 64, [9001, 4096, 5], [1, 2, 1], dtype))
+    _check_attention(Batch(("long2", hq, hk, D), hq, hk, D, 16, [6007], [40], dtype))
+
+
+def test_attention_rows_that_see_nothing():
+    """More rows than tokens: the first see none and are 0; a sequence without tokens likewise."""
+    b = Batch(("none",), 4, 2, 64, 16, [3, 0, 40], [9, 2, 45], torch.float16)
+    out = _check_attention(b)
+    assert not out[:6].any() and not out[9:11].any() and not out[11:16].any() and out[6].any()
+    b = Batch(("none2",), 4, 2, 64, 16, [3, 0, 40], [100, 70, 45], torch.float16)
+    assert not _check_attention(b)[:97].any()
+
+
+@pytest.mark.parametrize("news", [[1], [80]])
+def test_attention_without_a_page(news):
+    b = Batch(("hole", news), 4, 2, 64, 16, [100], news, torch.float16)
+    b.table[0, 2], b.table[0, 4] = -5, 10 ** 8
+    _check_attention(b)
+    b.table[:] = -1
+    assert not _check_attention(b).any()
+
+
+@pytest.mark.parametrize("news", [[1, 1], [90, 33]])
+def test_attention_bounds_of_the_caller(news):
+    """Loose bounds change nothing; max_kv cuts; a table that is too short cuts too."""
+    b = Batch(("bounds", news), 4, 2, 64, 16, [100, 64], news, torch.float16)
+    one = _check_attention(b)
+    two = _check_attention(b, max_new=b.rows, max_kv=100000)
+    assert (one.float() - two.float()).abs().max() < 2e-3
+    b.table[:, 3:] = -1
+    three = _check_attention(b)
+    c, cu, kv_len, table = b.dev()
+    four = awsrc.awsrc_kv_attention(c, b.q.to(DEV), cu, kv_len, table[:, :3].contiguous(), max(news), 100)
+    five = awsrc.awsrc_kv_attention(c, b.q.to(DEV), cu, kv_len, table, max(news), 48)
+    assert (three.float() - four.float()).abs().max() < 2e-3 and (three.float() - five.float()).abs().max() < 2e-3
+
+
+@pytest.mark.parametrize("news", [[1], [70]])
+def test_attention_ignores_what_lies_past_the_end(news):
+    """Scales of pages that are not the sequence's and codes after its last token have no say."""
+    b = Batch(("past", news), 4, 2, 64, 32, [75], news, torch.float16)
+    one = _check_attention(b)
+    used = set(int(p) for p in b.table[0, :3])
+    for p in range(b.pages):
+        if p not in used:
+            b.cache[2][p], b.cache[3][p] = float("nan"), float("inf")
+    last = int(b.table[0, 2])
+    b.cache[0][last, :, 75 % 32:] = 127
+    b.cache[1][last, :, :, 75 % 32:] = -127
+    two = _check_attention(b)
+    assert torch.equal(one, two)
+
+
+@pytest.mark.parametrize("news", [[1], [70]])
+def test_attention_pages_of_very_different_loudness(news):
+    """Value scales 2^-60 .. 2^40 in one sequence, pages that hold zeros alone, and very quiet sequences."""
+    b = Batch(("loud", news), 4, 2, 64, 16, [200], news, torch.bfloat16)
+    for i in range(13):
+        p = int(b.table[0, i])
+        b.cache[3][p] = 2.0 ** (-60 + 8 * i)
+        if i % 4 == 1:
+            b.cache[1][p], b.cache[3][p] = 0, 0.0
+        if i % 5 == 2:
+            b.cache[0][p], b.cache[2][p] = 0, 0.0
+    _check_attention(b)
+    b.cache[3][:] = 2.0 ** -60
+    _check_attention(b)
+    b.cache[1][:], b.cache[3][:] = 0, 0.0
+    assert not _check_attention(b).any()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("news", [[1, 1], [40, 70]])
+def test_attention_query_magnitudes(news, dtype):
+    """Queries at the ends of their type's range, sharp and flat softmaxes, zero queries."""
+    b = Batch(("mag", news), 4, 2, 64, 16, [90, 70], news, dtype)
+    for m in ((1e30, 1e-30) if dtype == torch.bfloat16 else (3e4, 1e-3)):
+        b.q = (_randn(b.g, b.rows, 4, 64).clamp(-2, 2) * m).to(dtype)
+        _check_attention(b, scale=0.1 / m)
+    b.q = torch.zeros_like(b.q)
+    _check_attention(b)
+    b.q = (_randn(b.g, b.rows, 4, 64) * 20).to(dtype)
+    _check_attention(b, scale=1.0)
+    _check_attention(b, scale=-0.5)
+    _check_attention(b, scale=0.0)
+
+
+@pytest.mark.parametrize("news", [[1], [70]])
+def test_attention_nan_stays_with_those_who_see_it(news):
+    b = Batch(("nan", news), 4, 2, 64, 16, [100], news, torch.bfloat16)
+    b.cache[2][int(b.table[0, 5]), 1] = float("nan")   # keys of head 1, tokens 80..95
+    b.cache[3][int(b.table[0, 6]), 0] = float("nan")   # values of head 0, tokens 96..99
+    cache, cu, kv_len, table = b.dev()
+    out = awsrc.awsrc_kv_attention(cache, b.q.to(DEV), cu, kv_len, table, max(news), 100).cpu()
+    pos = 100 - news[0] + torch.arange(news[0])
+    nan = torch.isnan(out).all(-1)
+    assert torch.equal(nan[:, 0:2], (pos >= 96)[:, None].expand(-1, 2))
+    assert torch.equal(nan[:, 2:4], (pos >= 80)[:, None].expand(-1, 2))
+    assert torch.equal(torch.isnan(out).any(-1), nan)
+    b = Batch(("nanq", news), 4, 2, 64, 16, [100], news, torch.bfloat16)
+    b.q[0, 1, 3] = float("nan")
+    cache, cu, kv_len, table = b.dev()
+    out = awsrc.awsrc_kv_attention(cache, b.q.to(DEV), cu, kv_len, table, max(news), 100).cpu()
+    assert torch.isnan(out[0, 1]).all()
+    out[0, 1] = 0
+    assert torch.isfinite(out).all()
+
+
+@pytest.mark.parametrize("news", [[1, 1], [30, 61]])
+def test_attention_views(news):
+    """Queries inside a fused projection's rows, results inside a wider buffer that stays otherwise."""
+    b = Batch(("views", news), 4, 2, 64, 16, [90, 61], news, torch.bfloat16)
+    plain = _check_attention(b)
+    wide = torch.zeros(b.rows, 9, 64, dtype=b.dtype, device=DEV)
+    wide[:, 2:6] = b.q.to(DEV)
+    buf = torch.full((b.rows + 1, 6, 64), 7.0, dtype=b.dtype, device=DEV)
+    cache, cu, kv_len, table = b.dev()
+    awsrc.awsrc_kv_attention(cache, wide[:, 2:6], cu, kv_len, table, max(news), 90, out=buf[:b.rows, 1:5])
+    assert torch.equal(buf[:b.rows, 1:5], plain)
+    assert (buf[b.rows] == 7).all() and (buf[:, 0] == 7).all() and (buf[:, 5] == 7).all()
+
+
+def test_cache_past_32_bit_offsets():
+    """Pages whose codes lie more than 2^32 bytes into the cache."""
+    hk, D, T = 8, 256, 128
+    pages = (1 << 32) // (hk * D * T) + 40
+    cache = awsrc.make_kv_cache(pages, hk, D, T)
+    lens, news = [300, 130], [300, 130]
+    table = torch.tensor([[pages - 1, 3, pages - 7], [pages - 2, pages - 30, 10 ** 9]], dtype=torch.int32, device=DEV)
+    cu = torch.tensor([0, 300, 430], dtype=torch.int32, device=DEV)
+    kv_len = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    g = _gen("far")
+    k, v, q = (_randn(g, 430, hk, D).bfloat16().to(DEV) for _ in range(3))
+    awsrc.awsrc_kv_append(cache, k, v, cu, kv_len, table, 300)
+    small = awsrc.make_kv_cache(5, hk, D, T)
+    stable = torch.tensor([[0, 1, 2], [3, 4, 0]], dtype=torch.int32, device=DEV)
+    awsrc.awsrc_kv_append(small, k, v, cu, kv_len, stable, 300)
+    for x, y in zip(awsrc.awsrc_kv_read(cache, cu, kv_len, table, 430, 300), awsrc.awsrc_kv_read(small, cu, kv_len, stable, 430, 300)):
+        assert torch.equal(x, y) and torch.isfinite(x).all()
+    for m, c, n in ((300, cu, kv_len), (1, torch.tensor([0, 1, 2], dtype=torch.int32, device=DEV), kv_len)):
+        rows = int(c[-1])
+        a = awsrc.awsrc_kv_attention(cache, q[:rows], c, n, table, m, 300)
+        e = awsrc.awsrc_kv_attention(small, q[:rows], c, n, stable, m, 300)
+        assert torch.equal(a, e) and torch.isfinite(a).all()
+
+
+# ------------------------------------------------------------------ together
+def test_calls_on_another_stream():
+    st = torch.cuda.Stream()
+    g = _gen("stream")
+    x = _randn(g, 37, 512).bfloat16().to(DEV)
+    w, ws = awsrc.awsrc_quantize_rows_i8(_randn(g, 300, 512).to(DEV))
+    b = Batch(("stream",), 4, 2, 64, 16, [90, 70], [3, 1], torch.bfloat16)
+    cache, cu, kv_len, table = b.dev()
+    k, v, q = (_randn(g, 4, h, 64).bfloat16().to(DEV) for h in (2, 2, 4))
+    ref_cache = tuple(t.clone() for t in cache)
+    want = awsrc.awsrc_linear_i8(x, w, ws)
+    awsrc.awsrc_kv_append(ref_cache, k, v, cu, kv_len, table, 3)
+    want_o = awsrc.awsrc_kv_attention(ref_cache, q, cu, kv_len, table, 3, 90)
+    torch.cuda.synchronize()
+    for _ in range(3):
+        y = awsrc.awsrc_linear_i8(x, w, ws, stream=st)
+        awsrc.awsrc_kv_append(cache, k, v, cu, kv_len, table, 3, stream=st)
+        o = awsrc.awsrc_kv_attention(cache, q, cu, kv_len, table, 3, 90, stream=st)
+        st.synchronize()
+        assert torch.equal(y, want) and torch.equal(o, want_o)
+
+
+def test_a_captured_step_replays():
+    """The calls allocate nothing in the library: a graph of a decode step gives the eager step's results on every replay."""
+    g = _gen("graph")
+    b = Batch(("graph",), 8, 2, 128, 64, [700, 129], [1, 1], torch.bfloat16)
+    cache, cu, kv_len, table = b.dev()
+    w, ws = awsrc.awsrc_quantize_rows_i8((_randn(g, 12 * 128, 512) * 0.05).to(DEV))
+    wo, wos = awsrc.awsrc_quantize_rows_i8((_randn(g, 512, 1024) * 0.05).to(DEV))
+    cos, sin = (t.to(DEV) for t in _rope(1024, 128, g))
+    x = _randn(g, 2, 512).bfloat16().to(DEV)
+
+    def step():
+        qkv = awsrc.awsrc_linear_i8(x, w, ws).view(2, 12, 128)
+        q = awsrc.awsrc_kv_append(cache, qkv[:, 8:10], qkv[:, 10:], cu, kv_len, table, 1, cos=cos, sin=sin, q=qkv[:, :8])
+        o = awsrc.awsrc_kv_attention(cache, q, cu, kv_len, table, 1, 1024)
+        return awsrc.awsrc_linear_i8(o.view(2, -1), wo, wos)
+
+    start = tuple(t.clone() for t in cache)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = step()
+    for i in range(4):
+        for c, s in zip(cache, start):
+            c.copy_(s)
+        x.copy_(_randn(g, 2, 512).bfloat16())
+        graph.replay()
+        torch.cuda.synchronize()
+        got = y.clone()
+        for c, s in zip(cache, start):
+            c.copy_(s)
+        assert torch.equal(got, step()), i

@@ -1,0 +1,178 @@
+"""The 8-bit serving calls refuse bad arguments before anything touches a
+device, answer their workspace queries without one, and take empty batches."""
+import ctypes
+
+import pytest
+import torch
+
+awsrc = pytest.importorskip("paper_2608_23144_amd")
+
+L = awsrc.LIB
+OK, EINVAL, ENOSPC = awsrc.AWSRC_OK, awsrc.AWSRC_EINVAL, awsrc.AWSRC_ENOSPC
+F32, BF16, F16 = 0, 1, 2
+P = 4096  # an address that no refused call follows
+
+
+def _call(f, base, **bad):
+    args = dict(base)
+    for k in bad:
+        assert k in args
+    args.update(bad)
+    st = f(*args.values())
+    if st != OK:
+        assert L.awsrc_last_error()
+    return st
+
+
+QUANT = dict(X=P, x_dtype=F32, rows=4, cols=33, ldx=40, codes=P, ldc=48, scale=P, stream=None)
+
+
+@pytest.mark.parametrize("bad", [dict(x_dtype=3), dict(x_dtype=-1), dict(rows=-1), dict(cols=0), dict(ldx=32), dict(ldc=32),
+                                 dict(X=None), dict(codes=None), dict(scale=None), dict(X=P + 2), dict(scale=P + 2),
+                                 dict(rows=1 << 31), dict(ldx=1 << 31)])
+def test_quantize_rows_refuses(bad):
+    assert _call(L.awsrc_quantize_rows_i8, QUANT, **bad) == EINVAL
+
+
+def test_quantize_no_rows():
+    assert _call(L.awsrc_quantize_rows_i8, QUANT, rows=0, X=None, codes=None, scale=None) == OK
+
+
+def _ws(n=0):
+    return ctypes.byref(ctypes.c_size_t(n))
+
+
+MATMUL = dict(A=P, lda=48, a_scale=P, B=P, ldb=48, b_scale=P, bias=None, M=3, N=5, K=33, out=P, out_dtype=BF16, ldo=5, ws=P,
+              n=None, stream=None)
+LINEAR = dict(X=P, x_dtype=BF16, ldx=33, B=P, ldb=48, b_scale=P, bias=None, M=3, N=5, K=33, out=P, out_dtype=BF16, ldo=5, ws=P,
+              n=None, stream=None)
+
+
+@pytest.mark.parametrize("bad", [dict(out_dtype=7), dict(M=-1), dict(N=-1), dict(K=0), dict(K=131072, lda=131072, ldb=131072),
+                                 dict(lda=40), dict(ldb=40), dict(lda=32), dict(ldb=32), dict(ldo=4), dict(A=P + 8),
+                                 dict(B=P + 8), dict(out=P + 1), dict(A=None), dict(B=None), dict(a_scale=None),
+                                 dict(b_scale=None), dict(out=None), dict(bias=P + 2), dict(b_scale=P + 1), dict(a_scale=P + 1)])
+def test_matmul_refuses(bad):
+    assert _call(L.awsrc_matmul_i8, {**MATMUL, "n": _ws(1 << 40)}, **bad) == EINVAL
+
+
+def test_matmul_needs_ws_bytes():
+    assert _call(L.awsrc_matmul_i8, MATMUL) == EINVAL
+    assert _call(L.awsrc_linear_i8, LINEAR) == EINVAL
+
+
+@pytest.mark.parametrize("bad", [dict(out_dtype=7), dict(x_dtype=5), dict(M=-1), dict(K=0), dict(ldx=32), dict(ldb=40), dict(ldo=4),
+                                 dict(X=P + 1), dict(B=P + 8), dict(X=None), dict(B=None), dict(b_scale=None), dict(out=None),
+                                 dict(bias=P + 2), dict(ws=P + 8)])
+def test_linear_refuses(bad):
+    assert _call(L.awsrc_linear_i8, {**LINEAR, "n": _ws(1 << 40)}, **bad) == EINVAL
+
+
+def test_product_workspaces():
+    n = ctypes.c_size_t(0)
+    assert _call(L.awsrc_linear_i8, {**LINEAR, "n": ctypes.byref(n)}, X=None, B=None, b_scale=None, out=None, ws=None) == OK
+    assert n.value >= 3 * 48 + 3 * 4
+    assert _call(L.awsrc_linear_i8, {**LINEAR, "n": _ws(n.value - 1)}) == ENOSPC
+    assert awsrc.linear_i8_workspace_bytes(3, 5, 33) == n.value
+    for M, N, K in ((1, 2560, 2048), (13, 2048, 11008), (8192, 27648, 5120), (300, 64, 131071)):
+        ld = -(-K // 16) * 16
+        assert _call(L.awsrc_matmul_i8, {**MATMUL, "n": ctypes.byref(n)}, A=None, a_scale=None, B=None, b_scale=None, out=None,
+                     ws=None, M=M, N=N, K=K, lda=ld, ldb=ld, ldo=N) == OK
+        if n.value:
+            assert _call(L.awsrc_matmul_i8, {**MATMUL, "n": _ws(n.value - 1)}, M=M, N=N, K=K, lda=ld, ldb=ld, ldo=N) == ENOSPC
+            assert _call(L.awsrc_matmul_i8, {**MATMUL, "n": _ws(1 << 40)}, M=M, N=N, K=K, lda=ld, ldb=ld, ldo=N, ws=None) == ENOSPC
+    for empty in (dict(M=0), dict(N=0, ldo=0)):
+        assert _call(L.awsrc_matmul_i8, {**MATMUL, "n": _ws(0)}, **empty) == OK
+        assert _call(L.awsrc_linear_i8, {**LINEAR, "n": _ws(0)}, **empty) == OK
+
+
+def _cache(**bad):
+    c = dict(k=P, v=P, k_scale=P, v_scale=P, n_pages=4, kv_heads=2, head_dim=128, page_tokens=64, reserved=0)
+    c.update(bad)
+    return ctypes.byref(awsrc.awsrc_kv_cache(*c.values()))
+
+
+APPEND = dict(cache=None, k=P, ldk=256, v=P, ldv=256, q=P, ldq=1024, q_heads=8, q_out=P, ldqo=1024, dtype=BF16, cos=P, sin=P,
+              rope_len=100, rot=128, interleaved=0, n_seq=2, n_rows=5, cu=P, kv_len=P, table=P, table_ld=3, max_new=4, stream=None)
+READ = dict(cache=None, n_seq=2, n_rows=5, cu=P, kv_len=P, table=P, table_ld=3, max_new=4, k_out=P, v_out=P, dtype=BF16, stream=None)
+ATTEND = dict(cache=None, q=P, ldq=1024, q_heads=8, dtype=BF16, n_seq=2, n_rows=5, cu=P, kv_len=P, table=P, table_ld=3, max_new=4,
+              max_kv=100, scale=0.1, causal=1, out=P, ldo=1024, ws=P, n=None, stream=None)
+
+BAD_CACHES = [dict(n_pages=0), dict(kv_heads=0), dict(head_dim=96), dict(head_dim=32), dict(page_tokens=8), dict(page_tokens=48),
+              dict(page_tokens=256), dict(reserved=1), dict(k=None), dict(v=None), dict(k_scale=None), dict(v_scale=None),
+              dict(k=P + 8), dict(v=P + 4), dict(k_scale=P + 2), dict(v_scale=P + 1)]
+
+
+@pytest.mark.parametrize("bad", BAD_CACHES)
+def test_cache_refused(bad):
+    c = _cache(**bad)
+    assert _call(L.awsrc_kv_append, APPEND, cache=c) == EINVAL
+    assert _call(L.awsrc_kv_read, READ, cache=c) == EINVAL
+    assert _call(L.awsrc_kv_attention, {**ATTEND, "n": _ws(1 << 40)}, cache=c) == EINVAL
+
+
+BAD_BATCHES = [dict(cache=None), dict(n_seq=-1), dict(n_rows=-1), dict(table_ld=0), dict(max_new=-1), dict(max_new=6), dict(cu=None),
+               dict(kv_len=None), dict(table=None), dict(cu=P + 2), dict(kv_len=P + 1), dict(table=P + 2), dict(dtype=4),
+               dict(table_ld=1 << 31)]
+
+
+@pytest.mark.parametrize("bad", BAD_BATCHES)
+def test_batch_refused(bad):
+    bad = {"cache": _cache(), **bad}
+    assert _call(L.awsrc_kv_append, APPEND, **bad) == EINVAL
+    assert _call(L.awsrc_kv_read, READ, **bad) == EINVAL
+    assert _call(L.awsrc_kv_attention, {**ATTEND, "n": _ws(1 << 40)}, **bad) == EINVAL
+
+
+@pytest.mark.parametrize("bad", [dict(k=None), dict(v=None), dict(ldk=255), dict(ldv=255), dict(ldq=1023), dict(ldqo=1023),
+                                 dict(k=P + 1), dict(q_out=None), dict(q=None), dict(q_heads=0), dict(rot=129), dict(rot=130),
+                                 dict(rot=-2), dict(cos=None), dict(sin=None), dict(cos=P + 2), dict(rope_len=-1)])
+def test_append_refuses(bad):
+    assert _call(L.awsrc_kv_append, {**APPEND, "cache": _cache()}, **bad) == EINVAL
+
+
+@pytest.mark.parametrize("bad", [dict(k_out=None), dict(v_out=None), dict(k_out=P + 1)])
+def test_read_refuses(bad):
+    assert _call(L.awsrc_kv_read, {**READ, "cache": _cache()}, **bad) == EINVAL
+
+
+@pytest.mark.parametrize("bad", [dict(dtype=F32), dict(q_heads=7), dict(q_heads=0), dict(ldq=1020), dict(ldo=1028), dict(ldq=1000),
+                                 dict(q=P + 8), dict(out=P + 2), dict(out=None), dict(max_kv=-1), dict(scale=float("nan")),
+                                 dict(scale=float("inf")), dict(n=None)])
+def test_attention_refuses(bad):
+    assert _call(L.awsrc_kv_attention, {**ATTEND, "cache": _cache(), "n": _ws(1 << 40)}, **bad) == EINVAL
+
+
+def test_attention_workspace_query():
+    n = ctypes.c_size_t(7)
+    c = _cache(k=None, v=None, k_scale=None, v_scale=None)
+    q = dict(cache=c, q=None, out=None, ws=None, cu=None, kv_len=None, table=None, n=ctypes.byref(n))
+    assert _call(L.awsrc_kv_attention, {**ATTEND, **q}) == OK
+    assert _call(L.awsrc_kv_attention, {**ATTEND, **q}, n_seq=2, n_rows=2, max_new=1, max_kv=1 << 20, table_ld=1 << 14) == OK
+    if n.value:
+        bad = dict(n_seq=2, n_rows=2, max_new=1, max_kv=1 << 20, table_ld=1 << 14, cache=_cache(), n=_ws(n.value - 1))
+        assert _call(L.awsrc_kv_attention, ATTEND, **bad) == ENOSPC
+
+
+def test_empty_batches():
+    c = _cache()
+    for e in (dict(n_seq=0), dict(n_rows=0, max_new=0), dict(max_new=0)):
+        assert _call(L.awsrc_kv_append, {**APPEND, "cache": c}, **e) == OK
+        assert _call(L.awsrc_kv_read, {**READ, "cache": c}, **e) == OK
+        assert _call(L.awsrc_kv_attention, {**ATTEND, "cache": c, "n": _ws(0)}, **e) == OK
+
+
+def test_python_refuses_host_tensors_and_shapes():
+    x = torch.zeros(3, 32)
+    w = torch.zeros(4, 32, dtype=torch.int8)
+    for f in (lambda: awsrc.awsrc_quantize_rows_i8(x), lambda: awsrc.awsrc_linear_i8(x, w, torch.zeros(4)),
+              lambda: awsrc.awsrc_matmul_i8(w, torch.zeros(4), w, torch.zeros(4)),
+              lambda: awsrc.awsrc_quantize_rows_i8(x[:, ::2]), lambda: awsrc.awsrc_linear_i8(x, w[:, :16], torch.zeros(4))):
+        with pytest.raises(ValueError):
+            f()
+    with pytest.raises(TypeError):
+        awsrc.awsrc_linear_i8(x, x, torch.zeros(3))
+    cache = awsrc.make_kv_cache(2, 2, 64, 16, device="cpu")
+    i = torch.zeros(2, dtype=torch.int32)
+    with pytest.raises(ValueError):
+        awsrc.awsrc_kv_attention(cache, torch.zeros(1, 2, 64, dtype=torch.bfloat16), i, i[:1], i[None], 1, 1)
