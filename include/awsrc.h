@@ -503,7 +503,7 @@ awsrc_status awsrc_quantize_rows_i8(const void* X, int32_t x_dtype, int64_t rows
  * the sum exact in int32, then fp32 (sum * (a_scale * b_scale) + bias), rounded
  * once to out_dtype (nearest even).
  *  A, B     int8, row i at A + i * lda; 16-byte aligned, lda and ldb multiples
- *           of 16 and >= K rounded up to 16.  Each row is readable up to K
+ *           of 16, >= K rounded up to 16, <= 2^22.  Each row is readable up to K
  *           rounded up to 16; what lies past K does not matter.
  *  bias_or_null  [N] fp32.
  *  out      [M, N], row m at out + m * ldo, ldo >= N, aligned to its type.

@@ -1068,6 +1068,7 @@ int64_t act_size(int32_t t) { return t == AWSRC_DTYPE_F32 ? 4 : 2; }
 bool misaligned(const void* p, uintptr_t a) { return reinterpret_cast<uintptr_t>(p) & (a - 1); }
 
 constexpr int64_t kMaxDim = 1ll << 31;  // rows, columns and leading dimensions
+constexpr int64_t kMaxLdI8 = 1ll << 22;  // of int8 operands: 256 rows of one stay below 2^31 bytes
 
 awsrc_status check_quantize(const void* X, int32_t x_dtype, int64_t rows, int64_t cols, int64_t ldx) {
   if (!act_dtype(x_dtype)) return fail(AWSRC_EINVAL, "bad x_dtype %d", x_dtype);
@@ -1083,8 +1084,8 @@ awsrc_status check_product(const int8_t* B, int64_t ldb, const float* b_scale, i
   if (!act_dtype(out_dtype)) return fail(AWSRC_EINVAL, "bad out_dtype %d", out_dtype);
   if (M < 0 || N < 0 || M >= kMaxDim || N >= kMaxDim) return fail(AWSRC_EINVAL, "bad shape %lld x %lld", (long long)M, (long long)N);
   if (K < 1 || K > kMaxSumI8) return fail(AWSRC_EINVAL, "K=%lld out of range 1..%lld", (long long)K, (long long)kMaxSumI8);
-  if (ldb % 16 || ldb < round16(K) || ldb >= kMaxDim)
-    return fail(AWSRC_EINVAL, "ldb=%lld: must be a multiple of 16, at least K", (long long)ldb);
+  if (ldb % 16 || ldb < round16(K) || ldb > kMaxLdI8)
+    return fail(AWSRC_EINVAL, "ldb=%lld: must be a multiple of 16, at least K, at most 2^22", (long long)ldb);
   if (ldo < N || ldo >= kMaxDim) return fail(AWSRC_EINVAL, "ldo=%lld: must be at least N", (long long)ldo);
   if (B && misaligned(B, 16)) return fail(AWSRC_EINVAL, "int8 operands must be 16-byte aligned");
   if (b_scale && misaligned(b_scale, 4)) return fail(AWSRC_EINVAL, "scales must be 4-byte aligned");
@@ -1156,8 +1157,8 @@ extern "C" awsrc_status awsrc_matmul_i8(const int8_t* A, int64_t lda, const floa
                                         void* stream) {
   awsrc_status st = check_product(B, ldb, b_scale, M, N, K, out, out_dtype, ldo);
   if (st != AWSRC_OK) return st;
-  if (lda % 16 || lda < round16(K) || lda >= kMaxDim)
-    return fail(AWSRC_EINVAL, "lda=%lld: must be a multiple of 16, at least K", (long long)lda);
+  if (lda % 16 || lda < round16(K) || lda > kMaxLdI8)
+    return fail(AWSRC_EINVAL, "lda=%lld: must be a multiple of 16, at least K, at most 2^22", (long long)lda);
   if (!ws_bytes) return fail(AWSRC_EINVAL, "ws_bytes is NULL");
   const size_t need = M && N ? matmul_i8_ws_bytes(M, N, K) : 0;
   if (!workspace && !A && !B && !out) {

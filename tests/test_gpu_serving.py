@@ -220,6 +220,25 @@ def test_products_of_nothing():
     assert awsrc.awsrc_linear_i8(torch.randn(3, 64, device=DEV), w[:0], ws[:0]).shape == (3, 0)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("M,N,K", [(3590, 3850, 272), (2049, 6150, 1000), (1800, 1900, 513), (700, 27648, 200)])
+def test_matmul_i8_large(M, N, K, dtype):
+    """Enough tiles for the largest tile shapes, ragged at every end."""
+    g = _gen("large", M, N, K)
+    a, b = _codes(g, M, K, fill=3), _codes(g, N, K, fill=5)
+    sa, sb = (torch.exp(_randn(g, M)) * 1e-3).to(DEV), (torch.exp(_randn(g, N)) * 1e-3).to(DEV)
+    bias = _randn(g, N).to(DEV) if N % 4 else None
+    buf = torch.full((M, N + 8), 7.0, dtype=dtype, device=DEV)
+    out = awsrc.awsrc_matmul_i8(a, sa, b, sb, bias=bias, out=buf[:, :N])
+    want = (a.double() @ b.double().T) * sa.double()[:, None] * sb.double()
+    mag = want.abs()
+    if bias is not None:
+        want, mag = want + bias.double(), mag + bias.double().abs()
+    tol = 4 * 2.0 ** -24 * mag + EPS[dtype] * want.abs() * (1 + 2.0 ** -20) + FLOOR[dtype]
+    assert ((out.double() - want).abs() <= tol).all()
+    assert (buf[:, N:] == 7.0).all()
+
+
 def test_integer_sums_do_not_depend_on_the_run():
     g = _gen("again")
     for M, N, K in ((2, 500, 9000), (96, 700, 5000), (600, 600, 3000)):
