@@ -7,6 +7,7 @@
 // [16 (l / 16), + 16) of a 64-byte step; the result lane holds column l % 16
 // and rows 4 (l / 16) + i.  B (the weights) takes the rows' place and A the
 // columns', so that a lane ends with four consecutive n of one m.
+#include <type_traits>
 #include "serve_internal.h"
 
 namespace awsrc {
@@ -27,52 +28,75 @@ __device__ __forceinline__ void store4(TO* o, const float (&y)[4], int64_t n, in
   }
 }
 
-// 16 bytes of an operand row at byte k, zero past K (rows are readable to the
-// next multiple of 16) and for rows that do not exist.
-__device__ __forceinline__ i32x4 load_chunk(const int8_t* __restrict__ p, int64_t ld, int64_t row, int64_t rows,
-                                            int64_t k, int64_t K) {
-  i32x4 v = {0, 0, 0, 0};
-  if (row < rows && k < K) {
-    v = *reinterpret_cast<const i32x4*>(p + row * ld + k);
-    if (k + 16 > K) {
-      const int left = (int)(K - k);
+// Up to 16 rows: the weights' bytes are all that counts.  A workgroup takes 16
+// weight rows (columns of the result) against all activation rows, its W
+// wavefronts sharing the sum; both operands come straight from memory in the
+// matrix cores' layout, U steps of 64 bytes ahead of the products, and the
+// wavefronts' sums meet in LDS.  2560 x 2048: 3.4 us; 13 x 2048 x 11008: 11.3 us
+// (128 workgroups, whose CUs take in some 39 GB/s each).
+template <int W, int U, typename TO>
+__global__ __launch_bounds__(64 * W) void k_matmul_i8_rows(LinearArgs a) {
+  __shared__ i32x4 part[W][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t n0 = (int64_t)blockIdx.x * 16;
+  const int r = lane & 15, g = lane >> 4;
+  const int K = (int)a.K;
+  // rows that do not exist read the last one: their sums are not stored
+  const int8_t* pb = a.B + (n0 + r < a.N ? n0 + r : a.N - 1) * a.ldb + 16 * g;
+  const int8_t* pa = a.A + (r < a.M ? r : a.M - 1) * a.lda + 16 * g;
+  i32x4 acc = {0, 0, 0, 0};
+  i32x4 fb[2][U], fa[2][U];
+  auto load = [&](int buf, int k) {
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const int b = left - 4 * w;
-        v[w] = b <= 0 ? 0 : b >= 4 ? v[w] : (v[w] & (int)((1u << (8 * b)) - 1u));
-      }
+    for (int u = 0; u < U; ++u) {
+      fb[buf][u] = *reinterpret_cast<const i32x4*>(pb + k + 64 * u);
+      fa[buf][u] = *reinterpret_cast<const i32x4*>(pa + k + 64 * u);
+    }
+  };
+  auto products = [&](int buf) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[buf][u], fa[buf][u], acc, 0, 0, 0);
+  };
+  const int rounds = K / (64 * U);
+  int i = wave;
+  if (i < rounds) load(0, i * 64 * U);
+  for (; i < rounds; i += 2 * W) {
+    if (i + W < rounds) load(1, (i + W) * 64 * U);
+    products(0);
+    if (i + W < rounds) {
+      if (i + 2 * W < rounds) load(0, (i + 2 * W) * 64 * U);
+      products(1);
     }
   }
-  return v;
-}
-
-// One workgroup: 16 output columns and 16 rows, the sum split over 4 wavefronts.
-template <typename TO>
-__global__ __launch_bounds__(256) void k_matmul_i8_rows(LinearArgs a) {
-  __shared__ i32x4 part[4][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t n0 = (int64_t)blockIdx.x * 16, m0 = (int64_t)blockIdx.y * 16;
-  const int r = lane & 15, g = lane >> 4;
-  i32x4 acc = {0, 0, 0, 0};
-  for (int64_t k = (int64_t)wave * 64; k < a.K; k += 256) {
-    const i32x4 w = load_chunk(a.B, a.ldb, n0 + r, a.N, k + 16 * g, a.K);
-    const i32x4 x = load_chunk(a.A, a.lda, m0 + r, a.M, k + 16 * g, a.K);
-    acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(w, x, acc, 0, 0, 0);
+  if (wave == W - 1) {  // the rest of the sum, zeros past K on the weights' side
+    for (int k = rounds * 64 * U; k < K; k += 64) {
+      const int left = K - (k + 16 * g);
+      i32x4 w = {0, 0, 0, 0}, x = w;
+      if (left > 0) {
+        w = *reinterpret_cast<const i32x4*>(pb + k);
+        x = *reinterpret_cast<const i32x4*>(pa + k);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int n = left - 4 * e;  // bytes of this word that belong to the sum
+        if (n < 4) w[e] = n <= 0 ? 0 : w[e] & (int)((1u << (8 * n)) - 1u);
+      }
+      acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(w, x, acc, 0, 0, 0);
+    }
   }
   part[wave][lane] = acc;
   __syncthreads();
-  if (wave) return;
+  const int64_t m = r, n = n0 + 4 * g;
+  if (wave || m >= a.M) return;
 #pragma unroll
-  for (int w = 1; w < 4; ++w) acc += part[w][lane];
-  const int64_t m = m0 + r, n = n0 + 4 * g;
-  if (m >= a.M) return;
+  for (int w = 1; w < W; ++w) acc += part[w][lane];
   const float sa = a.a_scale[m];
   float y[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int64_t nn = n + i < a.N ? n + i : a.N - 1;
-    y[i] = (float)acc[i] * (sa * a.b_scale[nn]);
-    if (a.bias) y[i] += a.bias[nn];
+  for (int e = 0; e < 4; ++e) {
+    const int64_t nn = n + e < a.N ? n + e : a.N - 1;
+    y[e] = (float)acc[e] * (sa * a.b_scale[nn]);
+    if (a.bias) y[e] += a.bias[nn];
   }
   TO* o = static_cast<TO*>(a.out) + m * a.ldo;
   store4(o, y, n, a.N, ((reinterpret_cast<uintptr_t>(a.out) | (uintptr_t)(a.ldo * sizeof(TO))) & (4 * sizeof(TO) - 1)) == 0);
@@ -101,6 +125,12 @@ constexpr int kStep = 128;
 __device__ __forceinline__ int key_a(int row) { return row & 7; }
 __device__ __forceinline__ int key_b(int row) { return (row & 3) | ((row >> 2) & 4); }
 
+// A barrier for LDS contents alone: __syncthreads() would also wait for every
+// fill that is still to come.
+__device__ __forceinline__ void sync_lds() {
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
 template <int BM, int BN, int WM, int WN>
 struct TileShape {
   static constexpr int kWaves = (BM / WM) * (BN / WN);
@@ -108,13 +138,16 @@ struct TileShape {
   static constexpr int kStage = (BM + BN) * kStep;
 };
 
-template <int BM, int BN, int WM, int WN, int OCC, typename TO>
+template <int BM, int BN, int WM, int WN, int OCC, int NS, typename TO>
 __global__ __launch_bounds__((TileShape<BM, BN, WM, WN>::kThreads), OCC) void k_matmul_i8_tile(LinearArgs a, int tiles_m,
-                                                                                               int tiles_n) {
+                                                                                               int tiles_n,
+                                                                                               int split_steps,
+                                                                                               int32_t* parts) {
   using S = TileShape<BM, BN, WM, WN>;
   constexpr int TM = WM / 32, TN = WN / 32;
   constexpr int NA = BM * 8 / S::kThreads, NB = BN * 8 / S::kThreads;  // 16-byte pieces per thread and step
   constexpr int kRows = S::kThreads / 8;                              // rows that one round of fills covers
+  static_assert(kRows == 16 || kRows % 32 == 0, "keys of a round of fills");
   extern __shared__ __attribute__((aligned(1024))) char lds[];
 
   // neighbouring tiles on one XCD, in bands of 8 tile rows, share operands in its L2
@@ -140,20 +173,27 @@ __global__ __launch_bounds__((TileShape<BM, BN, WM, WN>::kThreads), OCC) void k_
   // fills: thread -> LDS row tid / 8 (+ kRows per round), place tid % 8
   const int frow = tid >> 3;
   const int pa = ((tid & 7) ^ key_a(frow)) * 16, pb = ((tid & 7) ^ key_b(frow)) * 16;
-  const uint32_t oa = (uint32_t)frow * (uint32_t)a.lda + pa, ob = (uint32_t)frow * (uint32_t)a.ldb + pb;
+  const uint32_t oa = (uint32_t)frow * (uint32_t)a.lda + pa, ob = (uint32_t)frow * (uint32_t)a.ldb;
   const uint32_t sa = kRows * (uint32_t)a.lda, sb = kRows * (uint32_t)a.ldb;
   typedef __attribute__((address_space(3))) void* lds_ptr;
-  auto fill = [&](int stage, int k) {
+  const int first = (int)blockIdx.y * split_steps;  // this workgroup's steps of the sum
+  const int all = (K + kStep - 1) / kStep;
+  const int steps = all - first < split_steps ? all - first : split_steps;
+  auto fill = [&](int stage, int t) {
+    const int k = t < steps ? (first + t) * kStep : K;
     char* base = lds + stage * S::kStage + wave * 1024;
-    const bool ina = k + pa < K, inb = k + pb < K;
+    const bool ina = k + pa < K;
 #pragma unroll
     for (int i = 0; i < NA; ++i)
       __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_ptr)(base + i * kRows * kStep), 16,
                                                ina ? (int)(oa + i * sa + k) : (int)0x80000000, 0, 0, 0);
 #pragma unroll
-    for (int i = 0; i < NB; ++i)
+    for (int i = 0; i < NB; ++i) {
+      // rows 16 on have bit 2 of the key flipped
+      const int p = kRows == 16 && (i & 1) ? pb ^ 64 : pb;
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_ptr)(base + (BM + i * kRows) * kStep), 16,
-                                               inb ? (int)(ob + i * sb + k) : (int)0x80000000, 0, 0, 0);
+                                               k + p < K ? (int)(ob + i * sb + p + k) : (int)0x80000000, 0, 0, 0);
+    }
   };
   // fragments: lane -> row lane % 32 of the tile, 16-byte piece 2 ks + lane / 32
   const int half = lane >> 5, r = lane & 31;
@@ -183,42 +223,69 @@ __global__ __launch_bounds__((TileShape<BM, BN, WM, WN>::kThreads), OCC) void k_
       for (int j = 0; j < TM; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fb[i], fa[j], acc[i][j], 0, 0, 0);
   };
 
-  const int steps = (K + kStep - 1) / kStep;
-  // waits for this wavefront's fills, then for everyone's; clears what lies past K in A's rows of the last step
-  auto arrived = [&](int stage, int t) {
-    __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
-    __syncthreads();                     // (with lgkmcnt(0): every fragment of the stage that is refilled next is read)
-    if (t == steps - 1 && K != K16) {
-      const int k = K - (K16 - 16), p = (K16 - 16 - t * kStep) >> 4;
+  // waits until step t's fills are in, this wavefront's and then everyone's (LATER fills follow them); clears what lies
+  // past K in A's rows of the last step
+  auto arrived = [&](auto later, int stage, int t) {
+    constexpr int n = decltype(later)::value * (NA + NB);
+    static_assert(n < 64, "vmcnt");
+    __builtin_amdgcn_s_waitcnt(0x0F70 | (n & 15) | (n >> 4) << 14);  // vmcnt(n)
+    sync_lds();                                                    // (every fragment of the stage that is refilled next is read)
+    if (first + t == all - 1 && K != K16) {
+      const int k = K - (K16 - 16), p = (K16 - 16 - (first + t) * kStep) >> 4;
       for (int row = tid; row < BM; row += S::kThreads) {
         char* c = lds + stage * S::kStage + row * kStep + (p ^ key_a(row)) * 16;
         for (int e = k; e < 16; ++e) c[e] = 0;
       }
-      __syncthreads();
+      sync_lds();
     }
   };
 
+  // fills past the last step come from beyond the resources: they keep the counts and read nothing
   i32x4 fa[2][TM], fb[2][TN];
-  fill(0, 0);
-  arrived(0, 0);
-  if (steps > 1) fill(1, kStep);
+#pragma unroll
+  for (int t = 0; t < NS; ++t) fill(t, t);
+  arrived(std::integral_constant<int, NS - 1>{}, 0, 0);
   frags(0, 0, fa[0], fb[0]);
+  int st = 0;
   for (int t = 0; t < steps; ++t) {
-    const int st = t & 1;
 #pragma unroll
     for (int ks = 0; ks < 3; ++ks) {
       frags(st, ks + 1, fa[(ks + 1) & 1], fb[(ks + 1) & 1]);
       products(fa[ks & 1], fb[ks & 1]);
     }
+    const int next = st + 1 == NS ? 0 : st + 1;
     if (t + 1 < steps) {
-      arrived(st ^ 1, t + 1);
-      if (t + 2 < steps) fill(st, (t + 2) * kStep);
-      frags(st ^ 1, 0, fa[0], fb[0]);
+      arrived(std::integral_constant<int, NS - 2>{}, next, t + 1);
+      fill(st, t + NS);
+      frags(next, 0, fa[0], fb[0]);
     }
     products(fa[1], fb[1]);
+    st = next;
   }
+  __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): no fill outlives the workgroup
 
   // results: lane -> row wm + 32 j + r, columns wn + 32 i + 16 half + e
+  if (parts) {  // a part of the sum, for k_matmul_i8_join
+    int32_t* o = parts + (int64_t)blockIdx.y * a.M * a.N;
+#pragma unroll
+    for (int i = 0; i < TN; ++i)
+#pragma unroll
+      for (int j = 0; j < TM; ++j) {
+        const int64_t m = m0 + wm + 32 * j + r, n = n0 + wn + 32 * i + 16 * half;
+        if (m >= a.M) continue;
+        if (n + 16 <= a.N && (a.N & 3) == 0) {
+#pragma unroll
+          for (int e = 0; e < 16; e += 4)
+            *reinterpret_cast<i32x4*>(o + m * a.N + n + e) =
+                i32x4{acc[i][j][e], acc[i][j][e + 1], acc[i][j][e + 2], acc[i][j][e + 3]};
+        } else {
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (n + e < a.N) o[m * a.N + n + e] = acc[i][j][e];
+        }
+      }
+    return;
+  }
   const bool wide = ((reinterpret_cast<uintptr_t>(a.out) | (uintptr_t)(a.ldo * sizeof(TO))) & 15) == 0;
 #pragma unroll
   for (int i = 0; i < TN; ++i) {
@@ -258,42 +325,119 @@ __global__ __launch_bounds__((TileShape<BM, BN, WM, WN>::kThreads), OCC) void k_
   }
 }
 
-template <int BM, int BN, int WM, int WN, int OCC, typename TO>
-hipError_t launch_tile(const LinearArgs& a, hipStream_t st) {
+// The parts of split sums together, with the epilogue; four columns a thread.
+template <typename TO>
+__global__ __launch_bounds__(256) void k_matmul_i8_join(LinearArgs a, const int32_t* __restrict__ parts, int n_parts) {
+  const int64_t quads = (a.N + 3) / 4;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= quads * a.M) return;
+  const int64_t m = i / quads, n = (i - m * quads) * 4;
+  int sum[4] = {0, 0, 0, 0};
+  for (int p = 0; p < n_parts; ++p) {
+    const int32_t* s = parts + ((int64_t)p * a.M + m) * a.N + n;
+    if ((a.N & 3) == 0) {
+      const i32x4 v = *reinterpret_cast<const i32x4*>(s);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[e] += v[e];
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[e] += n + e < a.N ? s[e] : 0;
+    }
+  }
+  const float sa = a.a_scale[m];
+  float y[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int64_t nn = n + e < a.N ? n + e : a.N - 1;
+    y[e] = (float)sum[e] * (sa * a.b_scale[nn]);
+    if (a.bias) y[e] += a.bias[nn];
+  }
+  TO* o = static_cast<TO*>(a.out) + m * a.ldo;
+  store4(o, y, n, a.N, ((reinterpret_cast<uintptr_t>(a.out) | (uintptr_t)(a.ldo * sizeof(TO))) & (4 * sizeof(TO) - 1)) == 0);
+}
+
+template <int BM, int BN, int WM, int WN, int OCC, int NS, typename TO>
+hipError_t launch_tile(const LinearArgs& a, int split, void* ws, hipStream_t st) {
   using S = TileShape<BM, BN, WM, WN>;
-  const auto k = k_matmul_i8_tile<BM, BN, WM, WN, OCC, TO>;
-  const size_t lds = 2 * S::kStage;
+  const auto k = k_matmul_i8_tile<BM, BN, WM, WN, OCC, NS, TO>;
+  const size_t lds = NS * S::kStage;
   if (lds > 65536) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (e != hipSuccess) return e;
   }
   const int64_t tm = (a.M + BM - 1) / BM, tn = (a.N + BN - 1) / BN;
   if (tm * tn > 0x7FFFFFFF / 8) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(k, dim3((unsigned)(tm * tn)), dim3(S::kThreads), lds, st, a, (int)tm, (int)tn);
+  const int all = (int)((a.K + kStep - 1) / kStep), per = (all + split - 1) / split;
+  split = (all + per - 1) / per;
+  int32_t* parts = split > 1 ? static_cast<int32_t*>(ws) : nullptr;
+  hipLaunchKernelGGL(k, dim3((unsigned)(tm * tn), (unsigned)split), dim3(S::kThreads), lds, st, a, (int)tm, (int)tn, per, parts);
+  if (parts) {
+    const int64_t quads = a.M * ((a.N + 3) / 4);
+    hipLaunchKernelGGL((k_matmul_i8_join<TO>), dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, st, a, parts, split);
+  }
   return hipGetLastError();
 }
 
-template <typename TO>
-hipError_t launch(const LinearArgs& a, hipStream_t st) {
-  const int64_t t256 = ((a.M + 255) / 256) * ((a.N + 255) / 256), t128 = ((a.M + 127) / 128) * ((a.N + 127) / 128);
-  if (a.M > 64) {
-    if (t256 >= 192) return launch_tile<256, 256, 128, 128, 1, TO>(a, st);
-    if (t128 >= 192) return launch_tile<128, 128, 64, 64, 2, TO>(a, st);
-    return launch_tile<64, 64, 32, 32, 4, TO>(a, st);
-  }
-  hipLaunchKernelGGL((k_matmul_i8_rows<TO>), dim3((unsigned)((a.N + 15) / 16), (unsigned)((a.M + 15) / 16)), dim3(256),
-                     0, st, a);
+template <int W, int U, typename TO>
+hipError_t launch_rows(const LinearArgs& a, hipStream_t st) {
+  hipLaunchKernelGGL((k_matmul_i8_rows<W, U, TO>), dim3((unsigned)((a.N + 15) / 16)), dim3(64 * W), 0, st, a);
   return hipGetLastError();
+}
+
+// Which kernel takes a product, and over how many parts of the sum.  Times below
+// are of whole calls in us on weights that are not in the caches.
+enum Path { kRows, kTile32, kTile64, kTile64Wide, kTile128, kTile256 };
+struct Choice {
+  Path path;
+  int split;
+};
+Choice choose(int64_t M, int64_t N, int64_t K) {
+  const auto tiles = [&](int64_t bm, int64_t bn) { return ((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
+  // Up to 16 rows: 16 columns a workgroup while that leaves at most two of them a
+  // CU (13 x 2048 x 11008: 11.3 against 26.5 through LDS tiles); with more the
+  // activations' reads, as many bytes as the weights', cost more than tiles do
+  // (16 x 11008 x 2048: 10.5 against 8.2; 16 x 27648 x 5120: 44 against 30).
+  if (M <= 16 && N < 8192) return {kRows, 1};
+  // Four tiles of 128 cost as much time as 1.07 of a 256 tile's, which also
+  // comes in whole rounds of one per CU (512 x 27648 x 5120: 115 and 102;
+  // 2048 x 5120 x 5120: 75 and 87; 8192 x 27648 x 5120: 1317 and 1260).
+  const int64_t t128 = tiles(128, 128), t256 = tiles(256, 256);
+  if (M > 64 && t128 >= 256) return {3.7 * ((t256 + 255) / 256) < t128 / 256.0 + 0.5 ? kTile256 : kTile128, 1};
+  // 64 x 27648 x 5120: 64 x 64 tiles 40.8, 64 x 128 tiles 37.4 (64 x 11008 x 2048: 8.8 and 10.9)
+  if (M > 32 && tiles(64, 128) >= 192) return {kTile64Wide, 1};
+  const Path path = M > 32 ? kTile64 : kTile32;
+  // Few tiles under a long sum: parts of at least 16 steps, joined by a second
+  // launch (64 x 2048 x 11008: 28 whole, 14.3 in 5 parts; 64 x 2560 x 2048: 7.8 whole, 8.9 in 4)
+  const int64_t t = path == kTile64 ? tiles(64, 64) : tiles(32, 64);
+  const int64_t want = (256 + t - 1) / t, most = (K + kStep - 1) / kStep / 16;
+  const int64_t split = want < most ? want : most;
+  return {path, t < 128 && split > 1 ? (int)split : 1};
+}
+
+template <typename TO>
+hipError_t launch(const LinearArgs& a, void* ws, hipStream_t st) {
+  const Choice c = choose(a.M, a.N, a.K);
+  switch (c.path) {
+    case kRows: return launch_rows<8, 4, TO>(a, st);
+    case kTile32: return launch_tile<32, 64, 32, 32, 2, 4, TO>(a, c.split, ws, st);
+    case kTile64: return launch_tile<64, 64, 32, 32, 3, 3, TO>(a, c.split, ws, st);
+    case kTile64Wide: return launch_tile<64, 128, 32, 64, 2, 3, TO>(a, 1, ws, st);
+    case kTile128: return launch_tile<128, 128, 64, 64, 2, 2, TO>(a, 1, ws, st);
+    default: return launch_tile<256, 256, 128, 128, 1, 2, TO>(a, 1, ws, st);
+  }
 }
 
 }  // namespace
 
-size_t matmul_i8_ws_bytes(int64_t, int64_t, int64_t) { return 0; }
+size_t matmul_i8_ws_bytes(int64_t M, int64_t N, int64_t K) {
+  const int split = choose(M, N, K).split;
+  return split > 1 ? (size_t)split * (size_t)M * (size_t)N * 4 : 0;
+}
 
-hipError_t launch_matmul_i8(const LinearArgs& a, void*, hipStream_t st) {
-  if (a.out_dtype == AWSRC_DTYPE_F32) return launch<float>(a, st);
-  if (a.out_dtype == AWSRC_DTYPE_BF16) return launch<__bf16>(a, st);
-  return launch<_Float16>(a, st);
+hipError_t launch_matmul_i8(const LinearArgs& a, void* ws, hipStream_t st) {
+  if (a.out_dtype == AWSRC_DTYPE_F32) return launch<float>(a, ws, st);
+  if (a.out_dtype == AWSRC_DTYPE_BF16) return launch<__bf16>(a, ws, st);
+  return launch<_Float16>(a, ws, st);
 }
 
 }  // namespace awsrc

@@ -10,36 +10,147 @@ namespace awsrc {
 
 namespace {
 
+// Eight values from x, of which n exist (the others are 0).
 template <typename T>
-__global__ __launch_bounds__(256) void k_quantize_rows(const T* __restrict__ X, int64_t cols, int64_t ldx,
-                                                       int8_t* __restrict__ codes, int64_t ldc, int64_t pad,
-                                                       float* __restrict__ scale) {
-  __shared__ float part[4];
-  const int64_t row = blockIdx.x;
+__device__ __forceinline__ void load8(const T* __restrict__ x, int64_t n, bool wide, float (&v)[8]) {
+  if (wide && n >= 8) {
+    struct alignas(16) Piece { T v[16 / sizeof(T)]; };
+    constexpr int V = 16 / sizeof(T);
+#pragma unroll
+    for (int p = 0; p < 8 / V; ++p) {
+      const Piece w = reinterpret_cast<const Piece*>(x)[p];
+#pragma unroll
+      for (int e = 0; e < V; ++e) v[p * V + e] = to_f32(w.v[e]);
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = e < n ? to_f32(x[e]) : 0.0f;
+  }
+}
+
+// Codes of eight values; `live` is false for a row whose scale is NaN.  No
+// clamp: |x| <= amax gives |x inv| <= 127 (1 + 2^-22).
+__device__ __forceinline__ uint2 codes8(const float (&v)[8], float inv, bool live) {
+  uint32_t q[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) q[e] = live ? (uint32_t)(int)rintf(v[e] * inv) : 0u;
+  uint2 o;
+  o.x = (q[0] & 255) | (q[1] & 255) << 8 | (q[2] & 255) << 16 | q[3] << 24;
+  o.y = (q[4] & 255) | (q[5] & 255) << 8 | (q[6] & 255) << 16 | q[7] << 24;
+  return o;
+}
+
+__device__ __forceinline__ void store8(int8_t* __restrict__ c, uint2 w, int64_t n, bool wide) {
+  if (wide && n >= 8) {
+    *reinterpret_cast<uint2*>(c) = w;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < n) c[e] = (int8_t)((e < 4 ? w.x : w.y) >> (8 * (e & 3)));
+  }
+}
+
+// WPR wavefronts per row, CH pieces of 8 values per lane in registers, so
+// that a row is read once; WPR = 1 takes four rows per workgroup.
+template <typename T, int WPR, int CH>
+__global__ __launch_bounds__(64 * (WPR == 1 ? 4 : WPR)) void k_quantize_rows(const T* __restrict__ X, int64_t rows, int64_t cols,
+                                                                             int64_t ldx, int8_t* __restrict__ codes,
+                                                                             int64_t ldc, int64_t pad, float* __restrict__ scale,
+                                                                             bool wide_x, bool wide_c) {
+  __shared__ float part[WPR];
+  const int wave = threadIdx.x >> 6;
+  const int64_t row = WPR == 1 ? (int64_t)blockIdx.x * 4 + wave : blockIdx.x;
+  if (row >= rows) return;
+  const int t = WPR == 1 ? (threadIdx.x & 63) : threadIdx.x;
   const T* x = X + row * ldx;
-  int8_t* c = codes + row * ldc;
+  float v[CH][8];
   float m = 0.0f;
-  for (int64_t i = threadIdx.x; i < cols; i += 256) m = amax_keep(m, to_f32(x[i]));
+#pragma unroll
+  for (int i = 0; i < CH; ++i) {
+    const int64_t at = (int64_t)(i * WPR * 64 + t) * 8;
+    load8(x + at, cols - at, wide_x, v[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < CH; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) m = amax_keep(m, v[i][e]);
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) m = amax_keep(m, __shfl_xor(m, off, 64));
+  if constexpr (WPR > 1) {
+    if ((t & 63) == 0) part[wave] = m;
+    __syncthreads();
+    m = part[0];
+#pragma unroll
+    for (int w = 1; w < WPR; ++w) m = amax_keep(m, part[w]);
+  }
+  const float s = scale_of_amax(m);
+  const float inv = inverse_scale(s);
+  const bool live = s == s;
+  int8_t* c = codes + row * ldc;
+#pragma unroll
+  for (int i = 0; i < CH; ++i) {
+    const int64_t at = (int64_t)(i * WPR * 64 + t) * 8;
+    if (at < pad) store8(c + at, codes8(v[i], inv, live), pad - at, wide_c);
+  }
+  if (t == 0) scale[row] = s;
+}
+
+// Rows longer than the registers take: read twice, the second time mostly from the caches.
+template <typename T>
+__global__ __launch_bounds__(1024) void k_quantize_long_rows(const T* __restrict__ X, int64_t cols, int64_t ldx,
+                                                             int8_t* __restrict__ codes, int64_t ldc, int64_t pad,
+                                                             float* __restrict__ scale, bool wide_x, bool wide_c) {
+  __shared__ float part[16];
+  const T* x = X + (int64_t)blockIdx.x * ldx;
+  int8_t* c = codes + (int64_t)blockIdx.x * ldc;
+  float m = 0.0f;
+  for (int64_t at = (int64_t)threadIdx.x * 8; at < cols; at += 8192) {
+    float v[8];
+    load8(x + at, cols - at, wide_x, v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) m = amax_keep(m, v[e]);
+  }
 #pragma unroll
   for (int off = 32; off >= 1; off >>= 1) m = amax_keep(m, __shfl_xor(m, off, 64));
   if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = m;
   __syncthreads();
   m = part[0];
 #pragma unroll
-  for (int w = 1; w < 4; ++w) m = amax_keep(m, part[w]);
+  for (int w = 1; w < 16; ++w) m = amax_keep(m, part[w]);
   const float s = scale_of_amax(m);
   const float inv = inverse_scale(s);
-  for (int64_t i = threadIdx.x; i < pad; i += 256) c[i] = i < cols ? (int8_t)code_of(to_f32(x[i]), inv) : (int8_t)0;
-  if (threadIdx.x == 0) scale[row] = s;
+  for (int64_t at = (int64_t)threadIdx.x * 8; at < pad; at += 8192) {
+    float v[8];
+    load8(x + at, cols - at, wide_x, v);
+    store8(c + at, codes8(v, inv, s == s), pad - at, wide_c);
+  }
+  if (threadIdx.x == 0) scale[blockIdx.x] = s;
 }
 
 template <typename T>
 hipError_t launch(const void* X, int64_t rows, int64_t cols, int64_t ldx, int8_t* codes, int64_t ldc, float* scale,
                   hipStream_t st) {
+  const T* x = static_cast<const T*>(X);
   int64_t pad = (cols + 15) / 16 * 16;
   if (pad > ldc) pad = ldc;
-  hipLaunchKernelGGL((k_quantize_rows<T>), dim3((unsigned)rows), dim3(256), 0, st, static_cast<const T*>(X), cols, ldx,
-                     codes, ldc, pad, scale);
+  const bool wx = ((reinterpret_cast<uintptr_t>(X) | (uintptr_t)(ldx * sizeof(T))) & 15) == 0;
+  const bool wc = ((reinterpret_cast<uintptr_t>(codes) | (uintptr_t)ldc) & 7) == 0;
+#define AWSRC_ROWS(WPR, CH)                                                                                            \
+  hipLaunchKernelGGL((k_quantize_rows<T, WPR, CH>), dim3((unsigned)(WPR == 1 ? (rows + 3) / 4 : rows)),                \
+                     dim3(64 * (WPR == 1 ? 4 : WPR)), 0, st, x, rows, cols, ldx, codes, ldc, pad, scale, wx, wc)
+  // One wavefront a row where there are rows enough to fill the machine and a
+  // row fits its registers; else as many as leave each lane one or two pieces,
+  // since a call of few rows waits for memory, not on bandwidth.
+  if (cols <= 512) AWSRC_ROWS(1, 1);
+  else if (rows >= 2048 && cols <= 2048) AWSRC_ROWS(1, 4);
+  else if (cols <= 2048) AWSRC_ROWS(4, 1);
+  else if (rows >= 1024 && cols <= 8192) AWSRC_ROWS(4, 4);
+  else if (cols <= 8192) AWSRC_ROWS(16, 1);
+  else if (cols <= 16384) AWSRC_ROWS(16, 2);
+  else
+    hipLaunchKernelGGL((k_quantize_long_rows<T>), dim3((unsigned)rows), dim3(1024), 0, st, x, cols, ldx, codes, ldc, pad,
+                       scale, wx, wc);
+#undef AWSRC_ROWS
   return hipGetLastError();
 }
 

@@ -123,7 +123,8 @@ def _check_product(out, a, sa, b, sb, bias, dtype):
 
 SHAPES = [(1, 1, 1), (1, 16, 16), (1, 2560, 2048), (2, 17, 33), (3, 100, 1000), (13, 96, 4100), (16, 64, 64), (17, 130, 127),
           (31, 48, 272), (33, 256, 128), (64, 300, 513), (65, 65, 65), (100, 257, 1040), (128, 128, 128), (129, 127, 2000),
-          (255, 513, 96), (256, 256, 256), (300, 1003, 1337), (511, 260, 144), (1, 33, 131071), (70, 40, 20000)]
+          (255, 513, 96), (256, 256, 256), (300, 1003, 1337), (511, 260, 144), (1, 33, 131071), (70, 40, 20000),
+          (5, 8200, 300), (30, 200, 9000), (50, 130, 5003), (64, 9001, 513), (40, 24700, 144), (129, 16640, 260), (90, 100, 12289)]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
