@@ -10,6 +10,7 @@ not been built (python paper_2608_23144_amd/build.py).
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Dict, List, Optional, Sequence, Tuple
 
@@ -524,46 +525,59 @@ def awsrc_reconstruct_bf16_sdq(plan: awsrc_decode_plan,
 
 
 # ------------------------------------------------------------------ 8-bit serving
+# These calls are made many times per token: what they check of their arguments
+# is kept to cheap attribute reads, sizes that depend on shapes alone are remembered.
 KVCache = Tuple[torch.Tensor, torch.Tensor, torch.Tensor, torch.Tensor]  # codes of keys and values, their scales
 
 _ACT_CODE = {torch.float32: AWSRC_DTYPE_F32, torch.bfloat16: AWSRC_DTYPE_BF16, torch.float16: AWSRC_DTYPE_F16}
+_WS_SIZES = 4096  # shapes whose workspace sizes are remembered
 
 
 def _act_code(dtype: torch.dtype) -> int:
-    try:
-        return _ACT_CODE[dtype]
-    except KeyError:
-        raise TypeError(f"unsupported dtype {dtype}") from None
+    code = _ACT_CODE.get(dtype)
+    if code is None:
+        raise TypeError(f"unsupported dtype {dtype}")
+    return code
 
 
-def _on_device(dev: torch.device, *ts: Optional[torch.Tensor]) -> None:
+def _device_of(t: torch.Tensor) -> int:
+    i = t.get_device()
+    if i < 0:
+        raise ValueError("tensors must be device tensors")
+    return i
+
+
+def _on_device(i: int, *ts: Optional[torch.Tensor]) -> None:
     for t in ts:
-        if t is not None and (not t.is_cuda or t.device != dev):
-            raise ValueError(f"tensors must be on one device: {t.device} and {dev}")
+        if t is not None and t.get_device() != i:
+            raise ValueError(f"tensors must be on one device: {t.device} and cuda:{i}")
 
 
-def _empty(shape, dtype, dev, stream):
+def _empty(shape, like: torch.Tensor, dtype, stream):
     """A new tensor whose memory belongs to the stream that will use it."""
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=dev)
+        return torch.empty(shape, dtype=dtype, device=like.device)
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=dev)
+        return torch.empty(shape, dtype=dtype, device=like.device)
 
 
-def _raw_stream(dev: torch.device, stream) -> int:
+def _raw_stream(i: int, stream) -> int:
     if stream is None:
-        return torch.cuda.current_stream(dev).cuda_stream
-    if stream.device != dev:
-        raise ValueError(f"stream on {stream.device}, tensors on {dev}")
+        return torch._C._cuda_getCurrentRawStream(i)
+    if stream.device_index != i:
+        raise ValueError(f"stream on {stream.device}, tensors on cuda:{i}")
     return stream.cuda_stream
 
 
 def _rows_of(t: torch.Tensor, what: str):
     """(rows, cols, row stride) of a matrix whose rows are contiguous."""
-    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
-        raise ValueError(f"{what} must be a matrix with contiguous rows")
+    if t.dim() != 2:
+        raise ValueError(f"{what} must be a matrix")
     rows, cols = t.shape
-    return rows, cols, t.stride(0) if rows > 1 else max(cols, t.stride(0))
+    ld, step = t.stride()
+    if step != 1 and cols > 1:
+        raise ValueError(f"{what} must be a matrix with contiguous rows")
+    return rows, cols, ld if rows > 1 else max(cols, ld)
 
 
 def _i8_rows(t: torch.Tensor, what: str):
@@ -571,22 +585,29 @@ def _i8_rows(t: torch.Tensor, what: str):
     rows, cols, ld = _rows_of(t, what)
     if t.dtype != torch.int8:
         raise TypeError(f"{what} must be int8, not {t.dtype}")
-    if rows == 1:
-        ld = max(ld, -(-cols // 16) * 16) if ld % 16 == 0 else -(-cols // 16) * 16
-    if rows and cols % 16 and t.untyped_storage().nbytes() < t.storage_offset() + (rows - 1) * ld + -(-cols // 16) * 16:
+    if cols % 16 == 0:
+        return rows, cols, ld if rows > 1 or ld % 16 == 0 else cols
+    wide = -(-cols // 16) * 16
+    if rows <= 1:
+        ld = max(ld, wide) if ld % 16 == 0 else wide
+    if rows and t.untyped_storage().nbytes() < t.storage_offset() + (rows - 1) * ld + wide:
         raise ValueError(f"{what}: the last row must be readable up to a multiple of 16 bytes")
     return rows, cols, ld
 
 
 def _heads_of(t: torch.Tensor, what: str, heads: Optional[int], dim: int, dtype: torch.dtype):
-    """Row stride of a [rows, heads, dim] tensor whose heads lie side by side."""
-    if t.dim() != 3 or t.shape[2] != dim or (heads is not None and t.shape[1] != heads):
+    """(rows, heads, row stride) of a [rows, heads, dim] tensor whose heads lie side by side."""
+    if t.dim() != 3:
+        raise ValueError(f"{what}: expected [rows, heads, {dim}]")
+    n, h, d = t.shape
+    if d != dim or (heads is not None and h != heads):
         raise ValueError(f"{what}: expected [rows, {heads if heads else 'heads'}, {dim}], got {tuple(t.shape)}")
     if t.dtype != dtype:
         raise TypeError(f"{what}: expected {dtype}, got {t.dtype}")
-    if t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != dim):
+    ld, sh, sd = t.stride()
+    if sd != 1 or (sh != dim and h > 1):
         raise ValueError(f"{what}: the heads of a row must lie side by side")
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * dim
+    return n, h, ld if n > 1 else h * dim
 
 
 def make_kv_cache(n_pages: int, kv_heads: int, head_dim: int, page_tokens: int = 64, device="cuda") -> KVCache:
@@ -598,51 +619,54 @@ def make_kv_cache(n_pages: int, kv_heads: int, head_dim: int, page_tokens: int =
             torch.empty(n_pages, kv_heads, dtype=torch.float32, device=device))
 
 
-def _cache_of(cache: KVCache) -> awsrc_kv_cache:
+def _cache_of(cache: KVCache):
+    """(the C description, kv_heads, head_dim, page_tokens, device index)"""
     k, v, ks, vs = cache
     n, h, p, d = k.shape
     if v.shape != (n, h, d, p) or ks.shape != (n, h) or vs.shape != (n, h):
         raise ValueError("cache: k [pages, heads, tokens, dim], v [pages, heads, dim, tokens], scales [pages, heads]")
     if k.dtype != torch.int8 or v.dtype != torch.int8 or ks.dtype != torch.float32 or vs.dtype != torch.float32:
         raise TypeError("cache: int8 codes and fp32 scales")
-    _dev(k, v, ks, vs)
-    _on_device(k.device, v, ks, vs)
-    return awsrc_kv_cache(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), n, h, d, p, 0)
+    if not (k.is_contiguous() and v.is_contiguous() and ks.is_contiguous() and vs.is_contiguous()):
+        raise ValueError("cache tensors must be contiguous")
+    dev = _device_of(k)
+    _on_device(dev, v, ks, vs)
+    return awsrc_kv_cache(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), n, h, d, p, 0), h, d, p, dev
 
 
-def _batch_of(dev, cu, kv_len, page_table):
+def _batch_of(dev: int, cu, kv_len, page_table):
     """(sequences, table stride) of a batch's int32 device tensors."""
-    for t in (cu, kv_len, page_table):
-        if t.dtype != torch.int32:
-            raise TypeError("cu, kv_len and page_table must be int32")
+    if cu.dtype != torch.int32 or kv_len.dtype != torch.int32 or page_table.dtype != torch.int32:
+        raise TypeError("cu, kv_len and page_table must be int32")
     _on_device(dev, cu, kv_len, page_table)
-    n = kv_len.shape[0]
-    if cu.shape != (n + 1,) or page_table.dim() != 2 or page_table.shape[0] != n:
+    if page_table.dim() != 2:
+        raise ValueError("page_table [sequences, pages]")
+    n, ld = page_table.shape
+    if cu.shape != (n + 1,) or kv_len.shape != (n,):
         raise ValueError("cu [sequences + 1], kv_len [sequences], page_table [sequences, pages]")
     if not (cu.is_contiguous() and kv_len.is_contiguous() and page_table.is_contiguous()):
         raise ValueError("cu, kv_len and page_table must be contiguous")
-    return n, page_table.shape[1]
+    return n, ld
 
 
 def awsrc_quantize_rows_i8(x: torch.Tensor, out=None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """int8 codes [rows, cols] and fp32 scales [rows] of a matrix (activations per token, weights per output channel).
     The codes' rows lie a multiple of 16 bytes apart, as awsrc_matmul_i8 and awsrc_linear_i8 take them."""
     rows, cols, ld = _rows_of(x, "x")
-    dev = x.device
-    _on_device(dev, x)
+    dev = _device_of(x)
     if out is None:
-        out = (_empty((rows, -(-cols // 16) * 16), torch.int8, dev, stream)[:, :cols],
-               _empty((rows,), torch.float32, dev, stream))
+        out = (_empty((rows, -(-cols // 16) * 16), x, torch.int8, stream)[:, :cols], _empty((rows,), x, torch.float32, stream))
     codes, scale = out
     _on_device(dev, codes, scale)
-    if codes.shape != x.shape or codes.dtype != torch.int8 or scale.shape != (rows,) or scale.dtype != torch.float32 or not scale.is_contiguous():
+    if (codes.shape != x.shape or codes.dtype != torch.int8 or scale.shape != (rows,) or scale.dtype != torch.float32
+            or not scale.is_contiguous()):
         raise ValueError("out: int8 codes of x's shape and fp32 scales [rows]")
     _check(LIB.awsrc_quantize_rows_i8(x.data_ptr(), _act_code(x.dtype), rows, cols, ld, codes.data_ptr(),
                                       _rows_of(codes, "codes")[2], scale.data_ptr(), _raw_stream(dev, stream)))
     return codes, scale
 
 
-def _check_product_args(dev, N, scale, bias, out, M):
+def _check_product_args(dev: int, N: int, scale, bias, out, M: int):
     _on_device(dev, scale, bias, out)
     if scale.shape != (N,) or scale.dtype != torch.float32 or not scale.is_contiguous():
         raise ValueError("weight scales: fp32 [N]")
@@ -650,6 +674,33 @@ def _check_product_args(dev, N, scale, bias, out, M):
         raise ValueError("bias: fp32 [N]")
     if out.shape != (M, N):
         raise ValueError(f"out: expected {(M, N)}, got {tuple(out.shape)}")
+
+
+@functools.lru_cache(_WS_SIZES)
+def matmul_i8_workspace_bytes(M: int, N: int, K: int) -> int:
+    n = ctypes.c_size_t(0)
+    ld = -(-K // 16) * 16
+    _check(LIB.awsrc_matmul_i8(None, ld, None, None, ld, None, None, M, N, K, None, AWSRC_DTYPE_F32, N, None,
+                               ctypes.byref(n), None))
+    return n.value
+
+
+@functools.lru_cache(_WS_SIZES)
+def linear_i8_workspace_bytes(M: int, N: int, K: int) -> int:
+    n = ctypes.c_size_t(0)
+    ld = -(-K // 16) * 16
+    _check(LIB.awsrc_linear_i8(None, AWSRC_DTYPE_F32, K, None, ld, None, None, M, N, K, None, AWSRC_DTYPE_F32, N, None,
+                               ctypes.byref(n), None))
+    return n.value
+
+
+def _sized_workspace(workspace, need: int, like: torch.Tensor, stream):
+    """(address, size, the tensor that holds it)"""
+    if need == 0 and workspace is None:
+        return None, 0, None
+    if workspace is None or workspace.numel() < need:
+        workspace = _empty((need,), like, torch.uint8, stream)
+    return workspace.data_ptr(), workspace.numel(), workspace
 
 
 def awsrc_matmul_i8(a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor, b_scale: torch.Tensor,
@@ -661,33 +712,19 @@ def awsrc_matmul_i8(a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor, b_s
     N, Kb, ldb = _i8_rows(b, "b")
     if K != Kb:
         raise ValueError(f"a has {K} columns, b {Kb}")
-    dev = a.device
-    _on_device(dev, a, a_scale, b)
+    dev = _device_of(a)
+    _on_device(dev, a_scale, b)
     if a_scale.shape != (M,) or a_scale.dtype != torch.float32 or not a_scale.is_contiguous():
         raise ValueError("a_scale: fp32 [M]")
     if out is None:
-        out = _empty((M, N), out_dtype, dev, stream)
+        out = _empty((M, N), a, out_dtype, stream)
     _check_product_args(dev, N, b_scale, bias, out, M)
-    n = ctypes.c_size_t(0)
-    _check(LIB.awsrc_matmul_i8(None, lda, None, None, ldb, None, None, M, N, K, None, _act_code(out.dtype), N, None,
-                               ctypes.byref(n), None))
-    if n.value and (workspace is None or workspace.numel() < n.value):
-        workspace = _empty((n.value,), torch.uint8, dev, stream)
-    n = ctypes.c_size_t(0 if workspace is None else workspace.numel())
+    ws, n, keep = _sized_workspace(workspace, matmul_i8_workspace_bytes(M, N, K), a, stream)
     if M and N:
         _check(LIB.awsrc_matmul_i8(a.data_ptr(), lda, a_scale.data_ptr(), b.data_ptr(), ldb, b_scale.data_ptr(),
                                    None if bias is None else bias.data_ptr(), M, N, K, out.data_ptr(), _act_code(out.dtype),
-                                   _rows_of(out, "out")[2], None if workspace is None else workspace.data_ptr(),
-                                   ctypes.byref(n), _raw_stream(dev, stream)))
+                                   _rows_of(out, "out")[2], ws, ctypes.c_size_t(n), _raw_stream(dev, stream)))
     return out
-
-
-def linear_i8_workspace_bytes(M: int, N: int, K: int) -> int:
-    n = ctypes.c_size_t(0)
-    ld = -(-K // 16) * 16
-    _check(LIB.awsrc_linear_i8(None, AWSRC_DTYPE_F32, K, None, ld, None, None, M, N, K, None, AWSRC_DTYPE_F32, N, None,
-                               ctypes.byref(n), None))
-    return n.value
 
 
 def awsrc_linear_i8(x: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, bias: Optional[torch.Tensor] = None,
@@ -699,19 +736,16 @@ def awsrc_linear_i8(x: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, bia
     N, Kw, ldw = _i8_rows(w, "w")
     if K != Kw:
         raise ValueError(f"x has {K} columns, w {Kw}")
-    dev = x.device
-    _on_device(dev, x, w)
+    dev = _device_of(x)
     if out is None:
-        out = _empty((M, N), x.dtype if out_dtype is None else out_dtype, dev, stream)
+        out = _empty((M, N), x, x.dtype if out_dtype is None else out_dtype, stream)
+    _on_device(dev, w)
     _check_product_args(dev, N, w_scale, bias, out, M)
-    need = linear_i8_workspace_bytes(M, N, K)
-    if workspace is None or workspace.numel() < need:
-        workspace = _empty((need,), torch.uint8, dev, stream)
-    n = ctypes.c_size_t(workspace.numel())
+    ws, n, keep = _sized_workspace(workspace, linear_i8_workspace_bytes(M, N, K), x, stream)
     if M and N:
         _check(LIB.awsrc_linear_i8(x.data_ptr(), _act_code(x.dtype), ldx, w.data_ptr(), ldw, w_scale.data_ptr(),
                                    None if bias is None else bias.data_ptr(), M, N, K, out.data_ptr(), _act_code(out.dtype),
-                                   _rows_of(out, "out")[2], workspace.data_ptr(), ctypes.byref(n), _raw_stream(dev, stream)))
+                                   _rows_of(out, "out")[2], ws, ctypes.c_size_t(n), _raw_stream(dev, stream)))
     return out
 
 
@@ -722,39 +756,42 @@ def awsrc_kv_append(cache: KVCache, k: torch.Tensor, v: torch.Tensor, cu: torch.
     """Appends rows of k and v [rows, kv_heads, head_dim] (views of a fused projection's output will do) to the cache,
     keys rotated by the tables cos, sin [positions, rot / 2]; returns q [rows, q_heads, head_dim] rotated the same way.
     kv_len counts the appended tokens; max_new is at least the most rows that one sequence brings."""
-    c = _cache_of(cache)
-    dev = cache[0].device
+    c, heads, dim, _, dev = _cache_of(cache)
     n_seq, table_ld = _batch_of(dev, cu, kv_len, page_table)
     _on_device(dev, k, v, q, cos, sin, q_out)
-    rows = k.shape[0]
-    ldk = _heads_of(k, "k", c.kv_heads, c.head_dim, k.dtype)
-    ldv = _heads_of(v, "v", c.kv_heads, c.head_dim, k.dtype)
-    if v.shape[0] != rows or (q is not None and q.shape[0] != rows):
+    dtype = k.dtype
+    rows, _, ldk = _heads_of(k, "k", heads, dim, dtype)
+    rows_v, _, ldv = _heads_of(v, "v", heads, dim, dtype)
+    if rows_v != rows:
         raise ValueError("k, v and q must have the same rows")
-    if (cos is None) != (sin is None):
-        raise ValueError("cos and sin go together")
     rot = rope_len = 0
+    cos_p = sin_p = q_p = qo_p = None
     if cos is not None:
-        if cos.shape != sin.shape or cos.dim() != 2 or cos.dtype != torch.float32 or sin.dtype != torch.float32:
+        if sin is None or cos.dim() != 2 or cos.shape != sin.shape or cos.dtype != torch.float32 or sin.dtype != torch.float32:
             raise ValueError("cos, sin: fp32 [positions, rot / 2]")
-        _dev(cos, sin)
-        rope_len, rot = cos.shape[0], 2 * cos.shape[1]
-    ldq = ldqo = heads = 0
+        if not (cos.is_contiguous() and sin.is_contiguous()):
+            raise ValueError("cos and sin must be contiguous")
+        rope_len, rot = cos.shape
+        rot, cos_p, sin_p = 2 * rot, cos.data_ptr(), sin.data_ptr()
+    elif sin is not None:
+        raise ValueError("cos and sin go together")
+    ldq = ldqo = q_heads = 0
     if q is not None:
-        heads = q.shape[1]
-        ldq = _heads_of(q, "q", None, c.head_dim, k.dtype)
+        rows_q, q_heads, ldq = _heads_of(q, "q", None, dim, dtype)
+        if rows_q != rows:
+            raise ValueError("k, v and q must have the same rows")
         if q_out is None:
-            q_out = _empty((rows, heads, c.head_dim), q.dtype, dev, stream)
+            q_out, ldqo = _empty((rows, q_heads, dim), q, dtype, stream), q_heads * dim
         elif q_out.shape != q.shape:
             raise ValueError("q_out: q's shape")
-        ldqo = _heads_of(q_out, "q_out", heads, c.head_dim, k.dtype)
+        else:
+            ldqo = _heads_of(q_out, "q_out", q_heads, dim, dtype)[2]
+        q_p, qo_p = q.data_ptr(), q_out.data_ptr()
     elif q_out is not None:
         raise ValueError("q_out without q")
-    _check(LIB.awsrc_kv_append(ctypes.byref(c), k.data_ptr(), ldk, v.data_ptr(), ldv, None if q is None else q.data_ptr(), ldq,
-                               heads, None if q is None else q_out.data_ptr(), ldqo, _act_code(k.dtype),
-                               None if cos is None else cos.data_ptr(), None if cos is None else sin.data_ptr(), rope_len, rot,
-                               int(interleaved), n_seq, rows, cu.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(),
-                               table_ld, min(int(max_new), rows), _raw_stream(dev, stream)))
+    _check(LIB.awsrc_kv_append(c, k.data_ptr(), ldk, v.data_ptr(), ldv, q_p, ldq, q_heads, qo_p, ldqo, _act_code(dtype), cos_p,
+                               sin_p, rope_len, rot, interleaved, n_seq, rows, cu.data_ptr(), kv_len.data_ptr(),
+                               page_table.data_ptr(), table_ld, min(max_new, rows), _raw_stream(dev, stream)))
     return q_out
 
 
@@ -762,14 +799,24 @@ def awsrc_kv_read(cache: KVCache, cu: torch.Tensor, kv_len: torch.Tensor, page_t
                   dtype: torch.dtype = torch.bfloat16, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """What the cache holds for the last cu[s + 1] - cu[s] tokens of each sequence: dense keys and values
     [rows, kv_heads, head_dim], rows = cu[-1]."""
-    c = _cache_of(cache)
-    dev = cache[0].device
+    c, heads, dim, _, dev = _cache_of(cache)
     n_seq, table_ld = _batch_of(dev, cu, kv_len, page_table)
-    k = _empty((rows, c.kv_heads, c.head_dim), dtype, dev, stream)
-    v = _empty((rows, c.kv_heads, c.head_dim), dtype, dev, stream)
-    _check(LIB.awsrc_kv_read(ctypes.byref(c), n_seq, rows, cu.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(), table_ld,
-                             min(int(max_new), rows), k.data_ptr(), v.data_ptr(), _act_code(dtype), _raw_stream(dev, stream)))
+    k = _empty((rows, heads, dim), cu, dtype, stream)
+    v = _empty((rows, heads, dim), cu, dtype, stream)
+    _check(LIB.awsrc_kv_read(c, n_seq, rows, cu.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(), table_ld,
+                             min(max_new, rows), k.data_ptr(), v.data_ptr(), _act_code(dtype), _raw_stream(dev, stream)))
     return k, v
+
+
+@functools.lru_cache(_WS_SIZES)
+def kv_attention_workspace_bytes(n_seq: int, rows: int, max_new: int, max_kv: int, table_ld: int, q_heads: int, kv_heads: int,
+                                 head_dim: int, page_tokens: int) -> int:
+    c = awsrc_kv_cache(None, None, None, None, 1, kv_heads, head_dim, page_tokens, 0)
+    n = ctypes.c_size_t(0)
+    w = q_heads * head_dim
+    _check(LIB.awsrc_kv_attention(c, None, w, q_heads, AWSRC_DTYPE_BF16, n_seq, rows, None, None, None, table_ld, max_new,
+                                  max_kv, 1.0, 1, None, w, None, ctypes.byref(n), None))
+    return n.value
 
 
 def awsrc_kv_attention(cache: KVCache, q: torch.Tensor, cu: torch.Tensor, kv_len: torch.Tensor, page_table: torch.Tensor,
@@ -778,29 +825,22 @@ def awsrc_kv_attention(cache: KVCache, q: torch.Tensor, cu: torch.Tensor, kv_len
                        stream=None) -> torch.Tensor:
     """Attention of q [rows, q_heads, head_dim] (rotated, bf16 or fp16) over the cache; scale defaults to
     head_dim ** -0.5.  max_new and max_kv bound the rows and the cached tokens of a sequence."""
-    c = _cache_of(cache)
-    dev = cache[0].device
+    c, kv_heads, dim, page, dev = _cache_of(cache)
     n_seq, table_ld = _batch_of(dev, cu, kv_len, page_table)
     _on_device(dev, q, out)
-    rows, heads = q.shape[0], q.shape[1]
-    ldq = _heads_of(q, "q", None, c.head_dim, q.dtype)
+    dtype = q.dtype
+    rows, heads, ldq = _heads_of(q, "q", None, dim, dtype)
     if out is None:
-        out = _empty((rows, heads, c.head_dim), q.dtype, dev, stream)
+        out, ldo = _empty((rows, heads, dim), q, dtype, stream), heads * dim
     elif out.shape != q.shape:
         raise ValueError("out: q's shape")
-    ldo = _heads_of(out, "out", heads, c.head_dim, q.dtype)
-    if scale is None:
-        scale = c.head_dim ** -0.5
-    code, max_new = _act_code(q.dtype), min(int(max_new), rows)
-    n = ctypes.c_size_t(0)
-    _check(LIB.awsrc_kv_attention(ctypes.byref(c), None, ldq, heads, code, n_seq, rows, None, None, None, table_ld, max_new,
-                                  max_kv, scale, int(causal), None, ldo, None, ctypes.byref(n), None))
-    if n.value and (workspace is None or workspace.numel() < n.value):
-        workspace = _empty((n.value,), torch.uint8, dev, stream)
-    n = ctypes.c_size_t(0 if workspace is None else workspace.numel())
+    else:
+        ldo = _heads_of(out, "out", heads, dim, dtype)[2]
+    max_new = min(max_new, rows)
+    ws, n, keep = _sized_workspace(workspace, kv_attention_workspace_bytes(n_seq, rows, max_new, max_kv, table_ld, heads,
+                                                                           kv_heads, dim, page), q, stream)
     if rows:
-        _check(LIB.awsrc_kv_attention(ctypes.byref(c), q.data_ptr(), ldq, heads, code, n_seq, rows, cu.data_ptr(),
-                                      kv_len.data_ptr(), page_table.data_ptr(), table_ld, max_new, max_kv, scale, int(causal),
-                                      out.data_ptr(), ldo, None if workspace is None else workspace.data_ptr(),
-                                      ctypes.byref(n), _raw_stream(dev, stream)))
+        _check(LIB.awsrc_kv_attention(c, q.data_ptr(), ldq, heads, _act_code(dtype), n_seq, rows, cu.data_ptr(), kv_len.data_ptr(),
+                                      page_table.data_ptr(), table_ld, max_new, max_kv, dim ** -0.5 if scale is None else scale,
+                                      causal, out.data_ptr(), ldo, ws, ctypes.c_size_t(n), _raw_stream(dev, stream)))
     return out
