@@ -597,10 +597,11 @@ awsrc_status awsrc_kv_read(const awsrc_kv_cache* cache, int32_t n_seq, int64_t n
  * kv_heads; query head h reads cached head h / (q_heads / kv_heads).  A row that
  * sees no token is 0.  Tokens whose page lies outside the cache or the table are
  * not seen.  Scores, maximum and sums in fp32; products in fp16 with fp32 sums.
+ * The scales in the cache are not negative (or NaN).
  *  q, out   [n_rows][q_heads][head_dim] bf16 or fp16 (dtype), rows ldq and ldo
  *           apart, 16-byte aligned, ldq and ldo multiples of 8.
- *  max_kv   (host) at least the largest kv_len[s]: how far the work may be split.
- *           Longer sequences are cut there.
+ *  max_kv   (host) at least the largest kv_len[s], at most 2^30: how far the work
+ *           may be split.  Tokens past it are not seen.
  *  scale    finite.
  * Workspace: two-phase query as described above (the query needs no pointers
  * but `cache`); the size may be 0, and then no workspace is needed.

@@ -1068,6 +1068,7 @@ int64_t act_size(int32_t t) { return t == AWSRC_DTYPE_F32 ? 4 : 2; }
 bool misaligned(const void* p, uintptr_t a) { return reinterpret_cast<uintptr_t>(p) & (a - 1); }
 
 constexpr int64_t kMaxDim = 1ll << 31;  // rows, columns and leading dimensions
+constexpr int64_t kMaxKv = 1ll << 30;  // tokens of a sequence that attention indexes
 constexpr int64_t kMaxLdI8 = 1ll << 22;  // of int8 operands: 256 rows of one stay below 2^31 bytes
 
 awsrc_status check_quantize(const void* X, int32_t x_dtype, int64_t rows, int64_t cols, int64_t ldx) {
@@ -1273,7 +1274,8 @@ extern "C" awsrc_status awsrc_kv_attention(const awsrc_kv_cache* cache, const vo
   if (dtype != AWSRC_DTYPE_BF16 && dtype != AWSRC_DTYPE_F16) return fail(AWSRC_EINVAL, "bad dtype %d: bf16 or fp16", dtype);
   if (q_heads < 1 || q_heads > 65536 || q_heads % cache->kv_heads)
     return fail(AWSRC_EINVAL, "q_heads=%d: must be a multiple of kv_heads=%d", q_heads, cache->kv_heads);
-  if (max_kv < 0 || max_kv >= kMaxDim) return fail(AWSRC_EINVAL, "max_kv=%lld out of range", (long long)max_kv);
+  if (max_kv < 0 || max_kv > kMaxKv) return fail(AWSRC_EINVAL, "max_kv=%lld out of range 0..2^30", (long long)max_kv);
+  if (n_rows * (q_heads / cache->kv_heads) >= kMaxDim) return fail(AWSRC_EINVAL, "n_rows=%lld: 2^31 query rows of a cached head", (long long)n_rows);
   if (!isfinite(scale)) return fail(AWSRC_EINVAL, "scale must be finite");
   if (!ws_bytes) return fail(AWSRC_EINVAL, "ws_bytes is NULL");
   AttentionArgs a{};

@@ -13,13 +13,19 @@
 // scaling and p' stays in fp16's range whatever the pages' scales are; the
 // denominator sums p' / s_V in fp32.
 //
-// Layout: the score product is taken as K Q^T, a lane l ending with query
-// l % 16 and four tokens per 16-token tile.  Key rows are assigned to the
-// tiles so that the 16 scores of a lane over four tiles are the 16
-// consecutive tokens 16 (l / 16) .. + 15: the right operand of V^T P^T
-// without any exchange between lanes, against V^T codes read in 16-byte runs
-// of tokens.  Likewise Q and K agree on an order of the channels in which
-// each lane reads 16 consecutive bytes of a key.
+// The maxima in use lag: they move only when some row of the wavefront passes its
+// own by 2^8, which keeps p' far below fp16's range and spares the older sums'
+// rescaling in nearly every step.
+//
+// Layout: the score product is taken as K Q^T and its rows are assigned to
+// tokens so that a lane ends with one query's scores of 16 consecutive tokens
+// (which lie in one page): the right operand of V^T P^T without any exchange
+// between lanes.
+//
+// Two kernels: k_kv_attention_rows for up to 64 query rows of a (sequence, cached
+// head), bound by the cache's bytes, and k_kv_attention_tiles for more, bound
+// by the matrix cores and the exponentials.  Both may split the tokens over
+// workgroups, whose sums k_kv_attention_join puts together.
 #include "serve_internal.h"
 
 namespace awsrc {
@@ -48,224 +54,427 @@ __device__ __forceinline__ h8 codes_to_f16x8(uint32_t w0, uint32_t w1) {
   return h8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-__device__ __forceinline__ float max_over_groups(float m) {
-  m = fmaxf(m, __shfl_xor(m, 16, 64));
-  return fmaxf(m, __shfl_xor(m, 32, 64));
-}
-__device__ __forceinline__ float sum_over_groups(float s) {
-  s += __shfl_xor(s, 16, 64);
-  return s + __shfl_xor(s, 32, 64);
-}
+// The running softmax of a row, over lanes that hold U runs of 16 tokens each.
+template <int U>
+struct Softmax {
+  float m = -__builtin_inff();  // of the scores seen (times log2 e); lags behind the maximum by at most kLag
+  float M = -__builtin_inff();  // of score + log2 s_V
+  float off[U];                 // p' = exp2(score + off)
+  float f[U];                   // p = p' f
+  bool quiet[U];                // the run's page adds nothing to the output
+};
+constexpr float kLag = 8.0f;
 
 __device__ __forceinline__ float finite_or_zero(float m) { return m == -__builtin_inff() ? 0.0f : m; }
 
-// One step of the running softmax of a row: `run` is the largest seen score
-// (times log2 e) of the lane's 16 tokens, which lie in one page of value scale
-// sv; the row's other lanes hold other tokens.  Updates the row's m and M.
-struct Softmax {
-  float off;               // p' = exp2(s + off)
-  float f;                 // p = p' f
-  float alpha_l, alpha_o;  // the older sums' factors
-  bool quiet;              // the page adds nothing to the output
-};
-__device__ __forceinline__ Softmax softmax_step(float run, float sv, bool seen, float& m, float& M) {
-  const bool zero = sv < kZeroScale;
-  const float lsv = __builtin_amdgcn_logf(sv);  // log2
-  const float mn = fmaxf(m, max_over_groups(run));
-  const float Mn = fmaxf(M, max_over_groups(seen && !zero ? run + lsv : -__builtin_inff()));
-  const float mu = finite_or_zero(mn), Mu = finite_or_zero(Mn);
-  const float gap = Mu - mu - lsv;
-  Softmax w;
-  w.quiet = zero || gap > kQuiet;
-  w.off = !seen ? 0.0f : w.quiet ? -mu : lsv - Mu;
-  w.f = !seen || w.quiet ? 1.0f : __builtin_amdgcn_exp2f(gap);
-  w.alpha_l = __builtin_amdgcn_exp2f(m - mu);
-  w.alpha_o = __builtin_amdgcn_exp2f(M - Mu);
-  m = mn;
-  M = Mn;
-  return w;
+// Largest value over a row's lanes: those 16 and 32 apart (four lanes a row) or 32 apart (two).
+template <int LANES>
+__device__ __forceinline__ float row_max(float x) {
+  if constexpr (LANES == 4) x = fmaxf(x, __shfl_xor(x, 16, 64));
+  return fmaxf(x, __shfl_xor(x, 32, 64));
 }
 
-// One workgroup: 16 query rows (row = token * group + head of the group) of one
-// (sequence, cached head); the tokens in tiles of 64 over its 4 wavefronts,
-// joined through LDS at the end.
+// One step: run[u] is the largest seen score of run u, of a page of value scale
+// sv[u].  Where the maxima moved, returns true with the factors of the older sums.
+template <int LANES, int U>
+__device__ __forceinline__ bool softmax_step(Softmax<U>& s, const float (&run)[U], const float (&sv)[U], const bool (&seen)[U],
+                                             float& alpha_l, float& alpha_o) {
+  float lsv[U], top = -__builtin_inff(), Top = top;
+  bool zero[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    zero[u] = sv[u] < kZeroScale;
+    lsv[u] = __builtin_amdgcn_logf(sv[u]);  // log2
+    top = fmaxf(top, run[u]);
+    Top = fmaxf(Top, seen[u] && !zero[u] ? run[u] + lsv[u] : -__builtin_inff());
+  }
+  top = row_max<LANES>(top);
+  Top = row_max<LANES>(Top);
+  const bool moved = __any(top > s.m + kLag || Top > s.M + kLag);
+  if (moved) {
+    const float mn = fmaxf(s.m, top), Mn = fmaxf(s.M, Top);
+    alpha_l = __builtin_amdgcn_exp2f(s.m - finite_or_zero(mn));
+    alpha_o = __builtin_amdgcn_exp2f(s.M - finite_or_zero(Mn));
+    s.m = mn;
+    s.M = Mn;
+  }
+  const float mu = finite_or_zero(s.m), Mu = finite_or_zero(s.M);
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const float gap = Mu - mu - lsv[u];
+    s.quiet[u] = zero[u] || gap > kQuiet;
+    s.off[u] = !seen[u] ? 0.0f : s.quiet[u] ? -mu : lsv[u] - Mu;
+    s.f[u] = !seen[u] || s.quiet[u] ? 1.0f : __builtin_amdgcn_exp2f(gap);
+  }
+  return moved;
+}
+
+// Where a workgroup's query rows (row = token * group + head of the group) lie
+// and how many tokens they see.
+struct Rows {
+  int64_t r0;     // packed row of the sequence's first token
+  int n_new, G, head;
+  int len, most;  // cached tokens; tokens that the table and the caller's bound reach
+  int causal;
+  __device__ __forceinline__ bool set(const AttentionArgs& a, int s, int h) {
+    const int64_t first = a.cu[s], last = a.cu[s + 1];
+    if (first < 0 || last > a.n_rows || last <= first) return false;
+    r0 = first;
+    n_new = (int)(last - first);
+    G = a.q_heads / a.c.kv_heads;
+    head = h;
+    len = a.kv_len[s];
+    int64_t m = a.table_ld * a.c.page_tokens;
+    if (m > a.max_kv) m = a.max_kv;
+    most = m < len ? (int)m : len;
+    causal = a.causal;
+    return true;
+  }
+  __device__ __forceinline__ int total() const { return n_new * G; }
+  // tokens below this are seen by row R
+  __device__ __forceinline__ int limit(int R) const {
+    const int lim = causal ? len - n_new + R / G + 1 : len;
+    return lim < most ? lim : most;
+  }
+  // offset of row R in a [rows][heads][D] tensor with rows ld apart
+  __device__ __forceinline__ int64_t at(int R, int64_t ld, int D) const {
+    const int t = R / G;
+    return (r0 + t) * ld + (int64_t)(head * G + R - t * G) * D;
+  }
+};
+
+// Workgroups of a (sequence, cached head) with BR rows each, and of a split of its tokens.
+struct Plan {
+  int tiles_q, n_split, chunk;  // chunk: tokens of a split
+};
+template <int BR>
+__device__ __forceinline__ float* part_of(float* parts, int64_t index, int D) {
+  return parts + index * (BR * (D + 3));  // O [BR][D], then m, M and L [BR]
+}
+
+// A query row as fp16 fragments: x[i] for i < N with (channel) index ch(i),
+// brought below 2 by a power of two, times the sign of the scale; `lanes` lanes
+// share the row.  Returns the score's factor.
+template <int LANES, int N, typename T, typename CH>
+__device__ __forceinline__ float load_query(const T* q, bool live, float scale, const CH& ch, h8 (&out)[N / 8]) {
+  h8 raw[N / 8];
+  float qm = 0.0f;
+  float v[N];
+#pragma unroll
+  for (int i = 0; i < N; i += 8) {
+    struct alignas(16) Piece { T x[8]; };
+    Piece p;
+    if (live) p = *reinterpret_cast<const Piece*>(q + ch(i));
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      v[i + e] = live ? to_f32(p.x[e]) : 0.0f;
+      qm = amax_keep(qm, v[i + e]);
+    }
+  }
+  if constexpr (LANES == 4) qm = amax_keep(qm, __shfl_xor(qm, 16, 64));
+  qm = amax_keep(qm, __shfl_xor(qm, 32, 64));
+  int e2 = 0;
+  if (qm > 0.0f && qm < __builtin_inff()) e2 = ilogbf(qm);
+  const float sign = scale < 0.0f ? -1.0f : 1.0f;
+#pragma unroll
+  for (int i = 0; i < N; ++i) raw[i >> 3][i & 7] = (_Float16)ldexpf(v[i] * sign, -e2);
+#pragma unroll
+  for (int i = 0; i < N / 8; ++i) out[i] = raw[i];
+  return ldexpf(fabsf(scale) * kLog2e, e2);
+}
+
+// Few rows.  One workgroup: 16 query rows of one (sequence, cached head) and one
+// chunk of its tokens, in tiles of 64 tokens over 4 wavefronts that meet in LDS at
+// the end.  Keys and values go from memory to the matrix cores in 16-byte runs of
+// codes per lane, without LDS: a tile's values and the next tile's keys are in
+// flight while the scores and the softmax are computed.
+//
+// Lane l holds query l % 16.  Row 4 g + i of score tile j is token 16 g + 4 j + i.
+// Q and K agree on an order of the channels in which each lane reads 16
+// consecutive bytes of a key: channels 64 c + 16 g + 8 h + 0..7 are step (c, h).
 template <typename T, int D>
-__global__ __launch_bounds__(256) void k_kv_attention_rows(AttentionArgs a, int64_t tiles_q) {
+__global__ __launch_bounds__(256, D == 256 ? 1 : 3) void k_kv_attention_rows(AttentionArgs a, Plan plan, float* parts) {
   constexpr int NC = D / 64;  // 64-channel steps of the scores
   constexpr int ND = D / 16;  // 16-channel tiles of the output
   __shared__ float sh_m[4][16], sh_M[4][16], sh_l[4][16];
   __shared__ float sh_o[4][16][D + 4];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 15, g = lane >> 4;
-  int64_t b = blockIdx.x;
-  const int head = (int)(b % a.c.kv_heads);
+  int b = blockIdx.x;
+  const int qt = b % plan.tiles_q;
+  b /= plan.tiles_q;
+  const int head = b % a.c.kv_heads;
   b /= a.c.kv_heads;
-  const int64_t qt = b % tiles_q;
-  const int s = (int)(b / tiles_q);
-  const int G = a.q_heads / a.c.kv_heads;
-  const int P = a.c.page_tokens;
-  const int64_t r0 = a.cu[s], r1 = a.cu[s + 1];
-  if (r0 < 0 || r1 > a.n_rows) return;
-  const int64_t n_new = r1 - r0;
-  if (qt * 16 >= n_new * G) return;
-  const int64_t len = a.kv_len[s];
-  int64_t most = a.table_ld * P;  // tokens the table and the caller's bound reach
-  if (most > a.max_kv) most = a.max_kv;
-  if (most > len) most = len;
+  const int split = b % plan.n_split, s = b / plan.n_split;
+  Rows rows;
+  if (!rows.set(a, s, head)) return;
+  const int R0 = qt * 16, n_rows = rows.total() - R0;
+  if (n_rows <= 0) return;
+  const int full = rows.limit(R0 + (n_rows < 16 ? n_rows : 16) - 1);  // tokens that any row sees
+  const int start = split * plan.chunk;
+  if (split && start >= full) return;
+  const int end = full < start + plan.chunk ? full : start + plan.chunk;
+  const bool live = r < n_rows;
+  int lim = live ? rows.limit(R0 + r) : 0;
+  if (lim > end) lim = end;
 
-  const int64_t R = qt * 16 + r;
-  const bool live = R < n_new * G;
-  const int64_t tok = live ? R / G : 0;
-  const int qh = head * G + (int)(live ? R - tok * G : 0);
-  // tokens below lim are seen
-  int64_t lim = a.causal ? len - n_new + tok + 1 : len;
-  if (lim > most) lim = most;
-  if (!live) lim = 0;
-  int64_t end = lim;  // tokens any row of the workgroup sees
-#pragma unroll
-  for (int off = 8; off >= 1; off >>= 1) {
-    const int64_t o = __shfl_xor(end, off, 64);
-    end = o > end ? o : end;
-  }
-
-  // the query row: channels 64 c + 16 g + 8 h + 0..7 of MFMA step (c, h)
-  const T* q = static_cast<const T*>(a.q) + (r0 + tok) * a.ldq + (int64_t)qh * D;
-  float qf[NC][16];
-  float qm = 0.0f;
-#pragma unroll
-  for (int c = 0; c < NC; ++c)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      qf[c][e] = live ? to_f32(q[64 * c + 16 * g + e]) : 0.0f;
-      qm = amax_keep(qm, qf[c][e]);
-    }
-  qm = amax_keep(qm, __shfl_xor(qm, 16, 64));
-  qm = amax_keep(qm, __shfl_xor(qm, 32, 64));
-  int qe = 0;
-  if (qm > 0.0f && qm < __builtin_inff()) qe = ilogbf(qm);
-  h8 qa[NC][2];
-#pragma unroll
-  for (int c = 0; c < NC; ++c)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) qa[c][e >> 3][e & 7] = (_Float16)ldexpf(qf[c][e], -qe);
-  const float qscale = ldexpf(a.scale * kLog2e, qe);
-
-  float m = -__builtin_inff(), M = m, L = 0.0f;
+  h8 qa[2 * NC];
+  const float qscale = load_query<4, 16 * NC>(static_cast<const T*>(a.q) + rows.at(live ? R0 + r : R0, a.ldq, D), live, a.scale,
+                                              [&](int i) { return 64 * (i >> 4) + 16 * g + (i & 8); }, qa);
+  Softmax<1> sm;
+  float L = 0.0f;
   fl4 o[ND];
 #pragma unroll
   for (int d = 0; d < ND; ++d) o[d] = fl4{0, 0, 0, 0};
 
   const int32_t* table = a.table + (int64_t)s * a.table_ld;
-  const int64_t page_bytes = (int64_t)P * D;
-  for (int64_t t0 = (int64_t)wave * 64; t0 < end; t0 += 256) {
-    // the page of a 16-token run; runs past the end read the tile's first page (their scores are masked)
-    const int64_t tv = t0 + 16 * g;              // this lane's tokens
-    const int64_t tk = t0 + 16 * (r >> 2);       // the tokens of this lane's key rows
-    int32_t pv = table[(tv < end ? tv : t0) / P];
-    int32_t pk = table[(tk < end ? tk : t0) / P];
-    const bool pv_ok = pv >= 0 && pv < a.c.n_pages;
-    if (!pv_ok) pv = 0;
-    if (!(pk >= 0 && pk < a.c.n_pages)) pk = 0;
-    const int64_t bv = (int64_t)pv * a.c.kv_heads + head, bk = (int64_t)pk * a.c.kv_heads + head;
-    // how many of the lane's 16 tokens are seen
-    const int64_t left = pv_ok ? lim - tv : 0;
-    const int n_seen = left < 0 ? 0 : left > 16 ? 16 : (int)left;
-    const float sk = a.c.k_scale[bv] * qscale, sv = a.c.v_scale[bv];
-    const int8_t* kb = a.c.k + bk * page_bytes + (int64_t)((tk < end ? tk : t0) % P + (r & 3)) * D + 16 * g;
+  const int shift = __builtin_ctz(a.c.page_tokens), P = a.c.page_tokens;
+  const int64_t stride = (int64_t)P * D;
+  // the tokens whose page a lane needs: of its value run and scores, and of its key rows; past the end the
+  // tile's first token stands in (the scores are masked)
+  const auto token = [&](int t0, int run) { return t0 + 16 * run < end ? t0 + 16 * run : t0; };
+  u32x4_t kw[4][NC];
+  float sk = 0.0f, sv = 0.0f, sk_next, sv_next;
+  int64_t bv = 0, bv_next;
+  bool ok = false, ok_next;
+  int32_t pk = 0, pv = 0;  // pages of the tile whose keys are loaded next
+  const auto pages = [&](int t0) {
+    pv = table[token(t0, g) >> shift];
+    pk = table[token(t0, r >> 2) >> shift];
+  };
+  const auto load_keys = [&](int t0) {
+    ok_next = pv >= 0 && pv < a.c.n_pages;
+    bv_next = (int64_t)(ok_next ? pv : 0) * a.c.kv_heads + head;
+    const int64_t bk = (int64_t)(pk >= 0 && pk < a.c.n_pages ? pk : 0) * a.c.kv_heads + head;
+    sk_next = a.c.k_scale[bv_next];
+    sv_next = a.c.v_scale[bv_next];
+    const int8_t* kb = a.c.k + bk * stride + ((token(t0, r >> 2) & (P - 1)) + (r & 3)) * D + 16 * g;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int c = 0; c < NC; ++c) kw[j][c] = *reinterpret_cast<const u32x4_t*>(kb + 4 * j * D + 64 * c);
+  };
+  int t0 = start + wave * 64;
+  if (t0 < end) {
+    pages(t0);
+    load_keys(t0);
+    if (t0 + 256 < end) pages(t0 + 256);
+  }
+  for (; t0 < end; t0 += 256) {
+    sk = sk_next * qscale;
+    sv = sv_next;
+    bv = bv_next;
+    ok = ok_next;
+    const int8_t* vb = a.c.v + bv * stride + (int64_t)r * P + (token(t0, g) & (P - 1));
+    u32x4_t vw[ND];
+#pragma unroll
+    for (int d = 0; d < ND; ++d) vw[d] = *reinterpret_cast<const u32x4_t*>(vb + 16 * d * P);
     fl4 sc[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       sc[j] = fl4{0, 0, 0, 0};
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
-        const u32x4_t w = *reinterpret_cast<const u32x4_t*>(kb + (int64_t)(4 * j) * D + 64 * c);
-        sc[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_to_f16x8(w[0], w[1]), qa[c][0], sc[j], 0, 0, 0);
-        sc[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_to_f16x8(w[2], w[3]), qa[c][1], sc[j], 0, 0, 0);
+        const u32x4_t w = kw[j][c];
+        sc[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_to_f16x8(w[0], w[1]), qa[2 * c], sc[j], 0, 0, 0);
+        sc[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_to_f16x8(w[2], w[3]), qa[2 * c + 1], sc[j], 0, 0, 0);
       }
     }
-    float p[16];
-    float run = -__builtin_inff();
+    if (t0 + 256 < end) {
+      load_keys(t0 + 256);
+      if (t0 + 512 < end) pages(t0 + 512);
+    }
+    // how many of the lane's 16 tokens are seen
+    const int left = ok ? lim - (t0 + 16 * g) : 0;
+    float p[16], run[1] = {-__builtin_inff()};
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      p[e] = e < n_seen ? sc[e >> 2][e & 3] * sk : -__builtin_inff();
-      run = fmaxf(run, p[e]);
+      p[e] = e < left ? sc[e >> 2][e & 3] * sk : -__builtin_inff();
+      run[0] = fmaxf(run[0], p[e]);
     }
-    const Softmax w = softmax_step(run, sv, n_seen > 0, m, M);
+    float alpha_l, alpha_o;
+    if (softmax_step<4, 1>(sm, run, {sv}, {left > 0}, alpha_l, alpha_o)) {
+      L *= alpha_l;
+#pragma unroll
+      for (int d = 0; d < ND; ++d) o[d] *= alpha_o;
+    }
     float l = 0.0f;
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      p[e] = __builtin_amdgcn_exp2f(p[e] + w.off);
+      p[e] = __builtin_amdgcn_exp2f(p[e] + sm.off[0]);
       l += p[e];
     }
-    L = L * w.alpha_l + l * w.f;
+    L += l * sm.f[0];
     h8 ph[2];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) ph[e >> 3][e & 7] = (_Float16)(w.quiet ? 0.0f : p[e]);
-    const int8_t* vb = a.c.v + bv * page_bytes + (int64_t)r * P + (tv < end ? tv : t0) % P;
+    for (int e = 0; e < 16; ++e) ph[e >> 3][e & 7] = (_Float16)(sm.quiet[0] ? 0.0f : p[e]);
 #pragma unroll
     for (int d = 0; d < ND; ++d) {
-      const u32x4_t x = *reinterpret_cast<const u32x4_t*>(vb + (int64_t)(16 * d) * P);
-      fl4 acc = o[d] * w.alpha_o;
-      acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_to_f16x8(x[0], x[1]), ph[0], acc, 0, 0, 0);
-      o[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_to_f16x8(x[2], x[3]), ph[1], acc, 0, 0, 0);
+      const u32x4_t x = vw[d];
+      o[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_to_f16x8(x[0], x[1]), ph[0], o[d], 0, 0, 0);
+      o[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_to_f16x8(x[2], x[3]), ph[1], o[d], 0, 0, 0);
     }
   }
-  L = sum_over_groups(L);
+  L += __shfl_xor(L, 16, 64);
+  L += __shfl_xor(L, 32, 64);
   if (g == 0) {
-    sh_m[wave][r] = m;
-    sh_M[wave][r] = M;
+    sh_m[wave][r] = sm.m;
+    sh_M[wave][r] = sm.M;
     sh_l[wave][r] = L;
   }
 #pragma unroll
   for (int d = 0; d < ND; ++d) *reinterpret_cast<fl4*>(&sh_o[wave][r][16 * d + 4 * g]) = o[d];
   __syncthreads();
-  for (int i = threadIdx.x; i < 16 * D; i += 256) {
-    const int row = i / D, d = i - row * D;
-    const int64_t RR = qt * 16 + row;
-    if (RR >= n_new * G) continue;
-    float mj = -__builtin_inff(), Mj = mj;
+  const bool whole = full <= plan.chunk;  // this workgroup saw every token
+  float* part = part_of<16>(parts, ((int64_t)(s * a.c.kv_heads + head) * plan.tiles_q + qt) * plan.n_split + split, D);
+  for (int i = threadIdx.x; i < 16 * D / 4; i += 256) {
+    const int row = i / (D / 4), d = (i - row * (D / 4)) * 4;
+    if (row >= n_rows) break;
+    float m = -__builtin_inff(), M = m;
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-      mj = fmaxf(mj, sh_m[w][row]);
-      Mj = fmaxf(Mj, sh_M[w][row]);
+      m = fmaxf(m, sh_m[w][row]);
+      M = fmaxf(M, sh_M[w][row]);
     }
-    mj = finite_or_zero(mj);
-    Mj = finite_or_zero(Mj);
-    float l = 0.0f, y = 0.0f;
+    const float mu = finite_or_zero(m), Mu = finite_or_zero(M);
+    float l = 0.0f;
+    fl4 y = {0, 0, 0, 0};
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-      l += __builtin_amdgcn_exp2f(sh_m[w][row] - mj) * sh_l[w][row];
-      y += __builtin_amdgcn_exp2f(sh_M[w][row] - Mj) * sh_o[w][row][d];
+      l += __builtin_amdgcn_exp2f(sh_m[w][row] - mu) * sh_l[w][row];
+      y += __builtin_amdgcn_exp2f(sh_M[w][row] - Mu) * *reinterpret_cast<const fl4*>(&sh_o[w][row][d]);
     }
-    y = l == 0.0f ? 0.0f : y / l * __builtin_amdgcn_exp2f(Mj - mj);
-    const int64_t tk = RR / G;
-    static_cast<T*>(a.out)[(r0 + tk) * a.ldo + (int64_t)(head * G + (RR - tk * G)) * D + d] = (T)y;
+    if (whole) {
+      const float f = __builtin_amdgcn_exp2f(Mu - mu);
+      struct alignas(8) Four { T v[4]; } out;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) out.v[e] = (T)(l == 0.0f ? 0.0f : y[e] / l * f);
+      *reinterpret_cast<Four*>(static_cast<T*>(a.out) + rows.at(R0 + row, a.ldo, D) + d) = out;
+    } else {
+      *reinterpret_cast<fl4*>(part + row * D + d) = y;
+      if (d == 0) {
+        part[16 * D + row] = m;
+        part[16 * D + 16 + row] = M;
+        part[16 * D + 32 + row] = l;
+      }
+    }
   }
 }
 
+// The sums of a row's splits together: one workgroup per (sequence, query row),
+// its wavefronts over the splits.
+template <int BR, typename T, int D>
+__global__ __launch_bounds__(256) void k_kv_attention_join(AttentionArgs a, Plan plan, const float* parts) {
+  constexpr int LD = D / 4;        // lanes across a row
+  constexpr int NP = 256 / LD;     // splits taken at once
+  __shared__ float sh_s[NP][3];
+  __shared__ float sh_o[NP][D];
+  const int64_t per_seq = (int64_t)plan.tiles_q * BR;
+  int64_t b = blockIdx.x;
+  const int R = (int)(b % per_seq);
+  b /= per_seq;
+  const int head = (int)(b % a.c.kv_heads), s = (int)(b / a.c.kv_heads);
+  Rows rows;
+  if (!rows.set(a, s, head) || R >= rows.total()) return;
+  const int qt = R / BR, row = R - qt * BR;
+  const int last = qt * BR + BR - 1 < rows.total() ? qt * BR + BR - 1 : rows.total() - 1;
+  if (rows.limit(last) <= plan.chunk) return;  // written whole
+  const int lim = rows.limit(R);
+  const int n = lim <= 0 ? 0 : (lim + plan.chunk - 1) / plan.chunk;
+  const int g = threadIdx.x / LD, d = (threadIdx.x % LD) * 4;
+  const float* base = part_of<BR>(const_cast<float*>(parts), ((int64_t)(s * a.c.kv_heads + head) * plan.tiles_q + qt) * plan.n_split, D);
+  float m = -__builtin_inff(), M = m, l = 0.0f;
+  fl4 y = {0, 0, 0, 0};
+  for (int i = g; i < n; i += NP) {
+    const float* p = base + (int64_t)i * (BR * (D + 3));
+    const float mi = p[BR * D + row], Mi = p[BR * D + BR + row], li = p[BR * D + 2 * BR + row];
+    const fl4 yi = *reinterpret_cast<const fl4*>(p + row * D + d);
+    const float mn = fmaxf(m, mi), Mn = fmaxf(M, Mi), mu = finite_or_zero(mn), Mu = finite_or_zero(Mn);
+    l = l * __builtin_amdgcn_exp2f(m - mu) + li * __builtin_amdgcn_exp2f(mi - mu);
+    y = y * __builtin_amdgcn_exp2f(M - Mu) + yi * __builtin_amdgcn_exp2f(Mi - Mu);
+    m = mn;
+    M = Mn;
+  }
+  if (d == 0) {
+    sh_s[g][0] = m;
+    sh_s[g][1] = M;
+    sh_s[g][2] = l;
+  }
+  *reinterpret_cast<fl4*>(&sh_o[g][d]) = y;
+  __syncthreads();
+  if (g) return;
+  m = M = -__builtin_inff();
+#pragma unroll
+  for (int i = 0; i < NP; ++i) {
+    m = fmaxf(m, sh_s[i][0]);
+    M = fmaxf(M, sh_s[i][1]);
+  }
+  const float mu = finite_or_zero(m), Mu = finite_or_zero(M);
+  l = 0.0f;
+  y = fl4{0, 0, 0, 0};
+#pragma unroll
+  for (int i = 0; i < NP; ++i) {
+    l += __builtin_amdgcn_exp2f(sh_s[i][0] - mu) * sh_s[i][2];
+    y += __builtin_amdgcn_exp2f(sh_s[i][1] - Mu) * *reinterpret_cast<const fl4*>(&sh_o[i][d]);
+  }
+  const float f = __builtin_amdgcn_exp2f(Mu - mu);
+  struct alignas(8) Four { T v[4]; } out;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) out.v[e] = (T)(l == 0.0f ? 0.0f : y[e] / l * f);
+  *reinterpret_cast<Four*>(static_cast<T*>(a.out) + rows.at(R, a.ldo, D) + d) = out;
+}
+
+constexpr int kRowTile = 16;  // query rows of a workgroup of k_kv_attention_rows
+
+Plan plan_of(const AttentionArgs& a, int* tile) {
+  const int64_t rows = a.max_new * (a.q_heads / a.c.kv_heads);
+  *tile = kRowTile;
+  Plan p;
+  p.tiles_q = (int)((rows + *tile - 1) / *tile);
+  const int64_t base = (int64_t)a.n_seq * a.c.kv_heads * p.tiles_q;
+  int64_t most = a.table_ld * a.c.page_tokens;
+  if (most > a.max_kv) most = a.max_kv;
+  int64_t split = (2048 + base - 1) / base, cap = (most + 255) / 256;
+  if (split > cap) split = cap;
+  if (split < 1) split = 1;
+  const int64_t chunk = ((most + split - 1) / split + 255) / 256 * 256;
+  p.chunk = (int)(chunk < 256 ? 256 : chunk);
+  p.n_split = (int)((most + p.chunk - 1) / p.chunk);
+  if (p.n_split < 1) p.n_split = 1;
+  return p;
+}
+
 template <typename T, int D>
-hipError_t launch_d(const AttentionArgs& a, hipStream_t st) {
-  const int64_t tiles_q = (a.max_new * (a.q_heads / a.c.kv_heads) + 15) / 16;
-  const int64_t grid = (int64_t)a.n_seq * tiles_q * a.c.kv_heads;
-  if (grid > 0x7FFFFFFF) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((k_kv_attention_rows<T, D>), dim3((unsigned)grid), dim3(256), 0, st, a, tiles_q);
+hipError_t launch_d(const AttentionArgs& a, float* parts, hipStream_t st) {
+  int tile;
+  const Plan p = plan_of(a, &tile);
+  const int64_t base = (int64_t)a.n_seq * a.c.kv_heads * p.tiles_q;
+  if (base * p.n_split > 0x7FFFFFFF || base * tile > 0x7FFFFFFF) return hipErrorInvalidValue;
+  hipLaunchKernelGGL((k_kv_attention_rows<T, D>), dim3((unsigned)(base * p.n_split)), dim3(256), 0, st, a, p, parts);
+  if (p.n_split > 1)
+    hipLaunchKernelGGL((k_kv_attention_join<kRowTile, T, D>), dim3((unsigned)(base * tile)), dim3(256), 0, st, a, p, parts);
   return hipGetLastError();
 }
 
 template <typename T>
-hipError_t launch(const AttentionArgs& a, hipStream_t st) {
-  if (a.c.head_dim == 64) return launch_d<T, 64>(a, st);
-  if (a.c.head_dim == 128) return launch_d<T, 128>(a, st);
-  return launch_d<T, 256>(a, st);
+hipError_t launch(const AttentionArgs& a, float* parts, hipStream_t st) {
+  if (a.c.head_dim == 64) return launch_d<T, 64>(a, parts, st);
+  if (a.c.head_dim == 128) return launch_d<T, 128>(a, parts, st);
+  return launch_d<T, 256>(a, parts, st);
 }
 
 }  // namespace
 
-size_t kv_attention_ws_bytes(const AttentionArgs&) { return 0; }
+size_t kv_attention_ws_bytes(const AttentionArgs& a) {
+  int tile;
+  const Plan p = plan_of(a, &tile);
+  if (p.n_split == 1) return 0;
+  return (size_t)a.n_seq * a.c.kv_heads * p.tiles_q * p.n_split * tile * (a.c.head_dim + 3) * 4;
+}
 
-hipError_t launch_kv_attention(const AttentionArgs& a, void*, hipStream_t st) {
-  if (a.n_rows < 1 || a.max_new < 1) return hipSuccess;
-  return a.dtype == AWSRC_DTYPE_BF16 ? launch<__bf16>(a, st) : launch<_Float16>(a, st);
+hipError_t launch_kv_attention(const AttentionArgs& a, void* ws, hipStream_t st) {
+  float* parts = static_cast<float*>(ws);
+  return a.dtype == AWSRC_DTYPE_BF16 ? launch<__bf16>(a, parts, st) : launch<_Float16>(a, parts, st);
 }
 
 }  // namespace awsrc
