@@ -144,6 +144,7 @@ struct Rows {
 };
 
 // Workgroups of a (sequence, cached head) with BR rows each, and of a split of its tokens.
+constexpr int kMaxSplit = 2048, kFewSplit = 8;
 struct Plan {
   int tiles_q, n_split, chunk;  // chunk: tokens of a split
 };
@@ -152,36 +153,33 @@ __device__ __forceinline__ float* part_of(float* parts, int64_t index, int D) {
   return parts + index * (BR * (D + 3));  // O [BR][D], then m, M and L [BR]
 }
 
-// A query row as fp16 fragments: x[i] for i < N with (channel) index ch(i),
-// brought below 2 by a power of two, times the sign of the scale; `lanes` lanes
-// share the row.  Returns the score's factor.
-template <int LANES, int N, typename T, typename CH>
-__device__ __forceinline__ float load_query(const T* q, bool live, float scale, const CH& ch, h8 (&out)[N / 8]) {
-  h8 raw[N / 8];
-  float qm = 0.0f;
-  float v[N];
+// A query row's N values of a lane, ch(i) the channel of the i-th (8 adjacent ones at a time).
+template <int N, typename T>
+struct Query {
+  struct alignas(16) Piece { T x[8]; };
+  Piece p[N / 8];
+  template <typename CH>
+  __device__ __forceinline__ void fetch(const T* q, const CH& ch) {
 #pragma unroll
-  for (int i = 0; i < N; i += 8) {
-    struct alignas(16) Piece { T x[8]; };
-    Piece p;
-    if (live) p = *reinterpret_cast<const Piece*>(q + ch(i));
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      v[i + e] = live ? to_f32(p.x[e]) : 0.0f;
-      qm = amax_keep(qm, v[i + e]);
-    }
+    for (int i = 0; i < N / 8; ++i) p[i] = *reinterpret_cast<const Piece*>(q + ch(8 * i));
   }
-  if constexpr (LANES == 4) qm = amax_keep(qm, __shfl_xor(qm, 16, 64));
-  qm = amax_keep(qm, __shfl_xor(qm, 32, 64));
-  int e2 = 0;
-  if (qm > 0.0f && qm < __builtin_inff()) e2 = ilogbf(qm);
-  const float sign = scale < 0.0f ? -1.0f : 1.0f;
+  // As fp16 fragments below 2 in magnitude, by a power of two, times the sign of
+  // the scale (0 for a row that is not live); returns the score's factor.
+  template <int LANES>
+  __device__ __forceinline__ float fragments(bool live, float scale, h8 (&out)[N / 8]) const {
+    float qm = 0.0f;
 #pragma unroll
-  for (int i = 0; i < N; ++i) raw[i >> 3][i & 7] = (_Float16)ldexpf(v[i] * sign, -e2);
+    for (int i = 0; i < N; ++i) qm = amax_keep(qm, live ? to_f32(p[i >> 3].x[i & 7]) : 0.0f);
+    if constexpr (LANES == 4) qm = amax_keep(qm, __shfl_xor(qm, 16, 64));
+    qm = amax_keep(qm, __shfl_xor(qm, 32, 64));
+    int e2 = 0;
+    if (qm > 0.0f && qm < __builtin_inff()) e2 = ilogbf(qm);
+    const float sign = scale < 0.0f ? -1.0f : 1.0f;
 #pragma unroll
-  for (int i = 0; i < N / 8; ++i) out[i] = raw[i];
-  return ldexpf(fabsf(scale) * kLog2e, e2);
-}
+    for (int i = 0; i < N; ++i) out[i >> 3][i & 7] = (_Float16)ldexpf(live ? to_f32(p[i >> 3].x[i & 7]) * sign : 0.0f, -e2);
+    return ldexpf(fabsf(scale) * kLog2e, e2);
+  }
+};
 
 // Few rows.  One workgroup: 16 query rows of one (sequence, cached head) and one
 // chunk of its tokens, in tiles of 64 tokens over 4 wavefronts that meet in LDS at
@@ -218,9 +216,11 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 3) void k_kv_attention_rows(Att
   int lim = live ? rows.limit(R0 + r) : 0;
   if (lim > end) lim = end;
 
+  Query<16 * NC, T> query;
+  query.fetch(static_cast<const T*>(a.q) + rows.at(live ? R0 + r : R0, a.ldq, D),
+              [&](int i) { return 64 * (i >> 4) + 16 * g + (i & 8); });
   h8 qa[2 * NC];
-  const float qscale = load_query<4, 16 * NC>(static_cast<const T*>(a.q) + rows.at(live ? R0 + r : R0, a.ldq, D), live, a.scale,
-                                              [&](int i) { return 64 * (i >> 4) + 16 * g + (i & 8); }, qa);
+  const float qscale = query.template fragments<4>(live, a.scale, qa);
   Softmax<1> sm;
   float L = 0.0f;
   fl4 o[ND];
@@ -268,7 +268,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 3) void k_kv_attention_rows(Att
     const int8_t* vb = a.c.v + bv * stride + (int64_t)r * P + (token(t0, g) & (P - 1));
     u32x4_t vw[ND];
 #pragma unroll
-    for (int d = 0; d < ND; ++d) vw[d] = *reinterpret_cast<const u32x4_t*>(vb + 16 * d * P);
+    for (int d = 0; d < ND; ++d) vw[d] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(vb + 16 * d * P));
     fl4 sc[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -361,72 +361,131 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 3) void k_kv_attention_rows(Att
   }
 }
 
-// The sums of a row's splits together: one workgroup per (sequence, query row),
-// its wavefronts over the splits.
+template <typename T>
+__device__ __forceinline__ void store_row4(T* out, fl4 y, float l, float f) {
+  struct alignas(8) Four { T v[4]; } w;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) w.v[e] = (T)(l == 0.0f ? 0.0f : y[e] / l * f);
+  *reinterpret_cast<Four*>(out) = w;
+}
+
+// The sums of a row's splits together, for up to kFewSplit of them: D / 4 lanes a
+// row, every lane with all statistics, so that all loads go out at once and no
+// lane waits for another.
 template <int BR, typename T, int D>
-__global__ __launch_bounds__(256) void k_kv_attention_join(AttentionArgs a, Plan plan, const float* parts) {
-  constexpr int LD = D / 4;        // lanes across a row
-  constexpr int NP = 256 / LD;     // splits taken at once
-  __shared__ float sh_s[NP][3];
-  __shared__ float sh_o[NP][D];
-  const int64_t per_seq = (int64_t)plan.tiles_q * BR;
-  int64_t b = blockIdx.x;
-  const int R = (int)(b % per_seq);
-  b /= per_seq;
-  const int head = (int)(b % a.c.kv_heads), s = (int)(b / a.c.kv_heads);
+__global__ __launch_bounds__(256) void k_kv_attention_join_few(AttentionArgs a, Plan plan, const float* parts, int n_items,
+                                                               int per_head) {
+  constexpr int LD = D / 4;
+  const int item = (int)blockIdx.x * (256 / LD) + threadIdx.x / LD, d = (threadIdx.x % LD) * 4;
+  if (item >= n_items) return;
+  const int sh = item / per_head, s = sh / a.c.kv_heads, R = item - sh * per_head;
   Rows rows;
-  if (!rows.set(a, s, head) || R >= rows.total()) return;
+  if (!rows.set(a, s, sh - s * a.c.kv_heads) || R >= rows.total()) return;
   const int qt = R / BR, row = R - qt * BR;
   const int last = qt * BR + BR - 1 < rows.total() ? qt * BR + BR - 1 : rows.total() - 1;
   if (rows.limit(last) <= plan.chunk) return;  // written whole
-  const int lim = rows.limit(R);
-  const int n = lim <= 0 ? 0 : (lim + plan.chunk - 1) / plan.chunk;
-  const int g = threadIdx.x / LD, d = (threadIdx.x % LD) * 4;
-  const float* base = part_of<BR>(const_cast<float*>(parts), ((int64_t)(s * a.c.kv_heads + head) * plan.tiles_q + qt) * plan.n_split, D);
-  float m = -__builtin_inff(), M = m, l = 0.0f;
+  const int lim = rows.limit(R), n = lim <= 0 ? 0 : (lim + plan.chunk - 1) / plan.chunk;
+  const float* base = part_of<BR>(const_cast<float*>(parts), ((int64_t)sh * plan.tiles_q + qt) * plan.n_split, D);
+  float m[kFewSplit], M[kFewSplit], l[kFewSplit];
+  fl4 y[kFewSplit];
+#pragma unroll
+  for (int i = 0; i < kFewSplit; ++i) {
+    const float* p = base + (int64_t)(i < n ? i : 0) * (BR * (D + 3));  // (split 0 is there whenever a row was split)
+    m[i] = p[BR * D + row];
+    M[i] = p[BR * D + BR + row];
+    l[i] = p[BR * D + 2 * BR + row];
+    y[i] = *reinterpret_cast<const fl4*>(p + row * D + d);
+  }
+  float mx = -__builtin_inff(), Mx = mx;
+#pragma unroll
+  for (int i = 0; i < kFewSplit; ++i) {
+    mx = fmaxf(mx, m[i]);
+    Mx = fmaxf(Mx, M[i]);
+  }
+  mx = finite_or_zero(mx);
+  Mx = finite_or_zero(Mx);
+  float sum = 0.0f;
+  fl4 o = {0, 0, 0, 0};
+#pragma unroll
+  for (int i = 0; i < kFewSplit; ++i)
+    if (i < n) {
+      sum += l[i] * __builtin_amdgcn_exp2f(m[i] - mx);
+      o += y[i] * __builtin_amdgcn_exp2f(M[i] - Mx);
+    }
+  store_row4(static_cast<T*>(a.out) + rows.at(R, a.ldo, D) + d, o, sum, __builtin_amdgcn_exp2f(Mx - mx));
+}
+
+// The same for more splits: a workgroup per row weighs them by their maxima
+// first, so that the sums' loads do not wait for one another.
+template <int BR, typename T, int D>
+__global__ __launch_bounds__(256) void k_kv_attention_join(AttentionArgs a, Plan plan, const float* parts, int per_head) {
+  constexpr int LD = D / 4;    // lanes across a row
+  constexpr int NP = 256 / LD; // splits summed at once
+  __shared__ float sh_w[kMaxSplit];
+  __shared__ float sh_s[4][3];
+  __shared__ fl4 sh_o[NP][LD];
+  const int t = threadIdx.x, wave = t >> 6;
+  const int sh = (int)blockIdx.x / per_head, s = sh / a.c.kv_heads, R = (int)blockIdx.x - sh * per_head;
+  Rows rows;
+  if (!rows.set(a, s, sh - s * a.c.kv_heads) || R >= rows.total()) return;
+  const int qt = R / BR, row = R - qt * BR;
+  const int last = qt * BR + BR - 1 < rows.total() ? qt * BR + BR - 1 : rows.total() - 1;
+  if (rows.limit(last) <= plan.chunk) return;  // written whole
+  const int lim = rows.limit(R), n = lim <= 0 ? 0 : (lim + plan.chunk - 1) / plan.chunk;
+  const float* base = part_of<BR>(const_cast<float*>(parts), ((int64_t)sh * plan.tiles_q + qt) * plan.n_split, D);
+  const int64_t step = BR * (D + 3);
+  float m = -__builtin_inff(), M = m;
+  for (int i = t; i < n; i += 256) {
+    const float* p = base + i * step + BR * D + row;
+    m = fmaxf(m, p[0]);
+    M = fmaxf(M, p[BR]);
+  }
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) {
+    m = fmaxf(m, __shfl_xor(m, off, 64));
+    M = fmaxf(M, __shfl_xor(M, off, 64));
+  }
+  if ((t & 63) == 0) {
+    sh_s[wave][0] = m;
+    sh_s[wave][1] = M;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    m = fmaxf(m, sh_s[w][0]);
+    M = fmaxf(M, sh_s[w][1]);
+  }
+  m = finite_or_zero(m);
+  M = finite_or_zero(M);
+  float l = 0.0f;
+  for (int i = t; i < n; i += 256) {
+    const float* p = base + i * step + BR * D + row;
+    l += p[2 * BR] * __builtin_amdgcn_exp2f(p[0] - m);
+    sh_w[i] = __builtin_amdgcn_exp2f(p[BR] - M);
+  }
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) l += __shfl_xor(l, off, 64);
+  if ((t & 63) == 0) sh_s[wave][2] = l;
+  __syncthreads();
+  const int g = t / LD, d = t % LD;
   fl4 y = {0, 0, 0, 0};
-  for (int i = g; i < n; i += NP) {
-    const float* p = base + (int64_t)i * (BR * (D + 3));
-    const float mi = p[BR * D + row], Mi = p[BR * D + BR + row], li = p[BR * D + 2 * BR + row];
-    const fl4 yi = *reinterpret_cast<const fl4*>(p + row * D + d);
-    const float mn = fmaxf(m, mi), Mn = fmaxf(M, Mi), mu = finite_or_zero(mn), Mu = finite_or_zero(Mn);
-    l = l * __builtin_amdgcn_exp2f(m - mu) + li * __builtin_amdgcn_exp2f(mi - mu);
-    y = y * __builtin_amdgcn_exp2f(M - Mu) + yi * __builtin_amdgcn_exp2f(Mi - Mu);
-    m = mn;
-    M = Mn;
-  }
-  if (d == 0) {
-    sh_s[g][0] = m;
-    sh_s[g][1] = M;
-    sh_s[g][2] = l;
-  }
-  *reinterpret_cast<fl4*>(&sh_o[g][d]) = y;
+#pragma unroll 8
+  for (int i = g; i < n; i += NP) y += sh_w[i] * *reinterpret_cast<const fl4*>(base + i * step + row * D + 4 * d);
+  sh_o[g][d] = y;
   __syncthreads();
   if (g) return;
-  m = M = -__builtin_inff();
 #pragma unroll
-  for (int i = 0; i < NP; ++i) {
-    m = fmaxf(m, sh_s[i][0]);
-    M = fmaxf(M, sh_s[i][1]);
-  }
-  const float mu = finite_or_zero(m), Mu = finite_or_zero(M);
-  l = 0.0f;
-  y = fl4{0, 0, 0, 0};
-#pragma unroll
-  for (int i = 0; i < NP; ++i) {
-    l += __builtin_amdgcn_exp2f(sh_s[i][0] - mu) * sh_s[i][2];
-    y += __builtin_amdgcn_exp2f(sh_s[i][1] - Mu) * *reinterpret_cast<const fl4*>(&sh_o[i][d]);
-  }
-  const float f = __builtin_amdgcn_exp2f(Mu - mu);
-  struct alignas(8) Four { T v[4]; } out;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) out.v[e] = (T)(l == 0.0f ? 0.0f : y[e] / l * f);
-  *reinterpret_cast<Four*>(static_cast<T*>(a.out) + rows.at(R, a.ldo, D) + d) = out;
+  for (int i = 1; i < NP; ++i) y += sh_o[i][d];
+  l = sh_s[0][2] + sh_s[1][2] + sh_s[2][2] + sh_s[3][2];
+  store_row4(static_cast<T*>(a.out) + rows.at(R, a.ldo, D) + 4 * d, y, l, __builtin_amdgcn_exp2f(M - m));
 }
 
 constexpr int kRowTile = 16;  // query rows of a workgroup of k_kv_attention_rows
 
 Plan plan_of(const AttentionArgs& a, int* tile) {
+  // Splits: about 1024 workgroups (2 x 131071 tokens of a group of 8: 34 us, 38 with 2048), but
+  // at least 256 tokens each (1501 tokens: 11.0 us, 12.1 with 512).
+  const int64_t target = 1024, least = 256;
   const int64_t rows = a.max_new * (a.q_heads / a.c.kv_heads);
   *tile = kRowTile;
   Plan p;
@@ -434,8 +493,9 @@ Plan plan_of(const AttentionArgs& a, int* tile) {
   const int64_t base = (int64_t)a.n_seq * a.c.kv_heads * p.tiles_q;
   int64_t most = a.table_ld * a.c.page_tokens;
   if (most > a.max_kv) most = a.max_kv;
-  int64_t split = (2048 + base - 1) / base, cap = (most + 255) / 256;
+  int64_t split = (target + base - 1) / base, cap = (most + least - 1) / least;
   if (split > cap) split = cap;
+  if (split > kMaxSplit) split = kMaxSplit;
   if (split < 1) split = 1;
   const int64_t chunk = ((most + split - 1) / split + 255) / 256 * 256;
   p.chunk = (int)(chunk < 256 ? 256 : chunk);
@@ -444,15 +504,26 @@ Plan plan_of(const AttentionArgs& a, int* tile) {
   return p;
 }
 
+template <int BR, typename T, int D>
+hipError_t launch_join(const AttentionArgs& a, const Plan& p, const float* parts, hipStream_t st) {
+  const int64_t per_head = a.max_new * (a.q_heads / a.c.kv_heads), items = (int64_t)a.n_seq * a.c.kv_heads * per_head;
+  if (items > 0x7FFFFFFF) return hipErrorInvalidValue;
+  if (p.n_split <= kFewSplit)
+    hipLaunchKernelGGL((k_kv_attention_join_few<BR, T, D>), dim3((unsigned)((items * (D / 4) + 255) / 256)), dim3(256), 0, st, a, p,
+                       parts, (int)items, (int)per_head);
+  else
+    hipLaunchKernelGGL((k_kv_attention_join<BR, T, D>), dim3((unsigned)items), dim3(256), 0, st, a, p, parts, (int)per_head);
+  return hipGetLastError();
+}
+
 template <typename T, int D>
 hipError_t launch_d(const AttentionArgs& a, float* parts, hipStream_t st) {
   int tile;
   const Plan p = plan_of(a, &tile);
   const int64_t base = (int64_t)a.n_seq * a.c.kv_heads * p.tiles_q;
-  if (base * p.n_split > 0x7FFFFFFF || base * tile > 0x7FFFFFFF) return hipErrorInvalidValue;
+  if (base * p.n_split > 0x7FFFFFFF) return hipErrorInvalidValue;
   hipLaunchKernelGGL((k_kv_attention_rows<T, D>), dim3((unsigned)(base * p.n_split)), dim3(256), 0, st, a, p, parts);
-  if (p.n_split > 1)
-    hipLaunchKernelGGL((k_kv_attention_join<kRowTile, T, D>), dim3((unsigned)(base * tile)), dim3(256), 0, st, a, p, parts);
+  if (p.n_split > 1) return launch_join<kRowTile, T, D>(a, p, parts, st);
   return hipGetLastError();
 }
 
