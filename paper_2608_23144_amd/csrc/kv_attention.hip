@@ -143,9 +143,10 @@ struct Rows {
   }
 };
 
-// Workgroups of a (sequence, cached head) with BR rows each, and of a split of its tokens.
+constexpr int kRowTile = 16, kTileRows = 128;  // of the two kernels
 constexpr int kMaxSplit = 2048, kFewSplit = 8;
 struct Plan {
+  int tile;                     // query rows of a workgroup
   int tiles_q, n_split, chunk;  // chunk: tokens of a split
 };
 template <int BR>
@@ -369,6 +370,265 @@ __device__ __forceinline__ void store_row4(T* out, fl4 y, float l, float f) {
   *reinterpret_cast<Four*>(out) = w;
 }
 
+// Many rows.  One workgroup: 128 query rows of one (sequence, cached head), 32 a
+// wavefront, over tiles of 64 tokens whose codes become fp16 once, on their way
+// into LDS (two stages), and then serve all four wavefronts through 32 x 32 x 16
+// products.  The next tile's codes are on their way from memory while the
+// current one is computed.
+//
+// Lane l (half h = l / 32) holds query l % 32.  Row 8 b + 4 h + i of a 32-token score
+// tile is token 16 h + 4 b + i.  Keys lie in LDS as [row][channel], values as
+// [channel][token], in pieces of 16 bytes at place p ^ (row % 8), so that 8 lanes
+// reading one piece of 8 rows meet 8 different banks.
+template <int D>
+struct TileLds {
+  static constexpr int kKeys = 64 * D * 2, kValues = D * 64 * 2;
+  static constexpr int kStage = kKeys + kValues;
+  // per stage and 16-token run: key scale, value scale, page (negative: none); pages of the tile after
+  static constexpr int kBytes = 2 * kStage + 2 * 4 * 12 + 2 * 4 * 4;
+};
+
+template <typename T, int D>
+__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_kv_attention_tiles(AttentionArgs a, Plan plan, float* parts) {
+  constexpr int BR = kTileRows;
+  constexpr int NS = D / 16;   // 16-channel steps of the scores
+  constexpr int ND = D / 32;   // 32-channel tiles of the output
+  constexpr int NL = D / 64;   // 16-byte runs of codes a thread moves per tile, of keys and of values
+  using S = TileLds<D>;
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  float* run_k = reinterpret_cast<float*>(lds + 2 * S::kStage);  // [2][4]
+  float* run_v = run_k + 8;
+  int* run_page = reinterpret_cast<int*>(run_v + 8);
+  int* next_page = run_page + 8;  // [2][4], by parity of the tile
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int r = lane & 31, h = lane >> 5;
+  int b = blockIdx.x;
+  const int head = b % a.c.kv_heads;
+  b /= a.c.kv_heads;
+  // the last rows see the most tokens: they start first
+  const int qt = plan.tiles_q - 1 - b % plan.tiles_q;
+  b /= plan.tiles_q;
+  const int split = b % plan.n_split, s = b / plan.n_split;
+  Rows rows;
+  if (!rows.set(a, s, head)) return;
+  const int R0 = qt * BR, n_rows = rows.total() - R0;
+  if (n_rows <= 0) return;
+  const int full = rows.limit(R0 + (n_rows < BR ? n_rows : BR) - 1);
+  const int start = split * plan.chunk;
+  if (split && start >= full) return;
+  const int end = full < start + plan.chunk ? full : start + plan.chunk;
+  const int R = R0 + wave * 32 + r;
+  const bool live = wave * 32 + r < n_rows;
+  int lim = live ? rows.limit(R) : 0;
+  if (lim > end) lim = end;
+  // tokens that every row of the wavefront sees: tiles below need no masks
+  int all = rows.limit(R0 + wave * 32 < rows.total() ? R0 + wave * 32 : rows.total() - 1);
+  if (all > end) all = end;
+  // tokens that any row of the wavefront sees
+  const int top_row = R0 + wave * 32 + 31 < rows.total() ? R0 + wave * 32 + 31 : rows.total() - 1;
+  int any = wave * 32 < n_rows ? rows.limit(top_row) : 0;
+  if (any > end) any = end;
+
+  Query<8 * NS, T> query;
+  query.fetch(static_cast<const T*>(a.q) + rows.at(live ? R : R0, a.ldq, D), [&](int i) { return 2 * i + 8 * h; });
+  h8 qa[NS];
+  const float qscale = query.template fragments<2>(live, a.scale, qa);
+
+  const int32_t* table = a.table + (int64_t)s * a.table_ld;
+  const int P = a.c.page_tokens, shift = __builtin_ctz(P);
+  const int64_t stride = (int64_t)P * D;
+  // this thread's runs: of keys, tokens (tid + 256 i) / (D / 16) from channel 16 (tid % (D / 16)); of values,
+  // channel (tid + 256 i) / 4, tokens from 16 (tid % 4)
+  constexpr int KR = D / 16;
+  const auto page_at = [&](int t0, int run) -> int {  // tokens past the end take the tile's first page (masked)
+    const int p = table[(t0 + 16 * run < end ? t0 + 16 * run : t0) >> shift];
+    return p >= 0 && p < a.c.n_pages ? p : -1;
+  };
+  u32x4_t kw[NL], vw[NL];
+  float gk = 0.0f, gv = 0.0f;
+  int gp = -1;
+  const auto block_of = [&](int page) { return (int64_t)(page < 0 ? 0 : page) * a.c.kv_heads + head; };
+  const auto load = [&](int t0, const int* pages) {
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int x = tid + 256 * i, t = x / KR, c = x % KR;
+      const int slot = ((t0 + (t & ~15) < end ? t0 + (t & ~15) : t0) & (P - 1)) + (t & 15);
+      kw[i] = *reinterpret_cast<const u32x4_t*>(a.c.k + block_of(pages[t >> 4]) * stride + slot * D + 16 * c);
+    }
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int x = tid + 256 * i, d = x >> 2, g = x & 3;
+      const int slot = (t0 + 16 * g < end ? t0 + 16 * g : t0) & (P - 1);
+      vw[i] = *reinterpret_cast<const u32x4_t*>(a.c.v + block_of(pages[g]) * stride + (int64_t)d * P + slot);
+    }
+    if (tid < 4) {
+      gp = pages[tid];
+      gk = a.c.k_scale[block_of(gp)];
+      gv = a.c.v_scale[block_of(gp)];
+    }
+  };
+  const auto store = [&](int stage) {
+    char* base = lds + stage * S::kStage;
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int x = tid + 256 * i, t = x / KR, c = x % KR;
+      // token 32 u + 16 h + 4 b + e is row 32 u + 8 b + 4 h + e
+      const int row = (t & 32) | ((t >> 2) & 3) << 3 | ((t >> 4) & 1) << 2 | (t & 3);
+      char* o = base + row * 2 * D;
+      *reinterpret_cast<h8*>(o + ((2 * c) ^ (row & 7)) * 16) = codes_to_f16x8(kw[i][0], kw[i][1]);
+      *reinterpret_cast<h8*>(o + ((2 * c + 1) ^ (row & 7)) * 16) = codes_to_f16x8(kw[i][2], kw[i][3]);
+    }
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int x = tid + 256 * i, d = x >> 2, g = x & 3;
+      char* o = base + S::kKeys + d * 128;
+      *reinterpret_cast<h8*>(o + ((2 * g) ^ (d & 7)) * 16) = codes_to_f16x8(vw[i][0], vw[i][1]);
+      *reinterpret_cast<h8*>(o + ((2 * g + 1) ^ (d & 7)) * 16) = codes_to_f16x8(vw[i][2], vw[i][3]);
+    }
+    if (tid < 4) {
+      run_k[stage * 4 + tid] = gk;
+      run_v[stage * 4 + tid] = gv;
+      run_page[stage * 4 + tid] = gp;
+    }
+  };
+
+  Softmax<2> sm;
+  float L = 0.0f;
+  fl16 o[ND];
+#pragma unroll
+  for (int d = 0; d < ND; ++d)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[d][e] = 0.0f;
+
+  if (start < end) {  // (uniform)
+    if (tid < 4) {
+      next_page[tid] = page_at(start, tid);
+      if (start + 64 < end) next_page[4 + tid] = page_at(start + 64, tid);
+    }
+    __syncthreads();
+    load(start, next_page);
+    store(0);
+    __syncthreads();
+  }
+  int stage = 0;
+  for (int t0 = start; t0 < end; t0 += 64, stage ^= 1) {
+    const bool more = t0 + 64 < end;
+    int page_after = -1;
+    if (more) {
+      load(t0 + 64, next_page + 4 * (stage ^ 1));
+      if (tid < 4 && t0 + 128 < end) page_after = page_at(t0 + 128, tid);
+    }
+    if (t0 < any) {
+      const char* base = lds + stage * S::kStage;
+      fl16 sc[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sc[u][e] = 0.0f;
+        const char* row = base + (32 * u + r) * 2 * D;
+#pragma unroll
+        for (int k = 0; k < NS; ++k)
+          sc[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const h8*>(row + ((2 * k + h) ^ (r & 7)) * 16), qa[k],
+                                                         sc[u], 0, 0, 0);
+      }
+      float sk[2], sv[2], run[2];
+      bool seen[2];
+      int left[2];
+      bool whole = t0 + 64 <= all;
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int g = stage * 4 + 2 * u + h;
+        sk[u] = run_k[g] * qscale;
+        sv[u] = run_v[g];
+        const bool ok = run_page[g] >= 0;
+        whole = whole && ok;
+        left[u] = ok ? lim - (t0 + 32 * u + 16 * h) : 0;
+        seen[u] = left[u] > 0;
+      }
+      whole = __all(whole);
+      if (!whole) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) sc[u][e] = e < left[u] ? sc[u][e] : -__builtin_inff();
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        float x = sc[u][0];
+#pragma unroll
+        for (int e = 1; e < 16; ++e) x = fmaxf(x, sc[u][e]);
+        run[u] = seen[u] ? x * sk[u] : -__builtin_inff();
+      }
+      float alpha_l, alpha_o;
+      if (softmax_step<2, 2>(sm, run, sv, seen, alpha_l, alpha_o)) {
+        L *= alpha_l;
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) o[d][e] *= alpha_o;
+      }
+      h8 ph[2][2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        float l = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          float p = __builtin_amdgcn_exp2f(sc[u][e] * sk[u] + sm.off[u]);
+          if (!whole) p = e < left[u] ? p : 0.0f;
+          l += p;
+          ph[u][e >> 3][e & 7] = (_Float16)p;
+        }
+        L += l * sm.f[u];
+      }
+      if (__any(sm.quiet[0] || sm.quiet[1])) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+          if (sm.quiet[u]) ph[u][0] = ph[u][1] = h8{0, 0, 0, 0, 0, 0, 0, 0};
+      }
+#pragma unroll
+      for (int d = 0; d < ND; ++d) {
+        const char* row = base + S::kKeys + (32 * d + r) * 128;
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int k = 0; k < 2; ++k)
+            o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+                *reinterpret_cast<const h8*>(row + ((4 * u + 2 * h + k) ^ (r & 7)) * 16), ph[u][k], o[d], 0, 0, 0);
+      }
+    }
+    if (more) {
+      store(stage ^ 1);
+      if (tid < 4) next_page[4 * stage + tid] = page_after;
+    }
+    __syncthreads();
+  }
+  L += __shfl_xor(L, 32, 64);
+  if (!live) return;
+  // lane: channels 32 d + 8 b + 4 h + e of its query
+  if (full <= plan.chunk) {
+    const float f = __builtin_amdgcn_exp2f(finite_or_zero(sm.M) - finite_or_zero(sm.m));
+    T* out = static_cast<T*>(a.out) + rows.at(R, a.ldo, D) + 4 * h;
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+      for (int e = 0; e < 16; e += 4)
+        store_row4(out + 32 * d + 2 * e, fl4{o[d][e], o[d][e + 1], o[d][e + 2], o[d][e + 3]}, L, f);
+  } else {
+    float* part = part_of<BR>(parts, ((int64_t)(s * a.c.kv_heads + head) * plan.tiles_q + qt) * plan.n_split + split, D);
+    const int row = wave * 32 + r;
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+      for (int e = 0; e < 16; e += 4)
+        *reinterpret_cast<fl4*>(part + row * D + 32 * d + 2 * e + 4 * h) = fl4{o[d][e], o[d][e + 1], o[d][e + 2], o[d][e + 3]};
+    if (h == 0) {
+      part[BR * D + row] = sm.m;
+      part[BR * D + BR + row] = sm.M;
+      part[BR * D + 2 * BR + row] = L;
+    }
+  }
+}
+
 // The sums of a row's splits together, for up to kFewSplit of them: D / 4 lanes a
 // row, every lane with all statistics, so that all loads go out at once and no
 // lane waits for another.
@@ -480,20 +740,20 @@ __global__ __launch_bounds__(256) void k_kv_attention_join(AttentionArgs a, Plan
   store_row4(static_cast<T*>(a.out) + rows.at(R, a.ldo, D) + 4 * d, y, l, __builtin_amdgcn_exp2f(M - m));
 }
 
-constexpr int kRowTile = 16;  // query rows of a workgroup of k_kv_attention_rows
-
-Plan plan_of(const AttentionArgs& a, int* tile) {
-  // Splits: about 1024 workgroups (2 x 131071 tokens of a group of 8: 34 us, 38 with 2048), but
-  // at least 256 tokens each (1501 tokens: 11.0 us, 12.1 with 512).
-  const int64_t target = 1024, least = 256;
+// Which kernel, and how the tokens are split.
+Plan plan_of(const AttentionArgs& a) {
   const int64_t rows = a.max_new * (a.q_heads / a.c.kv_heads);
-  *tile = kRowTile;
   Plan p;
-  p.tiles_q = (int)((rows + *tile - 1) / *tile);
+  p.tile = rows > 64 ? kTileRows : kRowTile;
+  p.tiles_q = (int)((rows + p.tile - 1) / p.tile);
   const int64_t base = (int64_t)a.n_seq * a.c.kv_heads * p.tiles_q;
   int64_t most = a.table_ld * a.c.page_tokens;
   if (most > a.max_kv) most = a.max_kv;
-  int64_t split = (target + base - 1) / base, cap = (most + least - 1) / least;
+  // Splits: about 1024 workgroups (2 x 131071 tokens of a group of 8: 34 us, 38 with 2048), but
+  // at least 256 tokens each (1501 tokens: 11.0 us, 12.1 with 512).
+  const int64_t target = p.tile == kTileRows ? 512 : 1024, least = p.tile == kTileRows ? 512 : 256;
+  int64_t split = p.tile == kTileRows ? target / base : (target + base - 1) / base;
+  const int64_t cap = (most + least - 1) / least;
   if (split > cap) split = cap;
   if (split > kMaxSplit) split = kMaxSplit;
   if (split < 1) split = 1;
@@ -518,12 +778,22 @@ hipError_t launch_join(const AttentionArgs& a, const Plan& p, const float* parts
 
 template <typename T, int D>
 hipError_t launch_d(const AttentionArgs& a, float* parts, hipStream_t st) {
-  int tile;
-  const Plan p = plan_of(a, &tile);
-  const int64_t base = (int64_t)a.n_seq * a.c.kv_heads * p.tiles_q;
-  if (base * p.n_split > 0x7FFFFFFF) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((k_kv_attention_rows<T, D>), dim3((unsigned)(base * p.n_split)), dim3(256), 0, st, a, p, parts);
-  if (p.n_split > 1) return launch_join<kRowTile, T, D>(a, p, parts, st);
+  const Plan p = plan_of(a);
+  const int64_t grid = (int64_t)a.n_seq * a.c.kv_heads * p.tiles_q * p.n_split;
+  if (grid > 0x7FFFFFFF) return hipErrorInvalidValue;
+  if (p.tile == kRowTile) {
+    hipLaunchKernelGGL((k_kv_attention_rows<T, D>), dim3((unsigned)grid), dim3(256), 0, st, a, p, parts);
+    if (p.n_split > 1) return launch_join<kRowTile, T, D>(a, p, parts, st);
+    return hipGetLastError();
+  }
+  const auto k = k_kv_attention_tiles<T, D>;
+  constexpr int bytes = TileLds<D>::kBytes;
+  if (bytes > 65536) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL(k, dim3((unsigned)grid), dim3(256), bytes, st, a, p, parts);
+  if (p.n_split > 1) return launch_join<kTileRows, T, D>(a, p, parts, st);
   return hipGetLastError();
 }
 
@@ -537,10 +807,9 @@ hipError_t launch(const AttentionArgs& a, float* parts, hipStream_t st) {
 }  // namespace
 
 size_t kv_attention_ws_bytes(const AttentionArgs& a) {
-  int tile;
-  const Plan p = plan_of(a, &tile);
+  const Plan p = plan_of(a);
   if (p.n_split == 1) return 0;
-  return (size_t)a.n_seq * a.c.kv_heads * p.tiles_q * p.n_split * tile * (a.c.head_dim + 3) * 4;
+  return (size_t)a.n_seq * a.c.kv_heads * p.tiles_q * p.n_split * p.tile * (a.c.head_dim + 3) * 4;
 }
 
 hipError_t launch_kv_attention(const AttentionArgs& a, void* ws, hipStream_t st) {
