@@ -64,8 +64,15 @@ struct Softmax {
   bool quiet[U];                // the run's page adds nothing to the output
 };
 constexpr float kLag = 8.0f;
+// p' is kept this much (log2) above 1 at its maximum, out of fp16's subnormals
+// for weights down to 2^-20 of the largest; with the lag it reaches 2^14
+constexpr float kLift = 6.0f;
 
 __device__ __forceinline__ float finite_or_zero(float m) { return m == -__builtin_inff() ? 0.0f : m; }
+// the factor of (sum p' c) / (sum p) in the output
+__device__ __forceinline__ float output_factor(float m, float M) {
+  return __builtin_amdgcn_exp2f(finite_or_zero(M) - kLift - finite_or_zero(m));
+}
 
 // Largest value over a row's lanes: those 16 and 32 apart (four lanes a row) or 32 apart (two).
 template <int LANES>
@@ -98,7 +105,7 @@ __device__ __forceinline__ bool softmax_step(Softmax<U>& s, const float (&run)[U
     s.m = mn;
     s.M = Mn;
   }
-  const float mu = finite_or_zero(s.m), Mu = finite_or_zero(s.M);
+  const float mu = finite_or_zero(s.m), Mu = finite_or_zero(s.M) - kLift;
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const float gap = Mu - mu - lsv[u];
@@ -346,7 +353,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 3) void k_kv_attention_rows(Att
       y += __builtin_amdgcn_exp2f(sh_M[w][row] - Mu) * *reinterpret_cast<const fl4*>(&sh_o[w][row][d]);
     }
     if (whole) {
-      const float f = __builtin_amdgcn_exp2f(Mu - mu);
+      const float f = output_factor(m, M);
       struct alignas(8) Four { T v[4]; } out;
 #pragma unroll
       for (int e = 0; e < 4; ++e) out.v[e] = (T)(l == 0.0f ? 0.0f : y[e] / l * f);
@@ -378,10 +385,12 @@ __device__ __forceinline__ void store_row4(T* out, fl4 y, float l, float f) {
 //
 // Lane l (half h = l / 32) holds query l % 32.  Row 8 b + 4 h + i of a 32-token score
 // tile is token 16 h + 4 b + i.  Keys lie in LDS as [row][channel], values as
-// [channel][token], in pieces of 16 bytes at place p ^ (row % 8), so that 8 lanes
-// reading one piece of 8 rows meet 8 different banks.
+// [channel][token], in pieces of 16 bytes at place p ^ key(row), so that the 16
+// lanes that LDS serves at once, reading one piece of 16 rows, meet all its banks.
+__device__ __forceinline__ int value_key(int d) { return (d >> 1) & 7; }
 template <int D>
 struct TileLds {
+  static __device__ __forceinline__ int key(int row) { return D == 64 ? (row >> 1) & 7 : row & 15; }
   static constexpr int kKeys = 64 * D * 2, kValues = D * 64 * 2;
   static constexpr int kStage = kKeys + kValues;
   // per stage and 16-token run: key scale, value scale, page (negative: none); pages of the tile after
@@ -475,15 +484,15 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_kv_attention_tiles(At
       // token 32 u + 16 h + 4 b + e is row 32 u + 8 b + 4 h + e
       const int row = (t & 32) | ((t >> 2) & 3) << 3 | ((t >> 4) & 1) << 2 | (t & 3);
       char* o = base + row * 2 * D;
-      *reinterpret_cast<h8*>(o + ((2 * c) ^ (row & 7)) * 16) = codes_to_f16x8(kw[i][0], kw[i][1]);
-      *reinterpret_cast<h8*>(o + ((2 * c + 1) ^ (row & 7)) * 16) = codes_to_f16x8(kw[i][2], kw[i][3]);
+      *reinterpret_cast<h8*>(o + ((2 * c) ^ S::key(row)) * 16) = codes_to_f16x8(kw[i][0], kw[i][1]);
+      *reinterpret_cast<h8*>(o + ((2 * c + 1) ^ S::key(row)) * 16) = codes_to_f16x8(kw[i][2], kw[i][3]);
     }
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
       const int x = tid + 256 * i, d = x >> 2, g = x & 3;
       char* o = base + S::kKeys + d * 128;
-      *reinterpret_cast<h8*>(o + ((2 * g) ^ (d & 7)) * 16) = codes_to_f16x8(vw[i][0], vw[i][1]);
-      *reinterpret_cast<h8*>(o + ((2 * g + 1) ^ (d & 7)) * 16) = codes_to_f16x8(vw[i][2], vw[i][3]);
+      *reinterpret_cast<h8*>(o + ((2 * g) ^ value_key(d)) * 16) = codes_to_f16x8(vw[i][0], vw[i][1]);
+      *reinterpret_cast<h8*>(o + ((2 * g + 1) ^ value_key(d)) * 16) = codes_to_f16x8(vw[i][2], vw[i][3]);
     }
     if (tid < 4) {
       run_k[stage * 4 + tid] = gk;
@@ -528,7 +537,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_kv_attention_tiles(At
         const char* row = base + (32 * u + r) * 2 * D;
 #pragma unroll
         for (int k = 0; k < NS; ++k)
-          sc[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const h8*>(row + ((2 * k + h) ^ (r & 7)) * 16), qa[k],
+          sc[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const h8*>(row + ((2 * k + h) ^ S::key(r)) * 16), qa[k],
                                                          sc[u], 0, 0, 0);
       }
       float sk[2], sv[2], run[2];
@@ -538,15 +547,17 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_kv_attention_tiles(At
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         const int g = stage * 4 + 2 * u + h;
-        sk[u] = run_k[g] * qscale;
-        sv[u] = run_v[g];
         const bool ok = run_page[g] >= 0;
         whole = whole && ok;
         left[u] = ok ? lim - (t0 + 32 * u + 16 * h) : 0;
         seen[u] = left[u] > 0;
+        // unseen scores become -inf: no product of one with 0 (2^-120 does as well) or NaN
+        sk[u] = run_k[g] * qscale;
+        sk[u] = !seen[u] ? 1.0f : sk[u] == 0.0f ? 0x1p-120f : sk[u];
+        sv[u] = run_v[g];
       }
-      whole = __all(whole);
-      if (!whole) {
+      if (!__all(whole)) {
+        asm volatile("");  // keeps this a branch: nearly every tile is seen whole
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -557,7 +568,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_kv_attention_tiles(At
         float x = sc[u][0];
 #pragma unroll
         for (int e = 1; e < 16; ++e) x = fmaxf(x, sc[u][e]);
-        run[u] = seen[u] ? x * sk[u] : -__builtin_inff();
+        run[u] = x * sk[u];
       }
       float alpha_l, alpha_o;
       if (softmax_step<2, 2>(sm, run, sv, seen, alpha_l, alpha_o)) {
@@ -573,8 +584,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_kv_attention_tiles(At
         float l = 0.0f;
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          float p = __builtin_amdgcn_exp2f(sc[u][e] * sk[u] + sm.off[u]);
-          if (!whole) p = e < left[u] ? p : 0.0f;
+          const float p = __builtin_amdgcn_exp2f(sc[u][e] * sk[u] + sm.off[u]);
           l += p;
           ph[u][e >> 3][e & 7] = (_Float16)p;
         }
@@ -593,7 +603,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_kv_attention_tiles(At
 #pragma unroll
           for (int k = 0; k < 2; ++k)
             o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
-                *reinterpret_cast<const h8*>(row + ((4 * u + 2 * h + k) ^ (r & 7)) * 16), ph[u][k], o[d], 0, 0, 0);
+                *reinterpret_cast<const h8*>(row + ((4 * u + 2 * h + k) ^ value_key(r)) * 16), ph[u][k], o[d], 0, 0, 0);
       }
     }
     if (more) {
@@ -606,7 +616,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_kv_attention_tiles(At
   if (!live) return;
   // lane: channels 32 d + 8 b + 4 h + e of its query
   if (full <= plan.chunk) {
-    const float f = __builtin_amdgcn_exp2f(finite_or_zero(sm.M) - finite_or_zero(sm.m));
+    const float f = output_factor(sm.m, sm.M);
     T* out = static_cast<T*>(a.out) + rows.at(R, a.ldo, D) + 4 * h;
 #pragma unroll
     for (int d = 0; d < ND; ++d)
@@ -672,7 +682,7 @@ __global__ __launch_bounds__(256) void k_kv_attention_join_few(AttentionArgs a, 
       sum += l[i] * __builtin_amdgcn_exp2f(m[i] - mx);
       o += y[i] * __builtin_amdgcn_exp2f(M[i] - Mx);
     }
-  store_row4(static_cast<T*>(a.out) + rows.at(R, a.ldo, D) + d, o, sum, __builtin_amdgcn_exp2f(Mx - mx));
+  store_row4(static_cast<T*>(a.out) + rows.at(R, a.ldo, D) + d, o, sum, output_factor(mx, Mx));
 }
 
 // The same for more splits: a workgroup per row weighs them by their maxima
@@ -737,7 +747,7 @@ __global__ __launch_bounds__(256) void k_kv_attention_join(AttentionArgs a, Plan
 #pragma unroll
   for (int i = 1; i < NP; ++i) y += sh_o[i][d];
   l = sh_s[0][2] + sh_s[1][2] + sh_s[2][2] + sh_s[3][2];
-  store_row4(static_cast<T*>(a.out) + rows.at(R, a.ldo, D) + 4 * d, y, l, __builtin_amdgcn_exp2f(M - m));
+  store_row4(static_cast<T*>(a.out) + rows.at(R, a.ldo, D) + 4 * d, y, l, output_factor(m, M));
 }
 
 // Which kernel, and how the tokens are split.

@@ -108,9 +108,10 @@ __global__ __launch_bounds__(64 * W) void k_matmul_i8_rows(LinearArgs a) {
 // wavefront WM x WN of them as 32 x 32 tiles of v_mfma_i32_32x32x32_i8.  The sum
 // advances 128 bytes at a time through two LDS stages filled by direct
 // global-to-LDS loads, which leave the registers to the sums.  A stage's rows
-// of 128 bytes are 8 pieces of 16; piece p of row r lies at place p ^ key(r), with
-// keys that differ over any 8 lanes that read together, so that neither the
-// fragment reads nor the fills collide in banks.  The fills of step t + 1 and the
+// of 128 bytes are 8 pieces of 16; piece p of row r lies at place p ^ key(r).  LDS
+// serves 16 lanes a cycle (64 banks), two rows side by side: over the 16 rows
+// that a fragment read takes together, (row % 2, key) takes 16 values.  (Keys of
+// 8 rows, row % 8, took twice the cycles.)  The fills of step t + 1 and the
 // fragment reads of the next 32 bytes are issued before the products of the
 // current ones.
 //
@@ -122,8 +123,8 @@ __global__ __launch_bounds__(64 * W) void k_matmul_i8_rows(LinearArgs a) {
 // that a lane (half h) ends with 16 consecutive columns of one result row.
 constexpr int kStep = 128;
 
-__device__ __forceinline__ int key_a(int row) { return row & 7; }
-__device__ __forceinline__ int key_b(int row) { return (row & 3) | ((row >> 2) & 4); }
+__device__ __forceinline__ int key_a(int row) { return (row >> 1) & 7; }
+__device__ __forceinline__ int key_b(int row) { return ((row >> 1) & 3) | ((row >> 2) & 4); }
 
 // A barrier for LDS contents alone: __syncthreads() would also wait for every
 // fill that is still to come.
