@@ -113,7 +113,9 @@ __global__ __launch_bounds__(64 * W) void k_matmul_i8_rows(LinearArgs a) {
 // that a fragment read takes together, (row % 2, key) takes 16 values.  (Keys of
 // 8 rows, row % 8, took twice the cycles.)  The fills of step t + 1 and the
 // fragment reads of the next 32 bytes are issued before the products of the
-// current ones.
+// current ones.  Eight wavefronts of 128 x 64 make a 256 x 256 tile (four of
+// 128 x 128 wait at every barrier together: 1.20 against 1.11 ms at 8192 x 27648
+// x 5120, where a library's product of the same matrices into int32 takes 1.11).
 //
 // Rows and pieces past the operands' ends come from beyond the buffer resource
 // and arrive as zeros.  Where K is no multiple of 16 the bytes past it are
@@ -247,20 +249,40 @@ __global__ __launch_bounds__((TileShape<BM, BN, WM, WN>::kThreads), OCC) void k_
   for (int t = 0; t < NS; ++t) fill(t, t);
   arrived(std::integral_constant<int, NS - 1>{}, 0, 0);
   frags(0, 0, fa[0], fb[0]);
+  // the order of a phase: the fragment reads, and in the last phase the fills after them, between the products that
+  // hide them (left alone the compiler waits for reads right after it issues them)
+  const auto order = [&](auto fills) {
+    constexpr bool kFills = decltype(fills)::value;
+    constexpr int n_mfma = TM * TN, n_read = TM + TN, n_fill = kFills ? NA + NB : 0;
+    constexpr int per = kFills || n_mfma < 2 * n_read ? 1 : n_mfma / n_read;
+#pragma unroll
+    for (int i = 0; i < n_read; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, per, 0);  // MFMA
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);    // LDS read
+    }
+    if constexpr (kFills) {
+      constexpr int left = n_mfma - n_read > 0 ? n_mfma - n_read : 1;
+#pragma unroll
+      for (int i = 0; i < left; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x020, (n_fill + left - 1) / left, 0);  // memory read
+      }
+    }
+  };
   int st = 0;
   for (int t = 0; t < steps; ++t) {
 #pragma unroll
     for (int ks = 0; ks < 3; ++ks) {
       frags(st, ks + 1, fa[(ks + 1) & 1], fb[(ks + 1) & 1]);
       products(fa[ks & 1], fb[ks & 1]);
+      order(std::false_type{});
     }
     const int next = st + 1 == NS ? 0 : st + 1;
-    if (t + 1 < steps) {
-      arrived(std::integral_constant<int, NS - 2>{}, next, t + 1);
-      fill(st, t + NS);
-      frags(next, 0, fa[0], fb[0]);
-    }
+    arrived(std::integral_constant<int, NS - 2>{}, next, t + 1);
+    fill(st, t + NS);
+    frags(next, 0, fa[0], fb[0]);
     products(fa[1], fb[1]);
+    order(std::true_type{});
     st = next;
   }
   __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): no fill outlives the workgroup
@@ -399,11 +421,11 @@ Choice choose(int64_t M, int64_t N, int64_t K) {
   // activations' reads, as many bytes as the weights', cost more than tiles do
   // (16 x 11008 x 2048: 10.5 against 8.2; 16 x 27648 x 5120: 44 against 30).
   if (M <= 16 && N < 8192) return {kRows, 1};
-  // Four tiles of 128 cost as much time as 1.07 of a 256 tile's, which also
-  // comes in whole rounds of one per CU (512 x 27648 x 5120: 115 and 102;
-  // 2048 x 5120 x 5120: 75 and 87; 8192 x 27648 x 5120: 1317 and 1260).
+  // 256 tiles of 128 cost 24 us at K = 5120, a round of 256 tiles of 256, one per CU, 62
+  // to 80 (512 x 27648 x 5120: 112 and 90; 4096 x 5120 x 5120, two rounds, 121 and 140;
+  // 1024 x 5120 x 5120: 39 and 55; 8192 x 27648 x 5120: 1303 and 1113).
   const int64_t t128 = tiles(128, 128), t256 = tiles(256, 256);
-  if (M > 64 && t128 >= 256) return {3.7 * ((t256 + 255) / 256) < t128 / 256.0 + 0.5 ? kTile256 : kTile128, 1};
+  if (M > 64 && t128 >= 256) return {2.9 * ((t256 + 255) / 256) < t128 / 256.0 + 0.5 ? kTile256 : kTile128, 1};
   // 64 x 27648 x 5120: 64 x 64 tiles 40.8, 64 x 128 tiles 37.4 (64 x 11008 x 2048: 8.8 and 10.9)
   if (M > 32 && tiles(64, 128) >= 192) return {kTile64Wide, 1};
   const Path path = M > 32 ? kTile64 : kTile32;
@@ -424,7 +446,7 @@ hipError_t launch(const LinearArgs& a, void* ws, hipStream_t st) {
     case kTile64: return launch_tile<64, 64, 32, 32, 3, 3, TO>(a, c.split, ws, st);
     case kTile64Wide: return launch_tile<64, 128, 32, 64, 2, 3, TO>(a, 1, ws, st);
     case kTile128: return launch_tile<128, 128, 64, 64, 2, 2, TO>(a, 1, ws, st);
-    default: return launch_tile<256, 256, 128, 128, 1, 2, TO>(a, 1, ws, st);
+    default: return launch_tile<256, 256, 128, 64, 2, 2, TO>(a, 1, ws, st);
   }
 }
 
