@@ -30,27 +30,95 @@ struct Rotary {
   int half, interleaved;
 };
 
+// Eight adjacent values.
 template <typename T>
-__device__ __forceinline__ float rotated(const T* __restrict__ x, int d, int64_t pos, const Rotary& r) {
-  const float v = to_f32(x[d]);
-  if (d >= 2 * r.half) return v;
-  const int i = r.interleaved ? d >> 1 : (d < r.half ? d : d - r.half);
-  const bool second = r.interleaved ? (d & 1) : d >= r.half;
-  const int mate = r.interleaved ? d ^ 1 : (second ? d - r.half : d + r.half);
-  const bool in = pos >= 0 && pos < r.len;
-  const float c = in ? r.cos[pos * r.half + i] : __builtin_nanf("");
-  const float s = in ? r.sin[pos * r.half + i] : __builtin_nanf("");
-  const float w = to_f32(x[mate]);
-  return second ? v * c + w * s : v * c - w * s;
+struct alignas(16) Eight {
+  T v[8];
+};
+template <typename T>
+__device__ __forceinline__ void load8(const T* __restrict__ x, bool wide, float (&v)[8]) {
+  if (wide) {
+    const Eight<T> w = *reinterpret_cast<const Eight<T>*>(x);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = to_f32(w.v[e]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = to_f32(x[e]);
+  }
+}
+template <typename T>
+__device__ __forceinline__ void store8(T* __restrict__ x, bool wide, const float (&v)[8]) {
+  if (wide) {
+    Eight<T> w;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w.v[e] = (T)v[e];
+    *reinterpret_cast<Eight<T>*>(x) = w;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = (T)v[e];
+  }
 }
 
-// The sequence of packed row i: the last s with cu[s] <= i, or -1 past the last row.
+// Channels d .. d + 7 (d a multiple of 8) of a rotated row; `wide`: the row lies on 16 bytes.
+template <typename T>
+__device__ __forceinline__ void rotated8(const T* __restrict__ x, int d, int64_t pos, const Rotary& r, bool wide, float (&y)[8]) {
+  load8(x + d, wide, y);
+  if (d >= 2 * r.half) return;
+  const bool in = pos >= 0 && pos < r.len;
+  const float* cp = r.cos + (in ? pos : 0) * r.half;
+  const float* sp = r.sin + (in ? pos : 0) * r.half;
+  const float nan = __builtin_nanf("");
+  if (!r.interleaved && r.half % 8 == 0) {  // all eight in one half, their mates in eight adjacent places
+    const bool second = d >= r.half;
+    const int i = second ? d - r.half : d;
+    float w[8], c[8], s[8];
+    load8(x + (second ? i : i + r.half), wide, w);
+    const bool four = ((reinterpret_cast<uintptr_t>(cp) | reinterpret_cast<uintptr_t>(sp)) & 15) == 0;
+    if (in && four) {
+#pragma unroll
+      for (int e = 0; e < 8; e += 4) {
+        const float4 a = *reinterpret_cast<const float4*>(cp + i + e), b = *reinterpret_cast<const float4*>(sp + i + e);
+        c[e] = a.x; c[e + 1] = a.y; c[e + 2] = a.z; c[e + 3] = a.w;
+        s[e] = b.x; s[e + 1] = b.y; s[e + 2] = b.z; s[e + 3] = b.w;
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        c[e] = in ? cp[i + e] : nan;
+        s[e] = in ? sp[i + e] : nan;
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = second ? y[e] * c[e] + w[e] * s[e] : y[e] * c[e] - w[e] * s[e];
+    return;
+  }
+  float own[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) own[e] = y[e];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const int ch = d + e;
+    if (ch >= 2 * r.half) continue;
+    const int i = r.interleaved ? ch >> 1 : (ch < r.half ? ch : ch - r.half);
+    const bool second = r.interleaved ? (ch & 1) : ch >= r.half;
+    const float w = to_f32(x[r.interleaved ? ch ^ 1 : (second ? ch - r.half : ch + r.half)]);
+    const float c = in ? cp[i] : nan, s = in ? sp[i] : nan;
+    y[e] = second ? own[e] * c + w * s : own[e] * c - w * s;
+  }
+}
+
+// The sequence of packed row i: the last s with cu[s] <= i, or -1 outside the
+// rows; a wavefront looks at 64 starts at a time.
 __device__ __forceinline__ int find_seq(const int32_t* __restrict__ cu, int n_seq, int64_t i) {
+  const int lane = threadIdx.x & 63;
   if (i < cu[0] || i >= cu[n_seq]) return -1;
-  int lo = 0, hi = n_seq;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (cu[mid] <= i) lo = mid; else hi = mid;
+  int lo = 0, n = n_seq;  // the answer lies in [lo, lo + n)
+  while (n > 1) {
+    const int step = (n + 63) / 64, at = lo + (lane + 1) * step;
+    const uint64_t below = __ballot((lane + 1) * step < n && cu[at] <= i);
+    const int k = __popcll(below);
+    n = n - k * step < step ? n - k * step : step;
+    lo += k * step;
   }
   return lo;
 }
@@ -94,111 +162,252 @@ __device__ __forceinline__ bool span_of(const int32_t* cu, const int32_t* kv_len
   return true;
 }
 
-template <typename T>
-__device__ void append_block(const AppendArgs& a, const Span& sp, int head, bool values, const Rotary& rot) {
-  const int D = a.c.head_dim, P = a.c.page_tokens;
-  const int64_t ld = values ? a.ldv : a.ldk;
-  const T* x = static_cast<const T*>(values ? a.v : a.k) + sp.row0 * ld + (int64_t)head * D;
-  const int n_new = (int)(sp.hi - sp.lo), at = (int)(sp.lo - sp.p0);
-  const int64_t block = (int64_t)sp.page * a.c.kv_heads + head;
-  int8_t* codes = (values ? a.c.v : a.c.k) + block * P * D;
-  float* scale = (values ? a.c.v_scale : a.c.k_scale) + block;
-
-  float m = 0.0f;
-  for (int i = threadIdx.x; i < n_new * D; i += 256) {
-    const int t = i / D, d = i - t * D;
-    m = amax_keep(m, values ? to_f32(x[t * ld + d]) : rotated(x + t * ld, d, sp.lo + t, rot));
-  }
-  const float fresh = scale_of_amax(block_amax(m));
-  const float was = at == 0 ? 0.0f : *scale;
-  const float now = (fresh > was || fresh != fresh) ? fresh : was;
-  const float inv = inverse_scale(now);
-  __syncthreads();  // every thread has read the old scale
-  if (threadIdx.x == 0) *scale = now;
-  if (now > was && at > 0) {
-    const float ratio = was * inv;
-    for (int i = threadIdx.x; i < at * D; i += 256) {
-      const int t = i / D, d = i - t * D;
-      int8_t* c = codes + (values ? (int64_t)d * P + t : (int64_t)t * D + d);
-      *c = (int8_t)code_of((float)*c, ratio);
+// What a thread holds of a block: four pieces of eight channels per item.  Of
+// keys, item i's pieces are the (i * 1024 + j * 256 + thread)-th of the block in
+// memory order.  Of values, an item is eight channels of four adjacent tokens
+// (one word of each channel's row of codes); neighbouring threads take
+// neighbouring words, so that a wavefront's accesses are runs of at least 16
+// (pages of 16) to 64 bytes on both sides.
+template <bool VALUES>
+struct Place {
+  int D, P;
+  __device__ __forceinline__ bool at(int item, int j, int& token, int& d) const {
+    if constexpr (VALUES) {
+      const int x = item * 256 + threadIdx.x, words = P >> 2;
+      token = (x & (words - 1)) * 4 + j;
+      d = (x / words) * 8;
+      return d < D;
+    } else {
+      const int x = (item * 4 + j) * 256 + threadIdx.x, per = D >> 3;
+      token = x / per;
+      d = (x - token * per) * 8;
+      return token < P;
     }
   }
-  for (int i = threadIdx.x; i < n_new * D; i += 256) {
-    const int t = i / D, d = i - t * D;
-    const float v = values ? to_f32(x[t * ld + d]) : rotated(x + t * ld, d, sp.lo + t, rot);
-    codes[values ? (int64_t)d * P + at + t : (int64_t)(at + t) * D + d] = (int8_t)code_of(v, inv);
+};
+
+__device__ __forceinline__ uint32_t byte_at(uint32_t w, int j, int code) {
+  return (w & ~(255u << (8 * j))) | (uint32_t)(code & 255) << (8 * j);
+}
+__device__ __forceinline__ int code_at(uint32_t w, int j) { return (int)(int8_t)(w >> (8 * j)); }
+
+template <typename T, int NI, bool VALUES>
+__device__ __forceinline__ void append_block(const AppendArgs& a, const Span& sp, int head, const Rotary& rot, bool wide) {
+  const int D = a.c.head_dim, P = a.c.page_tokens;
+  const int64_t ld = VALUES ? a.ldv : a.ldk;
+  const T* x = static_cast<const T*>(VALUES ? a.v : a.k) + sp.row0 * ld + (int64_t)head * D;
+  const int at = (int)(sp.lo - sp.p0), end = (int)(sp.hi - sp.p0);  // slots of the new tokens
+  const int64_t block = (int64_t)sp.page * a.c.kv_heads + head;
+  int8_t* codes = (VALUES ? a.c.v : a.c.k) + block * P * D;
+  float* scale = (VALUES ? a.c.v_scale : a.c.k_scale) + block;
+  const float was = at == 0 ? 0.0f : *scale;
+  const Place<VALUES> place{D, P};
+
+  float v[NI * 4][8];
+  float m = 0.0f;
+#pragma unroll
+  for (int i = 0; i < NI; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      int t, d;
+      if (!place.at(i, j, t, d) || t < at || t >= end) continue;
+      const T* row = x + (t - at) * ld;
+      if constexpr (VALUES) load8(row + d, wide, v[i * 4 + j]);
+      else rotated8(row, d, sp.p0 + t, rot, wide, v[i * 4 + j]);
+    }
+#pragma unroll
+  for (int i = 0; i < NI; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      int t, d;
+      if (!place.at(i, j, t, d) || t < at || t >= end) continue;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) m = amax_keep(m, v[i * 4 + j][e]);
+    }
+  const float fresh = scale_of_amax(block_amax(m));
+  const float now = (fresh > was || fresh != fresh) ? fresh : was;
+  const float inv = inverse_scale(now);
+  const bool grew = now > was && at > 0;
+  const float ratio = was * inv;
+  if (threadIdx.x == 0) *scale = now;  // (every thread read the old one before block_amax's barriers)
+#pragma unroll
+  for (int i = 0; i < NI; ++i) {
+    if constexpr (VALUES) {
+      int t, d;
+      if (!place.at(i, 0, t, d)) continue;
+      // words without a new token, or an old one to round again, stay
+      if (t >= end || t + 4 <= (grew ? 0 : at)) continue;
+      const bool keeps = t < at || t + 4 > end;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        uint32_t* word = reinterpret_cast<uint32_t*>(codes + (int64_t)(d + e) * P + t);
+        uint32_t w = keeps ? *word : 0u;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          if (t + j < at) w = grew ? byte_at(w, j, code_of((float)code_at(w, j), ratio)) : w;
+          else if (t + j < end) w = byte_at(w, j, code_of(v[i * 4 + j][e], inv));
+        }
+        *word = w;
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        int t, d;
+        if (!place.at(i, j, t, d) || t >= end || (t < at && !grew)) continue;
+        uint2* words = reinterpret_cast<uint2*>(codes + t * D + d);
+        uint32_t w[2] = {0, 0};
+        if (t < at) {
+          const uint2 old = *words;
+          w[0] = old.x;
+          w[1] = old.y;
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int c = t < at ? code_of((float)code_at(w[e >> 2], e & 3), ratio) : code_of(v[i * 4 + j][e], inv);
+          w[e >> 2] = byte_at(w[e >> 2], e & 3, c);
+        }
+        *words = make_uint2(w[0], w[1]);
+      }
+    }
   }
 }
 
-// Workgroups [0, n_blocks): keys and values; the rest: one row of queries each.
-template <typename T>
-__global__ __launch_bounds__(256) void k_kv_append(AppendArgs a, int64_t n_blocks, int64_t per_seq) {
+// Workgroups [0, n_blocks): keys and values; the rest: queries, a row a wavefront.
+template <typename T, int NI>
+__global__ __launch_bounds__(256) void k_kv_append(AppendArgs a, int n_blocks, int per_seq, bool wide_kv, bool wide_q) {
   const Rotary rot{a.cos, a.sin, a.rope_len, a.rot / 2, a.interleaved};
-  int64_t b = blockIdx.x;
+  int b = (int)blockIdx.x;
   if (b < n_blocks) {
     const bool values = b & 1;
     b >>= 1;
-    const int head = (int)(b % a.c.kv_heads);
+    const int head = b % a.c.kv_heads;
     b /= a.c.kv_heads;
-    const int s = (int)(b / per_seq);
+    const int s = b / per_seq;
     Span sp;
-    if (!span_of(a.cu, a.kv_len, a.table, a.table_ld, a.c.n_pages, a.n_rows, a.c.page_tokens, s, b % per_seq, &sp) || sp.page < 0) return;
-    append_block<T>(a, sp, head, values, rot);
+    if (!span_of(a.cu, a.kv_len, a.table, a.table_ld, a.c.n_pages, a.n_rows, a.c.page_tokens, s, b - s * per_seq, &sp) || sp.page < 0)
+      return;
+    if (values) append_block<T, NI, true>(a, sp, head, rot, wide_kv);
+    else append_block<T, NI, false>(a, sp, head, rot, wide_kv);
     return;
   }
-  const int64_t row = b - n_blocks;
+  const int64_t row = (int64_t)(b - n_blocks) * 4 + (threadIdx.x >> 6);
+  if (row >= a.n_rows) return;
   const int s = find_seq(a.cu, a.n_seq, row);
   if (s < 0) return;
   const int64_t pos = (int64_t)a.kv_len[s] - (a.cu[s + 1] - row);
-  const int D = a.c.head_dim;
-  for (int i = threadIdx.x; i < a.q_heads * D; i += 256) {
-    const int h = i / D, d = i - h * D;
-    static_cast<T*>(a.q_out)[row * a.ldqo + i] = (T)rotated(static_cast<const T*>(a.q) + row * a.ldq + (int64_t)h * D, d, pos, rot);
+  const int per = a.c.head_dim >> 3;
+  for (int i = threadIdx.x & 63; i < a.q_heads * per; i += 64) {
+    const int h = i / per, d = (i - h * per) * 8;
+    float y[8];
+    rotated8(static_cast<const T*>(a.q) + row * a.ldq + (int64_t)h * a.c.head_dim, d, pos, rot, wide_q, y);
+    store8(static_cast<T*>(a.q_out) + row * a.ldqo + (int64_t)h * a.c.head_dim + d, wide_q, y);
   }
 }
 
-template <typename T>
-__global__ __launch_bounds__(256) void k_kv_read(ReadArgs a, int64_t per_seq) {
+template <typename T, int NI, bool VALUES>
+__device__ __forceinline__ void read_block(const ReadArgs& a, const Span& sp, int head, bool wide) {
   const int D = a.c.head_dim, P = a.c.page_tokens;
-  int64_t b = blockIdx.x;
-  const bool values = b & 1;
-  b >>= 1;
-  const int head = (int)(b % a.c.kv_heads);
-  b /= a.c.kv_heads;
-  const int s = (int)(b / per_seq);
-  Span sp;
-  if (!span_of(a.cu, a.kv_len, a.table, a.table_ld, a.c.n_pages, a.n_rows, P, s, b % per_seq, &sp)) return;
   const bool there = sp.page >= 0;
   const int64_t block = (int64_t)(there ? sp.page : 0) * a.c.kv_heads + head;
-  const int8_t* codes = (values ? a.c.v : a.c.k) + block * P * D;
-  const float sc = there ? (values ? a.c.v_scale : a.c.k_scale)[block] : __builtin_nanf("");
-  T* out = static_cast<T*>(values ? a.v_out : a.k_out);
-  const int at = (int)(sp.lo - sp.p0), n = (int)(sp.hi - sp.lo);
-  for (int i = threadIdx.x; i < n * D; i += 256) {
-    const int t = i / D, d = i - t * D;
-    const int8_t c = codes[values ? (int64_t)d * P + at + t : (int64_t)(at + t) * D + d];
-    out[((sp.row0 + t) * a.c.kv_heads + head) * D + d] = (T)((float)c * sc);
+  const int8_t* codes = (VALUES ? a.c.v : a.c.k) + block * P * D;
+  const float sc = there ? (VALUES ? a.c.v_scale : a.c.k_scale)[block] : __builtin_nanf("");
+  T* out = static_cast<T*>(VALUES ? a.v_out : a.k_out) + (sp.row0 * a.c.kv_heads + head) * D;
+  const int at = (int)(sp.lo - sp.p0), end = (int)(sp.hi - sp.p0);
+  const Place<VALUES> place{D, P};
+#pragma unroll
+  for (int i = 0; i < NI; ++i) {
+    uint32_t w[8];
+    if constexpr (VALUES) {
+      int t, d;
+      if (!place.at(i, 0, t, d) || t >= end || t + 4 <= at) continue;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[e] = *reinterpret_cast<const uint32_t*>(codes + (int64_t)(d + e) * P + t);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      int t, d;
+      if (!place.at(i, j, t, d) || t < at || t >= end) continue;
+      float y[8];
+      if constexpr (VALUES) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = (float)code_at(w[e], j) * sc;
+      } else {
+        const uint2 x = *reinterpret_cast<const uint2*>(codes + t * D + d);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = (float)code_at(e < 4 ? x.x : x.y, e & 3) * sc;
+      }
+      store8(out + (int64_t)(t - at) * a.c.kv_heads * D + d, wide, y);
+    }
   }
+}
+
+template <typename T, int NI>
+__global__ __launch_bounds__(256) void k_kv_read(ReadArgs a, int per_seq, bool wide) {
+  int b = (int)blockIdx.x;
+  const bool values = b & 1;
+  b >>= 1;
+  const int head = b % a.c.kv_heads;
+  b /= a.c.kv_heads;
+  const int s = b / per_seq;
+  Span sp;
+  if (!span_of(a.cu, a.kv_len, a.table, a.table_ld, a.c.n_pages, a.n_rows, a.c.page_tokens, s, b - s * per_seq, &sp)) return;
+  if (values) read_block<T, NI, true>(a, sp, head, wide);
+  else read_block<T, NI, false>(a, sp, head, wide);
 }
 
 // Pages that n rows can touch from any starting position.
 int64_t pages_touched(int64_t n, int T) { return n < 1 ? 0 : (n + T - 2) / T + 1; }
+
+bool on16(const void* p, int64_t ld, int64_t size) { return ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ld * size)) & 15) == 0; }
+
+template <typename T, int NI>
+hipError_t launch_append(const AppendArgs& a, int64_t grid, int64_t n_blocks, int64_t per_seq, hipStream_t st) {
+  const bool kv = on16(a.k, a.ldk, sizeof(T)) && on16(a.v, a.ldv, sizeof(T));
+  const bool q = on16(a.q, a.ldq, sizeof(T)) && on16(a.q_out, a.ldqo, sizeof(T));
+  hipLaunchKernelGGL((k_kv_append<T, NI>), dim3((unsigned)grid), dim3(256), 0, st, a, (int)n_blocks, (int)per_seq, kv, q);
+  return hipGetLastError();
+}
+template <typename T, int NI>
+hipError_t launch_read(const ReadArgs& a, int64_t grid, int64_t per_seq, hipStream_t st) {
+  const bool wide = on16(a.k_out, 0, 0) && on16(a.v_out, 0, 0);  // rows are a multiple of 128 bytes apart
+  hipLaunchKernelGGL((k_kv_read<T, NI>), dim3((unsigned)grid), dim3(256), 0, st, a, (int)per_seq, wide);
+  return hipGetLastError();
+}
+
+// Items of four pieces that a block leaves each of 256 threads.
+int items_of(const awsrc_kv_cache& c) {
+  const int n = c.head_dim * c.page_tokens / 8192;
+  return n < 1 ? 1 : n;
+}
+
+template <typename T>
+hipError_t append_t(const AppendArgs& a, int64_t grid, int64_t n_blocks, int64_t per_seq, hipStream_t st) {
+  switch (items_of(a.c)) {
+    case 1: return launch_append<T, 1>(a, grid, n_blocks, per_seq, st);
+    case 2: return launch_append<T, 2>(a, grid, n_blocks, per_seq, st);
+    default: return launch_append<T, 4>(a, grid, n_blocks, per_seq, st);
+  }
+}
+template <typename T>
+hipError_t read_t(const ReadArgs& a, int64_t grid, int64_t per_seq, hipStream_t st) {
+  switch (items_of(a.c)) {
+    case 1: return launch_read<T, 1>(a, grid, per_seq, st);
+    case 2: return launch_read<T, 2>(a, grid, per_seq, st);
+    default: return launch_read<T, 4>(a, grid, per_seq, st);
+  }
+}
 
 }  // namespace
 
 hipError_t launch_kv_append(const AppendArgs& a, hipStream_t st) {
   const int64_t per_seq = pages_touched(a.max_new, a.c.page_tokens);
   const int64_t n_blocks = 2 * a.n_seq * per_seq * a.c.kv_heads;
-  const int64_t grid = n_blocks + (a.q ? a.n_rows : 0);
+  const int64_t grid = n_blocks + (a.q ? (a.n_rows + 3) / 4 : 0);
   if (grid <= 0) return hipSuccess;
   if (grid > 0x7FFFFFFF) return hipErrorInvalidValue;
-  if (a.dtype == AWSRC_DTYPE_F32)
-    hipLaunchKernelGGL((k_kv_append<float>), dim3((unsigned)grid), dim3(256), 0, st, a, n_blocks, per_seq);
-  else if (a.dtype == AWSRC_DTYPE_BF16)
-    hipLaunchKernelGGL((k_kv_append<__bf16>), dim3((unsigned)grid), dim3(256), 0, st, a, n_blocks, per_seq);
-  else
-    hipLaunchKernelGGL((k_kv_append<_Float16>), dim3((unsigned)grid), dim3(256), 0, st, a, n_blocks, per_seq);
-  return hipGetLastError();
+  if (a.dtype == AWSRC_DTYPE_F32) return append_t<float>(a, grid, n_blocks, per_seq, st);
+  if (a.dtype == AWSRC_DTYPE_BF16) return append_t<__bf16>(a, grid, n_blocks, per_seq, st);
+  return append_t<_Float16>(a, grid, n_blocks, per_seq, st);
 }
 
 hipError_t launch_kv_read(const ReadArgs& a, hipStream_t st) {
@@ -206,13 +415,9 @@ hipError_t launch_kv_read(const ReadArgs& a, hipStream_t st) {
   const int64_t grid = 2 * a.n_seq * per_seq * a.c.kv_heads;
   if (grid <= 0) return hipSuccess;
   if (grid > 0x7FFFFFFF) return hipErrorInvalidValue;
-  if (a.dtype == AWSRC_DTYPE_F32)
-    hipLaunchKernelGGL((k_kv_read<float>), dim3((unsigned)grid), dim3(256), 0, st, a, per_seq);
-  else if (a.dtype == AWSRC_DTYPE_BF16)
-    hipLaunchKernelGGL((k_kv_read<__bf16>), dim3((unsigned)grid), dim3(256), 0, st, a, per_seq);
-  else
-    hipLaunchKernelGGL((k_kv_read<_Float16>), dim3((unsigned)grid), dim3(256), 0, st, a, per_seq);
-  return hipGetLastError();
+  if (a.dtype == AWSRC_DTYPE_F32) return read_t<float>(a, grid, per_seq, st);
+  if (a.dtype == AWSRC_DTYPE_BF16) return read_t<__bf16>(a, grid, per_seq, st);
+  return read_t<_Float16>(a, grid, per_seq, st);
 }
 
 }  // namespace awsrc
