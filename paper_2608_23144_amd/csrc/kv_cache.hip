@@ -28,6 +28,7 @@ struct Rotary {
   const float *cos, *sin;
   int64_t len;
   int half, interleaved;
+  bool whole;  // every row turns by Turn
 };
 
 // Eight adjacent values.
@@ -107,6 +108,32 @@ __device__ __forceinline__ void rotated8(const T* __restrict__ x, int d, int64_t
   }
 }
 
+// Channels i .. i + 7 and their mates half a row on, of a row rotated whole
+// (rot = head_dim, halves, everything on 16 bytes).
+struct Turn {
+  float c[8], s[8];
+  __device__ __forceinline__ void fetch(const Rotary& r, int64_t pos, int i) {
+    const bool in = pos >= 0 && pos < r.len;
+    const float4* cp = reinterpret_cast<const float4*>(r.cos + (in ? pos : 0) * r.half + i);
+    const float4* sp = reinterpret_cast<const float4*>(r.sin + (in ? pos : 0) * r.half + i);
+    const float nan = __builtin_nanf("");
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const float4 a = cp[e], b = sp[e];
+      c[4 * e] = in ? a.x : nan; c[4 * e + 1] = in ? a.y : nan; c[4 * e + 2] = in ? a.z : nan; c[4 * e + 3] = in ? a.w : nan;
+      s[4 * e] = in ? b.x : nan; s[4 * e + 1] = in ? b.y : nan; s[4 * e + 2] = in ? b.z : nan; s[4 * e + 3] = in ? b.w : nan;
+    }
+  }
+  __device__ __forceinline__ void apply(float (&lo)[8], float (&hi)[8]) const {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float a = lo[e], b = hi[e];
+      lo[e] = a * c[e] - b * s[e];
+      hi[e] = b * c[e] + a * s[e];
+    }
+  }
+};
+
 // The sequence of packed row i: the last s with cu[s] <= i, or -1 outside the
 // rows; a wavefront looks at 64 starts at a time.
 __device__ __forceinline__ int find_seq(const int32_t* __restrict__ cu, int n_seq, int64_t i) {
@@ -139,22 +166,24 @@ __device__ __forceinline__ float block_amax(float m) {
 // Which tokens of page slot j (counted from the first touched page) are new:
 // positions [lo, hi), page positions from p0; the rows of k and v start at row0 for lo.
 struct Span {
-  int64_t p0, lo, hi, row0;
+  int p0, lo, hi;
+  int64_t row0;
   int32_t page;  // negative where there is none
 };
-__device__ __forceinline__ bool span_of(const int32_t* cu, const int32_t* kv_len, const int32_t* table, int64_t table_ld,
-                                        int64_t n_pages, int64_t n_rows, int T, int s, int64_t j, Span* o) {
-  int64_t r0 = cu[s], r1 = cu[s + 1];
-  if (r0 < 0) return false;
-  if (r1 > n_rows) r1 = n_rows;
-  const int64_t len = kv_len[s];
-  const int64_t first = len - (cu[s + 1] - r0);  // position of row r0; below 0 where a call brings more rows than tokens
-  const int64_t start = first < 0 ? 0 : first;
-  const int64_t slot = start / T + j;
-  o->p0 = slot * T;
+constexpr int kMaxTokens = 1 << 30;  // longer sequences take no part
+__device__ __forceinline__ bool span_of(const int32_t* __restrict__ cu, const int32_t* __restrict__ kv_len,
+                                        const int32_t* __restrict__ table, int64_t table_ld, int64_t n_pages, int64_t n_rows,
+                                        int T, int s, int j, Span* o) {
+  const int r0 = cu[s], r1 = cu[s + 1], len = kv_len[s];
+  if (r0 < 0 || r1 <= r0 || r1 > n_rows || len < 0 || len > kMaxTokens) return false;
+  const int64_t first = (int64_t)len - (r1 - r0);  // position of row r0; below 0 where a call brings more rows than tokens
+  const int start = first < 0 ? 0 : (int)first;
+  const int shift = __builtin_ctz(T);
+  const int slot = (start >> shift) + j;
+  if (slot > len >> shift) return false;
+  o->p0 = slot << shift;
   o->lo = start > o->p0 ? start : o->p0;
-  const int64_t end = len < first + (r1 - r0) ? len : first + (r1 - r0);
-  o->hi = end < o->p0 + T ? end : o->p0 + T;
+  o->hi = len < o->p0 + T ? len : o->p0 + T;
   if (o->lo >= o->hi) return false;
   o->row0 = r0 + (o->lo - first);
   o->page = slot < table_ld ? table[(int64_t)s * table_ld + slot] : -1;
@@ -163,8 +192,7 @@ __device__ __forceinline__ bool span_of(const int32_t* cu, const int32_t* kv_len
 }
 
 // What a thread holds of a block: four pieces of eight channels per item.  Of
-// keys, item i's pieces are the (i * 1024 + j * 256 + thread)-th of the block in
-// memory order.  Of values, an item is eight channels of four adjacent tokens
+// keys, an item is two times a piece and its mate half a row on.  Of values, an item is eight channels of four adjacent tokens
 // (one word of each channel's row of codes); neighbouring threads take
 // neighbouring words, so that a wavefront's accesses are runs of at least 16
 // (pages of 16) to 64 bytes on both sides.
@@ -173,14 +201,14 @@ struct Place {
   int D, P;
   __device__ __forceinline__ bool at(int item, int j, int& token, int& d) const {
     if constexpr (VALUES) {
-      const int x = item * 256 + threadIdx.x, words = P >> 2;
-      token = (x & (words - 1)) * 4 + j;
-      d = (x / words) * 8;
+      const int x = item * 256 + threadIdx.x, shift = __builtin_ctz(P) - 2;
+      token = (x & ((1 << shift) - 1)) * 4 + j;
+      d = (x >> shift) * 8;
       return d < D;
     } else {
-      const int x = (item * 4 + j) * 256 + threadIdx.x, per = D >> 3;
-      token = x / per;
-      d = (x - token * per) * 8;
+      const int x = (item * 2 + (j >> 1)) * 256 + threadIdx.x, shift = __builtin_ctz(D) - 4;
+      token = x >> shift;
+      d = (x & ((1 << shift) - 1)) * 8 + (j & 1) * (D >> 1);
       return token < P;
     }
   }
@@ -212,9 +240,23 @@ __device__ __forceinline__ void append_block(const AppendArgs& a, const Span& sp
       int t, d;
       if (!place.at(i, j, t, d) || t < at || t >= end) continue;
       const T* row = x + (t - at) * ld;
-      if constexpr (VALUES) load8(row + d, wide, v[i * 4 + j]);
+      if (VALUES || rot.whole) load8(row + d, wide, v[i * 4 + j]);
       else rotated8(row, d, sp.p0 + t, rot, wide, v[i * 4 + j]);
     }
+  if constexpr (!VALUES) {
+    if (rot.whole) {
+#pragma unroll
+      for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; j += 2) {
+          int t, d;
+          if (!place.at(i, j, t, d) || t < at || t >= end) continue;
+          Turn turn;
+          turn.fetch(rot, sp.p0 + t, d);
+          turn.apply(v[i * 4 + j], v[i * 4 + j + 1]);
+        }
+    }
+  }
 #pragma unroll
   for (int i = 0; i < NI; ++i)
 #pragma unroll
@@ -274,8 +316,9 @@ __device__ __forceinline__ void append_block(const AppendArgs& a, const Span& sp
 
 // Workgroups [0, n_blocks): keys and values; the rest: queries, a row a wavefront.
 template <typename T, int NI>
-__global__ __launch_bounds__(256) void k_kv_append(AppendArgs a, int n_blocks, int per_seq, bool wide_kv, bool wide_q) {
-  const Rotary rot{a.cos, a.sin, a.rope_len, a.rot / 2, a.interleaved};
+__global__ __launch_bounds__(256) void k_kv_append(AppendArgs a, int n_blocks, int per_seq, bool wide_kv, bool wide_q,
+                                                   bool whole) {
+  const Rotary rot{a.cos, a.sin, a.rope_len, a.rot / 2, a.interleaved, whole};
   int b = (int)blockIdx.x;
   if (b < n_blocks) {
     const bool values = b & 1;
@@ -295,12 +338,29 @@ __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a, int n_blocks, i
   const int s = find_seq(a.cu, a.n_seq, row);
   if (s < 0) return;
   const int64_t pos = (int64_t)a.kv_len[s] - (a.cu[s + 1] - row);
-  const int per = a.c.head_dim >> 3;
-  for (int i = threadIdx.x & 63; i < a.q_heads * per; i += 64) {
+  const int D = a.c.head_dim, lane = threadIdx.x & 63;
+  const T* q = static_cast<const T*>(a.q) + row * a.ldq;
+  T* out = static_cast<T*>(a.q_out) + row * a.ldqo;
+  if (whole) {  // a lane turns the same channels of every head
+    const int shift = __builtin_ctz(D) - 4, i = (lane & ((1 << shift) - 1)) * 8;
+    Turn turn;
+    turn.fetch(rot, pos, i);
+    for (int h = lane >> shift; h < a.q_heads; h += 64 >> shift) {
+      float lo[8], hi[8];
+      load8(q + h * D + i, true, lo);
+      load8(q + h * D + i + D / 2, true, hi);
+      turn.apply(lo, hi);
+      store8(out + h * D + i, true, lo);
+      store8(out + h * D + i + D / 2, true, hi);
+    }
+    return;
+  }
+  const int per = D >> 3;
+  for (int i = lane; i < a.q_heads * per; i += 64) {
     const int h = i / per, d = (i - h * per) * 8;
     float y[8];
-    rotated8(static_cast<const T*>(a.q) + row * a.ldq + (int64_t)h * a.c.head_dim, d, pos, rot, wide_q, y);
-    store8(static_cast<T*>(a.q_out) + row * a.ldqo + (int64_t)h * a.c.head_dim + d, wide_q, y);
+    rotated8(q + h * D, d, pos, rot, wide_q, y);
+    store8(out + h * D + d, wide_q, y);
   }
 }
 
@@ -313,20 +373,29 @@ __device__ __forceinline__ void read_block(const ReadArgs& a, const Span& sp, in
   const float sc = there ? (VALUES ? a.c.v_scale : a.c.k_scale)[block] : __builtin_nanf("");
   T* out = static_cast<T*>(VALUES ? a.v_out : a.k_out) + (sp.row0 * a.c.kv_heads + head) * D;
   const int at = (int)(sp.lo - sp.p0), end = (int)(sp.hi - sp.p0);
-  const Place<VALUES> place{D, P};
 #pragma unroll
   for (int i = 0; i < NI; ++i) {
     uint32_t w[8];
+    int vt = 0, vd = 0;
     if constexpr (VALUES) {
-      int t, d;
-      if (!place.at(i, 0, t, d) || t >= end || t + 4 <= at) continue;
+      // eight threads side by side take 64 channels of the same tokens: stores of whole lines
+      const int x = i * 256 + threadIdx.x, shift = __builtin_ctz(P) - 2;
+      vt = ((x >> 3) & ((1 << shift) - 1)) * 4;
+      vd = ((x >> 3 >> shift) * 8 + (x & 7)) * 8;
+      const int t = vt, d = vd;
+      if (d >= D || t >= end || t + 4 <= at) continue;
 #pragma unroll
       for (int e = 0; e < 8; ++e) w[e] = *reinterpret_cast<const uint32_t*>(codes + (int64_t)(d + e) * P + t);
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      int t, d;
-      if (!place.at(i, j, t, d) || t < at || t >= end) continue;
+      int t = vt + j, d = vd;
+      if constexpr (!VALUES) {
+        const int x = (i * 4 + j) * 256 + threadIdx.x, shift = __builtin_ctz(D) - 3;
+        t = x >> shift;
+        d = (x & ((1 << shift) - 1)) * 8;
+      }
+      if (t < at || t >= end) continue;
       float y[8];
       if constexpr (VALUES) {
 #pragma unroll
@@ -364,7 +433,8 @@ template <typename T, int NI>
 hipError_t launch_append(const AppendArgs& a, int64_t grid, int64_t n_blocks, int64_t per_seq, hipStream_t st) {
   const bool kv = on16(a.k, a.ldk, sizeof(T)) && on16(a.v, a.ldv, sizeof(T));
   const bool q = on16(a.q, a.ldq, sizeof(T)) && on16(a.q_out, a.ldqo, sizeof(T));
-  hipLaunchKernelGGL((k_kv_append<T, NI>), dim3((unsigned)grid), dim3(256), 0, st, a, (int)n_blocks, (int)per_seq, kv, q);
+  const bool whole = kv && (!a.q || q) && a.rot == a.c.head_dim && !a.interleaved && on16(a.cos, 0, 0) && on16(a.sin, 0, 0) && a.rope_len > 0;
+  hipLaunchKernelGGL((k_kv_append<T, NI>), dim3((unsigned)grid), dim3(256), 0, st, a, (int)n_blocks, (int)per_seq, kv, q, whole);
   return hipGetLastError();
 }
 template <typename T, int NI>
