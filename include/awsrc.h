@@ -500,8 +500,8 @@ awsrc_status awsrc_quantize_rows_i8(const void* X, int32_t x_dtype, int64_t rows
  * Product of int8 matrices with a scale per row of each operand (per token and
  * per output channel):
  *   out[m, n] = a_scale[m] * b_scale[n] * sum_k A[m, k] B[n, k] + bias[n],
- * the sum exact in int32, then fp32 (sum * (a_scale * b_scale) + bias), rounded
- * once to out_dtype (nearest even).
+ * the sum exact in int32, then fp32 (fma(f32(sum), a_scale * b_scale, bias)),
+ * rounded once to out_dtype (nearest even).
  *  A, B     int8, row i at A + i * lda; 16-byte aligned, lda and ldb multiples
  *           of 16, >= K rounded up to 16, <= 2^22.  Each row is readable up to K
  *           rounded up to 16; what lies past K does not matter.
@@ -518,8 +518,10 @@ awsrc_status awsrc_matmul_i8(const int8_t* A, int64_t lda, const float* a_scale,
 /*
  * A linear layer on int8 weights: awsrc_quantize_rows_i8 of X (one scale per
  * token) and awsrc_matmul_i8 of its codes with B, with the same results.  X is
- * [M, K] x_dtype, row m at X + m * ldx; the codes live in the workspace.
- * Workspace: two-phase query as described above, never 0.
+ * [M, K] x_dtype, row m at X + m * ldx; the codes live in the workspace, or in
+ * the kernel where the rows are few (then its size is 0).
+ * Workspace: two-phase query as described above (the query needs no pointers);
+ * the size may be 0, and then no workspace is needed.
  */
 awsrc_status awsrc_linear_i8(const void* X, int32_t x_dtype, int64_t ldx, const int8_t* B, int64_t ldb,
                              const float* b_scale, const float* bias_or_null, int64_t M, int64_t N, int64_t K, void* out,

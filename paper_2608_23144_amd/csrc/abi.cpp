@@ -1186,15 +1186,21 @@ extern "C" awsrc_status awsrc_linear_i8(const void* X, int32_t x_dtype, int64_t 
   if (st != AWSRC_OK) return st;
   if (!ws_bytes) return fail(AWSRC_EINVAL, "ws_bytes is NULL");
   const size_t b_codes = align_up((size_t)M * (size_t)round16(K), 256), b_scales = align_up((size_t)M * 4, 256);
-  const size_t need = 256 + b_codes + b_scales + (M && N ? matmul_i8_ws_bytes(M, N, K) : 0);
-  if (!workspace) {
+  const bool fused = linear_i8_fused(M, N, K);
+  const size_t need = M == 0 || N == 0 || fused ? 0 : b_codes + b_scales + matmul_i8_ws_bytes(M, N, K);
+  if (!workspace && !X && !B && !out) {
     *ws_bytes = need;
     return AWSRC_OK;
   }
   if (M == 0 || N == 0) return AWSRC_OK;
   if (!X || !B || !b_scale || !out) return fail(AWSRC_EINVAL, "NULL buffer");
   if (misaligned(bias_or_null, 4)) return fail(AWSRC_EINVAL, "bias must be 4-byte aligned");
-  if (*ws_bytes < need) return fail(AWSRC_ENOSPC, "workspace of %zu bytes needed", need);
+  if (fused) {
+    const LinearArgs a{nullptr, 0, nullptr, B, ldb, b_scale, bias_or_null, M, N, K, out, out_dtype, ldo};
+    HIPCHK(launch_linear_i8_fused(a, X, x_dtype, ldx, (hipStream_t)stream));
+    return AWSRC_OK;
+  }
+  if (!workspace || *ws_bytes < need) return fail(AWSRC_ENOSPC, "workspace of %zu bytes needed", need);
   if (misaligned(workspace, 16)) return fail(AWSRC_EINVAL, "workspace must be 16-byte aligned");
   char* ws = static_cast<char*>(workspace);
   int8_t* codes = reinterpret_cast<int8_t*>(ws);

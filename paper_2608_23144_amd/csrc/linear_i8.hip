@@ -14,6 +14,9 @@ namespace awsrc {
 
 namespace {
 
+// The epilogue, the same in every kernel: two roundings after the sum's own.
+__device__ __forceinline__ float scaled(int sum, float sa, float sb, float bias) { return __builtin_fmaf((float)sum, sa * sb, bias); }
+
 template <typename TO>
 __device__ __forceinline__ void store4(TO* o, const float (&y)[4], int64_t n, int64_t N, bool wide) {
   if (wide && n + 3 < N) {
@@ -30,76 +33,154 @@ __device__ __forceinline__ void store4(TO* o, const float (&y)[4], int64_t n, in
 
 // Up to 16 rows: the weights' bytes are all that counts.  A workgroup takes 16
 // weight rows (columns of the result) against all activation rows, its W
-// wavefronts sharing the sum; both operands come straight from memory in the
+// wavefronts sharing the sum; the weights come straight from memory in the
 // matrix cores' layout, U steps of 64 bytes ahead of the products, and the
-// wavefronts' sums meet in LDS.  2560 x 2048: 3.4 us; 13 x 2048 x 11008: 11.3 us
+// wavefronts' sums meet in LDS.
+template <int W, int U, bool AHEAD>
+struct RowSums {
+  const int8_t* pb;  // this lane's weight row, from its first piece
+  const int8_t* pa;  // its row of activation codes (AHEAD: in memory, fetched with the weights; else in LDS)
+  int K, wave, g;
+  i32x4 acc = {0, 0, 0, 0};
+  i32x4 fb[2][U], fa[2][U];
+
+  // rows that do not exist read the last one: their sums are not stored
+  __device__ __forceinline__ RowSums(const LinearArgs& a, int64_t n0, int lane, int wv, const int8_t* A, int64_t lda)
+      : pb(a.B + (n0 + (lane & 15) < a.N ? n0 + (lane & 15) : a.N - 1) * a.ldb + 16 * (lane >> 4)),
+        pa(A + ((lane & 15) < a.M ? (lane & 15) : a.M - 1) * lda + 16 * (lane >> 4)), K((int)a.K), wave(wv), g(lane >> 4) {}
+  __device__ __forceinline__ void load(int buf, int k) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      fb[buf][u] = *reinterpret_cast<const i32x4*>(pb + k + 64 * u);
+      if constexpr (AHEAD) fa[buf][u] = *reinterpret_cast<const i32x4*>(pa + k + 64 * u);
+    }
+  }
+  __device__ __forceinline__ int rounds() const { return K / (64 * U); }
+  __device__ __forceinline__ void begin() {
+    if (wave < rounds()) load(0, wave * 64 * U);
+  }
+  __device__ __forceinline__ void products(int buf, int k) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const i32x4 x = AHEAD ? fa[buf][u] : *reinterpret_cast<const i32x4*>(pa + k + 64 * u);
+      acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[buf][u], x, acc, 0, 0, 0);
+    }
+  }
+  __device__ __forceinline__ void run() {
+    const int n = rounds();
+    for (int i = wave; i < n; i += 2 * W) {
+      if (i + W < n) load(1, (i + W) * 64 * U);
+      products(0, i * 64 * U);
+      if (i + W < n) {
+        if (i + 2 * W < n) load(0, (i + 2 * W) * 64 * U);
+        products(1, (i + W) * 64 * U);
+      }
+    }
+    if (wave == W - 1) {  // the rest of the sum, zeros past K on the weights' side
+      for (int k = n * 64 * U; k < K; k += 64) {
+        const int left = K - (k + 16 * g);
+        i32x4 w = {0, 0, 0, 0}, y = w;
+        if (left > 0) {
+          w = *reinterpret_cast<const i32x4*>(pb + k);
+          y = *reinterpret_cast<const i32x4*>(pa + k);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int m = left - 4 * e;  // bytes of this word that belong to the sum
+          if (m < 4) w[e] = m <= 0 ? 0 : w[e] & (int)((1u << (8 * m)) - 1u);
+        }
+        acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(w, y, acc, 0, 0, 0);
+      }
+    }
+  }
+  // the wavefronts' sums together and the results out; sa: the scale of activation row `lane & 15`
+  template <typename TO, typename SA>
+  __device__ __forceinline__ void finish(const LinearArgs& a, int64_t n0, int lane, i32x4 (*part)[64], const SA& sa) {
+    part[wave][lane] = acc;
+    __syncthreads();
+    const int64_t m = lane & 15, n = n0 + 4 * g;
+    if (wave || m >= a.M) return;
+#pragma unroll
+    for (int w = 1; w < W; ++w) acc += part[w][lane];
+    const float s = sa(m);
+    float y[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int64_t nn = n + e < a.N ? n + e : a.N - 1;
+      y[e] = scaled(acc[e], s, a.b_scale[nn], a.bias ? a.bias[nn] : 0.0f);
+    }
+    TO* o = static_cast<TO*>(a.out) + m * a.ldo;
+    store4(o, y, n, a.N, ((reinterpret_cast<uintptr_t>(a.out) | (uintptr_t)(a.ldo * sizeof(TO))) & (4 * sizeof(TO) - 1)) == 0);
+  }
+};
+
+// On activation codes in memory.  2560 x 2048: 3.4 us; 13 x 2048 x 11008: 11.3 us
 // (128 workgroups, whose CUs take in some 39 GB/s each).
 template <int W, int U, typename TO>
 __global__ __launch_bounds__(64 * W) void k_matmul_i8_rows(LinearArgs a) {
   __shared__ i32x4 part[W][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t n0 = (int64_t)blockIdx.x * 16;
-  const int r = lane & 15, g = lane >> 4;
-  const int K = (int)a.K;
-  // rows that do not exist read the last one: their sums are not stored
-  const int8_t* pb = a.B + (n0 + r < a.N ? n0 + r : a.N - 1) * a.ldb + 16 * g;
-  const int8_t* pa = a.A + (r < a.M ? r : a.M - 1) * a.lda + 16 * g;
-  i32x4 acc = {0, 0, 0, 0};
-  i32x4 fb[2][U], fa[2][U];
-  auto load = [&](int buf, int k) {
+  RowSums<W, U, true> sums(a, n0, lane, wave, a.A, a.lda);
+  sums.begin();
+  sums.run();
+  sums.template finish<TO>(a, n0, lane, part, [&](int64_t m) { return a.a_scale[m]; });
+}
+
+// On activations: every workgroup quantizes the few rows itself (into LDS, as
+// quant_i8.hip does), while its first weights are on their way, which saves a
+// launch and its wait.  Each row's values are read twice, the second time from
+// the nearest cache.
+template <int W, int U, typename T, typename TO>
+__global__ __launch_bounds__(64 * W) void k_linear_i8_rows(LinearArgs a, const T* X, int64_t ldx, int pitch, bool wide) {
+  __shared__ i32x4 part[W][64];
+  __shared__ float peak[W];
+  __shared__ float scales[16];
+  extern __shared__ __attribute__((aligned(16))) int8_t codes[];  // [M][pitch]
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t n0 = (int64_t)blockIdx.x * 16;
+  RowSums<W, U, false> sums(a, n0, lane, wave, codes, pitch);
+  sums.begin();
+  const int M = (int)a.M, K = (int)a.K;
+  // G wavefronts a row, W / G rows at once
+  const int G = M <= 1 ? W : M <= 2 ? W / 2 : M <= 4 ? W / 4 : 1;
+  const int sub = wave & (G - 1), t = sub * 64 + lane;
+  for (int base = 0; base < M; base += W / G) {
+    const int m = base + wave / G;
+    const bool live = m < M;
+    const T* x = X + (live ? m : 0) * ldx;
+    float top = 0.0f;
+    if (live)
+#pragma unroll 4
+      for (int at = t * 8; at < K; at += G * 512) {
+        float v[8];
+        load8(x + at, K - at, wide, v);
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      fb[buf][u] = *reinterpret_cast<const i32x4*>(pb + k + 64 * u);
-      fa[buf][u] = *reinterpret_cast<const i32x4*>(pa + k + 64 * u);
-    }
-  };
-  auto products = [&](int buf) {
-#pragma unroll
-    for (int u = 0; u < U; ++u) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[buf][u], fa[buf][u], acc, 0, 0, 0);
-  };
-  const int rounds = K / (64 * U);
-  int i = wave;
-  if (i < rounds) load(0, i * 64 * U);
-  for (; i < rounds; i += 2 * W) {
-    if (i + W < rounds) load(1, (i + W) * 64 * U);
-    products(0);
-    if (i + W < rounds) {
-      if (i + 2 * W < rounds) load(0, (i + 2 * W) * 64 * U);
-      products(1);
-    }
-  }
-  if (wave == W - 1) {  // the rest of the sum, zeros past K on the weights' side
-    for (int k = rounds * 64 * U; k < K; k += 64) {
-      const int left = K - (k + 16 * g);
-      i32x4 w = {0, 0, 0, 0}, x = w;
-      if (left > 0) {
-        w = *reinterpret_cast<const i32x4*>(pb + k);
-        x = *reinterpret_cast<const i32x4*>(pa + k);
+        for (int e = 0; e < 8; ++e) top = amax_keep(top, v[e]);
       }
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int n = left - 4 * e;  // bytes of this word that belong to the sum
-        if (n < 4) w[e] = n <= 0 ? 0 : w[e] & (int)((1u << (8 * n)) - 1u);
+    for (int off = 32; off >= 1; off >>= 1) top = amax_keep(top, __shfl_xor(top, off, 64));
+    if (G > 1) {
+      if (lane == 0) peak[wave] = top;
+      __syncthreads();
+      for (int w = 0; w < G; ++w) top = amax_keep(top, peak[(wave & ~(G - 1)) + w]);
+      __syncthreads();
+    }
+    const float s = scale_of_amax(top);
+    const float inv = inverse_scale(s);
+    if (live) {
+#pragma unroll 4
+      for (int at = t * 8; at < pitch; at += G * 512) {
+        float v[8];
+        load8(x + at, K - at, wide, v);
+        *reinterpret_cast<uint2*>(codes + m * pitch + at) = codes8(v, inv, s == s);
       }
-      acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(w, x, acc, 0, 0, 0);
+      if (t == 0) scales[m] = s;
     }
   }
-  part[wave][lane] = acc;
   __syncthreads();
-  const int64_t m = r, n = n0 + 4 * g;
-  if (wave || m >= a.M) return;
-#pragma unroll
-  for (int w = 1; w < W; ++w) acc += part[w][lane];
-  const float sa = a.a_scale[m];
-  float y[4];
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const int64_t nn = n + e < a.N ? n + e : a.N - 1;
-    y[e] = (float)acc[e] * (sa * a.b_scale[nn]);
-    if (a.bias) y[e] += a.bias[nn];
-  }
-  TO* o = static_cast<TO*>(a.out) + m * a.ldo;
-  store4(o, y, n, a.N, ((reinterpret_cast<uintptr_t>(a.out) | (uintptr_t)(a.ldo * sizeof(TO))) & (4 * sizeof(TO) - 1)) == 0);
+  sums.run();
+  sums.template finish<TO>(a, n0, lane, part, [&](int64_t m) { return scales[m]; });
 }
 
 // Tiles through LDS, for products with enough rows to fill the matrix cores.
@@ -328,7 +409,7 @@ __global__ __launch_bounds__((TileShape<BM, BN, WM, WN>::kThreads), OCC) void k_
       TO* o = static_cast<TO*>(a.out) + m * a.ldo + n;
       float y[16];
 #pragma unroll
-      for (int e = 0; e < 16; ++e) y[e] = (float)acc[i][j][e] * (sav * sbv[e]) + bias[e];
+      for (int e = 0; e < 16; ++e) y[e] = scaled(acc[i][j][e], sav, sbv[e], bias[e]);
       if (wide && n + 16 <= a.N) {
         constexpr int V = 16 / sizeof(TO);
         struct alignas(16) Piece { TO v[V]; };
@@ -372,8 +453,7 @@ __global__ __launch_bounds__(256) void k_matmul_i8_join(LinearArgs a, const int3
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     const int64_t nn = n + e < a.N ? n + e : a.N - 1;
-    y[e] = (float)sum[e] * (sa * a.b_scale[nn]);
-    if (a.bias) y[e] += a.bias[nn];
+    y[e] = scaled(sum[e], sa, a.b_scale[nn], a.bias ? a.bias[nn] : 0.0f);
   }
   TO* o = static_cast<TO*>(a.out) + m * a.ldo;
   store4(o, y, n, a.N, ((reinterpret_cast<uintptr_t>(a.out) | (uintptr_t)(a.ldo * sizeof(TO))) & (4 * sizeof(TO) - 1)) == 0);
@@ -401,10 +481,28 @@ hipError_t launch_tile(const LinearArgs& a, int split, void* ws, hipStream_t st)
   return hipGetLastError();
 }
 
+// Bytes between rows of codes in LDS: whole steps, and 16 more so that rows start in different banks.
+int linear_rows_pitch(int64_t K) { return (int)((K + 63) / 64 * 64 + 16); }
+
 template <int W, int U, typename TO>
 hipError_t launch_rows(const LinearArgs& a, hipStream_t st) {
   hipLaunchKernelGGL((k_matmul_i8_rows<W, U, TO>), dim3((unsigned)((a.N + 15) / 16)), dim3(64 * W), 0, st, a);
   return hipGetLastError();
+}
+
+template <int W, int U, typename T, typename TO>
+hipError_t launch_linear_rows(const LinearArgs& a, const void* X, int64_t ldx, hipStream_t st) {
+  const bool wide = ((reinterpret_cast<uintptr_t>(X) | (uintptr_t)(ldx * sizeof(T))) & 15) == 0;
+  const int pitch = linear_rows_pitch(a.K);
+  hipLaunchKernelGGL((k_linear_i8_rows<W, U, T, TO>), dim3((unsigned)((a.N + 15) / 16)), dim3(64 * W), (size_t)a.M * pitch, st, a,
+                     static_cast<const T*>(X), ldx, pitch, wide);
+  return hipGetLastError();
+}
+template <typename T>
+hipError_t launch_linear_rows_t(const LinearArgs& a, const void* X, int64_t ldx, hipStream_t st) {
+  if (a.out_dtype == AWSRC_DTYPE_F32) return launch_linear_rows<8, 4, T, float>(a, X, ldx, st);
+  if (a.out_dtype == AWSRC_DTYPE_BF16) return launch_linear_rows<8, 4, T, __bf16>(a, X, ldx, st);
+  return launch_linear_rows<8, 4, T, _Float16>(a, X, ldx, st);
 }
 
 // Which kernel takes a product, and over how many parts of the sum.  Times below
@@ -461,6 +559,21 @@ hipError_t launch_matmul_i8(const LinearArgs& a, void* ws, hipStream_t st) {
   if (a.out_dtype == AWSRC_DTYPE_F32) return launch<float>(a, ws, st);
   if (a.out_dtype == AWSRC_DTYPE_BF16) return launch<__bf16>(a, ws, st);
   return launch<_Float16>(a, ws, st);
+}
+
+bool linear_i8_fused(int64_t M, int64_t N, int64_t K) {
+  // Where the wavefronts of a row read it in at most four pieces a lane (us, with the launch
+  // saved: 1 x 2560 x 2048 4.6 for 5.9; as many at 16 rows, 9.8 for 9, but for 3 x 10900 twice
+  // the time of two launches), and where there are not so many workgroups that quantizing
+  // over and over costs more than a launch (1 x 27648 x 5120: 37 for 33).
+  const int64_t share = M <= 1 ? 1 : M <= 2 ? 2 : M <= 4 ? 4 : 8;
+  return M <= 16 && K * share <= 16384 && N < 8192;
+}
+
+hipError_t launch_linear_i8_fused(const LinearArgs& a, const void* X, int x_dtype, int64_t ldx, hipStream_t st) {
+  if (x_dtype == AWSRC_DTYPE_F32) return launch_linear_rows_t<float>(a, X, ldx, st);
+  if (x_dtype == AWSRC_DTYPE_BF16) return launch_linear_rows_t<__bf16>(a, X, ldx, st);
+  return launch_linear_rows_t<_Float16>(a, X, ldx, st);
 }
 
 }  // namespace awsrc

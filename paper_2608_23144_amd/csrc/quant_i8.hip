@@ -10,36 +10,6 @@ namespace awsrc {
 
 namespace {
 
-// Eight values from x, of which n exist (the others are 0).
-template <typename T>
-__device__ __forceinline__ void load8(const T* __restrict__ x, int64_t n, bool wide, float (&v)[8]) {
-  if (wide && n >= 8) {
-    struct alignas(16) Piece { T v[16 / sizeof(T)]; };
-    constexpr int V = 16 / sizeof(T);
-#pragma unroll
-    for (int p = 0; p < 8 / V; ++p) {
-      const Piece w = reinterpret_cast<const Piece*>(x)[p];
-#pragma unroll
-      for (int e = 0; e < V; ++e) v[p * V + e] = to_f32(w.v[e]);
-    }
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = e < n ? to_f32(x[e]) : 0.0f;
-  }
-}
-
-// Codes of eight values; `live` is false for a row whose scale is NaN.  No
-// clamp: |x| <= amax gives |x inv| <= 127 (1 + 2^-22).
-__device__ __forceinline__ uint2 codes8(const float (&v)[8], float inv, bool live) {
-  uint32_t q[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) q[e] = live ? (uint32_t)(int)rintf(v[e] * inv) : 0u;
-  uint2 o;
-  o.x = (q[0] & 255) | (q[1] & 255) << 8 | (q[2] & 255) << 16 | q[3] << 24;
-  o.y = (q[4] & 255) | (q[5] & 255) << 8 | (q[6] & 255) << 16 | q[7] << 24;
-  return o;
-}
-
 __device__ __forceinline__ void store8(int8_t* __restrict__ c, uint2 w, int64_t n, bool wide) {
   if (wide && n >= 8) {
     *reinterpret_cast<uint2*>(c) = w;

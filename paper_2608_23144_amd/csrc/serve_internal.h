@@ -45,6 +45,36 @@ __device__ __forceinline__ float amax_keep(float m, float x) {
 template <typename T>
 __device__ __forceinline__ float to_f32(T x) { return (float)x; }
 
+// Eight values from x, of which n exist (the others are 0).
+template <typename T>
+__device__ __forceinline__ void load8(const T* __restrict__ x, int64_t n, bool wide, float (&v)[8]) {
+  if (wide && n >= 8) {
+    struct alignas(16) Piece { T v[16 / sizeof(T)]; };
+    constexpr int V = 16 / sizeof(T);
+#pragma unroll
+    for (int p = 0; p < 8 / V; ++p) {
+      const Piece w = reinterpret_cast<const Piece*>(x)[p];
+#pragma unroll
+      for (int e = 0; e < V; ++e) v[p * V + e] = to_f32(w.v[e]);
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = e < n ? to_f32(x[e]) : 0.0f;
+  }
+}
+
+// Codes of eight values; `live` is false for a row whose scale is NaN.  No
+// clamp: |x| <= amax gives |x inv| <= 127 (1 + 2^-22).
+__device__ __forceinline__ uint2 codes8(const float (&v)[8], float inv, bool live) {
+  uint32_t q[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) q[e] = live ? (uint32_t)(int)rintf(v[e] * inv) : 0u;
+  uint2 o;
+  o.x = (q[0] & 255) | (q[1] & 255) << 8 | (q[2] & 255) << 16 | q[3] << 24;
+  o.y = (q[4] & 255) | (q[5] & 255) << 8 | (q[6] & 255) << 16 | q[7] << 24;
+  return o;
+}
+
 struct LinearArgs {
   const int8_t* A;       // [M][lda] activation codes
   int64_t lda;
@@ -63,6 +93,9 @@ hipError_t launch_quantize_rows(const void* X, int x_dtype, int64_t rows, int64_
                                 int64_t ldc, float* scale, hipStream_t st);
 size_t matmul_i8_ws_bytes(int64_t M, int64_t N, int64_t K);
 hipError_t launch_matmul_i8(const LinearArgs& a, void* ws, hipStream_t st);
+// Whether a linear layer of this shape quantizes its rows in the product's kernel, and that kernel (a.A unused).
+bool linear_i8_fused(int64_t M, int64_t N, int64_t K);
+hipError_t launch_linear_i8_fused(const LinearArgs& a, const void* X, int x_dtype, int64_t ldx, hipStream_t st);
 
 struct AppendArgs {
   awsrc_kv_cache c;

@@ -182,7 +182,9 @@ def test_matmul_i8_nan_scales_stay_in_their_rows():
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("M,N,K", [(1, 70, 96), (1, 2560, 2048), (4, 65, 1000), (13, 200, 4100), (40, 90, 33), (200, 130, 257)])
+@pytest.mark.parametrize("M,N,K", [(1, 70, 96), (1, 2560, 2048), (4, 65, 1000), (13, 200, 4100), (40, 90, 33), (200, 130, 257),
+                                   (1, 40, 1), (1, 9000, 11008), (2, 16, 16384), (2, 9001, 100), (3, 50, 10922), (5, 300, 515),
+                                   (8, 1030, 4096), (16, 33, 2048), (16, 130, 2047), (16, 130, 2049), (9, 17, 65), (3, 9000, 70)])
 def test_linear_is_quantize_then_matmul(M, N, K, dtype):
     g = _gen("lin", M, N, K)
     x = (_randn(g, M, K) * torch.exp(_randn(g, K))).to(dtype).to(DEV)

@@ -63,17 +63,21 @@ def test_matmul_needs_ws_bytes():
 
 @pytest.mark.parametrize("bad", [dict(out_dtype=7), dict(x_dtype=5), dict(M=-1), dict(K=0), dict(ldx=32), dict(ldb=40), dict(ldo=4),
                                  dict(X=P + 1), dict(B=P + 8), dict(X=None), dict(B=None), dict(b_scale=None), dict(out=None),
-                                 dict(bias=P + 2), dict(ws=P + 8)])
+                                 dict(bias=P + 2)])
 def test_linear_refuses(bad):
     assert _call(L.awsrc_linear_i8, {**LINEAR, "n": _ws(1 << 40)}, **bad) == EINVAL
 
 
 def test_product_workspaces():
     n = ctypes.c_size_t(0)
-    assert _call(L.awsrc_linear_i8, {**LINEAR, "n": ctypes.byref(n)}, X=None, B=None, b_scale=None, out=None, ws=None) == OK
-    assert n.value >= 3 * 48 + 3 * 4
-    assert _call(L.awsrc_linear_i8, {**LINEAR, "n": _ws(n.value - 1)}) == ENOSPC
-    assert awsrc.linear_i8_workspace_bytes(3, 5, 33) == n.value
+    for M, N, K in ((17, 5, 33), (200, 500, 1000), (3, 9000, 33), (1, 9000, 33), (16, 64, 40000)):
+        shape = dict(M=M, N=N, K=K, ldx=K, ldb=-(-K // 16) * 16, ldo=N)
+        assert _call(L.awsrc_linear_i8, {**LINEAR, "n": ctypes.byref(n)}, X=None, B=None, b_scale=None, out=None, ws=None, **shape) == OK
+        assert n.value >= M * -(-K // 16) * 16 + M * 4
+        assert _call(L.awsrc_linear_i8, {**LINEAR, "n": _ws(n.value - 1)}, **shape) == ENOSPC
+        assert _call(L.awsrc_linear_i8, {**LINEAR, "n": _ws(n.value)}, ws=None, **shape) == ENOSPC
+        assert _call(L.awsrc_linear_i8, {**LINEAR, "n": _ws(n.value)}, ws=P + 8, **shape) == EINVAL
+        assert awsrc.linear_i8_workspace_bytes(M, N, K) == n.value
     for M, N, K in ((1, 2560, 2048), (13, 2048, 11008), (8192, 27648, 5120), (300, 64, 131071)):
         ld = -(-K // 16) * 16
         assert _call(L.awsrc_matmul_i8, {**MATMUL, "n": ctypes.byref(n)}, A=None, a_scale=None, B=None, b_scale=None, out=None,
