@@ -154,6 +154,7 @@ constexpr int kRowTile = 16, kTileRows = 128;  // of the two kernels
 constexpr int kMaxSplit = 2048, kFewSplit = 8;
 struct Plan {
   int tile;                     // query rows of a workgroup
+  int waves;                    // of k_kv_attention_rows
   int tiles_q, n_split, chunk;  // chunk: tokens of a split
 };
 template <int BR>
@@ -190,7 +191,7 @@ struct Query {
 };
 
 // Few rows.  One workgroup: 16 query rows of one (sequence, cached head) and one
-// chunk of its tokens, in tiles of 64 tokens over 4 wavefronts that meet in LDS at
+// chunk of its tokens, in tiles of 64 tokens over W wavefronts that meet in LDS at
 // the end.  Keys and values go from memory to the matrix cores in 16-byte runs of
 // codes per lane, without LDS: a tile's values and the next tile's keys are in
 // flight while the scores and the softmax are computed.
@@ -198,12 +199,13 @@ struct Query {
 // Lane l holds query l % 16.  Row 4 g + i of score tile j is token 16 g + 4 j + i.
 // Q and K agree on an order of the channels in which each lane reads 16
 // consecutive bytes of a key: channels 64 c + 16 g + 8 h + 0..7 are step (c, h).
-template <typename T, int D>
-__global__ __launch_bounds__(256, D == 256 ? 1 : 3) void k_kv_attention_rows(AttentionArgs a, Plan plan, float* parts) {
+template <typename T, int D, int W>
+__global__ __launch_bounds__(64 * W, W == 8 ? 2 : D == 256 ? 1 : 3) void k_kv_attention_rows(AttentionArgs a, Plan plan, float* parts) {
   constexpr int NC = D / 64;  // 64-channel steps of the scores
   constexpr int ND = D / 16;  // 16-channel tiles of the output
-  __shared__ float sh_m[4][16], sh_M[4][16], sh_l[4][16];
-  __shared__ float sh_o[4][16][D + 4];
+  constexpr int kTurn = 64 * W;  // tokens of a round
+  __shared__ float sh_m[W][16], sh_M[W][16], sh_l[W][16];
+  __shared__ float sh_o[W][16][D + 4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 15, g = lane >> 4;
   int b = blockIdx.x;
@@ -266,9 +268,9 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 3) void k_kv_attention_rows(Att
   if (t0 < end) {
     pages(t0);
     load_keys(t0);
-    if (t0 + 256 < end) pages(t0 + 256);
+    if (t0 + kTurn < end) pages(t0 + kTurn);
   }
-  for (; t0 < end; t0 += 256) {
+  for (; t0 < end; t0 += kTurn) {
     sk = sk_next * qscale;
     sv = sv_next;
     bv = bv_next;
@@ -288,34 +290,41 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 3) void k_kv_attention_rows(Att
         sc[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_to_f16x8(w[2], w[3]), qa[2 * c + 1], sc[j], 0, 0, 0);
       }
     }
-    if (t0 + 256 < end) {
-      load_keys(t0 + 256);
-      if (t0 + 512 < end) pages(t0 + 512);
+    if (t0 + kTurn < end) {
+      load_keys(t0 + kTurn);
+      if (t0 + 2 * kTurn < end) pages(t0 + 2 * kTurn);
     }
     // how many of the lane's 16 tokens are seen
     const int left = ok ? lim - (t0 + 16 * g) : 0;
-    float p[16], run[1] = {-__builtin_inff()};
+    // unseen scores become -inf: no product of one with 0 (2^-120 does as well) or NaN
+    sk = left <= 0 ? 1.0f : sk == 0.0f ? 0x1p-120f : sk;
+    if (!__all(left >= 16 || !live)) {
+      asm volatile("");  // keeps this a branch: nearly every tile is seen whole
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      p[e] = e < left ? sc[e >> 2][e & 3] * sk : -__builtin_inff();
-      run[0] = fmaxf(run[0], p[e]);
+      for (int e = 0; e < 16; ++e) sc[e >> 2][e & 3] = e < left ? sc[e >> 2][e & 3] : -__builtin_inff();
     }
+    float x = sc[0][0];
+#pragma unroll
+    for (int e = 1; e < 16; ++e) x = fmaxf(x, sc[e >> 2][e & 3]);
     float alpha_l, alpha_o;
-    if (softmax_step<4, 1>(sm, run, {sv}, {left > 0}, alpha_l, alpha_o)) {
+    if (softmax_step<4, 1>(sm, {x * sk}, {sv}, {left > 0}, alpha_l, alpha_o)) {
       L *= alpha_l;
 #pragma unroll
       for (int d = 0; d < ND; ++d) o[d] *= alpha_o;
     }
-    float l = 0.0f;
+    float p[16], l = 0.0f;
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      p[e] = __builtin_amdgcn_exp2f(p[e] + sm.off[0]);
+      p[e] = __builtin_amdgcn_exp2f(sc[e >> 2][e & 3] * sk + sm.off[0]);
       l += p[e];
     }
     L += l * sm.f[0];
     h8 ph[2];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) ph[e >> 3][e & 7] = (_Float16)(sm.quiet[0] ? 0.0f : p[e]);
+    for (int e = 0; e < 16; ++e) ph[e >> 3][e & 7] = (_Float16)p[e];
+    if (__any(sm.quiet[0])) {
+      if (sm.quiet[0]) ph[0] = ph[1] = h8{0, 0, 0, 0, 0, 0, 0, 0};
+    }
 #pragma unroll
     for (int d = 0; d < ND; ++d) {
       const u32x4_t x = vw[d];
@@ -335,12 +344,12 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 3) void k_kv_attention_rows(Att
   __syncthreads();
   const bool whole = full <= plan.chunk;  // this workgroup saw every token
   float* part = part_of<16>(parts, ((int64_t)(s * a.c.kv_heads + head) * plan.tiles_q + qt) * plan.n_split + split, D);
-  for (int i = threadIdx.x; i < 16 * D / 4; i += 256) {
+  for (int i = threadIdx.x; i < 16 * D / 4; i += 64 * W) {
     const int row = i / (D / 4), d = (i - row * (D / 4)) * 4;
     if (row >= n_rows) break;
     float m = -__builtin_inff(), M = m;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
+    for (int w = 0; w < W; ++w) {
       m = fmaxf(m, sh_m[w][row]);
       M = fmaxf(M, sh_M[w][row]);
     }
@@ -348,7 +357,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 3) void k_kv_attention_rows(Att
     float l = 0.0f;
     fl4 y = {0, 0, 0, 0};
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
+    for (int w = 0; w < W; ++w) {
       l += __builtin_amdgcn_exp2f(sh_m[w][row] - mu) * sh_l[w][row];
       y += __builtin_amdgcn_exp2f(sh_M[w][row] - Mu) * *reinterpret_cast<const fl4*>(&sh_o[w][row][d]);
     }
@@ -767,6 +776,13 @@ Plan plan_of(const AttentionArgs& a) {
   if (split > cap) split = cap;
   if (split > kMaxSplit) split = kMaxSplit;
   if (split < 1) split = 1;
+  p.waves = 4;
+  // A short history and few sequences: eight wavefronts and no split cost less than the second
+  // launch does (1501 tokens: 13.6 us on the GPU and 10.4 on the host, 10.1 and 14.9 split; 2000: 17.3).
+  if (p.tile == kRowTile && split > 1 && most <= 1536 && a.c.head_dim <= 128) {
+    p.waves = 8;
+    split = 1;
+  }
   const int64_t chunk = ((most + split - 1) / split + 255) / 256 * 256;
   p.chunk = (int)(chunk < 256 ? 256 : chunk);
   p.n_split = (int)((most + p.chunk - 1) / p.chunk);
@@ -792,7 +808,13 @@ hipError_t launch_d(const AttentionArgs& a, float* parts, hipStream_t st) {
   const int64_t grid = (int64_t)a.n_seq * a.c.kv_heads * p.tiles_q * p.n_split;
   if (grid > 0x7FFFFFFF) return hipErrorInvalidValue;
   if (p.tile == kRowTile) {
-    hipLaunchKernelGGL((k_kv_attention_rows<T, D>), dim3((unsigned)grid), dim3(256), 0, st, a, p, parts);
+    if constexpr (D <= 128) {
+      if (p.waves == 8) {
+        hipLaunchKernelGGL((k_kv_attention_rows<T, D, 8>), dim3((unsigned)grid), dim3(512), 0, st, a, p, parts);
+        return hipGetLastError();
+      }
+    }
+    hipLaunchKernelGGL((k_kv_attention_rows<T, D, 4>), dim3((unsigned)grid), dim3(256), 0, st, a, p, parts);
     if (p.n_split > 1) return launch_join<kRowTile, T, D>(a, p, parts, st);
     return hipGetLastError();
   }
