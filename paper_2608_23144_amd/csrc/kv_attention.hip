@@ -768,9 +768,20 @@ Plan plan_of(const AttentionArgs& a) {
   const int64_t base = (int64_t)a.n_seq * a.c.kv_heads * p.tiles_q;
   int64_t most = a.table_ld * a.c.page_tokens;
   if (most > a.max_kv) most = a.max_kv;
-  // Splits: about 1024 workgroups (2 x 131071 tokens of a group of 8: 34 us, 38 with 2048), but
-  // at least 256 tokens each (1501 tokens: 11.0 us, 12.1 with 512).
-  const int64_t target = p.tile == kTileRows ? 512 : 1024, least = p.tile == kTileRows ? 512 : 256;
+  // Splits, as far as they fill the machine: each costs a join.  Few rows: as many
+  // workgroups as reside at once on half of the CUs' registers (D = 128: 2 x 131071 tokens of a
+  // group of 8 take 30.5 us in 512 workgroups, 34 in 1024; the ragged batch of 64 130, 141),
+  // of at least 256 tokens (1501 tokens: 11.0 us, 12.1 with 512).  Many rows: one sequence
+  // 512 workgroups (512 rows after 16000 tokens: 111 us, 128 in 1024), a batch, whose lengths differ,
+  // 4096 (ragged pieces of prompts: 109 us, 178 in 512).
+  int64_t target, least;
+  if (p.tile == kRowTile) {
+    target = a.c.head_dim == 64 ? 768 : a.c.head_dim == 128 ? 512 : 256;
+    least = 256;
+  } else {
+    target = a.n_seq == 1 ? 512 : 4096;
+    least = a.n_seq == 1 ? 512 : 1024;
+  }
   int64_t split = p.tile == kTileRows ? target / base : (target + base - 1) / base;
   const int64_t cap = (most + least - 1) / least;
   if (split > cap) split = cap;
