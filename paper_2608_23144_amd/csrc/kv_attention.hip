@@ -402,8 +402,11 @@ struct TileLds {
   static __device__ __forceinline__ int key(int row) { return D == 64 ? (row >> 1) & 7 : row & 15; }
   static constexpr int kKeys = 64 * D * 2, kValues = D * 64 * 2;
   static constexpr int kStage = kKeys + kValues;
-  // per stage and 16-token run: key scale, value scale, page (negative: none); pages of the tile after
-  static constexpr int kBytes = 2 * kStage + 2 * 4 * 12 + 2 * 4 * 4;
+  // by 16-token run: of the two stages the scales and the page (negative: none), of the two tiles to come where
+  // their codes start and the page
+  float run_k[2][4], run_v[2][4];
+  int run_page[2][4], next_page[2][4];
+  int64_t next_k[2][4], next_v[2][4];
 };
 
 template <typename T, int D>
@@ -414,10 +417,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_kv_attention_tiles(At
   constexpr int NL = D / 64;   // 16-byte runs of codes a thread moves per tile, of keys and of values
   using S = TileLds<D>;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
-  float* run_k = reinterpret_cast<float*>(lds + 2 * S::kStage);  // [2][4]
-  float* run_v = run_k + 8;
-  int* run_page = reinterpret_cast<int*>(run_v + 8);
-  int* next_page = run_page + 8;  // [2][4], by parity of the tile
+  S& sh = *reinterpret_cast<S*>(lds + 2 * S::kStage);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r = lane & 31, h = lane >> 5;
   int b = blockIdx.x;
@@ -455,34 +455,37 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_kv_attention_tiles(At
   const int32_t* table = a.table + (int64_t)s * a.table_ld;
   const int P = a.c.page_tokens, shift = __builtin_ctz(P);
   const int64_t stride = (int64_t)P * D;
-  // this thread's runs: of keys, tokens (tid + 256 i) / (D / 16) from channel 16 (tid % (D / 16)); of values,
+  // this thread's runs: of keys, token (tid + 256 i) / (D / 16) from channel 16 (tid % (D / 16)); of values,
   // channel (tid + 256 i) / 4, tokens from 16 (tid % 4)
   constexpr int KR = D / 16;
-  const auto page_at = [&](int t0, int run) -> int {  // tokens past the end take the tile's first page (masked)
-    const int p = table[(t0 + 16 * run < end ? t0 + 16 * run : t0) >> shift];
-    return p >= 0 && p < a.c.n_pages ? p : -1;
+  // where the codes of a tile's runs start, by its first four threads, into place `slot` of the ring; tokens past the
+  // end take the tile's first page (masked)
+  const auto find = [&](int t0, int slot) {
+    const int t = t0 + 16 * tid < end ? t0 + 16 * tid : t0;
+    int page = table[t >> shift];
+    if (page < 0 || page >= a.c.n_pages) page = -1;
+    const int64_t block = ((int64_t)(page < 0 ? 0 : page) * a.c.kv_heads + head) * stride;
+    sh.next_page[slot][tid] = page;
+    sh.next_k[slot][tid] = block + (t & (P - 1)) * D;
+    sh.next_v[slot][tid] = block + (t & (P - 1));
   };
   u32x4_t kw[NL], vw[NL];
   float gk = 0.0f, gv = 0.0f;
   int gp = -1;
-  const auto block_of = [&](int page) { return (int64_t)(page < 0 ? 0 : page) * a.c.kv_heads + head; };
-  const auto load = [&](int t0, const int* pages) {
+  const int8_t* k_mine = a.c.k + ((tid / KR) & 15) * D + 16 * (tid % KR);
+  const int8_t* v_mine = a.c.v + (int64_t)(tid >> 2) * P;
+  const auto load = [&](int slot) {
 #pragma unroll
-    for (int i = 0; i < NL; ++i) {
-      const int x = tid + 256 * i, t = x / KR, c = x % KR;
-      const int slot = ((t0 + (t & ~15) < end ? t0 + (t & ~15) : t0) & (P - 1)) + (t & 15);
-      kw[i] = *reinterpret_cast<const u32x4_t*>(a.c.k + block_of(pages[t >> 4]) * stride + slot * D + 16 * c);
-    }
+    for (int i = 0; i < NL; ++i)  // 256 / KR tokens on: a whole number of runs, but for D = 256, where KR = 16 is one
+      kw[i] = *reinterpret_cast<const u32x4_t*>(k_mine + sh.next_k[slot][(tid + 256 * i) / KR >> 4]);
+    const int8_t* vb = v_mine + sh.next_v[slot][tid & 3];
 #pragma unroll
-    for (int i = 0; i < NL; ++i) {
-      const int x = tid + 256 * i, d = x >> 2, g = x & 3;
-      const int slot = (t0 + 16 * g < end ? t0 + 16 * g : t0) & (P - 1);
-      vw[i] = *reinterpret_cast<const u32x4_t*>(a.c.v + block_of(pages[g]) * stride + (int64_t)d * P + slot);
-    }
+    for (int i = 0; i < NL; ++i) vw[i] = *reinterpret_cast<const u32x4_t*>(vb + (int64_t)(64 * i) * P);
     if (tid < 4) {
-      gp = pages[tid];
-      gk = a.c.k_scale[block_of(gp)];
-      gv = a.c.v_scale[block_of(gp)];
+      gp = sh.next_page[slot][tid];
+      const int64_t block = (int64_t)(gp < 0 ? 0 : gp) * a.c.kv_heads + head;
+      gk = a.c.k_scale[block];
+      gv = a.c.v_scale[block];
     }
   };
   const auto store = [&](int stage) {
@@ -504,9 +507,9 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_kv_attention_tiles(At
       *reinterpret_cast<h8*>(o + ((2 * g + 1) ^ value_key(d)) * 16) = codes_to_f16x8(vw[i][2], vw[i][3]);
     }
     if (tid < 4) {
-      run_k[stage * 4 + tid] = gk;
-      run_v[stage * 4 + tid] = gv;
-      run_page[stage * 4 + tid] = gp;
+      sh.run_k[stage][tid] = gk;
+      sh.run_v[stage][tid] = gv;
+      sh.run_page[stage][tid] = gp;
     }
   };
 
@@ -520,21 +523,20 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_kv_attention_tiles(At
 
   if (start < end) {  // (uniform)
     if (tid < 4) {
-      next_page[tid] = page_at(start, tid);
-      if (start + 64 < end) next_page[4 + tid] = page_at(start + 64, tid);
+      find(start, 0);
+      if (start + 64 < end) find(start + 64, 1);
     }
     __syncthreads();
-    load(start, next_page);
+    load(0);
     store(0);
     __syncthreads();
   }
   int stage = 0;
   for (int t0 = start; t0 < end; t0 += 64, stage ^= 1) {
     const bool more = t0 + 64 < end;
-    int page_after = -1;
     if (more) {
-      load(t0 + 64, next_page + 4 * (stage ^ 1));
-      if (tid < 4 && t0 + 128 < end) page_after = page_at(t0 + 128, tid);
+      load(stage ^ 1);
+      if (tid < 4 && t0 + 128 < end) find(t0 + 128, stage);  // (read a round ago)
     }
     if (t0 < any) {
       const char* base = lds + stage * S::kStage;
@@ -555,15 +557,15 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_kv_attention_tiles(At
       bool whole = t0 + 64 <= all;
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        const int g = stage * 4 + 2 * u + h;
-        const bool ok = run_page[g] >= 0;
+        const int g = 2 * u + h;
+        const bool ok = sh.run_page[stage][g] >= 0;
         whole = whole && ok;
         left[u] = ok ? lim - (t0 + 32 * u + 16 * h) : 0;
         seen[u] = left[u] > 0;
         // unseen scores become -inf: no product of one with 0 (2^-120 does as well) or NaN
-        sk[u] = run_k[g] * qscale;
+        sk[u] = sh.run_k[stage][g] * qscale;
         sk[u] = !seen[u] ? 1.0f : sk[u] == 0.0f ? 0x1p-120f : sk[u];
-        sv[u] = run_v[g];
+        sv[u] = sh.run_v[stage][g];
       }
       if (!__all(whole)) {
         asm volatile("");  // keeps this a branch: nearly every tile is seen whole
@@ -590,6 +592,8 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_kv_attention_tiles(At
       h8 ph[2][2];
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
+        // summed in fp32 before the rounding: p' of a page much quieter than the row's loudest may be 0 in fp16
+        // and still weigh in the denominator
         float l = 0.0f;
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
@@ -615,10 +619,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_kv_attention_tiles(At
                 *reinterpret_cast<const h8*>(row + ((4 * u + 2 * h + k) ^ value_key(r)) * 16), ph[u][k], o[d], 0, 0, 0);
       }
     }
-    if (more) {
-      store(stage ^ 1);
-      if (tid < 4) next_page[4 * stage + tid] = page_after;
-    }
+    if (more) store(stage ^ 1);
     __syncthreads();
   }
   L += __shfl_xor(L, 32, 64);
@@ -830,7 +831,7 @@ hipError_t launch_d(const AttentionArgs& a, float* parts, hipStream_t st) {
     return hipGetLastError();
   }
   const auto k = k_kv_attention_tiles<T, D>;
-  constexpr int bytes = TileLds<D>::kBytes;
+  constexpr int bytes = 2 * TileLds<D>::kStage + sizeof(TileLds<D>);
   if (bytes > 65536) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != hipSuccess) return e;
