@@ -556,9 +556,9 @@ def _on_device(i: int, *ts: Optional[torch.Tensor]) -> None:
 def _empty(shape, like: torch.Tensor, dtype, stream):
     """A new tensor whose memory belongs to the stream that will use it."""
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=like.device)
+        return like.new_empty(shape, dtype=dtype)
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=like.device)
+        return like.new_empty(shape, dtype=dtype)
 
 
 def _raw_stream(i: int, stream) -> int:
@@ -577,7 +577,7 @@ def _rows_of(t: torch.Tensor, what: str):
     ld, step = t.stride()
     if step != 1 and cols > 1:
         raise ValueError(f"{what} must be a matrix with contiguous rows")
-    return rows, cols, ld if rows > 1 else max(cols, ld)
+    return rows, cols, (ld if rows > 1 or ld > cols else cols)
 
 
 def _i8_rows(t: torch.Tensor, what: str):
@@ -666,14 +666,20 @@ def awsrc_quantize_rows_i8(x: torch.Tensor, out=None, stream=None) -> Tuple[torc
     return codes, scale
 
 
-def _check_product_args(dev: int, N: int, scale, bias, out, M: int):
-    _on_device(dev, scale, bias, out)
+def _check_product_args(dev: int, N: int, scale, bias):
+    if scale.get_device() != dev or (bias is not None and bias.get_device() != dev):
+        raise ValueError(f"scales and bias must be on cuda:{dev}")
     if scale.shape != (N,) or scale.dtype != torch.float32 or not scale.is_contiguous():
         raise ValueError("weight scales: fp32 [N]")
     if bias is not None and (bias.shape != (N,) or bias.dtype != torch.float32 or not bias.is_contiguous()):
         raise ValueError("bias: fp32 [N]")
+
+
+def _out_rows(dev: int, out, M: int, N: int) -> int:
+    _on_device(dev, out)
     if out.shape != (M, N):
         raise ValueError(f"out: expected {(M, N)}, got {tuple(out.shape)}")
+    return _rows_of(out, "out")[2]
 
 
 @functools.lru_cache(_WS_SIZES)
@@ -717,13 +723,15 @@ def awsrc_matmul_i8(a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor, b_s
     if a_scale.shape != (M,) or a_scale.dtype != torch.float32 or not a_scale.is_contiguous():
         raise ValueError("a_scale: fp32 [M]")
     if out is None:
-        out = _empty((M, N), a, out_dtype, stream)
-    _check_product_args(dev, N, b_scale, bias, out, M)
+        out, ldo = _empty((M, N), a, out_dtype, stream), N
+    else:
+        ldo = _out_rows(dev, out, M, N)
+    _check_product_args(dev, N, b_scale, bias)
     ws, n, keep = _sized_workspace(workspace, matmul_i8_workspace_bytes(M, N, K), a, stream)
     if M and N:
         _check(LIB.awsrc_matmul_i8(a.data_ptr(), lda, a_scale.data_ptr(), b.data_ptr(), ldb, b_scale.data_ptr(),
                                    None if bias is None else bias.data_ptr(), M, N, K, out.data_ptr(), _act_code(out.dtype),
-                                   _rows_of(out, "out")[2], ws, ctypes.c_size_t(n), _raw_stream(dev, stream)))
+                                   ldo, ws, ctypes.c_size_t(n), _raw_stream(dev, stream)))
     return out
 
 
@@ -738,14 +746,17 @@ def awsrc_linear_i8(x: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, bia
         raise ValueError(f"x has {K} columns, w {Kw}")
     dev = _device_of(x)
     if out is None:
-        out = _empty((M, N), x, x.dtype if out_dtype is None else out_dtype, stream)
-    _on_device(dev, w)
-    _check_product_args(dev, N, w_scale, bias, out, M)
+        out, ldo = _empty((M, N), x, x.dtype if out_dtype is None else out_dtype, stream), N
+    else:
+        ldo = _out_rows(dev, out, M, N)
+    if w.get_device() != dev:
+        raise ValueError(f"tensors must be on one device: {w.device} and cuda:{dev}")
+    _check_product_args(dev, N, w_scale, bias)
     ws, n, keep = _sized_workspace(workspace, linear_i8_workspace_bytes(M, N, K), x, stream)
     if M and N:
         _check(LIB.awsrc_linear_i8(x.data_ptr(), _act_code(x.dtype), ldx, w.data_ptr(), ldw, w_scale.data_ptr(),
                                    None if bias is None else bias.data_ptr(), M, N, K, out.data_ptr(), _act_code(out.dtype),
-                                   _rows_of(out, "out")[2], ws, ctypes.c_size_t(n), _raw_stream(dev, stream)))
+                                   ldo, ws, ctypes.c_size_t(n), _raw_stream(dev, stream)))
     return out
 
 

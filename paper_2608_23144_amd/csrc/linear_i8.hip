@@ -222,7 +222,7 @@ struct TileShape {
   static constexpr int kStage = (BM + BN) * kStep;
 };
 
-template <int BM, int BN, int WM, int WN, int OCC, int NS, typename TO>
+template <int BM, int BN, int WM, int WN, int OCC, int NS, bool ONCE, typename TO>
 __global__ __launch_bounds__((TileShape<BM, BN, WM, WN>::kThreads), OCC) void k_matmul_i8_tile(LinearArgs a, int tiles_m,
                                                                                                int tiles_n,
                                                                                                int split_steps,
@@ -276,7 +276,7 @@ __global__ __launch_bounds__((TileShape<BM, BN, WM, WN>::kThreads), OCC) void k_
       // rows 16 on have bit 2 of the key flipped
       const int p = kRows == 16 && (i & 1) ? pb ^ 64 : pb;
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_ptr)(base + (BM + i * kRows) * kStep), 16,
-                                               k + p < K ? (int)(ob + i * sb + p + k) : (int)0x80000000, 0, 0, 0);
+                                               k + p < K ? (int)(ob + i * sb + p + k) : (int)0x80000000, 0, 0, ONCE ? 2 : 0);
     }
   };
   // fragments: lane -> row lane % 32 of the tile, 16-byte piece 2 ks + lane / 32
@@ -459,10 +459,10 @@ __global__ __launch_bounds__(256) void k_matmul_i8_join(LinearArgs a, const int3
   store4(o, y, n, a.N, ((reinterpret_cast<uintptr_t>(a.out) | (uintptr_t)(a.ldo * sizeof(TO))) & (4 * sizeof(TO) - 1)) == 0);
 }
 
-template <int BM, int BN, int WM, int WN, int OCC, int NS, typename TO>
+template <int BM, int BN, int WM, int WN, int OCC, int NS, bool ONCE, typename TO>
 hipError_t launch_tile(const LinearArgs& a, int split, void* ws, hipStream_t st) {
   using S = TileShape<BM, BN, WM, WN>;
-  const auto k = k_matmul_i8_tile<BM, BN, WM, WN, OCC, NS, TO>;
+  const auto k = k_matmul_i8_tile<BM, BN, WM, WN, OCC, NS, ONCE, TO>;
   const size_t lds = NS * S::kStage;
   if (lds > 65536) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
@@ -538,13 +538,20 @@ Choice choose(int64_t M, int64_t N, int64_t K) {
 template <typename TO>
 hipError_t launch(const LinearArgs& a, void* ws, hipStream_t st) {
   const Choice c = choose(a.M, a.N, a.K);
+  // Weights read once that fill a good part of the last cache go past it (64 x 27648 x 5120: 36.5 us, 33.9 past
+  // it; 64 x 11008 x 2048, whose 23 MB stay there from call to call: 8.8, 10.1 past it).
+  const bool once = a.M <= 64 && a.N * a.K >= (int64_t)1 << 26;
   switch (c.path) {
     case kRows: return launch_rows<8, 4, TO>(a, st);
-    case kTile32: return launch_tile<32, 64, 32, 32, 2, 4, TO>(a, c.split, ws, st);
-    case kTile64: return launch_tile<64, 64, 32, 32, 3, 3, TO>(a, c.split, ws, st);
-    case kTile64Wide: return launch_tile<64, 128, 32, 64, 2, 3, TO>(a, 1, ws, st);
-    case kTile128: return launch_tile<128, 128, 64, 64, 2, 2, TO>(a, 1, ws, st);
-    default: return launch_tile<256, 256, 128, 64, 2, 2, TO>(a, 1, ws, st);
+    case kTile32:
+      return once ? launch_tile<32, 64, 32, 32, 2, 4, true, TO>(a, c.split, ws, st)
+                  : launch_tile<32, 64, 32, 32, 2, 4, false, TO>(a, c.split, ws, st);
+    case kTile64: return launch_tile<64, 64, 32, 32, 3, 3, false, TO>(a, c.split, ws, st);
+    case kTile64Wide:
+      return once ? launch_tile<64, 128, 32, 64, 2, 3, true, TO>(a, 1, ws, st)
+                  : launch_tile<64, 128, 32, 64, 2, 3, false, TO>(a, 1, ws, st);
+    case kTile128: return launch_tile<128, 128, 64, 64, 2, 2, false, TO>(a, 1, ws, st);
+    default: return launch_tile<256, 256, 128, 64, 2, 2, false, TO>(a, 1, ws, st);
   }
 }
 
