@@ -31,29 +31,15 @@ struct Rotary {
   bool whole;  // every row turns by Turn
 };
 
-// Eight adjacent values.
-template <typename T>
-struct alignas(16) Eight {
-  T v[8];
-};
+// Eight adjacent values; `wide`: they lie on 16 bytes.
 template <typename T>
 __device__ __forceinline__ void load8(const T* __restrict__ x, bool wide, float (&v)[8]) {
-  if (wide) {
-    const Eight<T> w = *reinterpret_cast<const Eight<T>*>(x);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = to_f32(w.v[e]);
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = to_f32(x[e]);
-  }
+  awsrc::load8(x, 8, wide, v);
 }
 template <typename T>
 __device__ __forceinline__ void store8(T* __restrict__ x, bool wide, const float (&v)[8]) {
   if (wide) {
-    Eight<T> w;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) w.v[e] = (T)v[e];
-    *reinterpret_cast<Eight<T>*>(x) = w;
+    store_vec8(x, v);
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = (T)v[e];
@@ -314,6 +300,17 @@ __device__ __forceinline__ void append_block(const AppendArgs& a, const Span& sp
   }
 }
 
+// Workgroup b of those for keys and values: which of them, which head, and which
+// of the n_seq * per_seq pages.
+struct Work {
+  int slot, head;
+  bool values;
+};
+__device__ __forceinline__ Work work_of(int b, int heads) {
+  const int slot = (b >> 1) / heads;
+  return {slot, (b >> 1) - slot * heads, (bool)(b & 1)};
+}
+
 // Workgroups [0, n_blocks): keys and values; the rest: queries, a row a wavefront.
 template <typename T, int NI>
 __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a, int n_blocks, int per_seq, bool wide_kv, bool wide_q,
@@ -321,16 +318,14 @@ __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a, int n_blocks, i
   const Rotary rot{a.cos, a.sin, a.rope_len, a.rot / 2, a.interleaved, whole};
   int b = (int)blockIdx.x;
   if (b < n_blocks) {
-    const bool values = b & 1;
-    b >>= 1;
-    const int head = b % a.c.kv_heads;
-    b /= a.c.kv_heads;
-    const int s = b / per_seq;
+    const Work w = work_of(b, a.c.kv_heads);
+    const int s = w.slot / per_seq;
     Span sp;
-    if (!span_of(a.cu, a.kv_len, a.table, a.table_ld, a.c.n_pages, a.n_rows, a.c.page_tokens, s, b - s * per_seq, &sp) || sp.page < 0)
+    if (!span_of(a.cu, a.kv_len, a.table, a.table_ld, a.c.n_pages, a.n_rows, a.c.page_tokens, s, w.slot - s * per_seq, &sp) ||
+        sp.page < 0)
       return;
-    if (values) append_block<T, NI, true>(a, sp, head, rot, wide_kv);
-    else append_block<T, NI, false>(a, sp, head, rot, wide_kv);
+    if (w.values) append_block<T, NI, true>(a, sp, w.head, rot, wide_kv);
+    else append_block<T, NI, false>(a, sp, w.head, rot, wide_kv);
     return;
   }
   const int64_t row = (int64_t)(b - n_blocks) * 4 + (threadIdx.x >> 6);
@@ -364,8 +359,12 @@ __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a, int n_blocks, i
   }
 }
 
+// Values lie turned in a page: their codes go through LDS (rows of P + 4 bytes,
+// so that no two of a wavefront's words share a bank), from where a thread takes
+// eight channels of four tokens; eight threads side by side take 64 channels of
+// the same tokens, for stores of whole lines.
 template <typename T, int NI, bool VALUES>
-__device__ __forceinline__ void read_block(const ReadArgs& a, const Span& sp, int head, bool wide) {
+__device__ __forceinline__ void read_block(const ReadArgs& a, const Span& sp, int head, bool wide, char* lds) {
   const int D = a.c.head_dim, P = a.c.page_tokens;
   const bool there = sp.page >= 0;
   const int64_t block = (int64_t)(there ? sp.page : 0) * a.c.kv_heads + head;
@@ -373,19 +372,29 @@ __device__ __forceinline__ void read_block(const ReadArgs& a, const Span& sp, in
   const float sc = there ? (VALUES ? a.c.v_scale : a.c.k_scale)[block] : __builtin_nanf("");
   T* out = static_cast<T*>(VALUES ? a.v_out : a.k_out) + (sp.row0 * a.c.kv_heads + head) * D;
   const int at = (int)(sp.lo - sp.p0), end = (int)(sp.hi - sp.p0);
+  if constexpr (VALUES) {
+    const int shift = __builtin_ctz(P) - 4;
+#pragma unroll
+    for (int i = 0; i < 2 * NI; ++i) {
+      const int x = i * 256 + threadIdx.x, d = x >> shift, t = (x & ((1 << shift) - 1)) * 16;
+      if (d >= D || t >= end || t + 16 <= at) continue;
+      const uint4 w = *reinterpret_cast<const uint4*>(codes + d * P + t);
+      uint32_t* o = reinterpret_cast<uint32_t*>(lds + d * (P + 4) + t);
+      o[0] = w.x; o[1] = w.y; o[2] = w.z; o[3] = w.w;
+    }
+    __syncthreads();
+  }
 #pragma unroll
   for (int i = 0; i < NI; ++i) {
     uint32_t w[8];
     int vt = 0, vd = 0;
     if constexpr (VALUES) {
-      // eight threads side by side take 64 channels of the same tokens: stores of whole lines
       const int x = i * 256 + threadIdx.x, shift = __builtin_ctz(P) - 2;
       vt = ((x >> 3) & ((1 << shift) - 1)) * 4;
       vd = ((x >> 3 >> shift) * 8 + (x & 7)) * 8;
-      const int t = vt, d = vd;
-      if (d >= D || t >= end || t + 4 <= at) continue;
+      if (vd >= D || vt >= end || vt + 4 <= at) continue;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) w[e] = *reinterpret_cast<const uint32_t*>(codes + (int64_t)(d + e) * P + t);
+      for (int e = 0; e < 8; ++e) w[e] = *reinterpret_cast<const uint32_t*>(lds + (vd + e) * (P + 4) + vt);
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -412,16 +421,14 @@ __device__ __forceinline__ void read_block(const ReadArgs& a, const Span& sp, in
 
 template <typename T, int NI>
 __global__ __launch_bounds__(256) void k_kv_read(ReadArgs a, int per_seq, bool wide) {
-  int b = (int)blockIdx.x;
-  const bool values = b & 1;
-  b >>= 1;
-  const int head = b % a.c.kv_heads;
-  b /= a.c.kv_heads;
-  const int s = b / per_seq;
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  const Work w = work_of((int)blockIdx.x, a.c.kv_heads);
+  const int s = w.slot / per_seq;
   Span sp;
-  if (!span_of(a.cu, a.kv_len, a.table, a.table_ld, a.c.n_pages, a.n_rows, a.c.page_tokens, s, b - s * per_seq, &sp)) return;
-  if (values) read_block<T, NI, true>(a, sp, head, wide);
-  else read_block<T, NI, false>(a, sp, head, wide);
+  if (!span_of(a.cu, a.kv_len, a.table, a.table_ld, a.c.n_pages, a.n_rows, a.c.page_tokens, s, w.slot - s * per_seq, &sp))
+    return;
+  if (w.values) read_block<T, NI, true>(a, sp, w.head, wide, lds);
+  else read_block<T, NI, false>(a, sp, w.head, wide, lds);
 }
 
 // Pages that n rows can touch from any starting position.
@@ -440,7 +447,8 @@ hipError_t launch_append(const AppendArgs& a, int64_t grid, int64_t n_blocks, in
 template <typename T, int NI>
 hipError_t launch_read(const ReadArgs& a, int64_t grid, int64_t per_seq, hipStream_t st) {
   const bool wide = on16(a.k_out, 0, 0) && on16(a.v_out, 0, 0);  // rows are a multiple of 128 bytes apart
-  hipLaunchKernelGGL((k_kv_read<T, NI>), dim3((unsigned)grid), dim3(256), 0, st, a, (int)per_seq, wide);
+  hipLaunchKernelGGL((k_kv_read<T, NI>), dim3((unsigned)grid), dim3(256), (size_t)a.c.head_dim * (a.c.page_tokens + 4), st, a,
+                     (int)per_seq, wide);
   return hipGetLastError();
 }
 

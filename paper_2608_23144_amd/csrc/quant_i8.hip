@@ -33,12 +33,21 @@ __global__ __launch_bounds__(64 * (WPR == 1 ? 4 : WPR)) void k_quantize_rows(con
   if (row >= rows) return;
   const int t = WPR == 1 ? (threadIdx.x & 63) : threadIdx.x;
   const T* x = X + row * ldx;
+  // Where rows do not lie on 16 bytes a lane takes every (64 WPR)-th value of a
+  // stretch instead of eight adjacent ones, so that a load still reads whole lines.
+  const int64_t step = wide_x ? 1 : WPR * 64;
+  const auto start = [&](int i) { return wide_x ? (int64_t)(i * WPR * 64 + t) * 8 : (int64_t)i * WPR * 512 + t; };
   float v[CH][8];
   float m = 0.0f;
 #pragma unroll
   for (int i = 0; i < CH; ++i) {
-    const int64_t at = (int64_t)(i * WPR * 64 + t) * 8;
-    load8(x + at, cols - at, wide_x, v[i]);
+    const int64_t at = start(i);
+    if (wide_x) {
+      load8(x + at, cols - at, true, v[i]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[i][e] = at + e * step < cols ? to_f32(x[at + e * step]) : 0.0f;
+    }
   }
 #pragma unroll
   for (int i = 0; i < CH; ++i)
@@ -59,8 +68,16 @@ __global__ __launch_bounds__(64 * (WPR == 1 ? 4 : WPR)) void k_quantize_rows(con
   int8_t* c = codes + row * ldc;
 #pragma unroll
   for (int i = 0; i < CH; ++i) {
-    const int64_t at = (int64_t)(i * WPR * 64 + t) * 8;
-    if (at < pad) store8(c + at, codes8(v[i], inv, live), pad - at, wide_c);
+    const int64_t at = start(i);
+    if (at >= pad) continue;
+    const uint2 w = codes8(v[i], inv, live);
+    if (wide_x) {
+      store8(c + at, w, pad - at, wide_c);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (at + e * step < pad) c[at + e * step] = (int8_t)((e < 4 ? w.x : w.y) >> (8 * (e & 3)));
+    }
   }
   if (t == 0) scale[row] = s;
 }

@@ -45,18 +45,40 @@ __device__ __forceinline__ float amax_keep(float m, float x) {
 template <typename T>
 __device__ __forceinline__ float to_f32(T x) { return (float)x; }
 
+// Eight adjacent values on 16 bytes, as vector accesses (copies of a struct of
+// eight are taken apart by the compiler and merged with the element-wise path).
+template <typename T>
+__device__ __forceinline__ void load_vec8(const T* __restrict__ x, float (&v)[8]) {
+  if constexpr (sizeof(T) == 4) {
+    const fl4 a = reinterpret_cast<const fl4*>(x)[0], b = reinterpret_cast<const fl4*>(x)[1];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = e < 4 ? a[e & 3] : b[e & 3];
+  } else {
+    typedef T t8 __attribute__((ext_vector_type(8)));
+    const t8 w = *reinterpret_cast<const t8*>(x);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = to_f32((T)w[e]);
+  }
+}
+template <typename T>
+__device__ __forceinline__ void store_vec8(T* __restrict__ x, const float (&v)[8]) {
+  if constexpr (sizeof(T) == 4) {
+    reinterpret_cast<fl4*>(x)[0] = fl4{v[0], v[1], v[2], v[3]};
+    reinterpret_cast<fl4*>(x)[1] = fl4{v[4], v[5], v[6], v[7]};
+  } else {
+    typedef T t8 __attribute__((ext_vector_type(8)));
+    t8 w;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w[e] = (T)v[e];
+    *reinterpret_cast<t8*>(x) = w;
+  }
+}
+
 // Eight values from x, of which n exist (the others are 0).
 template <typename T>
 __device__ __forceinline__ void load8(const T* __restrict__ x, int64_t n, bool wide, float (&v)[8]) {
   if (wide && n >= 8) {
-    struct alignas(16) Piece { T v[16 / sizeof(T)]; };
-    constexpr int V = 16 / sizeof(T);
-#pragma unroll
-    for (int p = 0; p < 8 / V; ++p) {
-      const Piece w = reinterpret_cast<const Piece*>(x)[p];
-#pragma unroll
-      for (int e = 0; e < V; ++e) v[p * V + e] = to_f32(w.v[e]);
-    }
+    load_vec8(x, v);
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = e < n ? to_f32(x[e]) : 0.0f;
