@@ -562,6 +562,8 @@ def _empty(shape, like: torch.Tensor, dtype, stream):
 
 
 def _raw_stream(i: int, stream) -> int:
+    if torch._C._cuda_getDevice() != i:
+        raise ValueError(f"tensors on cuda:{i}, which is not the current device")
     if stream is None:
         return torch._C._cuda_getCurrentRawStream(i)
     if stream.device_index != i:

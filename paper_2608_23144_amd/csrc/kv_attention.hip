@@ -154,7 +154,7 @@ constexpr int kRowTile = 16, kTileRows = 128;  // of the two kernels
 constexpr int kMaxSplit = 2048, kFewSplit = 8;
 struct Plan {
   int tile;                     // query rows of a workgroup
-  int waves;                    // of k_kv_attention_rows
+  int waves;                    // of a workgroup
   int tiles_q, n_split, chunk;  // chunk: tokens of a split
 };
 template <int BR>
@@ -386,9 +386,9 @@ __device__ __forceinline__ void store_row4(T* out, fl4 y, float l, float f) {
   *reinterpret_cast<Four*>(out) = w;
 }
 
-// Many rows.  One workgroup: 128 query rows of one (sequence, cached head), 32 a
+// Many rows.  One workgroup: 32 W query rows of one (sequence, cached head), 32 a
 // wavefront, over tiles of 64 tokens whose codes become fp16 once, on their way
-// into LDS (two stages), and then serve all four wavefronts through 32 x 32 x 16
+// into LDS (two stages), and then serve all W wavefronts through 32 x 32 x 16
 // products.  The next tile's codes are on their way from memory while the
 // current one is computed.
 //
@@ -409,12 +409,14 @@ struct TileLds {
   int64_t next_k[2][4], next_v[2][4];
 };
 
-template <typename T, int D>
-__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_kv_attention_tiles(AttentionArgs a, Plan plan, float* parts) {
-  constexpr int BR = kTileRows;
+template <typename T, int D, int W>
+__global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void k_kv_attention_tiles(AttentionArgs a, Plan plan, float* parts) {
+  constexpr int BR = 32 * W;
+  constexpr int kThreads = 64 * W;
   constexpr int NS = D / 16;   // 16-channel steps of the scores
   constexpr int ND = D / 32;   // 32-channel tiles of the output
-  constexpr int NL = D / 64;   // 16-byte runs of codes a thread moves per tile, of keys and of values
+  constexpr int NL = D * 4 / kThreads;  // 16-byte runs of codes a thread moves per tile, of keys and of values
+  static_assert(NL >= 1 && NL * kThreads == D * 4, "runs of a tile");
   using S = TileLds<D>;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   S& sh = *reinterpret_cast<S*>(lds + 2 * S::kStage);
@@ -455,8 +457,8 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_kv_attention_tiles(At
   const int32_t* table = a.table + (int64_t)s * a.table_ld;
   const int P = a.c.page_tokens, shift = __builtin_ctz(P);
   const int64_t stride = (int64_t)P * D;
-  // this thread's runs: of keys, token (tid + 256 i) / (D / 16) from channel 16 (tid % (D / 16)); of values,
-  // channel (tid + 256 i) / 4, tokens from 16 (tid % 4)
+  // this thread's runs: of keys, token (tid + kThreads i) / (D / 16) from channel 16 (tid % (D / 16)); of values,
+  // channel (tid + kThreads i) / 4, tokens from 16 (tid % 4)
   constexpr int KR = D / 16;
   // where the codes of a tile's runs start, by its first four threads, into place `slot` of the ring; tokens past the
   // end take the tile's first page (masked)
@@ -476,11 +478,11 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_kv_attention_tiles(At
   const int8_t* v_mine = a.c.v + (int64_t)(tid >> 2) * P;
   const auto load = [&](int slot) {
 #pragma unroll
-    for (int i = 0; i < NL; ++i)  // 256 / KR tokens on: a whole number of runs, but for D = 256, where KR = 16 is one
-      kw[i] = *reinterpret_cast<const u32x4_t*>(k_mine + sh.next_k[slot][(tid + 256 * i) / KR >> 4]);
+    for (int i = 0; i < NL; ++i)  // kThreads / KR tokens on: a whole number of runs
+      kw[i] = *reinterpret_cast<const u32x4_t*>(k_mine + sh.next_k[slot][(tid + kThreads * i) / KR >> 4]);
     const int8_t* vb = v_mine + sh.next_v[slot][tid & 3];
 #pragma unroll
-    for (int i = 0; i < NL; ++i) vw[i] = *reinterpret_cast<const u32x4_t*>(vb + (int64_t)(64 * i) * P);
+    for (int i = 0; i < NL; ++i) vw[i] = *reinterpret_cast<const u32x4_t*>(vb + (int64_t)(kThreads / 4 * i) * P);
     if (tid < 4) {
       gp = sh.next_page[slot][tid];
       const int64_t block = (int64_t)(gp < 0 ? 0 : gp) * a.c.kv_heads + head;
@@ -492,7 +494,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_kv_attention_tiles(At
     char* base = lds + stage * S::kStage;
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
-      const int x = tid + 256 * i, t = x / KR, c = x % KR;
+      const int x = tid + kThreads * i, t = x / KR, c = x % KR;
       // token 32 u + 16 h + 4 b + e is row 32 u + 8 b + 4 h + e
       const int row = (t & 32) | ((t >> 2) & 3) << 3 | ((t >> 4) & 1) << 2 | (t & 3);
       char* o = base + row * 2 * D;
@@ -501,7 +503,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_kv_attention_tiles(At
     }
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
-      const int x = tid + 256 * i, d = x >> 2, g = x & 3;
+      const int x = tid + kThreads * i, d = x >> 2, g = x & 3;
       char* o = base + S::kKeys + d * 128;
       *reinterpret_cast<h8*>(o + ((2 * g) ^ value_key(d)) * 16) = codes_to_f16x8(vw[i][0], vw[i][1]);
       *reinterpret_cast<h8*>(o + ((2 * g + 1) ^ value_key(d)) * 16) = codes_to_f16x8(vw[i][2], vw[i][3]);
@@ -799,6 +801,17 @@ Plan plan_of(const AttentionArgs& a) {
   p.chunk = (int)(chunk < 256 ? 256 : chunk);
   p.n_split = (int)((most + p.chunk - 1) / p.chunk);
   if (p.n_split < 1) p.n_split = 1;
+  // Rows enough for every CU twice without a split: 256 a workgroup, which halves the work of turning
+  // codes into fp16 (8192 tokens of a 3B layer: 363 us with 128, 333; 1000 tokens each of four
+  // sequences of a 32B layer, where whole workgroups of the shorter ones idle, 67 and 71).
+  if (p.tile == kTileRows && p.n_split == 1 && a.c.head_dim == 128 && rows >= 16384) {
+    const int64_t wide = (rows + 2 * kTileRows - 1) / (2 * kTileRows);
+    if ((int64_t)a.n_seq * a.c.kv_heads * wide >= 512) {
+      p.tile = 2 * kTileRows;
+      p.waves = 8;
+      p.tiles_q = (int)wide;
+    }
+  }
   return p;
 }
 
@@ -811,6 +824,18 @@ hipError_t launch_join(const AttentionArgs& a, const Plan& p, const float* parts
                        parts, (int)items, (int)per_head);
   else
     hipLaunchKernelGGL((k_kv_attention_join<BR, T, D>), dim3((unsigned)items), dim3(256), 0, st, a, p, parts, (int)per_head);
+  return hipGetLastError();
+}
+
+template <typename T, int D, int W>
+hipError_t launch_tiles(const AttentionArgs& a, const Plan& p, int64_t grid, float* parts, hipStream_t st) {
+  const auto k = k_kv_attention_tiles<T, D, W>;
+  constexpr int bytes = 2 * TileLds<D>::kStage + sizeof(TileLds<D>);
+  if (bytes > 65536) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL(k, dim3((unsigned)grid), dim3(64 * W), bytes, st, a, p, parts);
   return hipGetLastError();
 }
 
@@ -830,15 +855,10 @@ hipError_t launch_d(const AttentionArgs& a, float* parts, hipStream_t st) {
     if (p.n_split > 1) return launch_join<kRowTile, T, D>(a, p, parts, st);
     return hipGetLastError();
   }
-  const auto k = k_kv_attention_tiles<T, D>;
-  constexpr int bytes = 2 * TileLds<D>::kStage + sizeof(TileLds<D>);
-  if (bytes > 65536) {
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (e != hipSuccess) return e;
-  }
-  hipLaunchKernelGGL(k, dim3((unsigned)grid), dim3(256), bytes, st, a, p, parts);
-  if (p.n_split > 1) return launch_join<kTileRows, T, D>(a, p, parts, st);
-  return hipGetLastError();
+  if constexpr (D == 128)
+    if (p.waves == 8) return launch_tiles<T, D, 8>(a, p, grid, parts, st);
+  const hipError_t e = launch_tiles<T, D, 4>(a, p, grid, parts, st);
+  return e == hipSuccess && p.n_split > 1 ? launch_join<kTileRows, T, D>(a, p, parts, st) : e;
 }
 
 template <typename T>

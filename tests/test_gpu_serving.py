@@ -477,6 +477,34 @@ def test_attention_over_long_sequences(hq, hk, D, dtype):
     _check_attention(Batch(("long2", hq, hk, D), hq, hk, D, 16, [6007], [40], dtype))
 
 
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("hq,hk,lens,news", [(64, 8, [2050], [2050]), (16, 2, [4200, 3001, 2300], [4100, 3001, 2077]), (32, 1, [2600], [1111])])
+def test_attention_many_rows(hq, hk, lens, news, causal):
+    """Rows enough for the widest workgroups; some heads against 64 bits on the GPU."""
+    b = Batch(("many", hq, hk), hq, hk, 128, 64, lens, news, torch.float16)
+    cache, cu, kv_len, table = b.dev()
+    out = awsrc.awsrc_kv_attention(cache, b.q.to(DEV), cu, kv_len, table, max(news), max(lens), causal=causal)
+    G, scale = hq // hk, 128 ** -0.5
+    for s, (n, m) in enumerate(zip(lens, news)):
+        pages = table[s, :-(-n // 64)].long()
+        r0 = int(b.cu[s])
+        for h in sorted({0, hk - 1}):
+            k = (cache[0][pages, h].double() * cache[2][pages, h].double()[:, None, None]).reshape(-1, 128)[:n]
+            v = (cache[1][pages, h].double() * cache[3][pages, h].double()[:, None, None]).transpose(1, 2).reshape(-1, 128)[:n]
+            for g in sorted({0, G - 1}):
+                q = b.q[r0:r0 + m, h * G + g].to(DEV).double()
+                sc = q @ k.T * scale
+                if causal:
+                    sc = sc + torch.triu(torch.full_like(sc, -float("inf")), n - m + 1)
+                p = torch.softmax(sc, -1)
+                want = p @ v
+                mag = ((q.abs() @ k.abs().T).amax(1) * scale)[:, None]
+                tol = (2.0 ** -11 + 2 * 136 * 2.0 ** -24 * mag + (n + 16) * 2.0 ** -23) * (p @ v.abs()) + n * 2.0 ** -25 * v.abs().max()
+                tol = tol + EPS[b.dtype] * (want.abs() + tol) + FLOOR[b.dtype]
+                err = (out[r0:r0 + m, h * G + g].double() - want).abs()
+                assert (err <= tol).all(), float((err / tol).max())
+
+
 def test_attention_rows_that_see_nothing():
     """More rows than tokens: the first see none and are 0; a sequence without tokens likewise."""
     b = Batch(("none",), 4, 2, 64, 16, [3, 0, 40], [9, 2, 45], torch.float16)
