@@ -391,40 +391,79 @@ __global__ __launch_bounds__((TileShape<BM, BN, WM, WN>::kThreads), OCC) void k_
     return;
   }
   const bool wide = ((reinterpret_cast<uintptr_t>(a.out) | (uintptr_t)(a.ldo * sizeof(TO))) & 15) == 0;
+  float sav[TM];
 #pragma unroll
-  for (int i = 0; i < TN; ++i) {
-    const int64_t n = n0 + wn + 32 * i + 16 * half;
-    float sbv[16], bias[16];
+  for (int j = 0; j < TM; ++j) {
+    const int64_t m = m0 + wm + 32 * j + r;
+    sav[j] = a.a_scale[m < a.M ? m : a.M - 1];
+  }
+  // Results go out by groups of 64 or 128 bytes of a row: through the wavefront's own part of LDS (the stages are done
+  // with), so that a store covers whole lines instead of a 16-byte piece of each of 64.
+  constexpr int GT = WN * sizeof(TO) >= 128 && sizeof(TO) == 2 ? 2 : 1;  // 32-column tiles of a group
+  constexpr int V = 16 / sizeof(TO), kPieces = 32 * GT / V;              // values of a piece, pieces of a group's row
+  static_assert(WM * kPieces * 16 * S::kWaves <= NS * S::kStage, "LDS of the results");
+  typedef TO Piece __attribute__((ext_vector_type(16 / sizeof(TO))));
+  char* mine = lds + wave * (WM * kPieces * 16);
+  __syncthreads();
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const int64_t nn = n + e < a.N ? n + e : a.N - 1;
-      sbv[e] = a.b_scale[nn];
-      bias[e] = a.bias ? a.bias[nn] : 0.0f;
-    }
+  for (int i0 = 0; i0 < TN; i0 += GT) {
+    const bool whole = wide && n0 + wn + 32 * (i0 + GT) <= a.N;
 #pragma unroll
-    for (int j = 0; j < TM; ++j) {
-      const int64_t m = m0 + wm + 32 * j + r;
-      if (m >= a.M) continue;
-      const float sav = a.a_scale[m];
-      TO* o = static_cast<TO*>(a.out) + m * a.ldo + n;
-      float y[16];
+    for (int i = i0; i < i0 + GT; ++i) {
+      const int64_t n = n0 + wn + 32 * i + 16 * half;
+      float sbv[16], bias[16];
+      if (n0 + wn + 32 * (i + 1) <= a.N && (reinterpret_cast<uintptr_t>(a.b_scale) & 15) == 0 &&
+          (reinterpret_cast<uintptr_t>(a.bias) & 15) == 0) {
 #pragma unroll
-      for (int e = 0; e < 16; ++e) y[e] = scaled(acc[i][j][e], sav, sbv[e], bias[e]);
-      if (wide && n + 16 <= a.N) {
-        constexpr int V = 16 / sizeof(TO);
-        struct alignas(16) Piece { TO v[V]; };
+        for (int e = 0; e < 16; e += 4) {
+          const fl4 x = *reinterpret_cast<const fl4*>(a.b_scale + n + e);
+          const fl4 y = a.bias ? *reinterpret_cast<const fl4*>(a.bias + n + e) : fl4{0, 0, 0, 0};
 #pragma unroll
-        for (int p = 0; p < 16 / V; ++p) {
-          Piece w;
-#pragma unroll
-          for (int e = 0; e < V; ++e) w.v[e] = (TO)y[p * V + e];
-          *reinterpret_cast<Piece*>(o + p * V) = w;
+          for (int f = 0; f < 4; ++f) {
+            sbv[e + f] = x[f];
+            bias[e + f] = y[f];
+          }
         }
       } else {
 #pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if (n + e < a.N) o[e] = (TO)y[e];
+        for (int e = 0; e < 16; ++e) {
+          const int64_t nn = n + e < a.N ? n + e : a.N - 1;
+          sbv[e] = a.b_scale[nn];
+          bias[e] = a.bias ? a.bias[nn] : 0.0f;
+        }
       }
+#pragma unroll
+      for (int j = 0; j < TM; ++j) {
+        if (whole) {
+          const int row = 32 * j + r;
+#pragma unroll
+          for (int p = 0; p < 16 / V; ++p) {
+            Piece w;
+#pragma unroll
+            for (int e = 0; e < V; ++e) w[e] = (TO)scaled(acc[i][j][p * V + e], sav[j], sbv[p * V + e], bias[p * V + e]);
+            const int at = (32 * (i - i0) + 16 * half) / V + p;
+            *reinterpret_cast<Piece*>(mine + (row * kPieces + (at ^ (row & (kPieces - 1)))) * 16) = w;
+          }
+        } else {
+          const int64_t m = m0 + wm + 32 * j + r;
+          if (m >= a.M) continue;
+          TO* o = static_cast<TO*>(a.out) + m * a.ldo + n;
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (n + e < a.N) o[e] = (TO)scaled(acc[i][j][e], sav[j], sbv[e], bias[e]);
+        }
+      }
+    }
+    if (whole) {
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+      for (int p = 0; p < WM * kPieces / 64; ++p) {
+        const int x = p * 64 + lane, row = x / kPieces, at = x % kPieces;
+        const int64_t m = m0 + wm + row;
+        const Piece w = *reinterpret_cast<const Piece*>(mine + (row * kPieces + (at ^ (row & (kPieces - 1)))) * 16);
+        if (m < a.M) *reinterpret_cast<Piece*>(static_cast<TO*>(a.out) + m * a.ldo + n0 + wn + 32 * i0 + at * V) = w;
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
   }
 }
@@ -520,11 +559,11 @@ Choice choose(int64_t M, int64_t N, int64_t K) {
   // (16 x 11008 x 2048: 10.5 against 8.2; 16 x 27648 x 5120: 44 against 30).
   if (M <= 16 && N < 8192) return {kRows, 1};
   // 256 tiles of 128 cost 24 us at K = 5120, a round of 256 tiles of 256, one per CU, 62
-  // to 80 (512 x 27648 x 5120: 112 and 90; 4096 x 5120 x 5120, two rounds, 121 and 140;
-  // 1024 x 5120 x 5120: 39 and 55; 8192 x 27648 x 5120: 1303 and 1113).
+  // to 80 (512 x 27648 x 5120: 117 and 93; 4096 x 5120 x 5120, two rounds, 117 and 123;
+  // 1024 x 5120 x 5120: 40 and 54; 8192 x 27648 x 5120: 1249 and 1105).
   const int64_t t128 = tiles(128, 128), t256 = tiles(256, 256);
   if (M > 64 && t128 >= 256) return {2.9 * ((t256 + 255) / 256) < t128 / 256.0 + 0.5 ? kTile256 : kTile128, 1};
-  // 64 x 27648 x 5120: 64 x 64 tiles 40.8, 64 x 128 tiles 37.4 (64 x 11008 x 2048: 8.8 and 10.9)
+  // 64 x 27648 x 5120: 64 x 64 tiles 42.0, 64 x 128 tiles 35.1 (64 x 11008 x 2048: 8.8 and 10.5)
   if (M > 32 && tiles(64, 128) >= 192) return {kTile64Wide, 1};
   const Path path = M > 32 ? kTile64 : kTile32;
   // Few tiles under a long sum: parts of at least 16 steps, joined by a second

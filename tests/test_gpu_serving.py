@@ -169,6 +169,19 @@ def test_matmul_i8_strided_and_guarded(M, N, K, dtype):
         assert (buf[mask] == 7.0).all()
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("M,N,K", [(7, 70, 80), (33, 160, 300), (70, 24640, 96), (300, 272, 144)])
+def test_matmul_i8_scales_off_16_bytes(M, N, K, dtype):
+    """Scales and bias from any element of a longer vector."""
+    g = _gen("scales", M, N, K)
+    a, b = _codes(g, M, K), _codes(g, N, K)
+    sa, sb, bias = (torch.rand(n + 3, generator=g).to(DEV) for n in (M, N, N))
+    for i, j, k in ((0, 1, 0), (3, 0, 2), (1, 2, 3)):
+        v = (sa[i:i + M], sb[j:j + N], bias[k:k + N])
+        out = awsrc.awsrc_matmul_i8(a, v[0], b, v[1], bias=v[2], out_dtype=dtype)
+        _check_product(out, a, v[0], b, v[1], v[2], dtype)
+
+
 def test_matmul_i8_nan_scales_stay_in_their_rows():
     g = _gen("nan")
     a, b = _codes(g, 70, 128), _codes(g, 90, 128)
