@@ -409,6 +409,20 @@ struct TileLds {
   int64_t next_k[2][4], next_v[2][4];
 };
 
+// The order of a block of N matrix products, consecutive ones on different sums: every operand is read from LDS four
+// products ahead.  8192 tokens of a 3B layer: 331 us, 338 in the compiler's own order and with whole sums in a row.
+template <int N>
+__device__ __forceinline__ void reads_ahead() {
+  constexpr int kProduct = 0x8, kRead = 0x100;
+  __builtin_amdgcn_sched_group_barrier(kRead, 6, 0);  // (two may be others of the block)
+#pragma unroll
+  for (int i = 0; i < N - 4; ++i) {
+    __builtin_amdgcn_sched_group_barrier(kProduct, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(kRead, 1, 0);
+  }
+  __builtin_amdgcn_sched_group_barrier(kProduct, 4, 0);
+}
+
 template <typename T, int D, int W>
 __global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void k_kv_attention_tiles(AttentionArgs a, Plan plan, float* parts) {
   constexpr int BR = 32 * W;
@@ -544,15 +558,16 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void k_kv_attention_tiles
       const char* base = lds + stage * S::kStage;
       fl16 sc[2];
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
+      for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int e = 0; e < 16; ++e) sc[u][e] = 0.0f;
-        const char* row = base + (32 * u + r) * 2 * D;
 #pragma unroll
-        for (int k = 0; k < NS; ++k)
-          sc[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const h8*>(row + ((2 * k + h) ^ S::key(r)) * 16), qa[k],
-                                                         sc[u], 0, 0, 0);
-      }
+      for (int k = 0; k < NS; ++k)
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+          sc[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+              *reinterpret_cast<const h8*>(base + (32 * u + r) * 2 * D + ((2 * k + h) ^ S::key(r)) * 16), qa[k], sc[u], 0, 0, 0);
+      reads_ahead<2 * NS>();
       float sk[2], sv[2], run[2];
       bool seen[2];
       int left[2];
@@ -611,15 +626,14 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void k_kv_attention_tiles
           if (sm.quiet[u]) ph[u][0] = ph[u][1] = h8{0, 0, 0, 0, 0, 0, 0, 0};
       }
 #pragma unroll
-      for (int d = 0; d < ND; ++d) {
-        const char* row = base + S::kKeys + (32 * d + r) * 128;
+      for (int j = 0; j < 4; ++j)
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-          for (int k = 0; k < 2; ++k)
-            o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
-                *reinterpret_cast<const h8*>(row + ((4 * u + 2 * h + k) ^ value_key(r)) * 16), ph[u][k], o[d], 0, 0, 0);
-      }
+        for (int d = 0; d < ND; ++d)
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+              *reinterpret_cast<const h8*>(base + S::kKeys + (32 * d + r) * 128 +
+                                           ((4 * (j >> 1) + 2 * h + (j & 1)) ^ value_key(r)) * 16),
+              ph[j >> 1][j & 1], o[d], 0, 0, 0);
+      reads_ahead<4 * ND>();
     }
     if (more) store(stage ^ 1);
     __syncthreads();
