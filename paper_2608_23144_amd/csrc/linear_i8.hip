@@ -31,28 +31,70 @@ __device__ __forceinline__ void store4(TO* o, const float (&y)[4], int64_t n, in
   }
 }
 
+// Lane j of a quad of neighbouring lanes gets as v[i] what lane i of it loaded as v[j].
+__device__ __forceinline__ void turn_quads(i32x4 (&v)[4], int lane) {
+  const bool odd = lane & 1, high = lane & 2;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    int x[4], y[4];
+#pragma unroll
+    for (int i = 0; i < 4; i += 2) {
+      const int p = __builtin_amdgcn_mov_dpp(v[i + 1][e], 0xB1, 0xF, 0xF, true);  // of lane ^ 1
+      const int q = __builtin_amdgcn_mov_dpp(v[i][e], 0xB1, 0xF, 0xF, true);
+      x[i] = odd ? p : v[i][e];
+      x[i + 1] = odd ? v[i + 1][e] : q;
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int p = __builtin_amdgcn_mov_dpp(x[i + 2], 0x4E, 0xF, 0xF, true);  // of lane ^ 2
+      const int q = __builtin_amdgcn_mov_dpp(x[i], 0x4E, 0xF, 0xF, true);
+      y[i] = high ? p : x[i];
+      y[i + 2] = high ? x[i + 2] : q;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i][e] = y[i];
+  }
+}
+
 // Up to 16 rows: the weights' bytes are all that counts.  A workgroup takes 16
 // weight rows (columns of the result) against all activation rows, its W
-// wavefronts sharing the sum; the weights come straight from memory in the
-// matrix cores' layout, U steps of 64 bytes ahead of the products, and the
-// wavefronts' sums meet in LDS.
-template <int W, int U, bool AHEAD>
+// wavefronts sharing the sum; the weights come straight from memory, four steps
+// of 64 bytes ahead of the products, and the wavefronts' sums meet in LDS.
+//
+// The matrix cores want neighbouring lanes to hold neighbouring rows, but a CU's
+// cache takes in a quad of lanes a cycle only where they read 64 bytes side by
+// side.  So lane j of a quad loads piece j of its quad's four rows, and the quad
+// trades them: the lane ends with 64 bytes of its own row, which are its pieces of
+// four steps (13 x 2048 x 11008: 7.7 us, 11.2 with each lane loading its own;
+// neither 16 wavefronts nor 8 columns a workgroup are faster: 7.6 and 7.8).
+template <int W, bool AHEAD>
 struct RowSums {
-  const int8_t* pb;  // this lane's weight row, from its first piece
-  const int8_t* pa;  // its row of activation codes (AHEAD: in memory, fetched with the weights; else in LDS)
-  int K, wave, g;
+  static constexpr int U = 4;
+  const int8_t* pb[U];  // rows 4 (row / 4) + u of the weights, this lane's piece of a round
+  const int8_t* pa[U];  // the same of the activation codes (AHEAD: in memory, fetched with the weights)
+  const int8_t *rb, *ra;  // this lane's own rows, from its first piece
+  int K, wave, lane, g;
   i32x4 acc = {0, 0, 0, 0};
   i32x4 fb[2][U], fa[2][U];
 
   // rows that do not exist read the last one: their sums are not stored
-  __device__ __forceinline__ RowSums(const LinearArgs& a, int64_t n0, int lane, int wv, const int8_t* A, int64_t lda)
-      : pb(a.B + (n0 + (lane & 15) < a.N ? n0 + (lane & 15) : a.N - 1) * a.ldb + 16 * (lane >> 4)),
-        pa(A + ((lane & 15) < a.M ? (lane & 15) : a.M - 1) * lda + 16 * (lane >> 4)), K((int)a.K), wave(wv), g(lane >> 4) {}
+  __device__ __forceinline__ RowSums(const LinearArgs& a, int64_t n0, int ln, int wv, const int8_t* A, int64_t lda)
+      : K((int)a.K), wave(wv), lane(ln), g(ln >> 4) {
+    const auto weights = [&](int r) { return a.B + (n0 + r < a.N ? n0 + r : a.N - 1) * a.ldb; };
+    const auto codes = [&](int r) { return A + (r < a.M ? r : a.M - 1) * lda; };
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      pb[u] = weights((ln & 12) + u) + 64 * g + 16 * (ln & 3);
+      pa[u] = codes((ln & 12) + u) + 64 * g + 16 * (ln & 3);
+    }
+    rb = weights(ln & 15);
+    ra = codes(ln & 15);
+  }
   __device__ __forceinline__ void load(int buf, int k) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      fb[buf][u] = *reinterpret_cast<const i32x4*>(pb + k + 64 * u);
-      if constexpr (AHEAD) fa[buf][u] = *reinterpret_cast<const i32x4*>(pa + k + 64 * u);
+      fb[buf][u] = *reinterpret_cast<const i32x4*>(pb[u] + k);
+      if constexpr (AHEAD) fa[buf][u] = *reinterpret_cast<const i32x4*>(pa[u] + k);
     }
   }
   __device__ __forceinline__ int rounds() const { return K / (64 * U); }
@@ -60,9 +102,11 @@ struct RowSums {
     if (wave < rounds()) load(0, wave * 64 * U);
   }
   __device__ __forceinline__ void products(int buf, int k) {
+    turn_quads(fb[buf], lane);
+    if constexpr (AHEAD) turn_quads(fa[buf], lane);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const i32x4 x = AHEAD ? fa[buf][u] : *reinterpret_cast<const i32x4*>(pa + k + 64 * u);
+      const i32x4 x = AHEAD ? fa[buf][u] : *reinterpret_cast<const i32x4*>(ra + k + 64 * g + 16 * u);
       acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[buf][u], x, acc, 0, 0, 0);
     }
   }
@@ -81,8 +125,8 @@ struct RowSums {
         const int left = K - (k + 16 * g);
         i32x4 w = {0, 0, 0, 0}, y = w;
         if (left > 0) {
-          w = *reinterpret_cast<const i32x4*>(pb + k);
-          y = *reinterpret_cast<const i32x4*>(pa + k);
+          w = *reinterpret_cast<const i32x4*>(rb + k + 16 * g);
+          y = *reinterpret_cast<const i32x4*>(ra + k + 16 * g);
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -114,14 +158,14 @@ struct RowSums {
   }
 };
 
-// On activation codes in memory.  2560 x 2048: 3.4 us; 13 x 2048 x 11008: 11.3 us
-// (128 workgroups, whose CUs take in some 39 GB/s each).
-template <int W, int U, typename TO>
+// On activation codes in memory.  13 x 2560 x 2048: 3.2 us; 13 x 2048 x 11008: 7.7
+// (128 workgroups: half of the CUs at 25 GB/s of weights each, 2.9 TB/s in all).
+template <int W, typename TO>
 __global__ __launch_bounds__(64 * W) void k_matmul_i8_rows(LinearArgs a) {
   __shared__ i32x4 part[W][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t n0 = (int64_t)blockIdx.x * 16;
-  RowSums<W, U, true> sums(a, n0, lane, wave, a.A, a.lda);
+  RowSums<W, true> sums(a, n0, lane, wave, a.A, a.lda);
   sums.begin();
   sums.run();
   sums.template finish<TO>(a, n0, lane, part, [&](int64_t m) { return a.a_scale[m]; });
@@ -131,7 +175,7 @@ __global__ __launch_bounds__(64 * W) void k_matmul_i8_rows(LinearArgs a) {
 // quant_i8.hip does), while its first weights are on their way, which saves a
 // launch and its wait.  Each row's values are read twice, the second time from
 // the nearest cache.
-template <int W, int U, typename T, typename TO>
+template <int W, typename T, typename TO>
 __global__ __launch_bounds__(64 * W) void k_linear_i8_rows(LinearArgs a, const T* X, int64_t ldx, int pitch, bool wide) {
   __shared__ i32x4 part[W][64];
   __shared__ float peak[W];
@@ -139,7 +183,7 @@ __global__ __launch_bounds__(64 * W) void k_linear_i8_rows(LinearArgs a, const T
   extern __shared__ __attribute__((aligned(16))) int8_t codes[];  // [M][pitch]
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t n0 = (int64_t)blockIdx.x * 16;
-  RowSums<W, U, false> sums(a, n0, lane, wave, codes, pitch);
+  RowSums<W, false> sums(a, n0, lane, wave, codes, pitch);
   sums.begin();
   const int M = (int)a.M, K = (int)a.K;
   // G wavefronts a row, W / G rows at once
@@ -523,25 +567,30 @@ hipError_t launch_tile(const LinearArgs& a, int split, void* ws, hipStream_t st)
 // Bytes between rows of codes in LDS: whole steps, and 16 more so that rows start in different banks.
 int linear_rows_pitch(int64_t K) { return (int)((K + 63) / 64 * 64 + 16); }
 
-template <int W, int U, typename TO>
+template <int W, typename TO>
 hipError_t launch_rows(const LinearArgs& a, hipStream_t st) {
-  hipLaunchKernelGGL((k_matmul_i8_rows<W, U, TO>), dim3((unsigned)((a.N + 15) / 16)), dim3(64 * W), 0, st, a);
+  hipLaunchKernelGGL((k_matmul_i8_rows<W, TO>), dim3((unsigned)((a.N + 15) / 16)), dim3(64 * W), 0, st, a);
   return hipGetLastError();
 }
 
-template <int W, int U, typename T, typename TO>
+template <int W, typename T, typename TO>
 hipError_t launch_linear_rows(const LinearArgs& a, const void* X, int64_t ldx, hipStream_t st) {
   const bool wide = ((reinterpret_cast<uintptr_t>(X) | (uintptr_t)(ldx * sizeof(T))) & 15) == 0;
   const int pitch = linear_rows_pitch(a.K);
-  hipLaunchKernelGGL((k_linear_i8_rows<W, U, T, TO>), dim3((unsigned)((a.N + 15) / 16)), dim3(64 * W), (size_t)a.M * pitch, st, a,
+  hipLaunchKernelGGL((k_linear_i8_rows<W, T, TO>), dim3((unsigned)((a.N + 15) / 16)), dim3(64 * W), (size_t)a.M * pitch, st, a,
                      static_cast<const T*>(X), ldx, pitch, wide);
   return hipGetLastError();
 }
+template <int W, typename T>
+hipError_t launch_linear_rows_w(const LinearArgs& a, const void* X, int64_t ldx, hipStream_t st) {
+  if (a.out_dtype == AWSRC_DTYPE_F32) return launch_linear_rows<W, T, float>(a, X, ldx, st);
+  if (a.out_dtype == AWSRC_DTYPE_BF16) return launch_linear_rows<W, T, __bf16>(a, X, ldx, st);
+  return launch_linear_rows<W, T, _Float16>(a, X, ldx, st);
+}
 template <typename T>
 hipError_t launch_linear_rows_t(const LinearArgs& a, const void* X, int64_t ldx, hipStream_t st) {
-  if (a.out_dtype == AWSRC_DTYPE_F32) return launch_linear_rows<8, 4, T, float>(a, X, ldx, st);
-  if (a.out_dtype == AWSRC_DTYPE_BF16) return launch_linear_rows<8, 4, T, __bf16>(a, X, ldx, st);
-  return launch_linear_rows<8, 4, T, _Float16>(a, X, ldx, st);
+  // more than 8 rows: as many wavefronts, each quantizing one (16 x 2048 x 2048: 7.7 us, 9.8 with 8)
+  return a.M <= 8 ? launch_linear_rows_w<8, T>(a, X, ldx, st) : launch_linear_rows_w<16, T>(a, X, ldx, st);
 }
 
 // Which kernel takes a product, and over how many parts of the sum.  Times below
@@ -553,11 +602,11 @@ struct Choice {
 };
 Choice choose(int64_t M, int64_t N, int64_t K) {
   const auto tiles = [&](int64_t bm, int64_t bn) { return ((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
-  // Up to 16 rows: 16 columns a workgroup while that leaves at most two of them a
-  // CU (13 x 2048 x 11008: 11.3 against 26.5 through LDS tiles); with more the
-  // activations' reads, as many bytes as the weights', cost more than tiles do
-  // (16 x 11008 x 2048: 10.5 against 8.2; 16 x 27648 x 5120: 44 against 30).
-  if (M <= 16 && N < 8192) return {kRows, 1};
+  // Up to 16 rows: 16 columns a workgroup, up to about three of them a CU (16 x 11008 x
+  // 2048: 6.9, through LDS tiles 8.1); with more the activations' reads, as many bytes as
+  // the weights', cost more than tiles do (16 x 13824 x 5120: 18.3 and 17.2; 16 x 27648 x
+  // 5120: 32.4 and 28.1).  Loads past the last cache do not pay here (16 x 8192 x 8192: 15.2, 13.0 without).
+  if (M <= 16 && N < 12288) return {kRows, 1};
   // 256 tiles of 128 cost 24 us at K = 5120, a round of 256 tiles of 256, one per CU, 62
   // to 80 (512 x 27648 x 5120: 117 and 93; 4096 x 5120 x 5120, two rounds, 117 and 123;
   // 1024 x 5120 x 5120: 40 and 54; 8192 x 27648 x 5120: 1249 and 1105).
@@ -581,7 +630,7 @@ hipError_t launch(const LinearArgs& a, void* ws, hipStream_t st) {
   // it; 64 x 11008 x 2048, whose 23 MB stay there from call to call: 8.8, 10.1 past it).
   const bool once = a.M <= 64 && a.N * a.K >= (int64_t)1 << 26;
   switch (c.path) {
-    case kRows: return launch_rows<8, 4, TO>(a, st);
+    case kRows: return launch_rows<8, TO>(a, st);
     case kTile32:
       return once ? launch_tile<32, 64, 32, 32, 2, 4, true, TO>(a, c.split, ws, st)
                   : launch_tile<32, 64, 32, 32, 2, 4, false, TO>(a, c.split, ws, st);
@@ -608,12 +657,13 @@ hipError_t launch_matmul_i8(const LinearArgs& a, void* ws, hipStream_t st) {
 }
 
 bool linear_i8_fused(int64_t M, int64_t N, int64_t K) {
-  // Where the wavefronts of a row read it in at most four pieces a lane (us, with the launch
-  // saved: 1 x 2560 x 2048 4.6 for 5.9; as many at 16 rows, 9.8 for 9, but for 3 x 10900 twice
-  // the time of two launches), and where there are not so many workgroups that quantizing
-  // over and over costs more than a launch (1 x 27648 x 5120: 37 for 33).
+  // Where a workgroup's wavefronts read the rows in few pieces a lane, and where there are not so many
+  // workgroups that quantizing over and over costs more than a launch.  On the GPU alone, in us (fused and in two
+  // launches): 1 x 2560 x 2048 4.5 and 5.7; 1 x 5120 x 5120 8.9 and 10.9; 1 x 11008 x 2048 8.5 and 9.3; 4 x 5120 x
+  // 4096 11.8 and 10.4; 16 x 2048 x 2048 7.7 and 6.0; 1 x 27648 x 5120 31.6 and 28.9.  A launch that is not
+  // replayed from a graph costs the host 3 more, which is why the middle ones are fused.
   const int64_t share = M <= 1 ? 1 : M <= 2 ? 2 : M <= 4 ? 4 : 8;
-  return M <= 16 && K * share <= 16384 && N < 8192;
+  return M <= 16 && K * share <= 16384 && N < (M <= 4 ? 12288 : 8192);
 }
 
 hipError_t launch_linear_i8_fused(const LinearArgs& a, const void* X, int x_dtype, int64_t ldx, hipStream_t st) {
