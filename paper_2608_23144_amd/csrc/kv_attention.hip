@@ -442,7 +442,9 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void k_kv_attention_tiles
   // the last rows see the most tokens: they start first
   const int qt = plan.tiles_q - 1 - b % plan.tiles_q;
   b /= plan.tiles_q;
-  const int split = b % plan.n_split, s = b / plan.n_split;
+  // every sequence's first part before any second: the short last parts start late (seven pieces of 601 tokens of a
+  // 3B layer: 177 us sequence by sequence, 171)
+  const int s = b % (int)a.n_seq, split = b / (int)a.n_seq;
   Rows rows;
   if (!rows.set(a, s, head)) return;
   const int R0 = qt * BR, n_rows = rows.total() - R0;
