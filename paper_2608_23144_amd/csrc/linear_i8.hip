@@ -369,46 +369,71 @@ __global__ __launch_bounds__((TileShape<BM, BN, WM, WN>::kThreads), OCC) void k_
   };
 
   // fills past the last step come from beyond the resources: they keep the counts and read nothing
-  i32x4 fa[2][TM], fb[2][TN];
 #pragma unroll
   for (int t = 0; t < NS; ++t) fill(t, t);
   arrived(std::integral_constant<int, NS - 1>{}, 0, 0);
-  frags(0, 0, fa[0], fb[0]);
-  // the order of a phase: the fragment reads, and in the last phase the fills after them, between the products that
-  // hide them (left alone the compiler waits for reads right after it issues them)
-  const auto order = [&](auto fills) {
-    constexpr bool kFills = decltype(fills)::value;
-    constexpr int n_mfma = TM * TN, n_read = TM + TN, n_fill = kFills ? NA + NB : 0;
-    constexpr int per = kFills || n_mfma < 2 * n_read ? 1 : n_mfma / n_read;
+  int st = 0;
+  if constexpr (TM * TN == 1) {
+    // One product for two fragments: a whole step's are read during the products of the step before (read 32 bytes
+    // ahead, as below, each product waits for LDS: 100 x 5120 x 5120 15.4 us, 13.9; tiles of more products gain nothing).
+    i32x4 fa[2][4][TM], fb[2][4][TN];
+    const auto read = [&](int stage, int b) {
 #pragma unroll
-    for (int i = 0; i < n_read; ++i) {
-      __builtin_amdgcn_sched_group_barrier(0x008, per, 0);  // MFMA
-      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);    // LDS read
-    }
-    if constexpr (kFills) {
-      constexpr int left = n_mfma - n_read > 0 ? n_mfma - n_read : 1;
+      for (int ks = 0; ks < 4; ++ks) frags(stage, ks, fa[b][ks], fb[b][ks]);
+    };
+    read(0, 0);
+    for (int t0 = 0; t0 < steps; t0 += 2) {
 #pragma unroll
-      for (int i = 0; i < left; ++i) {
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x020, (n_fill + left - 1) / left, 0);  // memory read
+      for (int b = 0; b < 2; ++b) {
+        const int t = t0 + b;
+        if (t >= steps) break;
+        const int next = st + 1 == NS ? 0 : st + 1;
+        arrived(std::integral_constant<int, NS - 2>{}, next, t + 1);
+        fill(st, t + NS);
+        read(next, b ^ 1);
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) products(fa[b][ks], fb[b][ks]);
+        st = next;
       }
     }
-  };
-  int st = 0;
-  for (int t = 0; t < steps; ++t) {
+  } else {
+    i32x4 fa[2][TM], fb[2][TN];
+    frags(0, 0, fa[0], fb[0]);
+    // the order of a phase: the fragment reads, and in the last phase the fills after them, between the products that
+    // hide them (left alone the compiler waits for reads right after it issues them)
+    const auto order = [&](auto fills) {
+      constexpr bool kFills = decltype(fills)::value;
+      constexpr int n_mfma = TM * TN, n_read = TM + TN, n_fill = kFills ? NA + NB : 0;
+      constexpr int per = kFills || n_mfma < 2 * n_read ? 1 : n_mfma / n_read;
 #pragma unroll
-    for (int ks = 0; ks < 3; ++ks) {
-      frags(st, ks + 1, fa[(ks + 1) & 1], fb[(ks + 1) & 1]);
-      products(fa[ks & 1], fb[ks & 1]);
-      order(std::false_type{});
+      for (int i = 0; i < n_read; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, per, 0);  // MFMA
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);    // LDS read
+      }
+      if constexpr (kFills) {
+        constexpr int left = n_mfma - n_read > 0 ? n_mfma - n_read : 1;
+#pragma unroll
+        for (int i = 0; i < left; ++i) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(0x020, (n_fill + left - 1) / left, 0);  // memory read
+        }
+      }
+    };
+    for (int t = 0; t < steps; ++t) {
+#pragma unroll
+      for (int ks = 0; ks < 3; ++ks) {
+        frags(st, ks + 1, fa[(ks + 1) & 1], fb[(ks + 1) & 1]);
+        products(fa[ks & 1], fb[ks & 1]);
+        order(std::false_type{});
+      }
+      const int next = st + 1 == NS ? 0 : st + 1;
+      arrived(std::integral_constant<int, NS - 2>{}, next, t + 1);
+      fill(st, t + NS);
+      frags(next, 0, fa[0], fb[0]);
+      products(fa[1], fb[1]);
+      order(std::true_type{});
+      st = next;
     }
-    const int next = st + 1 == NS ? 0 : st + 1;
-    arrived(std::integral_constant<int, NS - 2>{}, next, t + 1);
-    fill(st, t + NS);
-    frags(next, 0, fa[0], fb[0]);
-    products(fa[1], fb[1]);
-    order(std::true_type{});
-    st = next;
   }
   __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): no fill outlives the workgroup
 
@@ -612,11 +637,11 @@ Choice choose(int64_t M, int64_t N, int64_t K) {
   // 1024 x 5120 x 5120: 40 and 54; 8192 x 27648 x 5120: 1249 and 1105).
   const int64_t t128 = tiles(128, 128), t256 = tiles(256, 256);
   if (M > 64 && t128 >= 256) return {2.9 * ((t256 + 255) / 256) < t128 / 256.0 + 0.5 ? kTile256 : kTile128, 1};
-  // 64 x 27648 x 5120: 64 x 64 tiles 42.0, 64 x 128 tiles 35.1 (64 x 11008 x 2048: 8.8 and 10.5)
+  // 64 x 27648 x 5120: 64 x 64 tiles 42.0, 64 x 128 tiles 35.1 (64 x 11008 x 2048: 7.8 and 10.5)
   if (M > 32 && tiles(64, 128) >= 192) return {kTile64Wide, 1};
   const Path path = M > 32 ? kTile64 : kTile32;
   // Few tiles under a long sum: parts of at least 16 steps, joined by a second
-  // launch (64 x 2048 x 11008: 28 whole, 14.3 in 5 parts; 64 x 2560 x 2048: 7.8 whole, 8.9 in 4)
+  // launch (64 x 2048 x 11008: 28 whole, 13.4 in 5 parts; 64 x 2560 x 2048: 6.7 whole, 8.9 in 4)
   const int64_t t = path == kTile64 ? tiles(64, 64) : tiles(32, 64);
   const int64_t want = (256 + t - 1) / t, most = (K + kStep - 1) / kStep / 16;
   const int64_t split = want < most ? want : most;
@@ -634,7 +659,7 @@ hipError_t launch(const LinearArgs& a, void* ws, hipStream_t st) {
     case kTile32:
       return once ? launch_tile<32, 64, 32, 32, 2, 4, true, TO>(a, c.split, ws, st)
                   : launch_tile<32, 64, 32, 32, 2, 4, false, TO>(a, c.split, ws, st);
-    case kTile64: return launch_tile<64, 64, 32, 32, 3, 3, false, TO>(a, c.split, ws, st);
+    case kTile64: return launch_tile<64, 64, 32, 32, 2, 4, false, TO>(a, c.split, ws, st);
     case kTile64Wide:
       return once ? launch_tile<64, 128, 32, 64, 2, 3, true, TO>(a, 1, ws, st)
                   : launch_tile<64, 128, 32, 64, 2, 3, false, TO>(a, 1, ws, st);
