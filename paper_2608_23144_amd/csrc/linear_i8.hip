@@ -56,7 +56,7 @@ __device__ __forceinline__ void turn_quads(i32x4 (&v)[4], int lane) {
   }
 }
 
-// Up to 16 rows: the weights' bytes are all that counts.  A workgroup takes 16
+// Up to 16 rows (or 32: R groups of 16): the weights' bytes are all that counts.  A workgroup takes 16
 // weight rows (columns of the result) against all activation rows, its W
 // wavefronts sharing the sum; the weights come straight from memory, four steps
 // of 64 bytes ahead of the products, and the wavefronts' sums meet in LDS.
@@ -67,15 +67,15 @@ __device__ __forceinline__ void turn_quads(i32x4 (&v)[4], int lane) {
 // trades them: the lane ends with 64 bytes of its own row, which are its pieces of
 // four steps (13 x 2048 x 11008: 7.7 us, 11.2 with each lane loading its own;
 // neither 16 wavefronts nor 8 columns a workgroup are faster: 7.6 and 7.8).
-template <int W, bool AHEAD>
+template <int W, int R, bool AHEAD>
 struct RowSums {
   static constexpr int U = 4;
   const int8_t* pb[U];  // rows 4 (row / 4) + u of the weights, this lane's piece of a round
-  const int8_t* pa[U];  // the same of the activation codes (AHEAD: in memory, fetched with the weights)
-  const int8_t *rb, *ra;  // this lane's own rows, from its first piece
+  const int8_t* pa[R][U];  // the same of R groups of 16 rows of activation codes (AHEAD: in memory, fetched with the weights)
+  const int8_t *rb, *ra[R];  // this lane's own rows
   int K, wave, lane, g;
-  i32x4 acc = {0, 0, 0, 0};
-  i32x4 fb[2][U], fa[2][U];
+  i32x4 acc[R];
+  i32x4 fb[2][U], fa[2][R][U];
 
   // rows that do not exist read the last one: their sums are not stored
   __device__ __forceinline__ RowSums(const LinearArgs& a, int64_t n0, int ln, int wv, const int8_t* A, int64_t lda)
@@ -85,16 +85,23 @@ struct RowSums {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       pb[u] = weights((ln & 12) + u) + 64 * g + 16 * (ln & 3);
-      pa[u] = codes((ln & 12) + u) + 64 * g + 16 * (ln & 3);
+#pragma unroll
+      for (int j = 0; j < R; ++j) pa[j][u] = codes(16 * j + (ln & 12) + u) + 64 * g + 16 * (ln & 3);
     }
     rb = weights(ln & 15);
-    ra = codes(ln & 15);
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+      ra[j] = codes(16 * j + (ln & 15));
+      acc[j] = i32x4{0, 0, 0, 0};
+    }
   }
   __device__ __forceinline__ void load(int buf, int k) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       fb[buf][u] = *reinterpret_cast<const i32x4*>(pb[u] + k);
-      if constexpr (AHEAD) fa[buf][u] = *reinterpret_cast<const i32x4*>(pa[u] + k);
+      if constexpr (AHEAD)
+#pragma unroll
+        for (int j = 0; j < R; ++j) fa[buf][j][u] = *reinterpret_cast<const i32x4*>(pa[j][u] + k);
     }
   }
   __device__ __forceinline__ int rounds() const { return K / (64 * U); }
@@ -103,11 +110,14 @@ struct RowSums {
   }
   __device__ __forceinline__ void products(int buf, int k) {
     turn_quads(fb[buf], lane);
-    if constexpr (AHEAD) turn_quads(fa[buf], lane);
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const i32x4 x = AHEAD ? fa[buf][u] : *reinterpret_cast<const i32x4*>(ra + k + 64 * g + 16 * u);
-      acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[buf][u], x, acc, 0, 0, 0);
+    for (int j = 0; j < R; ++j) {
+      if constexpr (AHEAD) turn_quads(fa[buf][j], lane);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const i32x4 x = AHEAD ? fa[buf][j][u] : *reinterpret_cast<const i32x4*>(ra[j] + k + 64 * g + 16 * u);
+        acc[j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[buf][u], x, acc[j], 0, 0, 0);
+      }
     }
   }
   __device__ __forceinline__ void run() {
@@ -123,35 +133,41 @@ struct RowSums {
     if (wave == W - 1) {  // the rest of the sum, zeros past K on the weights' side
       for (int k = n * 64 * U; k < K; k += 64) {
         const int left = K - (k + 16 * g);
-        i32x4 w = {0, 0, 0, 0}, y = w;
+        i32x4 w = {0, 0, 0, 0}, y[R];
+#pragma unroll
+        for (int j = 0; j < R; ++j) y[j] = w;
         if (left > 0) {
           w = *reinterpret_cast<const i32x4*>(rb + k + 16 * g);
-          y = *reinterpret_cast<const i32x4*>(ra + k + 16 * g);
+#pragma unroll
+          for (int j = 0; j < R; ++j) y[j] = *reinterpret_cast<const i32x4*>(ra[j] + k + 16 * g);
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int m = left - 4 * e;  // bytes of this word that belong to the sum
           if (m < 4) w[e] = m <= 0 ? 0 : w[e] & (int)((1u << (8 * m)) - 1u);
         }
-        acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(w, y, acc, 0, 0, 0);
+#pragma unroll
+        for (int j = 0; j < R; ++j) acc[j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w, y[j], acc[j], 0, 0, 0);
       }
     }
   }
-  // the wavefronts' sums together and the results out; sa: the scale of activation row `lane & 15`
+  // the wavefronts' sums together and the results out, group j by wavefront j; sa: the scale of an activation row
   template <typename TO, typename SA>
-  __device__ __forceinline__ void finish(const LinearArgs& a, int64_t n0, int lane, i32x4 (*part)[64], const SA& sa) {
-    part[wave][lane] = acc;
-    __syncthreads();
-    const int64_t m = lane & 15, n = n0 + 4 * g;
-    if (wave || m >= a.M) return;
+  __device__ __forceinline__ void finish(const LinearArgs& a, int64_t n0, i32x4 (*part)[R][64], const SA& sa) {
 #pragma unroll
-    for (int w = 1; w < W; ++w) acc += part[w][lane];
+    for (int j = 0; j < R; ++j) part[wave][j][lane] = acc[j];
+    __syncthreads();
+    const int64_t m = 16 * wave + (lane & 15), n = n0 + 4 * g;
+    if (wave >= R || m >= a.M) return;
+    i32x4 sum = part[0][wave][lane];
+#pragma unroll
+    for (int w = 1; w < W; ++w) sum += part[w][wave][lane];
     const float s = sa(m);
     float y[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int64_t nn = n + e < a.N ? n + e : a.N - 1;
-      y[e] = scaled(acc[e], s, a.b_scale[nn], a.bias ? a.bias[nn] : 0.0f);
+      y[e] = scaled(sum[e], s, a.b_scale[nn], a.bias ? a.bias[nn] : 0.0f);
     }
     TO* o = static_cast<TO*>(a.out) + m * a.ldo;
     store4(o, y, n, a.N, ((reinterpret_cast<uintptr_t>(a.out) | (uintptr_t)(a.ldo * sizeof(TO))) & (4 * sizeof(TO) - 1)) == 0);
@@ -160,15 +176,14 @@ struct RowSums {
 
 // On activation codes in memory.  13 x 2560 x 2048: 3.2 us; 13 x 2048 x 11008: 7.7
 // (128 workgroups: half of the CUs at 25 GB/s of weights each, 2.9 TB/s in all).
-template <int W, typename TO>
+template <int W, int R, typename TO>
 __global__ __launch_bounds__(64 * W) void k_matmul_i8_rows(LinearArgs a) {
-  __shared__ i32x4 part[W][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  __shared__ i32x4 part[W][R][64];
   const int64_t n0 = (int64_t)blockIdx.x * 16;
-  RowSums<W, true> sums(a, n0, lane, wave, a.A, a.lda);
+  RowSums<W, R, true> sums(a, n0, threadIdx.x & 63, threadIdx.x >> 6, a.A, a.lda);
   sums.begin();
   sums.run();
-  sums.template finish<TO>(a, n0, lane, part, [&](int64_t m) { return a.a_scale[m]; });
+  sums.template finish<TO>(a, n0, part, [&](int64_t m) { return a.a_scale[m]; });
 }
 
 // On activations: every workgroup quantizes the few rows itself (into LDS, as
@@ -177,13 +192,13 @@ __global__ __launch_bounds__(64 * W) void k_matmul_i8_rows(LinearArgs a) {
 // the nearest cache.
 template <int W, typename T, typename TO>
 __global__ __launch_bounds__(64 * W) void k_linear_i8_rows(LinearArgs a, const T* X, int64_t ldx, int pitch, bool wide) {
-  __shared__ i32x4 part[W][64];
+  __shared__ i32x4 part[W][1][64];
   __shared__ float peak[W];
   __shared__ float scales[16];
   extern __shared__ __attribute__((aligned(16))) int8_t codes[];  // [M][pitch]
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t n0 = (int64_t)blockIdx.x * 16;
-  RowSums<W, false> sums(a, n0, lane, wave, codes, pitch);
+  RowSums<W, 1, false> sums(a, n0, lane, wave, codes, pitch);
   sums.begin();
   const int M = (int)a.M, K = (int)a.K;
   // G wavefronts a row, W / G rows at once
@@ -224,7 +239,7 @@ __global__ __launch_bounds__(64 * W) void k_linear_i8_rows(LinearArgs a, const T
   }
   __syncthreads();
   sums.run();
-  sums.template finish<TO>(a, n0, lane, part, [&](int64_t m) { return scales[m]; });
+  sums.template finish<TO>(a, n0, part, [&](int64_t m) { return scales[m]; });
 }
 
 // Tiles through LDS, for products with enough rows to fill the matrix cores.
@@ -592,9 +607,9 @@ hipError_t launch_tile(const LinearArgs& a, int split, void* ws, hipStream_t st)
 // Bytes between rows of codes in LDS: whole steps, and 16 more so that rows start in different banks.
 int linear_rows_pitch(int64_t K) { return (int)((K + 63) / 64 * 64 + 16); }
 
-template <int W, typename TO>
+template <int W, int R, typename TO>
 hipError_t launch_rows(const LinearArgs& a, hipStream_t st) {
-  hipLaunchKernelGGL((k_matmul_i8_rows<W, TO>), dim3((unsigned)((a.N + 15) / 16)), dim3(64 * W), 0, st, a);
+  hipLaunchKernelGGL((k_matmul_i8_rows<W, R, TO>), dim3((unsigned)((a.N + 15) / 16)), dim3(64 * W), 0, st, a);
   return hipGetLastError();
 }
 
@@ -632,6 +647,10 @@ Choice choose(int64_t M, int64_t N, int64_t K) {
   // the weights', cost more than tiles do (16 x 13824 x 5120: 18.3 and 17.2; 16 x 27648 x
   // 5120: 32.4 and 28.1).  Loads past the last cache do not pay here (16 x 8192 x 8192: 15.2, 13.0 without).
   if (M <= 16 && N < 12288) return {kRows, 1};
+  // Up to 32 rows of them while the sum is not so long that its parts pay (30 x 2560 x 2048: 3.9, tiles 6.6; 32 x 4096 x
+  // 4096: 6.6 and 10.0; 24 x 5120 x 5120: 11.3 and 11.1; 32 x 8192 x 8192: 17.1 and 23.4; 32 x 11008 x 2048: 9.4 and 7.5;
+  // 32 x 4096 x 27648: 33.8 and 26.0).
+  if (M > 16 && M <= 32 && N <= 8192 && K <= 16384) return {kRows, 1};
   // 256 tiles of 128 cost 24 us at K = 5120, a round of 256 tiles of 256, one per CU, 62
   // to 80 (512 x 27648 x 5120: 117 and 93; 4096 x 5120 x 5120, two rounds, 117 and 123;
   // 1024 x 5120 x 5120: 40 and 54; 8192 x 27648 x 5120: 1249 and 1105).
@@ -655,7 +674,7 @@ hipError_t launch(const LinearArgs& a, void* ws, hipStream_t st) {
   // it; 64 x 11008 x 2048, whose 23 MB stay there from call to call: 8.8, 10.1 past it).
   const bool once = a.M <= 64 && a.N * a.K >= (int64_t)1 << 26;
   switch (c.path) {
-    case kRows: return launch_rows<8, TO>(a, st);
+    case kRows: return a.M <= 16 ? launch_rows<8, 1, TO>(a, st) : launch_rows<8, 2, TO>(a, st);
     case kTile32:
       return once ? launch_tile<32, 64, 32, 32, 2, 4, true, TO>(a, c.split, ws, st)
                   : launch_tile<32, 64, 32, 32, 2, 4, false, TO>(a, c.split, ws, st);

@@ -139,6 +139,17 @@ def test_matmul_i8(M, N, K, dtype):
     _check_product(out, a, sa, b, sb, bias, dtype)
 
 
+@pytest.mark.parametrize("M,N,K", [(16, 48, 512), (17, 48, 512), (32, 33, 1100), (33, 48, 512), (20, 8192, 272), (20, 8300, 200),
+                                   (9, 12288, 130), (32, 100, 17000), (27, 100, 16384), (25, 13000, 5300)])
+def test_matmul_i8_where_few_rows_end(M, N, K):
+    """Both sides of the bounds between the kernels of few rows and the tiles."""
+    g = _gen("few", M, N, K)
+    a, b = _codes(g, M, K, fill=7), _codes(g, N, K, fill=-9)
+    sa, sb, bias = torch.rand(M, generator=g).to(DEV), torch.rand(N, generator=g).to(DEV), _randn(g, N).to(DEV)
+    out = awsrc.awsrc_matmul_i8(a, sa, b, sb, bias=bias, out_dtype=torch.bfloat16)
+    _check_product(out, a, sa, b, sb, bias, torch.bfloat16)
+
+
 @pytest.mark.parametrize("M,N,K", [(5, 33, 100), (40, 70, 600), (150, 301, 260), (300, 300, 300)])
 def test_matmul_i8_extremes(M, N, K):
     """Every code at the end of its range: the largest sums, of both signs."""
