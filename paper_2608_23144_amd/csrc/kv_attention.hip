@@ -194,7 +194,8 @@ struct Query {
 // chunk of its tokens, in tiles of 64 tokens over W wavefronts that meet in LDS at
 // the end.  Keys and values go from memory to the matrix cores in 16-byte runs of
 // codes per lane, without LDS: a tile's values and the next tile's keys are in
-// flight while the scores and the softmax are computed.
+// flight while the scores and the softmax are computed.  Bound by the cache's bytes: a ragged batch of 64 sequences of
+// a 32B layer (684 MB) 126 us, 5.4 TB/s; short calls by the latency of a tile's loads.
 //
 // Lane l holds query l % 16.  Row 4 g + i of score tile j is token 16 g + 4 j + i.
 // Q and K agree on an order of the channels in which each lane reads 16
@@ -390,7 +391,10 @@ __device__ __forceinline__ void store_row4(T* out, fl4 y, float l, float f) {
 // wavefront, over tiles of 64 tokens whose codes become fp16 once, on their way
 // into LDS (two stages), and then serve all W wavefronts through 32 x 32 x 16
 // products.  The next tile's codes are on their way from memory while the
-// current one is computed.
+// current one is computed.  Bound by vector and matrix instructions one after the
+// other (8192 tokens of a 3B layer: 318 us, 864 TFLOP/s; of the CUs' busy cycles 57% issue
+// vector instructions and 39% run matrix ones).  Neither wavefront priorities nor
+// making the next tile's scores during this one's exponentials (too many registers) overlapped them.
 //
 // Lane l (half h = l / 32) holds query l % 32.  Row 8 b + 4 h + i of a 32-token score
 // tile is token 16 h + 4 b + i.  Keys lie in LDS as [row][channel], values as
@@ -669,7 +673,7 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void k_kv_attention_tiles
 
 // The sums of a row's splits together, for up to kFewSplit of them: D / 4 lanes a
 // row, every lane with all statistics, so that all loads go out at once and no
-// lane waits for another.
+// lane waits for another.  Bound by the sums' bytes (ragged pieces of prompts: 12 us, near 5 TB/s).
 template <int BR, typename T, int D>
 __global__ __launch_bounds__(256) void k_kv_attention_join_few(AttentionArgs a, Plan plan, const float* parts, int n_items,
                                                                int per_head) {
@@ -714,7 +718,7 @@ __global__ __launch_bounds__(256) void k_kv_attention_join_few(AttentionArgs a, 
 }
 
 // The same for more splits: a workgroup per row weighs them by their maxima
-// first, so that the sums' loads do not wait for one another.
+// first, so that the sums' loads do not wait for one another.  128 splits of 32 rows: 5.9 us, latency.
 template <int BR, typename T, int D>
 __global__ __launch_bounds__(256) void k_kv_attention_join(AttentionArgs a, Plan plan, const float* parts, int per_head) {
   constexpr int LD = D / 4;    // lanes across a row
@@ -789,10 +793,10 @@ Plan plan_of(const AttentionArgs& a) {
   if (most > a.max_kv) most = a.max_kv;
   // Splits, as far as they fill the machine: each costs a join.  Few rows: as many
   // workgroups as reside at once on half of the CUs' registers (D = 128: 2 x 131071 tokens of a
-  // group of 8 take 30.5 us in 512 workgroups, 34 in 1024; the ragged batch of 64 130, 141),
-  // of at least 256 tokens (1501 tokens: 11.0 us, 12.1 with 512).  Many rows: one sequence
-  // 512 workgroups (512 rows after 16000 tokens: 111 us, 128 in 1024), a batch, whose lengths differ,
-  // 4096 (ragged pieces of prompts: 109 us, 178 in 512).
+  // group of 8 take 30.7 us in 512 workgroups, 34.5 in 1024; the ragged batch of 64 133, 144),
+  // of at least 256 tokens (1501 tokens: 10.0 us, 11.4 with 512).  Many rows: one sequence
+  // 512 workgroups (512 rows after 16000 tokens: 116 us, 133 in 1024), a batch, whose lengths differ,
+  // 4096 of at least 1024 tokens (ragged pieces of prompts: 101 us, 171 in 512).
   int64_t target, least;
   if (p.tile == kRowTile) {
     target = a.c.head_dim == 64 ? 768 : a.c.head_dim == 128 ? 512 : 256;
@@ -804,11 +808,18 @@ Plan plan_of(const AttentionArgs& a) {
   int64_t split = p.tile == kTileRows ? target / base : (target + base - 1) / base;
   const int64_t cap = (most + least - 1) / least;
   if (split > cap) split = cap;
+  // Sequences of different lengths leave CUs idle at the end: where they have to be split at all, into twice as many
+  // parts, unless those get short (24 of up to 8192 tokens, 32B layer: 61 us, 71; 40 of 20000, 3B layer: 60 and 76).
+  if (p.tile == kRowTile && a.n_seq > 1 && base < target) {
+    int64_t even = (2 * target + base - 1) / base;
+    if (even > most / (8 * a.c.head_dim)) even = most / (8 * a.c.head_dim);
+    if (split < even) split = even;
+  }
   if (split > kMaxSplit) split = kMaxSplit;
   if (split < 1) split = 1;
   p.waves = 4;
   // A short history and few sequences: eight wavefronts and no split cost less than the second
-  // launch does (1501 tokens: 13.6 us on the GPU and 10.4 on the host, 10.1 and 14.9 split; 2000: 17.3).
+  // launch does (1501 tokens: 13.3 us on the GPU and 10.4 on the host, 10.0 and 14.9 split; 2000: 16.1 and 10.0).
   if (p.tile == kRowTile && split > 1 && most <= 1536 && a.c.head_dim <= 128) {
     p.waves = 8;
     split = 1;
@@ -818,7 +829,7 @@ Plan plan_of(const AttentionArgs& a) {
   p.n_split = (int)((most + p.chunk - 1) / p.chunk);
   if (p.n_split < 1) p.n_split = 1;
   // Rows enough for every CU twice without a split: 256 a workgroup, which halves the work of turning
-  // codes into fp16 (8192 tokens of a 3B layer: 363 us with 128, 333; 1000 tokens each of four
+  // codes into fp16 (8192 tokens of a 3B layer: 368 us with 128, 326; 1000 tokens each of four
   // sequences of a 32B layer, where whole workgroups of the shorter ones idle, 67 and 71).
   if (p.tile == kTileRows && p.n_split == 1 && a.c.head_dim == 128 && rows >= 16384) {
     const int64_t wide = (rows + 2 * kTileRows - 1) / (2 * kTileRows);

@@ -312,6 +312,8 @@ __device__ __forceinline__ Work work_of(int b, int heads) {
 }
 
 // Workgroups [0, n_blocks): keys and values; the rest: queries, a row a wavefront.
+// Bound by bytes where tokens are many (8563 of a 32B layer: 46 us, 5.0 TB/s, a copy's rate), else by the chain of
+// loads page, old scale, codes (a token each of 48 sequences of a 3B layer: 6.9 us).
 template <typename T, int NI>
 __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a, int n_blocks, int per_seq, bool wide_kv, bool wide_q,
                                                    bool whole) {
@@ -419,6 +421,7 @@ __device__ __forceinline__ void read_block(const ReadArgs& a, const Span& sp, in
   }
 }
 
+// Codes times scales, dense.  The same 8563 tokens: 10.5 us, 5.0 TB/s; 48 short ends of pages 4.4 us.
 template <typename T, int NI>
 __global__ __launch_bounds__(256) void k_kv_read(ReadArgs a, int per_seq, bool wide) {
   extern __shared__ __attribute__((aligned(16))) char lds[];

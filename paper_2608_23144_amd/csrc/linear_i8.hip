@@ -189,7 +189,7 @@ __global__ __launch_bounds__(64 * W) void k_matmul_i8_rows(LinearArgs a) {
 // On activations: every workgroup quantizes the few rows itself (into LDS, as
 // quant_i8.hip does), while its first weights are on their way, which saves a
 // launch and its wait.  Each row's values are read twice, the second time from
-// the nearest cache.
+// the nearest cache.  Bound by latency: 1 x 2560 x 2048 4.5 us, of which its 5 MB take 0.8.
 template <int W, typename T, typename TO>
 __global__ __launch_bounds__(64 * W) void k_linear_i8_rows(LinearArgs a, const T* X, int64_t ldx, int pitch, bool wide) {
   __shared__ i32x4 part[W][1][64];
@@ -246,16 +246,19 @@ __global__ __launch_bounds__(64 * W) void k_linear_i8_rows(LinearArgs a, const T
 //
 // A workgroup makes BM rows (m) times BN columns (n) of the result, a
 // wavefront WM x WN of them as 32 x 32 tiles of v_mfma_i32_32x32x32_i8.  The sum
-// advances 128 bytes at a time through two LDS stages filled by direct
+// advances 128 bytes at a time through two to four LDS stages filled by direct
 // global-to-LDS loads, which leave the registers to the sums.  A stage's rows
 // of 128 bytes are 8 pieces of 16; piece p of row r lies at place p ^ key(r).  LDS
 // serves 16 lanes a cycle (64 banks), two rows side by side: over the 16 rows
 // that a fragment read takes together, (row % 2, key) takes 16 values.  (Keys of
-// 8 rows, row % 8, took twice the cycles.)  The fills of step t + 1 and the
+// 8 rows, row % 8, took twice the cycles.)  The fills of the next steps and the
 // fragment reads of the next 32 bytes are issued before the products of the
 // current ones.  Eight wavefronts of 128 x 64 make a 256 x 256 tile (four of
 // 128 x 128 wait at every barrier together: 1.20 against 1.11 ms at 8192 x 27648
-// x 5120, where a library's product of the same matrices into int32 takes 1.11).
+// x 5120; 1.06 with results that leave in whole lines, 2.19 POPS, where a library's
+// product of the same matrices into int32 takes 1.11).  Bound by the matrix cores
+// there, by the weights' bytes with few rows (64 x 27648 x 5120: 33 us, 4.4 TB/s),
+// and by LDS and barriers a step where the tiles do not fill the machine.
 //
 // Rows and pieces past the operands' ends come from beyond the buffer resource
 // and arrive as zeros.  Where K is no multiple of 16 the bytes past it are
@@ -552,7 +555,7 @@ __global__ __launch_bounds__((TileShape<BM, BN, WM, WN>::kThreads), OCC) void k_
   }
 }
 
-// The parts of split sums together, with the epilogue; four columns a thread.
+// The parts of split sums together, with the epilogue; four columns a thread.  A few us of latency: 64 x 2048 in 5 parts, 2.6 MB.
 template <typename TO>
 __global__ __launch_bounds__(256) void k_matmul_i8_join(LinearArgs a, const int32_t* __restrict__ parts, int n_parts) {
   const int64_t quads = (a.N + 3) / 4;
