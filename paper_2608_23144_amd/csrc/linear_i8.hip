@@ -706,11 +706,11 @@ hipError_t launch_matmul_i8(const LinearArgs& a, void* ws, hipStream_t st) {
 bool linear_i8_fused(int64_t M, int64_t N, int64_t K) {
   // Where a workgroup's wavefronts read the rows in few pieces a lane, and where there are not so many
   // workgroups that quantizing over and over costs more than a launch.  On the GPU alone, in us (fused and in two
-  // launches): 1 x 2560 x 2048 4.5 and 5.7; 1 x 5120 x 5120 8.9 and 10.9; 1 x 11008 x 2048 8.5 and 9.3; 4 x 5120 x
-  // 4096 11.8 and 10.4; 16 x 2048 x 2048 7.7 and 6.0; 1 x 27648 x 5120 31.6 and 28.9.  A launch that is not
+  // launches): 1 x 2560 x 2048 4.5 and 5.7; 1 x 5120 x 5120 8.9 and 10.9; 4 x 5120 x 4096 11.8 and 10.4;
+  // 16 x 2048 x 2048 7.7 and 6.0; 4 x 11008 x 2048 10.3 and 10.0; 1 x 27648 x 5120 31.6 and 28.9.  A launch that is not
   // replayed from a graph costs the host 3 more, which is why the middle ones are fused.
   const int64_t share = M <= 1 ? 1 : M <= 2 ? 2 : M <= 4 ? 4 : 8;
-  return M <= 16 && K * share <= 16384 && N < (M <= 4 ? 12288 : 8192);
+  return M <= 16 && K * share <= 16384 && N < 8192;
 }
 
 hipError_t launch_linear_i8_fused(const LinearArgs& a, const void* X, int x_dtype, int64_t ldx, hipStream_t st) {
