@@ -393,8 +393,9 @@ __device__ __forceinline__ void store_row4(T* out, fl4 y, float l, float f) {
 // products.  The next tile's codes are on their way from memory while the
 // current one is computed.  Bound by vector and matrix instructions one after the
 // other (8192 tokens of a 3B layer: 318 us, 864 TFLOP/s; of the CUs' busy cycles 57% issue
-// vector instructions and 39% run matrix ones).  Neither wavefront priorities nor
-// making the next tile's scores during this one's exponentials (too many registers) overlapped them.
+// vector instructions and 39% run matrix ones).  Neither wavefront priorities, nor half
+// of the wavefronts a phase behind the others, nor the next tile's scores during this one's exponentials (too many
+// registers) overlapped them: four SIMDs at their products take LDS's whole rate, 1 KB in 32 cycles each.
 //
 // Lane l (half h = l / 32) holds query l % 32.  Row 8 b + 4 h + i of a 32-token score
 // tile is token 16 h + 4 b + i.  Keys lie in LDS as [row][channel], values as
