@@ -392,7 +392,7 @@ __device__ __forceinline__ void store_row4(T* out, fl4 y, float l, float f) {
 // into LDS (two stages), and then serve all W wavefronts through 32 x 32 x 16
 // products.  The next tile's codes are on their way from memory while the
 // current one is computed.  Bound by vector and matrix instructions one after the
-// other (8192 tokens of a 3B layer: 318 us, 864 TFLOP/s; of the CUs' busy cycles 57% issue
+// other (8192 tokens of a 3B layer: 316 us, 870 TFLOP/s; of the CUs' busy cycles 57% issue
 // vector instructions and 39% run matrix ones).  Neither wavefront priorities, nor half
 // of the wavefronts a phase behind the others, nor the next tile's scores during this one's exponentials (too many
 // registers) overlapped them: four SIMDs at their products take LDS's whole rate, 1 KB in 32 cycles each.
