@@ -69,9 +69,10 @@ constexpr float kLag = 8.0f;
 constexpr float kLift = 6.0f;
 
 __device__ __forceinline__ float finite_or_zero(float m) { return m == -__builtin_inff() ? 0.0f : m; }
-// the factor of (sum p' c) / (sum p) in the output
+// The factor of (sum p' c) / (sum p) in the output.  Where every seen page's value scale is 0, M stays -inf and the
+// sum p' c is 0: so is the factor, which the scores alone could take to infinity (m below -134).
 __device__ __forceinline__ float output_factor(float m, float M) {
-  return __builtin_amdgcn_exp2f(finite_or_zero(M) - kLift - finite_or_zero(m));
+  return M == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(M - kLift - finite_or_zero(m));
 }
 
 // Largest value over a row's lanes: those 16 and 32 apart (four lanes a row) or 32 apart (two).
@@ -705,15 +706,14 @@ __global__ __launch_bounds__(256) void k_kv_attention_join_few(AttentionArgs a, 
     mx = fmaxf(mx, m[i]);
     Mx = fmaxf(Mx, M[i]);
   }
-  mx = finite_or_zero(mx);
-  Mx = finite_or_zero(Mx);
+  const float mu = finite_or_zero(mx), Mu = finite_or_zero(Mx);
   float sum = 0.0f;
   fl4 o = {0, 0, 0, 0};
 #pragma unroll
   for (int i = 0; i < kFewSplit; ++i)
     if (i < n) {
-      sum += l[i] * __builtin_amdgcn_exp2f(m[i] - mx);
-      o += y[i] * __builtin_amdgcn_exp2f(M[i] - Mx);
+      sum += l[i] * __builtin_amdgcn_exp2f(m[i] - mu);
+      o += y[i] * __builtin_amdgcn_exp2f(M[i] - Mu);
     }
   store_row4(static_cast<T*>(a.out) + rows.at(R, a.ldo, D) + d, o, sum, output_factor(mx, Mx));
 }
@@ -758,13 +758,12 @@ __global__ __launch_bounds__(256) void k_kv_attention_join(AttentionArgs a, Plan
     m = fmaxf(m, sh_s[w][0]);
     M = fmaxf(M, sh_s[w][1]);
   }
-  m = finite_or_zero(m);
-  M = finite_or_zero(M);
+  const float mu = finite_or_zero(m), Mu = finite_or_zero(M);
   float l = 0.0f;
   for (int i = t; i < n; i += 256) {
     const float* p = base + i * step + BR * D + row;
-    l += p[2 * BR] * __builtin_amdgcn_exp2f(p[0] - m);
-    sh_w[i] = __builtin_amdgcn_exp2f(p[BR] - M);
+    l += p[2 * BR] * __builtin_amdgcn_exp2f(p[0] - mu);
+    sh_w[i] = __builtin_amdgcn_exp2f(p[BR] - Mu);
   }
 #pragma unroll
   for (int off = 32; off >= 1; off >>= 1) l += __shfl_xor(l, off, 64);

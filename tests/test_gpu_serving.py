@@ -597,6 +597,22 @@ def test_attention_pages_of_very_different_loudness(news):
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("lens,news", [([100], [1]), ([100], [70]), ([1900], [1]), ([9001], [1]), ([3000], [70]), ([9001], [70])])
+def test_attention_zero_values_under_scores_far_below_zero(lens, news, dtype):
+    """Pages of zeros alone give 0 whatever the scores are: whole, and joined from few parts and from many.  The scores
+    reach some thousands below 0, where exp2 of their negative is infinite."""
+    b = Batch(("zeros", lens, news), 4, 2, 64, 16, lens, news, dtype)
+    b.cache[0] = b.cache[0].int().abs().clamp(min=1).to(torch.int8)
+    b.q = -(b.q.abs() + 1) * 4
+    b.cache[1][:], b.cache[3][:] = 0, 0.0
+    assert not _check_attention(b, scale=1.0).any()
+    # one page with values, at the last token's place: rows before it still see zeros alone
+    last = int(b.table[0, (lens[0] - 1) // 16])
+    b.cache[1][last], b.cache[3][last] = 100, 0.01
+    _check_attention(b, scale=1.0)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
 @pytest.mark.parametrize("news", [[1, 1], [40, 70]])
 def test_attention_query_magnitudes(news, dtype):
     """Queries at the ends of their type's range, sharp and flat softmaxes, zero queries."""
