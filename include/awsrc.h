@@ -488,8 +488,10 @@ awsrc_status awsrc_reconstruct_bf16_sdq(const awsrc_decode_plan* plan, int32_t n
 /*
  * Rows as int8 codes with one scale each.
  *  X      [rows, cols] x_dtype, row i at X + i * ldx, ldx >= cols.
- *  codes  row i at codes + i * ldc, ldc >= cols.  Up to the next multiple of 16
- *         the codes of a row are filled with 0 as far as ldc reaches.
+ *  codes  row i at codes + i * ldc, ldc >= cols.  Where rows lie on 16 bytes (codes
+ *         16-byte aligned, ldc a multiple of 16: what the products take) each row
+ *         is filled with 0 up to the next multiple of 16; elsewhere nothing past
+ *         cols is written.
  *  scale  [rows] fp32.
  * cols >= 1.  EINVAL: bad shape or dtype, NULL buffer, X not aligned to its type.
  */

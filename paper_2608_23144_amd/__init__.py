@@ -597,6 +597,15 @@ def _i8_rows(t: torch.Tensor, what: str):
     return rows, cols, ld
 
 
+def _code_rows(t: torch.Tensor) -> int:
+    """The row stride of codes that are written; rows on 16 bytes are filled up to a multiple of 16."""
+    rows, cols, ld = _rows_of(t, "codes")
+    wide = -(-cols // 16) * 16
+    if rows and ld % 16 == 0 and t.data_ptr() % 16 == 0 and t.untyped_storage().nbytes() < t.storage_offset() + (rows - 1) * ld + wide:
+        raise ValueError("codes: the last row must be writable up to a multiple of 16 bytes")
+    return ld
+
+
 def _heads_of(t: torch.Tensor, what: str, heads: Optional[int], dim: int, dtype: torch.dtype):
     """(rows, heads, row stride) of a [rows, heads, dim] tensor whose heads lie side by side."""
     if t.dim() != 3:
@@ -653,7 +662,8 @@ def _batch_of(dev: int, cu, kv_len, page_table):
 
 def awsrc_quantize_rows_i8(x: torch.Tensor, out=None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """int8 codes [rows, cols] and fp32 scales [rows] of a matrix (activations per token, weights per output channel).
-    The codes' rows lie a multiple of 16 bytes apart, as awsrc_matmul_i8 and awsrc_linear_i8 take them."""
+    The codes' rows lie a multiple of 16 bytes apart, as awsrc_matmul_i8 and awsrc_linear_i8 take them.  Codes given in
+    `out` on such rows are filled with 0 up to the next multiple of 16; on others nothing past their columns is written."""
     rows, cols, ld = _rows_of(x, "x")
     dev = _device_of(x)
     if out is None:
@@ -664,7 +674,7 @@ def awsrc_quantize_rows_i8(x: torch.Tensor, out=None, stream=None) -> Tuple[torc
             or not scale.is_contiguous()):
         raise ValueError("out: int8 codes of x's shape and fp32 scales [rows]")
     _check(LIB.awsrc_quantize_rows_i8(x.data_ptr(), _act_code(x.dtype), rows, cols, ld, codes.data_ptr(),
-                                      _rows_of(codes, "codes")[2], scale.data_ptr(), _raw_stream(dev, stream)))
+                                      _code_rows(codes), scale.data_ptr(), _raw_stream(dev, stream)))
     return codes, scale
 
 

@@ -118,8 +118,10 @@ template <typename T>
 hipError_t launch(const void* X, int64_t rows, int64_t cols, int64_t ldx, int8_t* codes, int64_t ldc, float* scale,
                   hipStream_t st) {
   const T* x = static_cast<const T*>(X);
-  int64_t pad = (cols + 15) / 16 * 16;
-  if (pad > ldc) pad = ldc;
+  // Zeros up to the next 16 bytes only where rows lie on 16 bytes, as the products take them: the fill then ends inside the
+  // row's own stride.  Of a column slice that starts anywhere else it would reach into the next columns or the next row.
+  const bool on16 = ((reinterpret_cast<uintptr_t>(codes) | (uintptr_t)ldc) & 15) == 0;
+  const int64_t pad = on16 ? (cols + 15) / 16 * 16 : cols;
   const bool wx = ((reinterpret_cast<uintptr_t>(X) | (uintptr_t)(ldx * sizeof(T))) & 15) == 0;
   const bool wc = ((reinterpret_cast<uintptr_t>(codes) | (uintptr_t)ldc) & 7) == 0;
 #define AWSRC_ROWS(WPR, CH)                                                                                            \

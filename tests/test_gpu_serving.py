@@ -94,6 +94,28 @@ def test_quantize_rows_views(dtype, offset, stride):
     assert (tight[rows * cols:] == 77).all()
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows", [1, 5])
+@pytest.mark.parametrize("cols", [20, 700, 3001, 17000])
+@pytest.mark.parametrize("at,after", [(20, 8), (1, 0), (16, 12), (48, 44), (4, 60)])
+def test_quantize_rows_into_a_column_slice(at, after, cols, rows, dtype):
+    """Codes written to columns inside a wider buffer: the columns before them, the rows around them and, past the zeros
+    that rows on 16 bytes end with, the columns after them stay."""
+    g = _gen("slice", at, after, cols, rows)
+    x = _randn(g, rows, cols).to(dtype)
+    width = at + cols + after
+    buf = torch.full((rows + 2, width), 77, dtype=torch.int8, device=DEV)
+    s = torch.empty(rows, device=DEV)
+    awsrc.awsrc_quantize_rows_i8(x.to(DEV), out=(buf[1:rows + 1, at:at + cols], s))
+    want_c, want_s = R.quantize_rows(R.f32(x))
+    want = np.full((rows + 2, width), 77, np.int8)
+    want[1:rows + 1, at:at + cols] = want_c
+    if at % 16 == 0 and width % 16 == 0:
+        want[1:rows + 1, at + cols:at + -(-cols // 16) * 16] = 0
+    _same_bits(buf.cpu().numpy(), want)
+    _same_bits(s.cpu().numpy(), want_s)
+
+
 # ------------------------------------------------------------------ products
 def _codes(g, rows, cols, lo=-128, fill=0):
     ld = -(-cols // 16) * 16

@@ -180,3 +180,17 @@ def test_python_refuses_host_tensors_and_shapes():
     i = torch.zeros(2, dtype=torch.int32)
     with pytest.raises(ValueError):
         awsrc.awsrc_kv_attention(cache, torch.zeros(1, 2, 64, dtype=torch.bfloat16), i, i[:1], i[None], 1, 1)
+
+
+def test_codes_that_cannot_take_their_fill_are_refused():
+    """Rows on 16 bytes are filled with zeros up to a multiple of 16: the last one has to have the room."""
+    buf = torch.zeros(96, dtype=torch.int8)
+    assert buf.data_ptr() % 16 == 0
+    assert awsrc._code_rows(buf.view(2, 48)[:, 16:36]) == 48
+    assert awsrc._code_rows(buf.view(2, 48)[:, 20:40]) == 48
+    assert awsrc._code_rows(buf[:84].view(2, 42)[:, 1:38]) == 42
+    short = torch.zeros(85, dtype=torch.int8)
+    assert short.data_ptr() % 16 == 0
+    assert awsrc._code_rows(short.as_strided((2, 33), (48, 1), 1)) == 48  # not on 16 bytes: no fill
+    with pytest.raises(ValueError, match="multiple of 16"):
+        awsrc._code_rows(short.as_strided((2, 37), (48, 1)))
