@@ -714,11 +714,17 @@ def linear_i8_workspace_bytes(M: int, N: int, K: int) -> int:
 
 def _sized_workspace(workspace, need: int, like: torch.Tensor, stream):
     """(address, size, the tensor that holds it)"""
-    if need == 0 and workspace is None:
-        return None, 0, None
-    if workspace is None or workspace.numel() < need:
+    if workspace is None:
+        if need == 0:
+            return None, 0, None
+    else:  # a kernel writes to it: its own device's memory, as much as it says
+        if workspace.device != like.device:
+            raise ValueError(f"workspace on {workspace.device}, tensors on {like.device}")
+        if not workspace.is_contiguous():
+            raise ValueError("workspace must be contiguous")
+    if workspace is None or workspace.nbytes < need:
         workspace = _empty((need,), like, torch.uint8, stream)
-    return workspace.data_ptr(), workspace.numel(), workspace
+    return workspace.data_ptr(), workspace.nbytes, workspace
 
 
 def awsrc_matmul_i8(a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor, b_scale: torch.Tensor,

@@ -710,6 +710,22 @@ def test_cache_past_32_bit_offsets():
 
 
 # ------------------------------------------------------------------ together
+def test_host_workspaces_are_refused():
+    """Every call that takes a workspace, at shapes that need one, before any launch."""
+    g = _gen("ws")
+    host = torch.empty(1 << 22, dtype=torch.uint8)
+    x = _randn(g, 40, 4096).to(DEV)
+    w, ws = awsrc.awsrc_quantize_rows_i8(_randn(g, 64, 4096).to(DEV))
+    c, s = awsrc.awsrc_quantize_rows_i8(x)
+    b = Batch(("ws",), 4, 2, 64, 16, [3000], [1], torch.bfloat16)
+    cache, cu, kv_len, table = b.dev()
+    assert awsrc.matmul_i8_workspace_bytes(40, 64, 4096) and awsrc.linear_i8_workspace_bytes(40, 64, 4096)
+    for f in (lambda: awsrc.awsrc_matmul_i8(c, s, w, ws, workspace=host), lambda: awsrc.awsrc_linear_i8(x, w, ws, workspace=host),
+              lambda: awsrc.awsrc_kv_attention(cache, b.q.to(DEV), cu, kv_len, table, 1, 3000, workspace=host)):
+        with pytest.raises(ValueError, match="workspace on cpu"):
+            f()
+
+
 def test_calls_on_another_stream():
     st = torch.cuda.Stream()
     g = _gen("stream")

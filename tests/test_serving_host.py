@@ -194,3 +194,18 @@ def test_codes_that_cannot_take_their_fill_are_refused():
     assert awsrc._code_rows(short.as_strided((2, 33), (48, 1), 1)) == 48  # not on 16 bytes: no fill
     with pytest.raises(ValueError, match="multiple of 16"):
         awsrc._code_rows(short.as_strided((2, 37), (48, 1)))
+
+
+def test_workspaces_a_kernel_cannot_write_are_refused():
+    """Before any size is compared: on another device than the tensors, or claiming more elements than it has."""
+    x = torch.zeros(4)
+    for need in (0, 64, 1 << 20):
+        with pytest.raises(ValueError, match="workspace on meta"):
+            awsrc._sized_workspace(torch.empty(4096, dtype=torch.uint8, device="meta"), need, x, None)
+        with pytest.raises(ValueError, match="contiguous"):
+            awsrc._sized_workspace(torch.zeros(1, dtype=torch.uint8).expand(4096), need, x, None)
+    words = torch.zeros(32, dtype=torch.int32)  # its bytes count
+    at, n, keep = awsrc._sized_workspace(words, 128, x, None)
+    assert keep is words and at == words.data_ptr() and n == 128
+    at, n, keep = awsrc._sized_workspace(words, 129, x, None)
+    assert keep is not words and n >= 129
