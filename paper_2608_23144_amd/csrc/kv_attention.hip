@@ -210,12 +210,13 @@ __global__ __launch_bounds__(64 * W, W == 8 ? 2 : D == 256 ? 1 : 3) void k_kv_at
   __shared__ float sh_o[W][16][D + 4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 15, g = lane >> 4;
-  int b = blockIdx.x;
-  const int qt = b % plan.tiles_q;
-  b /= plan.tiles_q;
-  const int head = b % a.c.kv_heads;
-  b /= a.c.kv_heads;
-  const int split = b % plan.n_split, s = b / plan.n_split;
+  uint32_t b = workgroup<64 * W>();
+  const int qt = b % (uint32_t)plan.tiles_q;
+  b /= (uint32_t)plan.tiles_q;
+  const int head = b % (uint32_t)a.c.kv_heads;
+  b /= (uint32_t)a.c.kv_heads;
+  const int split = b % (uint32_t)plan.n_split, s = b / (uint32_t)plan.n_split;
+  if (s >= a.n_seq) return;
   Rows rows;
   if (!rows.set(a, s, head)) return;
   const int R0 = qt * 16, n_rows = rows.total() - R0;
@@ -442,15 +443,16 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void k_kv_attention_tiles
   S& sh = *reinterpret_cast<S*>(lds + 2 * S::kStage);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r = lane & 31, h = lane >> 5;
-  int b = blockIdx.x;
-  const int head = b % a.c.kv_heads;
-  b /= a.c.kv_heads;
+  uint32_t b = workgroup<64 * W>();
+  const int head = b % (uint32_t)a.c.kv_heads;
+  b /= (uint32_t)a.c.kv_heads;
   // the last rows see the most tokens: they start first
-  const int qt = plan.tiles_q - 1 - b % plan.tiles_q;
-  b /= plan.tiles_q;
+  const int qt = plan.tiles_q - 1 - (int)(b % (uint32_t)plan.tiles_q);
+  b /= (uint32_t)plan.tiles_q;
   // every sequence's first part before any second: the short last parts start late (seven pieces of 601 tokens of a
   // 3B layer: 177 us sequence by sequence, 171)
-  const int s = b % (int)a.n_seq, split = b / (int)a.n_seq;
+  const int s = b % (uint32_t)a.n_seq, split = b / (uint32_t)a.n_seq;
+  if (split >= plan.n_split) return;
   Rows rows;
   if (!rows.set(a, s, head)) return;
   const int R0 = qt * BR, n_rows = rows.total() - R0;
@@ -862,7 +864,7 @@ hipError_t launch_tiles(const AttentionArgs& a, const Plan& p, int64_t grid, flo
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL(k, dim3((unsigned)grid), dim3(64 * W), bytes, st, a, p, parts);
+  hipLaunchKernelGGL(k, grid_of<64 * W>(grid), dim3(64 * W), bytes, st, a, p, parts);
   return hipGetLastError();
 }
 
@@ -874,11 +876,11 @@ hipError_t launch_d(const AttentionArgs& a, float* parts, hipStream_t st) {
   if (p.tile == kRowTile) {
     if constexpr (D <= 128) {
       if (p.waves == 8) {
-        hipLaunchKernelGGL((k_kv_attention_rows<T, D, 8>), dim3((unsigned)grid), dim3(512), 0, st, a, p, parts);
+        hipLaunchKernelGGL((k_kv_attention_rows<T, D, 8>), grid_of<512>(grid), dim3(512), 0, st, a, p, parts);
         return hipGetLastError();
       }
     }
-    hipLaunchKernelGGL((k_kv_attention_rows<T, D, 4>), dim3((unsigned)grid), dim3(256), 0, st, a, p, parts);
+    hipLaunchKernelGGL((k_kv_attention_rows<T, D, 4>), grid_of<256>(grid), dim3(256), 0, st, a, p, parts);
     if (p.n_split > 1) return launch_join<kRowTile, T, D>(a, p, parts, st);
     return hipGetLastError();
   }

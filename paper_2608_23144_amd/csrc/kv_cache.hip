@@ -306,9 +306,9 @@ struct Work {
   int slot, head;
   bool values;
 };
-__device__ __forceinline__ Work work_of(int b, int heads) {
-  const int slot = (b >> 1) / heads;
-  return {slot, (b >> 1) - slot * heads, (bool)(b & 1)};
+__device__ __forceinline__ Work work_of(uint32_t b, int heads) {
+  const int slot = (int)(b >> 1) / heads;
+  return {slot, (int)(b >> 1) - slot * heads, (bool)(b & 1)};
 }
 
 // Workgroups [0, n_blocks): keys and values; the rest: queries, a row a wavefront.
@@ -318,8 +318,8 @@ template <typename T, int NI>
 __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a, int n_blocks, int per_seq, bool wide_kv, bool wide_q,
                                                    bool whole) {
   const Rotary rot{a.cos, a.sin, a.rope_len, a.rot / 2, a.interleaved, whole};
-  int b = (int)blockIdx.x;
-  if (b < n_blocks) {
+  const uint32_t b = workgroup<256>();
+  if (b < (uint32_t)n_blocks) {
     const Work w = work_of(b, a.c.kv_heads);
     const int s = w.slot / per_seq;
     Span sp;
@@ -330,8 +330,8 @@ __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a, int n_blocks, i
     else append_block<T, NI, false>(a, sp, w.head, rot, wide_kv);
     return;
   }
-  const int64_t row = (int64_t)(b - n_blocks) * 4 + (threadIdx.x >> 6);
-  if (row >= a.n_rows) return;
+  const int64_t row = ((int64_t)b - n_blocks) * 4 + (threadIdx.x >> 6);
+  if (!a.q || row >= a.n_rows) return;
   const int s = find_seq(a.cu, a.n_seq, row);
   if (s < 0) return;
   const int64_t pos = (int64_t)a.kv_len[s] - (a.cu[s + 1] - row);
@@ -425,8 +425,9 @@ __device__ __forceinline__ void read_block(const ReadArgs& a, const Span& sp, in
 template <typename T, int NI>
 __global__ __launch_bounds__(256) void k_kv_read(ReadArgs a, int per_seq, bool wide) {
   extern __shared__ __attribute__((aligned(16))) char lds[];
-  const Work w = work_of((int)blockIdx.x, a.c.kv_heads);
+  const Work w = work_of(workgroup<256>(), a.c.kv_heads);
   const int s = w.slot / per_seq;
+  if (s >= a.n_seq) return;
   Span sp;
   if (!span_of(a.cu, a.kv_len, a.table, a.table_ld, a.c.n_pages, a.n_rows, a.c.page_tokens, s, w.slot - s * per_seq, &sp))
     return;
@@ -444,13 +445,13 @@ hipError_t launch_append(const AppendArgs& a, int64_t grid, int64_t n_blocks, in
   const bool kv = on16(a.k, a.ldk, sizeof(T)) && on16(a.v, a.ldv, sizeof(T));
   const bool q = on16(a.q, a.ldq, sizeof(T)) && on16(a.q_out, a.ldqo, sizeof(T));
   const bool whole = kv && (!a.q || q) && a.rot == a.c.head_dim && !a.interleaved && on16(a.cos, 0, 0) && on16(a.sin, 0, 0) && a.rope_len > 0;
-  hipLaunchKernelGGL((k_kv_append<T, NI>), dim3((unsigned)grid), dim3(256), 0, st, a, (int)n_blocks, (int)per_seq, kv, q, whole);
+  hipLaunchKernelGGL((k_kv_append<T, NI>), grid_of<256>(grid), dim3(256), 0, st, a, (int)n_blocks, (int)per_seq, kv, q, whole);
   return hipGetLastError();
 }
 template <typename T, int NI>
 hipError_t launch_read(const ReadArgs& a, int64_t grid, int64_t per_seq, hipStream_t st) {
   const bool wide = on16(a.k_out, 0, 0) && on16(a.v_out, 0, 0);  // rows are a multiple of 128 bytes apart
-  hipLaunchKernelGGL((k_kv_read<T, NI>), dim3((unsigned)grid), dim3(256), (size_t)a.c.head_dim * (a.c.page_tokens + 4), st, a,
+  hipLaunchKernelGGL((k_kv_read<T, NI>), grid_of<256>(grid), dim3(256), (size_t)a.c.head_dim * (a.c.page_tokens + 4), st, a,
                      (int)per_seq, wide);
   return hipGetLastError();
 }

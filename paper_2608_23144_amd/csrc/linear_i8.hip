@@ -594,7 +594,7 @@ hipError_t launch_tile(const LinearArgs& a, int split, void* ws, hipStream_t st)
     if (e != hipSuccess) return e;
   }
   const int64_t tm = (a.M + BM - 1) / BM, tn = (a.N + BN - 1) / BN;
-  if (tm * tn > 0x7FFFFFFF / 8) return hipErrorInvalidValue;
+  if (tm * tn > 0x7FFFFFFF / S::kThreads) return hipErrorInvalidValue;  // (threads of a launch: more than memory holds results for)
   const int all = (int)((a.K + kStep - 1) / kStep), per = (all + split - 1) / split;
   split = (all + per - 1) / per;
   int32_t* parts = split > 1 ? static_cast<int32_t*>(ws) : nullptr;

@@ -29,7 +29,8 @@ __global__ __launch_bounds__(64 * (WPR == 1 ? 4 : WPR)) void k_quantize_rows(con
                                                                              bool wide_x, bool wide_c) {
   __shared__ float part[WPR];
   const int wave = threadIdx.x >> 6;
-  const int64_t row = WPR == 1 ? (int64_t)blockIdx.x * 4 + wave : blockIdx.x;
+  const int64_t wg = workgroup<64 * (WPR == 1 ? 4 : WPR)>();
+  const int64_t row = WPR == 1 ? wg * 4 + wave : wg;
   if (row >= rows) return;
   const int t = WPR == 1 ? (threadIdx.x & 63) : threadIdx.x;
   const T* x = X + row * ldx;
@@ -84,12 +85,14 @@ __global__ __launch_bounds__(64 * (WPR == 1 ? 4 : WPR)) void k_quantize_rows(con
 
 // Rows longer than the registers take: read twice, the second time mostly from the caches.
 template <typename T>
-__global__ __launch_bounds__(1024) void k_quantize_long_rows(const T* __restrict__ X, int64_t cols, int64_t ldx,
+__global__ __launch_bounds__(1024) void k_quantize_long_rows(const T* __restrict__ X, int64_t rows, int64_t cols, int64_t ldx,
                                                              int8_t* __restrict__ codes, int64_t ldc, int64_t pad,
                                                              float* __restrict__ scale, bool wide_x, bool wide_c) {
   __shared__ float part[16];
-  const T* x = X + (int64_t)blockIdx.x * ldx;
-  int8_t* c = codes + (int64_t)blockIdx.x * ldc;
+  const int64_t row = workgroup<1024>();
+  if (row >= rows) return;
+  const T* x = X + row * ldx;
+  int8_t* c = codes + row * ldc;
   float m = 0.0f;
   for (int64_t at = (int64_t)threadIdx.x * 8; at < cols; at += 8192) {
     float v[8];
@@ -111,7 +114,7 @@ __global__ __launch_bounds__(1024) void k_quantize_long_rows(const T* __restrict
     load8(x + at, cols - at, wide_x, v);
     store8(c + at, codes8(v, inv, s == s), pad - at, wide_c);
   }
-  if (threadIdx.x == 0) scale[blockIdx.x] = s;
+  if (threadIdx.x == 0) scale[row] = s;
 }
 
 template <typename T>
@@ -125,7 +128,8 @@ hipError_t launch(const void* X, int64_t rows, int64_t cols, int64_t ldx, int8_t
   const bool wx = ((reinterpret_cast<uintptr_t>(X) | (uintptr_t)(ldx * sizeof(T))) & 15) == 0;
   const bool wc = ((reinterpret_cast<uintptr_t>(codes) | (uintptr_t)ldc) & 7) == 0;
 #define AWSRC_ROWS(WPR, CH)                                                                                            \
-  hipLaunchKernelGGL((k_quantize_rows<T, WPR, CH>), dim3((unsigned)(WPR == 1 ? (rows + 3) / 4 : rows)),                \
+  hipLaunchKernelGGL((k_quantize_rows<T, WPR, CH>),                                                                    \
+                     grid_of<64 * (WPR == 1 ? 4 : WPR)>(WPR == 1 ? (rows + 3) / 4 : rows),                            \
                      dim3(64 * (WPR == 1 ? 4 : WPR)), 0, st, x, rows, cols, ldx, codes, ldc, pad, scale, wx, wc)
   // One wavefront a row where there are rows enough to fill the machine and a
   // row fits its registers; else as many as leave each lane one or two pieces,
@@ -140,8 +144,8 @@ hipError_t launch(const void* X, int64_t rows, int64_t cols, int64_t ldx, int8_t
   else if (rows >= 1024 && cols <= 12288) AWSRC_ROWS(8, 3);
   else if (cols <= 16384) AWSRC_ROWS(16, 2);
   else
-    hipLaunchKernelGGL((k_quantize_long_rows<T>), dim3((unsigned)rows), dim3(1024), 0, st, x, cols, ldx, codes, ldc, pad,
-                       scale, wx, wc);
+    hipLaunchKernelGGL((k_quantize_long_rows<T>), grid_of<1024>(rows), dim3(1024), 0, st, x, rows, cols, ldx, codes, ldc,
+                       pad, scale, wx, wc);
 #undef AWSRC_ROWS
   return hipGetLastError();
 }

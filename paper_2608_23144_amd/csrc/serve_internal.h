@@ -97,6 +97,19 @@ __device__ __forceinline__ uint2 codes8(const float (&v)[8], float inv, bool liv
   return o;
 }
 
+// A grid of n < 2^31 workgroups.  A launch counts its threads along x in 32 bits, and the runtime lets more of them wrap
+// around without an error (16.8 M workgroups of 256 ran 65,536): past 2^31 threads they go along y, in rows of 2^31
+// threads.  workgroup() is a workgroup's number, in the last row n or more.
+template <int THREADS>
+dim3 grid_of(int64_t n) {
+  constexpr int64_t kRow = ((int64_t)1 << 31) / THREADS;
+  return n <= kRow ? dim3((unsigned)n) : dim3((unsigned)kRow, (unsigned)((n + kRow - 1) / kRow));
+}
+template <int THREADS>
+__device__ __forceinline__ uint32_t workgroup() {
+  return blockIdx.x + blockIdx.y * (uint32_t)(((int64_t)1 << 31) / THREADS);
+}
+
 struct LinearArgs {
   const int8_t* A;       // [M][lda] activation codes
   int64_t lda;

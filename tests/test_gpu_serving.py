@@ -782,3 +782,77 @@ def test_a_captured_step_replays():
         for c, s in zip(cache, start):
             c.copy_(s)
         assert torch.equal(got, step()), i
+
+
+# ------------------------------------------------------------------ launches of more threads than 32 bits count
+def test_rows_of_a_large_launch():
+    """67.2 M short rows: a wavefront each is more than 2^32 threads."""
+    rows = (1 << 26) + 100003
+    x = torch.arange(rows, device=DEV).remainder_(255).sub_(127).bfloat16()[:, None]
+    c, s = awsrc.awsrc_quantize_rows_i8(x, out=(torch.full((rows, 1), 99, dtype=torch.int8, device=DEV), torch.full((rows,), 99.0, device=DEV)))
+    assert torch.equal(c.float(), x.float().sign() * 127)
+    assert torch.equal(s, torch.div(x.float().abs(), torch.full_like(s, 127.0)[:, None])[:, 0])
+
+
+@pytest.mark.parametrize("with_q", [False, True])
+def test_cache_calls_of_a_large_launch(with_q):
+    """32,768 sequences beside one that brings 4096 tokens: 16.8 M workgroups of 256 threads, each for one page at most.
+    The same tokens in groups of 1024 sequences take far fewer."""
+    n, new, T = 32768, 4096, 16
+    news = torch.ones(n, dtype=torch.int64)
+    news[5] = new
+    cu = torch.cat([torch.zeros(1, dtype=torch.int64), news.cumsum(0)])
+    table = torch.full((n, new // T), -1, dtype=torch.int32)
+    table[:, 0] = (torch.arange(n) + (torch.arange(n) > 5) * (new // T - 1)).int()
+    table[5] = 5 + torch.arange(new // T).int()
+    pages, rows = n - 1 + new // T, int(cu[-1])
+    cu_d, kv_len, table = cu.int().to(DEV), news.int().to(DEV), table.to(DEV)
+    g = _gen("large launch")
+    k, v, q = (_randn(g, rows, 1, 64).bfloat16().to(DEV) for _ in range(3))
+    cos, sin = (t.to(DEV) for t in _rope(new, 64, g))
+    one, two = awsrc.make_kv_cache(pages, 1, 64, T), awsrc.make_kv_cache(pages, 1, 64, T)
+    for c in (one, two):
+        for t in c:
+            t.zero_()
+    args = dict(cos=cos, sin=sin, q=q if with_q else None)
+    got_q = awsrc.awsrc_kv_append(one, k, v, cu_d, kv_len, table, new, **args)
+    got = awsrc.awsrc_kv_read(one, cu_d, kv_len, table, rows, new)
+    for s0 in range(0, n, 1024):
+        r0, r1 = int(cu[s0]), int(cu[s0 + 1024])
+        part = (cu_d[s0:s0 + 1025] - r0, kv_len[s0:s0 + 1024], table[s0:s0 + 1024])
+        want_q = awsrc.awsrc_kv_append(two, k[r0:r1], v[r0:r1], *part, new, cos=cos, sin=sin, q=q[r0:r1] if with_q else None)
+        want = awsrc.awsrc_kv_read(two, *part, r1 - r0, new)
+        assert torch.equal(got[0][r0:r1], want[0]) and torch.equal(got[1][r0:r1], want[1])
+        assert (got_q is None and want_q is None) if not with_q else torch.equal(got_q[r0:r1], want_q)
+    for x, y in zip(one, two):
+        assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("D,n,new", [(64, (1 << 22) + 100, 64), (64, (1 << 17) + 100, 16384), (128, (1 << 17) + 100, 16384)])
+def test_attention_of_a_large_launch(D, n, new):
+    """Single tokens beside one longer sequence, in more workgroups than 2^32 threads hold: by 16 rows (4 x 2^22), by 128
+    (128 x 2^17) and by 256 (64 x 2^17 of 512 threads).  The short sequences see one token, whose value is their result."""
+    news = torch.ones(n, dtype=torch.int64, device=DEV)
+    news[n - 3] = new
+    cu = torch.cat([torch.zeros(1, dtype=torch.int64, device=DEV), news.cumsum(0)]).int()
+    rows, T = n - 1 + new, 128
+    cache = awsrc.make_kv_cache(new // T + 1, 1, D, T)
+    g = torch.Generator(device=DEV)
+    g.manual_seed(3)
+    for c in cache[:2]:
+        c.copy_(torch.randint(-127, 128, c.shape, generator=g, device=DEV, dtype=torch.int32).to(torch.int8))
+    for c in cache[2:]:
+        c.fill_(0.01)
+    table = torch.zeros(n, max(1, new // T), dtype=torch.int32, device=DEV)
+    table[n - 3] = torch.arange(table.shape[1], device=DEV).int()
+    q = torch.randn(rows, 1, D, generator=g, device=DEV, dtype=torch.bfloat16)
+    out = torch.full_like(q, 99.0)
+    awsrc.awsrc_kv_attention(cache, q, cu, news.int(), table, new, new, out=out)
+    r0 = int(cu[n - 3])
+    alone = awsrc.awsrc_kv_attention(cache, q[r0:r0 + new], torch.tensor([0, new], dtype=torch.int32, device=DEV),
+                                     torch.tensor([new], dtype=torch.int32, device=DEV), table[n - 3:n - 2], new, new)
+    long = out[r0:r0 + new].float()
+    assert (long - alone.float()).abs().max() < 2e-2  # half an ulp of bf16 below 2 on each side, whatever the split
+    want = (cache[1][0, 0, :, 0].float() * cache[3][0, 0]).bfloat16()
+    short = torch.cat([out[:r0, 0], out[r0 + new:, 0]])
+    assert (short.float() - want.float()).abs().max() < 1e-2
