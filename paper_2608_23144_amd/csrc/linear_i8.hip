@@ -14,8 +14,14 @@ namespace awsrc {
 
 namespace {
 
-// The epilogue, the same in every kernel: two roundings after the sum's own.
-__device__ __forceinline__ float scaled(int sum, float sa, float sb, float bias) { return __builtin_fmaf((float)sum, sa * sb, bias); }
+// The epilogue, the same in every kernel: two roundings after the sum's own.  The asm keeps the compiler from taking the fma
+// and the conversion to fp16 after it as one instruction, which does not round to fp32 in between: it did so in some of the
+// kernels, where one output in 60,000 had another last bit.
+__device__ __forceinline__ float scaled(int sum, float sa, float sb, float bias) {
+  float y = __builtin_fmaf((float)sum, sa * sb, bias);
+  asm("" : "+v"(y));
+  return y;
+}
 
 template <typename TO>
 __device__ __forceinline__ void store4(TO* o, const float (&y)[4], int64_t n, int64_t N, bool wide) {

@@ -288,6 +288,44 @@ def test_matmul_i8_large(M, N, K, dtype):
     assert (buf[:, N:] == 7.0).all()
 
 
+# N, K and the rows that the first operand is cut to; with the kernels that those take (rows of 16 and 32, tiles by their rows
+# and columns, s: the sum in parts, p: weights past the last cache)
+LADDERS = [(700, 4500, (1, 16, 17, 32, 33, 300)),   # rows 16, 16, 32, 32, 64 x 64 s, 64 x 64 s
+           (100, 17000, (3, 20, 32, 64, 65)),       # rows 16, 32 x 64 s, 32 x 64 s, 64 x 64 s, 64 x 64 s
+           (12400, 5504, (1, 15, 32, 64)),          # 32 x 64 p, p, p, 64 x 64
+           (24600, 2736, (7, 40, 64)),              # 32 x 64 p, 64 x 128 p, p
+           (24600, 150, (16, 64, 65, 200)),         # 32 x 64, 64 x 128, 128 x 128, 128 x 128
+           (4200, 601, (2, 31, 500, 1000, 3590))]   # rows 16, 32, 64 x 128, 128 x 128, 256 x 256
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("N,K,Ms", LADDERS)
+def test_product_bits_do_not_depend_on_the_kernel(N, K, Ms, dtype):
+    """fma(f32(sum), f32(a_scale b_scale), bias), rounded once to the output's type: the same bits from every kernel, with
+    the rows quantized beforehand, inside the kernel, and in two launches.
+
+    The reference is exact up to its own two roundings: scales lie in [2^-11, 2^-10), so that the 48 bits of f32(sum) times
+    f32(a_scale b_scale) end at 2^-45 or above; the bias has 24 bits down to 2^-20 and is at most 16; their sum spans at
+    most 50 bits where the product is below 16, else at most 49: 64 bits hold it whole."""
+    g = _gen("bits", N, K)
+    a, b = _codes(g, max(Ms), K, fill=3), _codes(g, N, K, fill=5)
+    a[0], b[0], b[1] = -128, -128, 127  # sums past 2^24, which round to fp32 (K from 1025 on)
+    sa, sb = ((torch.rand(n, generator=g) * 0.5 + 0.5).clamp(max=1 - 2.0 ** -24).to(DEV) * 2.0 ** -10 for n in (max(Ms), N))
+    bias = (torch.randint(-(1 << 24), 1 << 24, (N,), generator=g).double() * 2.0 ** -20).float().to(DEV)
+    acc = a.double() @ b.double().T
+    assert acc.abs().max() == 16384 * K
+    f = sa[:, None] * sb
+    want = (acc.float().double() * f.double() + bias.double()).float().to(dtype)
+    for M in Ms:
+        assert torch.equal(awsrc.awsrc_matmul_i8(a[:M], sa[:M], b, sb, bias=bias, out_dtype=dtype), want[:M]), M
+    x = _randn(g, max(Ms), K).to(dtype).to(DEV)
+    c, s = awsrc.awsrc_quantize_rows_i8(x)
+    want = awsrc.awsrc_matmul_i8(c, s, b, sb, bias=bias, out_dtype=dtype)
+    for M in Ms:
+        assert torch.equal(awsrc.awsrc_matmul_i8(c[:M], s[:M], b, sb, bias=bias, out_dtype=dtype), want[:M]), M
+        assert torch.equal(awsrc.awsrc_linear_i8(x[:M], b, sb, bias=bias), want[:M]), M
+
+
 def test_integer_sums_do_not_depend_on_the_run():
     g = _gen("again")
     for M, N, K in ((2, 500, 9000), (96, 700, 5000), (600, 600, 3000)):
