@@ -209,3 +209,28 @@ def test_workspaces_a_kernel_cannot_write_are_refused():
     assert keep is words and at == words.data_ptr() and n == 128
     at, n, keep = awsrc._sized_workspace(words, 129, x, None)
     assert keep is not words and n >= 129
+
+
+def test_attention_over_long_sequences_needs_a_workspace():
+    """Two sequences of 2^20 tokens are split: the size is not 0, the binding's helper agrees, and less is refused."""
+    n = ctypes.c_size_t(0)
+    shape = dict(n_seq=2, n_rows=2, max_new=1, max_kv=1 << 20, table_ld=1 << 14)
+    query = dict(q=None, out=None, ws=None, cu=None, kv_len=None, table=None, n=ctypes.byref(n))
+    assert _call(L.awsrc_kv_attention, {**ATTEND, **query}, cache=_cache(k=None, v=None, k_scale=None, v_scale=None), **shape) == OK
+    # at least two parts of 16 rows of 128 sums and three statistics for each of the 2 x 2 sequences and cached heads
+    assert n.value >= 2 * 2 * 2 * 16 * 131 * 4
+    assert awsrc.kv_attention_workspace_bytes(2, 2, 1, 1 << 20, 1 << 14, 8, 2, 128, 64) == n.value
+    for bad, want in ((dict(n=_ws(n.value - 1)), ENOSPC), (dict(n=_ws(n.value), ws=None), ENOSPC), (dict(n=_ws(n.value), ws=P + 8), EINVAL)):
+        assert _call(L.awsrc_kv_attention, {**ATTEND, "cache": _cache(), "n": None}, **{**shape, **bad}) == want
+
+
+def test_product_of_few_tiles_under_a_long_sum_needs_a_workspace():
+    n = ctypes.c_size_t(0)
+    M, N, K = 300, 64, 131071
+    shape = dict(M=M, N=N, K=K, lda=131072, ldb=131072, ldo=N)
+    assert _call(L.awsrc_matmul_i8, {**MATMUL, "n": ctypes.byref(n)}, A=None, a_scale=None, B=None, b_scale=None, out=None, ws=None,
+                 **shape) == OK
+    assert n.value >= 2 * M * N * 4  # at least two parts of the sums
+    assert awsrc.matmul_i8_workspace_bytes(M, N, K) == n.value
+    for bad, want in ((dict(n=_ws(n.value - 1)), ENOSPC), (dict(n=_ws(n.value), ws=None), ENOSPC), (dict(n=_ws(n.value), ws=P + 8), EINVAL)):
+        assert _call(L.awsrc_matmul_i8, MATMUL, **{**shape, **bad}) == want
