@@ -547,6 +547,8 @@ awsrc_status awsrc_linear_i8(const void* X, int32_t x_dtype, int64_t ldx, const 
  *           page page_table[s][t / page_tokens].  Entries past the last token are
  *           not read.
  * max_new (host) is at least the largest cu[s + 1] - cu[s].
+ * Rows of no sequence (from cu[n_seq] on) are neither read nor written.  Keys and
+ * values of a sequence with kv_len above 2^30 are neither appended nor read back.
  */
 typedef struct awsrc_kv_cache {
   int8_t* k;
@@ -586,8 +588,9 @@ awsrc_status awsrc_kv_append(const awsrc_kv_cache* cache, const void* k, int64_t
  * The values that the cache holds for the batch's rows (the last
  * cu[s + 1] - cu[s] tokens of each sequence), as dense [n_rows][kv_heads][head_dim]
  * rows of `dtype`: code * scale, rounded once.  A token whose page lies outside
- * the cache or the table reads as NaN.  For moving a sequence elsewhere, or
- * for code that takes dense keys.
+ * the cache or the table reads as NaN; rows before a sequence's first token (more
+ * rows than tokens) are not written.  For moving a sequence elsewhere, or for
+ * code that takes dense keys.
  */
 awsrc_status awsrc_kv_read(const awsrc_kv_cache* cache, int32_t n_seq, int64_t n_rows, const int32_t* cu,
                            const int32_t* kv_len, const int32_t* page_table, int64_t table_ld, int64_t max_new,
@@ -600,7 +603,9 @@ awsrc_status awsrc_kv_read(const awsrc_kv_cache* cache, int32_t n_seq, int64_t n
  * causal != 0, all kv_len[s] of them otherwise.  q_heads is a multiple of
  * kv_heads; query head h reads cached head h / (q_heads / kv_heads).  A row that
  * sees no token is 0.  Tokens whose page lies outside the cache or the table are
- * not seen.  Scores, maximum and sums in fp32; products in fp16 with fp32 sums.
+ * not seen.  Scores, maximum and sums in fp32; products in fp16 with fp32 sums:
+ * the weights of the second one are rounded to fp16, which adds 2e-4 rms of an
+ * output.  The same call gives the same bits.
  * The scales in the cache are not negative (or NaN).
  *  q, out   [n_rows][q_heads][head_dim] bf16 or fp16 (dtype), rows ldq and ldo
  *           apart, 16-byte aligned, ldq and ldo multiples of 8.

@@ -527,6 +527,7 @@ def awsrc_reconstruct_bf16_sdq(plan: awsrc_decode_plan,
 # ------------------------------------------------------------------ 8-bit serving
 # These calls are made many times per token: what they check of their arguments
 # is kept to cheap attribute reads, sizes that depend on shapes alone are remembered.
+# They serve: none of them records a gradient, also for inputs that require one.
 KVCache = Tuple[torch.Tensor, torch.Tensor, torch.Tensor, torch.Tensor]  # codes of keys and values, their scales
 
 _ACT_CODE = {torch.float32: AWSRC_DTYPE_F32, torch.bfloat16: AWSRC_DTYPE_BF16, torch.float16: AWSRC_DTYPE_F16}
@@ -757,7 +758,8 @@ def awsrc_linear_i8(x: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, bia
                     out_dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None,
                     workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """A linear layer on int8 weights: x [M, K] quantized per row, times w [N, K] (codes and scales as
-    awsrc_quantize_rows_i8 makes them from the weight matrix) transposed, plus bias; [M, N] in x's type by default."""
+    awsrc_quantize_rows_i8 makes them from the weight matrix) transposed, plus bias; [M, N] in x's type by default.
+    For inference: the result carries no gradient."""
     M, K, ldx = _rows_of(x, "x")
     N, Kw, ldw = _i8_rows(w, "w")
     if K != Kw:
@@ -784,7 +786,8 @@ def awsrc_kv_append(cache: KVCache, k: torch.Tensor, v: torch.Tensor, cu: torch.
                     q_out: Optional[torch.Tensor] = None, stream=None) -> Optional[torch.Tensor]:
     """Appends rows of k and v [rows, kv_heads, head_dim] (views of a fused projection's output will do) to the cache,
     keys rotated by the tables cos, sin [positions, rot / 2]; returns q [rows, q_heads, head_dim] rotated the same way.
-    kv_len counts the appended tokens; max_new is at least the most rows that one sequence brings."""
+    kv_len counts the appended tokens; max_new is at least the most rows that one sequence brings.  q_out does not
+    overlap q.  For inference: no gradient is recorded."""
     c, heads, dim, _, dev = _cache_of(cache)
     n_seq, table_ld = _batch_of(dev, cu, kv_len, page_table)
     _on_device(dev, k, v, q, cos, sin, q_out)
@@ -853,7 +856,8 @@ def awsrc_kv_attention(cache: KVCache, q: torch.Tensor, cu: torch.Tensor, kv_len
                        out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
                        stream=None) -> torch.Tensor:
     """Attention of q [rows, q_heads, head_dim] (rotated, bf16 or fp16) over the cache; scale defaults to
-    head_dim ** -0.5.  max_new and max_kv bound the rows and the cached tokens of a sequence."""
+    head_dim ** -0.5.  max_new and max_kv bound the rows and the cached tokens of a sequence.  For inference: the result
+    carries no gradient."""
     c, kv_heads, dim, page, dev = _cache_of(cache)
     n_seq, table_ld = _batch_of(dev, cu, kv_len, page_table)
     _on_device(dev, q, out)

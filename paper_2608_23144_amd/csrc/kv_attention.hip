@@ -8,7 +8,10 @@
 // Matrix products in fp16 with fp32 sums: the codes are fp16 exactly, a query
 // row is brought to magnitudes below 2 by a power of two (exact, but for
 // channels 2^-14 below the row's largest), and p is at most 1 by the running
-// maximum.  The key scale multiplies the score.  The value scale goes into the
+// maximum.  p is rounded to fp16's 11 bits for the second product, which takes
+// the matrix cores' fp16 rate: fp16 outputs lie 2.8e-4 rms from the formula in
+// 64 bits, 2.1e-4 with fp32 weights; bf16 ones 1.7e-3 either way.  The key scale
+// multiplies the score.  The value scale goes into the
 // exponent, p' = exp2(s + log2 s_V - max), so that p' c needs no further
 // scaling and p' stays in fp16's range whatever the pages' scales are; the
 // denominator sums p' / s_V in fp32.
@@ -394,7 +397,7 @@ __device__ __forceinline__ void store_row4(T* out, fl4 y, float l, float f) {
 // into LDS (two stages), and then serve all W wavefronts through 32 x 32 x 16
 // products.  The next tile's codes are on their way from memory while the
 // current one is computed.  Bound by vector and matrix instructions one after the
-// other (8192 tokens of a 3B layer: 316 us, 870 TFLOP/s; of the CUs' busy cycles 57% issue
+// other (8192 tokens of a 3B layer: 320 us, 860 TFLOP/s, 315 to 330 by machine; of the CUs' busy cycles 58% issue
 // vector instructions and 39% run matrix ones).  Neither wavefront priorities, nor half
 // of the wavefronts a phase behind the others, nor the next tile's scores during this one's exponentials (too many
 // registers) overlapped them: four SIMDs at their products take LDS's whole rate, 1 KB in 32 cycles each.
@@ -417,7 +420,7 @@ struct TileLds {
 };
 
 // The order of a block of N matrix products, consecutive ones on different sums: every operand is read from LDS four
-// products ahead.  8192 tokens of a 3B layer: 331 us, 338 in the compiler's own order and with whole sums in a row.
+// products ahead.  8192 tokens of a 3B layer: 320 us, 325 in the compiler's own order.
 template <int N>
 __device__ __forceinline__ void reads_ahead() {
   constexpr int kProduct = 0x8, kRead = 0x100;
@@ -449,8 +452,8 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void k_kv_attention_tiles
   // the last rows see the most tokens: they start first
   const int qt = plan.tiles_q - 1 - (int)(b % (uint32_t)plan.tiles_q);
   b /= (uint32_t)plan.tiles_q;
-  // every sequence's first part before any second: the short last parts start late (seven pieces of 601 tokens of a
-  // 3B layer: 177 us sequence by sequence, 171)
+  // every sequence's first part before any second: the short last parts start late (pieces of 601 tokens in seven
+  // sequences of up to 6007, heads of 64: 123 us sequence by sequence, 120; of a 32B layer 513 and 508)
   const int s = b % (uint32_t)a.n_seq, split = b / (uint32_t)a.n_seq;
   if (split >= plan.n_split) return;
   Rows rows;
@@ -795,10 +798,11 @@ Plan plan_of(const AttentionArgs& a) {
   if (most > a.max_kv) most = a.max_kv;
   // Splits, as far as they fill the machine: each costs a join.  Few rows: as many
   // workgroups as reside at once on half of the CUs' registers (D = 128: 2 x 131071 tokens of a
-  // group of 8 take 30.7 us in 512 workgroups, 34.5 in 1024; the ragged batch of 64 133, 144),
-  // of at least 256 tokens (1501 tokens: 10.0 us, 11.4 with 512).  Many rows: one sequence
-  // 512 workgroups (512 rows after 16000 tokens: 116 us, 133 in 1024), a batch, whose lengths differ,
-  // 4096 of at least 1024 tokens (ragged pieces of prompts: 101 us, 171 in 512).
+  // group of 8 take 29.4 us in 512 workgroups, 33.9 in 1024; the ragged batch of 64 126, 138),
+  // of at least 256 tokens (2000 tokens: 10.3 us, 11.8 with 512).  Many rows: one sequence
+  // 512 workgroups (512 rows after 16000 tokens: 110 us, 133 in 1024), a batch, whose lengths differ,
+  // 4096 of at least 1024 tokens (pieces of 601 tokens in seven sequences of up to 6007, heads of 64:
+  // 120 us, 169 in 512; of a 3B layer, where it costs, 231 and 209).
   int64_t target, least;
   if (p.tile == kRowTile) {
     target = a.c.head_dim == 64 ? 768 : a.c.head_dim == 128 ? 512 : 256;
@@ -811,7 +815,9 @@ Plan plan_of(const AttentionArgs& a) {
   const int64_t cap = (most + least - 1) / least;
   if (split > cap) split = cap;
   // Sequences of different lengths leave CUs idle at the end: where they have to be split at all, into twice as many
-  // parts, unless those get short (24 of up to 8192 tokens, 32B layer: 61 us, 71; 40 of 20000, 3B layer: 60 and 76).
+  // parts, unless those get short.  Of up to 8192 tokens of a 32B layer, on the GPU in us with and without: 24 sequences
+  // 54 and 63, 32 70 and 65, 40 79 and 88, 48 92 and 91, 56 114 and 126, 63 128 and 134; 64, which fill the machine
+  // and stay whole, 126.
   if (p.tile == kRowTile && a.n_seq > 1 && base < target) {
     int64_t even = (2 * target + base - 1) / base;
     if (even > most / (8 * a.c.head_dim)) even = most / (8 * a.c.head_dim);
@@ -831,7 +837,7 @@ Plan plan_of(const AttentionArgs& a) {
   p.n_split = (int)((most + p.chunk - 1) / p.chunk);
   if (p.n_split < 1) p.n_split = 1;
   // Rows enough for every CU twice without a split: 256 a workgroup, which halves the work of turning
-  // codes into fp16 (8192 tokens of a 3B layer: 368 us with 128, 326; 1000 tokens each of four
+  // codes into fp16 (8192 tokens of a 3B layer: 358 us with 128, 320; 1000 tokens each of four
   // sequences of a 32B layer, where whole workgroups of the shorter ones idle, 67 and 71).
   if (p.tile == kTileRows && p.n_split == 1 && a.c.head_dim == 128 && rows >= 16384) {
     const int64_t wide = (rows + 2 * kTileRows - 1) / (2 * kTileRows);

@@ -71,7 +71,7 @@ __device__ __forceinline__ void turn_quads(i32x4 (&v)[4], int lane) {
 // cache takes in a quad of lanes a cycle only where they read 64 bytes side by
 // side.  So lane j of a quad loads piece j of its quad's four rows, and the quad
 // trades them: the lane ends with 64 bytes of its own row, which are its pieces of
-// four steps (13 x 2048 x 11008: 7.7 us, 11.2 with each lane loading its own;
+// four steps (13 x 2048 x 11008, weights in the last cache: 7.7 us, 11.2 with each lane loading its own;
 // neither 16 wavefronts nor 8 columns a workgroup are faster: 7.6 and 7.8).
 template <int W, int R, bool AHEAD>
 struct RowSums {
@@ -180,8 +180,8 @@ struct RowSums {
   }
 };
 
-// On activation codes in memory.  13 x 2560 x 2048: 3.2 us; 13 x 2048 x 11008: 7.7
-// (128 workgroups: half of the CUs at 25 GB/s of weights each, 2.9 TB/s in all).
+// On activation codes in memory.  Weights in the last cache: 13 x 2560 x 2048 3.2 us, 13 x 2048 x 11008 7.7
+// (128 workgroups: half of the CUs at 23 GB/s of weights each, 2.9 TB/s in all); from memory the latter takes 10.2.
 template <int W, int R, typename TO>
 __global__ __launch_bounds__(64 * W) void k_matmul_i8_rows(LinearArgs a) {
   __shared__ i32x4 part[W][R][64];
@@ -195,7 +195,7 @@ __global__ __launch_bounds__(64 * W) void k_matmul_i8_rows(LinearArgs a) {
 // On activations: every workgroup quantizes the few rows itself (into LDS, as
 // quant_i8.hip does), while its first weights are on their way, which saves a
 // launch and its wait.  Each row's values are read twice, the second time from
-// the nearest cache.  Bound by latency: 1 x 2560 x 2048 4.5 us, of which its 5 MB take 0.8.
+// the nearest cache.  Bound by latency: 1 x 2560 x 2048 4.5 us, 5.0 with weights from memory, of which the 5 MB take 0.8.
 template <int W, typename T, typename TO>
 __global__ __launch_bounds__(64 * W) void k_linear_i8_rows(LinearArgs a, const T* X, int64_t ldx, int pitch, bool wide) {
   __shared__ i32x4 part[W][1][64];
@@ -263,7 +263,7 @@ __global__ __launch_bounds__(64 * W) void k_linear_i8_rows(LinearArgs a, const T
 // 128 x 128 wait at every barrier together: 1.20 against 1.11 ms at 8192 x 27648
 // x 5120; 1.06 with results that leave in whole lines, 2.19 POPS, where a library's
 // product of the same matrices into int32 takes 1.11).  Bound by the matrix cores
-// there, by the weights' bytes with few rows (64 x 27648 x 5120: 33 us, 4.4 TB/s),
+// there, by the weights' bytes with few rows (64 x 27648 x 5120: 29.7 us, 4.9 TB/s),
 // and by LDS and barriers a step where the tiles do not fill the machine.
 //
 // Rows and pieces past the operands' ends come from beyond the buffer resource
@@ -642,7 +642,7 @@ hipError_t launch_linear_rows_t(const LinearArgs& a, const void* X, int64_t ldx,
 }
 
 // Which kernel takes a product, and over how many parts of the sum.  Times below
-// are of whole calls in us on weights that are not in the caches.
+// are in us, of calls on weights that are not in the caches.
 enum Path { kRows, kTile32, kTile64, kTile64Wide, kTile128, kTile256 };
 struct Choice {
   Path path;
@@ -664,7 +664,7 @@ Choice choose(int64_t M, int64_t N, int64_t K) {
   // 1024 x 5120 x 5120: 40 and 54; 8192 x 27648 x 5120: 1249 and 1105).
   const int64_t t128 = tiles(128, 128), t256 = tiles(256, 256);
   if (M > 64 && t128 >= 256) return {2.9 * ((t256 + 255) / 256) < t128 / 256.0 + 0.5 ? kTile256 : kTile128, 1};
-  // 64 x 27648 x 5120: 64 x 64 tiles 42.0, 64 x 128 tiles 35.1 (64 x 11008 x 2048: 7.8 and 10.5)
+  // 64 x 27648 x 5120: 64 x 64 tiles 37.7, 64 x 128 tiles 29.7 (64 x 11008 x 2048: 7.8 and 10.5)
   if (M > 32 && tiles(64, 128) >= 192) return {kTile64Wide, 1};
   const Path path = M > 32 ? kTile64 : kTile32;
   // Few tiles under a long sum: parts of at least 16 steps, joined by a second
@@ -678,8 +678,9 @@ Choice choose(int64_t M, int64_t N, int64_t K) {
 template <typename TO>
 hipError_t launch(const LinearArgs& a, void* ws, hipStream_t st) {
   const Choice c = choose(a.M, a.N, a.K);
-  // Weights read once that fill a good part of the last cache go past it (64 x 27648 x 5120: 36.5 us, 33.9 past
-  // it; 64 x 11008 x 2048, whose 23 MB stay there from call to call: 8.8, 10.1 past it).
+  // Weights read once that fill a good part of the last cache go past it (64 x 27648 x 5120: 33.0 us, 29.7 past
+  // it; 16 x 27648 x 5120 30.3 and 26.6; 64 x 11008 x 2048, whose 23 MB stay there from call to call: 8.8, 10.1 past
+  // it).  64 x 64 tiles, of fewer columns, keep theirs: not tried there.
   const bool once = a.M <= 64 && a.N * a.K >= (int64_t)1 << 26;
   switch (c.path) {
     case kRows: return a.M <= 16 ? launch_rows<8, 1, TO>(a, st) : launch_rows<8, 2, TO>(a, st);
@@ -712,8 +713,10 @@ bool linear_i8_fused(int64_t M, int64_t N, int64_t K) {
   // Where a workgroup's wavefronts read the rows in few pieces a lane, and where there are not so many
   // workgroups that quantizing over and over costs more than a launch.  On the GPU alone, in us (fused and in two
   // launches): 1 x 2560 x 2048 4.5 and 5.7; 1 x 5120 x 5120 8.9 and 10.9; 4 x 5120 x 4096 11.8 and 10.4;
-  // 16 x 2048 x 2048 7.7 and 6.0; 4 x 11008 x 2048 10.3 and 10.0; 1 x 27648 x 5120 31.6 and 28.9.  A launch that is not
-  // replayed from a graph costs the host 3 more, which is why the middle ones are fused.
+  // 16 x 2048 x 2048 7.7 and 6.0; 1 x 27648 x 5120 31.6 and 28.9.  A launch that is not
+  // replayed from a graph costs the host 3 more, which is why the middle ones are fused.  From 8192 columns a call has
+  // a workspace to give and takes two launches, also where fusing up to 12288 would gain on the GPU (1 x 11008 x 2048:
+  // 8.7 and 10.7; 4 x 11008 x 2048 10.4 and 10.9).
   const int64_t share = M <= 1 ? 1 : M <= 2 ? 2 : M <= 4 ? 4 : 8;
   return M <= 16 && K * share <= 16384 && N < 8192;
 }
