@@ -747,6 +747,42 @@ def test_cache_past_32_bit_offsets():
         assert torch.equal(a, e) and torch.isfinite(a).all()
 
 
+@pytest.mark.parametrize("hq,hk,D,lens,news", [(8, 2, 128, [700, 90], [1, 1]), (8, 2, 128, [1500], [1]), (16, 2, 128, [9001, 300, 5000], [1, 1, 2]),
+                                               (4, 2, 64, [1900], [1]), (4, 2, 256, [6007], [40]), (2, 1, 64, [3000, 0, 70], [70, 3, 70]),
+                                               (64, 8, 128, [2050], [2050])])
+def test_the_same_call_gives_the_same_bits(hq, hk, D, lens, news):
+    """Whatever the workspace and the results' memory held before, and however often."""
+    b = Batch(("same", hq, D, lens), hq, hk, D, 64, lens, news, torch.float16)
+    cache, cu, kv_len, table = b.dev()
+    q = b.q.to(DEV)
+    need = awsrc.kv_attention_workspace_bytes(len(lens), b.rows, max(news), max(lens), table.shape[1], hq, hk, D, 64)
+    want = None
+    for byte in (0, 255, 127, 255):  # 255: NaN in fp32 and fp16
+        ws = torch.full((need + 64,), byte, dtype=torch.uint8, device=DEV)
+        out = torch.full((q.nbytes,), byte, dtype=torch.uint8, device=DEV).view(torch.float16).view(q.shape)
+        awsrc.awsrc_kv_attention(cache, q, cu, kv_len, table, max(news), max(lens), out=out, workspace=ws)
+        assert torch.isfinite(out).all() and (ws[need:] == byte).all()
+        assert want is None or torch.equal(out, want)
+        want = out
+
+
+@pytest.mark.parametrize("M,N,K", [(24, 100, 17000), (40, 700, 4500), (3, 9000, 513), (300, 64, 9000)])
+def test_products_do_not_read_their_workspace_first(M, N, K):
+    g = _gen("stale", M, N, K)
+    x = _randn(g, M, K).to(DEV)
+    w, ws = awsrc.awsrc_quantize_rows_i8(_randn(g, N, K).to(DEV))
+    c, s = awsrc.awsrc_quantize_rows_i8(x)
+    want = None
+    for byte in (0, 255, 127):
+        for n, call in ((awsrc.linear_i8_workspace_bytes(M, N, K), lambda t: awsrc.awsrc_linear_i8(x, w, ws, workspace=t)),
+                        (awsrc.matmul_i8_workspace_bytes(M, N, K), lambda t: awsrc.awsrc_matmul_i8(c, s, w, ws, out_dtype=torch.float32, workspace=t))):
+            t = torch.full((n + 64,), byte, dtype=torch.uint8, device=DEV)
+            out = call(t)
+            assert (t[n:] == byte).all()
+            assert want is None or torch.equal(out, want)
+            want = out
+
+
 # ------------------------------------------------------------------ together
 def test_host_workspaces_are_refused():
     """Every call that takes a workspace, at shapes that need one, before any launch."""
