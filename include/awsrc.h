@@ -465,11 +465,12 @@ awsrc_status awsrc_reconstruct_bf16_sdq(const awsrc_decode_plan* plan, int32_t n
                                         const float* const* sdq_step, const uint8_t* const* zero, void* stream);
 
 /*
- * 8-bit serving of repaired weights: linear layers on int8 codes, and a paged
- * int8 cache of keys and values with the attention that reads it.
+ * 8-bit serving of repaired weights: linear layers on int8 or e4m3 codes, a paged
+ * int8 cache of keys and values with the attention that reads it, the plan of a
+ * step's pages and rows, and the verification of drafted tokens.
  *
- * The 8-bit recipe, fp32 with every operation rounded once, is the same for
- * all of them: over a group of values (a row of a matrix; the keys, or the
+ * The int8 recipe, fp32 with every operation rounded once, is the same for
+ * all int8 codes: over a group of values (a row of a matrix; the keys, or the
  * values, of one head in one page)
  *   scale = amax / 127,  inverse = 1 / scale,  code = rint(x * inverse), ties to even,
  * with scale = 0 and codes 0 where amax = max |x| is below 2^-100, and scale
@@ -526,6 +527,73 @@ awsrc_status awsrc_matmul_i8(const int8_t* A, int64_t lda, const float* a_scale,
  * the size may be 0, and then no workspace is needed.
  */
 awsrc_status awsrc_linear_i8(const void* X, int32_t x_dtype, int64_t ldx, const int8_t* B, int64_t ldb,
+                             const float* b_scale, const float* bias_or_null, int64_t M, int64_t N, int64_t K, void* out,
+                             int32_t out_dtype, int64_t ldo, void* workspace, size_t* ws_bytes, void* stream);
+
+/*
+ * The same weights in 8-bit floating point: e4m3 codes (sign, 4 exponent bits of bias
+ * 7, 3 bits of mantissa; largest 448, no infinities, NaN 0x7F and 0xFF) with an fp32
+ * scale for each block of 128 columns, so that a loud channel costs the
+ * precision of its own block and not of the whole row.  The recipe, fp32 with
+ * every operation rounded once, over a block of values:
+ *   scale = amax / 448,  inverse = 1 / scale,  code = x * inverse rounded to e4m3, ties to even,
+ * with the exceptions of the int8 recipe: scale 0 and codes 0 where amax is
+ * below 2^-100, scale NaN and codes 0 where a value of the block is infinite or NaN.
+ * The last block of a row, or of rows, is as short as the matrix ends.
+ */
+
+/*
+ * A matrix as e4m3 codes with one scale for each block.
+ *  X           [rows, cols] x_dtype, row i at X + i * ldx, ldx >= cols.
+ *  block_rows  1: blocks of 1 x 128, activations;
+ *              scale [ceil(cols / 128)][rows], a block's column of all rows side by side.
+ *              128: blocks of 128 x 128, weights;
+ *              scale [ceil(rows / 128)][ceil(cols / 128)].
+ *  codes       row i at codes + i * ldc, ldc >= cols; nothing past cols is written.
+ * cols >= 1.  EINVAL: bad shape, dtype or block_rows, NULL buffer, X not aligned to its type.
+ */
+awsrc_status awsrc_quantize_blocks_f8(const void* X, int32_t x_dtype, int64_t rows, int64_t cols, int64_t ldx,
+                                      int32_t block_rows, uint8_t* codes, int64_t ldc, float* scale, void* stream);
+
+/*
+ * The values that codes stand for, as a dense matrix: code * scale in fp32, rounded
+ * once to out_dtype (nearest even).  codes, scale and block_rows as
+ * awsrc_quantize_blocks_f8 writes them; out row i at out + i * ldo, ldo >= cols.
+ */
+awsrc_status awsrc_dequantize_blocks_f8(const uint8_t* codes, int64_t ldc, const float* scale, int64_t rows, int64_t cols,
+                                        int32_t block_rows, void* out, int32_t out_dtype, int64_t ldo, void* stream);
+
+/*
+ * Product of e4m3 matrices with a scale for each block of 128:
+ *   out[m, n] = sum_b a_scale[b][m] b_scale[n / 128][b] sum_{k in block b} A[m, k] B[n, k] + bias[n].
+ * Sums in fp32: a block's products first, then fma(block's sum, a_scale * b_scale, sum so
+ * far); the sum is rounded once to out_dtype (nearest even).  For results in bf16 and fp16
+ * the matrix cores take the products of a block eight by eight, each cut off 2^13 below the
+ * largest of its eight, which is 1.5e-5 rms of a result; for fp32 they do not.  The same
+ * call gives the same bits; calls of other shapes may add in another order.
+ *  A, B     e4m3, row i at A + i * lda; 16-byte aligned, lda and ldb multiples of
+ *           16, >= K rounded up to 16, <= 2^22.  Each row is readable up to K
+ *           rounded up to 16; what lies past K does not matter.
+ *  a_scale  [ceil(K / 128)][M] fp32;  b_scale  [ceil(N / 128)][ceil(K / 128)] fp32.
+ *  bias_or_null  [N] fp32.
+ *  out      [M, N], row m at out + m * ldo, ldo >= N, aligned to its type.
+ * 1 <= K <= 2^22.  M or N of 0 is a no-op.
+ * Workspace: two-phase query as described above (the query needs no pointers);
+ * the size may be 0, and then no workspace is needed.
+ */
+awsrc_status awsrc_matmul_f8(const uint8_t* A, int64_t lda, const float* a_scale, const uint8_t* B, int64_t ldb,
+                             const float* b_scale, const float* bias_or_null, int64_t M, int64_t N, int64_t K, void* out,
+                             int32_t out_dtype, int64_t ldo, void* workspace, size_t* ws_bytes, void* stream);
+
+/*
+ * A linear layer on e4m3 weights: awsrc_quantize_blocks_f8 of X with block_rows 1 and
+ * awsrc_matmul_f8 of its codes with B (the same codes and scales; the sums may be
+ * added in another order).  X is [M, K] x_dtype, row m at X + m * ldx; the codes
+ * live in the workspace, or in the kernel where the rows are few (then its size is 0).
+ * Workspace: two-phase query as described above (the query needs no pointers);
+ * the size may be 0, and then no workspace is needed.
+ */
+awsrc_status awsrc_linear_f8(const void* X, int32_t x_dtype, int64_t ldx, const uint8_t* B, int64_t ldb,
                              const float* b_scale, const float* bias_or_null, int64_t M, int64_t N, int64_t K, void* out,
                              int32_t out_dtype, int64_t ldo, void* workspace, size_t* ws_bytes, void* stream);
 
@@ -619,6 +687,87 @@ awsrc_status awsrc_kv_attention(const awsrc_kv_cache* cache, const void* q, int6
                                 int32_t n_seq, int64_t n_rows, const int32_t* cu, const int32_t* kv_len,
                                 const int32_t* page_table, int64_t table_ld, int64_t max_new, int64_t max_kv, float scale,
                                 int32_t causal, void* out, int64_t ldo, void* workspace, size_t* ws_bytes, void* stream);
+
+/*
+ * The pages of a cache that no sequence holds (device pointers, caller's memory): a
+ * stack, the next page to be taken is free_pages[n_free[0] - 1].
+ */
+typedef struct awsrc_page_pool {
+  int32_t* free_pages;   /* [n_pages] */
+  const int32_t* n_free; /* [1] */
+  int64_t n_pages;
+  int32_t page_tokens;
+  int32_t reserved; /* must be 0 */
+} awsrc_page_pool;
+
+/*
+ * Plans a step of n_seq request slots on the device: gives pages back and takes
+ * pages for the step's new tokens, and writes the batch description that
+ * awsrc_kv_append, awsrc_kv_read and awsrc_kv_attention take.
+ *  kv_len    [n_seq] int32: cached tokens; the slot holds the first
+ *            ceil(kv_len / page_tokens) pages of its row of page_table.
+ *  keep      [n_seq] int32: how many of them stay (refused drafts go, 0 for a finished sequence).
+ *  new_len   [n_seq] int32: tokens that the step appends after them; 0 for a slot that rests.
+ * With held = ceil(kv_len / page_tokens) and want = ceil((keep + new_len) / page_tokens) a
+ * slot takes want - held pages or gives held - want back.  A slot is served if want <= table_ld,
+ * if the new_len of it and all slots before it sum to at most max_rows, and if it takes
+ * nothing or the pages that it and all slots before it take are at most those of the
+ * pool and those that all slots give back.  A slot that is not served gets no rows and
+ * keeps its first keep tokens, without the pages past them.
+ * Pages given back, in order of slot and place, are taken first, then those of
+ * the stack; those left over lie on the stack, the last in order lowest.
+ *  kv_len_out  [n_seq] int32: keep + new_len (keep where a slot is not served); may be kv_len or keep.
+ *  n_free_out  [1] int32; may be the pool's n_free.
+ *  page_table  [n_seq][table_ld] int32, updated: entries of pages taken are written, others stay.
+ *  cu          [n_seq + 1] int32: starts of the slots' rows, cu[s + 1] - cu[s] is what was served.
+ *  row_seq, row_pos, row_slot  each may be NULL; [max_rows]: slot and position (int32) of each
+ *              row and page * page_tokens + position % page_tokens (int64); -1 for rows of no
+ *              slot, and row_slot -1 where the page lies outside the pool.
+ * Negative lengths count as 0, keep as at most kv_len, kv_len as at most what table_ld pages
+ * hold.  Nothing outside the buffers is read or written, whatever they hold.  Calls on one pool
+ * are ordered by `stream`.
+ * n_seq <= 2^20, n_seq * table_ld < 2^31, max_rows < 2^31; page_tokens 16, 32, 64 or 128.
+ * n_seq of 0 is a no-op (nothing is written).
+ * Workspace: two-phase query as described above (the query needs no pointers but
+ * `pool`).
+ */
+awsrc_status awsrc_kv_plan(const awsrc_page_pool* pool, int32_t n_seq, const int32_t* kv_len, const int32_t* keep,
+                           const int32_t* new_len, int32_t* page_table, int64_t table_ld, int64_t max_rows,
+                           int32_t* kv_len_out, int32_t* n_free_out, int32_t* cu, int32_t* row_seq, int32_t* row_pos,
+                           int64_t* row_slot, void* workspace, size_t* ws_bytes, void* stream);
+
+/*
+ * Verifies drafted tokens against the target's probabilities.  Sequence s owns the rows
+ * cu[s] .. cu[s + 1] - 1 of a step; tokens[cu[s]] is its last certain token, the tokens of the
+ * rows after it are drafts.  p_r is the target's distribution of the token after row r, q_r
+ * the one that the draft tokens[r + 1] was drawn from.  From the first row on a draft
+ * x = tokens[r + 1] is accepted while
+ *   u[r] q_r(x) < p_r(x),
+ * without a rounding.  At the first row a whose draft is refused the next token is drawn
+ * from the weights w_i = max(p_a(i) - q_a(i), 0), at the last row, when all are accepted, from
+ * w_i = p_a(i): the lowest i with
+ *   w_0 + ... + w_i > u[last row] (w_0 + ... + w_{vocab - 1}),
+ * or the last i with w_i > 0 where rounding leaves none; sums in fp64.  With u uniform in [0, 1)
+ * the tokens follow the target's distribution.
+ *  p, q    [n_rows][vocab] dtype (fp32, bf16 or fp16), row r at p + r * ldp; they need not sum to
+ *          1.  q NULL: drafts that were not drawn, q_r(x) = 1 for the draft and 0 for all
+ *          others.  q is not read at a sequence's last row.
+ *  tokens  [n_rows] int32, u [n_rows] fp32, cu [n_seq + 1] int32 as for awsrc_kv_append.
+ *  tokens_out  [n_rows] int32: from row cu[s] on the accepted drafts, then the token drawn, then
+ *          -1.  Rows of no sequence are not written.  Does not overlap tokens.
+ *  n_out   [n_seq] int32: how many there are, 1 to cu[s + 1] - cu[s]; 0 for a sequence without rows.
+ *  kv_len, keep  both or neither NULL; [n_seq] int32: keep = kv_len - rows + n_out is what a cache
+ *          that holds all of the step's rows keeps of them (awsrc_kv_plan takes it); may be one buffer.
+ * A draft outside 0 .. vocab - 1 is refused, and nothing is read for it.  Weights that are not
+ * finite, or not positive, count as 0.  If all do the token is drawn from p_a, and if all of p_a do
+ * it is -1.
+ * 1 <= vocab < 2^31.
+ * Workspace: two-phase query as described above (the query needs no pointers).
+ */
+awsrc_status awsrc_verify_drafts(const void* p, int64_t ldp, const void* q_or_null, int64_t ldq, int32_t dtype, int64_t vocab,
+                                 int32_t n_seq, int64_t n_rows, const int32_t* cu, const int32_t* tokens, const float* u,
+                                 const int32_t* kv_len_or_null, int32_t* tokens_out, int32_t* n_out, int32_t* keep_or_null,
+                                 void* workspace, size_t* ws_bytes, void* stream);
 
 /* Host-only helpers (no device needed). */
 /* L_rec in bytes for T_total tiles; -1 if p is invalid. */

@@ -31,7 +31,8 @@ EXPORTED = ("awsrc_abi_version", "awsrc_last_error", "awsrc_backbone_rtn", "awsr
             "awsrc_encode_scored", "awsrc_rank_prefix", "awsrc_decode_add", "awsrc_decode_prepare", "awsrc_decode_apply",
             "awsrc_reconstruct_bf16", "awsrc_reconstruct_bf16_prefixes", "awsrc_reconstruct_bf16_sdq",
             "awsrc_quantize_rows_i8", "awsrc_matmul_i8", "awsrc_linear_i8", "awsrc_kv_append", "awsrc_kv_read",
-            "awsrc_kv_attention", "awsrc_record_bytes", "awsrc_header_bytes", "awsrc_budget_bytes", "awsrc_prefix_K")
+            "awsrc_kv_attention", "awsrc_quantize_blocks_f8", "awsrc_dequantize_blocks_f8", "awsrc_matmul_f8", "awsrc_linear_f8",
+            "awsrc_kv_plan", "awsrc_verify_drafts", "awsrc_record_bytes", "awsrc_header_bytes", "awsrc_budget_bytes", "awsrc_prefix_K")
 
 
 class AwsrcError(RuntimeError):
@@ -58,6 +59,11 @@ class awsrc_kv_cache(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
                 ("v_scale", ctypes.c_void_p), ("n_pages", ctypes.c_int64), ("kv_heads", ctypes.c_int32),
                 ("head_dim", ctypes.c_int32), ("page_tokens", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class awsrc_page_pool(ctypes.Structure):
+    _fields_ = [("free_pages", ctypes.c_void_p), ("n_free", ctypes.c_void_p), ("n_pages", ctypes.c_int64),
+                ("page_tokens", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
 def make_params(C: int, P: int, b: int, S: int, basis_key: int = 0, ridge_lambda: float = 1e-6,
@@ -111,6 +117,14 @@ def _load() -> ctypes.CDLL:
         "awsrc_kv_read": (i32, [ctypes.POINTER(awsrc_kv_cache), i32, i64, vp, vp, vp, i64, i64, vp, vp, i32, vp]),
         "awsrc_kv_attention": (i32, [ctypes.POINTER(awsrc_kv_cache), vp, i64, i32, i32, i32, i64, vp, vp, vp, i64, i64,
                                      i64, ctypes.c_float, i32, vp, i64, vp, ctypes.POINTER(sz), vp]),
+        "awsrc_quantize_blocks_f8": (i32, [vp, i32, i64, i64, i64, i32, vp, i64, vp, vp]),
+        "awsrc_dequantize_blocks_f8": (i32, [vp, i64, vp, i64, i64, i32, vp, i32, i64, vp]),
+        "awsrc_matmul_f8": (i32, [vp, i64, vp, vp, i64, vp, vp, i64, i64, i64, vp, i32, i64, vp, ctypes.POINTER(sz), vp]),
+        "awsrc_linear_f8": (i32, [vp, i32, i64, vp, i64, vp, vp, i64, i64, i64, vp, i32, i64, vp, ctypes.POINTER(sz), vp]),
+        "awsrc_kv_plan": (i32, [ctypes.POINTER(awsrc_page_pool), i32, vp, vp, vp, vp, i64, i64, vp, vp, vp, vp, vp, vp, vp,
+                                ctypes.POINTER(sz), vp]),
+        "awsrc_verify_drafts": (i32, [vp, i64, vp, i64, i32, i64, i32, i64, vp, vp, vp, vp, vp, vp, vp, vp,
+                                      ctypes.POINTER(sz), vp]),
         "awsrc_record_bytes": (i64, [pp, i64]),
         "awsrc_header_bytes": (i64, [i32]),
         "awsrc_budget_bytes": (i64, [ctypes.c_double, i64]),
@@ -877,3 +891,254 @@ def awsrc_kv_attention(cache: KVCache, q: torch.Tensor, cu: torch.Tensor, kv_len
                                       page_table.data_ptr(), table_ld, max_new, max_kv, dim ** -0.5 if scale is None else scale,
                                       causal, out.data_ptr(), ldo, ws, ctypes.c_size_t(n), _raw_stream(dev, stream)))
     return out
+
+
+# ------------------------------------------------------------------ e4m3 codes
+BLOCK_F8 = 128  # columns, and rows of a weight matrix, that share a scale
+_F8 = torch.float8_e4m3fn
+
+
+def _f8_rows(t: torch.Tensor, what: str):
+    """_rows_of for an e4m3 operand: its rows are read in pieces of 16 bytes."""
+    if t.dtype != _F8:
+        raise TypeError(f"{what} must be {_F8}, not {t.dtype}")
+    return _i8_rows(t.view(torch.int8), what)
+
+
+def _blocks_shape(rows: int, cols: int, block_rows: int):
+    if block_rows not in (1, BLOCK_F8):
+        raise ValueError("block_rows must be 1 or 128")
+    nb = -(-cols // BLOCK_F8)
+    return (nb, rows) if block_rows == 1 else (-(-rows // BLOCK_F8), nb)
+
+
+def _check_scales(dev: int, scale: torch.Tensor, shape, what: str) -> None:
+    if scale.get_device() != dev:
+        raise ValueError(f"{what} must be on cuda:{dev}")
+    if scale.shape != shape or scale.dtype != torch.float32 or not scale.is_contiguous():
+        raise ValueError(f"{what}: contiguous fp32 {list(shape)}")
+
+
+def awsrc_quantize_blocks_f8(x: torch.Tensor, block_rows: int = 1, out=None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """e4m3 codes [rows, cols] (torch.float8_e4m3fn) and fp32 scales of a matrix: block_rows 1, a scale for each row and 128
+    columns, [ceil(cols / 128), rows] (activations); 128, one for each block of 128 x 128, [ceil(rows / 128),
+    ceil(cols / 128)] (weights).  The codes' rows lie a multiple of 16 bytes apart, as the products take them."""
+    rows, cols, ld = _rows_of(x, "x")
+    dev = _device_of(x)
+    shape = _blocks_shape(rows, cols, block_rows)
+    if out is None:
+        out = (_empty((rows, -(-cols // 16) * 16), x, _F8, stream)[:, :cols], _empty(shape, x, torch.float32, stream))
+    codes, scale = out
+    _on_device(dev, codes)
+    if codes.shape != x.shape or codes.dtype != _F8:
+        raise ValueError(f"out: codes of x's shape in {_F8}")
+    _check_scales(dev, scale, shape, "scales")
+    _check(LIB.awsrc_quantize_blocks_f8(x.data_ptr(), _act_code(x.dtype), rows, cols, ld, block_rows, codes.data_ptr(),
+                                        _rows_of(codes, "codes")[2], scale.data_ptr(), _raw_stream(dev, stream)))
+    return codes, scale
+
+
+def awsrc_dequantize_blocks_f8(codes: torch.Tensor, scale: torch.Tensor, block_rows: int = 1, dtype: torch.dtype = torch.bfloat16,
+                               out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """The values that codes stand for as a dense matrix of `dtype` (or out's): code * scale, rounded once."""
+    if codes.dtype != _F8:
+        raise TypeError(f"codes must be {_F8}, not {codes.dtype}")
+    rows, cols, ld = _rows_of(codes, "codes")
+    dev = _device_of(codes)
+    _check_scales(dev, scale, _blocks_shape(rows, cols, block_rows), "scales")
+    if out is None:
+        out, ldo = _empty((rows, cols), codes, dtype, stream), cols
+    else:
+        ldo = _out_rows(dev, out, rows, cols)
+    _check(LIB.awsrc_dequantize_blocks_f8(codes.data_ptr(), ld, scale.data_ptr(), rows, cols, block_rows, out.data_ptr(),
+                                          _act_code(out.dtype), ldo, _raw_stream(dev, stream)))
+    return out
+
+
+@functools.lru_cache(_WS_SIZES)
+def matmul_f8_workspace_bytes(M: int, N: int, K: int) -> int:
+    n = ctypes.c_size_t(0)
+    ld = -(-K // 16) * 16
+    _check(LIB.awsrc_matmul_f8(None, ld, None, None, ld, None, None, M, N, K, None, AWSRC_DTYPE_F32, N, None,
+                               ctypes.byref(n), None))
+    return n.value
+
+
+@functools.lru_cache(_WS_SIZES)
+def linear_f8_workspace_bytes(M: int, N: int, K: int) -> int:
+    n = ctypes.c_size_t(0)
+    ld = -(-K // 16) * 16
+    _check(LIB.awsrc_linear_f8(None, AWSRC_DTYPE_F32, K, None, ld, None, None, M, N, K, None, AWSRC_DTYPE_F32, N, None,
+                               ctypes.byref(n), None))
+    return n.value
+
+
+def _check_product_f8(dev: int, N: int, K: int, scale, bias):
+    _check_scales(dev, scale, (-(-N // BLOCK_F8), -(-K // BLOCK_F8)), "weight scales")
+    if bias is not None and (bias.get_device() != dev or bias.shape != (N,) or bias.dtype != torch.float32 or not bias.is_contiguous()):
+        raise ValueError(f"bias: fp32 [N] on cuda:{dev}")
+
+
+def awsrc_matmul_f8(a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor, b_scale: torch.Tensor,
+                    bias: Optional[torch.Tensor] = None, out_dtype: torch.dtype = torch.bfloat16,
+                    out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                    stream=None) -> torch.Tensor:
+    """a [M, K] times b [N, K] transposed, e4m3 codes with fp32 scales as awsrc_quantize_blocks_f8 makes them (a with
+    block_rows 1, b with 128): [M, N] in out_dtype (or out's)."""
+    M, K, lda = _f8_rows(a, "a")
+    N, Kb, ldb = _f8_rows(b, "b")
+    if K != Kb:
+        raise ValueError(f"a has {K} columns, b {Kb}")
+    dev = _device_of(a)
+    _on_device(dev, b)
+    _check_scales(dev, a_scale, (-(-K // BLOCK_F8), M), "a_scale")
+    if out is None:
+        out, ldo = _empty((M, N), a, out_dtype, stream), N
+    else:
+        ldo = _out_rows(dev, out, M, N)
+    _check_product_f8(dev, N, K, b_scale, bias)
+    ws, n, keep = _sized_workspace(workspace, matmul_f8_workspace_bytes(M, N, K), a, stream)
+    if M and N:
+        _check(LIB.awsrc_matmul_f8(a.data_ptr(), lda, a_scale.data_ptr(), b.data_ptr(), ldb, b_scale.data_ptr(),
+                                   None if bias is None else bias.data_ptr(), M, N, K, out.data_ptr(), _act_code(out.dtype),
+                                   ldo, ws, ctypes.c_size_t(n), _raw_stream(dev, stream)))
+    return out
+
+
+def awsrc_linear_f8(x: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                    out_dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None,
+                    workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """A linear layer on e4m3 weights: x [M, K] quantized per row and 128 columns, times w [N, K] (codes and scales as
+    awsrc_quantize_blocks_f8 makes them from the weight matrix with block_rows 128) transposed, plus bias; [M, N] in x's type
+    by default.  For inference: the result carries no gradient."""
+    M, K, ldx = _rows_of(x, "x")
+    N, Kw, ldw = _f8_rows(w, "w")
+    if K != Kw:
+        raise ValueError(f"x has {K} columns, w {Kw}")
+    dev = _device_of(x)
+    if out is None:
+        out, ldo = _empty((M, N), x, x.dtype if out_dtype is None else out_dtype, stream), N
+    else:
+        ldo = _out_rows(dev, out, M, N)
+    _on_device(dev, w)
+    _check_product_f8(dev, N, K, w_scale, bias)
+    ws, n, keep = _sized_workspace(workspace, linear_f8_workspace_bytes(M, N, K), x, stream)
+    if M and N:
+        _check(LIB.awsrc_linear_f8(x.data_ptr(), _act_code(x.dtype), ldx, w.data_ptr(), ldw, w_scale.data_ptr(),
+                                   None if bias is None else bias.data_ptr(), M, N, K, out.data_ptr(), _act_code(out.dtype),
+                                   ldo, ws, ctypes.c_size_t(n), _raw_stream(dev, stream)))
+    return out
+
+
+# ------------------------------------------------------------------ steps with drafted tokens
+PagePool = Tuple[torch.Tensor, torch.Tensor]  # free pages [n_pages], how many of them are free [1], int32
+
+
+def make_page_pool(n_pages: int, device="cuda") -> PagePool:
+    """The pool of a cache of which no page is held yet: (free pages, a stack; their number)."""
+    return (torch.arange(n_pages - 1, -1, -1, dtype=torch.int32, device=device),
+            torch.tensor([n_pages], dtype=torch.int32, device=device))
+
+
+def _ints(t: torch.Tensor, shape, what: str, dev: int) -> int:
+    if t.dtype != torch.int32 or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{what}: contiguous int32 {list(shape)}")
+    if t.get_device() != dev:
+        raise ValueError(f"{what} must be on cuda:{dev}")
+    return t.data_ptr()
+
+
+@functools.lru_cache(_WS_SIZES)
+def kv_plan_workspace_bytes(n_seq: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(LIB.awsrc_kv_plan(awsrc_page_pool(None, None, 1, 16, 0), n_seq, None, None, None, None, 1, 0, None, None, None, None,
+                             None, None, None, ctypes.byref(n), None))
+    return n.value
+
+
+def awsrc_kv_plan(pool: PagePool, kv_len: torch.Tensor, keep: torch.Tensor, new_len: torch.Tensor, page_table: torch.Tensor,
+                  page_tokens: int, rows: int, kv_len_out: Optional[torch.Tensor] = None, n_free_out: Optional[torch.Tensor] = None,
+                  out: Optional[Tuple[torch.Tensor, torch.Tensor, torch.Tensor, torch.Tensor]] = None,
+                  workspace: Optional[torch.Tensor] = None,
+                  stream=None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor, torch.Tensor]:
+    """Plans a step on the device: slot s of the batch holds kv_len[s] cached tokens, keeps the first keep[s] of them and
+    appends new_len[s], of at most `rows` in all.  Pages are given back to the pool and taken from it; page_table, kv_len
+    and the pool's count are brought up to date in place (or written to kv_len_out and n_free_out).  Returns cu [slots + 1],
+    and for each of the `rows` its slot, its position (int32) and page * page_tokens + position % page_tokens (int64), -1
+    past the last.  A slot for which there are no pages gets no rows (cu tells) and keeps its tokens."""
+    free, n_free = pool
+    dev = _device_of(kv_len)
+    n = kv_len.numel()
+    if page_table.dim() != 2 or page_table.shape[0] != n:
+        raise ValueError("page_table [slots, pages]")
+    ld = page_table.shape[1]
+    if free.dim() != 1:
+        raise ValueError("free pages [n_pages]")
+    if out is None:
+        out = (_empty((n + 1,), kv_len, torch.int32, stream), _empty((rows,), kv_len, torch.int32, stream),
+               _empty((rows,), kv_len, torch.int32, stream), _empty((rows,), kv_len, torch.int64, stream))
+    cu, seq, pos, slot = out
+    if slot.dtype != torch.int64 or slot.shape != (rows,) or not slot.is_contiguous() or slot.get_device() != dev:
+        raise ValueError(f"row slots: contiguous int64 [{rows}] on cuda:{dev}")
+    if kv_len_out is None:
+        kv_len_out = kv_len
+    if n_free_out is None:
+        n_free_out = n_free
+    c = awsrc_page_pool(_ints(free, free.shape, "free pages", dev), _ints(n_free, (1,), "number of free pages", dev),
+                        free.shape[0], page_tokens, 0)
+    args = (_ints(kv_len, (n,), "kv_len", dev), _ints(keep, (n,), "keep", dev), _ints(new_len, (n,), "new_len", dev),
+            _ints(page_table, page_table.shape, "page_table", dev), ld, rows, _ints(kv_len_out, (n,), "kv_len_out", dev),
+            _ints(n_free_out, (1,), "n_free_out", dev), _ints(cu, (n + 1,), "cu", dev), _ints(seq, (rows,), "row slots", dev),
+            _ints(pos, (rows,), "row positions", dev), slot.data_ptr())
+    ws, size, held = _sized_workspace(workspace, kv_plan_workspace_bytes(n), kv_len, stream)
+    _check(LIB.awsrc_kv_plan(c, n, *args, ws, ctypes.c_size_t(size), _raw_stream(dev, stream)))
+    return cu, seq, pos, slot
+
+
+@functools.lru_cache(_WS_SIZES)
+def verify_drafts_workspace_bytes(n_seq: int, vocab: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(LIB.awsrc_verify_drafts(None, vocab, None, 0, AWSRC_DTYPE_F32, vocab, n_seq, 0, None, None, None, None, None, None,
+                                   None, None, ctypes.byref(n), None))
+    return n.value
+
+
+def awsrc_verify_drafts(p: torch.Tensor, tokens: torch.Tensor, u: torch.Tensor, cu: torch.Tensor, q: Optional[torch.Tensor] = None,
+                        kv_len: Optional[torch.Tensor] = None, out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None,
+                        keep: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                        stream=None) -> Tuple[torch.Tensor, torch.Tensor, Optional[torch.Tensor]]:
+    """Verifies a step's drafts: tokens [rows] packed by cu, each sequence's last certain token and then its drafts; p
+    [rows, vocab] the target's probabilities of what follows each row, q those that the drafts were drawn from (None:
+    drafts that were not drawn); u [rows] uniform random numbers in [0, 1).  Returns the tokens that follow (int32 [rows],
+    from each sequence's first row on, then -1), how many they are (int32 [sequences]), and, given kv_len, how many cached
+    tokens stay (awsrc_kv_plan's keep), else None."""
+    V = p.shape[1] if p.dim() == 2 else 0
+    rows, _, ldp = _rows_of(p, "p")
+    dev = _device_of(p)
+    q_p = ldq = None
+    if q is not None:
+        if q.shape != p.shape or q.dtype != p.dtype:
+            raise ValueError("q: p's shape and type")
+        _on_device(dev, q)
+        ldq, q_p = _rows_of(q, "q")[2], q.data_ptr()
+    n = cu.numel() - 1
+    if n < 0:
+        raise ValueError("cu [sequences + 1]")
+    if u.dtype != torch.float32 or u.shape != (rows,) or not u.is_contiguous() or u.get_device() != dev:
+        raise ValueError(f"u: contiguous fp32 [{rows}] on cuda:{dev}")
+    if out is None:
+        out = (_empty((rows,), p, torch.int32, stream), _empty((n,), p, torch.int32, stream))
+    kv_p = keep_p = None
+    if kv_len is not None:
+        kv_p = _ints(kv_len, (n,), "kv_len", dev)
+        if keep is None:
+            keep = _empty((n,), p, torch.int32, stream)
+        keep_p = _ints(keep, (n,), "keep", dev)
+    elif keep is not None:
+        raise ValueError("keep without kv_len")
+    args = (_ints(cu, (n + 1,), "cu", dev), _ints(tokens, (rows,), "tokens", dev), u.data_ptr(), kv_p,
+            _ints(out[0], (rows,), "tokens that follow", dev), _ints(out[1], (n,), "numbers of tokens", dev), keep_p)
+    ws, size, held = _sized_workspace(workspace, verify_drafts_workspace_bytes(n, V), p, stream)
+    _check(LIB.awsrc_verify_drafts(p.data_ptr(), ldp, q_p, ldq or 0, _act_code(p.dtype), V, n, rows, *args, ws,
+                                   ctypes.c_size_t(size), _raw_stream(dev, stream)))
+    return out[0], out[1], keep

@@ -18,7 +18,8 @@ LIB = os.path.join(HERE, "libawsrc.so")
 ARCH = "gfx950"
 
 SOURCES = ["abi.cpp", "basis.hip", "backbone.hip", "sdq.hip", "encode.hip", "encode_mfma.hip", "encode_c16.hip", "encode_white.hip", "encode_pe.hip", "encode_perm.hip", "rescore_pe.hip", "rank.hip",
-           "decode.hip", "quant_i8.hip", "linear_i8.hip", "kv_cache.hip", "kv_attention.hip"]
+           "decode.hip", "quant_i8.hip", "linear_i8.hip", "kv_cache.hip", "kv_attention.hip",
+           "quant_f8.hip", "linear_f8.hip", "kv_plan.hip", "verify.hip"]
 
 COMMON = [
     f"--offload-arch={ARCH}", "-O3", "-fPIC", "-std=c++17",
@@ -27,8 +28,8 @@ COMMON = [
     "-fhip-fp32-correctly-rounded-divide-sqrt",
     "-Wall", "-Wno-unused-function",
 ]
-# the backbone, SDQ and int8 recipes are specified without fused multiply-add
-PER_FILE = {f: ["-ffp-contract=off"] for f in ("backbone.hip", "sdq.hip", "quant_i8.hip", "kv_cache.hip")}
+# the backbone, SDQ, int8 and e4m3 recipes are specified without fused multiply-add
+PER_FILE = {f: ["-ffp-contract=off"] for f in ("backbone.hip", "sdq.hip", "quant_i8.hip", "kv_cache.hip", "quant_f8.hip")}
 
 
 def hipcc() -> str:

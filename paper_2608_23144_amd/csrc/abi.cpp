@@ -2,7 +2,8 @@
 // and kernel orchestration.  Every step of the codec itself runs in the HIP
 // kernels of basis.hip, backbone.hip, encode*.hip, rank.hip and decode.hip,
 // the 8-bit serving calls in those of quant_i8.hip, linear_i8.hip,
-// kv_cache.hip and kv_attention.hip.
+// quant_f8.hip, linear_f8.hip, kv_cache.hip, kv_attention.hip, kv_plan.hip and
+// verify.hip.
 #include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
@@ -1304,5 +1305,187 @@ extern "C" awsrc_status awsrc_kv_attention(const awsrc_kv_cache* cache, const vo
   if (need && (!workspace || *ws_bytes < need)) return fail(AWSRC_ENOSPC, "workspace of %zu bytes needed", need);
   if (need && misaligned(workspace, 16)) return fail(AWSRC_EINVAL, "workspace must be 16-byte aligned");
   HIPCHK(launch_kv_attention(a, workspace, (hipStream_t)stream));
+  return AWSRC_OK;
+}
+
+// ---------------------------------------------------------------- e4m3 codes
+namespace {
+
+constexpr int64_t kMaxSumF8 = kMaxLdI8;
+
+awsrc_status check_codes(const uint8_t* codes, int64_t rows, int64_t cols, int64_t ldc, int32_t block_rows, const float* scale) {
+  if (block_rows != 1 && block_rows != kBlockF8) return fail(AWSRC_EINVAL, "block_rows=%d: must be 1 or 128", block_rows);
+  if (rows < 0 || rows >= kMaxDim || cols < 1 || cols >= kMaxDim)
+    return fail(AWSRC_EINVAL, "bad shape %lld x %lld", (long long)rows, (long long)cols);
+  if (ldc < cols || ldc >= kMaxDim) return fail(AWSRC_EINVAL, "ldc=%lld: must be at least cols", (long long)ldc);
+  if (rows && (!codes || !scale)) return fail(AWSRC_EINVAL, "NULL buffer");
+  if (rows && misaligned(scale, 4)) return fail(AWSRC_EINVAL, "scale must be 4-byte aligned");
+  return AWSRC_OK;
+}
+
+awsrc_status check_product_f8(const uint8_t* B, int64_t ldb, const float* b_scale, const float* bias, int64_t M, int64_t N,
+                              int64_t K, const void* out, int32_t out_dtype, int64_t ldo, const size_t* ws_bytes) {
+  if (!act_dtype(out_dtype)) return fail(AWSRC_EINVAL, "bad out_dtype %d", out_dtype);
+  if (M < 0 || N < 0 || M >= kMaxDim || N >= kMaxDim) return fail(AWSRC_EINVAL, "bad shape %lld x %lld", (long long)M, (long long)N);
+  if (K < 1 || K > kMaxSumF8) return fail(AWSRC_EINVAL, "K=%lld out of range 1..%lld", (long long)K, (long long)kMaxSumF8);
+  if (ldb % 16 || ldb < round16(K) || ldb > kMaxLdI8)
+    return fail(AWSRC_EINVAL, "ldb=%lld: must be a multiple of 16, at least K, at most 2^22", (long long)ldb);
+  if (ldo < N || ldo >= kMaxDim) return fail(AWSRC_EINVAL, "ldo=%lld: must be at least N", (long long)ldo);
+  if (B && misaligned(B, 16)) return fail(AWSRC_EINVAL, "e4m3 operands must be 16-byte aligned");
+  if (misaligned(b_scale, 4) || misaligned(bias, 4)) return fail(AWSRC_EINVAL, "scales and bias must be 4-byte aligned");
+  if (out && misaligned(out, act_size(out_dtype))) return fail(AWSRC_EINVAL, "out must be aligned to its type");
+  if (!ws_bytes) return fail(AWSRC_EINVAL, "ws_bytes is NULL");
+  return AWSRC_OK;
+}
+
+awsrc_status check_workspace(const void* workspace, const size_t* ws_bytes, size_t need) {
+  if (need && (!workspace || *ws_bytes < need)) return fail(AWSRC_ENOSPC, "workspace of %zu bytes needed", need);
+  if (need && misaligned(workspace, 16)) return fail(AWSRC_EINVAL, "workspace must be 16-byte aligned");
+  return AWSRC_OK;
+}
+
+awsrc_status run_product_f8(const LinearF8Args& a, char* ws, hipStream_t s) {
+  HIPCHK(launch_matmul_f8(a, ws, s));
+  return AWSRC_OK;
+}
+
+}  // namespace
+
+extern "C" awsrc_status awsrc_quantize_blocks_f8(const void* X, int32_t x_dtype, int64_t rows, int64_t cols, int64_t ldx,
+                                                 int32_t block_rows, uint8_t* codes, int64_t ldc, float* scale, void* stream) {
+  awsrc_status st = check_quantize(X, x_dtype, rows, cols, ldx);
+  if (st != AWSRC_OK) return st;
+  if ((st = check_codes(codes, rows, cols, ldc, block_rows, scale)) != AWSRC_OK) return st;
+  if (rows == 0) return AWSRC_OK;
+  if (!X) return fail(AWSRC_EINVAL, "NULL buffer");
+  HIPCHK(launch_quantize_blocks(X, x_dtype, rows, cols, ldx, block_rows, codes, ldc, scale, (hipStream_t)stream));
+  return AWSRC_OK;
+}
+
+extern "C" awsrc_status awsrc_dequantize_blocks_f8(const uint8_t* codes, int64_t ldc, const float* scale, int64_t rows,
+                                                   int64_t cols, int32_t block_rows, void* out, int32_t out_dtype,
+                                                   int64_t ldo, void* stream) {
+  if (!act_dtype(out_dtype)) return fail(AWSRC_EINVAL, "bad out_dtype %d", out_dtype);
+  awsrc_status st = check_codes(codes, rows, cols, ldc, block_rows, scale);
+  if (st != AWSRC_OK) return st;
+  if (ldo < cols || ldo >= kMaxDim) return fail(AWSRC_EINVAL, "ldo=%lld: must be at least cols", (long long)ldo);
+  if (rows == 0) return AWSRC_OK;
+  if (!out) return fail(AWSRC_EINVAL, "NULL buffer");
+  if (misaligned(out, act_size(out_dtype))) return fail(AWSRC_EINVAL, "out must be aligned to its type");
+  HIPCHK(launch_dequantize_blocks(codes, ldc, scale, rows, cols, block_rows, out, out_dtype, ldo, (hipStream_t)stream));
+  return AWSRC_OK;
+}
+
+extern "C" awsrc_status awsrc_matmul_f8(const uint8_t* A, int64_t lda, const float* a_scale, const uint8_t* B, int64_t ldb,
+                                        const float* b_scale, const float* bias_or_null, int64_t M, int64_t N, int64_t K,
+                                        void* out, int32_t out_dtype, int64_t ldo, void* workspace, size_t* ws_bytes,
+                                        void* stream) {
+  awsrc_status st = check_product_f8(B, ldb, b_scale, bias_or_null, M, N, K, out, out_dtype, ldo, ws_bytes);
+  if (st != AWSRC_OK) return st;
+  if (lda % 16 || lda < round16(K) || lda > kMaxLdI8)
+    return fail(AWSRC_EINVAL, "lda=%lld: must be a multiple of 16, at least K, at most 2^22", (long long)lda);
+  const size_t need = M && N ? matmul_f8_ws_bytes(M, N, K) : 0;
+  if (!workspace && !A && !B && !out) {
+    *ws_bytes = need;
+    return AWSRC_OK;
+  }
+  if (M == 0 || N == 0) return AWSRC_OK;
+  if (!A || !B || !a_scale || !b_scale || !out) return fail(AWSRC_EINVAL, "NULL buffer");
+  if (misaligned(A, 16)) return fail(AWSRC_EINVAL, "e4m3 operands must be 16-byte aligned");
+  if (misaligned(a_scale, 4)) return fail(AWSRC_EINVAL, "scales must be 4-byte aligned");
+  if ((st = check_workspace(workspace, ws_bytes, need)) != AWSRC_OK) return st;
+  const LinearF8Args a{A, lda, a_scale, B, ldb, b_scale, bias_or_null, M, N, K, out, out_dtype, ldo};
+  return run_product_f8(a, static_cast<char*>(workspace), (hipStream_t)stream);
+}
+
+extern "C" awsrc_status awsrc_linear_f8(const void* X, int32_t x_dtype, int64_t ldx, const uint8_t* B, int64_t ldb,
+                                        const float* b_scale, const float* bias_or_null, int64_t M, int64_t N, int64_t K,
+                                        void* out, int32_t out_dtype, int64_t ldo, void* workspace, size_t* ws_bytes,
+                                        void* stream) {
+  awsrc_status st = check_product_f8(B, ldb, b_scale, bias_or_null, M, N, K, out, out_dtype, ldo, ws_bytes);
+  if (st != AWSRC_OK) return st;
+  if ((st = check_quantize(X, x_dtype, M, K, ldx)) != AWSRC_OK) return st;
+  const int64_t blocks = (K + kBlockF8 - 1) / kBlockF8;
+  const size_t b_codes = align_up((size_t)M * (size_t)round16(K), 256), b_scales = align_up((size_t)M * (size_t)blocks * 4, 256);
+  const size_t need = M == 0 || N == 0 ? 0 : b_codes + b_scales + matmul_f8_ws_bytes(M, N, K);
+  if (!workspace && !X && !B && !out) {
+    *ws_bytes = need;
+    return AWSRC_OK;
+  }
+  if (M == 0 || N == 0) return AWSRC_OK;
+  if (!X || !B || !b_scale || !out) return fail(AWSRC_EINVAL, "NULL buffer");
+  if ((st = check_workspace(workspace, ws_bytes, need)) != AWSRC_OK) return st;
+  char* ws = static_cast<char*>(workspace);
+  uint8_t* codes = reinterpret_cast<uint8_t*>(ws);
+  float* scales = reinterpret_cast<float*>(ws + b_codes);
+  hipStream_t s = (hipStream_t)stream;
+  HIPCHK(launch_quantize_blocks(X, x_dtype, M, K, ldx, 1, codes, round16(K), scales, s));
+  const LinearF8Args a{codes, round16(K), scales, B, ldb, b_scale, bias_or_null, M, N, K, out, out_dtype, ldo};
+  return run_product_f8(a, ws + b_codes + b_scales, s);
+}
+
+// ---------------------------------------------------------------- steps with drafted tokens
+extern "C" awsrc_status awsrc_kv_plan(const awsrc_page_pool* pool, int32_t n_seq, const int32_t* kv_len, const int32_t* keep,
+                                      const int32_t* new_len, int32_t* page_table, int64_t table_ld, int64_t max_rows,
+                                      int32_t* kv_len_out, int32_t* n_free_out, int32_t* cu, int32_t* row_seq,
+                                      int32_t* row_pos, int64_t* row_slot, void* workspace, size_t* ws_bytes, void* stream) {
+  if (!pool) return fail(AWSRC_EINVAL, "pool is NULL");
+  if (pool->reserved != 0) return fail(AWSRC_EINVAL, "reserved field must be 0");
+  if (pool->n_pages < 1 || pool->n_pages >= kMaxDim) return fail(AWSRC_EINVAL, "n_pages=%lld out of range", (long long)pool->n_pages);
+  const int32_t P = pool->page_tokens;
+  if (P != 16 && P != 32 && P != 64 && P != 128) return fail(AWSRC_EINVAL, "page_tokens=%d: must be 16, 32, 64 or 128", P);
+  if (n_seq < 0 || n_seq > (1 << 20)) return fail(AWSRC_EINVAL, "n_seq=%d out of range 0..2^20", n_seq);
+  if (table_ld < 1 || table_ld >= kMaxDim / P || table_ld * n_seq >= kMaxDim)
+    return fail(AWSRC_EINVAL, "table_ld=%lld out of range", (long long)table_ld);
+  if (max_rows < 0 || max_rows >= kMaxDim) return fail(AWSRC_EINVAL, "max_rows=%lld out of range", (long long)max_rows);
+  if (!ws_bytes) return fail(AWSRC_EINVAL, "ws_bytes is NULL");
+  const size_t need = kv_plan_ws_bytes(n_seq);
+  if (!workspace && !kv_len && !page_table && !cu) {
+    *ws_bytes = need;
+    return AWSRC_OK;
+  }
+  if (n_seq == 0) return AWSRC_OK;
+  if (!pool->free_pages || !pool->n_free || !kv_len || !keep || !new_len || !page_table || !kv_len_out || !n_free_out || !cu)
+    return fail(AWSRC_EINVAL, "NULL buffer");
+  if (misaligned(pool->free_pages, 4) || misaligned(pool->n_free, 4) || misaligned(kv_len, 4) || misaligned(keep, 4) ||
+      misaligned(new_len, 4) || misaligned(page_table, 4) || misaligned(kv_len_out, 4) || misaligned(n_free_out, 4) ||
+      misaligned(cu, 4) || misaligned(row_seq, 4) || misaligned(row_pos, 4) || misaligned(row_slot, 8))
+    return fail(AWSRC_EINVAL, "buffers must be aligned to their types");
+  const awsrc_status st = check_workspace(workspace, ws_bytes, need);
+  if (st != AWSRC_OK) return st;
+  const PlanArgs a{*pool, n_seq, kv_len, keep, new_len, page_table, table_ld, max_rows, kv_len_out, n_free_out, cu, row_seq, row_pos, row_slot};
+  HIPCHK(launch_kv_plan(a, workspace, (hipStream_t)stream));
+  return AWSRC_OK;
+}
+
+extern "C" awsrc_status awsrc_verify_drafts(const void* p, int64_t ldp, const void* q_or_null, int64_t ldq, int32_t dtype,
+                                            int64_t vocab, int32_t n_seq, int64_t n_rows, const int32_t* cu,
+                                            const int32_t* tokens, const float* u, const int32_t* kv_len_or_null,
+                                            int32_t* tokens_out, int32_t* n_out, int32_t* keep_or_null, void* workspace,
+                                            size_t* ws_bytes, void* stream) {
+  if (!act_dtype(dtype)) return fail(AWSRC_EINVAL, "bad dtype %d", dtype);
+  if (vocab < 1 || vocab >= kMaxDim) return fail(AWSRC_EINVAL, "vocab=%lld out of range", (long long)vocab);
+  if (n_seq < 0 || n_seq > (1 << 24)) return fail(AWSRC_EINVAL, "n_seq=%d out of range", n_seq);
+  if (n_rows < 0 || n_rows >= kMaxDim) return fail(AWSRC_EINVAL, "n_rows=%lld out of range", (long long)n_rows);
+  if (!ws_bytes) return fail(AWSRC_EINVAL, "ws_bytes is NULL");
+  const size_t need = n_seq ? verify_ws_bytes(n_seq, vocab) : 0;
+  if (!workspace && !p && !cu && !tokens_out) {
+    *ws_bytes = need;
+    return AWSRC_OK;
+  }
+  if (!kv_len_or_null != !keep_or_null) return fail(AWSRC_EINVAL, "kv_len and keep go together");
+  if (n_seq == 0) return AWSRC_OK;
+  if (!cu || !n_out || (n_rows && (!tokens || !u || !tokens_out))) return fail(AWSRC_EINVAL, "NULL buffer");
+  if (misaligned(cu, 4) || misaligned(n_out, 4) || misaligned(tokens, 4) || misaligned(u, 4) || misaligned(tokens_out, 4) ||
+      misaligned(kv_len_or_null, 4) || misaligned(keep_or_null, 4))
+    return fail(AWSRC_EINVAL, "int32 and fp32 buffers must be 4-byte aligned");
+  awsrc_status st;
+  if (n_rows && (st = check_rows("p", p, ldp, vocab, dtype)) != AWSRC_OK) return st;
+  if (n_rows && q_or_null && (st = check_rows("q", q_or_null, ldq, vocab, dtype)) != AWSRC_OK) return st;
+  if ((st = check_workspace(workspace, ws_bytes, need)) != AWSRC_OK) return st;
+  VerifyArgs a{};
+  a.p = p; a.q = q_or_null; a.ldp = ldp; a.ldq = ldq; a.dtype = dtype; a.vocab = vocab; a.n_seq = n_seq; a.n_rows = n_rows;
+  a.cu = cu; a.tokens = tokens; a.u = u; a.kv_len = kv_len_or_null; a.tokens_out = tokens_out; a.n_out = n_out; a.keep = keep_or_null;
+  HIPCHK(launch_verify(a, workspace, (hipStream_t)stream));
   return AWSRC_OK;
 }

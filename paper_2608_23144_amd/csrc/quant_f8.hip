@@ -1,0 +1,189 @@
+// Matrices as e4m3 codes with one fp32 scale for each block of 1 x 128 values
+// (activations) or 128 x 128 (weights), and back.
+//
+// Built without FMA contraction: scale, inverse and codes are single fp32
+// operations, so that the codes are the recipe's to the bit.
+#include "serve_internal.h"
+
+namespace awsrc {
+
+namespace {
+
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(1)));
+
+// Eight codes to any byte address, of which n exist.
+__device__ __forceinline__ void store8_codes(uint8_t* __restrict__ c, uint2 w, int64_t n) {
+  if (n >= 8) {
+    *reinterpret_cast<u32x2_any*>(c) = u32x2_any{w.x, w.y};
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < n) c[e] = (uint8_t)((e < 4 ? w.x : w.y) >> (8 * (e & 3)));
+  }
+}
+
+// Blocks of 1 x 128: sixteen lanes a block, eight values each; a wavefront
+// takes 512 columns of RW rows.
+template <typename T, int RW>
+__global__ __launch_bounds__(256) void k_quantize_blocks_row(const T* __restrict__ X, int64_t rows, int64_t cols, int64_t ldx,
+                                                             uint8_t* __restrict__ codes, int64_t ldc,
+                                                             float* __restrict__ scale, uint32_t strips, int64_t n_wg) {
+  constexpr int R = 4 * RW;  // rows of a workgroup
+  __shared__ float s_scale[4][R];
+  const uint32_t wg = workgroup<256>();
+  if (wg >= n_wg) return;
+  const int64_t row0 = (int64_t)(wg / strips) * R;
+  const int64_t strip = wg % strips;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t at = strip * 512 + lane * 8;
+  float v[RW][8];
+#pragma unroll
+  for (int i = 0; i < RW; ++i) {
+    const int64_t row = row0 + wave * RW + i;
+    load8_any(X + (row < rows ? row : rows - 1) * ldx + at, cols - at, v[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < RW; ++i) {
+    const int64_t row = row0 + wave * RW + i;
+    float m = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) m = amax_keep(m, v[i][e]);
+    const float s = scale_of_amax_f8(amax_of_16(m));
+    const uint2 w = codes8_f8(v[i], inverse_scale(s), s > 0.0f);
+    if (row < rows) store8_codes(codes + row * ldc + at, w, cols - at);
+    if ((lane & 15) == 0) s_scale[lane >> 4][wave * RW + i] = s;
+  }
+  __syncthreads();
+  const int64_t blocks = (cols + kBlockF8 - 1) / kBlockF8;
+  for (int i = threadIdx.x; i < 4 * R; i += 256) {
+    const int64_t b = strip * 4 + i / R, row = row0 + i % R;
+    if (b < blocks && row < rows) scale[b * rows + row] = s_scale[i / R][i % R];
+  }
+}
+
+// Blocks of 128 x 128, one a workgroup, held in registers between its largest magnitude and its codes.
+template <typename T>
+__global__ __launch_bounds__(256) void k_quantize_blocks_square(const T* __restrict__ X, int64_t rows, int64_t cols,
+                                                                int64_t ldx, uint8_t* __restrict__ codes, int64_t ldc,
+                                                                float* __restrict__ scale, uint32_t col_blocks, int64_t n_wg) {
+  __shared__ float peak[4];
+  const uint32_t wg = workgroup<256>();
+  if (wg >= n_wg) return;
+  const int64_t rb = wg / col_blocks, cb = wg % col_blocks;
+  const int64_t row0 = rb * kBlockF8 + (threadIdx.x >> 4), at = cb * kBlockF8 + (threadIdx.x & 15) * 8;
+  float v[8][8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int64_t row = row0 + 16 * i;
+    load8_any(X + (row < rows ? row : rows - 1) * ldx + at, cols - at, v[i]);  // (rows past the end count the last one twice)
+  }
+  float m = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) m = amax_keep(m, v[i][e]);
+  m = amax_of_16(m);
+  m = amax_keep(m, __shfl_xor(m, 16, 64));
+  m = amax_keep(m, __shfl_xor(m, 32, 64));
+  if ((threadIdx.x & 63) == 0) peak[threadIdx.x >> 6] = m;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < 4; ++w) m = amax_keep(m, peak[w]);
+  const float s = scale_of_amax_f8(m);
+  const float inv = inverse_scale(s);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int64_t row = row0 + 16 * i;
+    if (row < rows) store8_codes(codes + row * ldc + at, codes8_f8(v[i], inv, s > 0.0f), cols - at);
+  }
+  if (threadIdx.x == 0) scale[wg] = s;
+}
+
+// Values of codes: eight a lane, 512 columns of a row a wavefront.
+template <typename T>
+__global__ __launch_bounds__(256) void k_dequantize_blocks(const uint8_t* __restrict__ codes, int64_t ldc,
+                                                           const float* __restrict__ scale, int64_t rows, int64_t cols,
+                                                           bool square, T* __restrict__ out, int64_t ldo, uint32_t strips,
+                                                           int64_t n_wg) {
+  const uint32_t wg = workgroup<256>();
+  if (wg >= n_wg) return;
+  const int64_t row = (int64_t)(wg / strips) * 4 + (threadIdx.x >> 6);
+  const int64_t at = (int64_t)(wg % strips) * 512 + (threadIdx.x & 63) * 8;
+  if (row >= rows || at >= cols) return;
+  const int64_t blocks = (cols + kBlockF8 - 1) / kBlockF8;
+  const float s = square ? scale[row / kBlockF8 * blocks + at / kBlockF8] : scale[at / kBlockF8 * rows + row];
+  const uint8_t* c = codes + row * ldc + at;
+  T* o = out + row * ldo + at;
+  if (cols - at >= 8) {
+    const u32x2_any w = *reinterpret_cast<const u32x2_any*>(c);
+    float y[8];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const auto a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[i], false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[i], true);
+      y[4 * i] = rounded(a[0] * s);
+      y[4 * i + 1] = rounded(a[1] * s);
+      y[4 * i + 2] = rounded(b[0] * s);
+      y[4 * i + 3] = rounded(b[1] * s);
+    }
+    typedef T V __attribute__((ext_vector_type(16 / sizeof(T)), aligned(sizeof(T))));
+    constexpr int kPer = 16 / sizeof(T);
+#pragma unroll
+    for (int i = 0; i < 8 / kPer; ++i) {
+      V z;
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) z[e] = (T)y[i * kPer + e];
+      *reinterpret_cast<V*>(o + i * kPer) = z;
+    }
+  } else {
+    for (int e = 0; e < cols - at; ++e) o[e] = (T)rounded(__builtin_amdgcn_cvt_f32_fp8((int)c[e], 0) * s);
+  }
+}
+
+template <typename T>
+hipError_t launch(const void* X, int64_t rows, int64_t cols, int64_t ldx, int block_rows, uint8_t* codes, int64_t ldc,
+                  float* scale, hipStream_t st) {
+  const T* x = static_cast<const T*>(X);
+  if (block_rows == 1) {
+    const uint32_t strips = (uint32_t)((cols + 511) / 512);
+    const int64_t n = (rows + 3) / 4 * strips;
+    if (n >= (int64_t)1 << 31) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((k_quantize_blocks_row<T, 1>), grid_of<256>(n), dim3(256), 0, st, x, rows, cols, ldx, codes, ldc, scale,
+                       strips, n);
+  } else {
+    const uint32_t cb = (uint32_t)((cols + kBlockF8 - 1) / kBlockF8);
+    const int64_t n = (rows + kBlockF8 - 1) / kBlockF8 * cb;
+    if (n >= (int64_t)1 << 31) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((k_quantize_blocks_square<T>), grid_of<256>(n), dim3(256), 0, st, x, rows, cols, ldx, codes, ldc, scale,
+                       cb, n);
+  }
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_back(const uint8_t* codes, int64_t ldc, const float* scale, int64_t rows, int64_t cols, int block_rows,
+                       void* out, int64_t ldo, hipStream_t st) {
+  const uint32_t strips = (uint32_t)((cols + 511) / 512);
+  const int64_t n = (rows + 3) / 4 * strips;
+  if (n >= (int64_t)1 << 31) return hipErrorInvalidValue;
+  hipLaunchKernelGGL((k_dequantize_blocks<T>), grid_of<256>(n), dim3(256), 0, st, codes, ldc, scale, rows, cols,
+                     block_rows != 1, static_cast<T*>(out), ldo, strips, n);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_quantize_blocks(const void* X, int x_dtype, int64_t rows, int64_t cols, int64_t ldx, int block_rows,
+                                  uint8_t* codes, int64_t ldc, float* scale, hipStream_t st) {
+  if (x_dtype == AWSRC_DTYPE_F32) return launch<float>(X, rows, cols, ldx, block_rows, codes, ldc, scale, st);
+  if (x_dtype == AWSRC_DTYPE_BF16) return launch<__bf16>(X, rows, cols, ldx, block_rows, codes, ldc, scale, st);
+  return launch<_Float16>(X, rows, cols, ldx, block_rows, codes, ldc, scale, st);
+}
+
+hipError_t launch_dequantize_blocks(const uint8_t* codes, int64_t ldc, const float* scale, int64_t rows, int64_t cols,
+                                    int block_rows, void* out, int out_dtype, int64_t ldo, hipStream_t st) {
+  if (out_dtype == AWSRC_DTYPE_F32) return launch_back<float>(codes, ldc, scale, rows, cols, block_rows, out, ldo, st);
+  if (out_dtype == AWSRC_DTYPE_BF16) return launch_back<__bf16>(codes, ldc, scale, rows, cols, block_rows, out, ldo, st);
+  return launch_back<_Float16>(codes, ldc, scale, rows, cols, block_rows, out, ldo, st);
+}
+
+}  // namespace awsrc

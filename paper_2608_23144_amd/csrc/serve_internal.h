@@ -1,5 +1,6 @@
-// Internal declarations of the 8-bit serving operators (quant_i8.hip,
-// linear_i8.hip, kv_cache.hip, kv_attention.hip; not part of the ABI).
+// Internal declarations of the serving operators (quant_i8.hip, linear_i8.hip,
+// quant_f8.hip, linear_f8.hip, kv_cache.hip, kv_attention.hip, kv_plan.hip,
+// verify.hip; not part of the ABI).
 #pragma once
 
 #include "awsrc_internal.h"
@@ -130,6 +131,115 @@ hipError_t launch_matmul_i8(const LinearArgs& a, void* ws, hipStream_t st);
 // Whether a linear layer of this shape quantizes its rows in the product's kernel, and that kernel (a.A unused).
 bool linear_i8_fused(int64_t M, int64_t N, int64_t K);
 hipError_t launch_linear_i8_fused(const LinearArgs& a, const void* X, int x_dtype, int64_t ldx, hipStream_t st);
+
+// A value that is fp32 before it is rounded to its type.  Without it the compiler takes an operation and the conversion to
+// fp16 after it as one instruction, which does not round in between, in some places and not in others.
+__device__ __forceinline__ float rounded(float y) {
+  asm("" : "+v"(y));
+  return y;
+}
+
+// Columns of a block of e4m3 codes with one scale, and rows of a weight block.
+constexpr int kBlockF8 = 128;
+
+// The e4m3 recipe's scale of a block's largest magnitude, NaN where that is not finite.
+__device__ __forceinline__ float scale_of_amax_f8(float amax) {
+  if (!(amax < __builtin_inff())) return __builtin_nanf("");
+  return amax < kTinyAmax ? 0.0f : amax / 448.0f;
+}
+
+// e4m3 codes of eight values; `live` is false for a block whose scale is 0 or NaN.  No clamp: |x| <= amax gives
+// |x inv| <= 448 (1 + 2^-22), which rounds to 448 (the next border is 464).
+__device__ __forceinline__ uint2 codes8_f8(const float (&v)[8], float inv, bool live) {
+  uint32_t w[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    int x = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * i] * inv, v[4 * i + 1] * inv, 0, false);
+    x = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * i + 2] * inv, v[4 * i + 3] * inv, x, true);
+    w[i] = live ? (uint32_t)x : 0u;
+  }
+  uint2 o;
+  o.x = w[0];
+  o.y = w[1];
+  return o;
+}
+
+// The largest of amax over the 16 lanes of a row of lanes (NaN where one has it).
+__device__ __forceinline__ float amax_of_16(float m) {
+#define AWSRC_ROR(n) m = amax_keep(m, __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, m), 0x120 + n, 0xF, 0xF, true)))
+  AWSRC_ROR(8);
+  AWSRC_ROR(4);
+  AWSRC_ROR(2);
+  AWSRC_ROR(1);
+#undef AWSRC_ROR
+  return m;
+}
+
+// Eight values from x at any alignment (memory takes vectors at any byte), of which n exist (the others are 0).
+template <typename T>
+__device__ __forceinline__ void load8_any(const T* __restrict__ x, int64_t n, float (&v)[8]) {
+  if (n >= 8) {
+    typedef T V __attribute__((ext_vector_type(16 / sizeof(T)), aligned(sizeof(T))));
+    constexpr int kPer = 16 / sizeof(T);
+#pragma unroll
+    for (int i = 0; i < 8 / kPer; ++i) {
+      const V w = *reinterpret_cast<const V*>(x + i * kPer);
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) v[i * kPer + e] = to_f32((T)w[e]);
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = e < n ? to_f32(x[e]) : 0.0f;
+  }
+}
+
+struct LinearF8Args {
+  const uint8_t* A;      // [M][lda] activation codes
+  int64_t lda;
+  const float* a_scale;  // [ceil(K / 128)][M]
+  const uint8_t* B;      // [N][ldb] weight codes
+  int64_t ldb;
+  const float* b_scale;  // [ceil(N / 128)][ceil(K / 128)]
+  const float* bias;     // [N] or NULL
+  int64_t M, N, K;
+  void* out;             // [M][ldo]
+  int out_dtype;
+  int64_t ldo;
+};
+
+hipError_t launch_quantize_blocks(const void* X, int x_dtype, int64_t rows, int64_t cols, int64_t ldx, int block_rows,
+                                  uint8_t* codes, int64_t ldc, float* scale, hipStream_t st);
+hipError_t launch_dequantize_blocks(const uint8_t* codes, int64_t ldc, const float* scale, int64_t rows, int64_t cols,
+                                    int block_rows, void* out, int out_dtype, int64_t ldo, hipStream_t st);
+size_t matmul_f8_ws_bytes(int64_t M, int64_t N, int64_t K);
+hipError_t launch_matmul_f8(const LinearF8Args& a, void* ws, hipStream_t st);
+
+struct PlanArgs {
+  awsrc_page_pool pool;
+  int n_seq;
+  const int32_t *kv_len, *keep, *new_len;
+  int32_t* table;
+  int64_t table_ld, max_rows;
+  int32_t *kv_out, *n_free_out, *cu, *row_seq, *row_pos;
+  int64_t* row_slot;
+};
+size_t kv_plan_ws_bytes(int n_seq);
+hipError_t launch_kv_plan(const PlanArgs& a, void* ws, hipStream_t st);
+
+struct VerifyArgs {
+  const void *p, *q;  // q may be NULL
+  int64_t ldp, ldq;
+  int dtype;
+  int64_t vocab;
+  int n_seq;
+  int64_t n_rows;
+  const int32_t *cu, *tokens;
+  const float* u;
+  const int32_t* kv_len;  // NULL where keep is
+  int32_t *tokens_out, *n_out, *keep;
+};
+size_t verify_ws_bytes(int n_seq, int64_t vocab);
+hipError_t launch_verify(const VerifyArgs& a, void* ws, hipStream_t st);
 
 struct AppendArgs {
   awsrc_kv_cache c;
