@@ -15,6 +15,7 @@
 // lane holds column l % 16 and rows 4 (l / 16) + i.  B (the weights) takes the rows'
 // place and A the columns', so that a lane ends with four consecutive n of one m,
 // and with one scale of A.
+#include <type_traits>
 #include "serve_internal.h"
 
 namespace awsrc {
@@ -96,8 +97,398 @@ __global__ __launch_bounds__(256) void k_matmul_f8(LinearF8Args a, int64_t tiles
   }
 }
 
+// Tiles through LDS, for products with enough rows to fill the matrix cores.
+//
+// A workgroup makes BM rows (m) times BN columns (n) of the result, a
+// wavefront WM x WN of them.  A step is a block of 128 of the sum: two or more LDS
+// stages are filled by direct global-to-LDS loads, the codes and the block's scales of
+// the tile's rows and columns.  A stage's rows of 128 bytes are 8 pieces of 16; piece p
+// of row r lies at place p ^ key(r), and a lane takes pieces g and g + 4 of its row:
+// over 16 lanes (row % 2, key) takes 16 values, which LDS serves without conflict.
+//
+// Rows past the operands' ends, and pieces that are not whole, come from beyond the buffer
+// resource and arrive as zeros.  Where K is no multiple of 16 the rest of the sum, less than
+// a piece, is added at the end straight from memory, zeros past K on both sides (a code
+// there may be NaN).
+//
+// Weight row 4 TN q + 4 t + i of a wavefront's columns is row 4 q + i of its t-th
+// operand, so that a lane ends with 4 TN consecutive columns of one result row.
+constexpr int kStep = kBlockF8;
+
+__device__ __forceinline__ int key_a(int row) { return (row >> 1) & 7; }
+template <int TN>
+__device__ __forceinline__ int key_b(int row) { return ((row >> 1) & 1) | ((row / (4 * TN)) & 3) << 1; }
+
+// A barrier for LDS contents alone: __syncthreads() would also wait for every
+// fill that is still to come.
+__device__ __forceinline__ void sync_lds() {
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
+template <int BM, int BN, int WM, int WN>
+struct TileShape {
+  static constexpr int kWaves = (BM / WM) * (BN / WN);
+  static constexpr int kThreads = 64 * kWaves;
+  static constexpr int kCodes = (BM + BN) * kStep;
+  static constexpr int kStage = kCodes + 4 * kThreads;  // and a scale of each row and column
+  static_assert(BM + BN <= kThreads, "one scale a thread");
+};
+
+// An operand's 32 bytes as the products take them: as they are, or as fp16.
+template <bool FULL>
+struct Operand {
+  i32x8 v;
+  __device__ __forceinline__ void set(i32x4 lo, i32x4 hi) {
+    v = i32x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+  }
+};
+template <>
+struct Operand<true> {
+  h8 v[4];
+  __device__ __forceinline__ void set(i32x4 lo, i32x4 hi) {
+    v[0] = halves(lo[0], lo[1]);
+    v[1] = halves(lo[2], lo[3]);
+    v[2] = halves(hi[0], hi[1]);
+    v[3] = halves(hi[2], hi[3]);
+  }
+};
+__device__ __forceinline__ fl4 sums_of(const Operand<false>& w, const Operand<false>& x) {
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w.v, x.v, fl4{0, 0, 0, 0}, 0, 0, 0, 0, 0, 0);
+}
+__device__ __forceinline__ fl4 sums_of(const Operand<true>& w, const Operand<true>& x) {
+  fl4 p = {0, 0, 0, 0};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) p = __builtin_amdgcn_mfma_f32_16x16x32_f16(w.v[i], x.v[i], p, 0, 0, 0);
+  return p;
+}
+
+template <int BM, int BN, int WM, int WN, int OCC, int NS, bool ONCE, typename TO>
+__global__ __launch_bounds__((TileShape<BM, BN, WM, WN>::kThreads), OCC) void k_matmul_f8_tile(LinearF8Args a, int tiles_m,
+                                                                                               int tiles_n, int split_steps,
+                                                                                               float* parts) {
+  using S = TileShape<BM, BN, WM, WN>;
+  using Op = Operand<sizeof(TO) == 4>;
+  constexpr int TM = WM / 16, TN = WN / 16;
+  constexpr int NA = BM * 8 / S::kThreads, NB = BN * 8 / S::kThreads;  // 16-byte pieces per thread and step
+  constexpr int kRows = S::kThreads / 8;                              // rows that one round of fills covers
+  static_assert(kRows % 16 == 0 && NA >= 1 && NB >= 1, "rounds of fills");
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  typedef __attribute__((address_space(3))) void* lds_ptr;
+
+  // neighbouring tiles on one XCD, in bands of 8 tile rows, share operands in its L2
+  const int total = tiles_m * tiles_n;
+  const int id = (int)xcd_item(blockIdx.x, total);
+  const int band = id / (8 * tiles_n), in = id - band * 8 * tiles_n;
+  const int bm = tiles_m - band * 8 < 8 ? tiles_m - band * 8 : 8;
+  const int64_t m0 = (int64_t)(band * 8 + in % bm) * BM, n0 = (int64_t)(in / bm) * BN;
+
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = (wave % (BM / WM)) * WM, wn = (wave / (BM / WM)) * WN;
+  const int K = (int)a.K, K16 = (K + 15) & ~15;
+
+  // buffer resources from the tile's first rows to the operands' last readable bytes
+  const int64_t ma = a.M - m0, nb = a.N - n0;
+  const int64_t end_a = (ma - 1) * a.lda + K16, end_b = (nb - 1) * a.ldb + K16;
+  const __amdgpu_buffer_rsrc_t ra = __builtin_amdgcn_make_buffer_rsrc(
+      const_cast<uint8_t*>(a.A + m0 * a.lda), 0, (int)(end_a < 0x7FFFFFFF ? end_a : 0x7FFFFFFF), 0x00020000);
+  const __amdgpu_buffer_rsrc_t rb = __builtin_amdgcn_make_buffer_rsrc(
+      const_cast<uint8_t*>(a.B + n0 * a.ldb), 0, (int)(end_b < 0x7FFFFFFF ? end_b : 0x7FFFFFFF), 0x00020000);
+
+  const int all = (K + kStep - 1) / kStep;
+  const int first = (int)blockIdx.y * split_steps;  // this workgroup's steps of the sum
+  const int steps = all - first < split_steps ? all - first : split_steps;
+
+  // fills: thread -> LDS row tid / 8 (+ kRows per round), place tid % 8; and one scale, of row or column tid
+  const int frow = tid >> 3;
+  const int pa = ((tid & 7) ^ key_a(frow)) * 16, pb = ((tid & 7) ^ key_b<TN>(frow)) * 16;
+  const uint32_t oa = (uint32_t)frow * (uint32_t)a.lda + pa, ob = (uint32_t)frow * (uint32_t)a.ldb;
+  const uint32_t sa = kRows * (uint32_t)a.lda, sb = kRows * (uint32_t)a.ldb;
+  const bool of_a = tid < BM;
+  const int64_t sm = m0 + tid < a.M ? m0 + tid : a.M - 1, sn = n0 + tid - BM < a.N ? n0 + tid - BM : a.N - 1;
+  const float* scales = of_a ? a.a_scale + first * a.M + sm : a.b_scale + sn / kBlockF8 * all + first;
+  const int64_t next_scale = of_a ? a.M : 1;
+  const auto fill = [&](int stage, int t) {
+    const int k = t < steps ? (first + t) * kStep : K;
+    char* base = lds + stage * S::kStage;
+    const bool ina = k + pa + 16 <= K;
+#pragma unroll
+    for (int i = 0; i < NA; ++i)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_ptr)(base + wave * 1024 + i * kRows * kStep), 16,
+                                               ina ? (int)(oa + i * sa + k) : (int)0x80000000, 0, 0, 0);
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+      const int p = pb ^ ((i * kRows / (4 * TN)) & 3) << 5;  // the key of the round's rows
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_ptr)(base + wave * 1024 + (BM + i * kRows) * kStep), 16,
+                                               k + p + 16 <= K ? (int)(ob + i * sb + p + k) : (int)0x80000000, 0, 0, ONCE ? 2 : 0);
+    }
+    __builtin_amdgcn_global_load_lds((__attribute__((address_space(1))) void*)scales, (lds_ptr)(base + S::kCodes + wave * 256), 4, 0, 0);
+    if (t + 1 < steps) scales += next_scale;  // (past the last step the last scales again: nothing uses them)
+  };
+  // fragments: lane -> row lane % 16 of the operand, pieces lane / 16 and lane / 16 + 4
+  const int g = lane >> 4, r = lane & 15;
+  const int rb_n = 4 * TN * (r >> 2) + (r & 3);
+  const int qa = (g ^ key_a(r)) * 16, qb = (g ^ key_b<TN>(rb_n)) * 16;
+  const auto read_a = [&](int stage, int j) {
+    const char* p = lds + stage * S::kStage + (wm + 16 * j + r) * kStep;
+    Op x;
+    x.set(*reinterpret_cast<const i32x4*>(p + qa), *reinterpret_cast<const i32x4*>(p + (qa ^ 64)));
+    return x;
+  };
+  const auto read_b = [&](int stage, int i) {
+    const char* p = lds + stage * S::kStage + (BM + wn + rb_n + 4 * i) * kStep;
+    Op w;
+    w.set(*reinterpret_cast<const i32x4*>(p + qb), *reinterpret_cast<const i32x4*>(p + (qb ^ 64)));
+    return w;
+  };
+  const auto scale_a = [&](int stage, int j) {
+    return *reinterpret_cast<const float*>(lds + stage * S::kStage + S::kCodes + (wm + 16 * j + r) * 4);
+  };
+  const auto scale_b = [&](int stage) {
+    return *reinterpret_cast<const float*>(lds + stage * S::kStage + S::kCodes + (BM + wn) * 4);
+  };
+
+  // waits until the oldest fills are in, this wavefront's and then everyone's (LATER fills follow them)
+  const auto arrived = [&](auto later) {
+    constexpr int n = decltype(later)::value * (NA + NB + 1);
+    static_assert(n < 64, "vmcnt");
+    __builtin_amdgcn_s_waitcnt(0x0F70 | (n & 15) | (n >> 4) << 14);  // vmcnt(n)
+    sync_lds();                                                    // (every fragment of the stage that is refilled next is read)
+  };
+
+  fl4 acc[TN][TM];
+#pragma unroll
+  for (int i = 0; i < TN; ++i)
+#pragma unroll
+    for (int j = 0; j < TM; ++j) acc[i][j] = fl4{0, 0, 0, 0};
+
+  // fills past the last step come from beyond the resources: they keep the counts and read nothing
+#pragma unroll
+  for (int t = 0; t < NS; ++t) fill(t, t);
+  arrived(std::integral_constant<int, NS - 1>{});
+  int st = 0;
+  // A phase multiplies one operand of A with all of B's, and adds the sums of the phase before while the matrix cores
+  // work.  The next operand is read at the phase's beginning; the last phase's reads are the next step's.
+  Op w[TN], x = read_a(0, 0);
+#pragma unroll
+  for (int i = 0; i < TN; ++i) w[i] = read_b(0, i);
+  float sb_now = scale_b(0), s = scale_a(0, 0) * sb_now;
+  fl4 p[TN];
+#pragma unroll
+  for (int i = 0; i < TN; ++i) p[i] = fl4{0, 0, 0, 0};
+  float s_was = 0.0f;
+  const auto phase = [&](auto is_last, int j, int next, int t) {
+    constexpr bool kLast = decltype(is_last)::value;
+    constexpr int kPer = sizeof(TO) == 4 ? 4 : 1;  // matrix instructions of a product
+    const int before = j == 0 ? TM - 1 : j - 1;
+    if constexpr (kLast) {
+      arrived(std::integral_constant<int, NS - 2>{});
+      fill(st, t + NS);
+      sb_now = scale_b(next);
+    }
+    const Op y = kLast ? read_a(next, 0) : read_a(st, j + 1);
+    const float s_next = (kLast ? scale_a(next, 0) : scale_a(st, j + 1)) * sb_now;
+#pragma unroll
+    for (int i = 0; i < TN; ++i) {
+      const fl4 q = sums_of(w[i], x);
+      if constexpr (kLast) w[i] = read_b(next, i);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[i][before][e] = __builtin_fmaf(p[i][e], s_was, acc[i][before][e]);
+      p[i] = q;
+    }
+    // the order of a phase: its reads first, B's each after the product that is the last to use the registers
+    __builtin_amdgcn_sched_group_barrier(0x100, kLast ? 4 : 3, 0);  // LDS read
+#pragma unroll
+    for (int i = 0; i < TN; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, kPer, 0);  // MFMA
+      if constexpr (kLast) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+      __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);  // VALU
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    x = y;
+    s_was = s;
+    s = s_next;
+  };
+  for (int t = 0; t < steps; ++t) {
+    const int next = st + 1 == NS ? 0 : st + 1;
+#pragma unroll
+    for (int j = 0; j + 1 < TM; ++j) phase(std::false_type{}, j, next, t);
+    phase(std::true_type{}, TM - 1, next, t);
+    st = next;
+  }
+#pragma unroll
+  for (int i = 0; i < TN; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[i][TM - 1][e] = __builtin_fmaf(p[i][e], s_was, acc[i][TM - 1][e]);
+  __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): no fill outlives the workgroup
+  if (K % 16 && first + steps == all) {
+    const int64_t k = K & ~15;
+    const i32x4 none = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < TN; ++i) {
+      const int64_t n = n0 + wn + rb_n + 4 * i;
+      w[i].set(g == 0 ? piece(a.B + (n < a.N ? n : a.N - 1) * a.ldb + k, K - k) : none, none);
+    }
+    const int64_t nb0 = n0 + wn < a.N ? n0 + wn : a.N - 1;
+    const float sb_last = a.b_scale[nb0 / kBlockF8 * all + all - 1];
+#pragma unroll
+    for (int j = 0; j < TM; ++j) {
+      const int64_t m = m0 + wm + 16 * j + r < a.M ? m0 + wm + 16 * j + r : a.M - 1;
+      x.set(g == 0 ? piece(a.A + m * a.lda + k, K - k) : none, none);
+      s = a.a_scale[(all - 1) * a.M + m] * sb_last;
+#pragma unroll
+      for (int i = 0; i < TN; ++i) {
+        const fl4 q = sums_of(w[i], x);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[i][j][e] = __builtin_fmaf(q[e], s, acc[i][j][e]);
+      }
+    }
+  }
+
+  // results: lane -> row wm + 16 j + r, columns wn + 4 TN g + 4 i + e
+  const int64_t n = n0 + wn + 4 * TN * g;
+  if (parts) {  // a part of the sum, for k_matmul_f8_join
+    float* o = parts + (int64_t)blockIdx.y * a.M * a.N;
+#pragma unroll
+    for (int j = 0; j < TM; ++j) {
+      const int64_t m = m0 + wm + 16 * j + r;
+      if (m >= a.M) continue;
+#pragma unroll
+      for (int i = 0; i < TN; ++i) {
+        if (n + 4 * i + 4 <= a.N && (a.N & 3) == 0) {
+          *reinterpret_cast<fl4*>(o + m * a.N + n + 4 * i) = acc[i][j];
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (n + 4 * i + e < a.N) o[m * a.N + n + 4 * i + e] = acc[i][j][e];
+        }
+      }
+    }
+    return;
+  }
+  float bias[TN][4];
+#pragma unroll
+  for (int i = 0; i < TN; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int64_t nn = n + 4 * i + e;
+      bias[i][e] = a.bias ? a.bias[nn < a.N ? nn : a.N - 1] : 0.0f;
+    }
+  // Results go out through the wavefront's own part of LDS (the stages are done with), so that a store covers whole lines.
+  constexpr int V = 16 / sizeof(TO), kPieces = WN / V;  // values of a piece, pieces of a row
+  constexpr int kMine = NS * S::kStage / S::kWaves / (16 * kPieces * 16);  // m-tiles that the part holds
+  constexpr int G = kMine >= TM ? TM : kMine >= TM / 2 ? TM / 2 : TM / 4;
+  static_assert(G >= 1 && TM % G == 0, "LDS of the results");
+  typedef TO Piece __attribute__((ext_vector_type(16 / sizeof(TO))));
+  char* mine = lds + wave * (G * 16 * kPieces * 16);
+  const bool wide = ((reinterpret_cast<uintptr_t>(a.out) | (uintptr_t)(a.ldo * sizeof(TO))) & 15) == 0;
+  __syncthreads();
+#pragma unroll
+  for (int j0 = 0; j0 < TM; j0 += G) {
+#pragma unroll
+    for (int j = j0; j < j0 + G; ++j) {
+      const int row = 16 * (j - j0) + r;
+#pragma unroll
+      for (int q = 0; q < 4 * TN / V; ++q) {
+        Piece w8;
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          const int c = q * V + e;
+          w8[e] = (TO)rounded(acc[c / 4][j][c % 4] + bias[c / 4][c % 4]);
+        }
+        const int at = 4 * TN / V * g + q;
+        *reinterpret_cast<Piece*>(mine + (row * kPieces + (at ^ ((row >> 1) & (kPieces - 1)))) * 16) = w8;
+      }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    TO* o = static_cast<TO*>(a.out) + (m0 + wm + 16 * j0) * a.ldo + n0 + wn;
+    const int64_t rows_left = a.M - (m0 + wm + 16 * j0), left = a.N - (n0 + wn);
+    if (wide && left >= WN) {
+#pragma unroll
+      for (int q = 0; q < G * 16 * kPieces / 64; ++q) {
+        const int y = q * 64 + lane, row = y / kPieces, at = y % kPieces;
+        const Piece w8 = *reinterpret_cast<const Piece*>(mine + (row * kPieces + (at ^ ((row >> 1) & (kPieces - 1)))) * 16);
+        if (row < rows_left) *reinterpret_cast<Piece*>(o + row * a.ldo + at * V) = w8;
+      }
+    } else {  // rows that do not lie on 16 bytes, or the last columns
+#pragma unroll 4
+      for (int q = 0; q < G * 16 * WN / 64; ++q) {
+        const int y = q * 64 + lane, row = y / WN, col = y % WN;
+        const char* c = mine + (row * kPieces + ((col / V) ^ ((row >> 1) & (kPieces - 1)))) * 16 + col % V * sizeof(TO);
+        if (row < rows_left && col < left) o[row * a.ldo + col] = *reinterpret_cast<const TO*>(c);
+      }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  }
+}
+
+// The parts of split sums together, with the epilogue; four columns a thread.
 template <typename TO>
-hipError_t launch(const LinearF8Args& a, hipStream_t st) {
+__global__ __launch_bounds__(256) void k_matmul_f8_join(LinearF8Args a, const float* __restrict__ parts, int n_parts) {
+  const int64_t quads = (a.N + 3) / 4;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= quads * a.M) return;
+  const int64_t m = i / quads, n = (i - m * quads) * 4;
+  float sum[4] = {0, 0, 0, 0};
+  for (int p = 0; p < n_parts; ++p) {
+    const float* q = parts + ((int64_t)p * a.M + m) * a.N + n;
+    if ((a.N & 3) == 0) {
+      const fl4 v = *reinterpret_cast<const fl4*>(q);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[e] += v[e];
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[e] += n + e < a.N ? q[e] : 0;
+    }
+  }
+  TO* o = static_cast<TO*>(a.out) + m * a.ldo;
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (n + e < a.N) o[n + e] = (TO)rounded(sum[e] + (a.bias ? a.bias[n + e] : 0.0f));
+}
+
+template <int BM, int BN, int WM, int WN, int OCC, int NS, bool ONCE, typename TO>
+hipError_t launch_tile(const LinearF8Args& a, int split, void* ws, hipStream_t st) {
+  using S = TileShape<BM, BN, WM, WN>;
+  const auto k = k_matmul_f8_tile<BM, BN, WM, WN, OCC, NS, ONCE, TO>;
+  const size_t lds = NS * S::kStage;
+  if (lds > 65536) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (e != hipSuccess) return e;
+  }
+  const int64_t tm = (a.M + BM - 1) / BM, tn = (a.N + BN - 1) / BN;
+  if (tm * tn > 0x7FFFFFFF / S::kThreads) return hipErrorInvalidValue;  // (threads of a launch: more than memory holds results for)
+  const int all = (int)((a.K + kStep - 1) / kStep), per = (all + split - 1) / split;
+  split = (all + per - 1) / per;
+  float* parts = split > 1 ? static_cast<float*>(ws) : nullptr;
+  hipLaunchKernelGGL(k, dim3((unsigned)(tm * tn), (unsigned)split), dim3(S::kThreads), lds, st, a, (int)tm, (int)tn, per, parts);
+  if (parts) {
+    const int64_t quads = a.M * ((a.N + 3) / 4);
+    hipLaunchKernelGGL((k_matmul_f8_join<TO>), dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, st, a, parts, split);
+  }
+  return hipGetLastError();
+}
+
+enum Path { kFew, kTile64, kTile128, kTile256 };
+Path choose(int64_t M, int64_t N) {
+  const auto tiles = [&](int64_t bm, int64_t bn) { return ((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
+  if (M <= 32) return kFew;
+  const int64_t t128 = tiles(128, 128), t256 = tiles(256, 256);
+  if (M > 64 && t128 >= 256) return 2.9 * ((t256 + 255) / 256) < t128 / 256.0 + 0.5 ? kTile256 : kTile128;
+  return kTile64;
+}
+
+template <typename TO>
+hipError_t launch(const LinearF8Args& a, void* ws, hipStream_t st) {
+  Path path = choose(a.M, a.N);
+  if (sizeof(TO) == 4 && path == kTile256) path = kTile128;
+  switch (path) {
+    case kFew: break;
+    case kTile64: return launch_tile<64, 64, 32, 32, 2, 4, false, TO>(a, 1, ws, st);
+    case kTile128: return launch_tile<128, 128, 64, 64, 2, 2, false, TO>(a, 1, ws, st);
+    case kTile256:
+      if constexpr (sizeof(TO) == 2) return launch_tile<256, 256, 128, 64, 2, 2, false, TO>(a, 1, ws, st);
+  }
   const int64_t tn = (a.N + 15) / 16, tiles = (a.M + 15) / 16 * tn;
   if (tiles >= (int64_t)1 << 32) return hipErrorInvalidValue;
   hipLaunchKernelGGL((k_matmul_f8<TO>), grid_of<256>((tiles + 3) / 4), dim3(256), 0, st, a, tn, tiles);
@@ -108,10 +499,10 @@ hipError_t launch(const LinearF8Args& a, hipStream_t st) {
 
 size_t matmul_f8_ws_bytes(int64_t, int64_t, int64_t) { return 0; }
 
-hipError_t launch_matmul_f8(const LinearF8Args& a, void*, hipStream_t st) {
-  if (a.out_dtype == AWSRC_DTYPE_F32) return launch<float>(a, st);
-  if (a.out_dtype == AWSRC_DTYPE_BF16) return launch<__bf16>(a, st);
-  return launch<_Float16>(a, st);
+hipError_t launch_matmul_f8(const LinearF8Args& a, void* ws, hipStream_t st) {
+  if (a.out_dtype == AWSRC_DTYPE_F32) return launch<float>(a, ws, st);
+  if (a.out_dtype == AWSRC_DTYPE_BF16) return launch<__bf16>(a, ws, st);
+  return launch<_Float16>(a, ws, st);
 }
 
 }  // namespace awsrc
