@@ -175,6 +175,57 @@ __device__ __forceinline__ float amax_of_16(float m) {
   return m;
 }
 
+// Inclusive sums over a wavefront's lanes, or (ROW) over each 16 of them, of 64-bit values; by moves between lanes' registers.
+template <int CTRL, int ROWS, typename T>
+__device__ __forceinline__ T add_from(T x) {
+  static_assert(sizeof(T) == 8, "64-bit values");
+  const uint64_t b = __builtin_bit_cast(uint64_t, x);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)b, CTRL, ROWS, 0xF, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(b >> 32), CTRL, ROWS, 0xF, false);
+  return x + __builtin_bit_cast(T, (uint64_t)hi << 32 | lo);
+}
+template <typename T>
+__device__ __forceinline__ T scan_row(T x) {
+  x = add_from<0x111, 0xF>(x);  // from the lanes 1, 2, 4 and 8 before, in each row of 16
+  x = add_from<0x112, 0xF>(x);
+  x = add_from<0x114, 0xF>(x);
+  return add_from<0x118, 0xF>(x);
+}
+template <typename T>
+__device__ __forceinline__ T scan_wave(T x) {
+  x = add_from<0x142, 0xA>(scan_row(x));  // the last lane of the row before, into rows 1 and 3
+  return add_from<0x143, 0xC>(x);         // lane 31 into rows 2 and 3
+}
+template <typename T>
+__device__ __forceinline__ T of_lane(T x, int lane) {
+  const uint64_t b = __builtin_bit_cast(uint64_t, x);
+  const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)b, lane), hi = __builtin_amdgcn_readlane((int)(uint32_t)(b >> 32), lane);
+  return __builtin_bit_cast(T, (uint64_t)hi << 32 | lo);
+}
+// Inclusive sums of N values over the threads of a workgroup of W <= 16 wavefronts, in their order; `total` is everyone's.
+// Every thread of the workgroup calls it; sums may be written again after the workgroup's next barrier.
+template <int W, int N, typename T>
+__device__ __forceinline__ void scan_workgroup(T (&x)[N], T (&total)[N], T (*sums)[W]) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll
+  for (int i = 0; i < N; ++i) x[i] = scan_wave(x[i]);
+  if constexpr (W == 1) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) total[i] = of_lane(x[i], 63);
+  } else {
+    if (lane == 63)
+#pragma unroll
+      for (int i = 0; i < N; ++i) sums[i][wave] = x[i];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const T upto = scan_row((lane & 15) < W ? sums[i][lane & 15 & (W - 1)] : T(0));
+      total[i] = of_lane(upto, W - 1);
+      if (wave) x[i] += of_lane(upto, wave - 1);
+    }
+  }
+}
+
 // Eight values from x at any alignment (memory takes vectors at any byte), of which n exist (the others are 0).
 template <typename T>
 __device__ __forceinline__ void load8_any(const T* __restrict__ x, int64_t n, float (&v)[8]) {

@@ -2,11 +2,14 @@
 //
 // Only one row of p (and of q) is read whole for each sequence: the one that
 // its next token is drawn from, known from single entries of the rows before it.  Two
-// launches: sums of the weights over pieces of that row, every workgroup finding
+// launches: sums of the weights over pieces of that row, every wavefront finding
 // the row by itself; then one workgroup a sequence finds the piece in which the running
 // sum passes its mark, and the token in it.  Sums in fp64: a product u q of fp32
 // numbers is exact there, and the order of adding moves a border between tokens
 // by 1e-16 of the whole.
+//
+// Bound by the rows' bytes for a batch, for one sequence by memory's latency: four
+// loads that wait for one another in the first launch, three in the second.
 #include "serve_internal.h"
 
 namespace awsrc {
@@ -14,16 +17,7 @@ namespace awsrc {
 namespace {
 
 constexpr int kThreads = 256;
-template <typename T>
-struct Vec {
-  static constexpr int n = 16 / sizeof(T);
-  typedef T type __attribute__((ext_vector_type(16 / sizeof(T)), aligned(sizeof(T))));
-};
-constexpr int kPiece = 8192;  // tokens of a workgroup's piece of a row
-
-struct Sums {
-  double w, p;  // of the weights, and of the target's probabilities
-};
+constexpr int kPiece = 2048;  // tokens of a piece of a row, 8 of a thread in the second launch
 
 struct Rows {
   int64_t begin, n;  // of a sequence
@@ -57,8 +51,6 @@ __device__ __forceinline__ int64_t place_of(const VerifyArgs& a, Rows rows) {
   return rows.n - 1;
 }
 
-__device__ __forceinline__ double counted(double w) { return w > 0.0 && w < __builtin_inf() ? w : 0.0; }
-
 // The weights that a sequence's token is drawn from.
 template <typename T>
 struct Weights {
@@ -71,111 +63,120 @@ struct Weights {
     q = a.q && cut ? static_cast<const T*>(a.q) + r * a.ldq : nullptr;
     less = !a.q && cut ? a.tokens[r + 1] : -1;
   }
-  // those of the tokens from i on (p's own where `plain`), 0 past the vocabulary
-  __device__ __forceinline__ void load(int64_t i, double (&w)[Vec<T>::n], double (&pp)[Vec<T>::n]) const {
-    constexpr int n = Vec<T>::n;
-    typedef typename Vec<T>::type V;
-    float x[n], y[n];
-    if (i + n <= vocab) {
-      const V u = *reinterpret_cast<const V*>(p + i);
-#pragma unroll
-      for (int e = 0; e < n; ++e) x[e] = to_f32((T)u[e]);
-      if (q) {
-        const V v = *reinterpret_cast<const V*>(q + i);
-#pragma unroll
-        for (int e = 0; e < n; ++e) y[e] = to_f32((T)v[e]);
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < n; ++e) {
-        x[e] = i + e < vocab ? to_f32(p[i + e]) : 0.0f;
-        y[e] = q && i + e < vocab ? to_f32(q[i + e]) : 0.0f;
-      }
-    }
-#pragma unroll
-    for (int e = 0; e < n; ++e) {
-      pp[e] = counted((double)x[e]);
-      w[e] = q ? counted((double)x[e] - (double)y[e]) : i + e == less ? counted((double)x[e] - 1.0) : pp[e];
-    }
+  __device__ __forceinline__ bool plain() const { return !q && less < 0; }
+  // p's own probabilities from here on
+  __device__ __forceinline__ void make_plain() {
+    q = nullptr;
+    less = -1;
+  }
+  __device__ __forceinline__ void load(int64_t i, float (&x)[8], float (&y)[8]) const {
+    load8_any(p + i, vocab - i, x);
+    if (q) load8_any(q + i, vocab - i, y);
+  }
+  // the weight of token i of the values loaded: 0 where one is not finite or the difference not positive, exact otherwise
+  // but for the rounding of a difference to 53 bits
+  __device__ __forceinline__ double of(int64_t i, float x, float y) const {
+    constexpr float inf = __builtin_inff();
+    const float l = q ? y : i == less ? 1.0f : 0.0f;
+    return x > l && x < inf && l > -inf ? (double)x - (double)l : 0.0;
   }
 };
 
-__device__ __forceinline__ double sum_of_wave(double x) {
-#pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) x += __shfl_xor(x, off, 64);
-  return x;
-}
+// 16 bytes of a row from any element on.
+template <typename T>
+struct Vec {
+  static constexpr int n = 16 / sizeof(T);
+  typedef T type __attribute__((ext_vector_type(16 / sizeof(T)), aligned(sizeof(T))));
+};
+
+// A wavefront takes two pieces of 16-bit values, one of fp32 ones (16 loads a lane and row on their way together).
+template <typename T>
+constexpr int kPerWave = sizeof(T) == 2 ? 2 : 1;
 
 template <typename T>
-__global__ __launch_bounds__(kThreads) void k_verify_sums(VerifyArgs a, int pieces, int64_t n_wg, Sums* sums, int32_t* places) {
-  __shared__ int64_t s_place;
-  __shared__ Sums part[kThreads / 64];
+__global__ __launch_bounds__(kThreads) void k_verify_sums(VerifyArgs a, int pieces, uint32_t groups, int64_t n_wg, double* sums,
+                                                          int32_t* places) {
+  typedef typename Vec<T>::type V;
+  constexpr int n = Vec<T>::n, kLoads = kPiece / (64 * n);
   const uint32_t wg = workgroup<kThreads>();
   if (wg >= n_wg) return;
-  const int s = (int)(wg / pieces), piece = (int)(wg % pieces);
+  const int s = (int)(wg / groups), first = ((int)(wg % groups) * (kThreads / 64) + (threadIdx.x >> 6)) * kPerWave<T>;
   const Rows rows = rows_of(a, s);
-  if (rows.n == 0) return;
-  if (threadIdx.x < 64) {
-    const int64_t place = place_of<T>(a, rows);
-    if (threadIdx.x == 0) s_place = place;
-  }
-  __syncthreads();
-  const int64_t place = s_place;
+  if (rows.n == 0 || first >= pieces) return;
+  const int64_t place = place_of<T>(a, rows);
   const Weights<T> weights(a, rows, place);
-  constexpr int n = Vec<T>::n;
-  double w = 0.0, p = 0.0;
-#pragma unroll 4
-  for (int j = 0; j < kPiece / (kThreads * n); ++j) {
-    double wv[n], pv[n];
-    weights.load((int64_t)piece * kPiece + (j * kThreads + threadIdx.x) * n, wv, pv);
+  const int lane = threadIdx.x & 63;
+  double w[kPerWave<T>];
+  if ((int64_t)(first + kPerWave<T>) * kPiece <= a.vocab) {
+    const T* p = weights.p + (int64_t)first * kPiece + lane * n;
+    V x[kPerWave<T>][kLoads], y[kPerWave<T>][kLoads];
 #pragma unroll
-    for (int e = 0; e < n; ++e) {
-      w += wv[e];
-      p += pv[e];
+    for (int k = 0; k < kPerWave<T>; ++k)
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j) x[k][j] = *reinterpret_cast<const V*>(p + k * kPiece + j * 64 * n);
+    if (weights.q) {
+      const T* q = weights.q + (int64_t)first * kPiece + lane * n;
+#pragma unroll
+      for (int k = 0; k < kPerWave<T>; ++k)
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) y[k][j] = *reinterpret_cast<const V*>(q + k * kPiece + j * 64 * n);
+    }
+#pragma unroll
+    for (int k = 0; k < kPerWave<T>; ++k) {
+      w[k] = 0.0;
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j)
+#pragma unroll
+        for (int e = 0; e < n; ++e)
+          w[k] += weights.of((int64_t)(first + k) * kPiece + (j * 64 + lane) * n + e, to_f32((T)x[k][j][e]), to_f32((T)y[k][j][e]));
+    }
+  } else {  // the row ends in here
+#pragma unroll
+    for (int k = 0; k < kPerWave<T>; ++k) {
+      w[k] = 0.0;
+      for (int j = 0; j < kPiece / 512; ++j) {
+        const int64_t at = (int64_t)(first + k) * kPiece + (j * 64 + lane) * 8;
+        float x[8], y[8];
+        weights.load(at, x, y);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[k] += weights.of(at + e, x[e], y[e]);
+      }
     }
   }
-  w = sum_of_wave(w);
-  p = sum_of_wave(p);
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = {w, p};
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    Sums t = part[0];
 #pragma unroll
-    for (int i = 1; i < kThreads / 64; ++i) {
-      t.w += part[i].w;
-      t.p += part[i].p;
-    }
-    sums[wg] = t;
-    if (piece == 0) places[s] = (int32_t)place;
+  for (int k = 0; k < kPerWave<T>; ++k) {
+    w[k] = scan_wave(w[k]);
+    if (lane == 63 && first + k < pieces) sums[(int64_t)s * pieces + first + k] = w[k];
   }
+  if (first == 0 && lane == 0) places[s] = (int32_t)place;
 }
 
-// Inclusive sums over the workgroup's threads, in their order; `total` is everyone's.
-__device__ __forceinline__ double scan(double x, double* wave_sums, double& total) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-  for (int off = 1; off < 64; off <<= 1) {
-    const double y = __shfl_up(x, off, 64);
-    if (lane >= off) x += y;
+__device__ __forceinline__ double scan(double x, double (*wave_sums)[kThreads / 64], double& total) {
+  double v[1] = {x}, t[1];
+  scan_workgroup<kThreads / 64, 1>(v, t, wave_sums);
+  total = t[0];
+  return v[0];
+}
+
+// The first thread whose running sum passes the mark, or else the last one that counts; one LDS operation a wavefront.
+struct Found {
+  int first, last;
+};
+__device__ __forceinline__ void find(Found* f, bool passes, bool counts) {
+  const int wave = threadIdx.x >> 6;
+  const uint64_t p = __ballot(passes), c = __ballot(counts);
+  if ((threadIdx.x & 63) == 0) {
+    if (p) atomicMin(&f->first, 64 * wave + (int)__builtin_ctzll(p));
+    if (c) atomicMax(&f->last, 64 * wave + 63 - (int)__builtin_clzll(c));
   }
-  if (lane == 63) wave_sums[wave] = x;
-  __syncthreads();
-  double before = 0.0;
-  total = 0.0;
-#pragma unroll
-  for (int w = 0; w < kThreads / 64; ++w) {
-    if (w < wave) before += wave_sums[w];
-    total += wave_sums[w];
-  }
-  __syncthreads();
-  return x + before;
 }
 
 template <typename T>
-__global__ __launch_bounds__(kThreads) void k_verify_draw(VerifyArgs a, int pieces, const Sums* sums, const int32_t* places) {
-  __shared__ double wave_sums[kThreads / 64];
-  __shared__ int s_first, s_last;
+__global__ __launch_bounds__(kThreads) void k_verify_draw(VerifyArgs a, int pieces, double* sums, const int32_t* places) {
+  __shared__ double wave_sums[3][kThreads / 64];
+  __shared__ Found found[2];
   __shared__ double s_base;
+  __shared__ int s_token;
   const uint32_t s = workgroup<kThreads>();
   if (s >= (uint32_t)a.n_seq) return;
   const int tid = threadIdx.x;
@@ -183,71 +184,81 @@ __global__ __launch_bounds__(kThreads) void k_verify_draw(VerifyArgs a, int piec
   int64_t place = -1, token = -1;
   if (rows.n > 0) {
     place = places[s];
-    const Weights<T> weights(a, rows, place);
+    const float u = a.u[rows.begin + rows.n - 1];
+    Weights<T> weights(a, rows, place);
     sums += (int64_t)s * pieces;
-    double wt = 0.0, pt = 0.0, total;
-    for (int c = tid; c < pieces; c += kThreads) {
-      wt += sums[c].w;
-      pt += sums[c].p;
-    }
-    scan(wt, wave_sums, wt);
-    scan(pt, wave_sums, pt);
-    const bool plain = !(wt > 0.0);  // nothing of p lies above q: p itself
-    const double mark = (double)a.u[rows.begin + rows.n - 1] * (plain ? pt : wt);
-    if (plain ? pt > 0.0 : true) {
-      // the piece in which the running sum passes the mark, or the last one that counts
-      if (tid == 0) {
-        s_first = 0x7FFFFFFF;
-        s_last = -1;
+    float x[8], y[8];
+    if (tid < 2) found[tid] = {0x7FFFFFFF, -1};
+    if (tid == 0) s_token = -1;
+    double all = 0.0;
+    for (int c = tid; c < pieces; c += kThreads) all += sums[c];
+    scan(all, &wave_sums[0], all);
+    if (!(all > 0.0) && !weights.plain()) {  // nothing of p lies above q: p's own sums, piece by piece
+      weights.make_plain();
+      for (int c = 0; c < pieces; ++c) {
+        const int64_t at = (int64_t)c * kPiece + tid * 8;
+        double w = 0.0, total;
+        weights.load(at, x, y);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w += weights.of(at + e, x[e], y[e]);
+        __syncthreads();
+        scan(w, &wave_sums[0], total);
+        all += total;
+        if (tid == 0) sums[c] = total;
       }
+      __threadfence_block();
       __syncthreads();
+    }
+    if (all > 0.0) {
+      const double mark = (double)u * all;
+      // the piece in which the running sum passes the mark
       double before = 0.0;
+      int piece = -1;
       for (int c0 = 0; c0 < pieces; c0 += kThreads) {
         const int c = c0 + tid;
-        const double x = c < pieces ? (plain ? sums[c].p : sums[c].w) : 0.0;
-        const double upto = before + scan(x, wave_sums, total);
-        if (x > 0.0) {
-          if (upto > mark) atomicMin(&s_first, c);
-          atomicMax(&s_last, c);
+        const double w = c < pieces ? sums[c] : 0.0;
+        double total;
+        const double upto = before + scan(w, &wave_sums[1], total);
+        find(&found[0], w > 0.0 && upto > mark, w > 0.0);
+        __syncthreads();
+        const bool here = found[0].first != 0x7FFFFFFF;
+        if (here || found[0].last >= 0) {
+          const int at = here ? found[0].first : found[0].last;
+          piece = c0 + at;
+          if (tid == at) s_base = upto - w;
         }
         __syncthreads();
-        if (c == s_first || (s_first == 0x7FFFFFFF && c == s_last)) s_base = upto - x;
-        if (s_first != 0x7FFFFFFF) break;
+        if (here) break;
+        if (tid == 0) found[0] = {0x7FFFFFFF, -1};
         before += total;
         __syncthreads();
       }
-      __syncthreads();
-      const int piece = s_first != 0x7FFFFFFF ? s_first : s_last;
+      // the token in it
       before = s_base;
-      __syncthreads();
-      if (tid == 0) {
-        s_first = 0x7FFFFFFF;
-        s_last = -1;
+      const int64_t at = (int64_t)piece * kPiece + tid * 8;
+      double w[8], sum = 0.0, total;
+      weights.load(at, x, y);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        w[e] = weights.of(at + e, x[e], y[e]);
+        sum += w[e];
       }
-      __syncthreads();
-      constexpr int n = Vec<T>::n;
-      for (int j = 0; j < kPiece / (kThreads * n); ++j) {
-        const int at = (j * kThreads + tid) * n;
-        double w[n], p[n], x = 0.0;
-        weights.load((int64_t)piece * kPiece + at, w, p);
-        if (plain)
+      double run = before + (scan(sum, &wave_sums[2], total) - sum);
+      int first = -1, last = -1;
 #pragma unroll
-          for (int e = 0; e < n; ++e) w[e] = p[e];
-#pragma unroll
-        for (int e = 0; e < n; ++e) x += w[e];
-        double run = before + (scan(x, wave_sums, total) - x);
-#pragma unroll
-        for (int e = 0; e < n; ++e) {
-          run += w[e];
-          if (w[e] > 0.0) {
-            if (run > mark) atomicMin(&s_first, at + e);
-            atomicMax(&s_last, at + e);
-          }
+      for (int e = 0; e < 8; ++e) {
+        run += w[e];
+        if (w[e] > 0.0) {
+          if (first < 0 && run > mark) first = e;
+          last = e;
         }
-        before += total;
       }
+      find(&found[1], first >= 0, last >= 0);
       __syncthreads();
-      token = (int64_t)piece * kPiece + (s_first != 0x7FFFFFFF ? s_first : s_last);
+      const bool here = found[1].first != 0x7FFFFFFF;
+      if (tid == (here ? found[1].first : found[1].last)) s_token = (int)(at + (here ? first : last));
+      __syncthreads();
+      token = s_token;
     }
   }
   for (int64_t i = tid; i < rows.n; i += kThreads)
@@ -258,22 +269,25 @@ __global__ __launch_bounds__(kThreads) void k_verify_draw(VerifyArgs a, int piec
   }
 }
 
+template <typename T>
+constexpr int kPieces = kPerWave<T> * kThreads / 64;  // of a workgroup of the first launch
+
 int64_t pieces_of(int64_t vocab) { return (vocab + kPiece - 1) / kPiece; }
 
 template <typename T>
 hipError_t launch(const VerifyArgs& a, void* ws, hipStream_t st) {
-  const int64_t pieces = pieces_of(a.vocab), n = pieces * a.n_seq;
+  const int64_t pieces = pieces_of(a.vocab), groups = (pieces + kPieces<T> - 1) / kPieces<T>, n = groups * a.n_seq;
   if (n >= (int64_t)1 << 31) return hipErrorInvalidValue;
-  Sums* sums = static_cast<Sums*>(ws);
-  int32_t* places = reinterpret_cast<int32_t*>(sums + n);
-  hipLaunchKernelGGL((k_verify_sums<T>), grid_of<kThreads>(n), dim3(kThreads), 0, st, a, (int)pieces, n, sums, places);
+  double* sums = static_cast<double*>(ws);
+  int32_t* places = reinterpret_cast<int32_t*>(sums + pieces * a.n_seq);
+  hipLaunchKernelGGL((k_verify_sums<T>), grid_of<kThreads>(n), dim3(kThreads), 0, st, a, (int)pieces, (uint32_t)groups, n, sums, places);
   hipLaunchKernelGGL((k_verify_draw<T>), grid_of<kThreads>(a.n_seq), dim3(kThreads), 0, st, a, (int)pieces, sums, places);
   return hipGetLastError();
 }
 
 }  // namespace
 
-size_t verify_ws_bytes(int n_seq, int64_t vocab) { return (size_t)n_seq * (pieces_of(vocab) * sizeof(Sums) + 4); }
+size_t verify_ws_bytes(int n_seq, int64_t vocab) { return (size_t)n_seq * (pieces_of(vocab) * sizeof(double) + 4); }
 
 hipError_t launch_verify(const VerifyArgs& a, void* ws, hipStream_t st) {
   if (a.dtype == AWSRC_DTYPE_F32) return launch<float>(a, ws, st);
