@@ -1407,13 +1407,19 @@ extern "C" awsrc_status awsrc_linear_f8(const void* X, int32_t x_dtype, int64_t 
   if ((st = check_quantize(X, x_dtype, M, K, ldx)) != AWSRC_OK) return st;
   const int64_t blocks = (K + kBlockF8 - 1) / kBlockF8;
   const size_t b_codes = align_up((size_t)M * (size_t)round16(K), 256), b_scales = align_up((size_t)M * (size_t)blocks * 4, 256);
-  const size_t need = M == 0 || N == 0 ? 0 : b_codes + b_scales + matmul_f8_ws_bytes(M, N, K);
+  const bool fused = linear_f8_fused(M, N, K);
+  const size_t need = M == 0 || N == 0 || fused ? 0 : b_codes + b_scales + matmul_f8_ws_bytes(M, N, K);
   if (!workspace && !X && !B && !out) {
     *ws_bytes = need;
     return AWSRC_OK;
   }
   if (M == 0 || N == 0) return AWSRC_OK;
   if (!X || !B || !b_scale || !out) return fail(AWSRC_EINVAL, "NULL buffer");
+  if (fused) {
+    const LinearF8Args a{nullptr, 0, nullptr, B, ldb, b_scale, bias_or_null, M, N, K, out, out_dtype, ldo};
+    HIPCHK(launch_linear_f8_fused(a, X, x_dtype, ldx, (hipStream_t)stream));
+    return AWSRC_OK;
+  }
   if ((st = check_workspace(workspace, ws_bytes, need)) != AWSRC_OK) return st;
   char* ws = static_cast<char*>(workspace);
   uint8_t* codes = reinterpret_cast<uint8_t*>(ws);

@@ -34,18 +34,6 @@ __device__ __forceinline__ h8 halves(int lo, int hi) {
             (_Float16)c[0], (_Float16)c[1], (_Float16)d[0], (_Float16)d[1]};
 }
 
-// A block's sums of a 16 x 16 tile, in fp32 throughout where FULL.
-template <bool FULL>
-__device__ __forceinline__ fl4 block_sums(i32x8 w, i32x8 x) {
-  fl4 p = {0, 0, 0, 0};
-  if constexpr (FULL) {
-#pragma unroll
-    for (int i = 0; i < 8; i += 2) p = __builtin_amdgcn_mfma_f32_16x16x32_f16(halves(w[i], w[i + 1]), halves(x[i], x[i + 1]), p, 0, 0, 0);
-    return p;
-  }
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, p, 0, 0, 0, 0, 0, 0);
-}
-
 // 16 bytes of which `left` belong to the sum, zeros past them.
 __device__ __forceinline__ i32x4 piece(const uint8_t* p, int64_t left) {
   i32x4 w = {0, 0, 0, 0};
@@ -58,43 +46,254 @@ __device__ __forceinline__ i32x4 piece(const uint8_t* p, int64_t left) {
   return w;
 }
 
-// A wavefront makes 16 x 16 values straight from memory.
+// An operand's 32 bytes as the products take them: as they are, or as fp16.
+template <bool FULL>
+struct Operand {
+  i32x8 v;
+  __device__ __forceinline__ void set(i32x4 lo, i32x4 hi) {
+    v = i32x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+  }
+};
+template <>
+struct Operand<true> {
+  h8 v[4];
+  __device__ __forceinline__ void set(i32x4 lo, i32x4 hi) {
+    v[0] = halves(lo[0], lo[1]);
+    v[1] = halves(lo[2], lo[3]);
+    v[2] = halves(hi[0], hi[1]);
+    v[3] = halves(hi[2], hi[3]);
+  }
+};
+__device__ __forceinline__ fl4 sums_of(const Operand<false>& w, const Operand<false>& x) {
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w.v, x.v, fl4{0, 0, 0, 0}, 0, 0, 0, 0, 0, 0);
+}
+__device__ __forceinline__ fl4 sums_of(const Operand<true>& w, const Operand<true>& x) {
+  fl4 p = {0, 0, 0, 0};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) p = __builtin_amdgcn_mfma_f32_16x16x32_f16(w.v[i], x.v[i], p, 0, 0, 0);
+  return p;
+}
+
 template <typename TO>
-__global__ __launch_bounds__(256) void k_matmul_f8(LinearF8Args a, int64_t tiles_n, int64_t tiles) {
-  const int64_t tile = (int64_t)workgroup<256>() * 4 + (threadIdx.x >> 6);
-  if (tile >= tiles) return;
-  const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
-  const int64_t m0 = tile / tiles_n * 16, n0 = tile % tiles_n * 16;
-  const int64_t m = m0 + r < a.M ? m0 + r : a.M - 1;  // (rows that do not exist read the last one and are not stored)
-  const uint8_t* pa = a.A + m * a.lda + 32 * g;
-  const uint8_t* pb = a.B + (n0 + r < a.N ? n0 + r : a.N - 1) * a.ldb + 32 * g;
-  const int64_t blocks = (a.K + kBlockF8 - 1) / kBlockF8;
-  const float* sb = a.b_scale + n0 / kBlockF8 * blocks;
-  fl4 acc = {0, 0, 0, 0};
-  for (int64_t b = 0; b < blocks; ++b) {
-    i32x8 w, x;
+__device__ __forceinline__ void store4(TO* o, const float (&y)[4], int64_t n, int64_t N, bool wide) {
+  if (wide && n + 3 < N) {
+    struct alignas(4 * sizeof(TO)) V { TO v[4]; } w;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int64_t left = a.K - (b * kBlockF8 + 32 * g + 16 * h);
-      const i32x4 u = piece(pb + b * kBlockF8 + 16 * h, left), v = piece(pa + b * kBlockF8 + 16 * h, left);
+    for (int i = 0; i < 4; ++i) w.v[i] = (TO)y[i];
+    *reinterpret_cast<V*>(o + n) = w;
+  } else {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        w[4 * h + e] = u[e];
-        x[4 * h + e] = v[e];
+    for (int i = 0; i < 4; ++i)
+      if (n + i < N) o[n + i] = (TO)y[i];
+  }
+}
+
+// Up to 16 rows (or 32: R groups of 16): the weights' bytes are all that counts.  A workgroup takes 16
+// weight rows (columns of the result) against all activation rows, its W
+// wavefronts sharing the sum; the weights come straight from memory, two blocks
+// ahead of the products, and the wavefronts' sums meet in LDS.
+//
+// The matrix cores want a lane to hold 32 bytes of its own row, but a CU's cache
+// takes in a quad of lanes a cycle only where they read 64 bytes side by side.  So
+// lane j of a quad loads piece j of its quad's four rows, and the quad trades them:
+// a lane of group g = lane / 16 ends with 64 bytes of its row, the first half of block 0,
+// of block 1, the second half of block 0 and of block 1 for g = 0 to 3.  Groups 0 and 1, 2 and 3
+// trade halves of those with one instruction a register: 32 bytes of each block.
+struct Quads {
+  static constexpr int kRound = 2 * kBlockF8;  // bytes of a row that a wavefront takes at a time
+  i32x4 v[4];
+  // `row` gives a row's address; the lane loads piece lane % 4 of rows 4 (lane % 16 / 4) + u
+  template <typename F>
+  static __device__ __forceinline__ void pointers(const uint8_t* (&p)[4], int lane, const F& row) {
+    const int g = lane >> 4;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) p[u] = row((lane & 12) + u) + ((g & 1) * kBlockF8 + (g >> 1) * 64) + 16 * (lane & 3);
+  }
+  __device__ __forceinline__ void load(const uint8_t* const (&p)[4], int k) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) v[u] = *reinterpret_cast<const i32x4*>(p[u] + k);
+  }
+  // lane j of a quad gets as v[i] what lane i of it loaded as v[j], then the groups trade
+  template <typename Op>
+  __device__ __forceinline__ void turn(int lane, Op& block0, Op& block1) {
+    const bool odd = lane & 1, high = lane & 2;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      int x[4], y[4];
+#pragma unroll
+      for (int i = 0; i < 4; i += 2) {
+        const int p = __builtin_amdgcn_mov_dpp(v[i + 1][e], 0xB1, 0xF, 0xF, true);  // of lane ^ 1
+        const int q = __builtin_amdgcn_mov_dpp(v[i][e], 0xB1, 0xF, 0xF, true);
+        x[i] = odd ? p : v[i][e];
+        x[i + 1] = odd ? v[i + 1][e] : q;
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int p = __builtin_amdgcn_mov_dpp(x[i + 2], 0x4E, 0xF, 0xF, true);  // of lane ^ 2
+        const int q = __builtin_amdgcn_mov_dpp(x[i], 0x4E, 0xF, 0xF, true);
+        y[i] = high ? p : x[i];
+        y[i + 2] = high ? x[i + 2] : q;
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {  // odd groups' first half against even groups' second half
+        const auto t = __builtin_amdgcn_permlane16_swap((uint32_t)y[i], (uint32_t)y[i + 2], false, false);
+        v[i][e] = (int)t[0];
+        v[i + 2][e] = (int)t[1];
       }
     }
-    const fl4 p = block_sums<sizeof(TO) == 4>(w, x);
-    const float s = a.a_scale[b * a.M + m] * sb[b];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) acc[e] = __builtin_fmaf(p[e], s, acc[e]);
+    block0.set(v[0], v[1]);
+    block1.set(v[2], v[3]);
   }
-  if (m0 + r >= a.M) return;
-  TO* o = static_cast<TO*>(a.out) + m * a.ldo;
+};
+
+template <int W, int R, bool AHEAD, typename TO>
+struct RowSums {
+  using Op = Operand<sizeof(TO) == 4>;
+  const uint8_t* pb[4];      // this lane's pieces of the weights
+  const uint8_t* pa[R][4];   // the same of R groups of 16 rows of activation codes (AHEAD: in memory, fetched with the weights)
+  const uint8_t *rb, *ra[R]; // this lane's own rows
+  const float* sb;           // the weights' scales of this workgroup's columns
+  int K, wave, lane, g;
+  fl4 acc[R];
+  Quads fb[2], fa[2][R];
+
+  // rows that do not exist read the last one: their sums are not stored
+  __device__ __forceinline__ RowSums(const LinearF8Args& a, int64_t n0, int ln, int wv, const uint8_t* A, int64_t lda)
+      : K((int)a.K), wave(wv), lane(ln), g(ln >> 4) {
+    const auto weights = [&](int r) { return a.B + (n0 + r < a.N ? n0 + r : a.N - 1) * a.ldb; };
+    Quads::pointers(pb, ln, weights);
+    rb = weights(ln & 15);
+    sb = a.b_scale + n0 / kBlockF8 * ((a.K + kBlockF8 - 1) / kBlockF8);
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const int64_t n = n0 + 4 * g + e;
-    if (n < a.N) o[n] = (TO)rounded(acc[e] + (a.bias ? a.bias[n] : 0.0f));
+    for (int j = 0; j < R; ++j) {
+      const auto codes = [&](int r) { return A + (16 * j + r < a.M ? 16 * j + r : a.M - 1) * lda; };
+      Quads::pointers(pa[j], ln, codes);
+      ra[j] = codes(ln & 15);
+      acc[j] = fl4{0, 0, 0, 0};
+    }
   }
+  __device__ __forceinline__ void load(int buf, int k) {
+    fb[buf].load(pb, k);
+    if constexpr (AHEAD)
+#pragma unroll
+      for (int j = 0; j < R; ++j) fa[buf][j].load(pa[j], k);
+  }
+  __device__ __forceinline__ int rounds() const { return K / Quads::kRound; }
+  __device__ __forceinline__ void begin() {
+    if (wave < rounds()) load(0, wave * Quads::kRound);
+  }
+  __device__ __forceinline__ void add(int j, const Op& w, const Op& x, float s) {
+    const fl4 p = sums_of(w, x);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[j][e] = __builtin_fmaf(p[e], s, acc[j][e]);
+  }
+  template <typename SA>
+  __device__ __forceinline__ void products(int buf, int k, const SA& sa) {
+    const int b = k / kBlockF8;
+    Op w[2];
+    fb[buf].turn(lane, w[0], w[1]);
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+      Op x[2];
+      if constexpr (AHEAD) {
+        fa[buf][j].turn(lane, x[0], x[1]);
+      } else {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const uint8_t* c = ra[j] + k + h * kBlockF8 + 32 * g;
+          x[h].set(*reinterpret_cast<const i32x4*>(c), *reinterpret_cast<const i32x4*>(c + 16));
+        }
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) add(j, w[h], x[h], sa(b + h, 16 * j + (lane & 15)) * sb[b + h]);
+    }
+  }
+  // sa(b, m): the scale of block b of activation row m (of any row where m is none)
+  template <typename SA>
+  __device__ __forceinline__ void run(const SA& sa) {
+    const int n = rounds();
+    for (int i = wave; i < n; i += 2 * W) {
+      if (i + W < n) load(1, (i + W) * Quads::kRound);
+      products(0, i * Quads::kRound, sa);
+      if (i + W < n) {
+        if (i + 2 * W < n) load(0, (i + 2 * W) * Quads::kRound);
+        products(1, (i + W) * Quads::kRound, sa);
+      }
+    }
+    if (wave == W - 1) {  // the rest of the sum, zeros past K on both sides
+      for (int k = n * Quads::kRound; k < K; k += kBlockF8) {
+        const int at = k + 32 * g, left = K - at;
+        Op w;
+        w.set(piece(rb + at, left), piece(rb + at + 16, left - 16));
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+          Op x;
+          x.set(piece(ra[j] + at, left), piece(ra[j] + at + 16, left - 16));
+          add(j, w, x, sa(k / kBlockF8, 16 * j + (lane & 15)) * sb[k / kBlockF8]);
+        }
+      }
+    }
+  }
+  // the wavefronts' sums together and the results out, group j by wavefront j
+  __device__ __forceinline__ void finish(const LinearF8Args& a, int64_t n0, fl4 (*part)[R][64]) {
+#pragma unroll
+    for (int j = 0; j < R; ++j) part[wave][j][lane] = acc[j];
+    __syncthreads();
+    const int64_t m = 16 * wave + (lane & 15), n = n0 + 4 * g;
+    if (wave >= R || m >= a.M) return;
+    fl4 sum = part[0][wave][lane];
+#pragma unroll
+    for (int w = 1; w < W; ++w) sum += part[w][wave][lane];
+    float y[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int64_t nn = n + e < a.N ? n + e : a.N - 1;
+      y[e] = rounded(sum[e] + (a.bias ? a.bias[nn] : 0.0f));
+    }
+    TO* o = static_cast<TO*>(a.out) + m * a.ldo;
+    store4(o, y, n, a.N, ((reinterpret_cast<uintptr_t>(a.out) | (uintptr_t)(a.ldo * sizeof(TO))) & (4 * sizeof(TO) - 1)) == 0);
+  }
+};
+
+// On activation codes in memory.
+template <int W, int R, typename TO>
+__global__ __launch_bounds__(64 * W) void k_matmul_f8_rows(LinearF8Args a) {
+  __shared__ fl4 part[W][R][64];
+  const int64_t n0 = (int64_t)blockIdx.x * 16;
+  RowSums<W, R, true, TO> sums(a, n0, threadIdx.x & 63, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), a.A, a.lda);
+  sums.begin();
+  sums.run([&](int b, int m) { return a.a_scale[(int64_t)b * a.M + (m < a.M ? m : a.M - 1)]; });
+  sums.finish(a, n0, part);
+}
+
+// On activations: every workgroup quantizes the few rows itself (into LDS, as
+// quant_f8.hip does, sixteen lanes a block), while its first weights are on their way, which saves a
+// launch and its wait.
+template <int W, typename T, typename TO>
+__global__ __launch_bounds__(64 * W) void k_linear_f8_rows(LinearF8Args a, const T* X, int64_t ldx, int pitch) {
+  __shared__ fl4 part[W][1][64];
+  extern __shared__ __attribute__((aligned(16))) uint8_t codes[];  // [M][pitch], then scales [blocks][16]
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t n0 = (int64_t)blockIdx.x * 16;
+  RowSums<W, 1, false, TO> sums(a, n0, lane, wave, codes, pitch);
+  sums.begin();
+  const int M = (int)a.M, K = (int)a.K, blocks = (K + kBlockF8 - 1) / kBlockF8;
+  float* scales = reinterpret_cast<float*>(codes + M * pitch);
+  const int at = (lane & 15) * 8;
+#pragma unroll 4
+  for (int i = threadIdx.x >> 4; i < M * blocks; i += 4 * W) {
+    const int m = i / blocks, b = i - m * blocks, k = b * kBlockF8 + at;
+    float v[8], top = 0.0f;
+    load8_any(X + m * ldx + k, K - k, v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) top = amax_keep(top, v[e]);
+    const float s = scale_of_amax_f8(amax_of_16(top));
+    *reinterpret_cast<uint2*>(codes + m * pitch + k) = codes8_f8(v, inverse_scale(s), s > 0.0f);
+    if (at == 0) scales[b * 16 + m] = s;
+  }
+  __syncthreads();
+  sums.run([&](int b, int m) { return scales[b * 16 + (m < M ? m : M - 1)]; });
+  sums.finish(a, n0, part);
 }
 
 // Tiles through LDS, for products with enough rows to fill the matrix cores.
@@ -133,34 +332,6 @@ struct TileShape {
   static constexpr int kStage = kCodes + 4 * kThreads;  // and a scale of each row and column
   static_assert(BM + BN <= kThreads, "one scale a thread");
 };
-
-// An operand's 32 bytes as the products take them: as they are, or as fp16.
-template <bool FULL>
-struct Operand {
-  i32x8 v;
-  __device__ __forceinline__ void set(i32x4 lo, i32x4 hi) {
-    v = i32x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-  }
-};
-template <>
-struct Operand<true> {
-  h8 v[4];
-  __device__ __forceinline__ void set(i32x4 lo, i32x4 hi) {
-    v[0] = halves(lo[0], lo[1]);
-    v[1] = halves(lo[2], lo[3]);
-    v[2] = halves(hi[0], hi[1]);
-    v[3] = halves(hi[2], hi[3]);
-  }
-};
-__device__ __forceinline__ fl4 sums_of(const Operand<false>& w, const Operand<false>& x) {
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w.v, x.v, fl4{0, 0, 0, 0}, 0, 0, 0, 0, 0, 0);
-}
-__device__ __forceinline__ fl4 sums_of(const Operand<true>& w, const Operand<true>& x) {
-  fl4 p = {0, 0, 0, 0};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) p = __builtin_amdgcn_mfma_f32_16x16x32_f16(w.v[i], x.v[i], p, 0, 0, 0);
-  return p;
-}
 
 template <int BM, int BN, int WM, int WN, int OCC, int NS, bool ONCE, typename TO>
 __global__ __launch_bounds__((TileShape<BM, BN, WM, WN>::kThreads), OCC) void k_matmul_f8_tile(LinearF8Args a, int tiles_m,
@@ -469,40 +640,101 @@ hipError_t launch_tile(const LinearF8Args& a, int split, void* ws, hipStream_t s
   return hipGetLastError();
 }
 
-enum Path { kFew, kTile64, kTile128, kTile256 };
-Path choose(int64_t M, int64_t N) {
+// Bytes between rows of codes in LDS: whole blocks, and 16 more so that rows start in different banks.
+int linear_rows_pitch(int64_t K) { return (int)((K + kBlockF8 - 1) / kBlockF8 * kBlockF8 + 16); }
+size_t linear_rows_lds(int64_t M, int64_t K) {
+  return (size_t)M * linear_rows_pitch(K) + (size_t)((K + kBlockF8 - 1) / kBlockF8) * 64;
+}
+
+template <int W, int R, typename TO>
+hipError_t launch_rows(const LinearF8Args& a, hipStream_t st) {
+  hipLaunchKernelGGL((k_matmul_f8_rows<W, R, TO>), dim3((unsigned)((a.N + 15) / 16)), dim3(64 * W), 0, st, a);
+  return hipGetLastError();
+}
+
+template <int W, typename T, typename TO>
+hipError_t launch_linear_rows(const LinearF8Args& a, const void* X, int64_t ldx, hipStream_t st) {
+  const auto k = k_linear_f8_rows<W, T, TO>;
+  const size_t lds = linear_rows_lds(a.M, a.K);
+  if (lds > 65536) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL(k, dim3((unsigned)((a.N + 15) / 16)), dim3(64 * W), lds, st, a, static_cast<const T*>(X), ldx, linear_rows_pitch(a.K));
+  return hipGetLastError();
+}
+template <int W, typename T>
+hipError_t launch_linear_rows_w(const LinearF8Args& a, const void* X, int64_t ldx, hipStream_t st) {
+  if (a.out_dtype == AWSRC_DTYPE_F32) return launch_linear_rows<W, T, float>(a, X, ldx, st);
+  if (a.out_dtype == AWSRC_DTYPE_BF16) return launch_linear_rows<W, T, __bf16>(a, X, ldx, st);
+  return launch_linear_rows<W, T, _Float16>(a, X, ldx, st);
+}
+template <typename T>
+hipError_t launch_linear_rows_t(const LinearF8Args& a, const void* X, int64_t ldx, hipStream_t st) {
+  return a.M <= 8 ? launch_linear_rows_w<8, T>(a, X, ldx, st) : launch_linear_rows_w<16, T>(a, X, ldx, st);
+}
+
+// Which kernel takes a product, and over how many parts of the sum.
+enum Path { kRows, kTile32, kTile64, kTile64Wide, kTile128, kTile256 };
+struct Choice {
+  Path path;
+  int split;
+};
+Choice choose(int64_t M, int64_t N, int64_t K) {
   const auto tiles = [&](int64_t bm, int64_t bn) { return ((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
-  if (M <= 32) return kFew;
+  if (M <= 16 && N < 12288) return {kRows, 1};
+  if (M > 16 && M <= 32 && N <= 8192 && K <= 16384) return {kRows, 1};
   const int64_t t128 = tiles(128, 128), t256 = tiles(256, 256);
-  if (M > 64 && t128 >= 256) return 2.9 * ((t256 + 255) / 256) < t128 / 256.0 + 0.5 ? kTile256 : kTile128;
-  return kTile64;
+  if (M > 64 && t128 >= 256) return {2.9 * ((t256 + 255) / 256) < t128 / 256.0 + 0.5 ? kTile256 : kTile128, 1};
+  if (M > 32 && tiles(64, 128) >= 192) return {kTile64Wide, 1};
+  const Path path = M > 32 ? kTile64 : kTile32;
+  const int64_t t = path == kTile64 ? tiles(64, 64) : tiles(32, 64);
+  const int64_t want = (256 + t - 1) / t, most = (K + kStep - 1) / kStep / 16;
+  const int64_t split = want < most ? want : most;
+  return {path, t < 128 && split > 1 ? (int)split : 1};
 }
 
 template <typename TO>
 hipError_t launch(const LinearF8Args& a, void* ws, hipStream_t st) {
-  Path path = choose(a.M, a.N);
-  if (sizeof(TO) == 4 && path == kTile256) path = kTile128;
-  switch (path) {
-    case kFew: break;
-    case kTile64: return launch_tile<64, 64, 32, 32, 2, 4, false, TO>(a, 1, ws, st);
-    case kTile128: return launch_tile<128, 128, 64, 64, 2, 2, false, TO>(a, 1, ws, st);
-    case kTile256:
+  const Choice c = choose(a.M, a.N, a.K);
+  const bool once = a.M <= 64 && a.N * a.K >= (int64_t)1 << 26;
+  switch (c.path) {
+    case kRows: return a.M <= 16 ? launch_rows<8, 1, TO>(a, st) : launch_rows<8, 2, TO>(a, st);
+    case kTile32:
+      return once ? launch_tile<32, 64, 32, 32, 2, 4, true, TO>(a, c.split, ws, st)
+                  : launch_tile<32, 64, 32, 32, 2, 4, false, TO>(a, c.split, ws, st);
+    case kTile64: return launch_tile<64, 64, 32, 32, 2, 4, false, TO>(a, c.split, ws, st);
+    case kTile64Wide:
+      return once ? launch_tile<64, 128, 32, 64, 2, 3, true, TO>(a, 1, ws, st)
+                  : launch_tile<64, 128, 32, 64, 2, 3, false, TO>(a, 1, ws, st);
+    case kTile256:  // (of results in fp32 the operands do not fit the registers as fp16)
       if constexpr (sizeof(TO) == 2) return launch_tile<256, 256, 128, 64, 2, 2, false, TO>(a, 1, ws, st);
+    default: return launch_tile<128, 128, 64, 64, 2, 2, false, TO>(a, 1, ws, st);
   }
-  const int64_t tn = (a.N + 15) / 16, tiles = (a.M + 15) / 16 * tn;
-  if (tiles >= (int64_t)1 << 32) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((k_matmul_f8<TO>), grid_of<256>((tiles + 3) / 4), dim3(256), 0, st, a, tn, tiles);
-  return hipGetLastError();
 }
 
 }  // namespace
 
-size_t matmul_f8_ws_bytes(int64_t, int64_t, int64_t) { return 0; }
+size_t matmul_f8_ws_bytes(int64_t M, int64_t N, int64_t K) {
+  const int split = choose(M, N, K).split;
+  return split > 1 ? (size_t)split * (size_t)M * (size_t)N * 4 : 0;
+}
 
 hipError_t launch_matmul_f8(const LinearF8Args& a, void* ws, hipStream_t st) {
   if (a.out_dtype == AWSRC_DTYPE_F32) return launch<float>(a, ws, st);
   if (a.out_dtype == AWSRC_DTYPE_BF16) return launch<__bf16>(a, ws, st);
   return launch<_Float16>(a, ws, st);
+}
+
+bool linear_f8_fused(int64_t M, int64_t N, int64_t K) {
+  const int64_t share = M <= 1 ? 1 : M <= 2 ? 2 : M <= 4 ? 4 : 8;
+  return M <= 16 && K * share <= 16384 && N < 8192;
+}
+
+hipError_t launch_linear_f8_fused(const LinearF8Args& a, const void* X, int x_dtype, int64_t ldx, hipStream_t st) {
+  if (x_dtype == AWSRC_DTYPE_F32) return launch_linear_rows_t<float>(a, X, ldx, st);
+  if (x_dtype == AWSRC_DTYPE_BF16) return launch_linear_rows_t<__bf16>(a, X, ldx, st);
+  return launch_linear_rows_t<_Float16>(a, X, ldx, st);
 }
 
 }  // namespace awsrc

@@ -264,6 +264,9 @@ hipError_t launch_dequantize_blocks(const uint8_t* codes, int64_t ldc, const flo
                                     int block_rows, void* out, int out_dtype, int64_t ldo, hipStream_t st);
 size_t matmul_f8_ws_bytes(int64_t M, int64_t N, int64_t K);
 hipError_t launch_matmul_f8(const LinearF8Args& a, void* ws, hipStream_t st);
+// Whether a linear layer of this shape quantizes its rows in the product's kernel, and that kernel (a.A unused).
+bool linear_f8_fused(int64_t M, int64_t N, int64_t K);
+hipError_t launch_linear_f8_fused(const LinearF8Args& a, const void* X, int x_dtype, int64_t ldx, hipStream_t st);
 
 struct PlanArgs {
   awsrc_page_pool pool;
