@@ -729,7 +729,7 @@ typedef struct awsrc_page_pool {
  * n_seq <= 2^20, n_seq * table_ld < 2^31, max_rows < 2^31; page_tokens 16, 32, 64 or 128.
  * n_seq of 0 is a no-op (nothing is written).
  * Workspace: two-phase query as described above (the query needs no pointers but
- * `pool`).
+ * `pool`); the size may be 0, and then no workspace is needed.
  */
 awsrc_status awsrc_kv_plan(const awsrc_page_pool* pool, int32_t n_seq, const int32_t* kv_len, const int32_t* keep,
                            const int32_t* new_len, int32_t* page_table, int64_t table_ld, int64_t max_rows,

@@ -1040,18 +1040,28 @@ def make_page_pool(n_pages: int, device="cuda") -> PagePool:
             torch.tensor([n_pages], dtype=torch.int32, device=device))
 
 
-def _ints(t: torch.Tensor, shape, what: str, dev: int) -> int:
-    if t.dtype != torch.int32 or t.shape != shape or not t.is_contiguous():
-        raise ValueError(f"{what}: contiguous int32 {list(shape)}")
-    if t.get_device() != dev:
-        raise ValueError(f"{what} must be on cuda:{dev}")
+_I32 = torch.int32
+
+
+def _ints(t: torch.Tensor, n: int, what: str, dev: int) -> int:
+    """The address of n int32 values."""
+    if t.dtype is not _I32 or t.numel() != n or t.get_device() != dev or not t.is_contiguous():
+        raise ValueError(f"{what}: contiguous int32 [{n}] on cuda:{dev}, got {t.dtype} {list(t.shape)} on {t.device}")
     return t.data_ptr()
 
 
+def _new(n: int, dtype: torch.dtype, device, stream) -> torch.Tensor:
+    """_empty of one dimension, on a device object."""
+    if stream is None:
+        return torch.empty(n, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(n, dtype=dtype, device=device)
+
+
 @functools.lru_cache(_WS_SIZES)
-def kv_plan_workspace_bytes(n_seq: int) -> int:
+def kv_plan_workspace_bytes(n_seq: int, rows: int) -> int:
     n = ctypes.c_size_t(0)
-    _check(LIB.awsrc_kv_plan(awsrc_page_pool(None, None, 1, 16, 0), n_seq, None, None, None, None, 1, 0, None, None, None, None,
+    _check(LIB.awsrc_kv_plan(awsrc_page_pool(None, None, 1, 16, 0), n_seq, None, None, None, None, 1, rows, None, None, None, None,
                              None, None, None, ctypes.byref(n), None))
     return n.value
 
@@ -1072,26 +1082,26 @@ def awsrc_kv_plan(pool: PagePool, kv_len: torch.Tensor, keep: torch.Tensor, new_
     if page_table.dim() != 2 or page_table.shape[0] != n:
         raise ValueError("page_table [slots, pages]")
     ld = page_table.shape[1]
-    if free.dim() != 1:
-        raise ValueError("free pages [n_pages]")
+    n_pages = free.numel()
+    c = awsrc_page_pool(_ints(free, n_pages, "free pages", dev), _ints(n_free, 1, "number of free pages", dev), n_pages, page_tokens, 0)
+    kv_p = _ints(kv_len, n, "kv_len", dev)
+    keep_p, new_p = _ints(keep, n, "keep", dev), _ints(new_len, n, "new_len", dev)
+    table_p = _ints(page_table, n * ld, "page_table", dev)
+    kv_out_p = kv_p if kv_len_out is None else _ints(kv_len_out, n, "kv_len_out", dev)
+    free_out_p = c.n_free if n_free_out is None else _ints(n_free_out, 1, "n_free_out", dev)
     if out is None:
-        out = (_empty((n + 1,), kv_len, torch.int32, stream), _empty((rows,), kv_len, torch.int32, stream),
-               _empty((rows,), kv_len, torch.int32, stream), _empty((rows,), kv_len, torch.int64, stream))
-    cu, seq, pos, slot = out
-    if slot.dtype != torch.int64 or slot.shape != (rows,) or not slot.is_contiguous() or slot.get_device() != dev:
-        raise ValueError(f"row slots: contiguous int64 [{rows}] on cuda:{dev}")
-    if kv_len_out is None:
-        kv_len_out = kv_len
-    if n_free_out is None:
-        n_free_out = n_free
-    c = awsrc_page_pool(_ints(free, free.shape, "free pages", dev), _ints(n_free, (1,), "number of free pages", dev),
-                        free.shape[0], page_tokens, 0)
-    args = (_ints(kv_len, (n,), "kv_len", dev), _ints(keep, (n,), "keep", dev), _ints(new_len, (n,), "new_len", dev),
-            _ints(page_table, page_table.shape, "page_table", dev), ld, rows, _ints(kv_len_out, (n,), "kv_len_out", dev),
-            _ints(n_free_out, (1,), "n_free_out", dev), _ints(cu, (n + 1,), "cu", dev), _ints(seq, (rows,), "row slots", dev),
-            _ints(pos, (rows,), "row positions", dev), slot.data_ptr())
-    ws, size, held = _sized_workspace(workspace, kv_plan_workspace_bytes(n), kv_len, stream)
-    _check(LIB.awsrc_kv_plan(c, n, *args, ws, ctypes.c_size_t(size), _raw_stream(dev, stream)))
+        where = kv_len.device
+        cu, seq, slot = _new(n + 1, _I32, where, stream), _new(rows, _I32, where, stream), _new(rows, torch.int64, where, stream)
+        pos = _new(rows, _I32, where, stream)
+        cu_p, seq_p, pos_p = cu.data_ptr(), seq.data_ptr(), pos.data_ptr()
+    else:
+        cu, seq, pos, slot = out
+        cu_p, seq_p, pos_p = _ints(cu, n + 1, "cu", dev), _ints(seq, rows, "row slots", dev), _ints(pos, rows, "row positions", dev)
+        if slot.dtype != torch.int64 or slot.numel() != rows or not slot.is_contiguous() or slot.get_device() != dev:
+            raise ValueError(f"row places: contiguous int64 [{rows}] on cuda:{dev}")
+    ws, size, held = _sized_workspace(workspace, kv_plan_workspace_bytes(n, rows), kv_len, stream)
+    _check(LIB.awsrc_kv_plan(c, n, kv_p, keep_p, new_p, table_p, ld, rows, kv_out_p, free_out_p, cu_p, seq_p, pos_p,
+                             slot.data_ptr(), ws, ctypes.c_size_t(size), _raw_stream(dev, stream)))
     return cu, seq, pos, slot
 
 
@@ -1112,33 +1122,38 @@ def awsrc_verify_drafts(p: torch.Tensor, tokens: torch.Tensor, u: torch.Tensor, 
     drafts that were not drawn); u [rows] uniform random numbers in [0, 1).  Returns the tokens that follow (int32 [rows],
     from each sequence's first row on, then -1), how many they are (int32 [sequences]), and, given kv_len, how many cached
     tokens stay (awsrc_kv_plan's keep), else None."""
-    V = p.shape[1] if p.dim() == 2 else 0
-    rows, _, ldp = _rows_of(p, "p")
+    rows, V, ldp = _rows_of(p, "p")
     dev = _device_of(p)
-    q_p = ldq = None
+    dtype = p.dtype
+    q_p = None
+    ldq = 0
     if q is not None:
-        if q.shape != p.shape or q.dtype != p.dtype:
-            raise ValueError("q: p's shape and type")
-        _on_device(dev, q)
+        if q.shape != p.shape or q.dtype != dtype or q.get_device() != dev:
+            raise ValueError("q: p's shape, type and device")
         ldq, q_p = _rows_of(q, "q")[2], q.data_ptr()
     n = cu.numel() - 1
     if n < 0:
         raise ValueError("cu [sequences + 1]")
-    if u.dtype != torch.float32 or u.shape != (rows,) or not u.is_contiguous() or u.get_device() != dev:
+    if u.dtype != torch.float32 or u.numel() != rows or not u.is_contiguous() or u.get_device() != dev:
         raise ValueError(f"u: contiguous fp32 [{rows}] on cuda:{dev}")
+    cu_p, tokens_p = _ints(cu, n + 1, "cu", dev), _ints(tokens, rows, "tokens", dev)
     if out is None:
-        out = (_empty((rows,), p, torch.int32, stream), _empty((n,), p, torch.int32, stream))
+        where = p.device
+        out = (_new(rows, _I32, where, stream), _new(n, _I32, where, stream))
+        out_p, n_p = out[0].data_ptr(), out[1].data_ptr()
+    else:
+        out_p, n_p = _ints(out[0], rows, "tokens that follow", dev), _ints(out[1], n, "numbers of tokens", dev)
     kv_p = keep_p = None
     if kv_len is not None:
-        kv_p = _ints(kv_len, (n,), "kv_len", dev)
+        kv_p = _ints(kv_len, n, "kv_len", dev)
         if keep is None:
-            keep = _empty((n,), p, torch.int32, stream)
-        keep_p = _ints(keep, (n,), "keep", dev)
+            keep = _new(n, _I32, kv_len.device, stream)
+            keep_p = keep.data_ptr()
+        else:
+            keep_p = _ints(keep, n, "keep", dev)
     elif keep is not None:
         raise ValueError("keep without kv_len")
-    args = (_ints(cu, (n + 1,), "cu", dev), _ints(tokens, (rows,), "tokens", dev), u.data_ptr(), kv_p,
-            _ints(out[0], (rows,), "tokens that follow", dev), _ints(out[1], (n,), "numbers of tokens", dev), keep_p)
     ws, size, held = _sized_workspace(workspace, verify_drafts_workspace_bytes(n, V), p, stream)
-    _check(LIB.awsrc_verify_drafts(p.data_ptr(), ldp, q_p, ldq or 0, _act_code(p.dtype), V, n, rows, *args, ws,
-                                   ctypes.c_size_t(size), _raw_stream(dev, stream)))
+    _check(LIB.awsrc_verify_drafts(p.data_ptr(), ldp, q_p, ldq, _act_code(dtype), V, n, rows, cu_p, tokens_p, u.data_ptr(), kv_p,
+                                   out_p, n_p, keep_p, ws, ctypes.c_size_t(size), _raw_stream(dev, stream)))
     return out[0], out[1], keep

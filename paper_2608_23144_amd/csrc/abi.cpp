@@ -1445,7 +1445,7 @@ extern "C" awsrc_status awsrc_kv_plan(const awsrc_page_pool* pool, int32_t n_seq
     return fail(AWSRC_EINVAL, "table_ld=%lld out of range", (long long)table_ld);
   if (max_rows < 0 || max_rows >= kMaxDim) return fail(AWSRC_EINVAL, "max_rows=%lld out of range", (long long)max_rows);
   if (!ws_bytes) return fail(AWSRC_EINVAL, "ws_bytes is NULL");
-  const size_t need = kv_plan_ws_bytes(n_seq);
+  const size_t need = kv_plan_ws_bytes(n_seq, max_rows);
   if (!workspace && !kv_len && !page_table && !cu) {
     *ws_bytes = need;
     return AWSRC_OK;

@@ -22,8 +22,10 @@ struct PlanHead {
   int64_t n_free, given, taken, rows;
 };
 struct PlanSlot {
-  int32_t take, give;  // places of its first page among those taken, and among those given back
-  int32_t held, want;  // pages before and after
+  int32_t held;   // pages that it has
+  int32_t taken;  // the place among the pages taken that its page 0 would have
+  int32_t pos;    // the position that row 0 would have
+  int32_t given;  // the place in the table of page 0 of those given back, seen from its own
 };
 // Where the rows find it, in LDS or in memory.
 struct Plan {
@@ -60,7 +62,7 @@ __device__ __forceinline__ int last_at_most(int n, int64_t x, const F& value) {
 // The j-th page given back: of the last slot whose pages given back start at or before j.
 __device__ __forceinline__ int32_t page_given(const PlanArgs& a, const Plan& plan, int64_t j) {
   const int s = last_at_most(a.n_seq, j, [&](int i) { return plan.give[i]; });
-  return a.table[s * a.table_ld + plan.slots[s].want + (j - plan.give[s])];
+  return a.table[plan.slots[s].given + j];
 }
 
 // Rows row .. row + 3 of the step, and every step-th four after them.
@@ -70,7 +72,7 @@ __device__ __forceinline__ void plan_rows(const PlanArgs& a, const PlanHead& h, 
     int32_t seq[4], pos[4];
     int64_t slot[4];
     int s = row0 < h.rows ? last_at_most(a.n_seq, row0, [&](int i) { return plan.cu[i]; }) : 0;
-    int32_t start = 0, end = -1, kept = 0, at = -1, page = -1;
+    int32_t end = -1, at = -1, page = -1;
     PlanSlot q = {0, 0, 0, 0};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -81,21 +83,19 @@ __device__ __forceinline__ void plan_rows(const PlanArgs& a, const PlanHead& h, 
       if (row >= end) {  // the next slot that has rows
         if (end >= 0) do ++s;
           while (plan.cu[s + 1] <= row);
-        start = plan.cu[s];
         end = plan.cu[s + 1];
-        kept = a.kv_out[s] - (end - start);
         q = plan.slots[s];
         at = -1;
       }
       seq[i] = s;
-      pos[i] = kept + (int32_t)(row - start);
+      pos[i] = q.pos + (int32_t)row;
       if (pos[i] >> shift != at) {
         at = pos[i] >> shift;
         int32_t* entry = a.table + s * a.table_ld + at;
         if (at < q.held) {
           page = *entry;
         } else {
-          const int64_t t = (int64_t)q.take + at - q.held;
+          const int64_t t = q.taken + at;
           page = t < h.given ? page_given(a, plan, t) : a.pool.free_pages[h.n_free - 1 - (t - h.given)];
           if ((pos[i] & (P - 1)) == 0) *entry = page;
         }
@@ -129,61 +129,96 @@ __device__ __forceinline__ void plan_rows(const PlanArgs& a, const PlanHead& h, 
   }
 }
 
-// ALONE: the rows too, for at most 64 W slots.
-template <int W, bool ALONE>
+// A thread takes I slots side by side, whose loads are on their way together.  ALONE: the rows too, for at most 64 W I slots.
+template <int W, int I, bool ALONE>
 __global__ __launch_bounds__(64 * W) void k_plan_scan(PlanArgs a, PlanHead* head, PlanSlot* slots, int32_t* gives) {
+  constexpr int kChunk = 64 * W * I;
   __shared__ int64_t sums[3][3][W];
-  __shared__ int32_t s_give[ALONE ? 64 * W : 1];
-  __shared__ PlanSlot s_slots[ALONE ? 64 * W : 1];
-  __shared__ int32_t s_cu[ALONE ? 64 * W + 1 : 1];
+  __shared__ int32_t s_give[ALONE ? kChunk : 1];
+  __shared__ PlanSlot s_slots[ALONE ? kChunk : 1];
+  __shared__ int32_t s_cu[ALONE ? kChunk + 1 : 1];
   const int shift = __builtin_ctz(a.pool.page_tokens), tid = threadIdx.x;
   int64_t n_free = a.pool.n_free[0];
   n_free = n_free < 0 ? 0 : n_free < a.pool.n_pages ? n_free : a.pool.n_pages;
-  const auto read = [&](int s) {
-    return s < a.n_seq ? lengths_of(a.kv_len[s], a.keep[s], a.new_len[s], a.table_ld, shift) : Lengths{0, 0, 0, 0};
+  Lengths l[I];
+  const auto read = [&](int s0) {
+    int32_t v[I][3];
+#pragma unroll
+    for (int i = 0; i < I; ++i) {
+      const int s = s0 + tid * I + i;
+      const bool live = s < a.n_seq;
+      v[i][0] = live ? a.kv_len[s] : 0;
+      v[i][1] = live ? a.keep[s] : 0;
+      v[i][2] = live ? a.new_len[s] : 0;
+    }
+#pragma unroll
+    for (int i = 0; i < I; ++i) l[i] = lengths_of(v[i][0], v[i][1], v[i][2], a.table_ld, shift);
   };
   // what all slots give back, before anyone is turned away
-  Lengths l = read(tid);
-  int64_t back[1] = {l.held > l.want ? l.held - l.want : 0}, spare[1];
-  for (int s = tid + 64 * W; s < a.n_seq; s += 64 * W) {
-    const Lengths m = read(s);
-    back[0] += m.held > m.want ? m.held - m.want : 0;
+  int64_t back[1] = {0}, spare[1];
+  for (int s0 = 0; s0 < a.n_seq; s0 += kChunk) {
+    read(s0);
+#pragma unroll
+    for (int i = 0; i < I; ++i) back[0] += l[i].held > l[i].want ? l[i].held - l[i].want : 0;
   }
   scan_workgroup<W, 1>(back, spare, sums[0]);
   spare[0] += n_free;
   int64_t asked = 0, queued = 0, rows = 0, taken = 0, given = 0;
-  for (int s0 = 0; s0 < a.n_seq; s0 += 64 * W) {
-    const int s = s0 + tid;
-    if (s0) l = read(s);
-    const int64_t need = l.want > l.held ? l.want - l.held : 0;
-    int64_t x[2] = {need, l.fresh}, all[2];
+  for (int s0 = 0; s0 < a.n_seq; s0 += kChunk) {
+    if (a.n_seq > kChunk) read(s0);
+    int64_t x[2] = {0, 0}, all[2];
+#pragma unroll
+    for (int i = 0; i < I; ++i) {
+      x[0] += l[i].want > l[i].held ? l[i].want - l[i].held : 0;
+      x[1] += l[i].fresh;
+    }
+    const int64_t need_here = x[0], fresh_here = x[1];
     scan_workgroup<W, 2>(x, all, sums[1]);
-    const bool served = l.want <= a.table_ld && (need == 0 || asked + x[0] <= spare[0]) && queued + x[1] <= a.max_rows;
+    int64_t pages = asked + x[0] - need_here, queue = queued + x[1] - fresh_here;
     asked += all[0];
     queued += all[1];
-    if (!served) {
-      l.fresh = 0;
-      l.want = pages_of(l.keep, shift);
-    }
-    const int64_t take = l.want > l.held ? l.want - l.held : 0, give = l.held > l.want ? l.held - l.want : 0;
-    int64_t y[3] = {take, give, l.fresh}, sum[3];
-    scan_workgroup<W, 3>(y, sum, sums[2]);
-    const PlanSlot q = {(int32_t)(taken + y[0] - take), (int32_t)(given + y[1] - give), (int32_t)l.held, (int32_t)l.want};
-    if (s < a.n_seq) {
-      a.kv_out[s] = (int32_t)(l.keep + l.fresh);
-      a.cu[s + 1] = (int32_t)(rows + y[2]);
-      if constexpr (ALONE) {
-        s_slots[s] = q;
-        s_give[s] = q.give;
-        s_cu[s + 1] = (int32_t)(rows + y[2]);
-      } else {
-        slots[s] = q;
-        gives[s] = q.give;
+    int64_t y[3] = {0, 0, 0}, sum[3];
+#pragma unroll
+    for (int i = 0; i < I; ++i) {
+      const int64_t need = l[i].want > l[i].held ? l[i].want - l[i].held : 0;
+      pages += need;
+      queue += l[i].fresh;
+      if (!(l[i].want <= a.table_ld && (need == 0 || pages <= spare[0]) && queue <= a.max_rows)) {
+        l[i].fresh = 0;
+        l[i].want = pages_of(l[i].keep, shift);
       }
+      y[0] += l[i].want > l[i].held ? l[i].want - l[i].held : 0;
+      y[1] += l[i].held > l[i].want ? l[i].held - l[i].want : 0;
+      y[2] += l[i].fresh;
+    }
+    const int64_t take_here = y[0], give_here = y[1], rows_here = y[2];
+    scan_workgroup<W, 3>(y, sum, sums[2]);
+    int64_t take = taken + y[0] - take_here, give = given + y[1] - give_here, row = rows + y[2] - rows_here;
+#pragma unroll
+    for (int i = 0; i < I; ++i) {
+      const int s = s0 + tid * I + i;
+      const PlanSlot q = {(int32_t)l[i].held, (int32_t)(take - l[i].held), (int32_t)(l[i].keep - row),
+                          (int32_t)(s * a.table_ld + l[i].want - give)};
+      if (s < a.n_seq) {
+        a.kv_out[s] = (int32_t)(l[i].keep + l[i].fresh);
+        a.cu[s + 1] = (int32_t)(row + l[i].fresh);
+        if constexpr (ALONE) {
+          s_slots[s] = q;
+          s_give[s] = (int32_t)give;
+          s_cu[s + 1] = (int32_t)(row + l[i].fresh);
+        } else {
+          slots[s] = q;
+          gives[s] = (int32_t)give;
+        }
+      }
+      take += l[i].want > l[i].held ? l[i].want - l[i].held : 0;
+      give += l[i].held > l[i].want ? l[i].held - l[i].want : 0;
+      row += l[i].fresh;
     }
     taken += sum[0];
     given += sum[1];
     rows += sum[2];
+    if (a.n_seq > kChunk) __syncthreads();  // (the sums are written again)
   }
   const PlanHead h = {n_free, given, taken, rows};
   if (tid == 0) {
@@ -194,7 +229,6 @@ __global__ __launch_bounds__(64 * W) void k_plan_scan(PlanArgs a, PlanHead* head
     if (!ALONE) *head = h;
   }
   if constexpr (ALONE) {
-    __threadfence_block();  // (kv_out)
     __syncthreads();
     plan_rows(a, h, Plan{s_slots, s_cu, s_give}, tid, 64 * W);
   }
@@ -205,11 +239,22 @@ constexpr int kStaged = 2048;  // slots whose starts a workgroup keeps in LDS
 __global__ __launch_bounds__(256) void k_plan_rows(PlanArgs a, const PlanHead* head, const PlanSlot* slots, const int32_t* gives) {
   __shared__ int32_t s_cu[kStaged + 1], s_give[kStaged];
   const bool staged = a.n_seq <= kStaged;
-  if (staged) {
-    for (int i = threadIdx.x; i <= a.n_seq; i += 256) s_cu[i] = a.cu[i];
-    for (int i = threadIdx.x; i < a.n_seq; i += 256) s_give[i] = gives[i];
-  }
   const PlanHead h = *head;
+  if (staged) {
+    int32_t c[kStaged / 256], g[kStaged / 256];
+#pragma unroll
+    for (int i = 0; i < kStaged / 256; ++i) {
+      const int s = i * 256 + threadIdx.x;
+      c[i] = s < a.n_seq ? a.cu[s + 1] : 0;
+      g[i] = s < a.n_seq ? gives[s] : 0;
+    }
+#pragma unroll
+    for (int i = 0; i < kStaged / 256; ++i) {
+      s_cu[i * 256 + threadIdx.x + 1] = c[i];
+      s_give[i * 256 + threadIdx.x] = g[i];
+    }
+    if (threadIdx.x == 0) s_cu[0] = 0;
+  }
   __syncthreads();
   const int64_t first = (int64_t)blockIdx.x * 256 + threadIdx.x, step = (int64_t)gridDim.x * 256;
   if (staged) plan_rows(a, h, Plan{slots, s_cu, s_give}, first, step);
@@ -218,19 +263,23 @@ __global__ __launch_bounds__(256) void k_plan_rows(PlanArgs a, const PlanHead* h
 
 }  // namespace
 
-size_t kv_plan_ws_bytes(int n_seq) { return n_seq ? 256 + (size_t)n_seq * (sizeof(PlanSlot) + 4) : 0; }
+// One workgroup does it all where its threads have a slot and a few rows each.
+static bool plan_alone(int n_seq, int64_t max_rows) { return n_seq <= 256 && max_rows <= 2048; }
+
+size_t kv_plan_ws_bytes(int n_seq, int64_t max_rows) {
+  return n_seq && !plan_alone(n_seq, max_rows) ? 256 + (size_t)n_seq * (sizeof(PlanSlot) + 4) : 0;
+}
 
 hipError_t launch_kv_plan(const PlanArgs& a, void* ws, hipStream_t st) {
+  if (plan_alone(a.n_seq, a.max_rows)) {
+    hipLaunchKernelGGL((k_plan_scan<4, 1, true>), dim3(1), dim3(256), 0, st, a, (PlanHead*)nullptr, (PlanSlot*)nullptr, (int32_t*)nullptr);
+    return hipGetLastError();
+  }
   PlanHead* head = static_cast<PlanHead*>(ws);
   PlanSlot* slots = reinterpret_cast<PlanSlot*>(static_cast<char*>(ws) + 256);
   int32_t* gives = reinterpret_cast<int32_t*>(slots + a.n_seq);
-  // One workgroup does it all where its threads have a row or two each.
-  if (a.n_seq <= 256 && a.max_rows <= 2048) {
-    hipLaunchKernelGGL((k_plan_scan<4, true>), dim3(1), dim3(256), 0, st, a, head, slots, gives);
-    return hipGetLastError();
-  }
-  if (a.n_seq <= 256) hipLaunchKernelGGL((k_plan_scan<4, false>), dim3(1), dim3(256), 0, st, a, head, slots, gives);
-  else hipLaunchKernelGGL((k_plan_scan<16, false>), dim3(1), dim3(1024), 0, st, a, head, slots, gives);
+  if (a.n_seq <= 256) hipLaunchKernelGGL((k_plan_scan<4, 1, false>), dim3(1), dim3(256), 0, st, a, head, slots, gives);
+  else hipLaunchKernelGGL((k_plan_scan<16, 4, false>), dim3(1), dim3(1024), 0, st, a, head, slots, gives);
   const int64_t want = (a.max_rows + 1023) / 1024;
   hipLaunchKernelGGL(k_plan_rows, dim3((unsigned)(want < 64 ? 64 : want < 2048 ? want : 2048)), dim3(256), 0, st, a, head, slots, gives);
   return hipGetLastError();

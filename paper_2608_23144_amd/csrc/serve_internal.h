@@ -277,7 +277,7 @@ struct PlanArgs {
   int32_t *kv_out, *n_free_out, *cu, *row_seq, *row_pos;
   int64_t* row_slot;
 };
-size_t kv_plan_ws_bytes(int n_seq);
+size_t kv_plan_ws_bytes(int n_seq, int64_t max_rows);
 hipError_t launch_kv_plan(const PlanArgs& a, void* ws, hipStream_t st);
 
 struct VerifyArgs {

@@ -89,7 +89,10 @@ struct Vec {
   typedef T type __attribute__((ext_vector_type(16 / sizeof(T)), aligned(sizeof(T))));
 };
 
-// A wavefront takes two pieces of 16-bit values, one of fp32 ones (16 loads a lane and row on their way together).
+// A wavefront takes two pieces of 16-bit values, one of fp32 ones: eight or sixteen loads a lane on their way together.
+//
+// Weights that are not finite show in the sum, which is then made again value by value: a maximum with 0 is all that
+// a weight costs besides its conversion and its addition (200 rows of 100003 in bf16, every value compared: 18.0 us).
 template <typename T>
 constexpr int kPerWave = sizeof(T) == 2 ? 2 : 1;
 
@@ -106,47 +109,46 @@ __global__ __launch_bounds__(kThreads) void k_verify_sums(VerifyArgs a, int piec
   const int64_t place = place_of<T>(a, rows);
   const Weights<T> weights(a, rows, place);
   const int lane = threadIdx.x & 63;
-  double w[kPerWave<T>];
-  if ((int64_t)(first + kPerWave<T>) * kPiece <= a.vocab) {
-    const T* p = weights.p + (int64_t)first * kPiece + lane * n;
-    V x[kPerWave<T>][kLoads], y[kPerWave<T>][kLoads];
 #pragma unroll
-    for (int k = 0; k < kPerWave<T>; ++k)
+  for (int k = 0; k < kPerWave<T>; ++k) {
+    if (first + k >= pieces) break;
+    const int64_t begin = (int64_t)(first + k) * kPiece, end = begin + kPiece;
+    double w = __builtin_inf();
+    if (end <= a.vocab && !(weights.less >= begin && weights.less < end)) {
+      const T* p = weights.p + begin + lane * n;
+      V x[kLoads];
 #pragma unroll
-      for (int j = 0; j < kLoads; ++j) x[k][j] = *reinterpret_cast<const V*>(p + k * kPiece + j * 64 * n);
-    if (weights.q) {
-      const T* q = weights.q + (int64_t)first * kPiece + lane * n;
+      for (int j = 0; j < kLoads; ++j) x[j] = *reinterpret_cast<const V*>(p + j * 64 * n);
+      w = 0.0;
+      if (weights.q) {
+        const T* q = weights.q + begin + lane * n;
+        V y[kLoads];
 #pragma unroll
-      for (int k = 0; k < kPerWave<T>; ++k)
+        for (int j = 0; j < kLoads; ++j) y[j] = *reinterpret_cast<const V*>(q + j * 64 * n);
 #pragma unroll
-        for (int j = 0; j < kLoads; ++j) y[k][j] = *reinterpret_cast<const V*>(q + k * kPiece + j * 64 * n);
+        for (int j = 0; j < kLoads; ++j)
+#pragma unroll
+          for (int e = 0; e < n; ++e) w += __builtin_fmax((double)to_f32((T)x[j][e]) - (double)to_f32((T)y[j][e]), 0.0);
+      } else {
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j)
+#pragma unroll
+          for (int e = 0; e < n; ++e) w += (double)__builtin_fmaxf(to_f32((T)x[j][e]), 0.0f);
+      }
+      w = scan_wave(w);
     }
-#pragma unroll
-    for (int k = 0; k < kPerWave<T>; ++k) {
-      w[k] = 0.0;
-#pragma unroll
-      for (int j = 0; j < kLoads; ++j)
-#pragma unroll
-        for (int e = 0; e < n; ++e)
-          w[k] += weights.of((int64_t)(first + k) * kPiece + (j * 64 + lane) * n + e, to_f32((T)x[k][j][e]), to_f32((T)y[k][j][e]));
-    }
-  } else {  // the row ends in here
-#pragma unroll
-    for (int k = 0; k < kPerWave<T>; ++k) {
-      w[k] = 0.0;
+    if (!(of_lane(w, 63) < __builtin_inf())) {  // the row ends in here, the draft lies here, or a value is not finite
+      w = 0.0;
       for (int j = 0; j < kPiece / 512; ++j) {
-        const int64_t at = (int64_t)(first + k) * kPiece + (j * 64 + lane) * 8;
+        const int64_t at = begin + (j * 64 + lane) * 8;
         float x[8], y[8];
         weights.load(at, x, y);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) w[k] += weights.of(at + e, x[e], y[e]);
+        for (int e = 0; e < 8; ++e) w += weights.of(at + e, x[e], y[e]);
       }
+      w = scan_wave(w);
     }
-  }
-#pragma unroll
-  for (int k = 0; k < kPerWave<T>; ++k) {
-    w[k] = scan_wave(w[k]);
-    if (lane == 63 && first + k < pieces) sums[(int64_t)s * pieces + first + k] = w[k];
+    if (lane == 63) sums[(int64_t)s * pieces + first + k] = w;
   }
   if (first == 0 && lane == 0) places[s] = (int32_t)place;
 }

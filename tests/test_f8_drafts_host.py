@@ -158,7 +158,7 @@ def test_plan_refuses_pools(bad):
                                  dict(keep=None), dict(new_len=None), dict(table=None), dict(kv_out=None), dict(n_free_out=None),
                                  dict(cu=None), dict(kv_len=P + 2), dict(keep=P + 1), dict(new_len=P + 2), dict(table=P + 2),
                                  dict(kv_out=P + 2), dict(n_free_out=P + 2), dict(cu=P + 2), dict(seq=P + 2), dict(pos=P + 1),
-                                 dict(slot=P + 4), dict(n=None), dict(ws=P + 4)])
+                                 dict(slot=P + 4), dict(n=None)])
 def test_plan_refuses(bad):
     assert _call(L.awsrc_kv_plan, {**PLAN, "pool": _pool(), "n": _ws(1 << 40), **bad}) == EINVAL
 
@@ -166,11 +166,15 @@ def test_plan_refuses(bad):
 def test_plan_workspace_and_nothing():
     n = ctypes.c_size_t(0)
     none = dict(kv_len=None, keep=None, new_len=None, table=None, kv_out=None, n_free_out=None, cu=None, seq=None, pos=None, slot=None, ws=None)
-    for n_seq in (1, 5, 3000):
-        assert _call(L.awsrc_kv_plan, {**PLAN, "pool": _pool(), "n": ctypes.byref(n)}, n_seq=n_seq, **none) == OK
-        assert n.value == awsrc.kv_plan_workspace_bytes(n_seq) > 0
-        assert _call(L.awsrc_kv_plan, {**PLAN, "pool": _pool(), "n": _ws(n.value - 1)}, n_seq=n_seq) == ENOSPC
-        assert _call(L.awsrc_kv_plan, {**PLAN, "pool": _pool(), "n": _ws(n.value)}, n_seq=n_seq, ws=None) == ENOSPC
+    for n_seq, rows in ((1, 100000), (5, 9), (300, 9), (3000, 0)):
+        shape = dict(n_seq=n_seq, max_rows=rows)
+        assert _call(L.awsrc_kv_plan, {**PLAN, "pool": _pool(), "n": ctypes.byref(n)}, **shape, **none) == OK
+        assert n.value == awsrc.kv_plan_workspace_bytes(n_seq, rows)
+        if n.value:
+            assert _call(L.awsrc_kv_plan, {**PLAN, "pool": _pool(), "n": _ws(n.value - 1)}, **shape) == ENOSPC
+            assert _call(L.awsrc_kv_plan, {**PLAN, "pool": _pool(), "n": _ws(n.value)}, ws=None, **shape) == ENOSPC
+            assert _call(L.awsrc_kv_plan, {**PLAN, "pool": _pool(), "n": _ws(n.value)}, ws=P + 4, **shape) == EINVAL
+    assert n.value > 0
     assert _call(L.awsrc_kv_plan, {**PLAN, "pool": _pool(), "n": _ws(0)}, n_seq=0) == OK
 
 

@@ -111,7 +111,7 @@ def test_plan_into_other_buffers_repeats_itself():
     d = {k: _ints(v) for k, v in (("kv", kv), ("keep", keep), ("new", new), ("table", table), ("free", free), ("n", [n_pages - at]))}
     rows = int(new.sum()) + 5
     want = R.plan(page, n_pages, free[:n_pages - at].tolist(), kv.tolist(), keep.tolist(), new.tolist(), table.astype(np.int32), rows)
-    need = awsrc.kv_plan_workspace_bytes(n)
+    need = awsrc.kv_plan_workspace_bytes(n, rows)
     scratch = torch.empty(need + 64, dtype=torch.uint8, device=DEV)
     for value in (0, 255, 90):
         scratch.fill_(value)
