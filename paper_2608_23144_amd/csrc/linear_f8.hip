@@ -280,7 +280,6 @@ __global__ __launch_bounds__(64 * W) void k_linear_f8_rows(LinearF8Args a, const
   const int M = (int)a.M, K = (int)a.K, blocks = (K + kBlockF8 - 1) / kBlockF8;
   float* scales = reinterpret_cast<float*>(codes + M * pitch);
   const int at = (lane & 15) * 8;
-#pragma unroll 4
   for (int i = threadIdx.x >> 4; i < M * blocks; i += 4 * W) {
     const int m = i / blocks, b = i - m * blocks, k = b * kBlockF8 + at;
     float v[8], top = 0.0f;
@@ -324,6 +323,22 @@ __device__ __forceinline__ void sync_lds() {
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
+// An operand from a row on: the bytes up to its last readable one, as a buffer resource takes them; none past its rows.
+struct Bytes {
+  uint8_t* base;
+  int size;
+};
+__device__ __forceinline__ Bytes bytes_from(const uint8_t* base, int64_t row, int64_t rows, int64_t ld, int cols) {
+  const int64_t end = row < rows ? (rows - row - 1) * ld + cols : 0;
+  return {const_cast<uint8_t*>(base + (row < rows ? row : 0) * ld), (int)(end < 0x7FFFFFFF ? end : 0x7FFFFFFF)};
+}
+// 16 bytes a lane from there to LDS, zeros past the end; ONCE: past the caches.
+template <bool ONCE>
+__device__ __forceinline__ void fill16(const Bytes& b, char* lds, int at) {
+  const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(b.base, 0, b.size, 0x00020000);
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)lds, 16, at, 0, 0, ONCE ? 2 : 0);
+}
+
 template <int BM, int BN, int WM, int WN>
 struct TileShape {
   static constexpr int kWaves = (BM / WM) * (BN / WN);
@@ -358,43 +373,39 @@ __global__ __launch_bounds__((TileShape<BM, BN, WM, WN>::kThreads), OCC) void k_
   const int wm = (wave % (BM / WM)) * WM, wn = (wave / (BM / WM)) * WN;
   const int K = (int)a.K, K16 = (K + 15) & ~15;
 
-  // buffer resources from the tile's first rows to the operands' last readable bytes
-  const int64_t ma = a.M - m0, nb = a.N - n0;
-  const int64_t end_a = (ma - 1) * a.lda + K16, end_b = (nb - 1) * a.ldb + K16;
-  const __amdgpu_buffer_rsrc_t ra = __builtin_amdgcn_make_buffer_rsrc(
-      const_cast<uint8_t*>(a.A + m0 * a.lda), 0, (int)(end_a < 0x7FFFFFFF ? end_a : 0x7FFFFFFF), 0x00020000);
-  const __amdgpu_buffer_rsrc_t rb = __builtin_amdgcn_make_buffer_rsrc(
-      const_cast<uint8_t*>(a.B + n0 * a.ldb), 0, (int)(end_b < 0x7FFFFFFF ? end_b : 0x7FFFFFFF), 0x00020000);
+  // fills: thread -> LDS row tid / 8 (+ kRows per round), place tid % 8; and one scale, of row or column tid
+  const int frow = tid >> 3;
+  const int pa = ((tid & 7) ^ key_a(frow)) * 16, pb = ((tid & 7) ^ key_b<TN>(frow)) * 16;
+  Bytes ra[NA], rb[NB];  // of the rounds' first rows on
+#pragma unroll
+  for (int i = 0; i < NA; ++i) ra[i] = bytes_from(a.A, m0 + i * kRows, a.M, a.lda, K16);
+#pragma unroll
+  for (int i = 0; i < NB; ++i) rb[i] = bytes_from(a.B, n0 + i * kRows, a.N, a.ldb, K16);
 
   const int all = (K + kStep - 1) / kStep;
   const int first = (int)blockIdx.y * split_steps;  // this workgroup's steps of the sum
   const int steps = all - first < split_steps ? all - first : split_steps;
 
-  // fills: thread -> LDS row tid / 8 (+ kRows per round), place tid % 8; and one scale, of row or column tid
-  const int frow = tid >> 3;
-  const int pa = ((tid & 7) ^ key_a(frow)) * 16, pb = ((tid & 7) ^ key_b<TN>(frow)) * 16;
-  const uint32_t oa = (uint32_t)frow * (uint32_t)a.lda + pa, ob = (uint32_t)frow * (uint32_t)a.ldb;
-  const uint32_t sa = kRows * (uint32_t)a.lda, sb = kRows * (uint32_t)a.ldb;
+  const int oa = frow * (int)a.lda + pa, ob = frow * (int)a.ldb;
   const bool of_a = tid < BM;
   const int64_t sm = m0 + tid < a.M ? m0 + tid : a.M - 1, sn = n0 + tid - BM < a.N ? n0 + tid - BM : a.N - 1;
   const float* scales = of_a ? a.a_scale + first * a.M + sm : a.b_scale + sn / kBlockF8 * all + first;
   const int64_t next_scale = of_a ? a.M : 1;
-  const auto fill = [&](int stage, int t) {
+  // Part c of step t's fills: a round of A's or B's rows, or the scales.  Past the last step they come from beyond the
+  // operands: they keep the counts and read nothing.
+  constexpr int kParts = NA + NB + 1;
+  const auto fill = [&](int stage, int t, int c) {
     const int k = t < steps ? (first + t) * kStep : K;
     char* base = lds + stage * S::kStage;
-    const bool ina = k + pa + 16 <= K;
-#pragma unroll
-    for (int i = 0; i < NA; ++i)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_ptr)(base + wave * 1024 + i * kRows * kStep), 16,
-                                               ina ? (int)(oa + i * sa + k) : (int)0x80000000, 0, 0, 0);
-#pragma unroll
-    for (int i = 0; i < NB; ++i) {
-      const int p = pb ^ ((i * kRows / (4 * TN)) & 3) << 5;  // the key of the round's rows
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_ptr)(base + wave * 1024 + (BM + i * kRows) * kStep), 16,
-                                               k + p + 16 <= K ? (int)(ob + i * sb + p + k) : (int)0x80000000, 0, 0, ONCE ? 2 : 0);
+    if (c < NA) {
+      fill16<false>(ra[c], base + wave * 1024 + c * kRows * kStep, k + pa + 16 <= K ? oa + k : (int)0x80000000);
+    } else if (c < NA + NB) {
+      const int i = c - NA, p = pb ^ ((i * kRows / (4 * TN)) & 3) << 5;  // the key of the round's rows
+      fill16<ONCE>(rb[i], base + wave * 1024 + (BM + i * kRows) * kStep, k + p + 16 <= K ? ob + p + k : (int)0x80000000);
+    } else {
+      __builtin_amdgcn_global_load_lds((__attribute__((address_space(1))) void*)scales, (lds_ptr)(base + S::kCodes + wave * 256), 4, 0, 0);
+      if (t + 1 < steps) scales += next_scale;  // (past the last step the last scales again: nothing uses them)
     }
-    __builtin_amdgcn_global_load_lds((__attribute__((address_space(1))) void*)scales, (lds_ptr)(base + S::kCodes + wave * 256), 4, 0, 0);
-    if (t + 1 < steps) scales += next_scale;  // (past the last step the last scales again: nothing uses them)
   };
   // fragments: lane -> row lane % 16 of the operand, pieces lane / 16 and lane / 16 + 4
   const int g = lane >> 4, r = lane & 15;
@@ -419,9 +430,9 @@ __global__ __launch_bounds__((TileShape<BM, BN, WM, WN>::kThreads), OCC) void k_
     return *reinterpret_cast<const float*>(lds + stage * S::kStage + S::kCodes + (BM + wn) * 4);
   };
 
-  // waits until the oldest fills are in, this wavefront's and then everyone's (LATER fills follow them)
+  // waits until the oldest fills are in, this wavefront's and then everyone's (`later` parts follow them)
   const auto arrived = [&](auto later) {
-    constexpr int n = decltype(later)::value * (NA + NB + 1);
+    constexpr int n = decltype(later)::value;
     static_assert(n < 64, "vmcnt");
     __builtin_amdgcn_s_waitcnt(0x0F70 | (n & 15) | (n >> 4) << 14);  // vmcnt(n)
     sync_lds();                                                    // (every fragment of the stage that is refilled next is read)
@@ -433,13 +444,26 @@ __global__ __launch_bounds__((TileShape<BM, BN, WM, WN>::kThreads), OCC) void k_
 #pragma unroll
     for (int j = 0; j < TM; ++j) acc[i][j] = fl4{0, 0, 0, 0};
 
-  // fills past the last step come from beyond the resources: they keep the counts and read nothing
+  // A product that follows a step's meeting, TN - 1 of them in its last phase and then those of the next step's phases, has
+  // kPer parts of the fills after it, so that they do not stop a wavefront for as long as they take to go out together
+  // (4096 x 4096 x 40960: 628 us with all parts after one product, 598).
+  constexpr int kSlots = TN - 1 + (TM - 1) * TN;
+  constexpr int kPer = (4 * kParts + 3 * kSlots - 1) / (3 * kSlots);
+  constexpr int kFirst = (TN - 1) * kPer < kParts ? (TN - 1) * kPer : kParts;  // parts in the last phase
+  const auto fills = [&](int stage, int t, int slot) {
 #pragma unroll
-  for (int t = 0; t < NS; ++t) fill(t, t);
-  arrived(std::integral_constant<int, NS - 1>{});
+    for (int c = slot * kPer; c < (slot + 1) * kPer && c < kParts; ++c) fill(stage, t, c);
+  };
+#pragma unroll
+  for (int t = 0; t < NS; ++t)
+#pragma unroll
+    for (int c = 0; c < (t + 1 < NS ? kParts : kFirst); ++c) fill(t, t, c);
+  arrived(std::integral_constant<int, (NS - 2) * kParts + kFirst>{});
   int st = 0;
   // A phase multiplies one operand of A with all of B's, and adds the sums of the phase before while the matrix cores
-  // work.  The next operand is read at the phase's beginning; the last phase's reads are the next step's.
+  // work.  The next operand is read at the phase's beginning.  In a step's last phase the workgroup meets after the first
+  // product, and the next step's operands and the fills of the one after it follow, each of B's operands into
+  // the registers that a product has just been the last to use.
   Op w[TN], x = read_a(0, 0);
 #pragma unroll
   for (int i = 0; i < TN; ++i) w[i] = read_b(0, i);
@@ -448,43 +472,54 @@ __global__ __launch_bounds__((TileShape<BM, BN, WM, WN>::kThreads), OCC) void k_
 #pragma unroll
   for (int i = 0; i < TN; ++i) p[i] = fl4{0, 0, 0, 0};
   float s_was = 0.0f;
-  const auto phase = [&](auto is_last, int j, int next, int t) {
-    constexpr bool kLast = decltype(is_last)::value;
-    constexpr int kPer = sizeof(TO) == 4 ? 4 : 1;  // matrix instructions of a product
-    const int before = j == 0 ? TM - 1 : j - 1;
-    if constexpr (kLast) {
-      arrived(std::integral_constant<int, NS - 2>{});
-      fill(st, t + NS);
-      sb_now = scale_b(next);
-    }
-    const Op y = kLast ? read_a(next, 0) : read_a(st, j + 1);
-    const float s_next = (kLast ? scale_a(next, 0) : scale_a(st, j + 1)) * sb_now;
+  const auto product = [&](int i, int before) {
+    const fl4 q = sums_of(w[i], x);
 #pragma unroll
-    for (int i = 0; i < TN; ++i) {
-      const fl4 q = sums_of(w[i], x);
-      if constexpr (kLast) w[i] = read_b(next, i);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) acc[i][before][e] = __builtin_fmaf(p[i][e], s_was, acc[i][before][e]);
-      p[i] = q;
-    }
-    // the order of a phase: its reads first, B's each after the product that is the last to use the registers
-    __builtin_amdgcn_sched_group_barrier(0x100, kLast ? 4 : 3, 0);  // LDS read
-#pragma unroll
-    for (int i = 0; i < TN; ++i) {
-      __builtin_amdgcn_sched_group_barrier(0x008, kPer, 0);  // MFMA
-      if constexpr (kLast) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-      __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);  // VALU
-    }
-    __builtin_amdgcn_sched_barrier(0);
-    x = y;
-    s_was = s;
-    s = s_next;
+    for (int e = 0; e < 4; ++e) acc[i][before][e] = __builtin_fmaf(p[i][e], s_was, acc[i][before][e]);
+    p[i] = q;
   };
   for (int t = 0; t < steps; ++t) {
-    const int next = st + 1 == NS ? 0 : st + 1;
+    const int next = st + 1 == NS ? 0 : st + 1, prev = st == 0 ? NS - 1 : st - 1;
+    Op y;
+    float s_next;
 #pragma unroll
-    for (int j = 0; j + 1 < TM; ++j) phase(std::false_type{}, j, next, t);
-    phase(std::true_type{}, TM - 1, next, t);
+    for (int j = 0; j + 1 < TM; ++j) {
+      y = read_a(st, j + 1);
+      s_next = scale_a(st, j + 1) * sb_now;
+#pragma unroll
+      for (int i = 0; i < TN; ++i) {
+        product(i, j == 0 ? TM - 1 : j - 1);
+        fills(prev, t - 1 + NS, TN - 1 + j * TN + i);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);  // LDS read
+#pragma unroll
+      for (int i = 0; i < TN; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, sizeof(TO) == 4 ? 4 : 1, 0);  // MFMA
+        __builtin_amdgcn_sched_group_barrier(0x020, kPer, 0);                     // memory read
+        __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);                        // VALU
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      x = y;
+      s_was = s;
+      s = s_next;
+    }
+#pragma unroll
+    for (int i = 0; i < TN; ++i) {
+      product(i, TM == 1 ? 0 : TM - 2);
+      __builtin_amdgcn_sched_barrier(0);
+      if (i == 0) {
+        arrived(std::integral_constant<int, (NS - 2) * kParts>{});
+        y = read_a(next, 0);
+        sb_now = scale_b(next);
+        s_next = scale_a(next, 0);
+      }
+      w[i] = read_b(next, i);
+      if (i > 0) fills(st, t + NS, i - 1);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    x = y;
+    s_was = s;
+    s = s_next * sb_now;
     st = next;
   }
 #pragma unroll
