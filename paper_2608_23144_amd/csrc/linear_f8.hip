@@ -348,7 +348,7 @@ struct TileShape {
   static_assert(BM + BN <= kThreads, "one scale a thread");
 };
 
-template <int BM, int BN, int WM, int WN, int OCC, int NS, bool ONCE, typename TO>
+template <int BM, int BN, int WM, int WN, int OCC, int NS, bool WHOLE, bool ONCE, typename TO>
 __global__ __launch_bounds__((TileShape<BM, BN, WM, WN>::kThreads), OCC) void k_matmul_f8_tile(LinearF8Args a, int tiles_m,
                                                                                                int tiles_n, int split_steps,
                                                                                                float* parts) {
@@ -449,7 +449,7 @@ __global__ __launch_bounds__((TileShape<BM, BN, WM, WN>::kThreads), OCC) void k_
   // (4096 x 4096 x 40960: 628 us with all parts after one product, 598).
   constexpr int kSlots = TN - 1 + (TM - 1) * TN;
   constexpr int kPer = (4 * kParts + 3 * kSlots - 1) / (3 * kSlots);
-  constexpr int kFirst = (TN - 1) * kPer < kParts ? (TN - 1) * kPer : kParts;  // parts in the last phase
+  constexpr int kFirst = WHOLE || (TN - 1) * kPer > kParts ? kParts : (TN - 1) * kPer;  // parts in the last phase
   const auto fills = [&](int stage, int t, int slot) {
 #pragma unroll
     for (int c = slot * kPer; c < (slot + 1) * kPer && c < kParts; ++c) fill(stage, t, c);
@@ -460,72 +460,118 @@ __global__ __launch_bounds__((TileShape<BM, BN, WM, WN>::kThreads), OCC) void k_
     for (int c = 0; c < (t + 1 < NS ? kParts : kFirst); ++c) fill(t, t, c);
   arrived(std::integral_constant<int, (NS - 2) * kParts + kFirst>{});
   int st = 0;
-  // A phase multiplies one operand of A with all of B's, and adds the sums of the phase before while the matrix cores
-  // work.  The next operand is read at the phase's beginning.  In a step's last phase the workgroup meets after the first
-  // product, and the next step's operands and the fills of the one after it follow, each of B's operands into
-  // the registers that a product has just been the last to use.
-  Op w[TN], x = read_a(0, 0);
+  Op w[TN], x;
+  float s;
+  if constexpr (WHOLE) {
+    // A step's operands are all read while the products of the step before run, into the other of two sets of registers
+    // (64 x 2560 x 2048: 8.8 with the phases below, 7.9; 4096 x 5120 x 5120 by 128 x 128 tiles 144 and 135; 256 x 256 tiles and
+    // results in fp32 of 128 x 128 have not the registers, 64 x 128 tiles of 16-bit results lose: 12.4, 13.0).
+    Op fa[2][TM], fb[2][TN];
+    float sc[2][TM];
+    const auto read = [&](int stage, int b) {
+      const float sb = scale_b(stage);
 #pragma unroll
-  for (int i = 0; i < TN; ++i) w[i] = read_b(0, i);
-  float sb_now = scale_b(0), s = scale_a(0, 0) * sb_now;
-  fl4 p[TN];
+      for (int i = 0; i < TN; ++i) fb[b][i] = read_b(stage, i);
 #pragma unroll
-  for (int i = 0; i < TN; ++i) p[i] = fl4{0, 0, 0, 0};
-  float s_was = 0.0f;
-  const auto product = [&](int i, int before) {
-    const fl4 q = sums_of(w[i], x);
+      for (int j = 0; j < TM; ++j) {
+        fa[b][j] = read_a(stage, j);
+        sc[b][j] = scale_a(stage, j) * sb;
+      }
+    };
+    read(0, 0);
+    for (int t0 = 0; t0 < steps; t0 += 2) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) acc[i][before][e] = __builtin_fmaf(p[i][e], s_was, acc[i][before][e]);
-    p[i] = q;
-  };
-  for (int t = 0; t < steps; ++t) {
-    const int next = st + 1 == NS ? 0 : st + 1, prev = st == 0 ? NS - 1 : st - 1;
-    Op y;
-    float s_next;
+      for (int b = 0; b < 2; ++b) {
+        const int t = t0 + b;
+        if (t >= steps) break;
+        const int next = st + 1 == NS ? 0 : st + 1;
+        arrived(std::integral_constant<int, (NS - 2) * kParts>{});
+        read(next, b ^ 1);
 #pragma unroll
-    for (int j = 0; j + 1 < TM; ++j) {
-      y = read_a(st, j + 1);
-      s_next = scale_a(st, j + 1) * sb_now;
+        for (int c = 0; c < kParts; ++c) fill(st, t + NS, c);
+        fl4 q[TN][TM];
+#pragma unroll
+        for (int i = 0; i < TN; ++i)
+#pragma unroll
+          for (int j = 0; j < TM; ++j) q[i][j] = sums_of(fb[b][i], fa[b][j]);
+#pragma unroll
+        for (int i = 0; i < TN; ++i)
+#pragma unroll
+          for (int j = 0; j < TM; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[i][j][e] = __builtin_fmaf(q[i][j][e], sc[b][j], acc[i][j][e]);
+        st = next;
+      }
+    }
+  } else {
+    // A phase multiplies one operand of A with all of B's, and adds the sums of the phase before while the matrix cores
+    // work.  The next operand is read at the phase's beginning.  In a step's last phase the workgroup meets after the first
+    // product, and the next step's operands and the fills of the one after it follow, each of B's operands into
+    // the registers that a product has just been the last to use.
+    x = read_a(0, 0);
+#pragma unroll
+    for (int i = 0; i < TN; ++i) w[i] = read_b(0, i);
+    float sb_now = scale_b(0);
+    s = scale_a(0, 0) * sb_now;
+    fl4 p[TN];
+#pragma unroll
+    for (int i = 0; i < TN; ++i) p[i] = fl4{0, 0, 0, 0};
+    float s_was = 0.0f;
+    const auto product = [&](int i, int before) {
+      const fl4 q = sums_of(w[i], x);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[i][before][e] = __builtin_fmaf(p[i][e], s_was, acc[i][before][e]);
+      p[i] = q;
+    };
+    for (int t = 0; t < steps; ++t) {
+      const int next = st + 1 == NS ? 0 : st + 1, prev = st == 0 ? NS - 1 : st - 1;
+      Op y;
+      float s_next;
+#pragma unroll
+      for (int j = 0; j + 1 < TM; ++j) {
+        y = read_a(st, j + 1);
+        s_next = scale_a(st, j + 1) * sb_now;
+#pragma unroll
+        for (int i = 0; i < TN; ++i) {
+          product(i, j == 0 ? TM - 1 : j - 1);
+          fills(prev, t - 1 + NS, TN - 1 + j * TN + i);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);  // LDS read
+#pragma unroll
+        for (int i = 0; i < TN; ++i) {
+          __builtin_amdgcn_sched_group_barrier(0x008, sizeof(TO) == 4 ? 4 : 1, 0);  // MFMA
+          __builtin_amdgcn_sched_group_barrier(0x020, kPer, 0);                     // memory read
+          __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);                        // VALU
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        x = y;
+        s_was = s;
+        s = s_next;
+      }
 #pragma unroll
       for (int i = 0; i < TN; ++i) {
-        product(i, j == 0 ? TM - 1 : j - 1);
-        fills(prev, t - 1 + NS, TN - 1 + j * TN + i);
+        product(i, TM == 1 ? 0 : TM - 2);
+        __builtin_amdgcn_sched_barrier(0);
+        if (i == 0) {
+          arrived(std::integral_constant<int, (NS - 2) * kParts>{});
+          y = read_a(next, 0);
+          sb_now = scale_b(next);
+          s_next = scale_a(next, 0);
+        }
+        w[i] = read_b(next, i);
+        if (i > 0) fills(st, t + NS, i - 1);
+        __builtin_amdgcn_sched_barrier(0);
       }
-      __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);  // LDS read
-#pragma unroll
-      for (int i = 0; i < TN; ++i) {
-        __builtin_amdgcn_sched_group_barrier(0x008, sizeof(TO) == 4 ? 4 : 1, 0);  // MFMA
-        __builtin_amdgcn_sched_group_barrier(0x020, kPer, 0);                     // memory read
-        __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);                        // VALU
-      }
-      __builtin_amdgcn_sched_barrier(0);
       x = y;
       s_was = s;
-      s = s_next;
+      s = s_next * sb_now;
+      st = next;
     }
 #pragma unroll
-    for (int i = 0; i < TN; ++i) {
-      product(i, TM == 1 ? 0 : TM - 2);
-      __builtin_amdgcn_sched_barrier(0);
-      if (i == 0) {
-        arrived(std::integral_constant<int, (NS - 2) * kParts>{});
-        y = read_a(next, 0);
-        sb_now = scale_b(next);
-        s_next = scale_a(next, 0);
-      }
-      w[i] = read_b(next, i);
-      if (i > 0) fills(st, t + NS, i - 1);
-      __builtin_amdgcn_sched_barrier(0);
-    }
-    x = y;
-    s_was = s;
-    s = s_next * sb_now;
-    st = next;
+    for (int i = 0; i < TN; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[i][TM - 1][e] = __builtin_fmaf(p[i][e], s_was, acc[i][TM - 1][e]);
   }
-#pragma unroll
-  for (int i = 0; i < TN; ++i)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) acc[i][TM - 1][e] = __builtin_fmaf(p[i][e], s_was, acc[i][TM - 1][e]);
   __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): no fill outlives the workgroup
   if (K % 16 && first + steps == all) {
     const int64_t k = K & ~15;
@@ -653,10 +699,10 @@ __global__ __launch_bounds__(256) void k_matmul_f8_join(LinearF8Args a, const fl
     if (n + e < a.N) o[n + e] = (TO)rounded(sum[e] + (a.bias ? a.bias[n + e] : 0.0f));
 }
 
-template <int BM, int BN, int WM, int WN, int OCC, int NS, bool ONCE, typename TO>
+template <int BM, int BN, int WM, int WN, int OCC, int NS, bool WHOLE, bool ONCE, typename TO>
 hipError_t launch_tile(const LinearF8Args& a, int split, void* ws, hipStream_t st) {
   using S = TileShape<BM, BN, WM, WN>;
-  const auto k = k_matmul_f8_tile<BM, BN, WM, WN, OCC, NS, ONCE, TO>;
+  const auto k = k_matmul_f8_tile<BM, BN, WM, WN, OCC, NS, WHOLE, ONCE, TO>;
   const size_t lds = NS * S::kStage;
   if (lds > 65536) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
@@ -706,45 +752,67 @@ hipError_t launch_linear_rows_w(const LinearF8Args& a, const void* X, int64_t ld
 }
 template <typename T>
 hipError_t launch_linear_rows_t(const LinearF8Args& a, const void* X, int64_t ldx, hipStream_t st) {
-  return a.M <= 8 ? launch_linear_rows_w<8, T>(a, X, ldx, st) : launch_linear_rows_w<16, T>(a, X, ldx, st);
+  // sixteen wavefronts where the workgroups leave CUs idle (1 x 2048 x 11008: 10.7 us with eight, 9.3; 16 x 2048 x 2048 8.5 and
+  // 7.3; 1 x 5120 x 5120 9.2 and 10.6)
+  return a.M > 8 || (a.N <= 2560 && (a.M >= 4 || a.K >= 8192)) ? launch_linear_rows_w<16, T>(a, X, ldx, st)
+                                                               : launch_linear_rows_w<8, T>(a, X, ldx, st);
 }
 
-// Which kernel takes a product, and over how many parts of the sum.
-enum Path { kRows, kTile32, kTile64, kTile64Wide, kTile128, kTile256 };
+// Which kernel takes a product, and over how many parts of the sum.  Times below are in us, into bf16, of calls on
+// weights that are not in the caches.
+enum Path { kRows, kTile32, kTile64, kTile64Wide, kTile128Deep, kTile128, kTile256 };
 struct Choice {
   Path path;
   int split;
 };
 Choice choose(int64_t M, int64_t N, int64_t K) {
   const auto tiles = [&](int64_t bm, int64_t bn) { return ((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
+  // Up to 16 rows: 16 columns a workgroup, up to about three of them a CU (16 x 2048 x 11008: 11.6, tiles 12.9 with their
+  // sums split; 16 x 11008 x 2048: 9.0 and 8.9; 16 x 13824 x 5120: 19.8 and 16.0).
   if (M <= 16 && N < 12288) return {kRows, 1};
-  if (M > 16 && M <= 32 && N <= 8192 && K <= 16384) return {kRows, 1};
+  // Up to 32 rows of weights that are not too large (32 x 4096 x 4096: 8.6 and 11.0; 24 x 5120 x 5120: 15.1 and 13.1; 32 x
+  // 8192 x 8192: 24.7 and 21.5).
+  if (M > 16 && M <= 32 && N * K <= 20000000) return {kRows, 1};
   const int64_t t128 = tiles(128, 128), t256 = tiles(256, 256);
-  if (M > 64 && t128 >= 256) return {2.9 * ((t256 + 255) / 256) < t128 / 256.0 + 0.5 ? kTile256 : kTile128, 1};
+  // 128 x 128 tiles, two workgroups a CU, or 256 x 256, one: a round of 256 of the large ones costs what 2.6 times as many
+  // small ones do (512 x 27648 x 5120: 116 and 82; 1024 x 5120 x 5120: 50 and 71; 4096 x 5120 x 5120: 135 and 141; 2048 x
+  // 11008 x 2048: 70 and 63).
+  if (M > 64 && t128 > 256) return {2.9 * ((t256 + 255) / 256) < t128 / 256.0 + 0.5 ? kTile256 : kTile128, 1};
+  // One of them a CU: four stages instead of two (128 x 27648 x 5120: 40, with two 50, 64 x 128 tiles 49; 256 x 11008 x
+  // 2048: 16, 21 and 18; 512 x 5120 x 5120: 31, 43 and 37; 2048 x 2048 x 11008: 64 and 84; with 80 of them, 200 x 5120 x
+  // 5120, smaller tiles: 22).
+  if (M > 64 && t128 >= 128) return {kTile128Deep, 1};
+  // 64 x 27648 x 5120: 64 x 64 tiles 38.4, 64 x 128 tiles 30.7 (64 x 11008 x 2048: 9.5 and 11.9)
   if (M > 32 && tiles(64, 128) >= 192) return {kTile64Wide, 1};
   const Path path = M > 32 ? kTile64 : kTile32;
+  // Few tiles under a long sum: parts of at least 16 steps, joined by a second launch (64 x 2048 x 11008: 30 whole, 15 in 5
+  // parts; 256 x 2048 x 11008: 28 and 21 in 2; 32 x 2048 x 27648: 63 and 19 in 8; 64 x 2560 x 2048: 7.9 whole, 9.1 in 2)
   const int64_t t = path == kTile64 ? tiles(64, 64) : tiles(32, 64);
   const int64_t want = (256 + t - 1) / t, most = (K + kStep - 1) / kStep / 16;
   const int64_t split = want < most ? want : most;
-  return {path, t < 128 && split > 1 ? (int)split : 1};
+  return {path, t <= 128 && split > 1 ? (int)split : 1};
 }
 
 template <typename TO>
 hipError_t launch(const LinearF8Args& a, void* ws, hipStream_t st) {
   const Choice c = choose(a.M, a.N, a.K);
+  // Weights read once that fill a good part of the last cache go past it (64 x 27648 x 5120: 34.4, 30.7 past it; 16 x 13824 x
+  // 5120 17.6 and 16.0).
   const bool once = a.M <= 64 && a.N * a.K >= (int64_t)1 << 26;
+  constexpr bool kWide = sizeof(TO) == 4;  // operands as fp16: twice the registers
   switch (c.path) {
     case kRows: return a.M <= 16 ? launch_rows<8, 1, TO>(a, st) : launch_rows<8, 2, TO>(a, st);
     case kTile32:
-      return once ? launch_tile<32, 64, 32, 32, 2, 4, true, TO>(a, c.split, ws, st)
-                  : launch_tile<32, 64, 32, 32, 2, 4, false, TO>(a, c.split, ws, st);
-    case kTile64: return launch_tile<64, 64, 32, 32, 2, 4, false, TO>(a, c.split, ws, st);
+      return once ? launch_tile<32, 64, 32, 32, 2, 4, true, true, TO>(a, c.split, ws, st)
+                  : launch_tile<32, 64, 32, 32, 2, 4, true, false, TO>(a, c.split, ws, st);
+    case kTile64: return launch_tile<64, 64, 32, 32, 2, 4, true, false, TO>(a, c.split, ws, st);
     case kTile64Wide:
-      return once ? launch_tile<64, 128, 32, 64, 2, 3, true, TO>(a, 1, ws, st)
-                  : launch_tile<64, 128, 32, 64, 2, 3, false, TO>(a, 1, ws, st);
-    case kTile256:  // (of results in fp32 the operands do not fit the registers as fp16)
-      if constexpr (sizeof(TO) == 2) return launch_tile<256, 256, 128, 64, 2, 2, false, TO>(a, 1, ws, st);
-    default: return launch_tile<128, 128, 64, 64, 2, 2, false, TO>(a, 1, ws, st);
+      return once ? launch_tile<64, 128, 32, 64, 2, 3, kWide, true, TO>(a, 1, ws, st)
+                  : launch_tile<64, 128, 32, 64, 2, 3, kWide, false, TO>(a, 1, ws, st);
+    case kTile128Deep: return launch_tile<128, 128, 64, 64, 2, 4, false, false, TO>(a, 1, ws, st);
+    case kTile256:  // (of results in fp32 the operands do not fit the registers)
+      if constexpr (!kWide) return launch_tile<256, 256, 128, 64, 2, 2, false, false, TO>(a, 1, ws, st);
+    default: return launch_tile<128, 128, 64, 64, 2, 2, !kWide, false, TO>(a, 1, ws, st);
   }
 }
 
@@ -762,8 +830,13 @@ hipError_t launch_matmul_f8(const LinearF8Args& a, void* ws, hipStream_t st) {
 }
 
 bool linear_f8_fused(int64_t M, int64_t N, int64_t K) {
-  const int64_t share = M <= 1 ? 1 : M <= 2 ? 2 : M <= 4 ? 4 : 8;
-  return M <= 16 && K * share <= 16384 && N < 8192;
+  // Where quantizing over and over costs a workgroup less than a launch.  On the GPU, in us, fused and in two launches:
+  // 1 x 2560 x 2048 4.2 and 6.0; 1 x 11008 x 2048 7.0 and 10.9; 1 x 27648 x 5120 29.2 and 29.7; 1 x 5120 x 27648 37.3 and 39.5;
+  // 2 x 5120 x 5120 10.4 and 12.5; 4 x 11008 x 2048 8.9 and 11.1; 8 x 11008 x 2048 11.4 and 11.4; 16 x 2048 x 2048 7.3 and 6.3
+  // (but a launch that is not replayed from a graph costs the host 3); 4 x 2048 x 11008 13.1 and 13.8; 8 x 5120 x 5120 17.6
+  // and 12.8; 16 x 11008 x 2048 16.6 and 11.8.
+  if (M == 1) return K <= 32768;
+  return M <= 16 && N < 12288 && (M * K <= 16384 || (K <= 2048 && N <= 4096));
 }
 
 hipError_t launch_linear_f8_fused(const LinearF8Args& a, const void* X, int x_dtype, int64_t ldx, hipStream_t st) {
