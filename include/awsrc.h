@@ -762,7 +762,8 @@ awsrc_status awsrc_kv_plan(const awsrc_page_pool* pool, int32_t n_seq, const int
  * finite, or not positive, count as 0.  If all do the token is drawn from p_a, and if all of p_a do
  * it is -1.
  * 1 <= vocab < 2^31.
- * Workspace: two-phase query as described above (the query needs no pointers).
+ * Workspace: two-phase query as described above (the query needs no pointers);
+ * the size may be 0, and then no workspace is needed.
  */
 awsrc_status awsrc_verify_drafts(const void* p, int64_t ldp, const void* q_or_null, int64_t ldq, int32_t dtype, int64_t vocab,
                                  int32_t n_seq, int64_t n_rows, const int32_t* cu, const int32_t* tokens, const float* u,

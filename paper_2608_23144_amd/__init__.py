@@ -597,11 +597,11 @@ def _rows_of(t: torch.Tensor, what: str):
     return rows, cols, (ld if rows > 1 or ld > cols else cols)
 
 
-def _i8_rows(t: torch.Tensor, what: str):
-    """_rows_of for an int8 operand: its rows are read in pieces of 16 bytes."""
+def _i8_rows(t: torch.Tensor, what: str, dtype: torch.dtype = torch.int8):
+    """_rows_of for an operand of 8-bit codes: its rows are read in pieces of 16 bytes."""
     rows, cols, ld = _rows_of(t, what)
-    if t.dtype != torch.int8:
-        raise TypeError(f"{what} must be int8, not {t.dtype}")
+    if t.dtype != dtype:
+        raise TypeError(f"{what} must be {dtype}, not {t.dtype}")
     if cols % 16 == 0:
         return rows, cols, ld if rows > 1 or ld % 16 == 0 else cols
     wide = -(-cols // 16) * 16
@@ -898,13 +898,6 @@ BLOCK_F8 = 128  # columns, and rows of a weight matrix, that share a scale
 _F8 = torch.float8_e4m3fn
 
 
-def _f8_rows(t: torch.Tensor, what: str):
-    """_rows_of for an e4m3 operand: its rows are read in pieces of 16 bytes."""
-    if t.dtype != _F8:
-        raise TypeError(f"{what} must be {_F8}, not {t.dtype}")
-    return _i8_rows(t.view(torch.int8), what)
-
-
 def _blocks_shape(rows: int, cols: int, block_rows: int):
     if block_rows not in (1, BLOCK_F8):
         raise ValueError("block_rows must be 1 or 128")
@@ -985,8 +978,8 @@ def awsrc_matmul_f8(a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor, b_s
                     stream=None) -> torch.Tensor:
     """a [M, K] times b [N, K] transposed, e4m3 codes with fp32 scales as awsrc_quantize_blocks_f8 makes them (a with
     block_rows 1, b with 128): [M, N] in out_dtype (or out's)."""
-    M, K, lda = _f8_rows(a, "a")
-    N, Kb, ldb = _f8_rows(b, "b")
+    M, K, lda = _i8_rows(a, "a", _F8)
+    N, Kb, ldb = _i8_rows(b, "b", _F8)
     if K != Kb:
         raise ValueError(f"a has {K} columns, b {Kb}")
     dev = _device_of(a)
@@ -1012,7 +1005,7 @@ def awsrc_linear_f8(x: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, bia
     awsrc_quantize_blocks_f8 makes them from the weight matrix with block_rows 128) transposed, plus bias; [M, N] in x's type
     by default.  For inference: the result carries no gradient."""
     M, K, ldx = _rows_of(x, "x")
-    N, Kw, ldw = _f8_rows(w, "w")
+    N, Kw, ldw = _i8_rows(w, "w", _F8)
     if K != Kw:
         raise ValueError(f"x has {K} columns, w {Kw}")
     dev = _device_of(x)
@@ -1050,14 +1043,6 @@ def _ints(t: torch.Tensor, n: int, what: str, dev: int) -> int:
     return t.data_ptr()
 
 
-def _new(n: int, dtype: torch.dtype, device, stream) -> torch.Tensor:
-    """_empty of one dimension, on a device object."""
-    if stream is None:
-        return torch.empty(n, dtype=dtype, device=device)
-    with torch.cuda.stream(stream):
-        return torch.empty(n, dtype=dtype, device=device)
-
-
 @functools.lru_cache(_WS_SIZES)
 def kv_plan_workspace_bytes(n_seq: int, rows: int) -> int:
     n = ctypes.c_size_t(0)
@@ -1090,9 +1075,8 @@ def awsrc_kv_plan(pool: PagePool, kv_len: torch.Tensor, keep: torch.Tensor, new_
     kv_out_p = kv_p if kv_len_out is None else _ints(kv_len_out, n, "kv_len_out", dev)
     free_out_p = c.n_free if n_free_out is None else _ints(n_free_out, 1, "n_free_out", dev)
     if out is None:
-        where = kv_len.device
-        cu, seq, slot = _new(n + 1, _I32, where, stream), _new(rows, _I32, where, stream), _new(rows, torch.int64, where, stream)
-        pos = _new(rows, _I32, where, stream)
+        cu, seq, slot = _empty(n + 1, kv_len, _I32, stream), _empty(rows, kv_len, _I32, stream), _empty(rows, kv_len, torch.int64, stream)
+        pos = _empty(rows, kv_len, _I32, stream)
         cu_p, seq_p, pos_p = cu.data_ptr(), seq.data_ptr(), pos.data_ptr()
     else:
         cu, seq, pos, slot = out
@@ -1138,8 +1122,7 @@ def awsrc_verify_drafts(p: torch.Tensor, tokens: torch.Tensor, u: torch.Tensor, 
         raise ValueError(f"u: contiguous fp32 [{rows}] on cuda:{dev}")
     cu_p, tokens_p = _ints(cu, n + 1, "cu", dev), _ints(tokens, rows, "tokens", dev)
     if out is None:
-        where = p.device
-        out = (_new(rows, _I32, where, stream), _new(n, _I32, where, stream))
+        out = (_empty(rows, p, _I32, stream), _empty(n, p, _I32, stream))
         out_p, n_p = out[0].data_ptr(), out[1].data_ptr()
     else:
         out_p, n_p = _ints(out[0], rows, "tokens that follow", dev), _ints(out[1], n, "numbers of tokens", dev)
@@ -1147,7 +1130,7 @@ def awsrc_verify_drafts(p: torch.Tensor, tokens: torch.Tensor, u: torch.Tensor, 
     if kv_len is not None:
         kv_p = _ints(kv_len, n, "kv_len", dev)
         if keep is None:
-            keep = _new(n, _I32, kv_len.device, stream)
+            keep = _empty(n, p, _I32, stream)
             keep_p = keep.data_ptr()
         else:
             keep_p = _ints(keep, n, "keep", dev)

@@ -9,16 +9,57 @@ namespace awsrc {
 
 namespace {
 
+typedef uint32_t u32_any __attribute__((aligned(1)));
 typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(1)));
 
-// Eight codes to any byte address, of which n exist.
-__device__ __forceinline__ void store8_codes(uint8_t* __restrict__ c, uint2 w, int64_t n) {
-  if (n >= 8) {
-    *reinterpret_cast<u32x2_any*>(c) = u32x2_any{w.x, w.y};
+// Which eight columns of a block of 128 a lane of its sixteen takes: in two groups of four where that lets neighbouring lanes
+// read and write 16 bytes side by side (fp32), else all together.  `at` and `second` count from the block's first.
+template <typename T>
+struct Part {
+  static constexpr bool kTwo = sizeof(T) == 4;
+  int at;
+  __device__ __forceinline__ Part(int lane) : at((lane & 15) * (kTwo ? 4 : 8)) {}
+  static constexpr int second = kTwo ? 64 : 4;  // from the first four columns to the others
+};
+
+// A lane's eight values of a block at x, of whose columns n exist (the others are 0).
+template <typename T>
+__device__ __forceinline__ void load_part(const T* __restrict__ x, Part<T> p, int64_t n, float (&v)[8]) {
+  if constexpr (Part<T>::kTwo) {
+    typedef float V __attribute__((ext_vector_type(4), aligned(4)));
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int at = p.at + h * Part<T>::second;
+      if (at + 4 <= n) {
+        const V w = *reinterpret_cast<const V*>(x + at);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[4 * h + e] = w[e];
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[4 * h + e] = at + e < n ? x[at + e] : 0.0f;
+      }
+    }
+  } else {
+    load8_any(x + p.at, n - p.at, v);
+  }
+}
+
+// And its codes, to any byte address.
+template <typename T>
+__device__ __forceinline__ void store_part(uint8_t* __restrict__ c, Part<T> p, int64_t n, uint2 w) {
+  if (p.at + Part<T>::second + 4 <= n) {
+    if constexpr (Part<T>::kTwo) {
+      *reinterpret_cast<u32_any*>(c + p.at) = w.x;
+      *reinterpret_cast<u32_any*>(c + p.at + Part<T>::second) = w.y;
+    } else {
+      *reinterpret_cast<u32x2_any*>(c + p.at) = u32x2_any{w.x, w.y};
+    }
   } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (e < n) c[e] = (uint8_t)((e < 4 ? w.x : w.y) >> (8 * (e & 3)));
+    for (int e = 0; e < 8; ++e) {
+      const int at = p.at + (e < 4 ? e : Part<T>::second + e - 4);
+      if (at < n) c[at] = (uint8_t)((e < 4 ? w.x : w.y) >> (8 * (e & 3)));
+    }
   }
 }
 
@@ -35,12 +76,13 @@ __global__ __launch_bounds__(256) void k_quantize_blocks_row(const T* __restrict
   const int64_t row0 = (int64_t)(wg / strips) * R;
   const int64_t strip = wg % strips;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t at = strip * 512 + lane * 8;
+  const int64_t at = strip * 512 + (lane >> 4) * kBlockF8;  // the first column of this lane's block
+  const Part<T> part(lane);
   float v[RW][8];
 #pragma unroll
   for (int i = 0; i < RW; ++i) {
     const int64_t row = row0 + wave * RW + i;
-    load8_any(X + (row < rows ? row : rows - 1) * ldx + at, cols - at, v[i]);
+    load_part(X + (row < rows ? row : rows - 1) * ldx + at, part, cols - at, v[i]);
   }
 #pragma unroll
   for (int i = 0; i < RW; ++i) {
@@ -50,7 +92,7 @@ __global__ __launch_bounds__(256) void k_quantize_blocks_row(const T* __restrict
     for (int e = 0; e < 8; ++e) m = amax_keep(m, v[i][e]);
     const float s = scale_of_amax_f8(amax_of_16(m));
     const uint2 w = codes8_f8(v[i], inverse_scale(s), s > 0.0f);
-    if (row < rows) store8_codes(codes + row * ldc + at, w, cols - at);
+    if (row < rows) store_part(codes + row * ldc + at, part, cols - at, w);
     if ((lane & 15) == 0) s_scale[lane >> 4][wave * RW + i] = s;
   }
   __syncthreads();
@@ -70,12 +112,13 @@ __global__ __launch_bounds__(256) void k_quantize_blocks_square(const T* __restr
   const uint32_t wg = workgroup<256>();
   if (wg >= n_wg) return;
   const int64_t rb = wg / col_blocks, cb = wg % col_blocks;
-  const int64_t row0 = rb * kBlockF8 + (threadIdx.x >> 4), at = cb * kBlockF8 + (threadIdx.x & 15) * 8;
+  const int64_t row0 = rb * kBlockF8 + (threadIdx.x >> 4), at = cb * kBlockF8;
+  const Part<T> part(threadIdx.x);
   float v[8][8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int64_t row = row0 + 16 * i;
-    load8_any(X + (row < rows ? row : rows - 1) * ldx + at, cols - at, v[i]);  // (rows past the end count the last one twice)
+    load_part(X + (row < rows ? row : rows - 1) * ldx + at, part, cols - at, v[i]);  // (rows past the end count the last one twice)
   }
   float m = 0.0f;
 #pragma unroll
@@ -94,7 +137,7 @@ __global__ __launch_bounds__(256) void k_quantize_blocks_square(const T* __restr
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int64_t row = row0 + 16 * i;
-    if (row < rows) store8_codes(codes + row * ldc + at, codes8_f8(v[i], inv, s > 0.0f), cols - at);
+    if (row < rows) store_part(codes + row * ldc + at, part, cols - at, codes8_f8(v[i], inv, s > 0.0f));
   }
   if (threadIdx.x == 0) scale[wg] = s;
 }
@@ -108,14 +151,23 @@ __global__ __launch_bounds__(256) void k_dequantize_blocks(const uint8_t* __rest
   const uint32_t wg = workgroup<256>();
   if (wg >= n_wg) return;
   const int64_t row = (int64_t)(wg / strips) * 4 + (threadIdx.x >> 6);
-  const int64_t at = (int64_t)(wg % strips) * 512 + (threadIdx.x & 63) * 8;
+  const int64_t at = (int64_t)(wg % strips) * 512 + ((threadIdx.x & 63) >> 4) * kBlockF8;
   if (row >= rows || at >= cols) return;
-  const int64_t blocks = (cols + kBlockF8 - 1) / kBlockF8;
+  const int64_t blocks = (cols + kBlockF8 - 1) / kBlockF8, n = cols - at;
   const float s = square ? scale[row / kBlockF8 * blocks + at / kBlockF8] : scale[at / kBlockF8 * rows + row];
   const uint8_t* c = codes + row * ldc + at;
   T* o = out + row * ldo + at;
-  if (cols - at >= 8) {
-    const u32x2_any w = *reinterpret_cast<const u32x2_any*>(c);
+  const Part<T> part(threadIdx.x);
+  if (part.at + Part<T>::second + 4 <= n) {
+    uint32_t w[2];
+    if constexpr (Part<T>::kTwo) {
+      w[0] = *reinterpret_cast<const u32_any*>(c + part.at);
+      w[1] = *reinterpret_cast<const u32_any*>(c + part.at + Part<T>::second);
+    } else {
+      const u32x2_any x = *reinterpret_cast<const u32x2_any*>(c + part.at);
+      w[0] = x[0];
+      w[1] = x[1];
+    }
     float y[8];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -125,17 +177,21 @@ __global__ __launch_bounds__(256) void k_dequantize_blocks(const uint8_t* __rest
       y[4 * i + 2] = rounded(b[0] * s);
       y[4 * i + 3] = rounded(b[1] * s);
     }
-    typedef T V __attribute__((ext_vector_type(16 / sizeof(T)), aligned(sizeof(T))));
     constexpr int kPer = 16 / sizeof(T);
+    typedef T V __attribute__((ext_vector_type(16 / sizeof(T)), aligned(sizeof(T))));
 #pragma unroll
     for (int i = 0; i < 8 / kPer; ++i) {
       V z;
 #pragma unroll
       for (int e = 0; e < kPer; ++e) z[e] = (T)y[i * kPer + e];
-      *reinterpret_cast<V*>(o + i * kPer) = z;
+      *reinterpret_cast<V*>(o + part.at + i * Part<T>::second) = z;
     }
   } else {
-    for (int e = 0; e < cols - at; ++e) o[e] = (T)rounded(__builtin_amdgcn_cvt_f32_fp8((int)c[e], 0) * s);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int j = part.at + (e < 4 ? e : Part<T>::second + e - 4);
+      if (j < n) o[j] = (T)rounded(__builtin_amdgcn_cvt_f32_fp8((int)c[j], 0) * s);
+    }
   }
 }
 

@@ -89,18 +89,62 @@ struct Vec {
   typedef T type __attribute__((ext_vector_type(16 / sizeof(T)), aligned(sizeof(T))));
 };
 
-// A wavefront takes two pieces of 16-bit values, one of fp32 ones: eight or sixteen loads a lane on their way together.
+// The sum of a piece's weights, by one wavefront, whose eight or sixteen loads a lane and row are on their way together; in
+// lane 63.
 //
 // Weights that are not finite show in the sum, which is then made again value by value: a maximum with 0 is all that
-// a weight costs besides its conversion and its addition (200 rows of 100003 in bf16, every value compared: 18.0 us).
+// a weight costs besides its conversion and its addition (200 rows of 100003 in bf16 12.7 us, 18.0 with every value compared).
+template <typename T>
+__device__ __forceinline__ double sum_of_piece(const Weights<T>& weights, int64_t piece) {
+  typedef typename Vec<T>::type V;
+  constexpr int n = Vec<T>::n, kLoads = kPiece / (64 * n);
+  const int lane = threadIdx.x & 63;
+  const int64_t begin = piece * kPiece, end = begin + kPiece;
+  double w = __builtin_inf();
+  if (end <= weights.vocab && !(weights.less >= begin && weights.less < end)) {
+    const T* p = weights.p + begin + lane * n;
+    V x[kLoads];
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) x[j] = *reinterpret_cast<const V*>(p + j * 64 * n);
+    w = 0.0;
+    if (weights.q) {
+      const T* q = weights.q + begin + lane * n;
+      V y[kLoads];
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j) y[j] = *reinterpret_cast<const V*>(q + j * 64 * n);
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j)
+#pragma unroll
+        for (int e = 0; e < n; ++e) w += __builtin_fmax((double)to_f32((T)x[j][e]) - (double)to_f32((T)y[j][e]), 0.0);
+    } else {
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j)
+#pragma unroll
+        for (int e = 0; e < n; ++e) w += (double)__builtin_fmaxf(to_f32((T)x[j][e]), 0.0f);
+    }
+    w = scan_wave(w);
+  }
+  if (!(of_lane(w, 63) < __builtin_inf())) {  // the row ends in here, the draft lies here, or a value is not finite
+    w = 0.0;
+    for (int j = 0; j < kPiece / 512; ++j) {
+      const int64_t at = begin + (j * 64 + lane) * 8;
+      float x[8], y[8];
+      weights.load(at, x, y);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w += weights.of(at + e, x[e], y[e]);
+    }
+    w = scan_wave(w);
+  }
+  return w;
+}
+
+// A wavefront takes two pieces of 16-bit values, one of fp32 ones.
 template <typename T>
 constexpr int kPerWave = sizeof(T) == 2 ? 2 : 1;
 
 template <typename T>
 __global__ __launch_bounds__(kThreads) void k_verify_sums(VerifyArgs a, int pieces, uint32_t groups, int64_t n_wg, double* sums,
                                                           int32_t* places) {
-  typedef typename Vec<T>::type V;
-  constexpr int n = Vec<T>::n, kLoads = kPiece / (64 * n);
   const uint32_t wg = workgroup<kThreads>();
   if (wg >= n_wg) return;
   const int s = (int)(wg / groups), first = ((int)(wg % groups) * (kThreads / 64) + (threadIdx.x >> 6)) * kPerWave<T>;
@@ -112,45 +156,82 @@ __global__ __launch_bounds__(kThreads) void k_verify_sums(VerifyArgs a, int piec
 #pragma unroll
   for (int k = 0; k < kPerWave<T>; ++k) {
     if (first + k >= pieces) break;
-    const int64_t begin = (int64_t)(first + k) * kPiece, end = begin + kPiece;
-    double w = __builtin_inf();
-    if (end <= a.vocab && !(weights.less >= begin && weights.less < end)) {
-      const T* p = weights.p + begin + lane * n;
-      V x[kLoads];
-#pragma unroll
-      for (int j = 0; j < kLoads; ++j) x[j] = *reinterpret_cast<const V*>(p + j * 64 * n);
-      w = 0.0;
-      if (weights.q) {
-        const T* q = weights.q + begin + lane * n;
-        V y[kLoads];
-#pragma unroll
-        for (int j = 0; j < kLoads; ++j) y[j] = *reinterpret_cast<const V*>(q + j * 64 * n);
-#pragma unroll
-        for (int j = 0; j < kLoads; ++j)
-#pragma unroll
-          for (int e = 0; e < n; ++e) w += __builtin_fmax((double)to_f32((T)x[j][e]) - (double)to_f32((T)y[j][e]), 0.0);
-      } else {
-#pragma unroll
-        for (int j = 0; j < kLoads; ++j)
-#pragma unroll
-          for (int e = 0; e < n; ++e) w += (double)__builtin_fmaxf(to_f32((T)x[j][e]), 0.0f);
-      }
-      w = scan_wave(w);
-    }
-    if (!(of_lane(w, 63) < __builtin_inf())) {  // the row ends in here, the draft lies here, or a value is not finite
-      w = 0.0;
-      for (int j = 0; j < kPiece / 512; ++j) {
-        const int64_t at = begin + (j * 64 + lane) * 8;
-        float x[8], y[8];
-        weights.load(at, x, y);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) w += weights.of(at + e, x[e], y[e]);
-      }
-      w = scan_wave(w);
-    }
+    const double w = sum_of_piece(weights, first + k);
     if (lane == 63) sums[(int64_t)s * pieces + first + k] = w;
   }
   if (first == 0 && lane == 0) places[s] = (int32_t)place;
+}
+
+// Small vocabularies: one workgroup a sequence does it all, without a workspace.  Every wavefront finds the row and sums
+// pieces of it; the first one then draws, its lanes holding 32 tokens side by side.
+constexpr int kAlone = 32;  // pieces at most: 65536 tokens
+constexpr int kAloneWaves = 16;
+
+template <typename T>
+__global__ __launch_bounds__(64 * kAloneWaves) void k_verify_alone(VerifyArgs a, int pieces) {
+  __shared__ double sums[64];
+  const uint32_t s = workgroup<64 * kAloneWaves>();
+  if (s >= (uint32_t)a.n_seq) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const Rows rows = rows_of(a, (int)s);
+  int64_t place = -1, token = -1;
+  if (rows.n > 0) {
+    place = place_of<T>(a, rows);
+    const float u = a.u[rows.begin + rows.n - 1];
+    Weights<T> weights(a, rows, place);
+    if (tid < 64) sums[tid] = 0.0;
+    double upto, all;
+    for (;;) {
+      __syncthreads();
+      for (int c = wave; c < pieces; c += kAloneWaves) {
+        const double w = sum_of_piece(weights, c);
+        if (lane == 63) sums[c] = w;
+      }
+      __syncthreads();
+      upto = scan_wave(sums[lane]);
+      all = of_lane(upto, 63);
+      if (all > 0.0 || weights.plain()) break;
+      weights.make_plain();  // nothing of p lies above q: p itself
+    }
+    if (all > 0.0 && wave == 0) {
+      const double mark = (double)u * all;
+      const uint64_t passes = __ballot(sums[lane] > 0.0 && upto > mark), counts = __ballot(sums[lane] > 0.0);
+      const int piece = passes ? (int)__builtin_ctzll(passes) : 63 - (int)__builtin_clzll(counts);
+      const double before = of_lane(upto, piece) - sums[piece];
+      const int64_t at = (int64_t)piece * kPiece + lane * (kPiece / 64);
+      float x[kPiece / 512][8], y[kPiece / 512][8];
+#pragma unroll
+      for (int j = 0; j < kPiece / 512; ++j) weights.load(at + j * 8, x[j], y[j]);
+      double sum = 0.0;
+#pragma unroll
+      for (int j = 0; j < kPiece / 512; ++j)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum += weights.of(at + j * 8 + e, x[j][e], y[j][e]);
+      double run = before + (scan_wave(sum) - sum);
+      int first = -1, last = -1;
+#pragma unroll
+      for (int j = 0; j < kPiece / 512; ++j)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const double w = weights.of(at + j * 8 + e, x[j][e], y[j][e]);
+          run += w;
+          if (w > 0.0) {
+            if (first < 0 && run > mark) first = j * 8 + e;
+            last = j * 8 + e;
+          }
+        }
+      const uint64_t here = __ballot(first >= 0), some = __ballot(last >= 0);
+      const int l = here ? (int)__builtin_ctzll(here) : 63 - (int)__builtin_clzll(some);
+      token = (int64_t)piece * kPiece + l * (kPiece / 64) + __shfl(here ? first : last, l, 64);
+    }
+  }
+  if (wave) return;
+  for (int64_t i = lane; i < rows.n; i += 64)
+    a.tokens_out[rows.begin + i] = i < place ? a.tokens[rows.begin + i + 1] : i == place ? (int32_t)token : -1;
+  if (lane == 0) {
+    a.n_out[s] = (int32_t)(place + 1);
+    if (a.keep) a.keep[s] = (int32_t)(a.kv_len[s] - rows.n + place + 1);
+  }
 }
 
 __device__ __forceinline__ double scan(double x, double (*wave_sums)[kThreads / 64], double& total) {
@@ -275,9 +356,14 @@ template <typename T>
 constexpr int kPieces = kPerWave<T> * kThreads / 64;  // of a workgroup of the first launch
 
 int64_t pieces_of(int64_t vocab) { return (vocab + kPiece - 1) / kPiece; }
+bool verify_alone(int64_t vocab) { return pieces_of(vocab) <= kAlone; }
 
 template <typename T>
 hipError_t launch(const VerifyArgs& a, void* ws, hipStream_t st) {
+  if (verify_alone(a.vocab)) {
+    hipLaunchKernelGGL((k_verify_alone<T>), grid_of<64 * kAloneWaves>(a.n_seq), dim3(64 * kAloneWaves), 0, st, a, (int)pieces_of(a.vocab));
+    return hipGetLastError();
+  }
   const int64_t pieces = pieces_of(a.vocab), groups = (pieces + kPieces<T> - 1) / kPieces<T>, n = groups * a.n_seq;
   if (n >= (int64_t)1 << 31) return hipErrorInvalidValue;
   double* sums = static_cast<double*>(ws);
@@ -289,7 +375,9 @@ hipError_t launch(const VerifyArgs& a, void* ws, hipStream_t st) {
 
 }  // namespace
 
-size_t verify_ws_bytes(int n_seq, int64_t vocab) { return (size_t)n_seq * (pieces_of(vocab) * sizeof(double) + 4); }
+size_t verify_ws_bytes(int n_seq, int64_t vocab) {
+  return verify_alone(vocab) ? 0 : (size_t)n_seq * (pieces_of(vocab) * sizeof(double) + 4);
+}
 
 hipError_t launch_verify(const VerifyArgs& a, void* ws, hipStream_t st) {
   if (a.dtype == AWSRC_DTYPE_F32) return launch<float>(a, ws, st);

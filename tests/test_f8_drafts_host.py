@@ -186,8 +186,7 @@ VERIFY = dict(p=P, ldp=100, q=P, ldq=100, dtype=BF16, vocab=100, n_seq=3, n_rows
                                  dict(n_rows=1 << 31), dict(ldp=99), dict(ldq=99), dict(p=None), dict(tokens=None), dict(u=None),
                                  dict(cu=None), dict(tokens_out=None), dict(n_out=None), dict(keep=None), dict(kv_len=None),
                                  dict(p=P + 1), dict(q=P + 1), dict(cu=P + 2), dict(tokens=P + 1), dict(u=P + 2), dict(kv_len=P + 2),
-                                 dict(keep=P + 2), dict(tokens_out=P + 1), dict(n_out=P + 2), dict(n=None), dict(ws=P + 8),
-                                 dict(n_seq=(1 << 24) + 1)])
+                                 dict(keep=P + 2), dict(tokens_out=P + 1), dict(n_out=P + 2), dict(n=None), dict(n_seq=(1 << 24) + 1)])
 def test_verify_refuses(bad):
     assert _call(L.awsrc_verify_drafts, {**VERIFY, "n": _ws(1 << 40), **bad}) == EINVAL
 
@@ -195,11 +194,14 @@ def test_verify_refuses(bad):
 def test_verify_workspace_and_nothing():
     n = ctypes.c_size_t(0)
     none = dict(p=None, q=None, cu=None, tokens=None, u=None, kv_len=None, tokens_out=None, n_out=None, keep=None, ws=None)
-    for n_seq, vocab in ((1, 1), (3, 100), (64, 131072)):
+    for n_seq, vocab in ((1, 1), (3, 100), (3, 65537), (64, 131072)):
         shape = dict(n_seq=n_seq, vocab=vocab, ldp=vocab, ldq=vocab)
         assert _call(L.awsrc_verify_drafts, {**VERIFY, "n": ctypes.byref(n)}, **shape, **none) == OK
-        assert n.value == awsrc.verify_drafts_workspace_bytes(n_seq, vocab) > 0
-        assert _call(L.awsrc_verify_drafts, {**VERIFY, "n": _ws(n.value - 1)}, **shape) == ENOSPC
+        assert n.value == awsrc.verify_drafts_workspace_bytes(n_seq, vocab)
+        if n.value:
+            assert _call(L.awsrc_verify_drafts, {**VERIFY, "n": _ws(n.value - 1)}, **shape) == ENOSPC
+            assert _call(L.awsrc_verify_drafts, {**VERIFY, "n": _ws(n.value)}, ws=P + 8, **shape) == EINVAL
+    assert n.value > 0
     assert _call(L.awsrc_verify_drafts, {**VERIFY, "n": _ws(0)}, n_seq=0) == OK
 
 

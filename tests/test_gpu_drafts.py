@@ -220,7 +220,7 @@ def _check(p, q, tokens, u, cu):
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("with_q", [True, False])
-@pytest.mark.parametrize("V", [1, 2, 7, 255, 2047, 2049, 8191, 8193, 33001])
+@pytest.mark.parametrize("V", [1, 2, 7, 255, 2047, 2049, 8191, 8193, 33001, 65536, 65537, 70001, 140001])
 def test_verify(V, with_q, dtype):
     rng = np.random.default_rng(V + with_q)
     counts = [1, 5, 0, 2, 9, 1, 3, 0]
@@ -230,11 +230,12 @@ def test_verify(V, with_q, dtype):
 
 
 @pytest.mark.parametrize("with_q", [True, False])
-def test_verify_many_sequences_and_long_drafts(with_q):
+@pytest.mark.parametrize("V,more", [(50, 300), (65600, 5)])
+def test_verify_many_sequences_and_long_drafts(V, more, with_q):
     """More drafts than a wavefront has lanes, sequences beyond a workgroup's threads."""
     rng = np.random.default_rng(3)
-    counts = [200, 65, 66, 1] + [int(c) for c in rng.integers(0, 5, 300)]
-    p, q, tokens, u = _case(rng, counts, 50, torch.float32, with_q, agree=1.0)
+    counts = [200, 65, 66, 1] + [int(c) for c in rng.integers(0, 5, more)]
+    p, q, tokens, u = _case(rng, counts, V, torch.float32, with_q, agree=1.0)
     u[:330] *= 0.01  # long runs of accepted drafts
     _, count = _check(p, q, tokens, u, np.concatenate([[0], np.cumsum(counts)]))
     assert count[0] > 64
@@ -252,10 +253,11 @@ def test_verify_borders_of_the_random_numbers():
 
 
 @pytest.mark.parametrize("with_q", [True, False])
-def test_verify_values_that_cannot_be(with_q):
+@pytest.mark.parametrize("V", [700, 66001])
+def test_verify_values_that_cannot_be(V, with_q):
     """NaN and infinite probabilities, negative ones, drafts outside the vocabulary, rows of zeros."""
     rng = np.random.default_rng(1)
-    V, counts = 700, [4] * 12
+    counts = [4] * 12
     p, q, tokens, u = _case(rng, counts, V, torch.float32, with_q, agree=0.5)
     bad = [float("nan"), float("inf"), -float("inf"), -0.5]
     for r in range(len(tokens)):
@@ -311,9 +313,10 @@ def test_verify_follows_the_targets_distribution():
     assert ((second - p.double()).abs() <= 6 * (p.double() * (1 - p.double()) / int((count == 2).sum())).sqrt()).all()
 
 
-def test_verify_repeats_itself_and_can_be_captured():
+@pytest.mark.parametrize("V", [9001, 70003])
+def test_verify_repeats_itself_and_can_be_captured(V):
     rng = np.random.default_rng(2)
-    counts, V = [5, 1, 3, 4], 9001
+    counts = [5, 1, 3, 4]
     cu = _ints(np.concatenate([[0], np.cumsum(counts)]))
     p, q, tokens, u = _case(rng, counts, V, torch.float16, True)
     p, q, tokens, u = p.to(DEV), q.to(DEV), _ints(tokens), torch.from_numpy(u).to(DEV)
@@ -322,7 +325,7 @@ def test_verify_repeats_itself_and_can_be_captured():
     first = awsrc.awsrc_verify_drafts(p, tokens, u, cu, q=q)
     for value in (0, 255):
         scratch.fill_(value)
-        again = awsrc.awsrc_verify_drafts(p, tokens, u, cu, q=q, workspace=scratch[:need])
+        again = awsrc.awsrc_verify_drafts(p, tokens, u, cu, q=q, workspace=scratch[:need] if need else None)
         assert torch.equal(again[0], first[0]) and torch.equal(again[1], first[1]) and (scratch[need:] == value).all()
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
