@@ -737,7 +737,7 @@ template <int W, typename T, typename TO>
 hipError_t launch_linear_rows(const LinearF8Args& a, const void* X, int64_t ldx, hipStream_t st) {
   const auto k = k_linear_f8_rows<W, T, TO>;
   const size_t lds = linear_rows_lds(a.M, a.K);
-  if (lds > 65536) {
+  if (lds > 32768) {  // (beside the sums of 16 wavefronts)
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (e != hipSuccess) return e;
   }
@@ -835,7 +835,7 @@ bool linear_f8_fused(int64_t M, int64_t N, int64_t K) {
   // 2 x 5120 x 5120 10.4 and 12.5; 4 x 11008 x 2048 8.9 and 11.1; 8 x 11008 x 2048 11.4 and 11.4; 16 x 2048 x 2048 7.3 and 6.3
   // (but a launch that is not replayed from a graph costs the host 3); 4 x 2048 x 11008 13.1 and 13.8; 8 x 5120 x 5120 17.6
   // and 12.8; 16 x 11008 x 2048 16.6 and 11.8.
-  if (M == 1) return K <= 32768;
+  if (M == 1) return K <= 32768 && N <= (int64_t)1 << 26;  // (2^31 threads of a launch)
   return M <= 16 && N < 12288 && (M * K <= 16384 || (K <= 2048 && N <= 4096));
 }
 
