@@ -10,7 +10,9 @@
 // written only where more is given back than taken, when nothing is taken from it.
 //
 // Bound by latency: a few loads that wait for one another and the scans between
-// them.  Small steps run in one launch of one workgroup.
+// them.  Steps of at most 256 slots and 2048 rows run in one launch of one workgroup:
+// 48 sequences of up to 5 rows 5.4 us.  2048 slots with prompts, 325764 rows: 8.4 us (of which the
+// scan of one workgroup is all) + 10.4 for the rows, 16 bytes each.
 #include "serve_internal.h"
 
 namespace awsrc {

@@ -1,15 +1,18 @@
 // Drafted tokens against the target's probabilities.
 //
 // Only one row of p (and of q) is read whole for each sequence: the one that
-// its next token is drawn from, known from single entries of the rows before it.  Two
-// launches: sums of the weights over pieces of that row, every wavefront finding
-// the row by itself; then one workgroup a sequence finds the piece in which the running
-// sum passes its mark, and the token in it.  Sums in fp64: a product u q of fp32
-// numbers is exact there, and the order of adding moves a border between tokens
-// by 1e-16 of the whole.
+// its next token is drawn from, known from single entries of the rows before it.
+// Where one CU reads that row quickly enough, one workgroup a sequence does it all.
+// Longer rows take two launches: sums of the weights over pieces of the row, every
+// wavefront finding the row by itself; then one workgroup a sequence finds the piece in
+// which the running sum passes its mark, and the token in it.  Sums in fp64: a
+// product u q of fp32 numbers is exact there, and the order of adding moves a border
+// between tokens by 1e-16 of the whole.
 //
-// Bound by the rows' bytes for a batch, for one sequence by memory's latency: four
-// loads that wait for one another in the first launch, three in the second.
+// Bound by the rows' bytes for a batch, for one sequence by memory's latency: offsets,
+// tokens, their probabilities, the row and a piece of it again wait for one another.
+// One sequence of four drafts and 32768 tokens in fp32 6.8 us; 64 of 131072 with their
+// drafts' probabilities 9.4 (67 MB, 7 TB/s: some of it from the last level of cache) + 5.3.
 #include "serve_internal.h"
 
 namespace awsrc {
@@ -162,9 +165,9 @@ __global__ __launch_bounds__(kThreads) void k_verify_sums(VerifyArgs a, int piec
   if (first == 0 && lane == 0) places[s] = (int32_t)place;
 }
 
-// Small vocabularies: one workgroup a sequence does it all, without a workspace.  Every wavefront finds the row and sums
+// Rows that are not too long: one workgroup a sequence does it all, without a workspace.  Every wavefront finds the row and sums
 // pieces of it; the first one then draws, its lanes holding 32 tokens side by side.
-constexpr int kAlone = 32;  // pieces at most: 65536 tokens
+constexpr int kAlone = 64;  // pieces at most, one a lane
 constexpr int kAloneWaves = 16;
 
 template <typename T>
@@ -356,11 +359,17 @@ template <typename T>
 constexpr int kPieces = kPerWave<T> * kThreads / 64;  // of a workgroup of the first launch
 
 int64_t pieces_of(int64_t vocab) { return (vocab + kPiece - 1) / kPiece; }
-bool verify_alone(int64_t vocab) { return pieces_of(vocab) <= kAlone; }
+// A CU reads 131072 probabilities in as long as two launches take over the whole machine (64 sequences of 65536 tokens in
+// fp32 with their drafts' probabilities: 10.8 us, 11.0 in two; 200: 16.9 and 17.9; 64 in bf16 of 65537: 15.4 alone, 13.2 in
+// two; 64 of 131072 without drafts' probabilities 12.7, of 131073 in two 15.7; 300, two rounds of the machine, of 65536 in
+// fp32 25.3 and 22.1).
+bool verify_alone(int n_seq, int64_t vocab, bool with_q) {
+  return pieces_of(vocab) <= kAlone && vocab * (with_q ? 2 : 1) * ((n_seq + 255) / 256) <= kAlone * kPiece;
+}
 
 template <typename T>
 hipError_t launch(const VerifyArgs& a, void* ws, hipStream_t st) {
-  if (verify_alone(a.vocab)) {
+  if (verify_alone(a.n_seq, a.vocab, a.q != nullptr)) {
     hipLaunchKernelGGL((k_verify_alone<T>), grid_of<64 * kAloneWaves>(a.n_seq), dim3(64 * kAloneWaves), 0, st, a, (int)pieces_of(a.vocab));
     return hipGetLastError();
   }
@@ -375,8 +384,9 @@ hipError_t launch(const VerifyArgs& a, void* ws, hipStream_t st) {
 
 }  // namespace
 
+// (as for drafts with probabilities of their own, which a query does not know of)
 size_t verify_ws_bytes(int n_seq, int64_t vocab) {
-  return verify_alone(vocab) ? 0 : (size_t)n_seq * (pieces_of(vocab) * sizeof(double) + 4);
+  return verify_alone(n_seq, vocab, true) ? 0 : (size_t)n_seq * (pieces_of(vocab) * sizeof(double) + 4);
 }
 
 hipError_t launch_verify(const VerifyArgs& a, void* ws, hipStream_t st) {

@@ -194,7 +194,7 @@ def test_verify_refuses(bad):
 def test_verify_workspace_and_nothing():
     n = ctypes.c_size_t(0)
     none = dict(p=None, q=None, cu=None, tokens=None, u=None, kv_len=None, tokens_out=None, n_out=None, keep=None, ws=None)
-    for n_seq, vocab in ((1, 1), (3, 100), (3, 65537), (64, 131072)):
+    for n_seq, vocab in ((1, 1), (3, 100), (3, 65537), (257, 65537), (3, 131073), (64, 262144)):
         shape = dict(n_seq=n_seq, vocab=vocab, ldp=vocab, ldq=vocab)
         assert _call(L.awsrc_verify_drafts, {**VERIFY, "n": ctypes.byref(n)}, **shape, **none) == OK
         assert n.value == awsrc.verify_drafts_workspace_bytes(n_seq, vocab)

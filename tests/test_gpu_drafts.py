@@ -220,7 +220,7 @@ def _check(p, q, tokens, u, cu):
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("with_q", [True, False])
-@pytest.mark.parametrize("V", [1, 2, 7, 255, 2047, 2049, 8191, 8193, 33001, 65536, 65537, 70001, 140001])
+@pytest.mark.parametrize("V", [1, 2, 7, 255, 2047, 2049, 8191, 8193, 33001, 65536, 65537, 70001, 131072, 131073, 270001])
 def test_verify(V, with_q, dtype):
     rng = np.random.default_rng(V + with_q)
     counts = [1, 5, 0, 2, 9, 1, 3, 0]
@@ -253,7 +253,7 @@ def test_verify_borders_of_the_random_numbers():
 
 
 @pytest.mark.parametrize("with_q", [True, False])
-@pytest.mark.parametrize("V", [700, 66001])
+@pytest.mark.parametrize("V", [700, 3000, 66001])
 def test_verify_values_that_cannot_be(V, with_q):
     """NaN and infinite probabilities, negative ones, drafts outside the vocabulary, rows of zeros."""
     rng = np.random.default_rng(1)
@@ -313,7 +313,7 @@ def test_verify_follows_the_targets_distribution():
     assert ((second - p.double()).abs() <= 6 * (p.double() * (1 - p.double()) / int((count == 2).sum())).sqrt()).all()
 
 
-@pytest.mark.parametrize("V", [9001, 70003])
+@pytest.mark.parametrize("V", [9001, 140003])
 def test_verify_repeats_itself_and_can_be_captured(V):
     rng = np.random.default_rng(2)
     counts = [5, 1, 3, 4]
