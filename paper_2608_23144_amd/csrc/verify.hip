@@ -129,13 +129,13 @@ __device__ __forceinline__ double sum_of_piece(const Weights<T>& weights, int64_
   }
   if (!(of_lane(w, 63) < __builtin_inf())) {  // the row ends in here, the draft lies here, or a value is not finite
     w = 0.0;
-    for (int j = 0; j < kPiece / 512; ++j) {
-      const int64_t at = begin + (j * 64 + lane) * 8;
-      float x[8], y[8];
-      weights.load(at, x, y);
+    float x[kPiece / 512][8], y[kPiece / 512][8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) w += weights.of(at + e, x[e], y[e]);
-    }
+    for (int j = 0; j < kPiece / 512; ++j) weights.load(begin + (j * 64 + lane) * 8, x[j], y[j]);
+#pragma unroll
+    for (int j = 0; j < kPiece / 512; ++j)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w += weights.of(begin + (j * 64 + lane) * 8 + e, x[j][e], y[j][e]);
     w = scan_wave(w);
   }
   return w;
@@ -359,10 +359,10 @@ template <typename T>
 constexpr int kPieces = kPerWave<T> * kThreads / 64;  // of a workgroup of the first launch
 
 int64_t pieces_of(int64_t vocab) { return (vocab + kPiece - 1) / kPiece; }
-// A CU reads 131072 probabilities in as long as two launches take over the whole machine (64 sequences of 65536 tokens in
-// fp32 with their drafts' probabilities: 10.8 us, 11.0 in two; 200: 16.9 and 17.9; 64 in bf16 of 65537: 15.4 alone, 13.2 in
-// two; 64 of 131072 without drafts' probabilities 12.7, of 131073 in two 15.7; 300, two rounds of the machine, of 65536 in
-// fp32 25.3 and 22.1).
+// A CU reads 131072 probabilities in about as long as two launches take over the whole machine, and a launch less saves the
+// host 3 us.  64 sequences of 65536 tokens in fp32 with their drafts' probabilities: 10.7 us, of 65537 in two launches 10.9; 200:
+// 16.9 and 17.9; of 131072 in bf16 without them 64: 12.5 and 11.5, 200: 16.3 and 19.8.  A second round of the machine, 300 of
+// 65536 in fp32: 25.3 alone and 21.3 in two.
 bool verify_alone(int n_seq, int64_t vocab, bool with_q) {
   return pieces_of(vocab) <= kAlone && vocab * (with_q ? 2 : 1) * ((n_seq + 255) / 256) <= kAlone * kPiece;
 }
