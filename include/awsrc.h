@@ -727,7 +727,7 @@ typedef struct awsrc_page_pool {
  * hold.  Nothing outside the buffers is read or written, whatever they hold.  Calls on one pool
  * are ordered by `stream`.
  * n_seq <= 2^20, n_seq * table_ld < 2^31, max_rows < 2^31; page_tokens 16, 32, 64 or 128.
- * n_seq of 0 is a no-op (nothing is written).
+ * n_seq of 0 serves nobody (cu[0] is 0, rows -1, n_free_out the pool's n_free), and then the slots' buffers may be NULL.
  * Workspace: two-phase query as described above (the query needs no pointers but
  * `pool`); the size may be 0, and then no workspace is needed.
  */

@@ -1450,8 +1450,7 @@ extern "C" awsrc_status awsrc_kv_plan(const awsrc_page_pool* pool, int32_t n_seq
     *ws_bytes = need;
     return AWSRC_OK;
   }
-  if (n_seq == 0) return AWSRC_OK;
-  if (!pool->free_pages || !pool->n_free || !kv_len || !keep || !new_len || !page_table || !kv_len_out || !n_free_out || !cu)
+  if (!pool->free_pages || !pool->n_free || !n_free_out || !cu || (n_seq && (!kv_len || !keep || !new_len || !page_table || !kv_len_out)))
     return fail(AWSRC_EINVAL, "NULL buffer");
   if (misaligned(pool->free_pages, 4) || misaligned(pool->n_free, 4) || misaligned(kv_len, 4) || misaligned(keep, 4) ||
       misaligned(new_len, 4) || misaligned(page_table, 4) || misaligned(kv_len_out, 4) || misaligned(n_free_out, 4) ||

@@ -269,7 +269,7 @@ __global__ __launch_bounds__(256) void k_plan_rows(PlanArgs a, const PlanHead* h
 static bool plan_alone(int n_seq, int64_t max_rows) { return n_seq <= 256 && max_rows <= 2048; }
 
 size_t kv_plan_ws_bytes(int n_seq, int64_t max_rows) {
-  return n_seq && !plan_alone(n_seq, max_rows) ? 256 + (size_t)n_seq * (sizeof(PlanSlot) + 4) : 0;
+  return !plan_alone(n_seq, max_rows) ? 256 + (size_t)n_seq * (sizeof(PlanSlot) + 4) : 0;
 }
 
 hipError_t launch_kv_plan(const PlanArgs& a, void* ws, hipStream_t st) {

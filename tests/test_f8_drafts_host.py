@@ -175,7 +175,9 @@ def test_plan_workspace_and_nothing():
             assert _call(L.awsrc_kv_plan, {**PLAN, "pool": _pool(), "n": _ws(n.value)}, ws=None, **shape) == ENOSPC
             assert _call(L.awsrc_kv_plan, {**PLAN, "pool": _pool(), "n": _ws(n.value)}, ws=P + 4, **shape) == EINVAL
     assert n.value > 0
-    assert _call(L.awsrc_kv_plan, {**PLAN, "pool": _pool(), "n": _ws(0)}, n_seq=0) == OK
+    for missing in (dict(cu=None), dict(n_free_out=None)):  # without slots too
+        assert _call(L.awsrc_kv_plan, {**PLAN, "pool": _pool(), "n": _ws(0)}, n_seq=0, **missing) == EINVAL
+    assert _call(L.awsrc_kv_plan, {**PLAN, "pool": _pool(), "n": _ws(0)}, n_seq=0, max_rows=5000) == ENOSPC
 
 
 VERIFY = dict(p=P, ldp=100, q=P, ldq=100, dtype=BF16, vocab=100, n_seq=3, n_rows=7, cu=P, tokens=P, u=P, kv_len=P, tokens_out=P, n_out=P,

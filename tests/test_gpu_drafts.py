@@ -180,8 +180,13 @@ def test_plan_captured_and_replayed():
 def test_plan_of_nothing():
     pool = awsrc.make_page_pool(4, DEV)
     none = _ints([])
-    out = awsrc.awsrc_kv_plan(pool, none, none, none, torch.empty(0, 3, dtype=torch.int32, device=DEV), 16, 0)
-    assert out[0].shape == (1,) and pool[1].item() == 4
+    for rows in (0, 1, 7, 5003):
+        left = _ints([-1])
+        filled = (_ints([9]), _ints([9] * rows), _ints([9] * rows), _ints([9] * rows).long())
+        cu, *of_rows = awsrc.awsrc_kv_plan(pool, none, none, none, torch.empty(0, 3, dtype=torch.int32, device=DEV), 16, rows,
+                                           n_free_out=left, out=filled)
+        assert cu.tolist() == [0] and left.item() == 4 and all((t == -1).all() for t in of_rows)
+    assert pool[1].item() == 4 and pool[0].tolist() == [3, 2, 1, 0]
     cu, seq, pos, slot = awsrc.awsrc_kv_plan(pool, _ints([0]), _ints([0]), _ints([0]), _ints([[0, 0, 0]]), 16, 0)
     assert cu.tolist() == [0, 0] and seq.numel() == 0
 
