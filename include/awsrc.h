@@ -754,7 +754,7 @@ awsrc_status awsrc_kv_plan(const awsrc_page_pool* pool, int32_t n_seq, const int
  *          others.  q is not read at a sequence's last row.
  *  tokens  [n_rows] int32, u [n_rows] fp32, cu [n_seq + 1] int32 as for awsrc_kv_append.
  *  tokens_out  [n_rows] int32: from row cu[s] on the accepted drafts, then the token drawn, then
- *          -1.  Rows of no sequence are not written.  Does not overlap tokens.
+ *          -1.  Rows of no sequence are not written.  May be tokens.
  *  n_out   [n_seq] int32: how many there are, 1 to cu[s + 1] - cu[s]; 0 for a sequence without rows.
  *  kv_len, keep  both or neither NULL; [n_seq] int32: keep = kv_len - rows + n_out is what a cache
  *          that holds all of the step's rows keeps of them (awsrc_kv_plan takes it); may be one buffer.

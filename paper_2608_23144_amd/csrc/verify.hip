@@ -347,7 +347,8 @@ __global__ __launch_bounds__(kThreads) void k_verify_draw(VerifyArgs a, int piec
       token = s_token;
     }
   }
-  for (int64_t i = tid; i < rows.n; i += kThreads)
+  if (tid >= 64) return;  // (one wavefront: tokens_out may be tokens)
+  for (int64_t i = tid; i < rows.n; i += 64)
     a.tokens_out[rows.begin + i] = i < place ? a.tokens[rows.begin + i + 1] : i == place ? (int32_t)token : -1;
   if (tid == 0) {
     a.n_out[s] = (int32_t)(place + 1);

@@ -220,6 +220,10 @@ def _check(p, q, tokens, u, cu):
     end = cu[-1]
     assert np.array_equal(out.cpu().numpy()[:end], want[:end])
     assert np.array_equal(keep.cpu().numpy(), kv - np.diff(cu) + count)
+    here, same = _ints(tokens), _ints(kv)  # over the tokens, and over the lengths
+    awsrc.awsrc_verify_drafts(p.to(DEV), here, torch.from_numpy(u).to(DEV), _ints(cu), q=None if q is None else q.to(DEV),
+                              kv_len=same, keep=same, out=(here, torch.empty_like(n)))
+    assert torch.equal(here[:end], out[:end]) and torch.equal(same, keep)
     return want, count
 
 
