@@ -5,10 +5,10 @@
 // operations, so that the codes are the recipe's to the bit.
 //
 // Bound by memory: every value is read once and kept in registers between its block's
-// largest magnitude and its code.  Weights of 2048 x 11008 in bf16 to codes 17.7 us
-// (68 MB, 3.8 TB/s: the launch is too short for a copy's 4.9), back 11.1; 5003 x 27001 in
-// fp32 163 us (676 MB, 4.1 TB/s) and 111 (6.1).  Activations of 64 x 5120 are 4 us of latency,
-// of 8192 x 5120 in bf16 23 to 30 us (126 MB).
+// largest magnitude and its code.  From memory, to codes and back: weights of 5120 x 27648 in
+// bf16 81 and 78 us (425 MB, 5.2 and 5.4 TB/s; a copy does 4.9), of 5003 x 27001 in fp32 129
+// and 125, of 2048 x 11008 in bf16 16.6 and 16.2 (68 MB: too short for that rate).
+// Activations of 64 x 5120 are 2.7 us of latency, of 8192 x 5120 in bf16 27 us (126 MB).
 #include "serve_internal.h"
 
 namespace awsrc {
@@ -47,6 +47,40 @@ __device__ __forceinline__ void load_part(const T* __restrict__ x, Part<T> p, in
     }
   } else {
     load8_any(x + p.at, n - p.at, v);
+  }
+}
+
+// The same of eight rows, all of whose loads are on their way before a value is converted.
+template <typename T>
+__device__ __forceinline__ void load_parts(const T* const (&x)[8], Part<T> p, int64_t n, float (&v)[8][8]) {
+  constexpr int kPer = 16 / sizeof(T), kLoads = 8 / kPer;
+  typedef T V __attribute__((ext_vector_type(16 / sizeof(T)), aligned(sizeof(T))));
+  if (p.at + Part<T>::second + 4 <= n) {
+    V w[8][kLoads];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int h = 0; h < kLoads; ++h) w[i][h] = *reinterpret_cast<const V*>(x[i] + p.at + h * Part<T>::second);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[i][e] = to_f32((T)w[i][e / kPer][e % kPer]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {  // (two rows at a time: their addresses take registers)
+      T w[2][8];
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        const int e = j & 7, at = p.at + (e < 4 ? e : Part<T>::second + e - 4);
+        w[j >> 3][e] = x[i + (j >> 3)][at < n ? at : 0];
+      }
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        const int e = j & 7, at = p.at + (e < 4 ? e : Part<T>::second + e - 4);
+        v[i + (j >> 3)][e] = at < n ? to_f32(w[j >> 3][e]) : 0.0f;
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
   }
 }
 
@@ -109,7 +143,8 @@ __global__ __launch_bounds__(256) void k_quantize_blocks_row(const T* __restrict
   }
 }
 
-// Blocks of 128 x 128, one a workgroup, held in registers between its largest magnitude and its codes.
+// Blocks of 128 x 128, one a workgroup, held in registers between its largest magnitude and its codes (2048 x 11008 in bf16:
+// 21.2 us where a row's values are converted before the next row is asked for).
 template <typename T>
 __global__ __launch_bounds__(256) void k_quantize_blocks_square(const T* __restrict__ X, int64_t rows, int64_t cols,
                                                                 int64_t ldx, uint8_t* __restrict__ codes, int64_t ldc,
@@ -120,12 +155,11 @@ __global__ __launch_bounds__(256) void k_quantize_blocks_square(const T* __restr
   const int64_t rb = wg / col_blocks, cb = wg % col_blocks;
   const int64_t row0 = rb * kBlockF8 + (threadIdx.x >> 4), at = cb * kBlockF8;
   const Part<T> part(threadIdx.x);
-  float v[8][8];
+  const T* x[8];  // (rows past the end count the last one twice)
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int64_t row = row0 + 16 * i;
-    load_part(X + (row < rows ? row : rows - 1) * ldx + at, part, cols - at, v[i]);  // (rows past the end count the last one twice)
-  }
+  for (int i = 0; i < 8; ++i) x[i] = X + (row0 + 16 * i < rows ? row0 + 16 * i : rows - 1) * ldx + at;
+  float v[8][8];
+  load_parts(x, part, cols - at, v);
   float m = 0.0f;
 #pragma unroll
   for (int i = 0; i < 8; ++i)
