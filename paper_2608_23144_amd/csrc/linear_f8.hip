@@ -100,8 +100,8 @@ __device__ __forceinline__ void store4(TO* o, const float (&y)[4], int64_t n, in
 // of block 1, the second half of block 0 and of block 1 for g = 0 to 3.  Groups 0 and 1, 2 and 3
 // trade halves of those with one instruction a register: 32 bytes of each block.
 //
-// 13 x 2048 x 11008 (23 MB): 7.3 us with the weights in the caches, 10.6 to 11 from memory, of which 3.7 are their
-// bytes: 128 workgroups of 8 wavefronts do not keep enough on its way for more.
+// 13 x 2048 x 11008 (23 MB): 6.9 us with the weights in the caches, 10.1 from memory, of which 3.7 are their
+// bytes: 128 workgroups do not keep enough on its way for more.
 struct Quads {
   static constexpr int kRound = 2 * kBlockF8;  // bytes of a row that a wavefront takes at a time
   i32x4 v[4];
@@ -812,7 +812,12 @@ hipError_t launch(const LinearF8Args& a, void* ws, hipStream_t st) {
   const bool once = a.M <= 64 && a.N * a.K >= (int64_t)1 << 26;
   constexpr bool kWide = sizeof(TO) == 4;  // operands as fp16: twice the registers
   switch (c.path) {
-    case kRows: return a.M <= 16 ? launch_rows<8, 1, TO>(a, st) : launch_rows<8, 2, TO>(a, st);
+    case kRows:
+      // sixteen wavefronts where the workgroups leave CUs idle and the sum is long (13 x 2048 x 11008: 11.0 and 10.1; 16 x 4096 x
+      // 4096 6.6 and 6.3; 5 x 5120 x 5120 9.6 and 10.3; for fp32 they do not have the registers)
+      if constexpr (!kWide)
+        if (a.M <= 16 && a.N <= 4096 && a.K >= 4096) return launch_rows<16, 1, TO>(a, st);
+      return a.M <= 16 ? launch_rows<8, 1, TO>(a, st) : launch_rows<8, 2, TO>(a, st);
     case kTile32:
       return once ? launch_tile<32, 64, 32, 32, 2, 4, true, true, TO>(a, c.split, ws, st)
                   : launch_tile<32, 64, 32, 32, 2, 4, true, false, TO>(a, c.split, ws, st);
