@@ -131,6 +131,9 @@ __device__ __forceinline__ void plan_rows(const PlanArgs& a, const PlanHead& h, 
   }
 }
 
+template <int N>
+using Ints = int32_t __attribute__((ext_vector_type(N), aligned(4)));
+
 // A thread takes I slots side by side, whose loads are on their way together.  ALONE: the rows too, for at most 64 W I slots.
 template <int W, int I, bool ALONE>
 __global__ __launch_bounds__(64 * W) void k_plan_scan(PlanArgs a, PlanHead* head, PlanSlot* slots, int32_t* gives) {
@@ -144,17 +147,23 @@ __global__ __launch_bounds__(64 * W) void k_plan_scan(PlanArgs a, PlanHead* head
   n_free = n_free < 0 ? 0 : n_free < a.pool.n_pages ? n_free : a.pool.n_pages;
   Lengths l[I];
   const auto read = [&](int s0) {
-    int32_t v[I][3];
+    Ints<I> kv = {}, keep = {}, fresh = {};
+    const int s = s0 + tid * I;
+    if (s + I <= a.n_seq) {
+      kv = *reinterpret_cast<const Ints<I>*>(a.kv_len + s);
+      keep = *reinterpret_cast<const Ints<I>*>(a.keep + s);
+      fresh = *reinterpret_cast<const Ints<I>*>(a.new_len + s);
+    } else {
 #pragma unroll
-    for (int i = 0; i < I; ++i) {
-      const int s = s0 + tid * I + i;
-      const bool live = s < a.n_seq;
-      v[i][0] = live ? a.kv_len[s] : 0;
-      v[i][1] = live ? a.keep[s] : 0;
-      v[i][2] = live ? a.new_len[s] : 0;
+      for (int i = 0; i < I; ++i)
+        if (s + i < a.n_seq) {
+          kv[i] = a.kv_len[s + i];
+          keep[i] = a.keep[s + i];
+          fresh[i] = a.new_len[s + i];
+        }
     }
 #pragma unroll
-    for (int i = 0; i < I; ++i) l[i] = lengths_of(v[i][0], v[i][1], v[i][2], a.table_ld, shift);
+    for (int i = 0; i < I; ++i) l[i] = lengths_of(kv[i], keep[i], fresh[i], a.table_ld, shift);
   };
   // what all slots give back, before anyone is turned away
   int64_t back[1] = {0}, spare[1];
@@ -196,26 +205,39 @@ __global__ __launch_bounds__(64 * W) void k_plan_scan(PlanArgs a, PlanHead* head
     const int64_t take_here = y[0], give_here = y[1], rows_here = y[2];
     scan_workgroup<W, 3>(y, sum, sums[2]);
     int64_t take = taken + y[0] - take_here, give = given + y[1] - give_here, row = rows + y[2] - rows_here;
+    Ints<I> kv_out, cu, starts;
+    const bool whole = s0 + tid * I + I <= a.n_seq;
 #pragma unroll
     for (int i = 0; i < I; ++i) {
       const int s = s0 + tid * I + i;
       const PlanSlot q = {(int32_t)l[i].held, (int32_t)(take - l[i].held), (int32_t)(l[i].keep - row),
                           (int32_t)(s * a.table_ld + l[i].want - give)};
+      kv_out[i] = (int32_t)(l[i].keep + l[i].fresh);
+      cu[i] = (int32_t)(row + l[i].fresh);
+      starts[i] = (int32_t)give;
       if (s < a.n_seq) {
-        a.kv_out[s] = (int32_t)(l[i].keep + l[i].fresh);
-        a.cu[s + 1] = (int32_t)(row + l[i].fresh);
         if constexpr (ALONE) {
           s_slots[s] = q;
-          s_give[s] = (int32_t)give;
-          s_cu[s + 1] = (int32_t)(row + l[i].fresh);
+          s_give[s] = starts[i];
+          s_cu[s + 1] = cu[i];
         } else {
           slots[s] = q;
-          gives[s] = (int32_t)give;
+          if (!whole) gives[s] = starts[i];
+        }
+        if (!whole) {
+          a.kv_out[s] = kv_out[i];
+          a.cu[s + 1] = cu[i];
         }
       }
       take += l[i].want > l[i].held ? l[i].want - l[i].held : 0;
       give += l[i].held > l[i].want ? l[i].held - l[i].want : 0;
       row += l[i].fresh;
+    }
+    if (whole) {
+      const int s = s0 + tid * I;
+      *reinterpret_cast<Ints<I>*>(a.kv_out + s) = kv_out;
+      *reinterpret_cast<Ints<I>*>(a.cu + s + 1) = cu;
+      if (!ALONE) *reinterpret_cast<Ints<I>*>(gives + s) = starts;
     }
     taken += sum[0];
     given += sum[1];

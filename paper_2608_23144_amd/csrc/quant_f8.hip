@@ -104,42 +104,32 @@ __device__ __forceinline__ void store_part(uint8_t* __restrict__ c, Part<T> p, i
 }
 
 // Blocks of 1 x 128: sixteen lanes a block, eight values each; a wavefront
-// takes 512 columns of RW rows, whose loads are on their way together.
-template <typename T, int RW>
+// takes 512 columns of a row.
+template <typename T>
 __global__ __launch_bounds__(256) void k_quantize_blocks_row(const T* __restrict__ X, int64_t rows, int64_t cols, int64_t ldx,
                                                              uint8_t* __restrict__ codes, int64_t ldc,
                                                              float* __restrict__ scale, uint32_t strips, int64_t n_wg) {
-  constexpr int R = 4 * RW;  // rows of a workgroup
+  constexpr int R = 4;  // rows of a workgroup
   __shared__ float s_scale[4][R];
   const uint32_t wg = workgroup<256>();
   if (wg >= n_wg) return;
-  const int64_t row0 = (int64_t)(wg / strips) * R;
+  const int64_t row0 = (int64_t)(wg / strips) * R, row = row0 + (threadIdx.x >> 6);
   const int64_t strip = wg % strips;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63;
   const int64_t at = strip * 512 + (lane >> 4) * kBlockF8;  // the first column of this lane's block
   const Part<T> part(lane);
-  float v[RW][8];
+  float v[8], m = 0.0f;
+  load_part(X + (row < rows ? row : rows - 1) * ldx + at, part, cols - at, v);
 #pragma unroll
-  for (int i = 0; i < RW; ++i) {
-    const int64_t row = row0 + wave * RW + i;
-    load_part(X + (row < rows ? row : rows - 1) * ldx + at, part, cols - at, v[i]);
-  }
-#pragma unroll
-  for (int i = 0; i < RW; ++i) {
-    const int64_t row = row0 + wave * RW + i;
-    float m = 0.0f;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) m = amax_keep(m, v[i][e]);
-    const float s = scale_of_amax_f8(amax_of_16(m));
-    const uint2 w = codes8_f8(v[i], inverse_scale(s), s > 0.0f);
-    if (row < rows) store_part(codes + row * ldc + at, part, cols - at, w);
-    if ((lane & 15) == 0) s_scale[lane >> 4][wave * RW + i] = s;
-  }
+  for (int e = 0; e < 8; ++e) m = amax_keep(m, v[e]);
+  const float s = scale_of_amax_f8(amax_of_16(m));
+  if (row < rows) store_part(codes + row * ldc + at, part, cols - at, codes8_f8(v, inverse_scale(s), s > 0.0f));
+  if ((lane & 15) == 0) s_scale[lane >> 4][threadIdx.x >> 6] = s;
   __syncthreads();
   const int64_t blocks = (cols + kBlockF8 - 1) / kBlockF8;
   for (int i = threadIdx.x; i < 4 * R; i += 256) {
-    const int64_t b = strip * 4 + i / R, row = row0 + i % R;
-    if (b < blocks && row < rows) scale[b * rows + row] = s_scale[i / R][i % R];
+    const int64_t b = strip * 4 + i / R, r = row0 + i % R;
+    if (b < blocks && r < rows) scale[b * rows + r] = s_scale[i / R][i % R];
   }
 }
 
@@ -246,7 +236,7 @@ hipError_t launch(const void* X, int64_t rows, int64_t cols, int64_t ldx, int bl
     const uint32_t strips = (uint32_t)((cols + 511) / 512);
     const int64_t n = (rows + 3) / 4 * strips;
     if (n >= (int64_t)1 << 31) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((k_quantize_blocks_row<T, 1>), grid_of<256>(n), dim3(256), 0, st, x, rows, cols, ldx, codes, ldc, scale,
+    hipLaunchKernelGGL((k_quantize_blocks_row<T>), grid_of<256>(n), dim3(256), 0, st, x, rows, cols, ldx, codes, ldc, scale,
                        strips, n);
   } else {
     const uint32_t cb = (uint32_t)((cols + kBlockF8 - 1) / kBlockF8);
