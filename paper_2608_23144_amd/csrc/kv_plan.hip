@@ -10,9 +10,9 @@
 // written only where more is given back than taken, when nothing is taken from it.
 //
 // Bound by latency: a few loads that wait for one another and the scans between
-// them.  Steps of at most 256 slots and 2048 rows run in one launch of one workgroup:
-// 48 sequences of up to 5 rows 5.4 us.  2048 slots with prompts, 325764 rows: 8.4 us (of which the
-// scan of one workgroup is all) + 10.4 for the rows, 16 bytes each.
+// them.  Steps of at most 2048 slots and 8192 rows run in one launch of one workgroup:
+// 48 sequences of up to 5 rows 5.4 us, 2048 with 2051 rows 9.4.  2048 slots with prompts, 325764
+// rows: 17.4 us in two launches, 7 of them the scan by one workgroup.
 #include "serve_internal.h"
 
 namespace awsrc {
@@ -287,17 +287,26 @@ __global__ __launch_bounds__(256) void k_plan_rows(PlanArgs a, const PlanHead* h
 
 }  // namespace
 
-// One workgroup does it all where its threads have a slot and a few rows each.
-static bool plan_alone(int n_seq, int64_t max_rows) { return n_seq <= 256 && max_rows <= 2048; }
+// One workgroup does it all where its threads have a few slots and rows each (in one launch and in two: 300 slots with 1499
+// rows 9.2 and 12.5 us, 1000 with 5001 12.4 and 14.2, 2048 with 6147 13.1 and 14.4; 1000 with 8998 16.1 and 14.3, but a launch
+// costs the host 3).
+static bool plan_alone(int n_seq, int64_t max_rows) { return n_seq <= 2048 && max_rows <= 8192; }
 
 size_t kv_plan_ws_bytes(int n_seq, int64_t max_rows) {
   return !plan_alone(n_seq, max_rows) ? 256 + (size_t)n_seq * (sizeof(PlanSlot) + 4) : 0;
 }
 
+template <int W, int I>
+static hipError_t launch_alone(const PlanArgs& a, hipStream_t st) {
+  hipLaunchKernelGGL((k_plan_scan<W, I, true>), dim3(1), dim3(64 * W), 0, st, a, (PlanHead*)nullptr, (PlanSlot*)nullptr, (int32_t*)nullptr);
+  return hipGetLastError();
+}
+
 hipError_t launch_kv_plan(const PlanArgs& a, void* ws, hipStream_t st) {
   if (plan_alone(a.n_seq, a.max_rows)) {
-    hipLaunchKernelGGL((k_plan_scan<4, 1, true>), dim3(1), dim3(256), 0, st, a, (PlanHead*)nullptr, (PlanSlot*)nullptr, (int32_t*)nullptr);
-    return hipGetLastError();
+    // (200 slots with 994 rows by four wavefronts 7.0 us; with 1783 10.0, with 3371 by sixteen 9.1)
+    if (a.n_seq <= 256 && a.max_rows <= 1024) return launch_alone<4, 1>(a, st);
+    return a.n_seq <= 1024 ? launch_alone<16, 1>(a, st) : launch_alone<16, 2>(a, st);
   }
   PlanHead* head = static_cast<PlanHead*>(ws);
   PlanSlot* slots = reinterpret_cast<PlanSlot*>(static_cast<char*>(ws) + 256);

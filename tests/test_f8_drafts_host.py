@@ -166,7 +166,7 @@ def test_plan_refuses(bad):
 def test_plan_workspace_and_nothing():
     n = ctypes.c_size_t(0)
     none = dict(kv_len=None, keep=None, new_len=None, table=None, kv_out=None, n_free_out=None, cu=None, seq=None, pos=None, slot=None, ws=None)
-    for n_seq, rows in ((1, 100000), (5, 9), (300, 9), (3000, 0)):
+    for n_seq, rows in ((1, 100000), (5, 9), (300, 9), (2048, 8192), (2048, 8193), (3000, 0)):
         shape = dict(n_seq=n_seq, max_rows=rows)
         assert _call(L.awsrc_kv_plan, {**PLAN, "pool": _pool(), "n": ctypes.byref(n)}, **shape, **none) == OK
         assert n.value == awsrc.kv_plan_workspace_bytes(n_seq, rows)
@@ -177,7 +177,7 @@ def test_plan_workspace_and_nothing():
     assert n.value > 0
     for missing in (dict(cu=None), dict(n_free_out=None)):  # without slots too
         assert _call(L.awsrc_kv_plan, {**PLAN, "pool": _pool(), "n": _ws(0)}, n_seq=0, **missing) == EINVAL
-    assert _call(L.awsrc_kv_plan, {**PLAN, "pool": _pool(), "n": _ws(0)}, n_seq=0, max_rows=5000) == ENOSPC
+    assert _call(L.awsrc_kv_plan, {**PLAN, "pool": _pool(), "n": _ws(0)}, n_seq=0, max_rows=9000) == ENOSPC
 
 
 VERIFY = dict(p=P, ldp=100, q=P, ldq=100, dtype=BF16, vocab=100, n_seq=3, n_rows=7, cu=P, tokens=P, u=P, kv_len=P, tokens_out=P, n_out=P,

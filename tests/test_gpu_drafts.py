@@ -68,6 +68,19 @@ def test_plan_over_many_steps(n_seq, page, width, n_pages):
     assert served and (refused or n_seq == 3)
 
 
+@pytest.mark.parametrize("n_seq,rows", [(100, 1024), (100, 1025), (256, 1000), (256, 8192), (256, 8193), (257, 300), (1000, 8000), (1024, 5000),
+                                        (1025, 1500), (2047, 8192), (2048, 8192), (2048, 8193), (2049, 4000)])
+def test_plan_of_decode_steps(n_seq, rows):
+    """Every sequence at work with about as many rows as there is room for: both sides of the bounds between launches."""
+    rng = np.random.default_rng(n_seq + rows)
+    server = Server(rng, n_seq, 32, 12, n_seq * 6)
+    most = 2 * rows // n_seq + 1
+    for i in range(5):
+        keep = np.maximum(0, server.kv - rng.integers(0, 5, n_seq)) * (rng.random(n_seq) > 0.1)
+        server.step(keep, rng.integers(0, most, n_seq), rows)
+        assert sorted(server.held() + server.free) == list(range(n_seq * 6))
+
+
 def test_plan_longer_than_the_pool_and_the_table():
     """A slot that is not served gives up what it does not keep; slots after it that need no page are served."""
     rng = np.random.default_rng(5)
@@ -180,7 +193,7 @@ def test_plan_captured_and_replayed():
 def test_plan_of_nothing():
     pool = awsrc.make_page_pool(4, DEV)
     none = _ints([])
-    for rows in (0, 1, 7, 5003):
+    for rows in (0, 1, 7, 5003, 9001):
         left = _ints([-1])
         filled = (_ints([9]), _ints([9] * rows), _ints([9] * rows), _ints([9] * rows).long())
         cu, *of_rows = awsrc.awsrc_kv_plan(pool, none, none, none, torch.empty(0, 3, dtype=torch.int32, device=DEV), 16, rows,
