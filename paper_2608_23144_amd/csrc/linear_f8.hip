@@ -781,9 +781,10 @@ Choice choose(int64_t M, int64_t N, int64_t K) {
   // Up to 16 rows: 16 columns a workgroup, up to about three of them a CU (16 x 2048 x 11008: 11.6, tiles 12.9 with their
   // sums split; 16 x 11008 x 2048: 9.0 and 8.9; 16 x 13824 x 5120: 19.8 and 16.0).
   if (M <= 16 && N < 12288) return {kRows, 1};
-  // Up to 32 rows of weights that are not too large (32 x 4096 x 4096: 8.6 and 11.0; 24 x 5120 x 5120: 15.1 and 13.1; 32 x
-  // 8192 x 8192: 24.7 and 21.5).
-  if (M > 16 && M <= 32 && N * K <= 20000000) return {kRows, 1};
+  // Up to 32 rows of weights that are not too large, nor with too many columns (32 x 4096 x 4096: 8.6 and 11.0; 24 x 5120 x 5120:
+  // 15.1 and 13.1; 32 x 8192 x 8192: 24.7 and 21.5; 24 x 8192 x 2400: 8.5 and 9.3; 24 x 11008 x 1024: 7.4 and 6.3; 24 x 27648 x
+  // 512: 13.0 and 6.3).
+  if (M > 16 && M <= 32 && N * K <= 20000000 && N <= 8192) return {kRows, 1};
   const int64_t t128 = tiles(128, 128), t256 = tiles(256, 256);
   // 128 x 128 tiles, two workgroups a CU, or 256 x 256, one: a round of 256 of the large ones costs what 2.6 times as many
   // small ones do (512 x 27648 x 5120: 116 and 82; 1024 x 5120 x 5120: 50 and 71; 4096 x 5120 x 5120: 135 and 141; 2048 x
@@ -796,12 +797,21 @@ Choice choose(int64_t M, int64_t N, int64_t K) {
   // 64 x 27648 x 5120: 64 x 64 tiles 38.4, 64 x 128 tiles 30.7 (64 x 11008 x 2048: 9.5 and 11.9)
   if (M > 32 && tiles(64, 128) >= 192) return {kTile64Wide, 1};
   const Path path = M > 32 ? kTile64 : kTile32;
-  // Few tiles under a long sum: parts of at least 16 steps, joined by a second launch (64 x 2048 x 11008: 30 whole, 15 in 5
-  // parts; 256 x 2048 x 11008: 28 and 21 in 2; 32 x 2048 x 27648: 63 and 19 in 8; 64 x 2560 x 2048: 7.9 whole, 9.1 in 2)
-  const int64_t t = path == kTile64 ? tiles(64, 64) : tiles(32, 64);
-  const int64_t want = (256 + t - 1) / t, most = (K + kStep - 1) / kStep / 16;
-  const int64_t split = want < most ? want : most;
-  return {path, t <= 128 && split > 1 ? (int)split : 1};
+  // Few tiles under a long sum: as many parts as cost least, joined by a second launch.  A step costs 0.25 us, into fp32 0.41;
+  // the join 2.1, 0.3 more a part and what the parts' bytes take (64 x 2048 x 11008: 26 whole, 13.8 in 8 parts, 17.5 in 16; 256
+  // x 1024 x 4096: 12.5, 11.4 in 4, 14.2 in 8; 128 x 2048 x 2048: 8.4 whole, 9.9 in 2).
+  const int64_t t = path == kTile64 ? tiles(64, 64) : tiles(32, 64), steps = (K + kStep - 1) / kStep;
+  const double step = 0.33, bytes = 1.8e-6 * (double)M * (double)N;
+  Choice best = {path, 1};
+  double least = step * (double)steps;
+  for (int s = 2; s <= 16 && s * t <= 256; ++s) {
+    const double us = 2.1 + 0.3 * s + step * (double)((steps + s - 1) / s) + bytes * s;
+    if (us < least) {
+      least = us;
+      best.split = s;
+    }
+  }
+  return best;
 }
 
 template <typename TO>
