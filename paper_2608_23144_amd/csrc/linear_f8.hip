@@ -818,7 +818,7 @@ template <typename TO>
 hipError_t launch(const LinearF8Args& a, void* ws, hipStream_t st) {
   const Choice c = choose(a.M, a.N, a.K);
   // Weights read once that fill a good part of the last cache go past it (64 x 27648 x 5120: 34.4, 30.7 past it; 16 x 13824 x
-  // 5120 17.6 and 16.0).
+  // 5120 17.6 and 16.0; 64 x 8192 x 8192 22.3 and 19.8; in the caches 64 x 13824 x 5120 15.7 and 18.0).
   const bool once = a.M <= 64 && a.N * a.K >= (int64_t)1 << 26;
   constexpr bool kWide = sizeof(TO) == 4;  // operands as fp16: twice the registers
   switch (c.path) {
@@ -831,7 +831,9 @@ hipError_t launch(const LinearF8Args& a, void* ws, hipStream_t st) {
     case kTile32:
       return once ? launch_tile<32, 64, 32, 32, 2, 4, true, true, TO>(a, c.split, ws, st)
                   : launch_tile<32, 64, 32, 32, 2, 4, true, false, TO>(a, c.split, ws, st);
-    case kTile64: return launch_tile<64, 64, 32, 32, 2, 4, true, false, TO>(a, c.split, ws, st);
+    case kTile64:
+      return once ? launch_tile<64, 64, 32, 32, 2, 4, true, true, TO>(a, c.split, ws, st)
+                  : launch_tile<64, 64, 32, 32, 2, 4, true, false, TO>(a, c.split, ws, st);
     case kTile64Wide:
       return once ? launch_tile<64, 128, 32, 64, 2, 3, kWide, true, TO>(a, 1, ws, st)
                   : launch_tile<64, 128, 32, 64, 2, 3, kWide, false, TO>(a, 1, ws, st);
