@@ -112,9 +112,13 @@ struct Quads {
 #pragma unroll
     for (int u = 0; u < 4; ++u) p[u] = row((lane & 12) + u) + ((g & 1) * kBlockF8 + (g >> 1) * 64) + 16 * (lane & 3);
   }
+  template <bool ONCE>  // past the caches
   __device__ __forceinline__ void load(const uint8_t* const (&p)[4], int k) {
 #pragma unroll
-    for (int u = 0; u < 4; ++u) v[u] = *reinterpret_cast<const i32x4*>(p[u] + k);
+    for (int u = 0; u < 4; ++u) {
+      const i32x4* w = reinterpret_cast<const i32x4*>(p[u] + k);
+      v[u] = ONCE ? __builtin_nontemporal_load(w) : *w;
+    }
   }
   // lane j of a quad gets as v[i] what lane i of it loaded as v[j], then the groups trade
   template <typename Op>
@@ -149,7 +153,7 @@ struct Quads {
   }
 };
 
-template <int W, int R, bool AHEAD, typename TO>
+template <int W, int R, bool AHEAD, bool ONCE, typename TO>
 struct RowSums {
   using Op = Operand<sizeof(TO) == 4>;
   const uint8_t* pb[4];      // this lane's pieces of the weights
@@ -176,10 +180,10 @@ struct RowSums {
     }
   }
   __device__ __forceinline__ void load(int buf, int k) {
-    fb[buf].load(pb, k);
+    fb[buf].template load<ONCE>(pb, k);
     if constexpr (AHEAD)
 #pragma unroll
-      for (int j = 0; j < R; ++j) fa[buf][j].load(pa[j], k);
+      for (int j = 0; j < R; ++j) fa[buf][j].template load<false>(pa[j], k);
   }
   __device__ __forceinline__ int rounds() const { return K / Quads::kRound; }
   __device__ __forceinline__ void begin() {
@@ -259,11 +263,11 @@ struct RowSums {
 };
 
 // On activation codes in memory.
-template <int W, int R, typename TO>
+template <int W, int R, bool ONCE, typename TO>
 __global__ __launch_bounds__(64 * W) void k_matmul_f8_rows(LinearF8Args a) {
   __shared__ fl4 part[W][R][64];
   const int64_t n0 = (int64_t)blockIdx.x * 16;
-  RowSums<W, R, true, TO> sums(a, n0, threadIdx.x & 63, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), a.A, a.lda);
+  RowSums<W, R, true, ONCE, TO> sums(a, n0, threadIdx.x & 63, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), a.A, a.lda);
   sums.begin();
   sums.run([&](int b, int m) { return a.a_scale[(int64_t)b * a.M + (m < a.M ? m : a.M - 1)]; });
   sums.finish(a, n0, part);
@@ -273,13 +277,13 @@ __global__ __launch_bounds__(64 * W) void k_matmul_f8_rows(LinearF8Args a) {
 // quant_f8.hip does, sixteen lanes a block), while its first weights are on their way, which saves a
 // launch and its wait.  1 x 2560 x 2048 (5.3 MB) 4.2 us, 3.4 with the weights in the caches: one wait for X, one for the
 // weights, and the wavefronts' meeting.
-template <int W, typename T, typename TO>
+template <int W, bool ONCE, typename T, typename TO>
 __global__ __launch_bounds__(64 * W) void k_linear_f8_rows(LinearF8Args a, const T* X, int64_t ldx, int pitch) {
   __shared__ fl4 part[W][1][64];
   extern __shared__ __attribute__((aligned(16))) uint8_t codes[];  // [M][pitch], then scales [blocks][16]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t n0 = (int64_t)blockIdx.x * 16;
-  RowSums<W, 1, false, TO> sums(a, n0, lane, wave, codes, pitch);
+  RowSums<W, 1, false, ONCE, TO> sums(a, n0, lane, wave, codes, pitch);
   sums.begin();
   const int M = (int)a.M, K = (int)a.K, blocks = (K + kBlockF8 - 1) / kBlockF8;
   float* scales = reinterpret_cast<float*>(codes + M * pitch);
@@ -738,15 +742,21 @@ size_t linear_rows_lds(int64_t M, int64_t K) {
   return (size_t)M * linear_rows_pitch(K) + (size_t)((K + kBlockF8 - 1) / kBlockF8) * 64;
 }
 
+// Weights read once that fill a good part of the last cache go past it (64 x 27648 x 5120: 34.4, 30.7 past it; 16 x 13824 x
+// 5120 17.6 and 16.0; 64 x 8192 x 8192 22.3 and 19.8; 1 x 27648 x 5120 29.0 and 26.4; 1 x 8192 x 8192 16.1 and 14.7; in the
+// caches 64 x 13824 x 5120 15.7 and 18.0).
+bool weights_once(int64_t M, int64_t N, int64_t K) { return M <= 64 && N * K >= (int64_t)1 << 26; }
+
 template <int W, int R, typename TO>
 hipError_t launch_rows(const LinearF8Args& a, hipStream_t st) {
-  hipLaunchKernelGGL((k_matmul_f8_rows<W, R, TO>), dim3((unsigned)((a.N + 15) / 16)), dim3(64 * W), 0, st, a);
+  const auto k = weights_once(a.M, a.N, a.K) ? k_matmul_f8_rows<W, R, true, TO> : k_matmul_f8_rows<W, R, false, TO>;
+  hipLaunchKernelGGL(k, dim3((unsigned)((a.N + 15) / 16)), dim3(64 * W), 0, st, a);
   return hipGetLastError();
 }
 
 template <int W, typename T, typename TO>
 hipError_t launch_linear_rows(const LinearF8Args& a, const void* X, int64_t ldx, hipStream_t st) {
-  const auto k = k_linear_f8_rows<W, T, TO>;
+  const auto k = weights_once(a.M, a.N, a.K) ? k_linear_f8_rows<W, true, T, TO> : k_linear_f8_rows<W, false, T, TO>;
   const size_t lds = linear_rows_lds(a.M, a.K);
   if (lds > 32768) {  // (beside the sums of 16 wavefronts)
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
@@ -817,9 +827,7 @@ Choice choose(int64_t M, int64_t N, int64_t K) {
 template <typename TO>
 hipError_t launch(const LinearF8Args& a, void* ws, hipStream_t st) {
   const Choice c = choose(a.M, a.N, a.K);
-  // Weights read once that fill a good part of the last cache go past it (64 x 27648 x 5120: 34.4, 30.7 past it; 16 x 13824 x
-  // 5120 17.6 and 16.0; 64 x 8192 x 8192 22.3 and 19.8; in the caches 64 x 13824 x 5120 15.7 and 18.0).
-  const bool once = a.M <= 64 && a.N * a.K >= (int64_t)1 << 26;
+  const bool once = weights_once(a.M, a.N, a.K);
   constexpr bool kWide = sizeof(TO) == 4;  // operands as fp16: twice the registers
   switch (c.path) {
     case kRows:

@@ -187,7 +187,7 @@ SHAPES = [(1, 1, 1), (1, 16, 16), (1, 2560, 2048), (2, 17, 33), (3, 100, 1000), 
           (255, 513, 96), (256, 256, 256), (300, 1003, 1337), (511, 260, 144), (1, 33, 131071), (70, 40, 20000),
           (5, 8200, 300), (30, 200, 9000), (50, 130, 5003), (64, 9001, 513), (40, 24700, 144), (129, 16640, 260), (90, 100, 12289),
           (9, 12400, 129), (20, 8300, 200), (32, 100, 17000), (700, 3000, 640), (2000, 4100, 200), (1500, 9001, 333), (1025, 12300, 384),
-          (130, 2050, 6000), (16, 4096, 4097), (7, 4097, 4096), (16, 100, 4095), (40, 8203, 8200), (24, 5120, 4000), (64, 2048, 11008), (300, 12000, 250), (16, 12289, 2049), (48, 24600, 2100)]
+          (130, 2050, 6000), (16, 4096, 4097), (7, 4097, 4096), (16, 100, 4095), (40, 8203, 8200), (5, 8203, 8200), (24, 5120, 4000), (64, 2048, 11008), (300, 12000, 250), (16, 12289, 2049), (48, 24600, 2100)]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
@@ -282,7 +282,7 @@ def test_matmul_rows_past_2_31_bytes(M, N, K):
 LINEAR = [(1, 70, 96), (1, 2560, 2048), (4, 65, 1000), (13, 200, 4100), (40, 90, 33), (200, 130, 257), (1, 40, 1), (1, 9000, 11008),
           (2, 16, 16384), (2, 9001, 100), (3, 50, 10922), (5, 300, 515), (8, 1030, 4096), (16, 33, 2048), (16, 130, 2047),
           (16, 130, 2049), (9, 17, 65), (3, 9000, 70), (300, 1003, 1337), (1, 1000, 32768), (1, 3000, 32767), (1, 100, 32769),
-          (1, 30000, 500), (16, 4096, 1024), (16, 4112, 1025), (2, 100, 8192), (2, 100, 8193)]
+          (1, 30000, 500), (16, 4096, 1024), (16, 4112, 1025), (2, 100, 8192), (2, 100, 8193), (1, 8203, 8200)]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
