@@ -866,13 +866,13 @@ hipError_t launch_matmul_f8(const LinearF8Args& a, void* ws, hipStream_t st) {
 }
 
 bool linear_f8_fused(int64_t M, int64_t N, int64_t K) {
-  // Where quantizing over and over costs a workgroup less than a launch.  On the GPU, in us, fused and in two launches:
-  // 1 x 2560 x 2048 4.2 and 6.0; 1 x 11008 x 2048 7.0 and 10.9; 1 x 27648 x 5120 29.2 and 29.7; 1 x 5120 x 27648 37.3 and 39.5;
-  // 2 x 5120 x 5120 10.4 and 12.5; 4 x 11008 x 2048 8.9 and 11.1; 8 x 11008 x 2048 11.4 and 11.4; 16 x 2048 x 2048 7.3 and 6.3
-  // (but a launch that is not replayed from a graph costs the host 3); 4 x 2048 x 11008 13.1 and 13.8; 8 x 5120 x 5120 17.6
-  // and 12.8; 16 x 11008 x 2048 16.6 and 11.8.
+  // Where quantizing over and over costs a workgroup less than a launch, or little more: one that is not replayed from a graph
+  // costs the host 3.  On the GPU, in us, fused and in two launches: 1 x 2560 x 2048 4.2 and 6.2; 1 x 11008 x 2048 6.9 and 10.6; 1 x
+  // 27648 x 5120 26.4 and 29.6; 1 x 5120 x 27648 33.6 and 37.2; 2 x 5120 x 5120 10.2 and 12.3; 4 x 5120 x 5120 12.3 and 12.6; 8 x
+  // 11008 x 2048 10.5 and 11.0; 16 x 2048 x 2560 7.6 and 7.0; 8 x 5120 x 5120 16.1 and 13.0; 16 x 11008 x 2048 18.2 and 11.5; 16 x
+  // 2048 x 4096 10.6 and 7.5.
   if (M == 1) return K <= 32768 && N <= (int64_t)1 << 26;  // (2^31 threads of a launch)
-  return M <= 16 && N < 12288 && (M * K <= 16384 || (K <= 2048 && N <= 4096));
+  return M <= 16 && N < 12288 && M * K <= (N <= 4096 ? 40960 : 20480);
 }
 
 hipError_t launch_linear_f8_fused(const LinearF8Args& a, const void* X, int x_dtype, int64_t ldx, hipStream_t st) {

@@ -282,7 +282,8 @@ def test_matmul_rows_past_2_31_bytes(M, N, K):
 LINEAR = [(1, 70, 96), (1, 2560, 2048), (4, 65, 1000), (13, 200, 4100), (40, 90, 33), (200, 130, 257), (1, 40, 1), (1, 9000, 11008),
           (2, 16, 16384), (2, 9001, 100), (3, 50, 10922), (5, 300, 515), (8, 1030, 4096), (16, 33, 2048), (16, 130, 2047),
           (16, 130, 2049), (9, 17, 65), (3, 9000, 70), (300, 1003, 1337), (1, 1000, 32768), (1, 3000, 32767), (1, 100, 32769),
-          (1, 30000, 500), (16, 4096, 1024), (16, 4112, 1025), (2, 100, 8192), (2, 100, 8193), (1, 8203, 8200)]
+          (1, 30000, 500), (16, 4096, 1024), (16, 4112, 1025), (2, 100, 8192), (2, 100, 8193), (1, 8203, 8200), (4, 5000, 5120), (4, 5000, 5121),
+          (16, 4096, 2560), (16, 4097, 2560), (16, 130, 2561), (5, 33, 8192), (2, 300, 20480)]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
