@@ -795,17 +795,19 @@ Choice choose(int64_t M, int64_t N, int64_t K) {
   // 15.1 and 13.1; 32 x 8192 x 8192: 24.7 and 21.5; 24 x 8192 x 2400: 8.5 and 9.3; 24 x 11008 x 1024: 7.4 and 6.3; 24 x 27648 x
   // 512: 13.0 and 6.3).
   if (M > 16 && M <= 32 && N * K <= 20000000 && N <= 8192) return {kRows, 1};
-  const int64_t t128 = tiles(128, 128), t256 = tiles(256, 256);
+  const int64_t wide = tiles(64, 128), t128 = tiles(128, 128), t256 = tiles(256, 256);
+  // 64 x 128 tiles where a CU has one at most, and 64 x 64 ones would not all have a CU: 64 x 27648 x 5120: 64 x 64 tiles 38.4,
+  // 30.7; 48 x 20000 x 4096: 25.3 and 24.1; 256 x 8192 x 8192: 128 x 128 tiles 43.5, 34.5; 1000 x 2048 x 11008: 55 and 39.6.
+  if (M > 32 && wide > 128 && (wide <= 256 || M <= 64)) return {kTile64Wide, 1};
+  // 128 x 128 tiles with four stages where a CU has one of them (128 x 27648 x 5120: 41.0, 64 x 128 tiles 49.5, with two stages 50; 512 x
+  // 5120 x 5120: 31.3, 37.1 and 43; 200 x 11008 x 2048: 15.5 and 16.9), 64 x 128 ones where a CU has two of those (320 x 11008 x
+  // 5120: 39.3, 128 x 128 tiles 45.9).
+  if (M > 64 && wide > 256 && t128 <= 256) return {kTile128Deep, 1};
+  if (M > 64 && wide > 256 && wide <= 512) return {kTile64Wide, 1};
   // 128 x 128 tiles, two workgroups a CU, or 256 x 256, one: a round of 256 of the large ones costs what 2.6 times as many
-  // small ones do (512 x 27648 x 5120: 116 and 82; 1024 x 5120 x 5120: 50 and 71; 4096 x 5120 x 5120: 135 and 141; 2048 x
-  // 11008 x 2048: 70 and 63).
-  if (M > 64 && t128 > 256) return {2.9 * ((t256 + 255) / 256) < t128 / 256.0 + 0.5 ? kTile256 : kTile128, 1};
-  // One of them a CU: four stages instead of two (128 x 27648 x 5120: 40, with two 50, 64 x 128 tiles 49; 256 x 11008 x
-  // 2048: 16, 21 and 18; 512 x 5120 x 5120: 31, 43 and 37; 2048 x 2048 x 11008: 64 and 84; with 80 of them, 200 x 5120 x
-  // 5120, smaller tiles: 22).
-  if (M > 64 && t128 >= 128) return {kTile128Deep, 1};
-  // 64 x 27648 x 5120: 64 x 64 tiles 38.4, 64 x 128 tiles 30.7 (64 x 11008 x 2048: 9.5 and 11.9)
-  if (M > 32 && tiles(64, 128) >= 192) return {kTile64Wide, 1};
+  // small ones do (1000 x 11008 x 2048: 35.6 and 29.5; 512 x 27648 x 5120: 83 and 66; 4096 x 5120 x 5120: 141 and 135; 1100 x 16384 x
+  // 1024: 33.3 and 34.4).
+  if (M > 64 && wide > 512) return {2.9 * ((t256 + 255) / 256) < t128 / 256.0 + 0.5 ? kTile256 : kTile128, 1};
   const Path path = M > 32 ? kTile64 : kTile32;
   // Few tiles under a long sum: as many parts as cost least, joined by a second launch.  A step costs 0.25 us, into fp32 0.41;
   // the join 2.1, 0.3 more a part and what the parts' bytes take (64 x 2048 x 11008: 26 whole, 13.8 in 8 parts, 17.5 in 16; 256

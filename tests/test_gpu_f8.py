@@ -187,7 +187,7 @@ SHAPES = [(1, 1, 1), (1, 16, 16), (1, 2560, 2048), (2, 17, 33), (3, 100, 1000), 
           (255, 513, 96), (256, 256, 256), (300, 1003, 1337), (511, 260, 144), (1, 33, 131071), (70, 40, 20000),
           (5, 8200, 300), (30, 200, 9000), (50, 130, 5003), (64, 9001, 513), (40, 24700, 144), (129, 16640, 260), (90, 100, 12289),
           (9, 12400, 129), (20, 8300, 200), (32, 100, 17000), (700, 3000, 640), (2000, 4100, 200), (1500, 9001, 333), (1025, 12300, 384),
-          (130, 2050, 6000), (16, 4096, 4097), (7, 4097, 4096), (16, 100, 4095), (40, 8203, 8200), (5, 8203, 8200), (24, 5120, 4000), (64, 2048, 11008), (300, 12000, 250), (16, 12289, 2049), (48, 24600, 2100)]
+          (130, 2050, 6000), (16, 4096, 4097), (7, 4097, 4096), (16, 100, 4095), (40, 8203, 8200), (5, 8203, 8200), (130, 8200, 300), (513, 4097, 260), (24, 5120, 4000), (64, 2048, 11008), (300, 12000, 250), (16, 12289, 2049), (48, 24600, 2100)]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
