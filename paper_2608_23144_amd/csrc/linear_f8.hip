@@ -811,13 +811,14 @@ Choice choose(int64_t M, int64_t N, int64_t K) {
   const Path path = M > 32 ? kTile64 : kTile32;
   // Few tiles under a long sum: as many parts as cost least, joined by a second launch.  A step costs 0.25 us, into fp32 0.41;
   // the join 2.1, 0.3 more a part and what the parts' bytes take (64 x 2048 x 11008: 26 whole, 13.8 in 8 parts, 17.5 in 16; 256
-  // x 1024 x 4096: 12.5, 11.4 in 4, 14.2 in 8; 128 x 2048 x 2048: 8.4 whole, 9.9 in 2).
+  // x 1024 x 4096: 12.5, 11.4 in 4, 14.2 in 8; 128 x 2048 x 2048: 8.4 whole, 9.9 in 2).  And half of the 3 that a launch
+  // costs the host where it is not replayed from a graph.
   const int64_t t = path == kTile64 ? tiles(64, 64) : tiles(32, 64), steps = (K + kStep - 1) / kStep;
   const double step = 0.33, bytes = 1.8e-6 * (double)M * (double)N;
   Choice best = {path, 1};
   double least = step * (double)steps;
   for (int s = 2; s <= 16 && s * t <= 256; ++s) {
-    const double us = 2.1 + 0.3 * s + step * (double)((steps + s - 1) / s) + bytes * s;
+    const double us = 2.1 + 1.5 + 0.3 * s + step * (double)((steps + s - 1) / s) + bytes * s;
     if (us < least) {
       least = us;
       best.split = s;
