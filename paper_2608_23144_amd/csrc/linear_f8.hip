@@ -773,10 +773,10 @@ hipError_t launch_linear_rows_w(const LinearF8Args& a, const void* X, int64_t ld
 }
 template <typename T>
 hipError_t launch_linear_rows_t(const LinearF8Args& a, const void* X, int64_t ldx, hipStream_t st) {
-  // sixteen wavefronts where the workgroups leave CUs idle (1 x 2048 x 11008: 10.7 us with eight, 9.3; 16 x 2048 x 2048 8.5 and
-  // 7.3; 1 x 5120 x 5120 9.2 and 10.6)
-  return a.M > 8 || (a.N <= 2560 && (a.M >= 4 || a.K >= 8192)) ? launch_linear_rows_w<16, T>(a, X, ldx, st)
-                                                               : launch_linear_rows_w<8, T>(a, X, ldx, st);
+  // sixteen wavefronts where the workgroups leave CUs idle (with eight and sixteen: 1 x 2048 x 11008 10.4 and 9.0; 16 x 2048 x 2048 7.6
+  // and 6.7; 8 x 4096 x 2048 6.2 and 5.8; 1 x 2560 x 2048 4.2 and 4.3; 1 x 5120 x 5120 9.0 and 10.6; 9 x 11008 x 2048 10.9 and 14.1)
+  return a.N <= 4096 && (a.M >= 4 || a.K >= 8192) ? launch_linear_rows_w<16, T>(a, X, ldx, st)
+                                                  : launch_linear_rows_w<8, T>(a, X, ldx, st);
 }
 
 // Which kernel takes a product, and over how many parts of the sum.  Times below are in us, into bf16, of calls on
