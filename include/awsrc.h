@@ -566,10 +566,8 @@ awsrc_status awsrc_dequantize_blocks_f8(const uint8_t* codes, int64_t ldc, const
 /*
  * Product of e4m3 matrices with a scale for each block of 128:
  *   out[m, n] = sum_b a_scale[b][m] b_scale[n / 128][b] sum_{k in block b} A[m, k] B[n, k] + bias[n].
- * Sums in fp32: a block's products first, then fma(block's sum, a_scale * b_scale, sum so
- * far); the sum is rounded once to out_dtype (nearest even).  For results in bf16 and fp16
- * the matrix cores take the products of a block eight by eight, each cut off 2^13 below the
- * largest of its eight, which is 1.5e-5 rms of a result; for fp32 they do not.  The same
+ * Sums in fp32 for every out_dtype: a block's products first, then fma(block's sum, a_scale *
+ * b_scale, sum so far); the sum is rounded once to out_dtype (nearest even).  The same
  * call gives the same bits; calls of other shapes may add in another order.
  *  A, B     e4m3, row i at A + i * lda; 16-byte aligned, lda and ldb multiples of
  *           16, >= K rounded up to 16, <= 2^22.  Each row is readable up to K

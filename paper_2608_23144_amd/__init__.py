@@ -977,7 +977,7 @@ def awsrc_matmul_f8(a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor, b_s
                     out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
                     stream=None) -> torch.Tensor:
     """a [M, K] times b [N, K] transposed, e4m3 codes with fp32 scales as awsrc_quantize_blocks_f8 makes them (a with
-    block_rows 1, b with 128): [M, N] in out_dtype (or out's)."""
+    block_rows 1, b with 128): [M, N] in out_dtype (or out's), sums in fp32 for each type."""
     M, K, lda = _i8_rows(a, "a", _F8)
     N, Kb, ldb = _i8_rows(b, "b", _F8)
     if K != Kb:

@@ -1,14 +1,14 @@
 // Products of e4m3 matrices with a scale for each block of 128:
 //   out[m][n] = sum_b a_scale[b][m] b_scale[n / 128][b] sum_{k in b} A[m][k] B[n][k] + bias[n].
-// One v_mfma_f32_16x16x128_f8f6f4 from a zero accumulator is a block's sums of
-// a 16 x 16 tile; one fma a value then adds them with their scale.
+// Four v_mfma_f32_16x16x32_f16 from a zero accumulator are a block's sums of
+// a 16 x 16 tile; one fma a value then adds them with their scale.  The codes go as
+// fp16, which holds them exactly.
 //
-// That instruction adds eight adjacent products at a time at the exponent of the largest and
-// cuts off what lies 2^13 below it (measured: beside a product of 2^16 one of 8 counts, one
-// of 4 does not; between the eights it adds in fp32).  The results are 1.5e-5
-// rms off, a tenth of fp16's own rounding and a hundredth of bf16's.  Results in fp32
-// would show it: for them the codes, which fp16 holds exactly, go as fp16 through
-// v_mfma_f32_16x16x32_f16, at half the rate, which adds in fp32 throughout.
+// The matrix cores take e4m3 as well, at twice the rate, but then they add eight adjacent products
+// at the exponent of the largest and cut off what lies 2^13 below it (measured, of
+// v_mfma_f32_16x16x128_f8f6f4 and v_mfma_f32_16x16x32_fp8_fp8 alike): random codes come out 1.5e-5 to 5e-5
+// rms off, and products that a louder neighbour hides are lost where the loud ones cancel.  In fp16
+// they add in fp32: whole numbers below 2^24 exactly, random codes within 8e-8 rms.
 //
 // Matrix-core layout: an operand lane l holds row l % 16 and 32 bytes of a block
 // of 128, the same ones in both operands; the result
@@ -21,8 +21,6 @@
 namespace awsrc {
 
 namespace {
-
-typedef int32_t i32x8 __attribute__((ext_vector_type(8)));
 
 // Eight codes as fp16.
 __device__ __forceinline__ h8 halves(int lo, int hi) {
@@ -46,16 +44,8 @@ __device__ __forceinline__ i32x4 piece(const uint8_t* p, int64_t left) {
   return w;
 }
 
-// An operand's 32 bytes as the products take them: as they are, or as fp16.
-template <bool FULL>
+// An operand's 32 bytes as the products take them.
 struct Operand {
-  i32x8 v;
-  __device__ __forceinline__ void set(i32x4 lo, i32x4 hi) {
-    v = i32x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-  }
-};
-template <>
-struct Operand<true> {
   h8 v[4];
   __device__ __forceinline__ void set(i32x4 lo, i32x4 hi) {
     v[0] = halves(lo[0], lo[1]);
@@ -64,10 +54,7 @@ struct Operand<true> {
     v[3] = halves(hi[2], hi[3]);
   }
 };
-__device__ __forceinline__ fl4 sums_of(const Operand<false>& w, const Operand<false>& x) {
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w.v, x.v, fl4{0, 0, 0, 0}, 0, 0, 0, 0, 0, 0);
-}
-__device__ __forceinline__ fl4 sums_of(const Operand<true>& w, const Operand<true>& x) {
+__device__ __forceinline__ fl4 sums_of(const Operand& w, const Operand& x) {
   fl4 p = {0, 0, 0, 0};
 #pragma unroll
   for (int i = 0; i < 4; ++i) p = __builtin_amdgcn_mfma_f32_16x16x32_f16(w.v[i], x.v[i], p, 0, 0, 0);
@@ -121,8 +108,7 @@ struct Quads {
     }
   }
   // lane j of a quad gets as v[i] what lane i of it loaded as v[j], then the groups trade
-  template <typename Op>
-  __device__ __forceinline__ void turn(int lane, Op& block0, Op& block1) {
+  __device__ __forceinline__ void turn(int lane, Operand& block0, Operand& block1) {
     const bool odd = lane & 1, high = lane & 2;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -155,7 +141,6 @@ struct Quads {
 
 template <int W, int R, bool AHEAD, bool ONCE, typename TO>
 struct RowSums {
-  using Op = Operand<sizeof(TO) == 4>;
   const uint8_t* pb[4];      // this lane's pieces of the weights
   const uint8_t* pa[R][4];   // the same of R groups of 16 rows of activation codes (AHEAD: in memory, fetched with the weights)
   const uint8_t *rb, *ra[R]; // this lane's own rows
@@ -189,7 +174,7 @@ struct RowSums {
   __device__ __forceinline__ void begin() {
     if (wave < rounds()) load(0, wave * Quads::kRound);
   }
-  __device__ __forceinline__ void add(int j, const Op& w, const Op& x, float s) {
+  __device__ __forceinline__ void add(int j, const Operand& w, const Operand& x, float s) {
     const fl4 p = sums_of(w, x);
 #pragma unroll
     for (int e = 0; e < 4; ++e) acc[j][e] = __builtin_fmaf(p[e], s, acc[j][e]);
@@ -197,11 +182,11 @@ struct RowSums {
   template <typename SA>
   __device__ __forceinline__ void products(int buf, int k, const SA& sa) {
     const int b = k / kBlockF8;
-    Op w[2];
+    Operand w[2];
     fb[buf].turn(lane, w[0], w[1]);
 #pragma unroll
     for (int j = 0; j < R; ++j) {
-      Op x[2];
+      Operand x[2];
       if constexpr (AHEAD) {
         fa[buf][j].turn(lane, x[0], x[1]);
       } else {
@@ -230,11 +215,11 @@ struct RowSums {
     if (wave == W - 1) {  // the rest of the sum, zeros past K on both sides
       for (int k = n * Quads::kRound; k < K; k += kBlockF8) {
         const int at = k + 32 * g, left = K - at;
-        Op w;
+        Operand w;
         w.set(piece(rb + at, left), piece(rb + at + 16, left - 16));
 #pragma unroll
         for (int j = 0; j < R; ++j) {
-          Op x;
+          Operand x;
           x.set(piece(ra[j] + at, left), piece(ra[j] + at + 16, left - 16));
           add(j, w, x, sa(k / kBlockF8, 16 * j + (lane & 15)) * sb[k / kBlockF8]);
         }
@@ -319,12 +304,6 @@ __global__ __launch_bounds__(64 * W) void k_linear_f8_rows(LinearF8Args a, const
 //
 // Weight row 4 TN q + 4 t + i of a wavefront's columns is row 4 q + i of its t-th
 // operand, so that a lane ends with 4 TN consecutive columns of one result row.
-//
-// 8192 x 27648 x 5120 in 256 x 256 tiles: 1.04 to 1.06 ms, 2.2 PFLOP/s, beside 0.88 of a library product with one scale
-// for each whole operand.  A step of 128 takes 3300 cycles, 2050 of them in the matrix cores; the four scaling fmas of
-// each product's results add 350.  The clock is bound by power (1.84 GHz on random codes, 2.3 on zeros): cycles saved
-// elsewhere lower it.  512 x 27648 x 5120 82 us, 64 x 27648 x 5120 30.7 (146 MB, 4.8 TB/s), 517 x 1003 x 1337 into fp32
-// 9.9, of which the launch's latencies are most.
 constexpr int kStep = kBlockF8;
 
 __device__ __forceinline__ int key_a(int row) { return (row >> 1) & 7; }
@@ -367,7 +346,6 @@ __global__ __launch_bounds__((TileShape<BM, BN, WM, WN>::kThreads), OCC) void k_
                                                                                                int tiles_n, int split_steps,
                                                                                                float* parts) {
   using S = TileShape<BM, BN, WM, WN>;
-  using Op = Operand<sizeof(TO) == 4>;
   constexpr int TM = WM / 16, TN = WN / 16;
   constexpr int NA = BM * 8 / S::kThreads, NB = BN * 8 / S::kThreads;  // 16-byte pieces per thread and step
   constexpr int kRows = S::kThreads / 8;                              // rows that one round of fills covers
@@ -427,13 +405,13 @@ __global__ __launch_bounds__((TileShape<BM, BN, WM, WN>::kThreads), OCC) void k_
   const int qa = (g ^ key_a(r)) * 16, qb = (g ^ key_b<TN>(rb_n)) * 16;
   const auto read_a = [&](int stage, int j) {
     const char* p = lds + stage * S::kStage + (wm + 16 * j + r) * kStep;
-    Op x;
+    Operand x;
     x.set(*reinterpret_cast<const i32x4*>(p + qa), *reinterpret_cast<const i32x4*>(p + (qa ^ 64)));
     return x;
   };
   const auto read_b = [&](int stage, int i) {
     const char* p = lds + stage * S::kStage + (BM + wn + rb_n + 4 * i) * kStep;
-    Op w;
+    Operand w;
     w.set(*reinterpret_cast<const i32x4*>(p + qb), *reinterpret_cast<const i32x4*>(p + (qb ^ 64)));
     return w;
   };
@@ -474,13 +452,12 @@ __global__ __launch_bounds__((TileShape<BM, BN, WM, WN>::kThreads), OCC) void k_
     for (int c = 0; c < (t + 1 < NS ? kParts : kFirst); ++c) fill(t, t, c);
   arrived(std::integral_constant<int, (NS - 2) * kParts + kFirst>{});
   int st = 0;
-  Op w[TN], x;
+  Operand w[TN], x;
   float s;
   if constexpr (WHOLE) {
-    // A step's operands are all read while the products of the step before run, into the other of two sets of registers
-    // (64 x 2560 x 2048: 8.8 with the phases below, 7.9; 4096 x 5120 x 5120 by 128 x 128 tiles 144 and 135; 256 x 256 tiles and
-    // results in fp32 of 128 x 128 have not the registers, 64 x 128 tiles of 16-bit results lose: 12.4, 13.0).
-    Op fa[2][TM], fb[2][TN];
+    // A step's operands are all read while the products of the step before run, into the other of two sets of registers (tiles
+    // of 128 x 128 have not the registers).
+    Operand fa[2][TM], fb[2][TN];
     float sc[2][TM];
     const auto read = [&](int stage, int b) {
       const float sb = scale_b(stage);
@@ -539,7 +516,7 @@ __global__ __launch_bounds__((TileShape<BM, BN, WM, WN>::kThreads), OCC) void k_
     };
     for (int t = 0; t < steps; ++t) {
       const int next = st + 1 == NS ? 0 : st + 1, prev = st == 0 ? NS - 1 : st - 1;
-      Op y;
+      Operand y;
       float s_next;
 #pragma unroll
       for (int j = 0; j + 1 < TM; ++j) {
@@ -553,7 +530,7 @@ __global__ __launch_bounds__((TileShape<BM, BN, WM, WN>::kThreads), OCC) void k_
         __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);  // LDS read
 #pragma unroll
         for (int i = 0; i < TN; ++i) {
-          __builtin_amdgcn_sched_group_barrier(0x008, sizeof(TO) == 4 ? 4 : 1, 0);  // MFMA
+          __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);  // MFMA
           __builtin_amdgcn_sched_group_barrier(0x020, kPer, 0);                     // memory read
           __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);                        // VALU
         }
@@ -781,7 +758,7 @@ hipError_t launch_linear_rows_t(const LinearF8Args& a, const void* X, int64_t ld
 
 // Which kernel takes a product, and over how many parts of the sum.  Times below are in us, into bf16, of calls on
 // weights that are not in the caches.
-enum Path { kRows, kTile32, kTile64, kTile64Wide, kTile128Deep, kTile128, kTile256 };
+enum Path { kRows, kTile32, kTile64, kTile64Wide, kTile128Deep, kTile128 };
 struct Choice {
   Path path;
   int split;
@@ -795,7 +772,7 @@ Choice choose(int64_t M, int64_t N, int64_t K) {
   // 15.1 and 13.1; 32 x 8192 x 8192: 24.7 and 21.5; 24 x 8192 x 2400: 8.5 and 9.3; 24 x 11008 x 1024: 7.4 and 6.3; 24 x 27648 x
   // 512: 13.0 and 6.3).
   if (M > 16 && M <= 32 && N * K <= 20000000 && N <= 8192) return {kRows, 1};
-  const int64_t wide = tiles(64, 128), t128 = tiles(128, 128), t256 = tiles(256, 256);
+  const int64_t wide = tiles(64, 128), t128 = tiles(128, 128);
   // 64 x 128 tiles where a CU has one at most, and 64 x 64 ones would not all have a CU: 64 x 27648 x 5120: 64 x 64 tiles 38.4,
   // 30.7; 48 x 20000 x 4096: 25.3 and 24.1; 256 x 8192 x 8192: 128 x 128 tiles 43.5, 34.5; 1000 x 2048 x 11008: 55 and 39.6.
   if (M > 32 && wide > 128 && (wide <= 256 || M <= 64)) return {kTile64Wide, 1};
@@ -804,10 +781,8 @@ Choice choose(int64_t M, int64_t N, int64_t K) {
   // 5120: 39.3, 128 x 128 tiles 45.9).
   if (M > 64 && wide > 256 && t128 <= 256) return {kTile128Deep, 1};
   if (M > 64 && wide > 256 && wide <= 512) return {kTile64Wide, 1};
-  // 128 x 128 tiles, two workgroups a CU, or 256 x 256, one: a round of 256 of the large ones costs what 2.6 times as many
-  // small ones do (1000 x 11008 x 2048: 35.6 and 29.5; 512 x 27648 x 5120: 83 and 66; 4096 x 5120 x 5120: 141 and 135; 1100 x 16384 x
-  // 1024: 33.3 and 34.4).
-  if (M > 64 && wide > 512) return {2.9 * ((t256 + 255) / 256) < t128 / 256.0 + 0.5 ? kTile256 : kTile128, 1};
+  // 128 x 128 tiles, two workgroups a CU.
+  if (M > 64 && wide > 512) return {kTile128, 1};
   const Path path = M > 32 ? kTile64 : kTile32;
   // Few tiles under a long sum: as many parts as cost least, joined by a second launch.  A step costs 0.25 us, into fp32 0.41;
   // the join 2.1, 0.3 more a part and what the parts' bytes take (64 x 2048 x 11008: 26 whole, 13.8 in 8 parts, 17.5 in 16; 256
@@ -831,14 +806,8 @@ template <typename TO>
 hipError_t launch(const LinearF8Args& a, void* ws, hipStream_t st) {
   const Choice c = choose(a.M, a.N, a.K);
   const bool once = weights_once(a.M, a.N, a.K);
-  constexpr bool kWide = sizeof(TO) == 4;  // operands as fp16: twice the registers
   switch (c.path) {
-    case kRows:
-      // sixteen wavefronts where the workgroups leave CUs idle and the sum is long (13 x 2048 x 11008: 11.0 and 10.1; 16 x 4096 x
-      // 4096 6.6 and 6.3; 5 x 5120 x 5120 9.6 and 10.3; for fp32 they do not have the registers)
-      if constexpr (!kWide)
-        if (a.M <= 16 && a.N <= 4096 && a.K >= 4096) return launch_rows<16, 1, TO>(a, st);
-      return a.M <= 16 ? launch_rows<8, 1, TO>(a, st) : launch_rows<8, 2, TO>(a, st);
+    case kRows: return a.M <= 16 ? launch_rows<8, 1, TO>(a, st) : launch_rows<8, 2, TO>(a, st);
     case kTile32:
       return once ? launch_tile<32, 64, 32, 32, 2, 4, true, true, TO>(a, c.split, ws, st)
                   : launch_tile<32, 64, 32, 32, 2, 4, true, false, TO>(a, c.split, ws, st);
@@ -846,12 +815,10 @@ hipError_t launch(const LinearF8Args& a, void* ws, hipStream_t st) {
       return once ? launch_tile<64, 64, 32, 32, 2, 4, true, true, TO>(a, c.split, ws, st)
                   : launch_tile<64, 64, 32, 32, 2, 4, true, false, TO>(a, c.split, ws, st);
     case kTile64Wide:
-      return once ? launch_tile<64, 128, 32, 64, 2, 3, kWide, true, TO>(a, 1, ws, st)
-                  : launch_tile<64, 128, 32, 64, 2, 3, kWide, false, TO>(a, 1, ws, st);
+      return once ? launch_tile<64, 128, 32, 64, 2, 3, true, true, TO>(a, 1, ws, st)
+                  : launch_tile<64, 128, 32, 64, 2, 3, true, false, TO>(a, 1, ws, st);
     case kTile128Deep: return launch_tile<128, 128, 64, 64, 2, 4, false, false, TO>(a, 1, ws, st);
-    case kTile256:  // (of results in fp32 the operands do not fit the registers)
-      if constexpr (!kWide) return launch_tile<256, 256, 128, 64, 2, 2, false, false, TO>(a, 1, ws, st);
-    default: return launch_tile<128, 128, 64, 64, 2, 2, !kWide, false, TO>(a, 1, ws, st);
+    default: return launch_tile<128, 128, 64, 64, 2, 2, false, false, TO>(a, 1, ws, st);
   }
 }
 
