@@ -87,7 +87,7 @@ __device__ __forceinline__ void store4(TO* o, const float (&y)[4], int64_t n, in
 // of block 1, the second half of block 0 and of block 1 for g = 0 to 3.  Groups 0 and 1, 2 and 3
 // trade halves of those with one instruction a register: 32 bytes of each block.
 //
-// 13 x 2048 x 11008 (23 MB): 6.9 us with the weights in the caches, 10.1 from memory, of which 3.7 are their
+// 13 x 2048 x 11008 (23 MB): 8.3 us with the weights in the caches, 11.7 from memory, of which 3.7 are their
 // bytes: 128 workgroups do not keep enough on its way for more.
 struct Quads {
   static constexpr int kRound = 2 * kBlockF8;  // bytes of a row that a wavefront takes at a time
@@ -260,7 +260,7 @@ __global__ __launch_bounds__(64 * W) void k_matmul_f8_rows(LinearF8Args a) {
 
 // On activations: every workgroup quantizes the few rows itself (into LDS, as
 // quant_f8.hip does, sixteen lanes a block), while its first weights are on their way, which saves a
-// launch and its wait.  1 x 2560 x 2048 (5.3 MB) 4.2 us, 3.4 with the weights in the caches: one wait for X, one for the
+// launch and its wait.  1 x 2560 x 2048 (5.3 MB) 4.3 us, 3.5 with the weights in the caches: one wait for X, one for the
 // weights, and the wavefronts' meeting.
 template <int W, bool ONCE, typename T, typename TO>
 __global__ __launch_bounds__(64 * W) void k_linear_f8_rows(LinearF8Args a, const T* X, int64_t ldx, int pitch) {
@@ -304,6 +304,11 @@ __global__ __launch_bounds__(64 * W) void k_linear_f8_rows(LinearF8Args a, const
 //
 // Weight row 4 TN q + 4 t + i of a wavefront's columns is row 4 q + i of its t-th
 // operand, so that a lane ends with 4 TN consecutive columns of one result row.
+//
+// Bound by the matrix cores and by what stands beside them: the turn of codes into fp16 (sixteen
+// instructions for an operand of a step) and an fma a value and block.  8192 x 27648 x 5120 1.99 ms, 1.17 PFLOP/s, 8192 x 8192 x 8192
+// into fp32 0.91 ms, 1.21.  64 x 27648 x 5120 33.4 us (146 MB, 4.4 TB/s), 517 x 1003 x 1337 into
+// fp32 11.2, of which the launch's latencies are most.
 constexpr int kStep = kBlockF8;
 
 __device__ __forceinline__ int key_a(int row) { return (row >> 1) & 7; }
@@ -719,9 +724,9 @@ size_t linear_rows_lds(int64_t M, int64_t K) {
   return (size_t)M * linear_rows_pitch(K) + (size_t)((K + kBlockF8 - 1) / kBlockF8) * 64;
 }
 
-// Weights read once that fill a good part of the last cache go past it (64 x 27648 x 5120: 34.4, 30.7 past it; 16 x 13824 x
-// 5120 17.6 and 16.0; 64 x 8192 x 8192 22.3 and 19.8; 1 x 27648 x 5120 29.0 and 26.4; 1 x 8192 x 8192 16.1 and 14.7; in the
-// caches 64 x 13824 x 5120 15.7 and 18.0).
+// Weights read once that fill a good part of the last cache go past it (64 x 27648 x 5120: 36.8, 33.4 past it; 8 x 27648 x
+// 5120 33.3 and 31.4; 16 x 13824 x 5120 22.8 and 22.0; 48 x 20000 x 4096 28.0 and 27.4; 1 x 8192 x 8192 18.9 and 18.2; in the
+// caches 64 x 27648 x 5120 32.5 and 33.3).
 bool weights_once(int64_t M, int64_t N, int64_t K) { return M <= 64 && N * K >= (int64_t)1 << 26; }
 
 template <int W, int R, typename TO>
@@ -750,14 +755,15 @@ hipError_t launch_linear_rows_w(const LinearF8Args& a, const void* X, int64_t ld
 }
 template <typename T>
 hipError_t launch_linear_rows_t(const LinearF8Args& a, const void* X, int64_t ldx, hipStream_t st) {
-  // sixteen wavefronts where the workgroups leave CUs idle (with eight and sixteen: 1 x 2048 x 11008 10.4 and 9.0; 16 x 2048 x 2048 7.6
-  // and 6.7; 8 x 4096 x 2048 6.2 and 5.8; 1 x 2560 x 2048 4.2 and 4.3; 1 x 5120 x 5120 9.0 and 10.6; 9 x 11008 x 2048 10.9 and 14.1)
+  // sixteen wavefronts where the workgroups leave CUs idle (with eight and sixteen: 1 x 2048 x 11008 10.7 and 10.2; 3 x 2048 x 11008
+  // 13.3 and 12.3; 16 x 2048 x 2048 7.7 and 6.7; 8 x 4096 x 2048 6.2 and 5.8; 1 x 2560 x 2048 4.3 and 4.3; 1 x 5120 x 5120 10.0
+  // and 11.5; 9 x 11008 x 2048 12.3 and 15.4)
   return a.N <= 4096 && (a.M >= 4 || a.K >= 8192) ? launch_linear_rows_w<16, T>(a, X, ldx, st)
                                                   : launch_linear_rows_w<8, T>(a, X, ldx, st);
 }
 
 // Which kernel takes a product, and over how many parts of the sum.  Times below are in us, into bf16, of calls on
-// weights that are not in the caches.
+// weights that are not in the caches; into fp32 they are within a tenth.
 enum Path { kRows, kTile32, kTile64, kTile64Wide, kTile128Deep, kTile128 };
 struct Choice {
   Path path;
@@ -765,31 +771,31 @@ struct Choice {
 };
 Choice choose(int64_t M, int64_t N, int64_t K) {
   const auto tiles = [&](int64_t bm, int64_t bn) { return ((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
-  // Up to 16 rows: 16 columns a workgroup, up to about three of them a CU (16 x 2048 x 11008: 11.6, tiles 12.9 with their
-  // sums split; 16 x 11008 x 2048: 9.0 and 8.9; 16 x 13824 x 5120: 19.8 and 16.0).
+  // Up to 16 rows: 16 columns a workgroup, up to about three of them a CU (16 x 2048 x 11008: 12.0, tiles 14.5 with their
+  // sums split; 16 x 11008 x 2048: 9.6 and 11.5; 16 x 13824 x 5120: 23.1 and 22.0; 8 x 27648 x 5120: 38.1 and 31.4).
   if (M <= 16 && N < 12288) return {kRows, 1};
-  // Up to 32 rows of weights that are not too large, nor with too many columns (32 x 4096 x 4096: 8.6 and 11.0; 24 x 5120 x 5120:
-  // 15.1 and 13.1; 32 x 8192 x 8192: 24.7 and 21.5; 24 x 8192 x 2400: 8.5 and 9.3; 24 x 11008 x 1024: 7.4 and 6.3; 24 x 27648 x
-  // 512: 13.0 and 6.3).
+  // Up to 32 rows of weights that are not too large, nor with too many columns (32 x 4096 x 4096: 9.1 and 12.3; 24 x 5120 x 5120:
+  // 16.3 and 16.2; 32 x 8192 x 8192: 25.3 and 23.1; 24 x 8192 x 2400: 12.0 and 11.8; 24 x 11008 x 1024: 9.0 and 7.8; 24 x 27648 x
+  // 512: 18.6 and 8.3).
   if (M > 16 && M <= 32 && N * K <= 20000000 && N <= 8192) return {kRows, 1};
   const int64_t wide = tiles(64, 128), t128 = tiles(128, 128);
-  // 64 x 128 tiles where a CU has one at most, and 64 x 64 ones would not all have a CU: 64 x 27648 x 5120: 64 x 64 tiles 38.4,
-  // 30.7; 48 x 20000 x 4096: 25.3 and 24.1; 256 x 8192 x 8192: 128 x 128 tiles 43.5, 34.5; 1000 x 2048 x 11008: 55 and 39.6.
+  // 64 x 128 tiles where a CU has one at most, and 64 x 64 ones would not all have a CU: 64 x 27648 x 5120: 64 x 64 tiles 38.5,
+  // 33.4; 48 x 20000 x 4096: 28.5 and 27.4; 256 x 8192 x 8192: 54.7 and 49.2; 1000 x 2048 x 11008: 70 and 63.
   if (M > 32 && wide > 128 && (wide <= 256 || M <= 64)) return {kTile64Wide, 1};
-  // 128 x 128 tiles with four stages where a CU has one of them (128 x 27648 x 5120: 41.0, 64 x 128 tiles 49.5, with two stages 50; 512 x
-  // 5120 x 5120: 31.3, 37.1 and 43; 200 x 11008 x 2048: 15.5 and 16.9), 64 x 128 ones where a CU has two of those (320 x 11008 x
-  // 5120: 39.3, 128 x 128 tiles 45.9).
+  // 128 x 128 tiles with four stages where a CU has one of them (128 x 27648 x 5120: 51.6, 64 x 128 tiles 57.3, with two stages
+  // 66.9; 512 x 5120 x 5120: 48.5, 47.4 and 59.7; 200 x 11008 x 2048: 23.3, 22.7 and 27.5), 64 x 128 ones where a CU has two of
+  // those (320 x 11008 x 5120: 49.2, 128 x 128 tiles 70.3).
   if (M > 64 && wide > 256 && t128 <= 256) return {kTile128Deep, 1};
   if (M > 64 && wide > 256 && wide <= 512) return {kTile64Wide, 1};
-  // 128 x 128 tiles, two workgroups a CU.
+  // 128 x 128 tiles, two workgroups a CU (4096 x 5120 x 5120: 193, 64 x 128 tiles 231; 1000 x 11008 x 2048: 55 and 61).
   if (M > 64 && wide > 512) return {kTile128, 1};
   const Path path = M > 32 ? kTile64 : kTile32;
-  // Few tiles under a long sum: as many parts as cost least, joined by a second launch.  A step costs 0.25 us, into fp32 0.41;
-  // the join 2.1, 0.3 more a part and what the parts' bytes take (64 x 2048 x 11008: 26 whole, 13.8 in 8 parts, 17.5 in 16; 256
-  // x 1024 x 4096: 12.5, 11.4 in 4, 14.2 in 8; 128 x 2048 x 2048: 8.4 whole, 9.9 in 2).  And half of the 3 that a launch
+  // Few tiles under a long sum: as many parts as cost least, joined by a second launch.  A step costs 0.48 us;
+  // the join 2.1, 0.3 more a part and what the parts' bytes take (64 x 2048 x 11008: 41 whole, 15.7 in 8 parts, 19.5 in 16; 256
+  // x 1024 x 4096: 17.7, 12.5 in 4, 15.1 in 8; 128 x 2048 x 2048: 10.8 whole, 10.9 in 2).  And half of the 3 that a launch
   // costs the host where it is not replayed from a graph.
   const int64_t t = path == kTile64 ? tiles(64, 64) : tiles(32, 64), steps = (K + kStep - 1) / kStep;
-  const double step = 0.33, bytes = 1.8e-6 * (double)M * (double)N;
+  const double step = 0.48, bytes = 1.8e-6 * (double)M * (double)N;
   Choice best = {path, 1};
   double least = step * (double)steps;
   for (int s = 2; s <= 16 && s * t <= 256; ++s) {
@@ -837,10 +843,10 @@ hipError_t launch_matmul_f8(const LinearF8Args& a, void* ws, hipStream_t st) {
 
 bool linear_f8_fused(int64_t M, int64_t N, int64_t K) {
   // Where quantizing over and over costs a workgroup less than a launch, or little more: one that is not replayed from a graph
-  // costs the host 3.  On the GPU, in us, fused and in two launches: 1 x 2560 x 2048 4.2 and 6.2; 1 x 11008 x 2048 6.9 and 10.6; 1 x
-  // 27648 x 5120 26.4 and 29.6; 1 x 5120 x 27648 33.6 and 37.2; 2 x 5120 x 5120 10.2 and 12.3; 4 x 5120 x 5120 12.3 and 12.6; 8 x
-  // 11008 x 2048 10.5 and 11.0; 16 x 2048 x 2560 7.6 and 7.0; 8 x 5120 x 5120 16.1 and 13.0; 16 x 11008 x 2048 18.2 and 11.5; 16 x
-  // 2048 x 4096 10.6 and 7.5.
+  // costs the host 3.  On the GPU, in us, fused and in two launches: 1 x 2560 x 2048 4.3 and 6.4; 1 x 11008 x 2048 8.8 and 12.2; 1 x
+  // 27648 x 5120 30.4 and 35.8; 1 x 5120 x 27648 35.2 and 46.1; 2 x 5120 x 5120 11.0 and 14.2; 4 x 5120 x 5120 13.1 and 14.3; 8 x
+  // 11008 x 2048 11.9 and 12.2; 16 x 2048 x 2560 7.9 and 7.2; 8 x 5120 x 5120 16.9 and 14.7; 16 x 11008 x 2048 16.7 and 12.3; 16 x
+  // 2048 x 4096 11.2 and 8.3.
   if (M == 1) return K <= 32768 && N <= (int64_t)1 << 26;  // (2^31 threads of a launch)
   return M <= 16 && N < 12288 && M * K <= (N <= 4096 ? 40960 : 20480);
 }
