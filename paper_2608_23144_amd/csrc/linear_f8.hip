@@ -360,7 +360,9 @@ __global__ __launch_bounds__((TileShape<BM, BN, WM, WN>::kThreads), OCC) void k_
 
   // neighbouring tiles on one XCD, in bands of 8 tile rows, share operands in its L2
   const int total = tiles_m * tiles_n;
-  const int id = (int)xcd_item(blockIdx.x, total);
+  const uint32_t wg = workgroup<S::kThreads>();
+  if (wg >= (uint32_t)total) return;
+  const int id = (int)xcd_item(wg, total);
   const int band = id / (8 * tiles_n), in = id - band * 8 * tiles_n;
   const int bm = tiles_m - band * 8 < 8 ? tiles_m - band * 8 : 8;
   const int64_t m0 = (int64_t)(band * 8 + in % bm) * BM, n0 = (int64_t)(in / bm) * BN;
@@ -380,7 +382,7 @@ __global__ __launch_bounds__((TileShape<BM, BN, WM, WN>::kThreads), OCC) void k_
   for (int i = 0; i < NB; ++i) rb[i] = bytes_from(a.B, n0 + i * kRows, a.N, a.ldb, K16);
 
   const int all = (K + kStep - 1) / kStep;
-  const int first = (int)blockIdx.y * split_steps;  // this workgroup's steps of the sum
+  const int first = (int)blockIdx.z * split_steps;  // this workgroup's steps of the sum
   const int steps = all - first < split_steps ? all - first : split_steps;
 
   const int oa = frow * (int)a.lda + pa, ob = frow * (int)a.ldb;
@@ -596,7 +598,7 @@ __global__ __launch_bounds__((TileShape<BM, BN, WM, WN>::kThreads), OCC) void k_
   // results: lane -> row wm + 16 j + r, columns wn + 4 TN g + 4 i + e
   const int64_t n = n0 + wn + 4 * TN * g;
   if (parts) {  // a part of the sum, for k_matmul_f8_join
-    float* o = parts + (int64_t)blockIdx.y * a.M * a.N;
+    float* o = parts + (int64_t)blockIdx.z * a.M * a.N;
 #pragma unroll
     for (int j = 0; j < TM; ++j) {
       const int64_t m = m0 + wm + 16 * j + r;
@@ -706,11 +708,13 @@ hipError_t launch_tile(const LinearF8Args& a, int split, void* ws, hipStream_t s
     if (e != hipSuccess) return e;
   }
   const int64_t tm = (a.M + BM - 1) / BM, tn = (a.N + BN - 1) / BN;
-  if (tm * tn > 0x7FFFFFFF / S::kThreads) return hipErrorInvalidValue;  // (threads of a launch: more than memory holds results for)
+  if (tm * tn > 0x7FFFFFFF) return hipErrorInvalidValue;  // (8 TB of results)
   const int all = (int)((a.K + kStep - 1) / kStep), per = (all + split - 1) / split;
   split = (all + per - 1) / per;
   float* parts = split > 1 ? static_cast<float*>(ws) : nullptr;
-  hipLaunchKernelGGL(k, dim3((unsigned)(tm * tn), (unsigned)split), dim3(S::kThreads), lds, st, a, (int)tm, (int)tn, per, parts);
+  dim3 grid = grid_of<S::kThreads>(tm * tn);
+  grid.z = (unsigned)split;
+  hipLaunchKernelGGL(k, grid, dim3(S::kThreads), lds, st, a, (int)tm, (int)tn, per, parts);
   if (parts) {
     const int64_t quads = a.M * ((a.N + 3) / 4);
     hipLaunchKernelGGL((k_matmul_f8_join<TO>), dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, st, a, parts, split);

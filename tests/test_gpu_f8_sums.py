@@ -76,3 +76,20 @@ def test_sums_of_random_codes(M, N, K, dtype):
     share = (most / step[fine]).clamp_max(1)
     expect = share.sum().item()
     assert (got != once)[fine].sum().item() <= expect + 6 * (expect ** 0.5 + 1)
+
+
+def test_more_columns_than_a_launch_has_threads_for():
+    """One row against 2^30 + 100 columns, in tiles of 64 columns and 128 threads: past 2^31 threads."""
+    g = torch.Generator(DEV)
+    g.manual_seed(1)
+    N, K = 2 ** 30 + 100, 16
+    w = torch.randint(0, 3, (N, K), generator=g, device=DEV, dtype=torch.uint8).mul_(24).view(F8)  # 0, 2^-4 or 0.5
+    sb = torch.exp2(torch.randint(0, 2, (-(-N // 128), 1), generator=g, device=DEV).float())
+    x = torch.randint(-3, 4, (1, K), generator=g, device=DEV).float()
+    a, sa = x.to(F8), torch.ones(1, 1, device=DEV)
+    out = awsrc.awsrc_matmul_f8(a, sa, w, sb)
+    for n in (0, 2 ** 26 - 64, 2 ** 29 + 1, 2 ** 30 - 2 ** 26, 2 ** 30 - 64, 2 ** 30 + 99):
+        m = min(N, n + 2 ** 24)
+        columns = torch.arange(n, m, device=DEV) // 128
+        want = (w[n:m].float() * x).sum(1) * sb[columns, 0]  # (multiples of 2^-4 below 2^6: exact)
+        assert torch.equal(out[0, n:m], want.bfloat16())
