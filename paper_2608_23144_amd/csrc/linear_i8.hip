@@ -304,7 +304,9 @@ __global__ __launch_bounds__((TileShape<BM, BN, WM, WN>::kThreads), OCC) void k_
 
   // neighbouring tiles on one XCD, in bands of 8 tile rows, share operands in its L2
   const int total = tiles_m * tiles_n;
-  const int id = (int)xcd_item(blockIdx.x, total);
+  const uint32_t wg = workgroup<S::kThreads>();
+  if (wg >= (uint32_t)total) return;
+  const int id = (int)xcd_item(wg, total);
   const int band = id / (8 * tiles_n), in = id - band * 8 * tiles_n;
   const int bm = tiles_m - band * 8 < 8 ? tiles_m - band * 8 : 8;
   const int64_t m0 = (int64_t)(band * 8 + in % bm) * BM, n0 = (int64_t)(in / bm) * BN;
@@ -328,7 +330,7 @@ __global__ __launch_bounds__((TileShape<BM, BN, WM, WN>::kThreads), OCC) void k_
   const uint32_t oa = (uint32_t)frow * (uint32_t)a.lda + pa, ob = (uint32_t)frow * (uint32_t)a.ldb;
   const uint32_t sa = kRows * (uint32_t)a.lda, sb = kRows * (uint32_t)a.ldb;
   typedef __attribute__((address_space(3))) void* lds_ptr;
-  const int first = (int)blockIdx.y * split_steps;  // this workgroup's steps of the sum
+  const int first = (int)blockIdx.z * split_steps;  // this workgroup's steps of the sum
   const int all = (K + kStep - 1) / kStep;
   const int steps = all - first < split_steps ? all - first : split_steps;
   auto fill = [&](int stage, int t) {
@@ -463,7 +465,7 @@ __global__ __launch_bounds__((TileShape<BM, BN, WM, WN>::kThreads), OCC) void k_
 
   // results: lane -> row wm + 32 j + r, columns wn + 32 i + 16 half + e
   if (parts) {  // a part of the sum, for k_matmul_i8_join
-    int32_t* o = parts + (int64_t)blockIdx.y * a.M * a.N;
+    int32_t* o = parts + (int64_t)blockIdx.z * a.M * a.N;
 #pragma unroll
     for (int i = 0; i < TN; ++i)
 #pragma unroll
@@ -600,11 +602,13 @@ hipError_t launch_tile(const LinearArgs& a, int split, void* ws, hipStream_t st)
     if (e != hipSuccess) return e;
   }
   const int64_t tm = (a.M + BM - 1) / BM, tn = (a.N + BN - 1) / BN;
-  if (tm * tn > 0x7FFFFFFF / S::kThreads) return hipErrorInvalidValue;  // (threads of a launch: more than memory holds results for)
+  if (tm * tn > 0x7FFFFFFF) return hipErrorInvalidValue;  // (8 TB of results)
   const int all = (int)((a.K + kStep - 1) / kStep), per = (all + split - 1) / split;
   split = (all + per - 1) / per;
   int32_t* parts = split > 1 ? static_cast<int32_t*>(ws) : nullptr;
-  hipLaunchKernelGGL(k, dim3((unsigned)(tm * tn), (unsigned)split), dim3(S::kThreads), lds, st, a, (int)tm, (int)tn, per, parts);
+  dim3 grid = grid_of<S::kThreads>(tm * tn);
+  grid.z = (unsigned)split;
+  hipLaunchKernelGGL(k, grid, dim3(S::kThreads), lds, st, a, (int)tm, (int)tn, per, parts);
   if (parts) {
     const int64_t quads = a.M * ((a.N + 3) / 4);
     hipLaunchKernelGGL((k_matmul_i8_join<TO>), dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, st, a, parts, split);
