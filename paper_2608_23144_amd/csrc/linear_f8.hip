@@ -724,6 +724,7 @@ hipError_t launch_tile(const LinearF8Args& a, int split, void* ws, hipStream_t s
 
 // Bytes between rows of codes in LDS: whole blocks, and 16 more so that rows start in different banks.
 int linear_rows_pitch(int64_t K) { return (int)((K + kBlockF8 - 1) / kBlockF8 * kBlockF8 + 16); }
+constexpr int kLinearRowsLds = 53248;  // at most, where linear_f8_fused() says so (16 x 2560: 42496, 2 x 20480: 51232)
 size_t linear_rows_lds(int64_t M, int64_t K) {
   return (size_t)M * linear_rows_pitch(K) + (size_t)((K + kBlockF8 - 1) / kBlockF8) * 64;
 }
@@ -744,8 +745,9 @@ template <int W, typename T, typename TO>
 hipError_t launch_linear_rows(const LinearF8Args& a, const void* X, int64_t ldx, hipStream_t st) {
   const auto k = weights_once(a.M, a.N, a.K) ? k_linear_f8_rows<W, true, T, TO> : k_linear_f8_rows<W, false, T, TO>;
   const size_t lds = linear_rows_lds(a.M, a.K);
-  if (lds > 32768) {  // (beside the sums of 16 wavefronts)
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+  if (lds > kLinearRowsLds) return hipErrorInvalidValue;
+  if (lds > 32768) {  // (beside the sums of 16 wavefronts; the same limit in every call: another thread's may come in between)
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, kLinearRowsLds);
     if (e != hipSuccess) return e;
   }
   hipLaunchKernelGGL(k, dim3((unsigned)((a.N + 15) / 16)), dim3(64 * W), lds, st, a, static_cast<const T*>(X), ldx, linear_rows_pitch(a.K));
