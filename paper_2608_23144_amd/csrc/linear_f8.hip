@@ -61,20 +61,6 @@ __device__ __forceinline__ fl4 sums_of(const Operand& w, const Operand& x) {
   return p;
 }
 
-template <typename TO>
-__device__ __forceinline__ void store4(TO* o, const float (&y)[4], int64_t n, int64_t N, bool wide) {
-  if (wide && n + 3 < N) {
-    struct alignas(4 * sizeof(TO)) V { TO v[4]; } w;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w.v[i] = (TO)y[i];
-    *reinterpret_cast<V*>(o + n) = w;
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (n + i < N) o[n + i] = (TO)y[i];
-  }
-}
-
 // Up to 16 rows (or 32: R groups of 16): the weights' bytes are all that counts.  A workgroup takes 16
 // weight rows (columns of the result) against all activation rows, its W
 // wavefronts sharing the sum; the weights come straight from memory, two blocks
@@ -107,29 +93,14 @@ struct Quads {
       v[u] = ONCE ? __builtin_nontemporal_load(w) : *w;
     }
   }
-  // lane j of a quad gets as v[i] what lane i of it loaded as v[j], then the groups trade
+  // the quads trade, then the groups
   __device__ __forceinline__ void turn(int lane, Operand& block0, Operand& block1) {
-    const bool odd = lane & 1, high = lane & 2;
+    turn_quads(v, lane);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      int x[4], y[4];
-#pragma unroll
-      for (int i = 0; i < 4; i += 2) {
-        const int p = __builtin_amdgcn_mov_dpp(v[i + 1][e], 0xB1, 0xF, 0xF, true);  // of lane ^ 1
-        const int q = __builtin_amdgcn_mov_dpp(v[i][e], 0xB1, 0xF, 0xF, true);
-        x[i] = odd ? p : v[i][e];
-        x[i + 1] = odd ? v[i + 1][e] : q;
-      }
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int p = __builtin_amdgcn_mov_dpp(x[i + 2], 0x4E, 0xF, 0xF, true);  // of lane ^ 2
-        const int q = __builtin_amdgcn_mov_dpp(x[i], 0x4E, 0xF, 0xF, true);
-        y[i] = high ? p : x[i];
-        y[i + 2] = high ? x[i + 2] : q;
-      }
 #pragma unroll
       for (int i = 0; i < 2; ++i) {  // odd groups' first half against even groups' second half
-        const auto t = __builtin_amdgcn_permlane16_swap((uint32_t)y[i], (uint32_t)y[i + 2], false, false);
+        const auto t = __builtin_amdgcn_permlane16_swap((uint32_t)v[i][e], (uint32_t)v[i + 2][e], false, false);
         v[i][e] = (int)t[0];
         v[i + 2][e] = (int)t[1];
       }
@@ -314,12 +285,6 @@ constexpr int kStep = kBlockF8;
 __device__ __forceinline__ int key_a(int row) { return (row >> 1) & 7; }
 template <int TN>
 __device__ __forceinline__ int key_b(int row) { return ((row >> 1) & 1) | ((row / (4 * TN)) & 3) << 1; }
-
-// A barrier for LDS contents alone: __syncthreads() would also wait for every
-// fill that is still to come.
-__device__ __forceinline__ void sync_lds() {
-  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-}
 
 // An operand from a row on: the bytes up to its last readable one, as a buffer resource takes them; none past its rows.
 struct Bytes {
@@ -736,7 +701,9 @@ bool weights_once(int64_t M, int64_t N, int64_t K) { return M <= 64 && N * K >= 
 
 template <int W, int R, typename TO>
 hipError_t launch_rows(const LinearF8Args& a, hipStream_t st) {
-  const auto k = weights_once(a.M, a.N, a.K) ? k_matmul_f8_rows<W, R, true, TO> : k_matmul_f8_rows<W, R, false, TO>;
+  auto k = k_matmul_f8_rows<W, R, false, TO>;
+  if constexpr (R == 1)  // (more rows take smaller weights only)
+    if (weights_once(a.M, a.N, a.K)) k = k_matmul_f8_rows<W, R, true, TO>;
   hipLaunchKernelGGL(k, dim3((unsigned)((a.N + 15) / 16)), dim3(64 * W), 0, st, a);
   return hipGetLastError();
 }

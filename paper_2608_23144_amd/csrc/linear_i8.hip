@@ -14,52 +14,10 @@ namespace awsrc {
 
 namespace {
 
-// The epilogue, the same in every kernel: two roundings after the sum's own.  The asm keeps the compiler from taking the fma
-// and the conversion to fp16 after it as one instruction, which does not round to fp32 in between: it did so in some of the
-// kernels, where one output in 60,000 had another last bit.
+// The epilogue, the same in every kernel: two roundings after the sum's own (one output in 60,000 had another last bit where
+// the conversion to fp16 was joined to the fma).
 __device__ __forceinline__ float scaled(int sum, float sa, float sb, float bias) {
-  float y = __builtin_fmaf((float)sum, sa * sb, bias);
-  asm("" : "+v"(y));
-  return y;
-}
-
-template <typename TO>
-__device__ __forceinline__ void store4(TO* o, const float (&y)[4], int64_t n, int64_t N, bool wide) {
-  if (wide && n + 3 < N) {
-    struct alignas(4 * sizeof(TO)) V { TO v[4]; } w;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w.v[i] = (TO)y[i];
-    *reinterpret_cast<V*>(o + n) = w;
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (n + i < N) o[n + i] = (TO)y[i];
-  }
-}
-
-// Lane j of a quad of neighbouring lanes gets as v[i] what lane i of it loaded as v[j].
-__device__ __forceinline__ void turn_quads(i32x4 (&v)[4], int lane) {
-  const bool odd = lane & 1, high = lane & 2;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    int x[4], y[4];
-#pragma unroll
-    for (int i = 0; i < 4; i += 2) {
-      const int p = __builtin_amdgcn_mov_dpp(v[i + 1][e], 0xB1, 0xF, 0xF, true);  // of lane ^ 1
-      const int q = __builtin_amdgcn_mov_dpp(v[i][e], 0xB1, 0xF, 0xF, true);
-      x[i] = odd ? p : v[i][e];
-      x[i + 1] = odd ? v[i + 1][e] : q;
-    }
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int p = __builtin_amdgcn_mov_dpp(x[i + 2], 0x4E, 0xF, 0xF, true);  // of lane ^ 2
-      const int q = __builtin_amdgcn_mov_dpp(x[i], 0x4E, 0xF, 0xF, true);
-      y[i] = high ? p : x[i];
-      y[i + 2] = high ? x[i + 2] : q;
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i][e] = y[i];
-  }
+  return rounded(__builtin_fmaf((float)sum, sa * sb, bias));
 }
 
 // Up to 16 rows (or 32: R groups of 16): the weights' bytes are all that counts.  A workgroup takes 16
@@ -276,12 +234,6 @@ constexpr int kStep = 128;
 
 __device__ __forceinline__ int key_a(int row) { return (row >> 1) & 7; }
 __device__ __forceinline__ int key_b(int row) { return ((row >> 1) & 3) | ((row >> 2) & 4); }
-
-// A barrier for LDS contents alone: __syncthreads() would also wait for every
-// fill that is still to come.
-__device__ __forceinline__ void sync_lds() {
-  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-}
 
 template <int BM, int BN, int WM, int WN>
 struct TileShape {

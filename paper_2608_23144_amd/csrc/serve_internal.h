@@ -136,6 +136,52 @@ __device__ __forceinline__ float rounded(float y) {
   return y;
 }
 
+// Four values of a result row, those of them that exist.
+template <typename TO>
+__device__ __forceinline__ void store4(TO* o, const float (&y)[4], int64_t n, int64_t N, bool wide) {
+  if (wide && n + 3 < N) {
+    struct alignas(4 * sizeof(TO)) V { TO v[4]; } w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w.v[i] = (TO)y[i];
+    *reinterpret_cast<V*>(o + n) = w;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (n + i < N) o[n + i] = (TO)y[i];
+  }
+}
+
+// Lane j of a quad of neighbouring lanes gets as v[i] what lane i of it loaded as v[j].
+__device__ __forceinline__ void turn_quads(i32x4 (&v)[4], int lane) {
+  const bool odd = lane & 1, high = lane & 2;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    int x[4], y[4];
+#pragma unroll
+    for (int i = 0; i < 4; i += 2) {
+      const int p = __builtin_amdgcn_mov_dpp(v[i + 1][e], 0xB1, 0xF, 0xF, true);  // of lane ^ 1
+      const int q = __builtin_amdgcn_mov_dpp(v[i][e], 0xB1, 0xF, 0xF, true);
+      x[i] = odd ? p : v[i][e];
+      x[i + 1] = odd ? v[i + 1][e] : q;
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int p = __builtin_amdgcn_mov_dpp(x[i + 2], 0x4E, 0xF, 0xF, true);  // of lane ^ 2
+      const int q = __builtin_amdgcn_mov_dpp(x[i], 0x4E, 0xF, 0xF, true);
+      y[i] = high ? p : x[i];
+      y[i + 2] = high ? x[i + 2] : q;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i][e] = y[i];
+  }
+}
+
+// A barrier for LDS contents alone: __syncthreads() would also wait for every
+// fill that is still to come.
+__device__ __forceinline__ void sync_lds() {
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
 // Columns of a block of e4m3 codes with one scale, and rows of a weight block.
 constexpr int kBlockF8 = 128;
 
@@ -199,27 +245,22 @@ __device__ __forceinline__ T of_lane(T x, int lane) {
   const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)b, lane), hi = __builtin_amdgcn_readlane((int)(uint32_t)(b >> 32), lane);
   return __builtin_bit_cast(T, (uint64_t)hi << 32 | lo);
 }
-// Inclusive sums of N values over the threads of a workgroup of W <= 16 wavefronts, in their order; `total` is everyone's.
+// Inclusive sums of N values over the threads of a workgroup of 4, 8 or 16 wavefronts (W), in their order; `total` is everyone's.
 // Every thread of the workgroup calls it; sums may be written again after the workgroup's next barrier.
 template <int W, int N, typename T>
 __device__ __forceinline__ void scan_workgroup(T (&x)[N], T (&total)[N], T (*sums)[W]) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll
   for (int i = 0; i < N; ++i) x[i] = scan_wave(x[i]);
-  if constexpr (W == 1) {
+  if (lane == 63)
 #pragma unroll
-    for (int i = 0; i < N; ++i) total[i] = of_lane(x[i], 63);
-  } else {
-    if (lane == 63)
+    for (int i = 0; i < N; ++i) sums[i][wave] = x[i];
+  __syncthreads();
 #pragma unroll
-      for (int i = 0; i < N; ++i) sums[i][wave] = x[i];
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const T upto = scan_row((lane & 15) < W ? sums[i][lane & 15 & (W - 1)] : T(0));
-      total[i] = of_lane(upto, W - 1);
-      if (wave) x[i] += of_lane(upto, wave - 1);
-    }
+  for (int i = 0; i < N; ++i) {
+    const T upto = scan_row((lane & 15) < W ? sums[i][lane & 15 & (W - 1)] : T(0));
+    total[i] = of_lane(upto, W - 1);
+    if (wave) x[i] += of_lane(upto, wave - 1);
   }
 }
 
