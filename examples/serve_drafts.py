@@ -94,7 +94,8 @@ def main(argv=None) -> dict:
     dev = "cuda"
     prompts = [int(n) for n in args.prompts.split(",")]
     slots, D = len(prompts), args.drafts
-    longest = max(prompts) + args.turns * (D + 1) + D + 1
+    later = prompts[-1] + 7  # tokens of the prompt that takes the first slot half way
+    longest = max(prompts + [later]) + args.turns * (D + 1) + D + 1
     weights = repaired_weights(args.seeds, dev)
     n_pages = slots * -(-longest // PAGE)
     model = Model(weights, slots, longest, n_pages, dev)
@@ -125,9 +126,9 @@ def main(argv=None) -> dict:
     out, accepted, offered = [], [], []
     for t in range(args.turns):
         if t == args.turns // 2 and slots > 1:  # the first sequence ends, another prompt takes its slot
-            texts[0], out = torch.randint(0, VOCAB, (prompts[-1] + 7,), generator=g, device=dev), out + [None]
+            texts[0], out = torch.randint(0, VOCAB, (later,), generator=g, device=dev), out + [None]
             keep = keep * (torch.arange(slots, device=dev) > 0)
-            last = prompt(keep, [prompts[-1] + 7] + [0] * (slots - 1), last)
+            last = prompt(keep, [later] + [0] * (slots - 1), last)
             keep = model.kv_len.clone()
         drafts, q = model.draft(last, D, g)
         cu, packed, logits = model.turn(keep, new, drafts, rows, D + 1)
