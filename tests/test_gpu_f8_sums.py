@@ -93,3 +93,24 @@ def test_more_columns_than_a_launch_has_threads_for():
         columns = torch.arange(n, m, device=DEV) // 128
         want = (w[n:m].float() * x).sum(1) * sb[columns, 0]  # (multiples of 2^-4 below 2^6: exact)
         assert torch.equal(out[0, n:m], want.bfloat16())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("M,N,K", [(1, 4091, 16411), (2, 4096, 16384), (1, 2101, 32767), (1, 9001, 8203), (1, 4097, 16400), (1, 70001, 1001),
+                                   (16, 13825, 4861), (64, 24600, 2750)])
+def test_linear_on_weights_past_the_caches(M, N, K, dtype):
+    """Layers whose weights are read once, quantized in the product's launch and in one of its own.  The sum of each block's 128
+    products is off by 127 steps of fp32 at most, the scales' product, each block's fma, up to 16 parts, the bias and the result's
+    rounding by half a step each."""
+    g = _gen("once", M, N, K)
+    x = (torch.randn(M, K, generator=g) * torch.exp(torch.randn(K, generator=g))).to(dtype).to(DEV)
+    w, sb = _codes(g, N, K), _scales(g, *_blocks(M, N, K)[1])
+    bias = torch.randn(N, generator=g).to(DEV)
+    codes, sa = awsrc.awsrc_quantize_blocks_f8(x)
+    a, b = _dense(codes, sa, 1), _dense(w, sb, 128)
+    want, mag = a @ b.T + bias.double(), a.abs() @ b.abs().T + bias.double().abs()
+    tol = mag * (127 * 2.0 ** -23 + (-(-K // 128) + 18) * 2.0 ** -24) + EPS[dtype] * want.abs() * (1 + 2.0 ** -10) + FLOOR[dtype]
+    got = awsrc.awsrc_linear_f8(x, w, sb, bias=bias).double()
+    sure = want.abs() + tol < torch.finfo(dtype).max
+    assert ((got - want).abs() <= tol)[sure].all()
+    assert sure.double().mean() > 0.9
