@@ -575,7 +575,7 @@ awsrc_status awsrc_dequantize_blocks_f8(const uint8_t* codes, int64_t ldc, const
  *  a_scale  [ceil(K / 128)][M] fp32;  b_scale  [ceil(N / 128)][ceil(K / 128)] fp32.
  *  bias_or_null  [N] fp32.
  *  out      [M, N], row m at out + m * ldo, ldo >= N, aligned to its type.
- * 1 <= K <= 2^22.  M or N of 0 is a no-op.
+ * 1 <= K <= 2^22.  M or N of 0 is a no-op.  out does not overlap what is read.
  * Workspace: two-phase query as described above (the query needs no pointers);
  * the size may be 0, and then no workspace is needed.
  */
@@ -711,7 +711,9 @@ typedef struct awsrc_page_pool {
  * if the new_len of it and all slots before it sum to at most max_rows, and if it takes
  * nothing or the pages that it and all slots before it take are at most those of the
  * pool and those that all slots give back.  A slot that is not served gets no rows and
- * keeps its first keep tokens, without the pages past them.
+ * keeps its first keep tokens, without the pages past them; what it asked for counts for the
+ * slots after it all the same.  One with want > table_ld, which the host can tell, is never
+ * served and may turn away all that follow: callers end it, or ask for less.
  * Pages given back, in order of slot and place, are taken first, then those of
  * the stack; those left over lie on the stack, the last in order lowest.
  *  kv_len_out  [n_seq] int32: keep + new_len (keep where a slot is not served); may be kv_len or keep.
