@@ -1104,8 +1104,8 @@ def awsrc_verify_drafts(p: torch.Tensor, tokens: torch.Tensor, u: torch.Tensor, 
     """Verifies a step's drafts: tokens [rows] packed by cu, each sequence's last certain token and then its drafts; p
     [rows, vocab] the target's probabilities of what follows each row, q those that the drafts were drawn from (None:
     drafts that were not drawn); u [rows] uniform random numbers in [0, 1).  Returns the tokens that follow (int32 [rows],
-    from each sequence's first row on, then -1), how many they are (int32 [sequences]), and, given kv_len, how many cached
-    tokens stay (awsrc_kv_plan's keep), else None."""
+    from each sequence's first row on, then -1; rows of no sequence stay as they were), how many they are (int32
+    [sequences]), and, given kv_len, how many cached tokens stay (awsrc_kv_plan's keep), else None."""
     rows, V, ldp = _rows_of(p, "p")
     dev = _device_of(p)
     dtype = p.dtype
